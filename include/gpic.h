@@ -434,6 +434,131 @@ gpic_status gpic_kmeans1d(const double *v, int64_t n, int32_t k,
  * compared with, timed on the same buffer.  Asynchronous. */
 gpic_status gpic_read_stream(const float *x, int64_t n, double *sink, void *stream);
 
+/* ------------------------------------------------ 7. layers of an encoder
+ *
+ * The points that are clustered are in practice what an encoder has made
+ * of raw data.  These calls are its layers, their gradients and the step
+ * that updates their weights: matrix products on the matrix cores with
+ * everything around them in their epilogues.
+ *
+ * Matrices are row-major with a pitch in elements; all matrices of a call
+ * have one type.  Sums are float32 or wider.  float32 matrices are
+ * multiplied as two half-precision parts (22 significant bits, one power of
+ * two per matrix from its largest finite magnitude, so entries down to 2^-17
+ * of it keep all 22).  A NaN or an infinity in a row of X (a column's
+ * weights) makes that row (column) of the result non-finite and no other.
+ * Results are bitwise reproducible.  Asynchronous. */
+
+/* Element types. */
+enum { GPIC_F32 = 0, GPIC_F16 = 1, GPIC_BF16 = 2 };
+
+/* Activations: z; max(z, 0); z Phi(z) with the normal distribution's Phi;
+ * z / (1 + exp(-z)).  Phi to 1e-7 absolute. */
+enum { GPIC_ACT_NONE = 0, GPIC_ACT_RELU = 1, GPIC_ACT_GELU = 2, GPIC_ACT_SILU = 3 };
+
+typedef struct gpic_layer_params {
+    int64_t n, k, m;     /* rows (0 .. 2^31 - 1), inputs, outputs (1 .. 2^20 each;
+                            gated: 2 m <= 2^20)                                   */
+    int64_t ldx, ldw;    /* pitches of X [n x k] and W [m x k] (gated [2 m x k])  */
+    int64_t ldy;         /* of Y, H [n x m] (backward: of dY, dH)                 */
+    int64_t ldr;         /* of the residual [n x m] (ignored without one)         */
+    int64_t ldz;         /* of Z [n x m] (gated [n x 2 m]; ignored without)       */
+    int32_t dtype;       /* GPIC_F32, GPIC_F16 or GPIC_BF16                       */
+    int32_t activation;  /* GPIC_ACT_*                                            */
+    int32_t aligned16;   /* 1: X, W and dY start on 16 bytes; with pitches and
+                            row lengths that are multiples of 8, 16-bit operands
+                            are then read as they lie, else copied to ws first    */
+    int32_t reserved;    /* must be 0                                             */
+} gpic_layer_params;     /* pitches at most 2^22 */
+
+/* Operation codes for gpic_layer_workspace_bytes. */
+enum {
+    GPIC_LAYER_FORWARD = 0,
+    GPIC_LAYER_BACKWARD = 1,
+    GPIC_GATED_FORWARD = 2,
+    GPIC_GATED_BACKWARD = 3
+};
+
+/* Workspace bytes of a call below with these parameters (0 also for
+ * parameters that the call refuses). */
+size_t gpic_layer_workspace_bytes(int32_t op, const gpic_layer_params *p);
+
+/* Y = act(X W^T + bias) + residual.  bias [m], residual and Z nullable; Z
+ * receives X W^T + bias, which the gradient needs.  Y may be the residual's
+ * own buffer (same pitch); no other overlap.  n = 0 does nothing.
+ * ws: gpic_layer_workspace_bytes(GPIC_LAYER_FORWARD, p).  Errors:
+ * INVALID_ARG, WORKSPACE. */
+gpic_status gpic_linear(const gpic_layer_params *p, const void *X, const void *W,
+                        const void *bias, const void *residual, void *Y, void *Z,
+                        void *ws, size_t ws_bytes, void *stream);
+
+/* Gradients of the same: dZ = dY * act'(Z) (act' of the rectifier is 0 at
+ * 0), dX [n x k] = dZ W, dW [m x k] = dZ^T X, db [m] = column sums of dZ;
+ * the residual's gradient is dY itself.  dX, dW and db are contiguous, any
+ * may be null (not wanted).  Z may be null without an activation.  dZ is
+ * rounded to the matrices' type for the products (db sums it unrounded).
+ * With n = 0, dW and db are zeros.
+ * ws: gpic_layer_workspace_bytes(GPIC_LAYER_BACKWARD, p). */
+gpic_status gpic_linear_backward(const gpic_layer_params *p, const void *dY, const void *X,
+                                 const void *W, const void *Z, void *dX, void *dW,
+                                 void *db, void *ws, size_t ws_bytes, void *stream);
+
+/* H = act(X Wg^T) * (X Wu^T), W = [Wg; Wu] (gate rows 0 .. m - 1, up rows m
+ * .. 2 m - 1); Z [n x 2 m] (nullable) receives X W^T, in float32 whatever
+ * the type: its gradient multiplies by Z itself, and a Z of 16 bits would
+ * add as much error as all other roundings (bfloat16, 8192 x 2048 -> 5504:
+ * dX and dW 3.0e-3 off in the 2-norm, against 2.3e-3).  The block's second
+ * product is gpic_linear with the residual.
+ * ws: gpic_layer_workspace_bytes(GPIC_GATED_FORWARD, p). */
+gpic_status gpic_gated(const gpic_layer_params *p, const void *X, const void *W, void *H,
+                       void *Z, void *ws, size_t ws_bytes, void *stream);
+
+/* Gradients of the same: dZg = dH * Zu * act'(Zg), dZu = dH * act(Zg), dX =
+ * dZ W, dW = dZ^T X.  As gpic_linear_backward.
+ * ws: gpic_layer_workspace_bytes(GPIC_GATED_BACKWARD, p). */
+gpic_status gpic_gated_backward(const gpic_layer_params *p, const void *dH, const void *X,
+                                const void *W, const void *Z, void *dX, void *dW, void *ws,
+                                size_t ws_bytes, void *stream);
+
+typedef struct gpic_polar_params {
+    int64_t batch, m, n; /* a stack of m x n matrices, contiguous (batch 0 ..
+                            65535; m, n 1 .. 2^20)                                */
+    int32_t dtype;       /* GPIC_F32, GPIC_F16 or GPIC_BF16                       */
+    int32_t steps;       /* 1 .. 64                                               */
+    float a, b, c;       /* the polynomial a x + b x^3 + c x^5; each at most 16 in
+                            magnitude.  It has to keep [0, 1] below 2 (as the
+                            usual 3.4445, -4.7750, 2.0315 and the quintic 15/8,
+                            -10/8, 3/8 do)                                        */
+    int32_t reserved;    /* must be 0                                             */
+    double eps;          /* >= 0; added to the Frobenius norm                     */
+} gpic_polar_params;
+
+size_t gpic_polar_workspace_bytes(const gpic_polar_params *p);
+
+/* O = the Newton-Schulz iterate of each matrix: X_0 = G / (|G|_F + eps),
+ * then `steps` times X <- a X + (b A + c A^2) X with A = X X^T (X^T X on the
+ * right for m > n): the singular vectors of G with its singular values
+ * taken near 1.  O may be G.  A zero matrix gives zeros (with eps > 0).
+ * float32 and float16 matrices in split halves; bfloat16 matrices with
+ * half-precision products, to about 2e-3 of |O|.
+ * ws: gpic_polar_workspace_bytes(p).  Asynchronous. */
+gpic_status gpic_orthogonalize(const gpic_polar_params *p, const void *G, void *O, void *ws,
+                               size_t ws_bytes, void *stream);
+
+typedef struct gpic_muon_params {
+    float lr, momentum, weight_decay;
+    float scale;         /* of the update; the usual one is sqrt(max(1, m / n))   */
+    int32_t nesterov;    /* 0 or 1                                                */
+    int32_t reserved;    /* must be 0                                             */
+} gpic_muon_params;
+
+/* One optimiser step, in place: M <- momentum M + G (M is float32 whatever
+ * the type of W and G), U = G + momentum M (nesterov) or M, W <- (1 - lr
+ * weight_decay) W - lr scale O(U), O as above.  W, G, M: stacks of m x n.
+ * ws: gpic_polar_workspace_bytes(p).  Asynchronous. */
+gpic_status gpic_muon_step(const gpic_polar_params *p, const gpic_muon_params *h, void *W,
+                           const void *G, float *M, void *ws, size_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -45,7 +45,13 @@ EXPORTS = (
     "gpic_sym_bytes", "gpic_affinity_sym", "gpic_matvec_sym", "gpic_power_iterate_sym",
     "gpic_power_iterate_dense_host", "gpic_read_stream",
     "gpic_power_iterate_dense_noalloc", "gpic_knn_graph_local",
+    "gpic_layer_workspace_bytes", "gpic_linear", "gpic_linear_backward", "gpic_gated",
+    "gpic_gated_backward", "gpic_polar_workspace_bytes", "gpic_orthogonalize",
+    "gpic_muon_step",
 )
+DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
+LAYER_OP = {"linear": 0, "linear_backward": 1, "gated": 2, "gated_backward": 3}
 
 # the static scratch of gpic_power_iterate_dense_noalloc (include/gpic.h)
 NOALLOC_SCRATCH_BYTES = 8 << 20
@@ -70,6 +76,24 @@ class PiResult(C.Structure):
                 ("last_stat", C.c_double)]
 
 
+class LayerParams(C.Structure):
+    _fields_ = [("n", C.c_int64), ("k", C.c_int64), ("m", C.c_int64), ("ldx", C.c_int64),
+                ("ldw", C.c_int64), ("ldy", C.c_int64), ("ldr", C.c_int64), ("ldz", C.c_int64),
+                ("dtype", C.c_int32), ("activation", C.c_int32), ("aligned16", C.c_int32),
+                ("reserved", C.c_int32)]
+
+
+class PolarParams(C.Structure):
+    _fields_ = [("batch", C.c_int64), ("m", C.c_int64), ("n", C.c_int64), ("dtype", C.c_int32),
+                ("steps", C.c_int32), ("a", C.c_float), ("b", C.c_float), ("c", C.c_float),
+                ("reserved", C.c_int32), ("eps", C.c_double)]
+
+
+class MuonParams(C.Structure):
+    _fields_ = [("lr", C.c_float), ("momentum", C.c_float), ("weight_decay", C.c_float),
+                ("scale", C.c_float), ("nesterov", C.c_int32), ("reserved", C.c_int32)]
+
+
 _lib = None
 
 
@@ -88,6 +112,10 @@ def lib() -> C.CDLL:
         L.gpic_last_error.restype = C.c_char_p
         L.gpic_workspace_bytes.restype = sz
         L.gpic_workspace_bytes.argtypes = [i32, i64, i64, i32]
+        L.gpic_layer_workspace_bytes.restype = sz
+        L.gpic_layer_workspace_bytes.argtypes = [i32, C.POINTER(LayerParams)]
+        L.gpic_polar_workspace_bytes.restype = sz
+        L.gpic_polar_workspace_bytes.argtypes = [C.POINTER(PolarParams)]
         L.gpic_sym_bytes.restype = sz
         L.gpic_sym_bytes.argtypes = [i64]
         sigs = {
@@ -121,6 +149,12 @@ def lib() -> C.CDLL:
             "gpic_kmeans1d": [p, i64, i32, p, p, C.POINTER(i32), C.POINTER(C.c_double),
                               p, sz, p],
             "gpic_read_stream": [p, i64, p, p],
+            "gpic_linear": [C.POINTER(LayerParams), p, p, p, p, p, p, p, sz, p],
+            "gpic_linear_backward": [C.POINTER(LayerParams), p, p, p, p, p, p, p, p, sz, p],
+            "gpic_gated": [C.POINTER(LayerParams), p, p, p, p, p, sz, p],
+            "gpic_gated_backward": [C.POINTER(LayerParams), p, p, p, p, p, p, p, sz, p],
+            "gpic_orthogonalize": [C.POINTER(PolarParams), p, p, p, sz, p],
+            "gpic_muon_step": [C.POINTER(PolarParams), C.POINTER(MuonParams), p, p, p, p, sz, p],
         }
         for name, args in sigs.items():
             fn = getattr(L, name)
@@ -165,7 +199,10 @@ def workspace_bytes(op: str, n: int, nnz: int = 0, k: int = 0) -> int:
 
 def workspace(op: str, n: int, nnz: int = 0, k: int = 0, device="cuda"):
     """A 256-byte aligned uint8 workspace tensor for `op` (plus its size)."""
-    nbytes = workspace_bytes(op, n, nnz, k)
+    return _workspace(workspace_bytes(op, n, nnz, k), device)
+
+
+def _workspace(nbytes: int, device):
     if nbytes == 0:
         return None, 0
     buf = torch.empty(nbytes + 256, dtype=torch.uint8, device=device)
@@ -598,6 +635,236 @@ def gpic_kmeans1d(v: torch.Tensor, k: int) -> KMOut:
     _check(lib().gpic_kmeans1d(_ptr(v), n, int(k), _ptr(labels), _ptr(cent),
                                C.byref(ke), C.byref(cost), _ptr(ws), nb, _stream(dev)))
     return KMOut(labels, cent[: ke.value], int(ke.value), float(cost.value))
+
+
+# ------------------------------------------------ 7. layers of an encoder
+@dataclasses.dataclass
+class LayerGrads:
+    dX: Optional[torch.Tensor]
+    dW: Optional[torch.Tensor]
+    db: Optional[torch.Tensor] = None
+
+
+def _matrix(t, shape, dtype, device, name):
+    """t as a 2-D tensor of that shape with unit column stride (copied only
+    when its columns are strided or its rows overlap)."""
+    _dev(t, dtype, name)
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not on {device}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {tuple(shape)}, got {tuple(t.shape)}")
+    rows, cols = shape
+    if (cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < cols):
+        t = t.contiguous()
+    return t
+
+
+def _pitch(t, cols):
+    return t.stride(0) if t is not None and t.shape[0] > 1 else cols
+
+
+def _layer_type(X):
+    if not isinstance(X, torch.Tensor) or not X.is_cuda:
+        raise TypeError("X must be a CUDA (HIP) tensor")
+    if X.dtype not in DTYPES:
+        raise TypeError(f"X must be float32, float16 or bfloat16, got {X.dtype}")
+    if X.dim() != 2:
+        raise ValueError("X must be [n, k]")
+
+
+def _activation(name):
+    if name not in ACTIVATIONS:
+        raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)}, got {name!r}")
+    return ACTIVATIONS[name]
+
+
+def _layer(op, X, W, Y, Z, residual, activation, gated):
+    """LayerParams for these tensors and a workspace for `op`."""
+    n, k = X.shape
+    m = W.shape[0] // 2 if gated else W.shape[0]
+    p = LayerParams(n=n, k=k, m=m, ldx=_pitch(X, k), ldw=_pitch(W, k), ldy=_pitch(Y, m),
+                    ldr=_pitch(residual, m), ldz=_pitch(Z, W.shape[0]), dtype=DTYPES[X.dtype],
+                    activation=_activation(activation), reserved=0)
+    p.aligned16 = int(all(t.data_ptr() % 16 == 0 for t in (X, W, Y)))
+    ws, nb = _workspace(int(lib().gpic_layer_workspace_bytes(LAYER_OP[op], C.byref(p))), X.device)
+    return p, ws, nb
+
+
+def _weights(X, W, gated):
+    if not isinstance(W, torch.Tensor) or W.dim() != 2:
+        raise ValueError("W must be [m, k]" if not gated else "W must be [2 m, k]")
+    if gated and W.shape[0] % 2:
+        raise ValueError("W must be [2 m, k]: an even number of rows")
+    return _matrix(W, (W.shape[0], X.shape[1]), X.dtype, X.device, "W")
+
+
+def _output(t, shape, X, name):
+    if t is None:
+        return torch.empty(shape, dtype=X.dtype, device=X.device)
+    if _matrix(t, shape, X.dtype, X.device, name) is not t:
+        raise ValueError(f"{name} must have unit column stride and rows that do not overlap")
+    return t
+
+
+def gpic_linear(X: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                activation: str = "none", residual: Optional[torch.Tensor] = None,
+                want_pre: bool = False, Y: Optional[torch.Tensor] = None):
+    """Y = act(X W^T + bias) + residual for X [n, k], W [m, k] (float32,
+    float16 or bfloat16, all the same); activation "none", "relu", "gelu" or
+    "silu".  want_pre: returns (Y, Z) with Z = X W^T + bias, which
+    gpic_linear_backward reads.  Y (optional) may be the residual itself."""
+    _layer_type(X)
+    X = _matrix(X, X.shape, X.dtype, X.device, "X")
+    W = _weights(X, W, False)
+    n, m = X.shape[0], W.shape[0]
+    if bias is not None:
+        _dev(bias, X.dtype, "bias")
+        if tuple(bias.shape) != (m,) or bias.device != X.device:
+            raise ValueError(f"bias must be [{m}] on {X.device}")
+        bias = bias.contiguous()
+    if residual is not None:
+        residual = _matrix(residual, (n, m), X.dtype, X.device, "residual")
+    Y = _output(Y, (n, m), X, "Y")
+    Z = torch.empty((n, m), dtype=X.dtype, device=X.device) if want_pre else None
+    p, ws, nb = _layer("linear", X, W, Y, Z, residual, activation, False)
+    _check(lib().gpic_linear(C.byref(p), _ptr(X), _ptr(W), _ptr(bias), _ptr(residual), _ptr(Y),
+                             _ptr(Z), _ptr(ws), nb, _stream(X.device)))
+    return (Y, Z) if want_pre else Y
+
+
+def gpic_linear_backward(dY: torch.Tensor, X: torch.Tensor, W: torch.Tensor,
+                         Z: Optional[torch.Tensor] = None, activation: str = "none",
+                         want_x: bool = True, want_w: bool = True,
+                         want_bias: bool = True) -> LayerGrads:
+    """Gradients of gpic_linear: dX, dW and db (those wanted).  Z as
+    gpic_linear gave it (not needed without an activation); the residual's
+    gradient is dY itself."""
+    _layer_type(X)
+    X = _matrix(X, X.shape, X.dtype, X.device, "X")
+    W = _weights(X, W, False)
+    n, m, dev = X.shape[0], W.shape[0], X.device
+    dY = _matrix(dY, (n, m), X.dtype, dev, "dY")
+    if _activation(activation) == 0:
+        Z = None
+    elif Z is None:
+        raise ValueError(f"the gradient of {activation!r} needs Z")
+    else:
+        Z = _matrix(Z, (n, m), X.dtype, dev, "Z")
+    dX = torch.empty(X.shape, dtype=X.dtype, device=dev) if want_x else None
+    dW = torch.empty(W.shape, dtype=X.dtype, device=dev) if want_w else None
+    db = torch.empty(m, dtype=X.dtype, device=dev) if want_bias else None
+    p, ws, nb = _layer("linear_backward", X, W, dY, Z, None, activation, False)
+    _check(lib().gpic_linear_backward(C.byref(p), _ptr(dY), _ptr(X), _ptr(W), _ptr(Z), _ptr(dX),
+                                      _ptr(dW), _ptr(db), _ptr(ws), nb, _stream(dev)))
+    return LayerGrads(dX, dW, db)
+
+
+def gpic_gated(X: torch.Tensor, W: torch.Tensor, activation: str = "silu",
+               want_pre: bool = False, H: Optional[torch.Tensor] = None):
+    """H = act(X Wg^T) * (X Wu^T) for W = [Wg; Wu] [2 m, k].  want_pre:
+    returns (H, Z) with Z = X W^T [n, 2 m] (float32 whatever the type), which
+    gpic_gated_backward reads."""
+    _layer_type(X)
+    X = _matrix(X, X.shape, X.dtype, X.device, "X")
+    W = _weights(X, W, True)
+    n, m = X.shape[0], W.shape[0] // 2
+    H = _output(H, (n, m), X, "H")
+    Z = torch.empty((n, 2 * m), dtype=torch.float32, device=X.device) if want_pre else None
+    p, ws, nb = _layer("gated", X, W, H, Z, None, activation, True)
+    _check(lib().gpic_gated(C.byref(p), _ptr(X), _ptr(W), _ptr(H), _ptr(Z), _ptr(ws), nb,
+                            _stream(X.device)))
+    return (H, Z) if want_pre else H
+
+
+def gpic_gated_backward(dH: torch.Tensor, X: torch.Tensor, W: torch.Tensor, Z: torch.Tensor,
+                        activation: str = "silu", want_x: bool = True,
+                        want_w: bool = True) -> LayerGrads:
+    """Gradients of gpic_gated: dX and dW (those wanted)."""
+    _layer_type(X)
+    X = _matrix(X, X.shape, X.dtype, X.device, "X")
+    W = _weights(X, W, True)
+    n, m, dev = X.shape[0], W.shape[0] // 2, X.device
+    dH = _matrix(dH, (n, m), X.dtype, dev, "dH")
+    Z = _matrix(Z, (n, 2 * m), torch.float32, dev, "Z")
+    dX = torch.empty(X.shape, dtype=X.dtype, device=dev) if want_x else None
+    dW = torch.empty(W.shape, dtype=X.dtype, device=dev) if want_w else None
+    p, ws, nb = _layer("gated_backward", X, W, dH, Z, None, activation, True)
+    _check(lib().gpic_gated_backward(C.byref(p), _ptr(dH), _ptr(X), _ptr(W), _ptr(Z), _ptr(dX),
+                                     _ptr(dW), _ptr(ws), nb, _stream(dev)))
+    return LayerGrads(dX, dW)
+
+
+# the quintic in common use for orthogonalised updates
+POLAR_COEFFICIENTS = (3.4445, -4.7750, 2.0315)
+
+
+def _stack(t, dtype, name):
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA (HIP) tensor")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.dim() not in (2, 3):
+        raise ValueError(f"{name} must be [m, n] or a stack [b, m, n]")
+
+
+def _polar(G, steps, coefficients, eps):
+    if G.dtype not in DTYPES:
+        raise TypeError(f"G must be float32, float16 or bfloat16, got {G.dtype}")
+    b = G.shape[0] if G.dim() == 3 else 1
+    a0, b0, c0 = (float(x) for x in coefficients)
+    p = PolarParams(batch=b, m=G.shape[-2], n=G.shape[-1], dtype=DTYPES[G.dtype],
+                    steps=int(steps), a=a0, b=b0, c=c0, reserved=0, eps=float(eps))
+    ws, nb = _workspace(int(lib().gpic_polar_workspace_bytes(C.byref(p))), G.device)
+    return p, ws, nb
+
+
+def gpic_orthogonalize(G: torch.Tensor, steps: int = 5, coefficients=POLAR_COEFFICIENTS,
+                       eps: float = 1e-7, O: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The Newton-Schulz iterate of G / (|G|_F + eps) after `steps` products
+    with a + b A + c A^2 (A the Gram matrix of the smaller side): G's
+    singular vectors with its singular values taken near 1.  G [m, n] or a
+    stack [b, m, n]; O (optional, contiguous) may be G."""
+    _stack(G, None, "G")
+    out = O
+    if out is None:
+        out = torch.empty(G.shape, dtype=G.dtype, device=G.device)
+    else:
+        _stack(out, G.dtype, "O")
+        if out.shape != G.shape or out.device != G.device or not out.is_contiguous():
+            raise ValueError("O must be contiguous, of G's shape and on its device")
+    G = G.contiguous()
+    p, ws, nb = _polar(G, steps, coefficients, eps)
+    _check(lib().gpic_orthogonalize(C.byref(p), _ptr(G), _ptr(out), _ptr(ws), nb,
+                                    _stream(G.device)))
+    return out
+
+
+def gpic_muon_step(W: torch.Tensor, G: torch.Tensor, M: torch.Tensor, lr: float,
+                   momentum: float = 0.95, nesterov: bool = True, weight_decay: float = 0.0,
+                   scale: Optional[float] = None, steps: int = 5,
+                   coefficients=POLAR_COEFFICIENTS, eps: float = 1e-7) -> None:
+    """One optimiser step in place: M <- momentum M + G, U = G + momentum M
+    (nesterov) or M, W <- (1 - lr weight_decay) W - lr scale O(U) with O as
+    gpic_orthogonalize.  W and G of one type, M float32; [m, n] or stacks.
+    scale: by default sqrt(max(1, m / n))."""
+    _stack(W, None, "W")
+    _stack(G, W.dtype, "G")
+    _stack(M, torch.float32, "M")
+    if G.shape != W.shape or M.shape != W.shape:
+        raise ValueError("W, G and M must have one shape")
+    if G.device != W.device or M.device != W.device:
+        raise ValueError("W, G and M must be on one device")
+    if not W.is_contiguous() or not M.is_contiguous():
+        raise ValueError("W and M are updated in place and must be contiguous")
+    G = G.contiguous()
+    m, n = W.shape[-2:]
+    if scale is None:
+        scale = max(1.0, m / max(n, 1)) ** 0.5
+    p, ws, nb = _polar(W, steps, coefficients, eps)
+    h = MuonParams(lr=float(lr), momentum=float(momentum), weight_decay=float(weight_decay),
+                   scale=float(scale), nesterov=int(bool(nesterov)), reserved=0)
+    _check(lib().gpic_muon_step(C.byref(p), C.byref(h), _ptr(W), _ptr(G), _ptr(M), _ptr(ws), nb,
+                                _stream(W.device)))
 
 
 # ----------------------------------------------- whole paths (call chains)

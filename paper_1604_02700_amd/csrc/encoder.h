@@ -1,0 +1,246 @@
+// Internal declarations of the encoder operators (layers, their gradients,
+// the orthogonalised update): operand and epilogue descriptions of the
+// tiled matrix product, activations, and the host launchers.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/gpic.h"
+
+namespace gpic {
+
+using half8 = _Float16 __attribute__((ext_vector_type(8)));
+using bfrag8 = __bf16 __attribute__((ext_vector_type(8)));
+using half4 = _Float16 __attribute__((ext_vector_type(4)));
+using bf4 = __bf16 __attribute__((ext_vector_type(4)));
+using f32x4 = float __attribute__((ext_vector_type(4)));
+using u32x4 = unsigned int __attribute__((ext_vector_type(4)));
+using s16x4 = short __attribute__((ext_vector_type(4)));
+
+// ------------------------------------------------------------ activations
+// Phi(z) and phi(z) of the normal distribution.  erfc(x) for x = |z| /
+// sqrt(2) by Abramowitz and Stegun 7.1.26 (t = 1 / (1 + p x), a quintic in t
+// times exp(-x^2); absolute error 1.5e-7, half of that in Phi, about a
+// float32 rounding of Phi near 1), taken on the side where nothing cancels:
+// one exponential, one reciprocal and seven multiply-adds, where the
+// library's erff costs about forty instructions and would take a quarter
+// of the time of a large layer's product.
+__device__ __forceinline__ void normal_cdf_pdf(float z, float &cdf, float &pdf)
+{
+    const float e = __builtin_amdgcn_exp2f(z * z * -0.72134752044448170f);
+    const float t = __builtin_amdgcn_rcpf(1.0f + 0.23164189f * fabsf(z));
+    float q = 0.53070271f;                      // half of the table's a_5 .. a_1
+    q = q * t - 0.72657601f;
+    q = q * t + 0.71070687f;
+    q = q * t - 0.14224837f;
+    q = q * t + 0.12741480f;
+    const float tail = q * t * e;               // Phi(-|z|)
+    cdf = z > 0.0f ? 1.0f - tail : tail;
+    pdf = 0.39894228040143268f * e;
+}
+
+__device__ __forceinline__ float sigmoidf(float z)
+{
+    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.4426950408889634f));
+}
+
+// act(z).  Infinities go where the function's limit is (silu and gelu of
+// -inf are 0), NaN stays NaN.
+__device__ __forceinline__ float activate(float z, int act)
+{
+    if (act == GPIC_ACT_RELU)
+        return z > 0.0f || z != z ? z : 0.0f;
+    if (act == GPIC_ACT_GELU) {
+        float c, p;
+        normal_cdf_pdf(z, c, p);
+        return z < -14.0f ? 0.0f : z * c;
+    }
+    if (act == GPIC_ACT_SILU)
+        return z < -104.0f ? 0.0f : z * sigmoidf(z);
+    return z;
+}
+
+// act(z) and act'(z); act' is 0 at z = 0 for the rectifier
+__device__ __forceinline__ void activate_grad(float z, int act, float &a, float &da)
+{
+    a = z;
+    da = 1.0f;
+    if (act == GPIC_ACT_RELU) {
+        a = z > 0.0f || z != z ? z : 0.0f;
+        da = z > 0.0f ? 1.0f : (z != z ? z : 0.0f);
+    } else if (act == GPIC_ACT_GELU) {
+        float c, p;
+        normal_cdf_pdf(z, c, p);
+        a = z < -14.0f ? 0.0f : z * c;
+        da = fabsf(z) > 14.0f ? c : c + z * p;
+    } else if (act == GPIC_ACT_SILU) {
+        const float s = sigmoidf(z);
+        a = z < -104.0f ? 0.0f : z * s;
+        da = fabsf(z) > 104.0f ? s : s * (1.0f + z * (1.0f - s));
+    }
+}
+
+// ------------------------------------------------- typed loads and stores
+__device__ __forceinline__ float load1(const void *p, int64_t i, int dtype)
+{
+    if (dtype == GPIC_F32)
+        return static_cast<const float *>(p)[i];
+    if (dtype == GPIC_F16)
+        return (float)static_cast<const _Float16 *>(p)[i];
+    return (float)static_cast<const __bf16 *>(p)[i];
+}
+
+__device__ __forceinline__ void store1(void *p, int64_t i, float v, int dtype)
+{
+    if (dtype == GPIC_F32)
+        static_cast<float *>(p)[i] = v;
+    else if (dtype == GPIC_F16)
+        static_cast<_Float16 *>(p)[i] = (_Float16)v;
+    else
+        static_cast<__bf16 *>(p)[i] = (__bf16)v;
+}
+
+// four consecutive values, p + i aligned to four of them
+__device__ __forceinline__ f32x4 load4(const void *p, int64_t i, int dtype)
+{
+    if (dtype == GPIC_F32)
+        return *reinterpret_cast<const f32x4 *>(static_cast<const float *>(p) + i);
+    if (dtype == GPIC_F16)
+        return __builtin_convertvector(
+            *reinterpret_cast<const half4 *>(static_cast<const _Float16 *>(p) + i), f32x4);
+    return __builtin_convertvector(
+        *reinterpret_cast<const bf4 *>(static_cast<const __bf16 *>(p) + i), f32x4);
+}
+
+__device__ __forceinline__ void store4(void *p, int64_t i, f32x4 v, int dtype)
+{
+    if (dtype == GPIC_F32)
+        *reinterpret_cast<f32x4 *>(static_cast<float *>(p) + i) = v;
+    else if (dtype == GPIC_F16)
+        *reinterpret_cast<half4 *>(static_cast<_Float16 *>(p) + i) =
+            __builtin_convertvector(v, half4);
+    else
+        *reinterpret_cast<bf4 *>(static_cast<__bf16 *>(p) + i) =
+            __builtin_convertvector(v, bf4);
+}
+
+// ---------------------------------------------------------- split matrices
+// A float32 matrix as 16-bit parts: x = (hi + lo) / s, s a power of two,
+// hi = half(s x), lo = half(s x - hi), 22 significant bits together.  The
+// columns come in groups of 32, each as 32 hi and then 32 lo values, so a
+// matrix of c columns has rows of 2 * ceil(c / 32) * 32 halves (zeros
+// beyond c) and any 128-byte line holds both parts of its 32 values.
+__host__ __device__ __forceinline__ int64_t split_ld(int64_t cols)
+{
+    return (cols + 31) / 32 * 64;
+}
+__host__ __device__ __forceinline__ int64_t split_at(int64_t col)
+{
+    return (col >> 5) * 64 + (col & 31);
+}
+
+// -------------------------------------------------------- matrix product
+// out[M x N] = epilogue(sum_k A(i, k) B(j, k)) over 16-bit operands on the
+// matrix cores, float32 accumulation, an optional batch in the grid.
+// An operand is either k-contiguous (rows i, row pitch ld) or k-strided
+// (rows k, row pitch ld, i contiguous).  Rows are 16-byte aligned, ld % 8
+// == 0 and the contiguous extent % 8 == 0.
+struct Operand {
+    const void *p;
+    int64_t ld;        // row pitch in 16-bit values
+    int64_t batch;     // pitch between matrices of a batch, 16-bit values
+    int64_t cols;      // 16-bit values of a row that may be read
+};
+
+enum { kEpiLayer = 0, kEpiGated = 1, kEpiSym = 2, kEpiUpdate = 3 };
+
+struct Epilogue {
+    // operand scales: acc is divided by their product (device pointers to
+    // the scales, null = 1), then multiplied by alpha
+    const float *sa, *sb;
+    float alpha;
+    // kEpiLayer, kEpiGated: z = acc (+ bias); y = act(z) (+ residual)
+    const void *bias, *res;
+    void *out, *pre;
+    int64_t ldr, ldo, ldz;
+    int dtype, act;
+    int vec;           // four consecutive columns may be moved at once
+    int64_t half;      // gated: columns of one half
+    // kEpiSym: P = beta * C + gamma * acc over the upper triangle of tiles,
+    // mirrored, C and P symmetric r x r; kEpiUpdate: X' = beta * X + acc.
+    // 16-bit parts of C, P (X, X'): split matrices (lo = null), or a hi
+    // matrix and, where lo is given, a lo matrix of the same pitch.
+    float beta;
+    const void *c_hi, *c_lo;
+    void *p_hi, *p_lo;
+    int64_t ldp, batch_p;      // of C, P, X, X' (16-bit values)
+    float store_scale;         // P, X' are stored times this
+    float load_scale;          // C, X are multiplied by this when read
+    int is_split;
+    // kEpiUpdate's last product: out (dtype, ldo) = beta X + acc, or, with
+    // weights, out = decay * out - step * (beta X + acc)
+    int to_out, is_step;
+    float decay, step;
+    int64_t batch_o;
+};
+
+struct ProductArgs {
+    Operand A, B;
+    int M, N;          // output rows, columns
+    int64_t K;         // contraction length
+    int batch;
+    int splits;        // parts of the contraction (partial sums in part)
+    float *part;       // [splits][batch][M][N4], N4 = N rounded up to 4
+    Epilogue e;
+};
+
+enum { kOpF16 = 0, kOpBf16 = 1, kOpSplit = 2 };    // operand kinds
+enum { kKK = 0, kKM = 1, kMM = 2 };                // A, B k-contiguous (K) or k-strided (M)
+
+// The number of parts of the contraction launch_product would take, 1 =
+// none, and the bytes of partial sums that they need.
+int product_splits(int M, int N, int64_t K, int batch, int op, bool sym);
+size_t product_part_bytes(int M, int N, int batch, int splits);
+
+// One product (and the sum of its parts where splits > 1).
+hipError_t launch_product(int modes, int op, int epi, const ProductArgs &a, hipStream_t s);
+
+// instantiations, one translation unit per pair of operand orders
+hipError_t launch_product_kk(int op, int epi, const ProductArgs &a, hipStream_t s);
+hipError_t launch_product_km(int op, int epi, const ProductArgs &a, hipStream_t s);
+hipError_t launch_product_mm(int op, int epi, const ProductArgs &a, hipStream_t s);
+
+// ------------------------------------------------------------- layers.hip
+struct Shape {         // a layer: n rows, k inputs, m outputs
+    int64_t n, k, m;
+    int dtype, act;
+    int64_t ldx, ldw, ldr, ldy, ldz;
+    bool aligned16;    // every matrix starts on 16 bytes
+};
+size_t layer_ws(const Shape &s, bool gated, bool backward);
+hipError_t run_layer(const Shape &s, bool gated, const void *X, const void *W,
+                     const void *bias, const void *res, void *Y, void *Z, void *ws,
+                     hipStream_t st);
+hipError_t run_layer_backward(const Shape &s, bool gated, const void *dY, const void *X,
+                              const void *W, const void *Z, void *dX, void *dW, void *db,
+                              void *ws, hipStream_t st);
+
+// ------------------------------------------------------ orthogonalize.hip
+struct Polar {
+    int64_t batch, m, n;
+    int dtype, steps;
+    float a, b, c;
+    double eps;
+};
+// the optimiser step around it
+struct MuonStep {
+    float lr, momentum, decay, scale;
+    int nesterov;
+};
+size_t polar_ws(const Polar &p);
+hipError_t run_orthogonalize(const Polar &p, const void *G, void *O, void *ws, hipStream_t st);
+hipError_t run_muon(const Polar &p, const MuonStep &h, void *W, const void *G, float *M,
+                    void *ws, hipStream_t st);
+
+} // namespace gpic

@@ -1,0 +1,674 @@
+// Layers of an encoder and their gradients: Y = act(X W^T + b) + R, the
+// gated projection H = act(X Wg^T) * (X Wu^T), and the passes around their
+// matrix products (product.h): packing of operands that the product cannot
+// read as they lie, dZ = dY act'(Z), and the column sums of the bias.
+//
+// float32 operands are multiplied as split halves (encoder.h); each matrix
+// has one power of two as its scale, from its largest finite magnitude.
+#include "encoder.h"
+
+namespace gpic {
+
+namespace {
+
+constexpr int kMaxParts = 256;        // partial maxima per matrix
+constexpr int kSumRows = 64;          // rows of a partial column sum
+
+inline size_t up(size_t x) { return (x + 255) & ~(size_t)255; }
+__host__ __device__ inline int64_t up64(int64_t x) { return (x + 63) & ~(int64_t)63; }
+
+// Lays a workspace out; with a null base it only counts.
+struct Cursor {
+    char *base;
+    size_t at = 0;
+    void *take(size_t bytes)
+    {
+        void *p = base ? base + at : nullptr;
+        at += up(bytes);
+        return p;
+    }
+};
+
+// ---------------------------------------------------------------- maxima
+struct MaxJob {
+    const void *x;
+    int64_t rows, cols, ld;
+    int dtype;
+    float *part;           // [kMaxParts]
+};
+struct MaxJobs {
+    MaxJob j[3];
+};
+
+// Largest finite |x| of up to three matrices (grid.y), one partial a
+// workgroup.  Reads the matrices once.
+__global__ __launch_bounds__(256) void absmax_kernel(MaxJobs jobs)
+{
+    const MaxJob m = jobs.j[blockIdx.y];
+    const int64_t total = m.rows * m.cols, stride = (int64_t)gridDim.x * 256;
+    float best = 0.0f;
+    if (m.ld == m.cols && ((uintptr_t)m.x & 15) == 0) {
+        const int64_t quads = total / 4;
+        for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < quads; i += stride) {
+            const f32x4 v = load4(m.x, i * 4, m.dtype);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const float a = fabsf(v[c]);
+                best = a < INFINITY && a > best ? a : best;
+            }
+        }
+        for (int64_t i = quads * 4 + (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += stride) {
+            const float a = fabsf(load1(m.x, i, m.dtype));
+            best = a < INFINITY && a > best ? a : best;
+        }
+    } else {
+        for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += stride) {
+            const int64_t r = i / m.cols;
+            const float a = fabsf(load1(m.x, r * m.ld + (i - r * m.cols), m.dtype));
+            best = a < INFINITY && a > best ? a : best;
+        }
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1)
+        best = fmaxf(best, __shfl_xor(best, o, 64));
+    __shared__ float w[4];
+    if ((threadIdx.x & 63) == 0)
+        w[threadIdx.x >> 6] = best;
+    __syncthreads();
+    if (threadIdx.x == 0)
+        m.part[blockIdx.x] = fmaxf(fmaxf(w[0], w[1]), fmaxf(w[2], w[3]));
+}
+
+// The block's largest of the kMaxParts partial maxima (256 threads).
+__device__ __forceinline__ float join_max(const float *part)
+{
+    float best = part[threadIdx.x];
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1)
+        best = fmaxf(best, __shfl_xor(best, o, 64));
+    __shared__ float w[4];
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0)
+        w[threadIdx.x >> 6] = best;
+    __syncthreads();
+    return fmaxf(fmaxf(w[0], w[1]), fmaxf(w[2], w[3]));
+}
+
+// The power of two that brings `most` into [2^14, 2^15): half-precision
+// parts of the scaled values neither overflow nor, down to 2^-17 of the
+// largest, lose bits.
+__device__ __forceinline__ float scale_for(float most)
+{
+    if (!(most > 0.0f))
+        return 1.0f;
+    int e;
+    frexpf(most, &e);                 // most = f 2^e, f in [1/2, 1)
+    int p = 15 - e;
+    p = p > 120 ? 120 : (p < -120 ? -120 : p);
+    return ldexpf(1.0f, p);
+}
+
+__device__ __forceinline__ void split2(float x, _Float16 &hi, _Float16 &lo)
+{
+    hi = (_Float16)x;
+    const float r = x - (float)hi;
+    lo = fabsf((float)hi) < INFINITY ? (_Float16)r : (_Float16)0.0f;
+}
+
+// --------------------------------------------------------------- packing
+struct PackJob {
+    const void *x;
+    int64_t rows, cols, ld;
+    void *to;              // split matrix (float32) or rows of up64(cols)
+    const float *part;     // float32: the partial maxima
+    float *scale;          // float32: receives the scale
+};
+struct PackJobs {
+    PackJob j[3];
+};
+
+// Copies of operands in the form that the product reads (grid.y: which).
+// Eight columns a thread.  float32: split parts; 16 bits: zero-padded rows.
+template <bool SPLIT>
+__global__ __launch_bounds__(256) void pack_kernel(PackJobs jobs)
+{
+    const PackJob m = jobs.j[blockIdx.y];
+    float s = 1.0f;
+    if (SPLIT) {
+        s = scale_for(join_max(m.part));
+        if (blockIdx.x == 0 && threadIdx.x == 0)
+            *m.scale = s;
+    }
+    const int64_t width = SPLIT ? (m.cols + 31) / 32 * 32 : up64(m.cols);
+    const int64_t groups = width / 8, total = m.rows * groups;
+    const bool vec = SPLIT && (m.ld & 3) == 0 && ((uintptr_t)m.x & 15) == 0;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total;
+         i += (int64_t)gridDim.x * 256) {
+        const int64_t r = i / groups, c = (i - r * groups) * 8;
+        if (SPLIT) {
+            const float *x = static_cast<const float *>(m.x) + r * m.ld + c;
+            float v[8];
+            if (vec && c + 8 <= m.cols) {
+                const f32x4 a = reinterpret_cast<const f32x4 *>(x)[0];
+                const f32x4 b = reinterpret_cast<const f32x4 *>(x)[1];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    v[k] = a[k];
+                    v[4 + k] = b[k];
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    v[k] = c + k < m.cols ? x[k] : 0.0f;
+            }
+            half8 h, l;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                _Float16 a, b;
+                split2(v[k] * s, a, b);
+                h[k] = a;
+                l[k] = b;
+            }
+            _Float16 *to = static_cast<_Float16 *>(m.to) + r * 2 * width + split_at(c);
+            *reinterpret_cast<half8 *>(to) = h;
+            *reinterpret_cast<half8 *>(to + 32) = l;
+        } else {
+            const unsigned short *x = static_cast<const unsigned short *>(m.x) + r * m.ld + c;
+            union {
+                unsigned short h[8];
+                u32x4 v;
+            } u;
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                u.h[k] = c + k < m.cols ? x[k] : (unsigned short)0;
+            *reinterpret_cast<u32x4 *>(static_cast<unsigned short *>(m.to) + r * width + c) = u.v;
+        }
+    }
+}
+
+// ------------------------------------------------------- dZ, column sums
+struct GradArgs {
+    const void *dY, *Z;
+    int64_t ldy, ldz, n, m;
+    int dtype, ztype, act, gated;
+    void *dZ;              // null: only the column sums
+    int64_t ldd;           // row pitch of dZ in 16-bit values
+    int vec;               // four columns at once
+    float *sums;           // [ceil(n / 64)][m] partial column sums, or null
+    const float *max_dy, *max_z;     // partial maxima (Z: gated only)
+    float *scale;          // dZ is stored times this; null: 1
+};
+
+__device__ __forceinline__ f32x4 read4(const void *p, int64_t row_at, int64_t col, int64_t cols,
+                                       int dtype, bool vec)
+{
+    if (vec && col + 4 <= cols)
+        return load4(p, row_at + col, dtype);
+    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (col + j < cols)
+            v[j] = load1(p, row_at + col + j, dtype);
+    return v;
+}
+
+// four values of dZ from column col on (`end`: no column of this half lies
+// at or beyond it)
+__device__ __forceinline__ void write4(const GradArgs &a, int64_t row, int64_t col, int64_t end,
+                                       f32x4 v, float s)
+{
+    const bool split = a.dtype == GPIC_F32;
+    if (split) {
+        _Float16 *d = static_cast<_Float16 *>(a.dZ) + row * a.ldd;
+        half4 h, l;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            _Float16 x, y;
+            split2(v[j] * s, x, y);
+            h[j] = x;
+            l[j] = y;
+        }
+        if ((col & 3) == 0 && col + 4 <= end) {
+            *reinterpret_cast<half4 *>(d + split_at(col)) = h;
+            *reinterpret_cast<half4 *>(d + split_at(col) + 32) = l;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (col + j < end) {
+                    d[split_at(col + j)] = h[j];
+                    d[split_at(col + j) + 32] = l[j];
+                }
+        }
+        return;
+    }
+    if ((col & 3) == 0 && col + 4 <= end) {
+        store4(a.dZ, row * a.ldd + col, v * s, a.dtype);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (col + j < end)
+                store1(a.dZ, row * a.ldd + col + j, v[j] * s, a.dtype);
+    }
+}
+
+// dZ of 64 rows x 256 columns a workgroup (four rows at a time, four
+// columns a thread) and their column sums, in float32 in a fixed order.
+// Memory-bound: reads dY and Z, writes dZ once.
+__global__ __launch_bounds__(256) void grad_kernel(GradArgs a)
+{
+    float s = 1.0f;
+    if (a.scale) {
+        // |act'| <= 1.13, and the gated forms multiply by |Z| or |act(Z)| <= |Z|
+        float most = 1.25f * join_max(a.max_dy);
+        if (a.max_z)
+            most *= fmaxf(1.0f, join_max(a.max_z));
+        s = scale_for(most < INFINITY ? most : 3.0e38f);
+        if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0)
+            *a.scale = s;
+    }
+    const int64_t col = (int64_t)blockIdx.y * 256 + (threadIdx.x & 63) * 4;
+    const int64_t r0 = (int64_t)blockIdx.x * kSumRows;
+    const int64_t r1 = r0 + kSumRows < a.n ? r0 + kSumRows : a.n;
+    f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+    // the padding of dZ's rows (zeros): a layer's columns m .. end, the
+    // gated layer's 2 m .. end
+    const int64_t all = a.gated ? 2 * a.m : a.m;
+    const int64_t width = a.dtype == GPIC_F32 ? (all + 31) / 32 * 32 : up64(all);
+    const int64_t end = a.gated ? a.m : width;
+    for (int64_t r = r0 + (threadIdx.x >> 6); r < r1; r += 4) {
+        if (col < a.m) {
+            const f32x4 dy = read4(a.dY, r * a.ldy, col, a.m, a.dtype, a.vec);
+            f32x4 d = dy;
+            if (a.gated) {
+                const f32x4 g = read4(a.Z, r * a.ldz, col, a.m, a.ztype, a.vec);
+                const f32x4 u = read4(a.Z, r * a.ldz + a.m, col, a.m, a.ztype, a.vec);
+                f32x4 du;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float y, dy1;
+                    activate_grad(g[j], a.act, y, dy1);
+                    d[j] = dy[j] * u[j] * dy1;
+                    du[j] = dy[j] * y;
+                }
+                write4(a, r, col, a.m, d, s);
+                write4(a, r, a.m + col, 2 * a.m, du, s);
+            } else {
+                if (a.act != GPIC_ACT_NONE) {
+                    const f32x4 z = read4(a.Z, r * a.ldz, col, a.m, a.ztype, a.vec);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        float y, dy1;
+                        activate_grad(z[j], a.act, y, dy1);
+                        d[j] = dy[j] * dy1;
+                    }
+                    // beyond the last column z and dy are 0, and d too
+                }
+                if (a.dZ)
+                    write4(a, r, col, end, d, s);
+                sum += d;
+            }
+        } else if (a.dZ && !a.gated && col < end) {
+            write4(a, r, col, end, f32x4{0.0f, 0.0f, 0.0f, 0.0f}, s);
+        }
+        // the thread at the gate's last column also writes the padding
+        if (a.gated && col < a.m && col + 4 >= a.m)
+            for (int64_t c = all; c < width; ++c) {
+                if (a.dtype == GPIC_F32) {
+                    _Float16 *d = static_cast<_Float16 *>(a.dZ) + r * a.ldd + split_at(c);
+                    d[0] = d[32] = (_Float16)0.0f;
+                } else {
+                    store1(a.dZ, r * a.ldd + c, 0.0f, a.dtype);
+                }
+            }
+    }
+    if (a.sums == nullptr)
+        return;
+    __shared__ f32x4 part[256];
+    part[threadIdx.x] = sum;
+    __syncthreads();
+    if (threadIdx.x < 64) {
+        sum = ((part[threadIdx.x] + part[threadIdx.x + 64]) + part[threadIdx.x + 128]) +
+              part[threadIdx.x + 192];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (col + j < a.m)
+                a.sums[(int64_t)blockIdx.x * a.m + col + j] = sum[j];
+    }
+}
+
+// Column sums from the partial ones, in float64 in a fixed order: 64
+// columns a workgroup, four runs of parts.
+__global__ __launch_bounds__(256) void sum_parts_kernel(const float *sums, int64_t parts, int64_t m,
+                                                        void *db, int dtype)
+{
+    const int64_t col = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
+    const int w = threadIdx.x >> 6;
+    double t = 0.0;
+    if (col < m)
+        for (int64_t p = w; p < parts; p += 4)
+            t += (double)sums[p * m + col];
+    __shared__ double part[256];
+    part[threadIdx.x] = t;
+    __syncthreads();
+    if (w == 0 && col < m) {
+        t = ((part[threadIdx.x] + part[threadIdx.x + 64]) + part[threadIdx.x + 128]) +
+            part[threadIdx.x + 192];
+        store1(db, col, (float)t, dtype);
+    }
+}
+
+// ------------------------------------------------------------------- host
+unsigned blocks_for(int64_t items)
+{
+    const int64_t b = (items + 255) / 256;
+    return (unsigned)(b < 1 ? 1 : (b > 4096 ? 4096 : b));
+}
+
+// A matrix that a product reads: as it lies where it can, else a packed
+// copy in the workspace.
+struct Source {
+    const void *x;
+    int64_t rows, cols, ld;
+    bool pack;
+    void *to = nullptr;
+    float *part = nullptr, *scale = nullptr;
+    Operand operand(int dtype) const
+    {
+        if (!pack)
+            return Operand{x, ld, 0, cols};
+        const int64_t p = dtype == GPIC_F32 ? split_ld(cols) : up64(cols);
+        return Operand{to, p, 0, p};
+    }
+};
+
+// 16-bit matrices are read as they lie when rows start on 16 bytes and
+// hold whole chunks of 8 values; float32 ones are always split.  `vec16`:
+// every matrix starts on 16 bytes.
+bool must_pack(int dtype, int64_t cols, int64_t ld, bool aligned16)
+{
+    return dtype == GPIC_F32 || !aligned16 || cols % 8 || ld % 8;
+}
+
+void place(Source &s, int dtype, Cursor &c)
+{
+    if (!s.pack)
+        return;
+    const int64_t p = dtype == GPIC_F32 ? split_ld(s.cols) : up64(s.cols);
+    s.to = c.take((size_t)s.rows * p * 2);
+    if (dtype == GPIC_F32) {
+        s.part = static_cast<float *>(c.take(kMaxParts * 4));
+        s.scale = static_cast<float *>(c.take(4));
+    }
+}
+
+hipError_t launch_absmax(const MaxJob *jobs, int count, hipStream_t st)
+{
+    MaxJobs j{};
+    for (int i = 0; i < count; ++i)
+        j.j[i] = jobs[i];
+    absmax_kernel<<<dim3(kMaxParts, (unsigned)count), 256, 0, st>>>(j);
+    return hipGetLastError();
+}
+
+hipError_t launch_pack(const Source *const *list, int count, int dtype, hipStream_t st)
+{
+    PackJobs j{};
+    int used = 0;
+    int64_t most = 0;
+    for (int i = 0; i < count; ++i)
+        if (list[i]->pack && list[i]->rows > 0) {
+            const Source &s = *list[i];
+            j.j[used++] = PackJob{s.x, s.rows, s.cols, s.ld, s.to, s.part, s.scale};
+            const int64_t groups = s.rows * ((s.cols + 63) / 64 * 8);
+            most = groups > most ? groups : most;
+        }
+    if (used == 0)
+        return hipSuccess;
+    const dim3 grid(blocks_for(most), (unsigned)used);
+    if (dtype == GPIC_F32)
+        pack_kernel<true><<<grid, 256, 0, st>>>(j);
+    else
+        pack_kernel<false><<<grid, 256, 0, st>>>(j);
+    return hipGetLastError();
+}
+
+int kind_of(int dtype)
+{
+    return dtype == GPIC_F32 ? kOpSplit : (dtype == GPIC_F16 ? kOpF16 : kOpBf16);
+}
+
+bool quads(const void *p, int64_t ld, int dtype)
+{
+    const uintptr_t bytes = dtype == GPIC_F32 ? 16 : 8;
+    return p == nullptr || (ld % 4 == 0 && (uintptr_t)p % bytes == 0);
+}
+
+// What a forward call keeps in its workspace.
+struct Forward {
+    Source X, W;
+    int splits;
+    float *part;
+    Forward(const Shape &s, bool gated, const void *x, const void *w, Cursor &c)
+    {
+        const int64_t rows = gated ? 2 * s.m : s.m;
+        X = Source{x, s.n, s.k, s.ldx, must_pack(s.dtype, s.k, s.ldx, s.aligned16)};
+        W = Source{w, rows, s.k, s.ldw, must_pack(s.dtype, s.k, s.ldw, s.aligned16)};
+        place(X, s.dtype, c);
+        place(W, s.dtype, c);
+        splits = gated ? 1 : product_splits((int)s.n, (int)s.m, s.k, 1, kind_of(s.dtype), false);
+        part = static_cast<float *>(
+            c.take(product_part_bytes((int)s.n, (int)s.m, 1, splits)));
+    }
+};
+
+// What a backward call keeps in its workspace.
+struct Backward {
+    Source dZ, X, W;
+    bool form;             // dZ is formed by grad_kernel (else dY is read)
+    float *sums;
+    float *max_dy, *max_z, *scale;
+    int splits_x, splits_w;
+    float *part;
+    int64_t rows;
+    Backward(const Shape &s, bool gated, const void *dy, const void *x, const void *w, Cursor &c)
+    {
+        rows = gated ? 2 * s.m : s.m;
+        form = gated || s.act != GPIC_ACT_NONE || s.dtype == GPIC_F32;
+        dZ = Source{dy, s.n, rows, s.ldy,
+                    form || must_pack(s.dtype, rows, s.ldy, s.aligned16)};
+        X = Source{x, s.n, s.k, s.ldx, must_pack(s.dtype, s.k, s.ldx, s.aligned16)};
+        W = Source{w, rows, s.k, s.ldw, must_pack(s.dtype, s.k, s.ldw, s.aligned16)};
+        place(dZ, s.dtype, c);
+        place(X, s.dtype, c);
+        place(W, s.dtype, c);
+        // a dZ that is formed in half precision has a scale too: gradients
+        // times act' soon fall below 6e-5, where halves lose bits
+        if (form && s.dtype == GPIC_F16) {
+            dZ.part = static_cast<float *>(c.take(kMaxParts * 4));
+            dZ.scale = static_cast<float *>(c.take(4));
+        }
+        max_dy = dZ.part;
+        scale = dZ.scale;
+        max_z = scale && gated ? static_cast<float *>(c.take(kMaxParts * 4)) : nullptr;
+        sums = static_cast<float *>(
+            c.take((size_t)((s.n + kSumRows - 1) / kSumRows) * s.m * 4));
+        const int op = kind_of(s.dtype);
+        splits_x = product_splits((int)s.n, (int)s.k, rows, 1, op, false);
+        splits_w = product_splits((int)rows, (int)s.k, s.n, 1, op, false);
+        const size_t bx = product_part_bytes((int)s.n, (int)s.k, 1, splits_x);
+        const size_t bw = product_part_bytes((int)rows, (int)s.k, 1, splits_w);
+        part = static_cast<float *>(c.take(bx > bw ? bx : bw));
+    }
+};
+
+#define RUN(expr)                                                              \
+    do {                                                                       \
+        hipError_t e_ = (expr);                                                \
+        if (e_ != hipSuccess)                                                  \
+            return e_;                                                         \
+    } while (0)
+
+} // namespace
+
+size_t layer_ws(const Shape &s, bool gated, bool backward)
+{
+    Cursor c{nullptr};
+    if (backward)
+        Backward b(s, gated, nullptr, nullptr, nullptr, c);
+    else
+        Forward f(s, gated, nullptr, nullptr, c);
+    return c.at;
+}
+
+hipError_t run_layer(const Shape &s, bool gated, const void *X, const void *W, const void *bias,
+                     const void *res, void *Y, void *Z, void *ws, hipStream_t st)
+{
+    if (s.n == 0)
+        return hipSuccess;
+    Cursor c{static_cast<char *>(ws)};
+    Forward f(s, gated, X, W, c);
+    const Source *list[2] = {&f.X, &f.W};
+    if (s.dtype == GPIC_F32) {
+        const MaxJob jobs[2] = {
+            {X, f.X.rows, s.k, s.ldx, s.dtype, f.X.part},
+            {W, f.W.rows, s.k, s.ldw, s.dtype, f.W.part}};
+        RUN(launch_absmax(jobs, 2, st));
+    }
+    RUN(launch_pack(list, 2, s.dtype, st));
+    ProductArgs a{};
+    a.A = f.X.operand(s.dtype);
+    a.B = f.W.operand(s.dtype);
+    a.M = (int)s.n;
+    a.N = (int)f.W.rows;
+    a.K = s.k;
+    a.batch = 1;
+    a.splits = f.splits;
+    a.part = f.part;
+    Epilogue &e = a.e;
+    e.sa = f.X.scale;
+    e.sb = f.W.scale;
+    e.alpha = 1.0f;
+    e.bias = bias;
+    e.res = res;
+    e.out = Y;
+    e.pre = Z;
+    e.ldr = s.ldr;
+    e.ldo = s.ldy;
+    e.ldz = s.ldz;
+    e.dtype = s.dtype;
+    e.act = s.act;
+    e.half = s.m;
+    e.vec = quads(Y, s.ldy, s.dtype) && quads(Z, s.ldz, gated ? GPIC_F32 : s.dtype) &&
+            quads(res, s.ldr, s.dtype) &&
+            quads(bias, 4, s.dtype) && (!gated || s.m % 4 == 0);
+    return launch_product(kKK, kind_of(s.dtype), gated ? kEpiGated : kEpiLayer, a, st);
+}
+
+hipError_t run_layer_backward(const Shape &s, bool gated, const void *dY, const void *X,
+                              const void *W, const void *Z, void *dX, void *dW, void *db, void *ws,
+                              hipStream_t st)
+{
+    Cursor c{static_cast<char *>(ws)};
+    Backward b(s, gated, dY, X, W, c);
+    const int op = kind_of(s.dtype);
+    const int ztype = gated ? GPIC_F32 : s.dtype;
+    // operands: what the wanted gradients read
+    if (!dW)
+        b.X.pack = false;
+    if (!dX)
+        b.W.pack = false;
+    const bool need_dz = dX || dW;
+    if (b.scale) {
+        MaxJob jobs[3];
+        int count = 0;
+        if (need_dz)
+            jobs[count++] = {dY, s.n, s.m, s.ldy, s.dtype, b.max_dy};
+        if (dW && b.X.part)
+            jobs[count++] = {X, s.n, s.k, s.ldx, s.dtype, b.X.part};
+        if (dX && b.W.part)
+            jobs[count++] = {W, b.rows, s.k, s.ldw, s.dtype, b.W.part};
+        if (count)
+            RUN(launch_absmax(jobs, count, st));
+        if (b.max_z && need_dz) {
+            const MaxJob z = {Z, s.n, b.rows, s.ldz, ztype, b.max_z};
+            RUN(launch_absmax(&z, 1, st));
+        }
+    }
+    {
+        Source plain = b.dZ;
+        plain.pack = b.dZ.pack && !b.form && need_dz;
+        const Source *list[3] = {&b.X, &b.W, &plain};
+        RUN(launch_pack(list, 3, s.dtype, st));
+    }
+    if (s.n > 0 && ((b.form && need_dz) || db)) {
+        GradArgs g{};
+        g.dY = dY;
+        g.Z = Z;
+        g.ldy = s.ldy;
+        g.ldz = s.ldz;
+        g.n = s.n;
+        g.m = s.m;
+        g.dtype = s.dtype;
+        g.ztype = ztype;
+        g.act = s.act;
+        g.gated = gated;
+        g.dZ = b.form && need_dz ? b.dZ.to : nullptr;
+        g.ldd = s.dtype == GPIC_F32 ? split_ld(b.rows) : up64(b.rows);
+        g.vec = quads(dY, s.ldy, s.dtype) &&
+                (s.act == GPIC_ACT_NONE && !gated ? true : quads(Z, s.ldz, ztype)) &&
+                (!gated || s.m % 4 == 0);
+        g.sums = db ? b.sums : nullptr;
+        if (need_dz) {
+            g.max_dy = b.max_dy;
+            g.max_z = b.max_z;
+            g.scale = b.scale;
+        }
+        const int64_t width = gated ? s.m : up64(s.m);
+        grad_kernel<<<dim3((unsigned)((s.n + kSumRows - 1) / kSumRows),
+                           (unsigned)((width + 255) / 256)),
+                      256, 0, st>>>(g);
+        RUN(hipGetLastError());
+    }
+    if (db) {
+        sum_parts_kernel<<<(unsigned)((s.m + 63) / 64), 256, 0, st>>>(
+            b.sums, (s.n + kSumRows - 1) / kSumRows, s.m, db, s.dtype);
+        RUN(hipGetLastError());
+    }
+    ProductArgs a{};
+    a.batch = 1;
+    a.part = b.part;
+    a.e.alpha = 1.0f;
+    a.e.dtype = s.dtype;
+    a.e.act = GPIC_ACT_NONE;
+    a.e.ldo = s.k;
+    const Operand dz = b.dZ.operand(s.dtype);
+    if (dX) {
+        a.A = dz;
+        a.B = b.W.operand(s.dtype);
+        a.M = (int)s.n;
+        a.N = (int)s.k;
+        a.K = b.rows;
+        a.splits = b.splits_x;
+        a.e.sa = b.scale;
+        a.e.sb = b.W.scale;
+        a.e.out = dX;
+        a.e.vec = quads(dX, s.k, s.dtype);
+        RUN(launch_product(kKM, op, kEpiLayer, a, st));
+    }
+    if (dW) {
+        a.A = dz;
+        a.B = b.X.operand(s.dtype);
+        a.M = (int)b.rows;
+        a.N = (int)s.k;
+        a.K = s.n;
+        a.splits = b.splits_w;
+        a.e.sa = s.n > 0 ? b.scale : nullptr;      // no rows: dW = 0, no scales
+        a.e.sb = s.n > 0 ? b.X.scale : nullptr;
+        a.e.out = dW;
+        a.e.vec = quads(dW, s.k, s.dtype);
+        RUN(launch_product(kMM, op, kEpiLayer, a, st));
+    }
+    return hipSuccess;
+}
+
+} // namespace gpic

@@ -1,0 +1,30 @@
+// Matrix products with both operands k-contiguous (product.h): layers
+// forward, Gram matrices of wide matrices and the polynomial's square.
+#include "product.h"
+
+namespace gpic {
+
+hipError_t launch_product_kk(int op, int epi, const ProductArgs &a, hipStream_t s)
+{
+    if (epi == kEpiLayer) {
+        if (op == kOpBf16)
+            return launch_any_tile<false, false, kOpBf16, kEpiLayer>(a, s);
+        if (op == kOpF16)
+            return launch_any_tile<false, false, kOpF16, kEpiLayer>(a, s);
+        return launch_any_tile<false, false, kOpSplit, kEpiLayer>(a, s);
+    }
+    if (epi == kEpiGated) {
+        if (op == kOpBf16)
+            return launch_any_tile<false, false, kOpBf16, kEpiGated>(a, s);
+        if (op == kOpF16)
+            return launch_any_tile<false, false, kOpF16, kEpiGated>(a, s);
+        return launch_any_tile<false, false, kOpSplit, kEpiGated>(a, s);
+    }
+    if (epi == kEpiSym)
+        return op == kOpF16 ? launch_any_tile<false, false, kOpF16, kEpiSym>(a, s)
+                            : launch_any_tile<false, false, kOpSplit, kEpiSym>(a, s);
+    return op == kOpF16 ? launch_any_tile<false, false, kOpF16, kEpiUpdate>(a, s)
+                        : launch_any_tile<false, false, kOpSplit, kEpiUpdate>(a, s);
+}
+
+} // namespace gpic

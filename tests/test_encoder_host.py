@@ -1,0 +1,150 @@
+"""Host-side checks of the encoder operators' entry points (no GPU needed):
+arguments are refused before any launch, workspaces grow with the sizes, and
+the binding refuses tensors it cannot pass on."""
+import ctypes as C
+
+import pytest
+import torch
+
+
+@pytest.fixture(scope="module")
+def g():
+    import paper_1604_02700_amd as g
+    g.lib()
+    return g
+
+
+def _layer(g, **kw):
+    p = g.LayerParams(n=10, k=16, m=24, ldx=16, ldw=16, ldy=24, ldr=24, ldz=48, dtype=2,
+                      activation=2, aligned16=1, reserved=0)
+    for k, v in kw.items():
+        setattr(p, k, v)
+    return p
+
+
+BAD_LAYERS = [dict(n=-1), dict(n=2 ** 31), dict(k=0), dict(k=2 ** 20 + 1), dict(m=0),
+              dict(m=2 ** 20 + 1), dict(ldx=15), dict(ldw=15), dict(ldy=23), dict(ldx=2 ** 22 + 1),
+              dict(ldw=2 ** 22 + 1), dict(dtype=3), dict(dtype=-1), dict(activation=4),
+              dict(activation=-1), dict(aligned16=2), dict(reserved=1)]
+
+
+@pytest.mark.parametrize("kw", BAD_LAYERS, ids=str)
+def test_layer_parameters_are_refused(g, kw):
+    L, d = g.lib(), C.c_void_p(4096)            # never dereferenced
+    p = C.byref(_layer(g, **kw))
+    ws = (d, 1 << 40)
+    assert L.gpic_linear(p, d, d, d, d, d, d, *ws, None) == 1
+    assert L.gpic_linear_backward(p, d, d, d, d, d, d, d, *ws, None) == 1
+    assert L.gpic_gated(p, d, d, d, d, *ws, None) == 1
+    assert L.gpic_gated_backward(p, d, d, d, d, d, d, *ws, None) == 1
+    for op in range(4):
+        assert L.gpic_layer_workspace_bytes(op, p) == 0
+
+
+def test_layer_buffers_are_refused(g):
+    L, d, odd, a8 = g.lib(), C.c_void_p(4096), C.c_void_p(4097), C.c_void_p(4104)
+    ws = (d, 1 << 40)
+    p = C.byref(_layer(g))
+    assert L.gpic_linear(None, d, d, d, d, d, d, *ws, None) == 1
+    assert L.gpic_linear(p, None, d, None, None, d, None, *ws, None) == 1
+    assert L.gpic_linear(p, d, None, None, None, d, None, *ws, None) == 1
+    assert L.gpic_linear(p, d, d, None, None, None, None, *ws, None) == 1
+    assert L.gpic_linear(p, a8, d, None, None, d, None, *ws, None) == 1      # aligned16 promised
+    assert L.gpic_linear(p, d, d, odd, None, d, None, *ws, None) == 1
+    assert L.gpic_linear(p, d, d, None, odd, d, None, *ws, None) == 1
+    assert L.gpic_linear(p, d, d, None, None, d, odd, *ws, None) == 1
+    assert L.gpic_linear(C.byref(_layer(g, ldr=23)), d, d, None, d, d, None, *ws, None) == 1
+    assert L.gpic_linear(C.byref(_layer(g, ldz=23)), d, d, None, None, d, d, *ws, None) == 1
+    assert b"ldz" in L.gpic_last_error()
+    assert L.gpic_linear_backward(p, d, d, d, None, d, d, d, *ws, None) == 1   # gelu needs Z
+    assert L.gpic_linear_backward(p, None, d, d, d, d, d, d, *ws, None) == 1
+    assert L.gpic_linear_backward(p, d, None, d, d, d, d, d, *ws, None) == 1   # dW needs X
+    assert L.gpic_linear_backward(p, d, d, None, d, d, d, d, *ws, None) == 1   # dX needs W
+    assert L.gpic_gated(C.byref(_layer(g, ldz=47)), d, d, d, d, *ws, None) == 1
+    assert L.gpic_gated(C.byref(_layer(g, m=2 ** 19 + 1, ldy=2 ** 20)), d, d, d, d, *ws, None) == 1
+    assert L.gpic_gated_backward(p, d, d, d, None, d, d, *ws, None) == 1
+    # float32 needs its packed copies
+    f = _layer(g, dtype=0)
+    need = L.gpic_layer_workspace_bytes(0, C.byref(f))
+    assert need > 0
+    assert L.gpic_linear(C.byref(f), d, d, None, None, d, None, d, need - 1, None) == 2
+    assert L.gpic_linear(C.byref(f), d, d, None, None, d, None, None, 0, None) == 2
+    assert L.gpic_linear(C.byref(f), d, d, None, None, d, None, C.c_void_p(4112), need, None) == 1
+
+
+def test_gated_offsets_are_limited(g):
+    """One half of the gated weights must be reachable with 32-bit offsets."""
+    L, d = g.lib(), C.c_void_p(4096)
+    p = _layer(g, m=2 ** 19, ldy=2 ** 19, k=8192, ldx=8192, ldw=8192, ldz=2 ** 20)
+    assert L.gpic_gated(C.byref(p), d, d, d, d, d, 1 << 40, None) == 5
+
+
+def test_layer_workspaces(g):
+    L = g.lib()
+    for op in range(4):
+        for dt in range(3):
+            def size(n, **kw):
+                w = dict(ldx=16, ldw=16, ldy=24, ldz=48)
+                w.update(kw)
+                return L.gpic_layer_workspace_bytes(op, C.byref(_layer(g, n=n, dtype=dt, **w)))
+            if dt == 0 or op in (1, 3):
+                assert 0 < size(1000) < size(10 ** 6) and size(10 ** 6) >= 10 ** 6 * 2 * 16
+            else:
+                assert size(1000) == size(10 ** 6) == 0          # read as they lie
+            # operands that may start anywhere are copied
+            assert size(10 ** 6, aligned16=0) >= 10 ** 6 * 2 * 16
+    assert L.gpic_layer_workspace_bytes(4, C.byref(_layer(g))) == 0
+    assert L.gpic_layer_workspace_bytes(0, None) == 0
+
+
+def _polar(g, **kw):
+    p = g.PolarParams(batch=2, m=64, n=96, dtype=0, steps=5, a=3.4445, b=-4.775, c=2.0315,
+                      reserved=0, eps=1e-7)
+    for k, v in kw.items():
+        setattr(p, k, v)
+    return p
+
+
+@pytest.mark.parametrize("kw", [dict(batch=-1), dict(batch=65536), dict(m=0), dict(n=0),
+                                dict(m=2 ** 20 + 1), dict(n=2 ** 20 + 1), dict(dtype=3),
+                                dict(steps=0), dict(steps=65), dict(a=17.0), dict(b=float("nan")),
+                                dict(c=float("inf")), dict(eps=-1.0), dict(eps=float("nan")),
+                                dict(reserved=1)], ids=str)
+def test_polar_parameters_are_refused(g, kw):
+    L, d = g.lib(), C.c_void_p(4096)
+    p = C.byref(_polar(g, **kw))
+    h = g.MuonParams(lr=0.1, momentum=0.9, weight_decay=0.0, scale=1.0, nesterov=1, reserved=0)
+    assert L.gpic_orthogonalize(p, d, d, d, 1 << 40, None) == 1
+    assert L.gpic_muon_step(p, C.byref(h), d, d, d, d, 1 << 40, None) == 1
+    assert L.gpic_polar_workspace_bytes(p) == 0
+
+
+def test_polar_buffers_and_step_are_refused(g):
+    L, d, odd = g.lib(), C.c_void_p(4096), C.c_void_p(4098)
+    p = C.byref(_polar(g))
+    need = L.gpic_polar_workspace_bytes(p)
+    assert need >= 2 * 64 * 96 * 4 * 2
+    assert L.gpic_orthogonalize(p, None, d, d, need, None) == 1
+    assert L.gpic_orthogonalize(p, d, None, d, need, None) == 1
+    assert L.gpic_orthogonalize(p, odd, d, d, need, None) == 1
+    assert L.gpic_orthogonalize(p, d, d, d, need - 1, None) == 2
+    ok = dict(lr=0.1, momentum=0.9, weight_decay=0.0, scale=1.0, nesterov=1, reserved=0)
+    for bad in (dict(lr=float("nan")), dict(momentum=float("inf")), dict(weight_decay=float("nan")),
+                dict(scale=float("inf")), dict(nesterov=2), dict(reserved=1)):
+        h = g.MuonParams(**{**ok, **bad})
+        assert L.gpic_muon_step(p, C.byref(h), d, d, d, d, need, None) == 1
+    h = C.byref(g.MuonParams(**ok))
+    assert L.gpic_muon_step(p, None, d, d, d, d, need, None) == 1
+    assert L.gpic_muon_step(p, h, None, d, d, d, need, None) == 1
+    assert L.gpic_muon_step(p, h, d, d, odd, d, need, None) == 1
+    assert L.gpic_muon_step(p, h, d, d, d, d, 0, None) == 2
+
+
+def test_binding_refuses_host_tensors(g):
+    x = torch.zeros((4, 8))
+    for call in (lambda: g.gpic_linear(x, x), lambda: g.gpic_gated(x, x),
+                 lambda: g.gpic_linear_backward(x, x, x), lambda: g.gpic_orthogonalize(x),
+                 lambda: g.gpic_gated_backward(x, x, x, x),
+                 lambda: g.gpic_muon_step(x, x, x, 0.1)):
+        with pytest.raises(TypeError):
+            call()
