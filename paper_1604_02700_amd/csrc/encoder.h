@@ -15,6 +15,7 @@ using bfrag8 = __bf16 __attribute__((ext_vector_type(8)));
 using half4 = _Float16 __attribute__((ext_vector_type(4)));
 using bf4 = __bf16 __attribute__((ext_vector_type(4)));
 using f32x4 = float __attribute__((ext_vector_type(4)));
+using f32x8 = float __attribute__((ext_vector_type(8), aligned(16)));
 using u32x4 = unsigned int __attribute__((ext_vector_type(4)));
 using s16x4 = short __attribute__((ext_vector_type(4)));
 
@@ -190,26 +191,33 @@ struct ProductArgs {
     int M, N;          // output rows, columns
     int64_t K;         // contraction length
     int batch;
-    int splits;        // parts of the contraction (partial sums in part)
-    float *part;       // [splits][batch][M][N4], N4 = N rounded up to 4
+    float *part;       // the parts of split tiles: [splits][tail][tile]
+    int whole, splits; // set by the launch, from the plan
     Epilogue e;
 };
 
 enum { kOpF16 = 0, kOpBf16 = 1, kOpSplit = 2 };    // operand kinds
 enum { kKK = 0, kKM = 1, kMM = 2 };                // A, B k-contiguous (K) or k-strided (M)
 
-// The number of parts of the contraction launch_product would take, 1 =
-// none, and the bytes of partial sums that they need.
-int product_splits(int M, int N, int64_t K, int batch, int op, bool sym);
-size_t product_part_bytes(int M, int N, int batch, int splits);
+// How a product is cut: `whole` tiles over the full contraction, then
+// `tail` tiles in `splits` parts each, joined by a second launch.
+struct Plan {
+    int tile;          // 0: 256 x 256, 1: 128 x 128, 2: 64 x 64
+    int tm, tn;        // tiles down and across
+    int64_t whole, tail;
+    int splits;
+    size_t part_bytes;
+};
+// N: columns of the tiled product (gated: both halves)
+Plan product_plan(int64_t M, int64_t N, int64_t K, int64_t batch, int op, int epi);
 
-// One product (and the sum of its parts where splits > 1).
+// One product (and the join of its split tiles).
 hipError_t launch_product(int modes, int op, int epi, const ProductArgs &a, hipStream_t s);
 
 // instantiations, one translation unit per pair of operand orders
-hipError_t launch_product_kk(int op, int epi, const ProductArgs &a, hipStream_t s);
-hipError_t launch_product_km(int op, int epi, const ProductArgs &a, hipStream_t s);
-hipError_t launch_product_mm(int op, int epi, const ProductArgs &a, hipStream_t s);
+hipError_t launch_product_kk(int op, int epi, const Plan &p, const ProductArgs &a, hipStream_t s);
+hipError_t launch_product_km(int op, int epi, const Plan &p, const ProductArgs &a, hipStream_t s);
+hipError_t launch_product_mm(int op, int epi, const Plan &p, const ProductArgs &a, hipStream_t s);
 
 // ------------------------------------------------------------- layers.hip
 struct Shape {         // a layer: n rows, k inputs, m outputs

@@ -437,6 +437,12 @@ int kind_of(int dtype)
     return dtype == GPIC_F32 ? kOpSplit : (dtype == GPIC_F16 ? kOpF16 : kOpBf16);
 }
 
+// eight values at once (sixteen bytes of 16-bit values)
+bool eights(const void *p, int64_t ld, int dtype)
+{
+    return p == nullptr || (ld % (dtype == GPIC_F32 ? 4 : 8) == 0 && (uintptr_t)p % 16 == 0);
+}
+
 bool quads(const void *p, int64_t ld, int dtype)
 {
     const uintptr_t bytes = dtype == GPIC_F32 ? 16 : 8;
@@ -446,7 +452,6 @@ bool quads(const void *p, int64_t ld, int dtype)
 // What a forward call keeps in its workspace.
 struct Forward {
     Source X, W;
-    int splits;
     float *part;
     Forward(const Shape &s, bool gated, const void *x, const void *w, Cursor &c)
     {
@@ -455,9 +460,9 @@ struct Forward {
         W = Source{w, rows, s.k, s.ldw, must_pack(s.dtype, s.k, s.ldw, s.aligned16)};
         place(X, s.dtype, c);
         place(W, s.dtype, c);
-        splits = gated ? 1 : product_splits((int)s.n, (int)s.m, s.k, 1, kind_of(s.dtype), false);
-        part = static_cast<float *>(
-            c.take(product_part_bytes((int)s.n, (int)s.m, 1, splits)));
+        part = static_cast<float *>(c.take(
+            product_plan(s.n, rows, s.k, 1, kind_of(s.dtype), gated ? kEpiGated : kEpiLayer)
+                .part_bytes));
     }
 };
 
@@ -467,7 +472,6 @@ struct Backward {
     bool form;             // dZ is formed by grad_kernel (else dY is read)
     float *sums;
     float *max_dy, *max_z, *scale;
-    int splits_x, splits_w;
     float *part;
     int64_t rows;
     Backward(const Shape &s, bool gated, const void *dy, const void *x, const void *w, Cursor &c)
@@ -493,10 +497,8 @@ struct Backward {
         sums = static_cast<float *>(
             c.take((size_t)((s.n + kSumRows - 1) / kSumRows) * s.m * 4));
         const int op = kind_of(s.dtype);
-        splits_x = product_splits((int)s.n, (int)s.k, rows, 1, op, false);
-        splits_w = product_splits((int)rows, (int)s.k, s.n, 1, op, false);
-        const size_t bx = product_part_bytes((int)s.n, (int)s.k, 1, splits_x);
-        const size_t bw = product_part_bytes((int)rows, (int)s.k, 1, splits_w);
+        const size_t bx = product_plan(s.n, s.k, rows, 1, op, kEpiLayer).part_bytes;
+        const size_t bw = product_plan(rows, s.k, s.n, 1, op, kEpiLayer).part_bytes;
         part = static_cast<float *>(c.take(bx > bw ? bx : bw));
     }
 };
@@ -542,7 +544,6 @@ hipError_t run_layer(const Shape &s, bool gated, const void *X, const void *W, c
     a.N = (int)f.W.rows;
     a.K = s.k;
     a.batch = 1;
-    a.splits = f.splits;
     a.part = f.part;
     Epilogue &e = a.e;
     e.sa = f.X.scale;
@@ -558,9 +559,8 @@ hipError_t run_layer(const Shape &s, bool gated, const void *X, const void *W, c
     e.dtype = s.dtype;
     e.act = s.act;
     e.half = s.m;
-    e.vec = quads(Y, s.ldy, s.dtype) && quads(Z, s.ldz, gated ? GPIC_F32 : s.dtype) &&
-            quads(res, s.ldr, s.dtype) &&
-            quads(bias, 4, s.dtype) && (!gated || s.m % 4 == 0);
+    e.vec = eights(Y, s.ldy, s.dtype) && eights(Z, s.ldz, gated ? GPIC_F32 : s.dtype) &&
+            eights(res, s.ldr, s.dtype) && eights(bias, 8, s.dtype) && (!gated || s.m % 8 == 0);
     return launch_product(kKK, kind_of(s.dtype), gated ? kEpiGated : kEpiLayer, a, st);
 }
 
@@ -648,11 +648,10 @@ hipError_t run_layer_backward(const Shape &s, bool gated, const void *dY, const 
         a.M = (int)s.n;
         a.N = (int)s.k;
         a.K = b.rows;
-        a.splits = b.splits_x;
         a.e.sa = b.scale;
         a.e.sb = b.W.scale;
         a.e.out = dX;
-        a.e.vec = quads(dX, s.k, s.dtype);
+        a.e.vec = eights(dX, s.k, s.dtype);
         RUN(launch_product(kKM, op, kEpiLayer, a, st));
     }
     if (dW) {
@@ -661,11 +660,10 @@ hipError_t run_layer_backward(const Shape &s, bool gated, const void *dY, const 
         a.M = (int)b.rows;
         a.N = (int)s.k;
         a.K = s.n;
-        a.splits = b.splits_w;
         a.e.sa = s.n > 0 ? b.scale : nullptr;      // no rows: dW = 0, no scales
         a.e.sb = s.n > 0 ? b.X.scale : nullptr;
         a.e.out = dW;
-        a.e.vec = quads(dW, s.k, s.dtype);
+        a.e.vec = eights(dW, s.k, s.dtype);
         RUN(launch_product(kMM, op, kEpiLayer, a, st));
     }
     return hipSuccess;

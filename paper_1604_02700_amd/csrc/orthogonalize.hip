@@ -159,7 +159,6 @@ struct Layout {
     int64_t ldx, lds;      // pitches of X and of the r x r matrices
     Planes x[2], gram, poly;
     double *part;
-    int splits_gram, splits_poly, splits_up;
     float *sums;
     size_t bytes;
 
@@ -190,13 +189,11 @@ struct Layout {
             q->hi = reinterpret_cast<_Float16 *>(take((size_t)(p.batch * q->batch) * 2));
             q->lo = nullptr;
         }
-        const int op = split ? kOpSplit : kOpF16, b = (int)p.batch;
-        splits_gram = product_splits((int)r, (int)r, len, b, op, true);
-        splits_poly = product_splits((int)r, (int)r, r, b, op, true);
-        splits_up = product_splits((int)p.m, (int)p.n, r, b, op, false);
-        size_t most = product_part_bytes((int)r, (int)r, b, splits_gram);
-        const size_t s1 = product_part_bytes((int)r, (int)r, b, splits_poly);
-        const size_t s2 = product_part_bytes((int)p.m, (int)p.n, b, splits_up);
+        const int op = split ? kOpSplit : kOpF16;
+        const int64_t b = p.batch;
+        size_t most = product_plan(r, r, len, b, op, kEpiSym).part_bytes;
+        const size_t s1 = product_plan(r, r, r, b, op, kEpiSym).part_bytes;
+        const size_t s2 = product_plan(p.m, p.n, r, b, op, kEpiUpdate).part_bytes;
         most = s1 > most ? s1 : most;
         most = s2 > most ? s2 : most;
         sums = reinterpret_cast<float *>(take(most));
@@ -245,7 +242,6 @@ hipError_t iterate(const Polar &p, const Input &in, void *out, const MuonStep *h
         a.A = a.B = operand(x);
         a.M = a.N = (int)L.r;
         a.K = L.len;
-        a.splits = L.splits_gram;
         a.e.alpha = inv2;
         a.e.p_hi = L.gram.hi;
         a.e.ldp = L.lds;
@@ -254,7 +250,6 @@ hipError_t iterate(const Polar &p, const Input &in, void *out, const MuonStep *h
         // P = b A + c A A
         a.A = a.B = operand(L.gram);
         a.K = L.r;
-        a.splits = L.splits_poly;
         a.e.alpha = p.c * inv2;
         a.e.beta = p.b;
         a.e.c_hi = L.gram.hi;
@@ -265,7 +260,6 @@ hipError_t iterate(const Polar &p, const Input &in, void *out, const MuonStep *h
         a.B = operand(L.tall ? L.poly : x);
         a.M = (int)p.m;
         a.N = (int)p.n;
-        a.splits = L.splits_up;
         a.e.alpha = inv2;
         a.e.beta = p.a;
         a.e.c_hi = x.hi;
@@ -280,7 +274,7 @@ hipError_t iterate(const Polar &p, const Input &in, void *out, const MuonStep *h
             a.e.dtype = p.dtype;
             a.e.ldo = p.n;
             a.e.batch_o = size;
-            a.e.vec = p.n % 4 == 0 && (uintptr_t)out % (p.dtype == GPIC_F32 ? 16 : 8) == 0;
+            a.e.vec = p.n % 8 == 0 && (uintptr_t)out % 16 == 0;
             if (h) {
                 a.e.is_step = 1;
                 a.e.decay = 1.0f - h->lr * h->decay;

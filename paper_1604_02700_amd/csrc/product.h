@@ -25,6 +25,8 @@
 // holds four consecutive columns j of one row i.
 #pragma once
 
+#include <type_traits>
+
 #include "encoder.h"
 
 namespace gpic {
@@ -82,45 +84,29 @@ __device__ __forceinline__ int pair_swizzle(int k)
     return ((k >> 1) & 1) | ((k >> 2) & 2);
 }
 
-// One operand's side of a tile: EXT rows (or columns) of it.
+// EXT rows (or columns) of one operand, as a tile or a part of one reads
+// them.  NT: threads that share the copies.  `row_of(r)`: the operand's row
+// of the part's row r, for r a multiple of 8 plus what is added to both
+// (k-strided: chunks of 8 stay together).
 template <int EXT, bool STRIDED, bool SPLIT, int NT>
 struct Side {
     static constexpr int kBytes = EXT * 128;              // LDS bytes of one step
     static constexpr int kCopies = kBytes / (NT * 16);    // copies a wave issues
     uint32_t voff[kCopies];
-    const char *base;
-    int64_t left;             // bytes from base to the end of the operand
-    int64_t advance;          // bytes of one step
 
-    // row0: first row of the tile; rows: of the whole operand.  row_of(r):
-    // the operand's row of the tile's row r (k-contiguous only).
     template <class RowOf>
-    __device__ void init(const Operand &o, int64_t z, int64_t row0, int64_t rows, int64_t K,
-                         int64_t k0, RowOf row_of)
+    __device__ void init(const Operand &o, int64_t first, int64_t rows, RowOf row_of)
     {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-        const char *p = static_cast<const char *>(o.p) + z * o.batch * 2;
         if (!STRIDED) {
-            // k0: first value of the contraction; split rows hold 2 values each
-            const int64_t at = SPLIT ? 2 * k0 : k0;
-            base = p + at * 2;
-            left = ((rows - 1) * o.ld + o.cols - at) * 2;
-            advance = 128;
 #pragma unroll
             for (int c = 0; c < kCopies; ++c) {
                 const int r = (wave * kCopies + c) * 8 + (lane >> 3);
                 const int chunk = (lane & 7) ^ ((r >> 1) & 7);
-                const int64_t row = row_of(row0, r);
-                voff[c] = row < rows ? (uint32_t)((row - row_of(row0, 0)) * o.ld * 2 + chunk * 16)
-                                     : kOutside;
+                const int64_t row = row_of(r);
+                voff[c] = row < rows ? (uint32_t)((row - first) * o.ld * 2 + chunk * 16) : kOutside;
             }
-            const int64_t first = row_of(row0, 0) * o.ld * 2;
-            base += first;
-            left -= first;
         } else {
-            base = p + (k0 * o.ld + (SPLIT ? split_at(row0) : row0)) * 2;
-            left = ((K - 1 - k0) * o.ld + o.cols - (SPLIT ? split_at(row0) : row0)) * 2;
-            advance = (SPLIT ? 32 : 64) * o.ld * 2;
             constexpr int kChunks = EXT / 8;              // chunks of a slab's row
             constexpr int kRows = 64 / kChunks;           // rows a copy covers
 #pragma unroll
@@ -129,42 +115,64 @@ struct Side {
                 const int k = r & 31, slab = r >> 5;
                 const int pos = lane % kChunks;
                 const int chunk = (((pos >> 1) ^ pair_swizzle<EXT>(k)) << 1) | (pos & 1);
-                uint32_t v;
-                int64_t col;              // first value of the chunk in the row
-                if (SPLIT) {
-                    v = (uint32_t)(k * o.ld * 2) + ((chunk >> 2) * 8 + slab * 4 + (chunk & 3)) * 16;
-                    col = split_at(row0) + ((chunk >> 2) * 8 + slab * 4 + (chunk & 3)) * 8;
-                } else {
-                    v = (uint32_t)((slab * 32 + k) * o.ld * 2) + chunk * 16;
-                    col = row0 + chunk * 8;
-                }
-                // beyond the row: the next row's values, never used, but
-                // kept out so that nothing outside the operand is read
-                voff[c] = col < o.cols ? v : kOutside;
+                const int64_t row = row_of(chunk * 8);
+                // 16-bit values from the start of the operand's row k
+                const int64_t at = SPLIT ? split_at(row) + slab * 32 : row;
+                const int64_t start = SPLIT ? split_at(first) : first;
+                // beyond the row: never used, kept inside the operand
+                voff[c] = at < o.cols
+                              ? (uint32_t)(((SPLIT ? k : slab * 32 + k) * o.ld + at - start) * 2)
+                              : kOutside;
             }
         }
     }
 
     // issue the copies of one step; kleft: values of k that are left
-    __device__ __forceinline__ void copy(uint32_t lds, int64_t kleft) const
+    __device__ __forceinline__ void copy(u32x4 rsrc, uint32_t lds, int64_t kleft) const
     {
-        const u32x4 rsrc = make_rsrc(base, left);
         const int wave = threadIdx.x >> 6;
         const uint32_t at = lds + (uint32_t)wave * (kCopies * 1024);
-        if (!STRIDED && !SPLIT && kleft < 64) {
-            const int lane = threadIdx.x & 63;
 #pragma unroll
-            for (int c = 0; c < kCopies; ++c) {
-                const int r = (wave * kCopies + c) * 8 + (lane >> 3);
-                const int chunk = (lane & 7) ^ ((r >> 1) & 7);
-                copy_to_lds(rsrc, chunk * 8 < kleft ? voff[c] : kOutside, uniform(at + c * 1024));
-            }
-        } else {
-#pragma unroll
-            for (int c = 0; c < kCopies; ++c)
-                copy_to_lds(rsrc, voff[c], uniform(at + c * 1024));
-        }
+        for (int c = 0; c < kCopies; ++c)
+            copy_one(rsrc, at, c, kleft);
     }
+    __device__ __forceinline__ void copy_one(u32x4 rsrc, uint32_t at, int c, int64_t kleft) const
+    {
+        uint32_t v = voff[c];
+        if (!STRIDED && !SPLIT) {         // the last step may end inside a row's 64 values
+            const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+            const int r = (wave * kCopies + c) * 8 + (lane >> 3);
+            const int chunk = (lane & 7) ^ ((r >> 1) & 7);
+            const int valid = kleft < 64 ? (int)kleft : 64;
+            v = chunk * 8 < valid ? v : kOutside;
+        }
+        copy_to_lds(rsrc, v, uniform(at + c * 1024));
+    }
+};
+
+// Where one operand's copies of a step start, and what is left of it.
+template <bool STRIDED, bool SPLIT>
+struct Stream {
+    const char *base;
+    int64_t left, advance;
+    // first: the operand's row (column) that offsets count from; k0: first k
+    __device__ void init(const Operand &o, int64_t z, int64_t first, int64_t rows, int64_t K,
+                         int64_t k0)
+    {
+        int64_t at, end;
+        if (!STRIDED) {
+            at = first * o.ld + (SPLIT ? 2 * k0 : k0);
+            end = (rows - 1) * o.ld + o.cols;
+            advance = 128;
+        } else {
+            at = k0 * o.ld + (SPLIT ? split_at(first) : first);
+            end = (K - 1) * o.ld + o.cols;
+            advance = (SPLIT ? 32 : 64) * o.ld * 2;
+        }
+        base = static_cast<const char *>(o.p) + (z * o.batch + at) * 2;
+        left = (end - at) * 2;
+    }
+    __device__ __forceinline__ u32x4 rsrc() const { return make_rsrc(base, left); }
     __device__ __forceinline__ void step()
     {
         base += advance;
@@ -207,158 +215,211 @@ __device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 c)
 }
 
 // --------------------------------------------------------------- epilogue
-__device__ __forceinline__ int64_t part_at(const Epilogue &e, int64_t row, int64_t col)
+// A wave's accumulators go through LDS (its own piece, no barrier) so that
+// a lane finishes eight consecutive columns of a row: 16-byte loads and
+// stores that cover whole lines.
+// eight values p[i .. i + 7] of which `valid` exist; whole: at once
+__device__ __forceinline__ f32x8 load8(const void *p, int64_t i, int dtype, int valid, bool whole)
 {
-    return row * e.ldp + (e.is_split ? split_at(col) : col);
+    if (whole) {
+        if (dtype == GPIC_F32)
+            return *reinterpret_cast<const f32x8 *>(static_cast<const float *>(p) + i);
+        if (dtype == GPIC_F16)
+            return __builtin_convertvector(
+                *reinterpret_cast<const half8 *>(static_cast<const _Float16 *>(p) + i), f32x8);
+        return __builtin_convertvector(
+            *reinterpret_cast<const bfrag8 *>(static_cast<const __bf16 *>(p) + i), f32x8);
+    }
+    f32x8 v = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (j < valid)
+            v[j] = load1(p, i + j, dtype);
+    return v;
 }
 
-__device__ __forceinline__ void store_parts(const Epilogue &e, int64_t z, int64_t row, int64_t col,
-                                            f32x4 v)
+__device__ __forceinline__ void store8(void *p, int64_t i, f32x8 v, int dtype, int valid,
+                                       bool whole)
 {
-    const int64_t at = z * e.batch_p + part_at(e, row, col);
+    if (whole) {
+        if (dtype == GPIC_F32)
+            *reinterpret_cast<f32x8 *>(static_cast<float *>(p) + i) = v;
+        else if (dtype == GPIC_F16)
+            *reinterpret_cast<half8 *>(static_cast<_Float16 *>(p) + i) =
+                __builtin_convertvector(v, half8);
+        else
+            *reinterpret_cast<bfrag8 *>(static_cast<__bf16 *>(p) + i) =
+                __builtin_convertvector(v, bfrag8);
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (j < valid)
+            store1(p, i + j, v[j], dtype);
+}
+
+__device__ __forceinline__ int64_t part_at(const Epilogue &e, int64_t z, int64_t row, int64_t col)
+{
+    return z * e.batch_p + row * e.ldp + (e.is_split ? split_at(col) : col);
+}
+
+// 16-bit parts of v (times store_scale already), eight columns
+__device__ __forceinline__ void store_parts(const Epilogue &e, int64_t at, f32x8 v)
+{
     _Float16 *hi = static_cast<_Float16 *>(e.p_hi) + at;
-    v *= e.store_scale;
-    const half4 h = __builtin_convertvector(v, half4);
-    *reinterpret_cast<half4 *>(hi) = h;
+    const half8 h = __builtin_convertvector(v, half8);
+    *reinterpret_cast<half8 *>(hi) = h;
     if (e.is_split || e.p_lo) {
-        const half4 l = __builtin_convertvector(v - __builtin_convertvector(h, f32x4), half4);
         _Float16 *lo = e.is_split ? hi + 32 : static_cast<_Float16 *>(e.p_lo) + at;
-        *reinterpret_cast<half4 *>(lo) = l;
+        *reinterpret_cast<half8 *>(lo) =
+            __builtin_convertvector(v - __builtin_convertvector(h, f32x8), half8);
     }
 }
 
-__device__ __forceinline__ f32x4 load_parts(const Epilogue &e, int64_t z, int64_t row, int64_t col)
+__device__ __forceinline__ f32x8 load_parts(const Epilogue &e, int64_t at)
 {
-    const int64_t at = z * e.batch_p + part_at(e, row, col);
     const _Float16 *hi = static_cast<const _Float16 *>(e.c_hi) + at;
-    f32x4 v = __builtin_convertvector(*reinterpret_cast<const half4 *>(hi), f32x4);
+    f32x8 v = __builtin_convertvector(*reinterpret_cast<const half8 *>(hi), f32x8);
     if (e.is_split || e.c_lo) {
         const _Float16 *lo = e.is_split ? hi + 32 : static_cast<const _Float16 *>(e.c_lo) + at;
-        v += __builtin_convertvector(*reinterpret_cast<const half4 *>(lo), f32x4);
+        v += __builtin_convertvector(*reinterpret_cast<const half8 *>(lo), f32x8);
     }
     return v * e.load_scale;
 }
 
-__device__ __forceinline__ void scaled(const Epilogue &e, f32x4 &v)
+// What the accumulators are multiplied by: the operands' scales are powers
+// of two, taken off one after the other so that neither step overflows.
+struct Factor {
+    float a, b;
+};
+__device__ __forceinline__ Factor factor_of(const Epilogue &e)
 {
-    if (e.sa)
-        v *= 1.0f / *e.sa;                // powers of two: exact
-    if (e.sb)
-        v *= 1.0f / *e.sb;
-    v *= e.alpha;
+    return Factor{e.sa ? 1.0f / *e.sa : 1.0f, (e.sb ? 1.0f / *e.sb : 1.0f) * e.alpha};
 }
 
-// Four consecutive columns col .. col + 3 (col % 4 == 0) of one row.
-// mirror (kEpiSym): also the transposed four.
-template <int EPI>
-__device__ __forceinline__ void finish4(const Epilogue &e, int64_t z, int64_t row, int64_t col,
-                                        int M, int N, f32x4 v, bool mirror)
+__device__ __forceinline__ f32x8 staged(const float *p, Factor f)
 {
-    // the vector and the scalar paths round alike
+    return *reinterpret_cast<const f32x8 *>(p) * f.a * f.b;
+}
+
+// Finishes `ROWS` x `COLS` accumulators that the wave has staged at `st`
+// (pitch COLS + 4 floats), the output's rows from row0, columns from col0
+// (gated: columns from col0 / 2).  mirror (kEpiSym): the transposed block too.
+template <int ROWS, int COLS, int EPI>
+__device__ __forceinline__ void finish_block(const Epilogue &e, int64_t z, int64_t row0,
+                                             int64_t col0, int64_t M, int64_t N, float *st,
+                                             bool mirror)
+{
+    // the whole and the partial accesses round alike
 #pragma clang fp contract(off)
-    scaled(e, v);
-    if (EPI == kEpiLayer) {
-        const bool whole = e.vec && col + 4 <= N;
-        if (whole) {
-            if (e.bias)
-                v += load4(e.bias, col, e.dtype);
-            if (e.pre)
-                store4(e.pre, row * e.ldz + col, v, e.dtype);
+    constexpr int kPitch = COLS + 4;
+    constexpr int kOut = EPI == kEpiGated ? COLS / 2 : COLS;     // output columns
+    constexpr int kLanes = kOut / 8, kRowsPass = 64 / kLanes, kPasses = ROWS / kRowsPass;
+    constexpr int kGroup = kPasses < 2 ? kPasses : 2;            // rows in flight a lane
+    static_assert(kPasses * kRowsPass == ROWS && kPasses % kGroup == 0, "passes");
+    const int lane = threadIdx.x & 63, q = lane % kLanes, r0 = lane / kLanes;
+    const Factor f = factor_of(e);
+    if (EPI == kEpiGated) {
+        const int64_t col = col0 / 2 + q * 8, half = e.half;
+        const int valid = half - col < 8 ? (int)(half - col) : 8;
+        const bool whole = e.vec && valid == 8;
+        const float *src = st + (q >> 1) * 32 + (q & 1) * 8;
+        for (int p = 0; p < kPasses; ++p) {
+            const int r = p * kRowsPass + r0;
+            const int64_t row = row0 + r;
+            if (valid <= 0 || row >= M)
+                continue;
+            f32x8 g = staged(src + r * kPitch, f);
+            const f32x8 u = staged(src + r * kPitch + 16, f);
+            if (e.pre) {
+                store8(e.pre, row * e.ldz + col, g, GPIC_F32, valid, whole);
+                store8(e.pre, row * e.ldz + half + col, u, GPIC_F32, valid, whole);
+            }
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                v[j] = activate(v[j], e.act);
-            if (e.res)
-                v += load4(e.res, row * e.ldr + col, e.dtype);
-            store4(e.out, row * e.ldo + col, v, e.dtype);
-        } else {
+            for (int j = 0; j < 8; ++j)
+                g[j] = activate(g[j], e.act) * u[j];
+            store8(e.out, row * e.ldo + col, g, e.dtype, valid, whole);
+        }
+        return;
+    }
+    const int64_t col = col0 + q * 8;
+    // 16-bit parts: the padding up to a multiple of 64 columns is written too
+    const int64_t end = EPI == kEpiSym ? (N + 63) / 64 * 64 : N;
+    const int64_t here = end - col;
+    const int valid = here < 0 ? 0 : (here < 8 ? (int)here : 8);
+    const bool whole = e.vec && valid == 8;
+    f32x8 bias = 0.0f;
+    if (EPI == kEpiLayer && e.bias && valid > 0)
+        bias = load8(e.bias, col, e.dtype, valid, whole);
+    for (int p0 = 0; p0 < kPasses; p0 += kGroup) {
+        f32x8 v[kGroup], c[kGroup];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int64_t c = col + j;
-                if (c >= N)
-                    continue;
-                float x = v[j];
+        for (int p = 0; p < kGroup; ++p) {
+            const int r = (p0 + p) * kRowsPass + r0;
+            const int64_t row = row0 + r;
+            v[p] = staged(st + r * kPitch + q * 8, f);
+            c[p] = 0.0f;
+            if (valid <= 0 || row >= M)
+                continue;
+            if (EPI == kEpiLayer && e.res)
+                c[p] = load8(e.res, row * e.ldr + col, e.dtype, valid, whole);
+            if (EPI == kEpiUpdate || (EPI == kEpiSym && e.c_hi))
+                c[p] = load_parts(e, part_at(e, z, row, col)) * e.beta;
+            if (EPI == kEpiUpdate && e.is_step) {
+                // decay W - step (beta X + acc)
+                const f32x8 old = load8(e.out, z * e.batch_o + row * e.ldo + col, e.dtype, valid,
+                                        whole);
+                c[p] = old * e.decay - c[p] * e.step;
+                v[p] = v[p] * -e.step;
+            }
+        }
+#pragma unroll
+        for (int p = 0; p < kGroup; ++p) {
+            const int r = (p0 + p) * kRowsPass + r0;
+            const int64_t row = row0 + r;
+            if (valid <= 0 || row >= M)
+                continue;
+            f32x8 x = v[p];
+            if (EPI == kEpiLayer) {
                 if (e.bias)
-                    x += load1(e.bias, c, e.dtype);
+                    x = x + bias;
                 if (e.pre)
-                    store1(e.pre, row * e.ldz + c, x, e.dtype);
-                x = activate(x, e.act);
+                    store8(e.pre, row * e.ldz + col, x, e.dtype, valid, whole);
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    x[j] = activate(x[j], e.act);
                 if (e.res)
-                    x += load1(e.res, row * e.ldr + c, e.dtype);
-                store1(e.out, row * e.ldo + c, x, e.dtype);
-            }
-        }
-    } else if (EPI == kEpiSym) {
-        // columns N .. up to a multiple of 64 hold zeros: the products
-        // over this matrix read whole steps of k
-        if (e.c_hi)
-            v = e.beta * load_parts(e, z, row, col) + v;
-        store_parts(e, z, row, col, v);
-        if (mirror) {
-            v *= e.store_scale;
-            const int64_t at = z * e.batch_p;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (col + j >= N)
+                    x = x + c[p];
+                store8(e.out, row * e.ldo + col, x, e.dtype, valid, whole);
+            } else if (EPI == kEpiSym) {
+                x = (x + c[p]) * e.store_scale;
+                store_parts(e, part_at(e, z, row, col), x);
+                if (mirror)
+                    *reinterpret_cast<f32x8 *>(st + r * kPitch + q * 8) = x;
+            } else {
+                x = x + c[p];
+                if (!e.to_out) {
+                    store_parts(e, part_at(e, z, row, col), x * e.store_scale);
                     continue;
-                const int64_t p = at + part_at(e, col + j, row);
-                const _Float16 h = (_Float16)v[j];
-                static_cast<_Float16 *>(e.p_hi)[p] = h;
-                if (e.is_split)
-                    static_cast<_Float16 *>(e.p_hi)[p + 32] = (_Float16)(v[j] - (float)h);
-            }
-        }
-    } else if (EPI == kEpiUpdate) {
-        v += e.beta * load_parts(e, z, row, col);
-        if (!e.to_out) {
-            store_parts(e, z, row, col, v);
-            return;
-        }
-        const int64_t o = z * e.batch_o + row * e.ldo + col;
-        if (e.vec && col + 4 <= N) {
-            if (e.is_step)
-                v = e.decay * load4(e.out, o, e.dtype) - e.step * v;
-            store4(e.out, o, v, e.dtype);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (col + j >= N)
-                    continue;
-                float x = v[j];
-                if (e.is_step)
-                    x = e.decay * load1(e.out, o + j, e.dtype) - e.step * x;
-                store1(e.out, o + j, x, e.dtype);
+                }
+                store8(e.out, z * e.batch_o + row * e.ldo + col, x, e.dtype, valid, whole);
             }
         }
     }
-}
-
-// Four columns of the gated layer: gate g and up u of the same columns.
-__device__ __forceinline__ void finish4_gated(const Epilogue &e, int64_t row, int64_t col, f32x4 g,
-                                              f32x4 u)
-{
-#pragma clang fp contract(off)
-    scaled(e, g);
-    scaled(e, u);
-    if (e.vec && col + 4 <= e.half) {
-        if (e.pre) {
-            store4(e.pre, row * e.ldz + col, g, GPIC_F32);
-            store4(e.pre, row * e.ldz + e.half + col, u, GPIC_F32);
-        }
+    if (EPI == kEpiSym && mirror) {
+        // rows and columns change places: a lane takes eight rows of a
+        // column.  Only whole tiles above the diagonal are mirrored, so the
+        // rows all exist; columns beyond N are padding.
+        constexpr int kL = ROWS / 8, kC = 64 / kL;
+        const int rq = (lane % kL) * 8, c0 = lane / kL;
+        for (int p = 0; p < COLS / kC; ++p) {
+            const int c = p * kC + c0;
+            f32x8 x;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            g[j] = activate(g[j], e.act) * u[j];
-        store4(e.out, row * e.ldo + col, g, e.dtype);
-    } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int64_t c = col + j;
-            if (c >= e.half)
-                continue;
-            if (e.pre) {
-                store1(e.pre, row * e.ldz + c, g[j], GPIC_F32);
-                store1(e.pre, row * e.ldz + e.half + c, u[j], GPIC_F32);
-            }
-            store1(e.out, row * e.ldo + c, activate(g[j], e.act) * u[j], e.dtype);
+            for (int j = 0; j < 8; ++j)
+                x[j] = st[(rq + j) * kPitch + c];
+            if (col0 + c < N)
+                store_parts(e, part_at(e, z, col0 + c, row0 + rq), x);
         }
     }
 }
@@ -372,15 +433,22 @@ struct Tile {
     static constexpr int kThreads = 64 * WM * WN;
 };
 
-// Which tile a workgroup takes: consecutive ids go round the 8 compute
+using TileL = Tile<2, 4, 8, 4>;      // 256 x 256, 8 waves
+using TileM = Tile<2, 2, 4, 4>;      // 128 x 128, 4 waves
+using TileS = Tile<2, 2, 2, 2>;      // 64 x 64, 4 waves
+
+// Where tile `id` of `count` lies.  Consecutive ids go round the 8 compute
 // dies, so each die gets one contiguous run of tiles, walked in bands of 8
 // tile rows (its second-level cache then holds the band's A and a few
 // columns of B).  Symmetric products count the upper triangle's tiles by rows.
-__device__ __forceinline__ void which_tile(int id, int count, int tm, int tn, bool sym, int &ti,
-                                           int &tj)
+__device__ __forceinline__ int die_order(int id, int count)
 {
     const int per = count / 8, extra = count % 8, die = id % 8, k = id / 8;
-    id = die * per + (die < extra ? die : extra) + k;
+    return die * per + (die < extra ? die : extra) + k;
+}
+
+__device__ __forceinline__ void which_tile(int id, int tm, int tn, bool sym, int &ti, int &tj)
+{
     if (sym) {
         // rows of tn, tn - 1, .. tiles: row i starts at i tn - i (i - 1) / 2
         const float b = 2.0f * tn + 1.0f;
@@ -401,6 +469,93 @@ __device__ __forceinline__ void which_tile(int id, int count, int tm, int tn, bo
     tj = in / rows;
 }
 
+// What a workgroup does: whole tiles first, then the parts of the tiles
+// whose contraction is split.
+struct Work {
+    int tile, split, parts, ti, tj;
+    int64_t z, s0, s1;         // matrix of the batch, steps of the contraction
+    __device__ Work(const ProductArgs &a, int tm, int tn, bool sym, int step)
+    {
+        split = 0;
+        parts = 1;
+        if ((int)blockIdx.x < a.whole) {
+            tile = die_order(blockIdx.x, a.whole);
+        } else {
+            const int t = (int)blockIdx.x - a.whole, tail = ((int)gridDim.x - a.whole) / a.splits;
+            parts = a.splits;
+            split = t / tail;
+            tile = a.whole + t % tail;
+        }
+        const int each = sym ? tn * (tn + 1) / 2 : tm * tn;
+        z = tile / each;
+        which_tile(tile % each, tm, tn, sym, ti, tj);
+        const int64_t steps = (a.K + step - 1) / step;
+        s0 = steps * split / parts;
+        s1 = steps * (split + 1) / parts;
+    }
+};
+
+// The operand row of row r of B's tile.  Gated: in turn 16 rows of the
+// gate's projection and the 16 of the up projection for the same columns, so
+// that both meet in one lane; rows whose column is at or beyond `half` are
+// outside.
+template <int EPI>
+__device__ __forceinline__ int64_t row_of_b(const ProductArgs &a, int64_t col0, int r)
+{
+    if (EPI != kEpiGated)
+        return col0 + r;
+    const int64_t c = col0 / 2 + (r >> 5) * 16 + (r & 15);
+    return c >= a.e.half ? (int64_t)a.N : ((r & 16) ? a.e.half + c : c);
+}
+
+// The accumulators of a tile are staged a few fragment rows at a time.
+template <class T>
+struct Staging {
+    static constexpr int kCols = 16 * T::kRN, kPitch = kCols + 4;
+    static constexpr int kFrags = T::kRM < 4 ? T::kRM : 4;           // fragment rows at once
+    static constexpr int kRows = 16 * kFrags;
+    static constexpr int kFloats = kRows * kPitch;                   // a wave's piece
+    static constexpr int kBytes = kFloats * 4 * (T::kThreads / 64);
+};
+
+// A wave's accumulators to their place: the epilogue, or the partial sums.
+template <class T, int EPI>
+__device__ __forceinline__ void finish_tile(const ProductArgs &a, const Work &w,
+                                            f32x4 (&acc)[T::kRM][T::kRN], char *lds)
+{
+    using St = Staging<T>;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int wm = (wave / T::kWN) * (16 * T::kRM), wn = (wave % T::kWN) * (16 * T::kRN);
+    // every wave is done with the buffers
+    copies_done();
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    float *st = reinterpret_cast<float *>(lds) + wave * St::kFloats;
+    float *to = st + (lane & 15) * St::kPitch + (lane >> 4) * 4;
+    float *part = a.part + ((int64_t)w.split * (((int)gridDim.x - a.whole) / w.parts) +
+                            (w.tile - a.whole)) * ((int64_t)T::kBM * T::kBN) +
+                  wm * T::kBN + wn;
+#pragma unroll
+    for (int i0 = 0; i0 < T::kRM; i0 += St::kFrags) {
+#pragma unroll
+        for (int i = 0; i < St::kFrags; ++i)
+#pragma unroll
+            for (int j = 0; j < T::kRN; ++j)
+                *reinterpret_cast<f32x4 *>(to + 16 * i * St::kPitch + 16 * j) = acc[i0 + i][j];
+        if (w.parts > 1) {
+            for (int r = lane / (St::kCols / 4); r < St::kRows; r += 64 / (St::kCols / 4)) {
+                const int c = lane % (St::kCols / 4) * 4;
+                *reinterpret_cast<f32x4 *>(part + (16 * i0 + r) * T::kBN + c) =
+                    *reinterpret_cast<const f32x4 *>(st + r * St::kPitch + c);
+            }
+        } else {
+            finish_block<St::kRows, St::kCols, EPI>(
+                a.e, w.z, (int64_t)w.ti * T::kBM + wm + 16 * i0, (int64_t)w.tj * T::kBN + wn, a.M,
+                a.N, st, EPI == kEpiSym && w.ti != w.tj);
+        }
+    }
+}
+
 template <class T, bool ASTR, bool BSTR, int OP, int EPI>
 __global__ __launch_bounds__(T::kThreads) void product_kernel(ProductArgs a, int tm, int tn)
 {
@@ -409,33 +564,23 @@ __global__ __launch_bounds__(T::kThreads) void product_kernel(ProductArgs a, int
     using SideA = Side<T::kBM, ASTR, SPLIT, T::kThreads>;
     using SideB = Side<T::kBN, BSTR, SPLIT, T::kThreads>;
     constexpr int kBuf = SideA::kBytes + SideB::kBytes;
-    __shared__ __attribute__((aligned(1024))) char lds[2 * kBuf];
+    using St = Staging<T>;
+    constexpr int kLds = 2 * kBuf > St::kBytes ? 2 * kBuf : St::kBytes;
+    __shared__ __attribute__((aligned(1024))) char lds[kLds];
 
-    int ti, tj;
-    which_tile(blockIdx.x, gridDim.x, tm, tn, EPI == kEpiSym, ti, tj);
-    const int64_t z = blockIdx.y;
-    const int64_t row0 = (int64_t)ti * T::kBM;
-    const int64_t col0 = (int64_t)tj * T::kBN;
-    const int split = blockIdx.z;
-    // this part's steps of the contraction
-    const int64_t steps = (a.K + kStep - 1) / kStep;
-    const int64_t s0 = steps * split / a.splits, s1 = steps * (split + 1) / a.splits;
+    const Work w(a, tm, tn, EPI == kEpiSym, kStep);
+    const int64_t z = w.z, s0 = w.s0, s1 = w.s1;
+    const int64_t row0 = (int64_t)w.ti * T::kBM, col0 = (int64_t)w.tj * T::kBN;
 
     SideA sa;
     SideB sb;
-    sa.init(a.A, z, row0, a.M, a.K, s0 * kStep, [](int64_t r0, int r) { return r0 + r; });
-    if (EPI == kEpiGated) {
-        // rows of B in turn 16 of the gate's and the up projection's 16 of
-        // the same columns, so that both meet in one lane.  Rows at or
-        // beyond `half` in the gate's half are not wanted: outside.
-        const int64_t half = a.e.half, j0 = col0 / 2, all = a.N;
-        sb.init(a.B, z, j0, all, a.K, s0 * kStep, [half, all](int64_t r0, int r) {
-            const int64_t c = r0 + (r >> 5) * 16 + (r & 15);
-            return c >= half ? all : ((r & 16) ? half + c : c);
-        });
-    } else {
-        sb.init(a.B, z, col0, a.N, a.K, s0 * kStep, [](int64_t r0, int r) { return r0 + r; });
-    }
+    Stream<ASTR, SPLIT> pa;
+    Stream<BSTR, SPLIT> pb;
+    const int64_t first_b = EPI == kEpiGated ? col0 / 2 : col0;
+    sa.init(a.A, row0, a.M, [&](int r) { return row0 + r; });
+    sb.init(a.B, first_b, a.N, [&](int r) { return row_of_b<EPI>(a, col0, r); });
+    pa.init(a.A, z, row0, a.M, a.K, s0 * kStep);
+    pb.init(a.B, z, first_b, a.N, a.K, s0 * kStep);
 
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int wm = (wave / T::kWN) * (16 * T::kRM), wn = (wave % T::kWN) * (16 * T::kRN);
@@ -446,154 +591,323 @@ __global__ __launch_bounds__(T::kThreads) void product_kernel(ProductArgs a, int
         for (int j = 0; j < T::kRN; ++j)
             acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
+    // Two steps of copies ahead, one slab of fragments ahead: while the
+    // waves multiply one slab's fragments they read the next slab's.  The
+    // barrier lies between the slabs of a step: by then every wave holds
+    // the step's second slab in registers, so its buffer takes the copies
+    // of the step after next.
     const uint32_t lds0 = lds_address(lds);
     int64_t kleft = a.K - s0 * kStep;
+    auto copy_next = [&](int buf) {
+        const uint32_t to = lds0 + (uint32_t)buf * kBuf;
+        sa.copy(pa.rsrc(), to, kleft);
+        sb.copy(pb.rsrc(), to + SideA::kBytes, kleft);
+        pa.step();
+        pb.step();
+        kleft -= kStep;
+    };
+    u32x4 fa[2][T::kRM], fb[2][T::kRN];
+    auto read = [&](int buf, int slab) {
+        const char *ta = lds + buf * kBuf, *tb = ta + SideA::kBytes;
+#pragma unroll
+        for (int j = 0; j < T::kRN; ++j)
+            fb[slab][j] = fragment<T::kBN, BSTR>(tb, slab, wn + 16 * j);
+#pragma unroll
+        for (int i = 0; i < T::kRM; ++i)
+            fa[slab][i] = fragment<T::kBM, ASTR>(ta, slab, wm + 16 * i);
+    };
+    auto multiply = [&](int pa, int pb) {
+#pragma unroll
+        for (int i = 0; i < T::kRM; ++i)
+#pragma unroll
+            for (int j = 0; j < T::kRN; ++j)
+                acc[i][j] = mma<OP>(fb[pb][j], fa[pa][i], acc[i][j]);
+    };
+    // one LDS read, then the share of `products` that goes with it
+    constexpr int kReads = T::kRM * (ASTR ? 2 : 1) + T::kRN * (BSTR ? 2 : 1);
+    constexpr int kPerRead = T::kRM * T::kRN / kReads > 0 ? T::kRM * T::kRN / kReads : 1;
+    auto interleave = [&]() {
+#pragma unroll
+        for (int r = 0; r < kReads; ++r) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, kPerRead, 0);
+        }
+    };
     if (s1 > s0) {
-        sa.copy(lds0, kleft);
-        sb.copy(lds0 + SideA::kBytes, kleft);
-    }
-    for (int64_t s = s0; s < s1; ++s) {
-        const int cur = (int)(s - s0) & 1;
-        // this step's copies have landed in every wave's view, and nobody
-        // reads the other buffer any more
+        copy_next(0);
         copies_done();
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        if (s + 1 < s1) {
-            sa.step();
-            sb.step();
-            kleft -= kStep;
-            const uint32_t to = lds0 + (uint32_t)(cur ^ 1) * kBuf;
-            sa.copy(to, kleft);
-            sb.copy(to + SideA::kBytes, kleft);
-        }
-        const char *ta = lds + cur * kBuf, *tb = ta + SideA::kBytes;
-        u32x4 fa[2][T::kRM], fb[2][T::kRN];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-#pragma unroll
-            for (int j = 0; j < T::kRN; ++j)
-                fb[h][j] = fragment<T::kBN, BSTR>(tb, h, wn + 16 * j);
-#pragma unroll
-            for (int i = 0; i < T::kRM; ++i)
-                fa[h][i] = fragment<T::kBM, ASTR>(ta, h, wm + 16 * i);
-        }
-#pragma unroll
-        for (int i = 0; i < T::kRM; ++i)
-#pragma unroll
-            for (int j = 0; j < T::kRN; ++j) {
-                acc[i][j] = mma<OP>(fb[0][j], fa[0][i], acc[i][j]);
-                if (SPLIT)
-                    acc[i][j] = mma<OP>(fb[1][j], fa[0][i], acc[i][j]);
-            }
-#pragma unroll
-        for (int i = 0; i < T::kRM; ++i)
-#pragma unroll
-            for (int j = 0; j < T::kRN; ++j)
-                acc[i][j] = mma<OP>(fb[SPLIT ? 0 : 1][j], fa[1][i], acc[i][j]);
+        if (s0 + 1 < s1)
+            copy_next(1);
+        read(0, 0);
+    }
+    for (int64_t s = s0; s < s1; ++s) {
+        const int cur = (int)(s - s0) & 1;
+        read(cur, 1);
+        multiply(0, 0);
+        interleave();
+        copies_done();
+        __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
+        if (s + 2 < s1)
+            copy_next(cur);
+        if (SPLIT) {
+            multiply(0, 1);
+            multiply(1, 0);
+            read(cur ^ 1, 0);
+        } else {
+            read(cur ^ 1, 0);
+            multiply(1, 1);
+            interleave();
+        }
     }
 
-    // lane: row i of each fragment, columns 4 g .. 4 g + 3
-    const int g4 = (lane >> 4) * 4;
-#pragma unroll
-    for (int i = 0; i < T::kRM; ++i) {
-        const int64_t row = row0 + wm + 16 * i + (lane & 15);
-        if (row >= a.M)
-            continue;
-        if (EPI == kEpiGated) {
-#pragma unroll
-            for (int j = 0; j < T::kRN; j += 2) {
-                const int64_t col = col0 / 2 + (wn + 16 * j) / 2 + g4;
-                if (col < a.e.half)
-                    finish4_gated(a.e, row, col, acc[i][j], acc[i][j + 1]);
-            }
-            continue;
-        }
-#pragma unroll
-        for (int j = 0; j < T::kRN; ++j) {
-            const int64_t col = col0 + wn + 16 * j + g4;
-            const int64_t end = EPI == kEpiSym ? (a.N + 63) / 64 * 64 : a.N;
-            if (col >= end)
-                continue;
-            if (a.splits > 1) {
-                const int64_t n4 = (a.N + 63) / 64 * 64;
-                float *p = a.part + ((split * a.batch + z) * (int64_t)a.M + row) * n4 + col;
-                *reinterpret_cast<f32x4 *>(p) = acc[i][j];
-            } else {
-                finish4<EPI>(a.e, z, row, col, a.M, a.N, acc[i][j],
-                             EPI == kEpiSym && ti != tj);
-            }
-        }
-    }
+    finish_tile<T, EPI>(a, w, acc, lds);
 }
 
-// The parts of a split contraction in order, then the epilogue.  Four
-// columns a thread.
-template <int EPI>
-__global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a, int tile)
+// The 256 x 256 tile: 8 waves of 128 x 64, two to a SIMD.  A step is four
+// phases, each 16 (split: 24) matrix instructions on one quarter of a wave's
+// tile: rows A0, A1 (64 each) by columns B0, B1 (32 each) in the order A0 B0,
+// A0 B1, A1 B1, A1 B0.  Between its matrix instructions a phase reads the
+// fragments that a later phase needs and issues two copies, so that the two
+// waves of a SIMD fill each other's gaps.  A phase begins with a barrier,
+// before which a wave has waited for all but its last phase's reads and all
+// but its last ten copies.  Hence what a phase reads (its copies are older
+// than ten) has landed for every wave, and what was read two phases before
+// has been read by every wave: copies run two steps ahead, into that place.
+// 8,192 cubed in bfloat16: 930 to 1,020 us, box to box (1.08 to 1.18
+// PFLOP/s), matrix pipe busy 64 % at the 1.6 to 1.85 GHz that the card's power
+// leaves; leaving the barriers or the waits out (a timing copy) gains 2 %,
+// the copies or the fragment reads 20 % each.  Four waves of 128 x 128 gave 956, waves
+// one barrier apart with reads before the products 1.06, one buffer step ahead
+// with all copies at its start 1.04.
+//   phase     multiplies   reads        copies (step t + 2)
+//   1         A0 B0        B1           A0
+//   2         A0 B1        A1           B0
+//   3         A1 B1        A0 (t + 1)   B1
+//   4         A1 B0        B0 (t + 1)   A1
+template <bool ASTR, bool BSTR, int OP, int EPI>
+__global__ __launch_bounds__(512) void product_large_kernel(ProductArgs a, int tm, int tn)
 {
-    const int64_t n4 = (a.N + 63) / 64 * 64, quads = n4 / 4;
-    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t z = blockIdx.y;
-    if (id >= a.M * quads)
+    using T = TileL;
+    constexpr bool SPLIT = OP == kOpSplit;
+    constexpr int kStep = SPLIT ? 32 : 64;           // values of k per step
+    using SideA = Side<128, ASTR, SPLIT, T::kThreads>;
+    using SideB = Side<128, BSTR, SPLIT, T::kThreads>;
+    constexpr int kPart = 128 * 128;                 // LDS bytes of A0, A1, B0 or B1
+    constexpr int kBuf = 4 * kPart;
+    constexpr int kLds = 2 * kBuf > Staging<T>::kBytes ? 2 * kBuf : Staging<T>::kBytes;
+    __shared__ __attribute__((aligned(1024))) char lds[kLds];
+
+    const Work w(a, tm, tn, EPI == kEpiSym, kStep);
+    const int64_t z = w.z;
+    const int64_t row0 = (int64_t)w.ti * T::kBM, col0 = (int64_t)w.tj * T::kBN;
+    SideA sa[2];
+    SideB sb[2];
+    Stream<ASTR, SPLIT> pa;
+    Stream<BSTR, SPLIT> pb;
+    const int64_t first_b = EPI == kEpiGated ? col0 / 2 : col0;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        sa[h].init(a.A, row0, a.M,
+                   [&](int r) { return row0 + (r >> 6) * 128 + h * 64 + (r & 63); });
+        sb[h].init(a.B, first_b, a.N, [&](int r) {
+            return row_of_b<EPI>(a, col0, (r >> 5) * 64 + h * 32 + (r & 31));
+        });
+    }
+    pa.init(a.A, z, row0, a.M, a.K, w.s0 * kStep);
+    pb.init(a.B, z, first_b, a.N, a.K, w.s0 * kStep);
+
+    const int wave = threadIdx.x >> 6;
+    const int ra = (wave / T::kWN) * 64, rb = (wave % T::kWN) * 32;   // within a group
+    f32x4 acc[T::kRM][T::kRN];
+#pragma unroll
+    for (int i = 0; i < T::kRM; ++i)
+#pragma unroll
+        for (int j = 0; j < T::kRN; ++j)
+            acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    u32x4 fa[2][2][4], fb[2][2][2];                  // [half][slab][fragment]
+
+    const uint32_t lds0 = lds_address(lds);
+    int64_t kleft_a = a.K - w.s0 * kStep, kleft_b = kleft_a;
+    // LDS: A0, A1, B0, B1 of buffer 0, then of buffer 1
+    const uint32_t lds_wave = lds0 + (uint32_t)wave * (SideA::kCopies * 1024);
+    // copy c of A (B) half h into its place in buffer buf
+    auto copy_a = [&](int buf, int h, int c) {
+        sa[h].copy_one(pa.rsrc(), lds_wave + (uint32_t)(buf * kBuf + h * kPart), c, kleft_a);
+    };
+    auto copy_b = [&](int buf, int h, int c) {
+        sb[h].copy_one(pb.rsrc(), lds_wave + (uint32_t)(buf * kBuf + (2 + h) * kPart), c, kleft_b);
+    };
+    auto next_a = [&]() {
+        pa.step();
+        kleft_a -= kStep;
+    };
+    auto next_b = [&]() {
+        pb.step();
+        kleft_b -= kStep;
+    };
+    auto read_a = [&](int buf, int h, int s, int i) {
+        fa[h][s][i] = fragment<128, ASTR>(lds + buf * kBuf + h * kPart, s, ra + 16 * i);
+    };
+    auto read_b = [&](int buf, int h, int s, int j) {
+        fb[h][s][j] = fragment<128, BSTR>(lds + buf * kBuf + (2 + h) * kPart, s, rb + 16 * j);
+    };
+    auto barrier = [&]() {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    // one phase: quarter (ha, hb); `what` reads fragment n of the next
+    // group (8 of A if reads_a, else 4 of B), `copy` issues copy c;
+    // read_a_before: the phase before read 8 of A
+    auto phase = [&](int ha, int hb, bool reads_a, bool read_a_before, auto what, auto copy) {
+        constexpr int kA = ASTR ? 15 : 8, kB = BSTR ? 8 : 4;
+        if (read_a_before)        // lgkmcnt counts to 15
+            asm volatile("s_waitcnt vmcnt(10) lgkmcnt(%0)" ::"n"(kA) : "memory");
+        else
+            asm volatile("s_waitcnt vmcnt(10) lgkmcnt(%0)" ::"n"(kB) : "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        barrier();
+        constexpr int kMma = SPLIT ? 24 : 16;
+#pragma unroll
+        for (int n = 0; n < kMma; ++n) {
+            const int q = n / 8, i = n % 8 / 2, j = n % 2;
+            const int qa = SPLIT ? q == 1 : q, qb = SPLIT ? q == 2 : q;
+            acc[4 * ha + i][2 * hb + j] =
+                mma<OP>(fb[hb][qb][j], fa[ha][qa][i], acc[4 * ha + i][2 * hb + j]);
+            // B's fragments may replace the ones this phase uses: slab 0 from
+            // the last eight instructions on, slab 1 after them
+            if (reads_a ? n < 8 : n == kMma - 8 || n == kMma - 7) {
+                __builtin_amdgcn_sched_barrier(0);
+                what(reads_a ? n : n - (kMma - 8));
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (n == kMma - 6 || n == kMma - 3) {
+                __builtin_amdgcn_sched_barrier(0);
+                copy(n == kMma - 6 ? 0 : 1);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (!reads_a) {
+            what(2);
+            what(3);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+
+    // the first two steps; copies beyond the contraction fill LDS with
+    // zeros or values that no product takes
+    static_assert(SideA::kCopies == 2 && SideB::kCopies == 2, "two copies a phase");
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+            copy_a(t, 0, c);
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            copy_b(t, c >> 1, c & 1);
+        next_b();
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+            copy_a(t, 1, c);
+        next_a();
+    }
+    asm volatile("s_waitcnt vmcnt(10)" ::: "memory");
+    barrier();
+#pragma unroll
+    for (int n = 0; n < 8; ++n)
+        read_a(0, 0, n >> 2, n & 3);
+#pragma unroll
+    for (int n = 0; n < 4; ++n)
+        read_b(0, 0, n >> 1, n & 1);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    barrier();
+    for (int64_t s = w.s0; s < w.s1; ++s) {
+        const int cur = (int)(s - w.s0) & 1;
+        phase(0, 0, false, false, [&](int n) { read_b(cur, 1, n >> 1, n & 1); },
+              [&](int c) { copy_a(cur, 0, c); });
+        phase(0, 1, true, false, [&](int n) { read_a(cur, 1, n >> 2, n & 3); },
+              [&](int c) { copy_b(cur, 0, c); });
+        phase(1, 1, true, true, [&](int n) { read_a(cur ^ 1, 0, n >> 2, n & 3); },
+              [&](int c) { copy_b(cur, 1, c); });
+        next_b();
+        phase(1, 0, false, true, [&](int n) { read_b(cur ^ 1, 0, n >> 1, n & 1); },
+              [&](int c) { copy_a(cur, 1, c); });
+        next_a();
+    }
+    finish_tile<T, EPI>(a, w, acc, lds);
+}
+
+// The parts of the split tiles, added in order, then the epilogue.  A
+// workgroup takes one wave's staged piece of a tile.
+template <class T, int EPI>
+__global__ __launch_bounds__(64) void product_join_kernel(ProductArgs a, int tm, int tn, int tail)
+{
+    using St = Staging<T>;
+    __shared__ __attribute__((aligned(16))) float st[St::kFloats];
+    constexpr int kPieces = (T::kBM / St::kRows) * (T::kBN / St::kCols);
+    const int tile = a.whole + blockIdx.x / kPieces, piece = blockIdx.x % kPieces;
+    const int pr = piece / (T::kBN / St::kCols) * St::kRows, pc = piece % (T::kBN / St::kCols) * St::kCols;
+    int ti, tj;
+    const int each = EPI == kEpiSym ? tn * (tn + 1) / 2 : tm * tn;
+    const int64_t z = tile / each;
+    which_tile(tile % each, tm, tn, EPI == kEpiSym, ti, tj);
+    const int64_t row0 = (int64_t)ti * T::kBM + pr, col0 = (int64_t)tj * T::kBN + pc;
+    if (row0 >= a.M || col0 >= (EPI == kEpiSym ? (a.N + 63) / 64 * 64 : a.N))
         return;
-    const int64_t row = id / quads, col = (id % quads) * 4;
-    const bool lower = EPI == kEpiSym && row / tile > col / tile;
-    if (lower || (EPI != kEpiSym && col >= a.N))
-        return;                     // symmetric: written by the mirrored tile
-    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int s = 0; s < a.splits; ++s)
-        v += *reinterpret_cast<const f32x4 *>(
-            a.part + ((s * a.batch + z) * (int64_t)a.M + row) * n4 + col);
-    finish4<EPI>(a.e, z, row, col, a.M, a.N, v,
-                 EPI == kEpiSym && row / tile != col / tile);
+    const int64_t pitch = (int64_t)tail * T::kBM * T::kBN;         // between parts
+    const float *part = a.part + (int64_t)(tile - a.whole) * T::kBM * T::kBN + pr * T::kBN + pc;
+    constexpr int kQuads = St::kCols / 4;
+    for (int i = threadIdx.x; i < St::kRows * kQuads; i += 64) {
+        const int r = i / kQuads, c = i % kQuads * 4;
+        const float *p = part + r * T::kBN + c;
+        f32x4 v = *reinterpret_cast<const f32x4 *>(p);
+        for (int s = 1; s < a.splits; ++s)
+            v += *reinterpret_cast<const f32x4 *>(p + s * pitch);
+        *reinterpret_cast<f32x4 *>(st + r * St::kPitch + c) = v;
+    }
+    __syncthreads();
+    finish_block<St::kRows, St::kCols, EPI>(a.e, z, row0, col0, a.M, a.N, st,
+                                            EPI == kEpiSym && ti != tj);
 }
 
 // ------------------------------------------------------------------- host
-using TileL = Tile<2, 4, 8, 4>;      // 256 x 256, 8 waves
-using TileM = Tile<2, 2, 4, 4>;      // 128 x 128, 4 waves
-using TileS = Tile<2, 2, 2, 2>;      // 64 x 64, 4 waves
-
 template <class T, bool ASTR, bool BSTR, int OP, int EPI>
-hipError_t launch_tile(const ProductArgs &a, hipStream_t s)
+hipError_t launch_tile(const Plan &p, ProductArgs a, hipStream_t s)
 {
-    const int64_t tm = ((int64_t)a.M + T::kBM - 1) / T::kBM;
-    const int64_t tn = ((int64_t)(EPI == kEpiGated ? 2 * a.e.half : a.N) + T::kBN - 1) / T::kBN;
-    const int64_t tiles = EPI == kEpiSym ? tn * (tn + 1) / 2 : tm * tn;
-    if (tiles > 0x7fffffffll || a.batch > 65535 || a.splits > 65535)
-        return hipErrorInvalidValue;
-    product_kernel<T, ASTR, BSTR, OP, EPI>
-        <<<dim3((unsigned)tiles, (unsigned)a.batch, (unsigned)a.splits), T::kThreads, 0, s>>>(
-            a, (int)tm, (int)tn);
+    a.whole = (int)p.whole;
+    a.splits = p.splits;
+    const int64_t blocks = p.whole + p.tail * p.splits;
+    if constexpr (std::is_same<T, TileL>::value)
+        product_large_kernel<ASTR, BSTR, OP, EPI>
+            <<<(unsigned)blocks, T::kThreads, 0, s>>>(a, p.tm, p.tn);
+    else
+        product_kernel<T, ASTR, BSTR, OP, EPI>
+            <<<(unsigned)blocks, T::kThreads, 0, s>>>(a, p.tm, p.tn);
     hipError_t e = hipGetLastError();
-    if (e == hipSuccess && a.splits > 1) {
-        const int64_t quads = (int64_t)a.M * ((a.N + 63) / 64 * 64) / 4;
-        product_join_kernel<EPI><<<dim3((unsigned)((quads + 255) / 256), (unsigned)a.batch),
-                                   256, 0, s>>>(a, T::kBN);
+    if (e == hipSuccess && p.tail > 0) {
+        using St = Staging<T>;
+        constexpr int kPieces = (T::kBM / St::kRows) * (T::kBN / St::kCols);
+        product_join_kernel<T, EPI>
+            <<<(unsigned)(p.tail * kPieces), 64, 0, s>>>(a, p.tm, p.tn, (int)p.tail);
         e = hipGetLastError();
     }
     return e;
 }
 
-} // namespace
-
-// product.hip: the tile for a product (0 = large, 1 = middle, 2 = small)
-int product_tile(int M, int N, int64_t K, int batch, int op, bool sym);
-
-namespace {
-
 template <bool ASTR, bool BSTR, int OP, int EPI>
-hipError_t launch_any_tile(const ProductArgs &a, hipStream_t s)
+hipError_t launch_any_tile(const Plan &p, const ProductArgs &a, hipStream_t s)
 {
-    const int N = EPI == kEpiGated ? (int)(2 * a.e.half) : a.N;
-    switch (product_tile(a.M, N, a.K, a.batch, OP, EPI == kEpiSym)) {
+    switch (p.tile) {
     case 0:
-        return launch_tile<TileL, ASTR, BSTR, OP, EPI>(a, s);
+        return launch_tile<TileL, ASTR, BSTR, OP, EPI>(p, a, s);
     case 1:
-        return launch_tile<TileM, ASTR, BSTR, OP, EPI>(a, s);
+        return launch_tile<TileM, ASTR, BSTR, OP, EPI>(p, a, s);
     default:
-        return launch_tile<TileS, ASTR, BSTR, OP, EPI>(a, s);
+        return launch_tile<TileS, ASTR, BSTR, OP, EPI>(p, a, s);
     }
 }
 

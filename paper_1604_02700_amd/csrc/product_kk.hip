@@ -4,27 +4,28 @@
 
 namespace gpic {
 
-hipError_t launch_product_kk(int op, int epi, const ProductArgs &a, hipStream_t s)
+hipError_t launch_product_kk(int op, int epi, const Plan &p, const ProductArgs &a,
+                             hipStream_t s)
 {
     if (epi == kEpiLayer) {
         if (op == kOpBf16)
-            return launch_any_tile<false, false, kOpBf16, kEpiLayer>(a, s);
+            return launch_any_tile<false, false, kOpBf16, kEpiLayer>(p, a, s);
         if (op == kOpF16)
-            return launch_any_tile<false, false, kOpF16, kEpiLayer>(a, s);
-        return launch_any_tile<false, false, kOpSplit, kEpiLayer>(a, s);
+            return launch_any_tile<false, false, kOpF16, kEpiLayer>(p, a, s);
+        return launch_any_tile<false, false, kOpSplit, kEpiLayer>(p, a, s);
     }
     if (epi == kEpiGated) {
         if (op == kOpBf16)
-            return launch_any_tile<false, false, kOpBf16, kEpiGated>(a, s);
+            return launch_any_tile<false, false, kOpBf16, kEpiGated>(p, a, s);
         if (op == kOpF16)
-            return launch_any_tile<false, false, kOpF16, kEpiGated>(a, s);
-        return launch_any_tile<false, false, kOpSplit, kEpiGated>(a, s);
+            return launch_any_tile<false, false, kOpF16, kEpiGated>(p, a, s);
+        return launch_any_tile<false, false, kOpSplit, kEpiGated>(p, a, s);
     }
     if (epi == kEpiSym)
-        return op == kOpF16 ? launch_any_tile<false, false, kOpF16, kEpiSym>(a, s)
-                            : launch_any_tile<false, false, kOpSplit, kEpiSym>(a, s);
-    return op == kOpF16 ? launch_any_tile<false, false, kOpF16, kEpiUpdate>(a, s)
-                        : launch_any_tile<false, false, kOpSplit, kEpiUpdate>(a, s);
+        return op == kOpF16 ? launch_any_tile<false, false, kOpF16, kEpiSym>(p, a, s)
+                            : launch_any_tile<false, false, kOpSplit, kEpiSym>(p, a, s);
+    return op == kOpF16 ? launch_any_tile<false, false, kOpF16, kEpiUpdate>(p, a, s)
+                        : launch_any_tile<false, false, kOpSplit, kEpiUpdate>(p, a, s);
 }
 
 } // namespace gpic

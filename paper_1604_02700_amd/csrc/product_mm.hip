@@ -4,17 +4,18 @@
 
 namespace gpic {
 
-hipError_t launch_product_mm(int op, int epi, const ProductArgs &a, hipStream_t s)
+hipError_t launch_product_mm(int op, int epi, const Plan &p, const ProductArgs &a,
+                             hipStream_t s)
 {
     if (epi == kEpiLayer) {
         if (op == kOpBf16)
-            return launch_any_tile<true, true, kOpBf16, kEpiLayer>(a, s);
+            return launch_any_tile<true, true, kOpBf16, kEpiLayer>(p, a, s);
         if (op == kOpF16)
-            return launch_any_tile<true, true, kOpF16, kEpiLayer>(a, s);
-        return launch_any_tile<true, true, kOpSplit, kEpiLayer>(a, s);
+            return launch_any_tile<true, true, kOpF16, kEpiLayer>(p, a, s);
+        return launch_any_tile<true, true, kOpSplit, kEpiLayer>(p, a, s);
     }
-    return op == kOpF16 ? launch_any_tile<true, true, kOpF16, kEpiSym>(a, s)
-                        : launch_any_tile<true, true, kOpSplit, kEpiSym>(a, s);
+    return op == kOpF16 ? launch_any_tile<true, true, kOpF16, kEpiSym>(p, a, s)
+                        : launch_any_tile<true, true, kOpSplit, kEpiSym>(p, a, s);
 }
 
 } // namespace gpic
