@@ -82,6 +82,25 @@ __device__ __forceinline__ void activate_grad(float z, int act, float &a, float 
     }
 }
 
+// eight values at once: one choice of the function for all of them
+__device__ __forceinline__ f32x8 activate8(f32x8 z, int act)
+{
+    if (act == GPIC_ACT_RELU) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            z[j] = activate(z[j], GPIC_ACT_RELU);
+    } else if (act == GPIC_ACT_GELU) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            z[j] = activate(z[j], GPIC_ACT_GELU);
+    } else if (act == GPIC_ACT_SILU) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            z[j] = activate(z[j], GPIC_ACT_SILU);
+    }
+    return z;
+}
+
 // ------------------------------------------------- typed loads and stores
 __device__ __forceinline__ float load1(const void *p, int64_t i, int dtype)
 {
@@ -233,6 +252,13 @@ hipError_t run_layer(const Shape &s, bool gated, const void *X, const void *W,
 hipError_t run_layer_backward(const Shape &s, bool gated, const void *dY, const void *X,
                               const void *W, const void *Z, void *dX, void *dW, void *db,
                               void *ws, hipStream_t st);
+
+// ---------------------------------------------------------------- rows.hip
+// The forward layer of few rows, straight from the operands as they lie
+// (any pitch and alignment, no workspace).
+constexpr int kFewRows = 32;
+hipError_t run_few_rows(const Shape &s, bool gated, const void *X, const void *W,
+                        const void *bias, const void *res, void *Y, void *Z, hipStream_t st);
 
 // ------------------------------------------------------ orthogonalize.hip
 struct Polar {

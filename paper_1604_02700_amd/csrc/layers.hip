@@ -190,7 +190,7 @@ __global__ __launch_bounds__(256) void pack_kernel(PackJobs jobs)
 struct GradArgs {
     const void *dY, *Z;
     int64_t ldy, ldz, n, m;
-    int dtype, ztype, act, gated;
+    int act;
     void *dZ;              // null: only the column sums
     int64_t ldd;           // row pitch of dZ in 16-bit values
     int vec;               // four columns at once
@@ -214,10 +214,11 @@ __device__ __forceinline__ f32x4 read4(const void *p, int64_t row_at, int64_t co
 
 // four values of dZ from column col on (`end`: no column of this half lies
 // at or beyond it)
+template <int DT>
 __device__ __forceinline__ void write4(const GradArgs &a, int64_t row, int64_t col, int64_t end,
                                        f32x4 v, float s)
 {
-    const bool split = a.dtype == GPIC_F32;
+    const bool split = DT == GPIC_F32;
     if (split) {
         _Float16 *d = static_cast<_Float16 *>(a.dZ) + row * a.ldd;
         half4 h, l;
@@ -242,20 +243,22 @@ __device__ __forceinline__ void write4(const GradArgs &a, int64_t row, int64_t c
         return;
     }
     if ((col & 3) == 0 && col + 4 <= end) {
-        store4(a.dZ, row * a.ldd + col, v * s, a.dtype);
+        store4(a.dZ, row * a.ldd + col, v * s, DT);
     } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
             if (col + j < end)
-                store1(a.dZ, row * a.ldd + col + j, v[j] * s, a.dtype);
+                store1(a.dZ, row * a.ldd + col + j, v[j] * s, DT);
     }
 }
 
 // dZ of 64 rows x 256 columns a workgroup (four rows at a time, four
 // columns a thread) and their column sums, in float32 in a fixed order.
 // Memory-bound: reads dY and Z, writes dZ once.
+template <int DT, int ACT, bool GATED>
 __global__ __launch_bounds__(256) void grad_kernel(GradArgs a)
 {
+    constexpr int ZT = GATED ? GPIC_F32 : DT;      // the type of Z
     float s = 1.0f;
     if (a.scale) {
         // |act'| <= 1.13, and the gated forms multiply by |Z| or |act(Z)| <= |Z|
@@ -272,52 +275,52 @@ __global__ __launch_bounds__(256) void grad_kernel(GradArgs a)
     f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
     // the padding of dZ's rows (zeros): a layer's columns m .. end, the
     // gated layer's 2 m .. end
-    const int64_t all = a.gated ? 2 * a.m : a.m;
-    const int64_t width = a.dtype == GPIC_F32 ? (all + 31) / 32 * 32 : up64(all);
-    const int64_t end = a.gated ? a.m : width;
+    const int64_t all = GATED ? 2 * a.m : a.m;
+    const int64_t width = DT == GPIC_F32 ? (all + 31) / 32 * 32 : up64(all);
+    const int64_t end = GATED ? a.m : width;
     for (int64_t r = r0 + (threadIdx.x >> 6); r < r1; r += 4) {
         if (col < a.m) {
-            const f32x4 dy = read4(a.dY, r * a.ldy, col, a.m, a.dtype, a.vec);
+            const f32x4 dy = read4(a.dY, r * a.ldy, col, a.m, DT, a.vec);
             f32x4 d = dy;
-            if (a.gated) {
-                const f32x4 g = read4(a.Z, r * a.ldz, col, a.m, a.ztype, a.vec);
-                const f32x4 u = read4(a.Z, r * a.ldz + a.m, col, a.m, a.ztype, a.vec);
+            if (GATED) {
+                const f32x4 g = read4(a.Z, r * a.ldz, col, a.m, ZT, a.vec);
+                const f32x4 u = read4(a.Z, r * a.ldz + a.m, col, a.m, ZT, a.vec);
                 f32x4 du;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     float y, dy1;
-                    activate_grad(g[j], a.act, y, dy1);
+                    activate_grad(g[j], ACT, y, dy1);
                     d[j] = dy[j] * u[j] * dy1;
                     du[j] = dy[j] * y;
                 }
-                write4(a, r, col, a.m, d, s);
-                write4(a, r, a.m + col, 2 * a.m, du, s);
+                write4<DT>(a, r, col, a.m, d, s);
+                write4<DT>(a, r, a.m + col, 2 * a.m, du, s);
             } else {
-                if (a.act != GPIC_ACT_NONE) {
-                    const f32x4 z = read4(a.Z, r * a.ldz, col, a.m, a.ztype, a.vec);
+                if (ACT != GPIC_ACT_NONE) {
+                    const f32x4 z = read4(a.Z, r * a.ldz, col, a.m, ZT, a.vec);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         float y, dy1;
-                        activate_grad(z[j], a.act, y, dy1);
+                        activate_grad(z[j], ACT, y, dy1);
                         d[j] = dy[j] * dy1;
                     }
                     // beyond the last column z and dy are 0, and d too
                 }
                 if (a.dZ)
-                    write4(a, r, col, end, d, s);
+                    write4<DT>(a, r, col, end, d, s);
                 sum += d;
             }
-        } else if (a.dZ && !a.gated && col < end) {
-            write4(a, r, col, end, f32x4{0.0f, 0.0f, 0.0f, 0.0f}, s);
+        } else if (a.dZ && !GATED && col < end) {
+            write4<DT>(a, r, col, end, f32x4{0.0f, 0.0f, 0.0f, 0.0f}, s);
         }
         // the thread at the gate's last column also writes the padding
-        if (a.gated && col < a.m && col + 4 >= a.m)
+        if (GATED && col < a.m && col + 4 >= a.m)
             for (int64_t c = all; c < width; ++c) {
-                if (a.dtype == GPIC_F32) {
+                if (DT == GPIC_F32) {
                     _Float16 *d = static_cast<_Float16 *>(a.dZ) + r * a.ldd + split_at(c);
                     d[0] = d[32] = (_Float16)0.0f;
                 } else {
-                    store1(a.dZ, r * a.ldd + c, 0.0f, a.dtype);
+                    store1(a.dZ, r * a.ldd + c, 0.0f, DT);
                 }
             }
     }
@@ -432,6 +435,31 @@ hipError_t launch_pack(const Source *const *list, int count, int dtype, hipStrea
     return hipGetLastError();
 }
 
+template <int DT, bool GATED>
+hipError_t launch_grad_act(const GradArgs &g, dim3 grid, hipStream_t st)
+{
+    switch (g.act) {
+    case GPIC_ACT_NONE:
+        grad_kernel<DT, GPIC_ACT_NONE, GATED><<<grid, 256, 0, st>>>(g);
+        break;
+    case GPIC_ACT_RELU:
+        grad_kernel<DT, GPIC_ACT_RELU, GATED><<<grid, 256, 0, st>>>(g);
+        break;
+    case GPIC_ACT_GELU:
+        grad_kernel<DT, GPIC_ACT_GELU, GATED><<<grid, 256, 0, st>>>(g);
+        break;
+    default:
+        grad_kernel<DT, GPIC_ACT_SILU, GATED><<<grid, 256, 0, st>>>(g);
+    }
+    return hipGetLastError();
+}
+
+template <int DT>
+hipError_t launch_grad(const GradArgs &g, bool gated, dim3 grid, hipStream_t st)
+{
+    return gated ? launch_grad_act<DT, true>(g, grid, st) : launch_grad_act<DT, false>(g, grid, st);
+}
+
 int kind_of(int dtype)
 {
     return dtype == GPIC_F32 ? kOpSplit : (dtype == GPIC_F16 ? kOpF16 : kOpBf16);
@@ -451,10 +479,12 @@ bool quads(const void *p, int64_t ld, int dtype)
 
 // What a forward call keeps in its workspace.
 struct Forward {
-    Source X, W;
-    float *part;
+    Source X{}, W{};
+    float *part = nullptr;
     Forward(const Shape &s, bool gated, const void *x, const void *w, Cursor &c)
     {
+        if (s.n <= kFewRows)
+            return;
         const int64_t rows = gated ? 2 * s.m : s.m;
         X = Source{x, s.n, s.k, s.ldx, must_pack(s.dtype, s.k, s.ldx, s.aligned16)};
         W = Source{w, rows, s.k, s.ldw, must_pack(s.dtype, s.k, s.ldw, s.aligned16)};
@@ -527,6 +557,8 @@ hipError_t run_layer(const Shape &s, bool gated, const void *X, const void *W, c
 {
     if (s.n == 0)
         return hipSuccess;
+    if (s.n <= kFewRows)
+        return run_few_rows(s, gated, X, W, bias, res, Y, Z, st);
     Cursor c{static_cast<char *>(ws)};
     Forward f(s, gated, X, W, c);
     const Source *list[2] = {&f.X, &f.W};
@@ -608,10 +640,7 @@ hipError_t run_layer_backward(const Shape &s, bool gated, const void *dY, const 
         g.ldz = s.ldz;
         g.n = s.n;
         g.m = s.m;
-        g.dtype = s.dtype;
-        g.ztype = ztype;
         g.act = s.act;
-        g.gated = gated;
         g.dZ = b.form && need_dz ? b.dZ.to : nullptr;
         g.ldd = s.dtype == GPIC_F32 ? split_ld(b.rows) : up64(b.rows);
         g.vec = quads(dY, s.ldy, s.dtype) &&
@@ -624,10 +653,11 @@ hipError_t run_layer_backward(const Shape &s, bool gated, const void *dY, const 
             g.scale = b.scale;
         }
         const int64_t width = gated ? s.m : up64(s.m);
-        grad_kernel<<<dim3((unsigned)((s.n + kSumRows - 1) / kSumRows),
-                           (unsigned)((width + 255) / 256)),
-                      256, 0, st>>>(g);
-        RUN(hipGetLastError());
+        const dim3 grid((unsigned)((s.n + kSumRows - 1) / kSumRows),
+                        (unsigned)((width + 255) / 256));
+        RUN(s.dtype == GPIC_F32    ? launch_grad<GPIC_F32>(g, gated, grid, st)
+            : s.dtype == GPIC_F16 ? launch_grad<GPIC_F16>(g, gated, grid, st)
+                                  : launch_grad<GPIC_BF16>(g, gated, grid, st));
     }
     if (db) {
         sum_parts_kernel<<<(unsigned)((s.m + 63) / 64), 256, 0, st>>>(

@@ -302,22 +302,36 @@ __device__ __forceinline__ f32x8 staged(const float *p, Factor f)
     return *reinterpret_cast<const f32x8 *>(p) * f.a * f.b;
 }
 
+// The type of what an epilogue reads and writes, known from the operands
+// where it can be (orthogonalised matrices of half-precision operands are
+// bfloat16, those of split ones float32 or float16).
+template <int OP, int EPI>
+__device__ __forceinline__ int out_type(const Epilogue &e)
+{
+    if (EPI == kEpiUpdate)
+        return OP == kOpF16 ? GPIC_BF16 : (e.dtype == GPIC_F32 ? GPIC_F32 : GPIC_F16);
+    return OP == kOpSplit ? GPIC_F32 : (OP == kOpF16 ? GPIC_F16 : GPIC_BF16);
+}
+
 // Finishes `ROWS` x `COLS` accumulators that the wave has staged at `st`
 // (pitch COLS + 4 floats), the output's rows from row0, columns from col0
 // (gated: columns from col0 / 2).  mirror (kEpiSym): the transposed block too.
-template <int ROWS, int COLS, int EPI>
+template <int ROWS, int COLS, int OP, int EPI>
 __device__ __forceinline__ void finish_block(const Epilogue &e, int64_t z, int64_t row0,
                                              int64_t col0, int64_t M, int64_t N, float *st,
                                              bool mirror)
 {
     // the whole and the partial accesses round alike
 #pragma clang fp contract(off)
+    const int dtype = out_type<OP, EPI>(e);
     constexpr int kPitch = COLS + 4;
     constexpr int kOut = EPI == kEpiGated ? COLS / 2 : COLS;     // output columns
-    constexpr int kLanes = kOut / 8, kRowsPass = 64 / kLanes, kPasses = ROWS / kRowsPass;
+    constexpr int kLanes = kOut / 8, kRowsPass = 64 / kLanes < ROWS ? 64 / kLanes : ROWS;
+    constexpr int kPasses = ROWS / kRowsPass;            // lanes beyond the rows do nothing
     constexpr int kGroup = kPasses < 2 ? kPasses : 2;            // rows in flight a lane
     static_assert(kPasses * kRowsPass == ROWS && kPasses % kGroup == 0, "passes");
     const int lane = threadIdx.x & 63, q = lane % kLanes, r0 = lane / kLanes;
+    const bool idle = kLanes * kRowsPass < 64 && r0 >= kRowsPass;
     const Factor f = factor_of(e);
     if (EPI == kEpiGated) {
         const int64_t col = col0 / 2 + q * 8, half = e.half;
@@ -327,7 +341,7 @@ __device__ __forceinline__ void finish_block(const Epilogue &e, int64_t z, int64
         for (int p = 0; p < kPasses; ++p) {
             const int r = p * kRowsPass + r0;
             const int64_t row = row0 + r;
-            if (valid <= 0 || row >= M)
+            if (valid <= 0 || row >= M || idle)
                 continue;
             f32x8 g = staged(src + r * kPitch, f);
             const f32x8 u = staged(src + r * kPitch + 16, f);
@@ -335,10 +349,7 @@ __device__ __forceinline__ void finish_block(const Epilogue &e, int64_t z, int64
                 store8(e.pre, row * e.ldz + col, g, GPIC_F32, valid, whole);
                 store8(e.pre, row * e.ldz + half + col, u, GPIC_F32, valid, whole);
             }
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                g[j] = activate(g[j], e.act) * u[j];
-            store8(e.out, row * e.ldo + col, g, e.dtype, valid, whole);
+            store8(e.out, row * e.ldo + col, activate8(g, e.act) * u, dtype, valid, whole);
         }
         return;
     }
@@ -350,24 +361,24 @@ __device__ __forceinline__ void finish_block(const Epilogue &e, int64_t z, int64
     const bool whole = e.vec && valid == 8;
     f32x8 bias = 0.0f;
     if (EPI == kEpiLayer && e.bias && valid > 0)
-        bias = load8(e.bias, col, e.dtype, valid, whole);
+        bias = load8(e.bias, col, dtype, valid, whole);
     for (int p0 = 0; p0 < kPasses; p0 += kGroup) {
         f32x8 v[kGroup], c[kGroup];
 #pragma unroll
         for (int p = 0; p < kGroup; ++p) {
             const int r = (p0 + p) * kRowsPass + r0;
             const int64_t row = row0 + r;
-            v[p] = staged(st + r * kPitch + q * 8, f);
+            v[p] = staged(st + (idle ? 0 : r) * kPitch + q * 8, f);
             c[p] = 0.0f;
-            if (valid <= 0 || row >= M)
+            if (valid <= 0 || row >= M || idle)
                 continue;
             if (EPI == kEpiLayer && e.res)
-                c[p] = load8(e.res, row * e.ldr + col, e.dtype, valid, whole);
+                c[p] = load8(e.res, row * e.ldr + col, dtype, valid, whole);
             if (EPI == kEpiUpdate || (EPI == kEpiSym && e.c_hi))
                 c[p] = load_parts(e, part_at(e, z, row, col)) * e.beta;
             if (EPI == kEpiUpdate && e.is_step) {
                 // decay W - step (beta X + acc)
-                const f32x8 old = load8(e.out, z * e.batch_o + row * e.ldo + col, e.dtype, valid,
+                const f32x8 old = load8(e.out, z * e.batch_o + row * e.ldo + col, dtype, valid,
                                         whole);
                 c[p] = old * e.decay - c[p] * e.step;
                 v[p] = v[p] * -e.step;
@@ -377,20 +388,18 @@ __device__ __forceinline__ void finish_block(const Epilogue &e, int64_t z, int64
         for (int p = 0; p < kGroup; ++p) {
             const int r = (p0 + p) * kRowsPass + r0;
             const int64_t row = row0 + r;
-            if (valid <= 0 || row >= M)
+            if (valid <= 0 || row >= M || idle)
                 continue;
             f32x8 x = v[p];
             if (EPI == kEpiLayer) {
                 if (e.bias)
                     x = x + bias;
                 if (e.pre)
-                    store8(e.pre, row * e.ldz + col, x, e.dtype, valid, whole);
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    x[j] = activate(x[j], e.act);
+                    store8(e.pre, row * e.ldz + col, x, dtype, valid, whole);
+                x = activate8(x, e.act);
                 if (e.res)
                     x = x + c[p];
-                store8(e.out, row * e.ldo + col, x, e.dtype, valid, whole);
+                store8(e.out, row * e.ldo + col, x, dtype, valid, whole);
             } else if (EPI == kEpiSym) {
                 x = (x + c[p]) * e.store_scale;
                 store_parts(e, part_at(e, z, row, col), x);
@@ -402,7 +411,7 @@ __device__ __forceinline__ void finish_block(const Epilogue &e, int64_t z, int64
                     store_parts(e, part_at(e, z, row, col), x * e.store_scale);
                     continue;
                 }
-                store8(e.out, z * e.batch_o + row * e.ldo + col, x, e.dtype, valid, whole);
+                store8(e.out, z * e.batch_o + row * e.ldo + col, x, dtype, valid, whole);
             }
         }
     }
@@ -519,7 +528,7 @@ struct Staging {
 };
 
 // A wave's accumulators to their place: the epilogue, or the partial sums.
-template <class T, int EPI>
+template <class T, int OP, int EPI>
 __device__ __forceinline__ void finish_tile(const ProductArgs &a, const Work &w,
                                             f32x4 (&acc)[T::kRM][T::kRN], char *lds)
 {
@@ -549,7 +558,7 @@ __device__ __forceinline__ void finish_tile(const ProductArgs &a, const Work &w,
                     *reinterpret_cast<const f32x4 *>(st + r * St::kPitch + c);
             }
         } else {
-            finish_block<St::kRows, St::kCols, EPI>(
+            finish_block<St::kRows, St::kCols, OP, EPI>(
                 a.e, w.z, (int64_t)w.ti * T::kBM + wm + 16 * i0, (int64_t)w.tj * T::kBN + wn, a.M,
                 a.N, st, EPI == kEpiSym && w.ti != w.tj);
         }
@@ -663,7 +672,7 @@ __global__ __launch_bounds__(T::kThreads) void product_kernel(ProductArgs a, int
         }
     }
 
-    finish_tile<T, EPI>(a, w, acc, lds);
+    finish_tile<T, OP, EPI>(a, w, acc, lds);
 }
 
 // The 256 x 256 tile: 8 waves of 128 x 64, two to a SIMD.  A step is four
@@ -838,39 +847,43 @@ __global__ __launch_bounds__(512) void product_large_kernel(ProductArgs a, int t
               [&](int c) { copy_a(cur, 1, c); });
         next_a();
     }
-    finish_tile<T, EPI>(a, w, acc, lds);
+    finish_tile<T, OP, EPI>(a, w, acc, lds);
 }
 
-// The parts of the split tiles, added in order, then the epilogue.  A
-// workgroup takes one wave's staged piece of a tile.
-template <class T, int EPI>
+// The parts of the split tiles, added in order, then the epilogue.  A wave
+// takes 16 rows of one wave's columns: few tiles have many parts, so the
+// pieces are small and eight parts' loads are in flight.
+constexpr int kJoinRows = 16;
+
+template <class T, int OP, int EPI>
 __global__ __launch_bounds__(64) void product_join_kernel(ProductArgs a, int tm, int tn, int tail)
 {
-    using St = Staging<T>;
-    __shared__ __attribute__((aligned(16))) float st[St::kFloats];
-    constexpr int kPieces = (T::kBM / St::kRows) * (T::kBN / St::kCols);
+    constexpr int kCols = Staging<T>::kCols, kPitch = Staging<T>::kPitch;
+    __shared__ __attribute__((aligned(16))) float st[kJoinRows * kPitch];
+    constexpr int kAcross = T::kBN / kCols, kPieces = T::kBM / kJoinRows * kAcross;
     const int tile = a.whole + blockIdx.x / kPieces, piece = blockIdx.x % kPieces;
-    const int pr = piece / (T::kBN / St::kCols) * St::kRows, pc = piece % (T::kBN / St::kCols) * St::kCols;
+    const int pr = piece / kAcross * kJoinRows, pc = piece % kAcross * kCols;
     int ti, tj;
     const int each = EPI == kEpiSym ? tn * (tn + 1) / 2 : tm * tn;
     const int64_t z = tile / each;
     which_tile(tile % each, tm, tn, EPI == kEpiSym, ti, tj);
     const int64_t row0 = (int64_t)ti * T::kBM + pr, col0 = (int64_t)tj * T::kBN + pc;
-    if (row0 >= a.M || col0 >= (EPI == kEpiSym ? (a.N + 63) / 64 * 64 : a.N))
+    if (row0 >= a.M || col0 >= (EPI == kEpiSym ? ((int64_t)a.N + 63) / 64 * 64 : a.N))
         return;
     const int64_t pitch = (int64_t)tail * T::kBM * T::kBN;         // between parts
     const float *part = a.part + (int64_t)(tile - a.whole) * T::kBM * T::kBN + pr * T::kBN + pc;
-    constexpr int kQuads = St::kCols / 4;
-    for (int i = threadIdx.x; i < St::kRows * kQuads; i += 64) {
+    constexpr int kQuads = kCols / 4;
+    for (int i = threadIdx.x; i < kJoinRows * kQuads; i += 64) {
         const int r = i / kQuads, c = i % kQuads * 4;
         const float *p = part + r * T::kBN + c;
         f32x4 v = *reinterpret_cast<const f32x4 *>(p);
+#pragma unroll 8
         for (int s = 1; s < a.splits; ++s)
             v += *reinterpret_cast<const f32x4 *>(p + s * pitch);
-        *reinterpret_cast<f32x4 *>(st + r * St::kPitch + c) = v;
+        *reinterpret_cast<f32x4 *>(st + r * kPitch + c) = v;
     }
     __syncthreads();
-    finish_block<St::kRows, St::kCols, EPI>(a.e, z, row0, col0, a.M, a.N, st,
+    finish_block<kJoinRows, kCols, OP, EPI>(a.e, z, row0, col0, a.M, a.N, st,
                                             EPI == kEpiSym && ti != tj);
 }
 
@@ -889,9 +902,8 @@ hipError_t launch_tile(const Plan &p, ProductArgs a, hipStream_t s)
             <<<(unsigned)blocks, T::kThreads, 0, s>>>(a, p.tm, p.tn);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && p.tail > 0) {
-        using St = Staging<T>;
-        constexpr int kPieces = (T::kBM / St::kRows) * (T::kBN / St::kCols);
-        product_join_kernel<T, EPI>
+        constexpr int kPieces = T::kBM / kJoinRows * (T::kBN / Staging<T>::kCols);
+        product_join_kernel<T, OP, EPI>
             <<<(unsigned)(p.tail * kPieces), 64, 0, s>>>(a, p.tm, p.tn, (int)p.tail);
         e = hipGetLastError();
     }
