@@ -121,18 +121,23 @@ __device__ __forceinline__ void store1(void *p, int64_t i, float v, int dtype)
         static_cast<__bf16 *>(p)[i] = (__bf16)v;
 }
 
-// four consecutive values, p + i aligned to four of them
+// four consecutive values at any alignment (the card's 16-byte accesses
+// need none)
 __device__ __forceinline__ f32x4 load4(const void *p, int64_t i, int dtype)
 {
+    using f = float __attribute__((ext_vector_type(4), aligned(4)));
+    using h = _Float16 __attribute__((ext_vector_type(4), aligned(2)));
+    using b = __bf16 __attribute__((ext_vector_type(4), aligned(2)));
     if (dtype == GPIC_F32)
-        return *reinterpret_cast<const f32x4 *>(static_cast<const float *>(p) + i);
+        return *reinterpret_cast<const f *>(static_cast<const float *>(p) + i);
     if (dtype == GPIC_F16)
         return __builtin_convertvector(
-            *reinterpret_cast<const half4 *>(static_cast<const _Float16 *>(p) + i), f32x4);
+            *reinterpret_cast<const h *>(static_cast<const _Float16 *>(p) + i), f32x4);
     return __builtin_convertvector(
-        *reinterpret_cast<const bf4 *>(static_cast<const __bf16 *>(p) + i), f32x4);
+        *reinterpret_cast<const b *>(static_cast<const __bf16 *>(p) + i), f32x4);
 }
 
+// the same, stored; p + i aligned to four values
 __device__ __forceinline__ void store4(void *p, int64_t i, f32x4 v, int dtype)
 {
     if (dtype == GPIC_F32)
@@ -173,7 +178,11 @@ struct Operand {
     int64_t cols;      // 16-bit values of a row that may be read
 };
 
-enum { kEpiLayer = 0, kEpiGated = 1, kEpiSym = 2, kEpiUpdate = 3 };
+// kEpiGram: P = acc; kEpiPoly: P = beta C + acc, both over the upper triangle
+// of tiles and mirrored, C and P symmetric; kEpiUpdate: X' = beta X + acc;
+// kEpiResult: the same as a result (or, is_step, weights moved by it)
+enum { kEpiLayer = 0, kEpiGated = 1, kEpiGram = 2, kEpiPoly = 3, kEpiUpdate = 4, kEpiResult = 5 };
+__host__ __device__ constexpr bool symmetric(int epi) { return epi == kEpiGram || epi == kEpiPoly; }
 
 struct Epilogue {
     // operand scales: acc is divided by their product (device pointers to
@@ -185,22 +194,17 @@ struct Epilogue {
     void *out, *pre;
     int64_t ldr, ldo, ldz;
     int dtype, act;
-    int vec;           // four consecutive columns may be moved at once
     int64_t half;      // gated: columns of one half
-    // kEpiSym: P = beta * C + gamma * acc over the upper triangle of tiles,
-    // mirrored, C and P symmetric r x r; kEpiUpdate: X' = beta * X + acc.
-    // 16-bit parts of C, P (X, X'): split matrices (lo = null), or a hi
-    // matrix and, where lo is given, a lo matrix of the same pitch.
+    // C, P, X, X' as 16-bit parts: split matrices, or for single operands
+    // a matrix of high halves and (X, X') one of low halves of the same pitch
     float beta;
     const void *c_hi, *c_lo;
     void *p_hi, *p_lo;
     int64_t ldp, batch_p;      // of C, P, X, X' (16-bit values)
     float store_scale;         // P, X' are stored times this
     float load_scale;          // C, X are multiplied by this when read
-    int is_split;
-    // kEpiUpdate's last product: out (dtype, ldo) = beta X + acc, or, with
-    // weights, out = decay * out - step * (beta X + acc)
-    int to_out, is_step;
+    // kEpiResult: out = beta X + acc, or out = decay out - step (beta X + acc)
+    int is_step;
     float decay, step;
     int64_t batch_o;
 };

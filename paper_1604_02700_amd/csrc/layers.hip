@@ -47,7 +47,7 @@ __global__ __launch_bounds__(256) void absmax_kernel(MaxJobs jobs)
     const MaxJob m = jobs.j[blockIdx.y];
     const int64_t total = m.rows * m.cols, stride = (int64_t)gridDim.x * 256;
     float best = 0.0f;
-    if (m.ld == m.cols && ((uintptr_t)m.x & 15) == 0) {
+    if (m.ld == m.cols) {
         const int64_t quads = total / 4;
         for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < quads; i += stride) {
             const f32x4 v = load4(m.x, i * 4, m.dtype);
@@ -141,16 +141,14 @@ __global__ __launch_bounds__(256) void pack_kernel(PackJobs jobs)
     }
     const int64_t width = SPLIT ? (m.cols + 31) / 32 * 32 : up64(m.cols);
     const int64_t groups = width / 8, total = m.rows * groups;
-    const bool vec = SPLIT && (m.ld & 3) == 0 && ((uintptr_t)m.x & 15) == 0;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total;
          i += (int64_t)gridDim.x * 256) {
         const int64_t r = i / groups, c = (i - r * groups) * 8;
         if (SPLIT) {
             const float *x = static_cast<const float *>(m.x) + r * m.ld + c;
             float v[8];
-            if (vec && c + 8 <= m.cols) {
-                const f32x4 a = reinterpret_cast<const f32x4 *>(x)[0];
-                const f32x4 b = reinterpret_cast<const f32x4 *>(x)[1];
+            if (c + 8 <= m.cols) {
+                const f32x4 a = load4(x, 0, GPIC_F32), b = load4(x, 4, GPIC_F32);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     v[k] = a[k];
@@ -178,9 +176,14 @@ __global__ __launch_bounds__(256) void pack_kernel(PackJobs jobs)
                 unsigned short h[8];
                 u32x4 v;
             } u;
+            using any = u32x4 __attribute__((aligned(2)));
+            if (c + 8 <= m.cols) {
+                u.v = *reinterpret_cast<const any *>(x);
+            } else {
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                u.h[k] = c + k < m.cols ? x[k] : (unsigned short)0;
+                for (int k = 0; k < 8; ++k)
+                    u.h[k] = c + k < m.cols ? x[k] : (unsigned short)0;
+            }
             *reinterpret_cast<u32x4 *>(static_cast<unsigned short *>(m.to) + r * width + c) = u.v;
         }
     }
@@ -193,16 +196,15 @@ struct GradArgs {
     int act;
     void *dZ;              // null: only the column sums
     int64_t ldd;           // row pitch of dZ in 16-bit values
-    int vec;               // four columns at once
     float *sums;           // [ceil(n / 64)][m] partial column sums, or null
     const float *max_dy, *max_z;     // partial maxima (Z: gated only)
     float *scale;          // dZ is stored times this; null: 1
 };
 
 __device__ __forceinline__ f32x4 read4(const void *p, int64_t row_at, int64_t col, int64_t cols,
-                                       int dtype, bool vec)
+                                       int dtype)
 {
-    if (vec && col + 4 <= cols)
+    if (col + 4 <= cols)
         return load4(p, row_at + col, dtype);
     f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
@@ -280,11 +282,11 @@ __global__ __launch_bounds__(256) void grad_kernel(GradArgs a)
     const int64_t end = GATED ? a.m : width;
     for (int64_t r = r0 + (threadIdx.x >> 6); r < r1; r += 4) {
         if (col < a.m) {
-            const f32x4 dy = read4(a.dY, r * a.ldy, col, a.m, DT, a.vec);
+            const f32x4 dy = read4(a.dY, r * a.ldy, col, a.m, DT);
             f32x4 d = dy;
             if (GATED) {
-                const f32x4 g = read4(a.Z, r * a.ldz, col, a.m, ZT, a.vec);
-                const f32x4 u = read4(a.Z, r * a.ldz + a.m, col, a.m, ZT, a.vec);
+                const f32x4 g = read4(a.Z, r * a.ldz, col, a.m, ZT);
+                const f32x4 u = read4(a.Z, r * a.ldz + a.m, col, a.m, ZT);
                 f32x4 du;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
@@ -297,7 +299,7 @@ __global__ __launch_bounds__(256) void grad_kernel(GradArgs a)
                 write4<DT>(a, r, a.m + col, 2 * a.m, du, s);
             } else {
                 if (ACT != GPIC_ACT_NONE) {
-                    const f32x4 z = read4(a.Z, r * a.ldz, col, a.m, ZT, a.vec);
+                    const f32x4 z = read4(a.Z, r * a.ldz, col, a.m, ZT);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         float y, dy1;
@@ -340,22 +342,24 @@ __global__ __launch_bounds__(256) void grad_kernel(GradArgs a)
 }
 
 // Column sums from the partial ones, in float64 in a fixed order: 64
-// columns a workgroup, four runs of parts.
-__global__ __launch_bounds__(256) void sum_parts_kernel(const float *sums, int64_t parts, int64_t m,
-                                                        void *db, int dtype)
+// columns a workgroup, sixteen runs of parts.
+__global__ __launch_bounds__(1024) void sum_parts_kernel(const float *sums, int64_t parts, int64_t m,
+                                                         void *db, int dtype)
 {
-    const int64_t col = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
-    const int w = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int64_t col = (int64_t)blockIdx.x * 64 + lane;
     double t = 0.0;
-    if (col < m)
-        for (int64_t p = w; p < parts; p += 4)
+    if (col < m) {
+#pragma unroll 8
+        for (int64_t p = w; p < parts; p += 16)
             t += (double)sums[p * m + col];
-    __shared__ double part[256];
-    part[threadIdx.x] = t;
+    }
+    __shared__ double part[16][64];
+    part[w][lane] = t;
     __syncthreads();
     if (w == 0 && col < m) {
-        t = ((part[threadIdx.x] + part[threadIdx.x + 64]) + part[threadIdx.x + 128]) +
-            part[threadIdx.x + 192];
+        for (int i = 1; i < 16; ++i)
+            t += part[i][lane];
         store1(db, col, (float)t, dtype);
     }
 }
@@ -463,18 +467,6 @@ hipError_t launch_grad(const GradArgs &g, bool gated, dim3 grid, hipStream_t st)
 int kind_of(int dtype)
 {
     return dtype == GPIC_F32 ? kOpSplit : (dtype == GPIC_F16 ? kOpF16 : kOpBf16);
-}
-
-// eight values at once (sixteen bytes of 16-bit values)
-bool eights(const void *p, int64_t ld, int dtype)
-{
-    return p == nullptr || (ld % (dtype == GPIC_F32 ? 4 : 8) == 0 && (uintptr_t)p % 16 == 0);
-}
-
-bool quads(const void *p, int64_t ld, int dtype)
-{
-    const uintptr_t bytes = dtype == GPIC_F32 ? 16 : 8;
-    return p == nullptr || (ld % 4 == 0 && (uintptr_t)p % bytes == 0);
 }
 
 // What a forward call keeps in its workspace.
@@ -591,8 +583,6 @@ hipError_t run_layer(const Shape &s, bool gated, const void *X, const void *W, c
     e.dtype = s.dtype;
     e.act = s.act;
     e.half = s.m;
-    e.vec = eights(Y, s.ldy, s.dtype) && eights(Z, s.ldz, gated ? GPIC_F32 : s.dtype) &&
-            eights(res, s.ldr, s.dtype) && eights(bias, 8, s.dtype) && (!gated || s.m % 8 == 0);
     return launch_product(kKK, kind_of(s.dtype), gated ? kEpiGated : kEpiLayer, a, st);
 }
 
@@ -643,9 +633,6 @@ hipError_t run_layer_backward(const Shape &s, bool gated, const void *dY, const 
         g.act = s.act;
         g.dZ = b.form && need_dz ? b.dZ.to : nullptr;
         g.ldd = s.dtype == GPIC_F32 ? split_ld(b.rows) : up64(b.rows);
-        g.vec = quads(dY, s.ldy, s.dtype) &&
-                (s.act == GPIC_ACT_NONE && !gated ? true : quads(Z, s.ldz, ztype)) &&
-                (!gated || s.m % 4 == 0);
         g.sums = db ? b.sums : nullptr;
         if (need_dz) {
             g.max_dy = b.max_dy;
@@ -660,7 +647,7 @@ hipError_t run_layer_backward(const Shape &s, bool gated, const void *dY, const 
                                   : launch_grad<GPIC_BF16>(g, gated, grid, st));
     }
     if (db) {
-        sum_parts_kernel<<<(unsigned)((s.m + 63) / 64), 256, 0, st>>>(
+        sum_parts_kernel<<<(unsigned)((s.m + 63) / 64), 1024, 0, st>>>(
             b.sums, (s.n + kSumRows - 1) / kSumRows, s.m, db, s.dtype);
         RUN(hipGetLastError());
     }
@@ -681,7 +668,6 @@ hipError_t run_layer_backward(const Shape &s, bool gated, const void *dY, const 
         a.e.sa = b.scale;
         a.e.sb = b.W.scale;
         a.e.out = dX;
-        a.e.vec = eights(dX, s.k, s.dtype);
         RUN(launch_product(kKM, op, kEpiLayer, a, st));
     }
     if (dW) {
@@ -693,7 +679,6 @@ hipError_t run_layer_backward(const Shape &s, bool gated, const void *dY, const 
         a.e.sa = s.n > 0 ? b.scale : nullptr;      // no rows: dW = 0, no scales
         a.e.sb = s.n > 0 ? b.X.scale : nullptr;
         a.e.out = dW;
-        a.e.vec = eights(dW, s.k, s.dtype);
         RUN(launch_product(kMM, op, kEpiLayer, a, st));
     }
     return hipSuccess;

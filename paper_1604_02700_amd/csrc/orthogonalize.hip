@@ -25,7 +25,7 @@ namespace gpic {
 
 namespace {
 
-constexpr int kParts = 256;            // partial sums of squares per matrix
+constexpr int kParts = 1024;           // partial sums of squares per matrix
 constexpr float kStore = 1024.0f;      // X, A, P are stored times this: entries of
                                        // X are <= 1.3, of P <= 64 for any coefficients
                                        // the entry points accept
@@ -37,46 +37,49 @@ struct Input {
     const void *G;
     float *M;              // null: U = G
     float momentum;
-    int nesterov, dtype;
+    int nesterov;
     int64_t m, n;
-    int vec;               // m n % 4 == 0 and aligned
 };
 
-// U of one or four entries; `update`: M is advanced first
+using loose4 = f32x4 __attribute__((aligned(4)));
+
+// U of one entry, M advanced already
 __device__ __forceinline__ float u_of(float g, float mom, const Input &in)
 {
     return in.nesterov ? g + in.momentum * mom : mom;
 }
 
 // Sum of squares of U (float64, partial per workgroup); with a momentum
-// also M <- momentum M + G, in place.
+// also M <- momentum M + G, in place.  Memory-bound: 16-byte accesses at
+// whatever alignment the matrix of the stack has.
+template <int DT, bool STEP>
 __global__ __launch_bounds__(256) void norm_kernel(Input in, double *part)
 {
     const int64_t size = in.m * in.n, z0 = (int64_t)blockIdx.y * size;
+    const int64_t stride = (int64_t)gridDim.x * 1024;
     double t = 0.0;
-    if (in.vec) {
-        for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < size;
-             i += (int64_t)gridDim.x * 1024) {
-            f32x4 u = load4(in.G, z0 + i, in.dtype);
-            if (in.M) {
-                f32x4 *pm = reinterpret_cast<f32x4 *>(in.M + z0 + i);
-                const f32x4 mo = *pm * in.momentum + u;
-                *pm = mo;
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    u[j] = u_of(u[j], mo[j], in);
-            }
+    int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+#pragma unroll 4
+    for (; i + 4 <= size; i += stride) {
+        f32x4 u = load4(in.G, z0 + i, DT);
+        if (STEP) {
+            loose4 *pm = reinterpret_cast<loose4 *>(in.M + z0 + i);
+            const f32x4 mo = *pm * in.momentum + u;
+            *pm = mo;
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                t += (double)u[j] * (double)u[j];
+                u[j] = u_of(u[j], mo[j], in);
         }
-    } else {
-        for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < size;
-             i += (int64_t)gridDim.x * 256) {
-            float u = load1(in.G, z0 + i, in.dtype);
-            if (in.M) {
-                const float mo = in.M[z0 + i] * in.momentum + u;
-                in.M[z0 + i] = mo;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            t += (double)u[j] * (double)u[j];
+    }
+    for (; i < size; i = size) {                      // the last one to three entries
+        for (int64_t k = i; k < size; ++k) {
+            float u = load1(in.G, z0 + k, DT);
+            if (STEP) {
+                const float mo = in.M[z0 + k] * in.momentum + u;
+                in.M[z0 + k] = mo;
                 u = u_of(u, mo, in);
             }
             t += (double)u * (double)u;
@@ -100,11 +103,14 @@ struct Planes {
 
 // X_0 = U / (|U|_F + eps) in 16-bit parts, zeros in the padding of both
 // buffers' rows.  Four columns a thread.
+template <int DT, bool STEP>
 __global__ __launch_bounds__(256) void start_kernel(Input in, const double *part, int parts,
                                                     double eps, Planes x0, Planes x1)
 {
     __shared__ double w[4];
-    double t = threadIdx.x < parts ? part[(int64_t)blockIdx.y * kParts + threadIdx.x] : 0.0;
+    double t = 0.0;
+    for (int i = threadIdx.x; i < parts; i += 256)
+        t += part[(int64_t)blockIdx.y * kParts + i];
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1)
         t += __shfl_xor(t, o, 64);
@@ -120,22 +126,20 @@ __global__ __launch_bounds__(256) void start_kernel(Input in, const double *part
         const int64_t r = i / quads, c = (i - r * quads) * 4;
         f32x4 u = {0.0f, 0.0f, 0.0f, 0.0f};
         const int64_t at = z0 + r * in.n + c;
-        if (in.vec && (in.n & 3) == 0) {
-            if (c < in.n) {
-                u = load4(in.G, at, in.dtype);
-                if (in.M) {
-                    const f32x4 mo = *reinterpret_cast<const f32x4 *>(in.M + at);
+        if (c + 4 <= in.n) {
+            u = load4(in.G, at, DT);
+            if (STEP) {
+                const f32x4 mo = *reinterpret_cast<const loose4 *>(in.M + at);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        u[j] = u_of(u[j], mo[j], in);
-                }
+                for (int j = 0; j < 4; ++j)
+                    u[j] = u_of(u[j], mo[j], in);
             }
         } else {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
                 if (c + j < in.n) {
-                    u[j] = load1(in.G, at + j, in.dtype);
-                    if (in.M)
+                    u[j] = load1(in.G, at + j, DT);
+                    if (STEP)
                         u[j] = u_of(u[j], in.M[at + j], in);
                 }
         }
@@ -191,8 +195,8 @@ struct Layout {
         }
         const int op = split ? kOpSplit : kOpF16;
         const int64_t b = p.batch;
-        size_t most = product_plan(r, r, len, b, op, kEpiSym).part_bytes;
-        const size_t s1 = product_plan(r, r, r, b, op, kEpiSym).part_bytes;
+        size_t most = product_plan(r, r, len, b, op, kEpiGram).part_bytes;
+        const size_t s1 = product_plan(r, r, r, b, op, kEpiGram).part_bytes;
         const size_t s2 = product_plan(p.m, p.n, r, b, op, kEpiUpdate).part_bytes;
         most = s1 > most ? s1 : most;
         most = s2 > most ? s2 : most;
@@ -210,6 +214,26 @@ Operand operand(const Planes &p) { return Operand{p.hi, p.ld, p.batch, p.ld}; }
             return e_;                                                         \
     } while (0)
 
+template <int DT, bool STEP>
+hipError_t launch_start(const Polar &p, const Input &in, const Layout &L, hipStream_t st)
+{
+    int64_t parts = (p.m * p.n + 4095) / 4096;
+    parts = parts > kParts ? kParts : parts;
+    norm_kernel<DT, STEP><<<dim3((unsigned)parts, (unsigned)p.batch), 256, 0, st>>>(in, L.part);
+    RUN(hipGetLastError());
+    int64_t blocks = (p.m * (up64(p.n) / 4) + 255) / 256;
+    blocks = blocks > 4096 ? 4096 : blocks;
+    start_kernel<DT, STEP><<<dim3((unsigned)blocks, (unsigned)p.batch), 256, 0, st>>>(
+        in, L.part, (int)parts, p.eps, L.x[0], L.x[1]);
+    return hipGetLastError();
+}
+
+template <int DT>
+hipError_t launch_start(const Polar &p, const Input &in, const Layout &L, hipStream_t st)
+{
+    return in.M ? launch_start<DT, true>(p, in, L, st) : launch_start<DT, false>(p, in, L, st);
+}
+
 hipError_t iterate(const Polar &p, const Input &in, void *out, const MuonStep *h, void *ws,
                    hipStream_t st)
 {
@@ -218,16 +242,9 @@ hipError_t iterate(const Polar &p, const Input &in, void *out, const MuonStep *h
     Layout L(p, static_cast<char *>(ws));
     const int op = L.split ? kOpSplit : kOpF16;
     const int64_t size = p.m * p.n;
-    int64_t parts = (size + 4095) / 4096;
-    parts = parts > kParts ? kParts : parts;
-    norm_kernel<<<dim3((unsigned)parts, (unsigned)p.batch), 256, 0, st>>>(in, L.part);
-    RUN(hipGetLastError());
-    int64_t blocks = (p.m * (up64(p.n) / 4) + 255) / 256;
-    blocks = blocks > 4096 ? 4096 : blocks;
-    start_kernel<<<dim3((unsigned)blocks, (unsigned)p.batch), 256, 0, st>>>(
-        in, L.part, (int)parts, p.eps, L.x[0], L.x[1]);
-    RUN(hipGetLastError());
-
+    RUN(p.dtype == GPIC_F32    ? launch_start<GPIC_F32>(p, in, L, st)
+        : p.dtype == GPIC_F16 ? launch_start<GPIC_F16>(p, in, L, st)
+                              : launch_start<GPIC_BF16>(p, in, L, st));
     const float inv2 = 1.0f / (kStore * kStore);
     for (int k = 0; k < p.steps; ++k) {
         const Planes &x = L.x[k & 1], &y = L.x[(k + 1) & 1];
@@ -235,7 +252,6 @@ hipError_t iterate(const Polar &p, const Input &in, void *out, const MuonStep *h
         ProductArgs a{};
         a.batch = (int)p.batch;
         a.part = L.sums;
-        a.e.is_split = L.split;
         a.e.store_scale = kStore;
         a.e.load_scale = 1.0f / kStore;
         // A = X X^T (X^T X)
@@ -246,7 +262,7 @@ hipError_t iterate(const Polar &p, const Input &in, void *out, const MuonStep *h
         a.e.p_hi = L.gram.hi;
         a.e.ldp = L.lds;
         a.e.batch_p = L.gram.batch;
-        RUN(launch_product(L.tall ? kMM : kKK, op, kEpiSym, a, st));
+        RUN(launch_product(L.tall ? kMM : kKK, op, kEpiGram, a, st));
         // P = b A + c A A
         a.A = a.B = operand(L.gram);
         a.K = L.r;
@@ -254,7 +270,7 @@ hipError_t iterate(const Polar &p, const Input &in, void *out, const MuonStep *h
         a.e.beta = p.b;
         a.e.c_hi = L.gram.hi;
         a.e.p_hi = L.poly.hi;
-        RUN(launch_product(kKK, op, kEpiSym, a, st));
+        RUN(launch_product(kKK, op, kEpiPoly, a, st));
         // X' = a X + P X (a X + X P)
         a.A = operand(L.tall ? x : L.poly);
         a.B = operand(L.tall ? L.poly : x);
@@ -269,19 +285,17 @@ hipError_t iterate(const Polar &p, const Input &in, void *out, const MuonStep *h
         a.e.ldp = L.ldx;
         a.e.batch_p = x.batch;
         if (last) {
-            a.e.to_out = 1;
             a.e.out = out;
             a.e.dtype = p.dtype;
             a.e.ldo = p.n;
             a.e.batch_o = size;
-            a.e.vec = p.n % 8 == 0 && (uintptr_t)out % 16 == 0;
             if (h) {
                 a.e.is_step = 1;
                 a.e.decay = 1.0f - h->lr * h->decay;
                 a.e.step = h->lr * h->scale;
             }
         }
-        RUN(launch_product(L.tall ? kKK : kKM, op, kEpiUpdate, a, st));
+        RUN(launch_product(L.tall ? kKK : kKM, op, last ? kEpiResult : kEpiUpdate, a, st));
     }
     return hipSuccess;
 }
@@ -297,10 +311,8 @@ hipError_t run_orthogonalize(const Polar &p, const void *G, void *O, void *ws, h
 {
     Input in{};
     in.G = G;
-    in.dtype = p.dtype;
     in.m = p.m;
     in.n = p.n;
-    in.vec = p.m * p.n % 4 == 0 && (uintptr_t)G % 16 == 0;
     return iterate(p, in, O, nullptr, ws, st);
 }
 
@@ -312,10 +324,8 @@ hipError_t run_muon(const Polar &p, const MuonStep &h, void *W, const void *G, f
     in.M = M;
     in.momentum = h.momentum;
     in.nesterov = h.nesterov;
-    in.dtype = p.dtype;
     in.m = p.m;
     in.n = p.n;
-    in.vec = p.m * p.n % 4 == 0 && (uintptr_t)G % 16 == 0 && (uintptr_t)M % 16 == 0;
     return iterate(p, in, W, &h, ws, st);
 }
 

@@ -218,17 +218,23 @@ __device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 c)
 // A wave's accumulators go through LDS (its own piece, no barrier) so that
 // a lane finishes eight consecutive columns of a row: 16-byte loads and
 // stores that cover whole lines.
-// eight values p[i .. i + 7] of which `valid` exist; whole: at once
-__device__ __forceinline__ f32x8 load8(const void *p, int64_t i, int dtype, int valid, bool whole)
+// Eight values p[i .. i + 7], of which `valid` exist, at any alignment (the
+// card's 16-byte accesses need none; where a row starts on 16 bytes they
+// cover whole lines).
+using f32x8_any = float __attribute__((ext_vector_type(8), aligned(4)));
+using half8_any = _Float16 __attribute__((ext_vector_type(8), aligned(2)));
+using bfrag8_any = __bf16 __attribute__((ext_vector_type(8), aligned(2)));
+
+__device__ __forceinline__ f32x8 load8(const void *p, int64_t i, int dtype, int valid)
 {
-    if (whole) {
+    if (valid >= 8) {
         if (dtype == GPIC_F32)
-            return *reinterpret_cast<const f32x8 *>(static_cast<const float *>(p) + i);
+            return *reinterpret_cast<const f32x8_any *>(static_cast<const float *>(p) + i);
         if (dtype == GPIC_F16)
             return __builtin_convertvector(
-                *reinterpret_cast<const half8 *>(static_cast<const _Float16 *>(p) + i), f32x8);
+                *reinterpret_cast<const half8_any *>(static_cast<const _Float16 *>(p) + i), f32x8);
         return __builtin_convertvector(
-            *reinterpret_cast<const bfrag8 *>(static_cast<const __bf16 *>(p) + i), f32x8);
+            *reinterpret_cast<const bfrag8_any *>(static_cast<const __bf16 *>(p) + i), f32x8);
     }
     f32x8 v = 0.0f;
 #pragma unroll
@@ -238,17 +244,16 @@ __device__ __forceinline__ f32x8 load8(const void *p, int64_t i, int dtype, int 
     return v;
 }
 
-__device__ __forceinline__ void store8(void *p, int64_t i, f32x8 v, int dtype, int valid,
-                                       bool whole)
+__device__ __forceinline__ void store8(void *p, int64_t i, f32x8 v, int dtype, int valid)
 {
-    if (whole) {
+    if (valid >= 8) {
         if (dtype == GPIC_F32)
-            *reinterpret_cast<f32x8 *>(static_cast<float *>(p) + i) = v;
+            *reinterpret_cast<f32x8_any *>(static_cast<float *>(p) + i) = v;
         else if (dtype == GPIC_F16)
-            *reinterpret_cast<half8 *>(static_cast<_Float16 *>(p) + i) =
+            *reinterpret_cast<half8_any *>(static_cast<_Float16 *>(p) + i) =
                 __builtin_convertvector(v, half8);
         else
-            *reinterpret_cast<bfrag8 *>(static_cast<__bf16 *>(p) + i) =
+            *reinterpret_cast<bfrag8_any *>(static_cast<__bf16 *>(p) + i) =
                 __builtin_convertvector(v, bfrag8);
         return;
     }
@@ -258,34 +263,42 @@ __device__ __forceinline__ void store8(void *p, int64_t i, f32x8 v, int dtype, i
             store1(p, i + j, v[j], dtype);
 }
 
-__device__ __forceinline__ int64_t part_at(const Epilogue &e, int64_t z, int64_t row, int64_t col)
-{
-    return z * e.batch_p + row * e.ldp + (e.is_split ? split_at(col) : col);
-}
+// 16-bit parts of iterates: of split operands one split matrix; of single
+// ones a matrix of high halves and, for X (kEpiUpdate, kEpiResult), one of low
+// halves beside it.
+template <int OP, int EPI>
+struct Parts {
+    static constexpr bool kSplit = OP == kOpSplit;
+    static constexpr bool kLow = !kSplit && (EPI == kEpiUpdate || EPI == kEpiResult);
 
-// 16-bit parts of v (times store_scale already), eight columns
-__device__ __forceinline__ void store_parts(const Epilogue &e, int64_t at, f32x8 v)
-{
-    _Float16 *hi = static_cast<_Float16 *>(e.p_hi) + at;
-    const half8 h = __builtin_convertvector(v, half8);
-    *reinterpret_cast<half8 *>(hi) = h;
-    if (e.is_split || e.p_lo) {
-        _Float16 *lo = e.is_split ? hi + 32 : static_cast<_Float16 *>(e.p_lo) + at;
-        *reinterpret_cast<half8 *>(lo) =
-            __builtin_convertvector(v - __builtin_convertvector(h, f32x8), half8);
+    static __device__ __forceinline__ int64_t at(const Epilogue &e, int64_t z, int64_t row,
+                                                 int64_t col)
+    {
+        return z * e.batch_p + row * e.ldp + (kSplit ? split_at(col) : col);
     }
-}
-
-__device__ __forceinline__ f32x8 load_parts(const Epilogue &e, int64_t at)
-{
-    const _Float16 *hi = static_cast<const _Float16 *>(e.c_hi) + at;
-    f32x8 v = __builtin_convertvector(*reinterpret_cast<const half8 *>(hi), f32x8);
-    if (e.is_split || e.c_lo) {
-        const _Float16 *lo = e.is_split ? hi + 32 : static_cast<const _Float16 *>(e.c_lo) + at;
-        v += __builtin_convertvector(*reinterpret_cast<const half8 *>(lo), f32x8);
+    // v (times store_scale already), eight columns
+    static __device__ __forceinline__ void store(const Epilogue &e, int64_t at, f32x8 v)
+    {
+        _Float16 *hi = static_cast<_Float16 *>(e.p_hi) + at;
+        const half8 h = __builtin_convertvector(v, half8);
+        *reinterpret_cast<half8 *>(hi) = h;
+        if (kSplit || kLow) {
+            _Float16 *lo = kSplit ? hi + 32 : static_cast<_Float16 *>(e.p_lo) + at;
+            *reinterpret_cast<half8 *>(lo) =
+                __builtin_convertvector(v - __builtin_convertvector(h, f32x8), half8);
+        }
     }
-    return v * e.load_scale;
-}
+    static __device__ __forceinline__ f32x8 load(const Epilogue &e, int64_t at)
+    {
+        const _Float16 *hi = static_cast<const _Float16 *>(e.c_hi) + at;
+        f32x8 v = __builtin_convertvector(*reinterpret_cast<const half8 *>(hi), f32x8);
+        if (kSplit || kLow) {
+            const _Float16 *lo = kSplit ? hi + 32 : static_cast<const _Float16 *>(e.c_lo) + at;
+            v += __builtin_convertvector(*reinterpret_cast<const half8 *>(lo), f32x8);
+        }
+        return v * e.load_scale;
+    }
+};
 
 // What the accumulators are multiplied by: the operands' scales are powers
 // of two, taken off one after the other so that neither step overflows.
@@ -308,14 +321,14 @@ __device__ __forceinline__ f32x8 staged(const float *p, Factor f)
 template <int OP, int EPI>
 __device__ __forceinline__ int out_type(const Epilogue &e)
 {
-    if (EPI == kEpiUpdate)
+    if (EPI == kEpiResult)
         return OP == kOpF16 ? GPIC_BF16 : (e.dtype == GPIC_F32 ? GPIC_F32 : GPIC_F16);
     return OP == kOpSplit ? GPIC_F32 : (OP == kOpF16 ? GPIC_F16 : GPIC_BF16);
 }
 
 // Finishes `ROWS` x `COLS` accumulators that the wave has staged at `st`
 // (pitch COLS + 4 floats), the output's rows from row0, columns from col0
-// (gated: columns from col0 / 2).  mirror (kEpiSym): the transposed block too.
+// (gated: columns from col0 / 2).  mirror (symmetric): the transposed block too.
 template <int ROWS, int COLS, int OP, int EPI>
 __device__ __forceinline__ void finish_block(const Epilogue &e, int64_t z, int64_t row0,
                                              int64_t col0, int64_t M, int64_t N, float *st,
@@ -324,11 +337,13 @@ __device__ __forceinline__ void finish_block(const Epilogue &e, int64_t z, int64
     // the whole and the partial accesses round alike
 #pragma clang fp contract(off)
     const int dtype = out_type<OP, EPI>(e);
+    using P = Parts<OP, EPI>;
+    constexpr bool kSym = symmetric(EPI);
     constexpr int kPitch = COLS + 4;
     constexpr int kOut = EPI == kEpiGated ? COLS / 2 : COLS;     // output columns
     constexpr int kLanes = kOut / 8, kRowsPass = 64 / kLanes < ROWS ? 64 / kLanes : ROWS;
     constexpr int kPasses = ROWS / kRowsPass;            // lanes beyond the rows do nothing
-    constexpr int kGroup = kPasses < 2 ? kPasses : 2;            // rows in flight a lane
+    constexpr int kGroup = kPasses < 4 ? 1 : 2;                  // rows in flight a lane
     static_assert(kPasses * kRowsPass == ROWS && kPasses % kGroup == 0, "passes");
     const int lane = threadIdx.x & 63, q = lane % kLanes, r0 = lane / kLanes;
     const bool idle = kLanes * kRowsPass < 64 && r0 >= kRowsPass;
@@ -336,7 +351,6 @@ __device__ __forceinline__ void finish_block(const Epilogue &e, int64_t z, int64
     if (EPI == kEpiGated) {
         const int64_t col = col0 / 2 + q * 8, half = e.half;
         const int valid = half - col < 8 ? (int)(half - col) : 8;
-        const bool whole = e.vec && valid == 8;
         const float *src = st + (q >> 1) * 32 + (q & 1) * 8;
         for (int p = 0; p < kPasses; ++p) {
             const int r = p * kRowsPass + r0;
@@ -346,22 +360,21 @@ __device__ __forceinline__ void finish_block(const Epilogue &e, int64_t z, int64
             f32x8 g = staged(src + r * kPitch, f);
             const f32x8 u = staged(src + r * kPitch + 16, f);
             if (e.pre) {
-                store8(e.pre, row * e.ldz + col, g, GPIC_F32, valid, whole);
-                store8(e.pre, row * e.ldz + half + col, u, GPIC_F32, valid, whole);
+                store8(e.pre, row * e.ldz + col, g, GPIC_F32, valid);
+                store8(e.pre, row * e.ldz + half + col, u, GPIC_F32, valid);
             }
-            store8(e.out, row * e.ldo + col, activate8(g, e.act) * u, dtype, valid, whole);
+            store8(e.out, row * e.ldo + col, activate8(g, e.act) * u, dtype, valid);
         }
         return;
     }
     const int64_t col = col0 + q * 8;
     // 16-bit parts: the padding up to a multiple of 64 columns is written too
-    const int64_t end = EPI == kEpiSym ? (N + 63) / 64 * 64 : N;
+    const int64_t end = symmetric(EPI) ? (N + 63) / 64 * 64 : N;
     const int64_t here = end - col;
     const int valid = here < 0 ? 0 : (here < 8 ? (int)here : 8);
-    const bool whole = e.vec && valid == 8;
     f32x8 bias = 0.0f;
     if (EPI == kEpiLayer && e.bias && valid > 0)
-        bias = load8(e.bias, col, dtype, valid, whole);
+        bias = load8(e.bias, col, dtype, valid);
     for (int p0 = 0; p0 < kPasses; p0 += kGroup) {
         f32x8 v[kGroup], c[kGroup];
 #pragma unroll
@@ -370,16 +383,18 @@ __device__ __forceinline__ void finish_block(const Epilogue &e, int64_t z, int64
             const int64_t row = row0 + r;
             v[p] = staged(st + (idle ? 0 : r) * kPitch + q * 8, f);
             c[p] = 0.0f;
+            if (EPI == kEpiPoly || EPI == kEpiUpdate || EPI == kEpiResult) {
+                // lanes that finish nothing load the first entry
+                const bool live = valid > 0 && row < M && !idle;
+                c[p] = P::load(e, live ? P::at(e, z, row, col) : z * e.batch_p) * e.beta;
+            }
             if (valid <= 0 || row >= M || idle)
                 continue;
             if (EPI == kEpiLayer && e.res)
-                c[p] = load8(e.res, row * e.ldr + col, dtype, valid, whole);
-            if (EPI == kEpiUpdate || (EPI == kEpiSym && e.c_hi))
-                c[p] = load_parts(e, part_at(e, z, row, col)) * e.beta;
-            if (EPI == kEpiUpdate && e.is_step) {
+                c[p] = load8(e.res, row * e.ldr + col, dtype, valid);
+            if (EPI == kEpiResult && e.is_step) {
                 // decay W - step (beta X + acc)
-                const f32x8 old = load8(e.out, z * e.batch_o + row * e.ldo + col, dtype, valid,
-                                        whole);
+                const f32x8 old = load8(e.out, z * e.batch_o + row * e.ldo + col, dtype, valid);
                 c[p] = old * e.decay - c[p] * e.step;
                 v[p] = v[p] * -e.step;
             }
@@ -395,41 +410,47 @@ __device__ __forceinline__ void finish_block(const Epilogue &e, int64_t z, int64
                 if (e.bias)
                     x = x + bias;
                 if (e.pre)
-                    store8(e.pre, row * e.ldz + col, x, dtype, valid, whole);
+                    store8(e.pre, row * e.ldz + col, x, dtype, valid);
                 x = activate8(x, e.act);
                 if (e.res)
                     x = x + c[p];
-                store8(e.out, row * e.ldo + col, x, dtype, valid, whole);
-            } else if (EPI == kEpiSym) {
-                x = (x + c[p]) * e.store_scale;
-                store_parts(e, part_at(e, z, row, col), x);
+                store8(e.out, row * e.ldo + col, x, dtype, valid);
+            } else if (kSym) {
+                x = (EPI == kEpiPoly ? x + c[p] : x) * e.store_scale;
+                P::store(e, P::at(e, z, row, col), x);
                 if (mirror)
                     *reinterpret_cast<f32x8 *>(st + r * kPitch + q * 8) = x;
             } else {
                 x = x + c[p];
-                if (!e.to_out) {
-                    store_parts(e, part_at(e, z, row, col), x * e.store_scale);
-                    continue;
-                }
-                store8(e.out, z * e.batch_o + row * e.ldo + col, x, dtype, valid, whole);
+                if (EPI == kEpiUpdate)
+                    P::store(e, P::at(e, z, row, col), x * e.store_scale);
+                else
+                    store8(e.out, z * e.batch_o + row * e.ldo + col, x, dtype, valid);
             }
         }
     }
-    if (EPI == kEpiSym && mirror) {
-        // rows and columns change places: a lane takes eight rows of a
-        // column.  Only whole tiles above the diagonal are mirrored, so the
-        // rows all exist; columns beyond N are padding.
-        constexpr int kL = ROWS / 8, kC = 64 / kL;
-        const int rq = (lane % kL) * 8, c0 = lane / kL;
-        for (int p = 0; p < COLS / kC; ++p) {
-            const int c = p * kC + c0;
-            f32x8 x;
+}
+
+// The transposed block of what finish_block has left at `st` (times
+// store_scale), a lane eight rows of a column; wave `first` of `waves`.  Only
+// whole tiles above the diagonal are mirrored, so the rows all exist;
+// columns beyond N are padding.
+template <int ROWS, int COLS, int OP, int EPI>
+__device__ __forceinline__ void mirror_block(const Epilogue &e, int64_t z, int64_t row0,
+                                             int64_t col0, int64_t N, const float *st, int first,
+                                             int waves)
+{
+    constexpr int kL = ROWS / 8, kC = 64 / kL, kPitch = COLS + 4;
+    static_assert(COLS % kC == 0, "columns");
+    const int lane = threadIdx.x & 63, rq = (lane % kL) * 8;
+    for (int p = first; p < COLS / kC; p += waves) {
+        const int c = p * kC + lane / kL;
+        f32x8 x;
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                x[j] = st[(rq + j) * kPitch + c];
-            if (col0 + c < N)
-                store_parts(e, part_at(e, z, col0 + c, row0 + rq), x);
-        }
+        for (int j = 0; j < 8; ++j)
+            x[j] = st[(rq + j) * kPitch + c];
+        if (col0 + c < N)
+            Parts<OP, EPI>::store(e, Parts<OP, EPI>::at(e, z, col0 + c, row0 + rq), x);
     }
 }
 
@@ -558,9 +579,11 @@ __device__ __forceinline__ void finish_tile(const ProductArgs &a, const Work &w,
                     *reinterpret_cast<const f32x4 *>(st + r * St::kPitch + c);
             }
         } else {
-            finish_block<St::kRows, St::kCols, OP, EPI>(
-                a.e, w.z, (int64_t)w.ti * T::kBM + wm + 16 * i0, (int64_t)w.tj * T::kBN + wn, a.M,
-                a.N, st, EPI == kEpiSym && w.ti != w.tj);
+            const int64_t r0 = (int64_t)w.ti * T::kBM + wm + 16 * i0, c0 = (int64_t)w.tj * T::kBN + wn;
+            const bool mirror = symmetric(EPI) && w.ti != w.tj;
+            finish_block<St::kRows, St::kCols, OP, EPI>(a.e, w.z, r0, c0, a.M, a.N, st, mirror);
+            if (mirror)
+                mirror_block<St::kRows, St::kCols, OP, EPI>(a.e, w.z, r0, c0, a.N, st, 0, 1);
         }
     }
 }
@@ -577,7 +600,7 @@ __global__ __launch_bounds__(T::kThreads) void product_kernel(ProductArgs a, int
     constexpr int kLds = 2 * kBuf > St::kBytes ? 2 * kBuf : St::kBytes;
     __shared__ __attribute__((aligned(1024))) char lds[kLds];
 
-    const Work w(a, tm, tn, EPI == kEpiSym, kStep);
+    const Work w(a, tm, tn, symmetric(EPI), kStep);
     const int64_t z = w.z, s0 = w.s0, s1 = w.s1;
     const int64_t row0 = (int64_t)w.ti * T::kBM, col0 = (int64_t)w.tj * T::kBN;
 
@@ -709,7 +732,7 @@ __global__ __launch_bounds__(512) void product_large_kernel(ProductArgs a, int t
     constexpr int kLds = 2 * kBuf > Staging<T>::kBytes ? 2 * kBuf : Staging<T>::kBytes;
     __shared__ __attribute__((aligned(1024))) char lds[kLds];
 
-    const Work w(a, tm, tn, EPI == kEpiSym, kStep);
+    const Work w(a, tm, tn, symmetric(EPI), kStep);
     const int64_t z = w.z;
     const int64_t row0 = (int64_t)w.ti * T::kBM, col0 = (int64_t)w.tj * T::kBN;
     SideA sa[2];
@@ -850,30 +873,31 @@ __global__ __launch_bounds__(512) void product_large_kernel(ProductArgs a, int t
     finish_tile<T, OP, EPI>(a, w, acc, lds);
 }
 
-// The parts of the split tiles, added in order, then the epilogue.  A wave
-// takes 16 rows of one wave's columns: few tiles have many parts, so the
-// pieces are small and eight parts' loads are in flight.
-constexpr int kJoinRows = 16;
-
+// The parts of the split tiles, added in order, then the epilogue.  A
+// workgroup takes the rows and columns that a wave stages; eight parts'
+// loads are in flight (few tiles have many parts).  The mirrored block goes
+// out by rows of at least 64 bytes: with 32 the dies' caches write parts of
+// each other's lines, and a join of 136 tiles takes 18 us for 6.
 template <class T, int OP, int EPI>
-__global__ __launch_bounds__(64) void product_join_kernel(ProductArgs a, int tm, int tn, int tail)
+__global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a, int tm, int tn, int tail)
 {
-    constexpr int kCols = Staging<T>::kCols, kPitch = Staging<T>::kPitch;
-    __shared__ __attribute__((aligned(16))) float st[kJoinRows * kPitch];
-    constexpr int kAcross = T::kBN / kCols, kPieces = T::kBM / kJoinRows * kAcross;
+    using St = Staging<T>;
+    constexpr int kCols = St::kCols, kPitch = St::kPitch, kRows = St::kRows;
+    __shared__ __attribute__((aligned(16))) float st[kRows * kPitch];
+    constexpr int kAcross = T::kBN / kCols, kPieces = T::kBM / kRows * kAcross;
     const int tile = a.whole + blockIdx.x / kPieces, piece = blockIdx.x % kPieces;
-    const int pr = piece / kAcross * kJoinRows, pc = piece % kAcross * kCols;
+    const int pr = piece / kAcross * kRows, pc = piece % kAcross * kCols;
     int ti, tj;
-    const int each = EPI == kEpiSym ? tn * (tn + 1) / 2 : tm * tn;
+    const int each = symmetric(EPI) ? tn * (tn + 1) / 2 : tm * tn;
     const int64_t z = tile / each;
-    which_tile(tile % each, tm, tn, EPI == kEpiSym, ti, tj);
+    which_tile(tile % each, tm, tn, symmetric(EPI), ti, tj);
     const int64_t row0 = (int64_t)ti * T::kBM + pr, col0 = (int64_t)tj * T::kBN + pc;
-    if (row0 >= a.M || col0 >= (EPI == kEpiSym ? ((int64_t)a.N + 63) / 64 * 64 : a.N))
+    if (row0 >= a.M || col0 >= (symmetric(EPI) ? ((int64_t)a.N + 63) / 64 * 64 : a.N))
         return;
     const int64_t pitch = (int64_t)tail * T::kBM * T::kBN;         // between parts
     const float *part = a.part + (int64_t)(tile - a.whole) * T::kBM * T::kBN + pr * T::kBN + pc;
     constexpr int kQuads = kCols / 4;
-    for (int i = threadIdx.x; i < kJoinRows * kQuads; i += 64) {
+    for (int i = threadIdx.x; i < kRows * kQuads; i += 256) {
         const int r = i / kQuads, c = i % kQuads * 4;
         const float *p = part + r * T::kBN + c;
         f32x4 v = *reinterpret_cast<const f32x4 *>(p);
@@ -883,8 +907,15 @@ __global__ __launch_bounds__(64) void product_join_kernel(ProductArgs a, int tm,
         *reinterpret_cast<f32x4 *>(st + r * kPitch + c) = v;
     }
     __syncthreads();
-    finish_block<kJoinRows, kCols, OP, EPI>(a.e, z, row0, col0, a.M, a.N, st,
-                                            EPI == kEpiSym && ti != tj);
+    const int wave = threadIdx.x >> 6;
+    const bool mirror = symmetric(EPI) && ti != tj;
+    constexpr int kWaveRows = kRows / 4;
+    finish_block<kWaveRows, kCols, OP, EPI>(a.e, z, row0 + wave * kWaveRows, col0, a.M, a.N,
+                                            st + wave * kWaveRows * kPitch, mirror);
+    if (mirror) {
+        __syncthreads();
+        mirror_block<kRows, kCols, OP, EPI>(a.e, z, row0, col0, a.N, st, wave, 4);
+    }
 }
 
 // ------------------------------------------------------------------- host
@@ -902,9 +933,10 @@ hipError_t launch_tile(const Plan &p, ProductArgs a, hipStream_t s)
             <<<(unsigned)blocks, T::kThreads, 0, s>>>(a, p.tm, p.tn);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && p.tail > 0) {
-        constexpr int kPieces = T::kBM / kJoinRows * (T::kBN / Staging<T>::kCols);
+        using St = Staging<T>;
+        constexpr int kPieces = T::kBM / St::kRows * (T::kBN / St::kCols);
         product_join_kernel<T, OP, EPI>
-            <<<(unsigned)(p.tail * kPieces), 64, 0, s>>>(a, p.tm, p.tn, (int)p.tail);
+            <<<(unsigned)(p.tail * kPieces), 256, 0, s>>>(a, p.tm, p.tn, (int)p.tail);
         e = hipGetLastError();
     }
     return e;

@@ -47,7 +47,7 @@ Plan product_plan(int64_t M, int64_t N, int64_t K, int64_t batch, int op, int ep
     best.splits = 1;
     if (M <= 0 || N <= 0 || batch <= 0)
         return best;
-    const bool sym = epi == kEpiSym, split = op == kOpSplit;
+    const bool sym = symmetric(epi), split = op == kOpSplit;
     const int64_t step = split ? 32 : 64, steps = (K + step - 1) / step;
     static const int kParts[] = {2, 3, 4, 6, 8, 12, 16, 24, 32};
     double least = 0.0;

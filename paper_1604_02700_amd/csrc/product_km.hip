@@ -14,8 +14,11 @@ hipError_t launch_product_km(int op, int epi, const Plan &p, const ProductArgs &
             return launch_any_tile<false, true, kOpF16, kEpiLayer>(p, a, s);
         return launch_any_tile<false, true, kOpSplit, kEpiLayer>(p, a, s);
     }
-    return op == kOpF16 ? launch_any_tile<false, true, kOpF16, kEpiUpdate>(p, a, s)
-                        : launch_any_tile<false, true, kOpSplit, kEpiUpdate>(p, a, s);
+    if (epi == kEpiUpdate)
+        return op == kOpF16 ? launch_any_tile<false, true, kOpF16, kEpiUpdate>(p, a, s)
+                            : launch_any_tile<false, true, kOpSplit, kEpiUpdate>(p, a, s);
+    return op == kOpF16 ? launch_any_tile<false, true, kOpF16, kEpiResult>(p, a, s)
+                        : launch_any_tile<false, true, kOpSplit, kEpiResult>(p, a, s);
 }
 
 } // namespace gpic

@@ -14,8 +14,8 @@ hipError_t launch_product_mm(int op, int epi, const Plan &p, const ProductArgs &
             return launch_any_tile<true, true, kOpF16, kEpiLayer>(p, a, s);
         return launch_any_tile<true, true, kOpSplit, kEpiLayer>(p, a, s);
     }
-    return op == kOpF16 ? launch_any_tile<true, true, kOpF16, kEpiSym>(p, a, s)
-                        : launch_any_tile<true, true, kOpSplit, kEpiSym>(p, a, s);
+    return op == kOpF16 ? launch_any_tile<true, true, kOpF16, kEpiGram>(p, a, s)
+                        : launch_any_tile<true, true, kOpSplit, kEpiGram>(p, a, s);
 }
 
 } // namespace gpic
