@@ -276,7 +276,10 @@ struct MuonStep {
     float lr, momentum, decay, scale;
     int nesterov;
 };
-size_t polar_ws(const Polar &p);
+size_t polar_ws(const Polar &p);           // 0 for what polar_small.hip takes
+bool polar_small(const Polar &p);
+hipError_t run_polar_small(const Polar &p, const MuonStep *h, void *out, const void *G, float *M,
+                           hipStream_t st);
 hipError_t run_orthogonalize(const Polar &p, const void *G, void *O, void *ws, hipStream_t st);
 hipError_t run_muon(const Polar &p, const MuonStep &h, void *W, const void *G, float *M,
                     void *ws, hipStream_t st);

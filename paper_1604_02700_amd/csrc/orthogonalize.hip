@@ -304,11 +304,13 @@ hipError_t iterate(const Polar &p, const Input &in, void *out, const MuonStep *h
 
 size_t polar_ws(const Polar &p)
 {
-    return Layout(p, nullptr).bytes;
+    return polar_small(p) ? 0 : Layout(p, nullptr).bytes;
 }
 
 hipError_t run_orthogonalize(const Polar &p, const void *G, void *O, void *ws, hipStream_t st)
 {
+    if (polar_small(p))
+        return p.batch ? run_polar_small(p, nullptr, O, G, nullptr, st) : hipSuccess;
     Input in{};
     in.G = G;
     in.m = p.m;
@@ -319,6 +321,8 @@ hipError_t run_orthogonalize(const Polar &p, const void *G, void *O, void *ws, h
 hipError_t run_muon(const Polar &p, const MuonStep &h, void *W, const void *G, float *M, void *ws,
                     hipStream_t st)
 {
+    if (polar_small(p))
+        return p.batch ? run_polar_small(p, &h, W, G, M, st) : hipSuccess;
     Input in{};
     in.G = G;
     in.M = M;
