@@ -173,7 +173,13 @@ def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else C.c_void_p(t.data_ptr())
 
 
+# the current stream's handle without a stream object around it (2 us a call)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(device) -> C.c_void_p:
+    if _raw_stream is not None and isinstance(device, torch.device) and device.index is not None:
+        return C.c_void_p(_raw_stream(device.index))
     return C.c_void_p(torch.cuda.current_stream(device).cuda_stream)
 
 
@@ -645,22 +651,24 @@ class LayerGrads:
     db: Optional[torch.Tensor] = None
 
 
-def _matrix(t, shape, dtype, device, name):
-    """t as a 2-D tensor of that shape with unit column stride (copied only
-    when its columns are strided or its rows overlap)."""
-    _dev(t, dtype, name)
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, not on {device}")
-    if tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} must be {tuple(shape)}, got {tuple(t.shape)}")
-    rows, cols = shape
-    if (cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < cols):
-        t = t.contiguous()
+def _matrix(t, rows, cols, like, name):
+    """t as a [rows, cols] tensor of like's type and device with unit column
+    stride (copied only when its columns are strided or its rows overlap)."""
+    _dev(t, like.dtype, name)
+    return _matrix_of(t, rows, cols, like, name)
+
+
+def _matrix_of(t, rows, cols, like, name):
+    if t.device != like.device:
+        raise ValueError(f"{name} is on {t.device}, not on {like.device}")
+    if t.shape != (rows, cols):
+        raise ValueError(f"{name} must be {(rows, cols)}, got {tuple(t.shape)}")
+    if t.is_contiguous():
+        return t
+    sr, sc = t.stride()
+    if (cols > 1 and sc != 1) or (rows > 1 and sr < cols):
+        return t.contiguous()
     return t
-
-
-def _pitch(t, cols):
-    return t.stride(0) if t is not None and t.shape[0] > 1 else cols
 
 
 def _layer_type(X):
@@ -670,6 +678,7 @@ def _layer_type(X):
         raise TypeError(f"X must be float32, float16 or bfloat16, got {X.dtype}")
     if X.dim() != 2:
         raise ValueError("X must be [n, k]")
+    return _matrix_of(X, X.shape[0], X.shape[1], X, "X")
 
 
 def _activation(name):
@@ -678,16 +687,21 @@ def _activation(name):
     return ACTIVATIONS[name]
 
 
-def _layer(op, X, W, Y, Z, residual, activation, gated):
+def _pitch(t, rows, cols):
+    return cols if t is None or rows < 2 else t.stride(0)
+
+
+def _layer(op, X, W, Y, Z, residual, activation, m):
     """LayerParams for these tensors and a workspace for `op`."""
     n, k = X.shape
-    m = W.shape[0] // 2 if gated else W.shape[0]
-    p = LayerParams(n=n, k=k, m=m, ldx=_pitch(X, k), ldw=_pitch(W, k), ldy=_pitch(Y, m),
-                    ldr=_pitch(residual, m), ldz=_pitch(Z, W.shape[0]), dtype=DTYPES[X.dtype],
-                    activation=_activation(activation), reserved=0)
-    p.aligned16 = int(all(t.data_ptr() % 16 == 0 for t in (X, W, Y)))
-    ws, nb = _workspace(int(lib().gpic_layer_workspace_bytes(LAYER_OP[op], C.byref(p))), X.device)
-    return p, ws, nb
+    rows = W.shape[0]
+    xp, wp, yp = X.data_ptr(), W.data_ptr(), Y.data_ptr()
+    p = LayerParams(n, k, m, _pitch(X, n, k), _pitch(W, rows, k), _pitch(Y, n, m),
+                    _pitch(residual, n, m), _pitch(Z, n, rows), DTYPES[X.dtype], activation,
+                    int((xp | wp | yp) % 16 == 0), 0)
+    ref = C.byref(p)
+    ws, nb = _workspace(lib().gpic_layer_workspace_bytes(LAYER_OP[op], ref), X.device)
+    return ref, xp, wp, yp, ws, nb
 
 
 def _weights(X, W, gated):
@@ -695,15 +709,19 @@ def _weights(X, W, gated):
         raise ValueError("W must be [m, k]" if not gated else "W must be [2 m, k]")
     if gated and W.shape[0] % 2:
         raise ValueError("W must be [2 m, k]: an even number of rows")
-    return _matrix(W, (W.shape[0], X.shape[1]), X.dtype, X.device, "W")
+    return _matrix(W, W.shape[0], X.shape[1], X, "W")
 
 
-def _output(t, shape, X, name):
+def _output(t, rows, cols, X, name):
     if t is None:
-        return torch.empty(shape, dtype=X.dtype, device=X.device)
-    if _matrix(t, shape, X.dtype, X.device, name) is not t:
+        return torch.empty((rows, cols), dtype=X.dtype, device=X.device)
+    if _matrix(t, rows, cols, X, name) is not t:
         raise ValueError(f"{name} must have unit column stride and rows that do not overlap")
     return t
+
+
+def _at(t):
+    return None if t is None else t.data_ptr()
 
 
 def gpic_linear(X: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] = None,
@@ -713,22 +731,22 @@ def gpic_linear(X: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] =
     float16 or bfloat16, all the same); activation "none", "relu", "gelu" or
     "silu".  want_pre: returns (Y, Z) with Z = X W^T + bias, which
     gpic_linear_backward reads.  Y (optional) may be the residual itself."""
-    _layer_type(X)
-    X = _matrix(X, X.shape, X.dtype, X.device, "X")
+    X = _layer_type(X)
     W = _weights(X, W, False)
     n, m = X.shape[0], W.shape[0]
+    act = _activation(activation)
     if bias is not None:
         _dev(bias, X.dtype, "bias")
-        if tuple(bias.shape) != (m,) or bias.device != X.device:
+        if bias.shape != (m,) or bias.device != X.device:
             raise ValueError(f"bias must be [{m}] on {X.device}")
         bias = bias.contiguous()
     if residual is not None:
-        residual = _matrix(residual, (n, m), X.dtype, X.device, "residual")
-    Y = _output(Y, (n, m), X, "Y")
+        residual = _matrix(residual, n, m, X, "residual")
+    Y = _output(Y, n, m, X, "Y")
     Z = torch.empty((n, m), dtype=X.dtype, device=X.device) if want_pre else None
-    p, ws, nb = _layer("linear", X, W, Y, Z, residual, activation, False)
-    _check(lib().gpic_linear(C.byref(p), _ptr(X), _ptr(W), _ptr(bias), _ptr(residual), _ptr(Y),
-                             _ptr(Z), _ptr(ws), nb, _stream(X.device)))
+    ref, xp, wp, yp, ws, nb = _layer("linear", X, W, Y, Z, residual, act, m)
+    _check(lib().gpic_linear(ref, xp, wp, _at(bias), _at(residual), yp, _at(Z), _at(ws), nb,
+                             _stream(X.device)))
     return (Y, Z) if want_pre else Y
 
 
@@ -739,23 +757,23 @@ def gpic_linear_backward(dY: torch.Tensor, X: torch.Tensor, W: torch.Tensor,
     """Gradients of gpic_linear: dX, dW and db (those wanted).  Z as
     gpic_linear gave it (not needed without an activation); the residual's
     gradient is dY itself."""
-    _layer_type(X)
-    X = _matrix(X, X.shape, X.dtype, X.device, "X")
+    X = _layer_type(X)
     W = _weights(X, W, False)
-    n, m, dev = X.shape[0], W.shape[0], X.device
-    dY = _matrix(dY, (n, m), X.dtype, dev, "dY")
-    if _activation(activation) == 0:
+    (n, k), m, dev = X.shape, W.shape[0], X.device
+    dY = _matrix(dY, n, m, X, "dY")
+    act = _activation(activation)
+    if act == 0:
         Z = None
     elif Z is None:
         raise ValueError(f"the gradient of {activation!r} needs Z")
     else:
-        Z = _matrix(Z, (n, m), X.dtype, dev, "Z")
-    dX = torch.empty(X.shape, dtype=X.dtype, device=dev) if want_x else None
-    dW = torch.empty(W.shape, dtype=X.dtype, device=dev) if want_w else None
+        Z = _matrix(Z, n, m, X, "Z")
+    dX = torch.empty((n, k), dtype=X.dtype, device=dev) if want_x else None
+    dW = torch.empty((m, k), dtype=X.dtype, device=dev) if want_w else None
     db = torch.empty(m, dtype=X.dtype, device=dev) if want_bias else None
-    p, ws, nb = _layer("linear_backward", X, W, dY, Z, None, activation, False)
-    _check(lib().gpic_linear_backward(C.byref(p), _ptr(dY), _ptr(X), _ptr(W), _ptr(Z), _ptr(dX),
-                                      _ptr(dW), _ptr(db), _ptr(ws), nb, _stream(dev)))
+    ref, xp, wp, yp, ws, nb = _layer("linear_backward", X, W, dY, Z, None, act, m)
+    _check(lib().gpic_linear_backward(ref, yp, xp, wp, _at(Z), _at(dX), _at(dW), _at(db), _at(ws),
+                                      nb, _stream(dev)))
     return LayerGrads(dX, dW, db)
 
 
@@ -764,15 +782,14 @@ def gpic_gated(X: torch.Tensor, W: torch.Tensor, activation: str = "silu",
     """H = act(X Wg^T) * (X Wu^T) for W = [Wg; Wu] [2 m, k].  want_pre:
     returns (H, Z) with Z = X W^T [n, 2 m] (float32 whatever the type), which
     gpic_gated_backward reads."""
-    _layer_type(X)
-    X = _matrix(X, X.shape, X.dtype, X.device, "X")
+    X = _layer_type(X)
     W = _weights(X, W, True)
     n, m = X.shape[0], W.shape[0] // 2
-    H = _output(H, (n, m), X, "H")
+    act = _activation(activation)
+    H = _output(H, n, m, X, "H")
     Z = torch.empty((n, 2 * m), dtype=torch.float32, device=X.device) if want_pre else None
-    p, ws, nb = _layer("gated", X, W, H, Z, None, activation, True)
-    _check(lib().gpic_gated(C.byref(p), _ptr(X), _ptr(W), _ptr(H), _ptr(Z), _ptr(ws), nb,
-                            _stream(X.device)))
+    ref, xp, wp, hp, ws, nb = _layer("gated", X, W, H, Z, None, act, m)
+    _check(lib().gpic_gated(ref, xp, wp, hp, _at(Z), _at(ws), nb, _stream(X.device)))
     return (H, Z) if want_pre else H
 
 
@@ -780,17 +797,18 @@ def gpic_gated_backward(dH: torch.Tensor, X: torch.Tensor, W: torch.Tensor, Z: t
                         activation: str = "silu", want_x: bool = True,
                         want_w: bool = True) -> LayerGrads:
     """Gradients of gpic_gated: dX and dW (those wanted)."""
-    _layer_type(X)
-    X = _matrix(X, X.shape, X.dtype, X.device, "X")
+    X = _layer_type(X)
     W = _weights(X, W, True)
-    n, m, dev = X.shape[0], W.shape[0] // 2, X.device
-    dH = _matrix(dH, (n, m), X.dtype, dev, "dH")
-    Z = _matrix(Z, (n, 2 * m), torch.float32, dev, "Z")
-    dX = torch.empty(X.shape, dtype=X.dtype, device=dev) if want_x else None
-    dW = torch.empty(W.shape, dtype=X.dtype, device=dev) if want_w else None
-    p, ws, nb = _layer("gated_backward", X, W, dH, Z, None, activation, True)
-    _check(lib().gpic_gated_backward(C.byref(p), _ptr(dH), _ptr(X), _ptr(W), _ptr(Z), _ptr(dX),
-                                     _ptr(dW), _ptr(ws), nb, _stream(dev)))
+    (n, k), m, dev = X.shape, W.shape[0] // 2, X.device
+    dH = _matrix(dH, n, m, X, "dH")
+    act = _activation(activation)
+    _dev(Z, torch.float32, "Z")
+    Z = _matrix_of(Z, n, 2 * m, X, "Z")
+    dX = torch.empty((n, k), dtype=X.dtype, device=dev) if want_x else None
+    dW = torch.empty((2 * m, k), dtype=X.dtype, device=dev) if want_w else None
+    ref, xp, wp, hp, ws, nb = _layer("gated_backward", X, W, dH, Z, None, act, m)
+    _check(lib().gpic_gated_backward(ref, hp, xp, wp, _at(Z), _at(dX), _at(dW), _at(ws), nb,
+                                     _stream(dev)))
     return LayerGrads(dX, dW)
 
 
@@ -812,10 +830,11 @@ def _polar(G, steps, coefficients, eps):
         raise TypeError(f"G must be float32, float16 or bfloat16, got {G.dtype}")
     b = G.shape[0] if G.dim() == 3 else 1
     a0, b0, c0 = (float(x) for x in coefficients)
-    p = PolarParams(batch=b, m=G.shape[-2], n=G.shape[-1], dtype=DTYPES[G.dtype],
-                    steps=int(steps), a=a0, b=b0, c=c0, reserved=0, eps=float(eps))
-    ws, nb = _workspace(int(lib().gpic_polar_workspace_bytes(C.byref(p))), G.device)
-    return p, ws, nb
+    p = PolarParams(b, G.shape[-2], G.shape[-1], DTYPES[G.dtype], int(steps), a0, b0, c0, 0,
+                    float(eps))
+    ref = C.byref(p)
+    ws, nb = _workspace(lib().gpic_polar_workspace_bytes(ref), G.device)
+    return ref, ws, nb
 
 
 def gpic_orthogonalize(G: torch.Tensor, steps: int = 5, coefficients=POLAR_COEFFICIENTS,
@@ -833,8 +852,8 @@ def gpic_orthogonalize(G: torch.Tensor, steps: int = 5, coefficients=POLAR_COEFF
         if out.shape != G.shape or out.device != G.device or not out.is_contiguous():
             raise ValueError("O must be contiguous, of G's shape and on its device")
     G = G.contiguous()
-    p, ws, nb = _polar(G, steps, coefficients, eps)
-    _check(lib().gpic_orthogonalize(C.byref(p), _ptr(G), _ptr(out), _ptr(ws), nb,
+    ref, ws, nb = _polar(G, steps, coefficients, eps)
+    _check(lib().gpic_orthogonalize(ref, G.data_ptr(), out.data_ptr(), _at(ws), nb,
                                     _stream(G.device)))
     return out
 
@@ -860,11 +879,11 @@ def gpic_muon_step(W: torch.Tensor, G: torch.Tensor, M: torch.Tensor, lr: float,
     m, n = W.shape[-2:]
     if scale is None:
         scale = max(1.0, m / max(n, 1)) ** 0.5
-    p, ws, nb = _polar(W, steps, coefficients, eps)
-    h = MuonParams(lr=float(lr), momentum=float(momentum), weight_decay=float(weight_decay),
-                   scale=float(scale), nesterov=int(bool(nesterov)), reserved=0)
-    _check(lib().gpic_muon_step(C.byref(p), C.byref(h), _ptr(W), _ptr(G), _ptr(M), _ptr(ws), nb,
-                                _stream(W.device)))
+    ref, ws, nb = _polar(W, steps, coefficients, eps)
+    h = MuonParams(float(lr), float(momentum), float(weight_decay), float(scale),
+                   int(bool(nesterov)), 0)
+    _check(lib().gpic_muon_step(ref, C.byref(h), W.data_ptr(), G.data_ptr(), M.data_ptr(), _at(ws),
+                                nb, _stream(W.device)))
 
 
 # ----------------------------------------------- whole paths (call chains)

@@ -11,7 +11,7 @@ namespace gpic {
 
 namespace {
 
-constexpr int kMaxParts = 256;        // partial maxima per matrix
+constexpr int kMaxParts = 1024;       // partial maxima per matrix
 constexpr int kSumRows = 64;          // rows of a partial column sum
 
 inline size_t up(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -82,7 +82,10 @@ __global__ __launch_bounds__(256) void absmax_kernel(MaxJobs jobs)
 // The block's largest of the kMaxParts partial maxima (256 threads).
 __device__ __forceinline__ float join_max(const float *part)
 {
-    float best = part[threadIdx.x];
+    float best = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kMaxParts / 256; ++i)
+        best = fmaxf(best, part[i * 256 + threadIdx.x]);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1)
         best = fmaxf(best, __shfl_xor(best, o, 64));

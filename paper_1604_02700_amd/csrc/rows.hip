@@ -7,6 +7,8 @@
 // operand and up to 32 rows of X as the second.  The waves' sums meet in
 // LDS and are added in wave order.  float32 uses the float32 matrix
 // instruction (the operands are not split: reading them is what counts).
+#include <type_traits>
+
 #include "encoder.h"
 
 namespace gpic {
@@ -22,15 +24,15 @@ struct RowArgs {
     int act;
 };
 
-// 16 bytes of a row from value k on, zeros beyond K; any alignment
-template <int DT>
+// 16 bytes of a row from value k on; any alignment.  LAST: zeros beyond K.
+template <int DT, bool LAST>
 __device__ __forceinline__ u32x4 chunk_at(const void *row, int64_t k, int64_t K)
 {
     constexpr int kSize = DT == GPIC_F32 ? 4 : 2, kValues = 16 / kSize;
     using loose = u32x4 __attribute__((aligned(2)));
     using loose4 = u32x4 __attribute__((aligned(4)));
     const char *p = static_cast<const char *>(row) + k * kSize;
-    if (k + kValues <= K) {
+    if (!LAST || k + kValues <= K) {
         if (DT == GPIC_F32)
             return *reinterpret_cast<const loose4 *>(p);
         return *reinterpret_cast<const loose *>(p);
@@ -94,20 +96,20 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(RowArgs a)
         for (int b = 0; b < NB; ++b)
             acc[i][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     u32x4 fw[kG][kUnroll], fx[NB][kUnroll];
-    auto load = [&](int64_t k0) {
+    auto load = [&](int64_t k0, auto last) {
+        constexpr bool kLast = decltype(last)::value;
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
             const int64_t k = k0 + u * 4 * kValues + g * kValues;
 #pragma unroll
             for (int i = 0; i < kG; ++i)
-                fw[i][u] = chunk_at<DT>(w[i], k, a.k);
+                fw[i][u] = chunk_at<DT, kLast>(w[i], k, a.k);
 #pragma unroll
             for (int b = 0; b < NB; ++b)
-                fx[b][u] = chunk_at<DT>(x[b], k, a.k);
+                fx[b][u] = chunk_at<DT, kLast>(x[b], k, a.k);
         }
     };
-    for (int64_t k0 = (int64_t)wave * kTurn; k0 < a.k; k0 += (int64_t)WAVES * kTurn) {
-        load(k0);
+    auto multiply = [&]() {
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u)
 #pragma unroll
@@ -115,6 +117,16 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(RowArgs a)
 #pragma unroll
                 for (int b = 0; b < NB; ++b)
                     acc[i][b] = mma16<DT>(fw[i][u], fx[b][u], acc[i][b]);
+    };
+    int64_t k0 = (int64_t)wave * kTurn;
+#pragma unroll 2
+    for (; k0 + kTurn <= a.k; k0 += (int64_t)WAVES * kTurn) {
+        load(k0, std::false_type{});
+        multiply();
+    }
+    if (k0 < a.k) {                    // the turn that the contraction ends in
+        load(k0, std::true_type{});
+        multiply();
     }
     __shared__ f32x4 part[WAVES][kG * NB][64];
 #pragma unroll
@@ -169,11 +181,14 @@ hipError_t launch_waves(const RowArgs &a, hipStream_t st)
     const int64_t blocks = (a.m + 15) / 16;
     if (blocks > 0x7fffffffll)
         return hipErrorInvalidValue;
-    // enough waves to keep every compute unit's loads in flight
-    if (blocks >= 512 || a.k <= 512)
+    // as many waves as there are turns: then all of W is on its way at once
+    const int64_t turns = (a.k + (DT == GPIC_F32 ? 63 : 127)) / (DT == GPIC_F32 ? 64 : 128);
+    if (turns <= 4)
         few_rows_kernel<DT, GATED, NB, 4><<<(unsigned)blocks, 256, 0, st>>>(a);
-    else
+    else if (turns <= 8 || (GATED && NB == 2))
         few_rows_kernel<DT, GATED, NB, 8><<<(unsigned)blocks, 512, 0, st>>>(a);
+    else
+        few_rows_kernel<DT, GATED, NB, 16><<<(unsigned)blocks, 1024, 0, st>>>(a);
     return hipGetLastError();
 }
 
