@@ -74,7 +74,9 @@ def _close(got, ref, bound, dtype, what):
 # the middle and the large tile
 SHAPES = [(1, 8, 8), (1, 2048, 520), (3, 5, 7), (7, 1000, 777), (17, 64, 64), (64, 64, 64),
           (65, 33, 129), (40, 4099, 40), (130, 72, 200), (257, 136, 300), (2100, 96, 1800),
-          (4100, 72, 3333)]
+          (4100, 72, 3333),
+          # whole and split tiles of the middle and the large size, in every operand order
+          (4099, 1003, 4200), (2600, 2900, 1400), (6000, 3200, 2800), (4300, 4100, 4300)]
 
 
 @pytest.mark.parametrize("dtype", list(T))
@@ -269,6 +271,76 @@ def test_outlier_row_float32(g):
            _product_error(X.double(), W.double(), "f32"), "f32", "Y")
 
 
+def test_offsets_beyond_32_bits(g):
+    """n m > 2^32 values of Y, Z, dY and dZ: the rows on both sides of every
+    power of two, and the gradients of the weights and the bias in chunks."""
+    n, k, m = 525000, 24, 8200
+    print(f"linear n={n} m={m} ({n * m} values)", flush=True)
+    X, W, b = _randn((n, k), "bf16", 1), _randn((m, k), "bf16", 2, k ** -0.5), _randn((m,), "bf16", 3)
+    Y, Z = g.gpic_linear(X, W, b, "gelu", want_pre=True)
+    gr = g.gpic_linear_backward(Y, X, W, Z, "gelu")
+    w = W.double()
+    rows = sorted({r for p in range(30, 33) for d in (-1, 0, 1) for r in [2 ** p // m + d] if r < n}
+                  | {0, 1, n - 2, n - 1})
+    x = X[rows].double()
+    z = x @ w.t() + b.double()
+    pe = _product_error(x, w, "bf16") + 2 * E * z.abs()
+    _close(Z[rows], z, pe, "bf16", "Z")
+    _close(Y[rows], _act(z, "gelu")[0], 1.13 * pe + 2e-7 * z.abs(), "bf16", "Y")
+    dy, zz = Y[rows].double(), Z[rows].double()
+    dz = dy * _act(zz, "gelu")[1]
+    off = U["bf16"] * dz.abs() + 1e-6 * dy.abs() * (1 + zz.abs())
+    _close(gr.dX[rows], dz @ w, off @ w.abs() + _product_error(dz, w.t(), "bf16"), "bf16", "dX")
+    dW = torch.zeros((m, k), dtype=torch.float64, device=DEV)
+    size, off, db, dba = torch.zeros_like(dW), torch.zeros_like(dW), 0.0, 0.0
+    for r in range(0, n, 35000):
+        zz, dy, x = Z[r:r + 35000].double(), Y[r:r + 35000].double(), X[r:r + 35000].double()
+        dz = dy * _act(zz, "gelu")[1]
+        dW += dz.t() @ x
+        size += dz.abs().t() @ x.abs()
+        db, dba = db + dz.sum(0), dba + (dy.abs() * (1 + zz.abs())).sum(0)
+        del zz, dy, dz, x
+    # sums of n values in float32: rounding errors of n partial sums, of
+    # random sign, 4 sqrt(n) of them at the most likely worst
+    _close(gr.dW, dW, (U["bf16"] + 1e-6 + 4 * math.sqrt(n) * E) * size, "bf16", "dW")
+    _close(gr.db, db, (1e-6 + 70 * E) * dba, "bf16", "db")
+
+
+def test_binding_refusals(g):
+    x = lambda *s, dt=torch.float32: torch.zeros(s, dtype=dt, device=DEV)  # noqa: E731
+    X, W = x(5, 8), x(6, 8)
+    bad = [
+        (ValueError, lambda: g.gpic_linear(X, x(6, 7))),
+        (ValueError, lambda: g.gpic_linear(x(8), W)),
+        (ValueError, lambda: g.gpic_linear(X, W, activation="tanh")),
+        (ValueError, lambda: g.gpic_linear(X, W, x(5))),
+        (ValueError, lambda: g.gpic_linear(X, W, residual=x(5, 7))),
+        (ValueError, lambda: g.gpic_linear(X, W, Y=x(6, 5).t())),
+        (ValueError, lambda: g.gpic_linear(X, W.cpu().to(DEV), Y=x(4, 6))),
+        (TypeError, lambda: g.gpic_linear(X, W.half())),
+        (TypeError, lambda: g.gpic_linear(X.double(), W.double())),
+        (TypeError, lambda: g.gpic_linear(X, W, x(6, dt=torch.float16))),
+        (ValueError, lambda: g.gpic_gated(X, x(7, 8))),
+        (ValueError, lambda: g.gpic_linear_backward(x(5, 6), X, W, None, "gelu")),
+        (ValueError, lambda: g.gpic_linear_backward(x(5, 5), X, W)),
+        (TypeError, lambda: g.gpic_gated_backward(x(5, 3).half(), X.half(), W.half(), x(5, 6).half())),
+        (ValueError, lambda: g.gpic_gated_backward(x(5, 3), X, W, x(5, 5))),
+        (ValueError, lambda: g.gpic_orthogonalize(x(5))),
+        (TypeError, lambda: g.gpic_orthogonalize(x(5, 4).double())),
+        (ValueError, lambda: g.gpic_orthogonalize(x(5, 4), O=x(4, 5).t())),
+        (ValueError, lambda: g.gpic_muon_step(W, x(6, 7), x(6, 8), 0.1)),
+        (TypeError, lambda: g.gpic_muon_step(W.half(), W.half(), W.half(), 0.1)),
+        (ValueError, lambda: g.gpic_muon_step(x(8, 6).t(), W, x(6, 8), 0.1)),
+        (g.GpicError, lambda: g.gpic_orthogonalize(x(5, 4), steps=0)),
+        (g.GpicError, lambda: g.gpic_orthogonalize(x(5, 4), coefficients=(20.0, 0.0, 0.0))),
+        (g.GpicError, lambda: g.gpic_muon_step(W, W.clone(), x(6, 8), float("nan"))),
+    ]
+    for i, (kind, call) in enumerate(bad):
+        with pytest.raises(kind):
+            call()
+            pytest.fail(f"case {i} was accepted")
+
+
 # ------------------------------------------------- orthogonalised updates
 COEF = (3.4445, -4.7750, 2.0315)
 
@@ -308,7 +380,8 @@ def _rel(got, ref):
 
 STACKS = [(1, 1, 1), (2, 1, 7), (2, 9, 1), (1, 16, 16), (12, 64, 256), (3, 256, 64), (5, 100, 300),
           (2, 513, 129), (3, 65, 65), (1, 300, 1000), (2, 20, 4100), (1, 2000, 33),
-          (1, 1100, 1500), (1, 2500, 1025)]
+          (1, 1100, 1500), (1, 2500, 1025), (1, 30, 1024), (4, 64, 448), (2, 448, 63), (1, 65, 448),
+          (3, 1500, 2100), (1, 4100, 2300), (1, 4000, 4100), (1, 5900, 6100)]
 
 
 @pytest.mark.parametrize("dtype", list(T))
