@@ -674,6 +674,12 @@ __global__ __launch_bounds__(T::kThreads) void product_kernel(ProductArgs a, int
             copy_next(1);
         read(0, 0);
     }
+    // The small tile's copies go out one by one between its few products (64
+    // to 512 tiles 10 % faster, K = 2,048); the middle tile's at once (spread,
+    // they cost it 7 %).
+    constexpr int kMma = T::kRM * T::kRN;
+    constexpr bool kSpread = kMma == SideA::kCopies + SideB::kCopies;
+    const uint32_t lds_wave = (uint32_t)wave * 1024;
     for (int64_t s = s0; s < s1; ++s) {
         const int cur = (int)(s - s0) & 1;
         read(cur, 1);
@@ -682,6 +688,31 @@ __global__ __launch_bounds__(T::kThreads) void product_kernel(ProductArgs a, int
         copies_done();
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
+        if (kSpread) {
+            // copies between the products; beyond the contraction they fill
+            // the buffer with what no product takes
+            const uint32_t to = lds0 + (uint32_t)cur * kBuf;
+            const u32x4 ra = pa.rsrc(), rb = pb.rsrc();
+            if (!SPLIT)
+                read(cur ^ 1, 0);
+#pragma unroll
+            for (int n = 0; n < kMma * (SPLIT ? 2 : 1); ++n) {
+                const int q = n / kMma, i = n % kMma / T::kRN, j = n % T::kRN;
+                const int ha = SPLIT ? q : 1, hb = SPLIT ? 1 - q : 1;
+                acc[i][j] = mma<OP>(fb[hb][j], fa[ha][i], acc[i][j]);
+                if (n < SideA::kCopies)
+                    sa.copy_one(ra, to + lds_wave * SideA::kCopies, n, kleft);
+                else if (n < SideA::kCopies + SideB::kCopies)
+                    sb.copy_one(rb, to + SideA::kBytes + lds_wave * SideB::kCopies,
+                                n - SideA::kCopies, kleft);
+            }
+            if (SPLIT)
+                read(cur ^ 1, 0);
+            pa.step();
+            pb.step();
+            kleft -= kStep;
+            continue;
+        }
         if (s + 2 < s1)
             copy_next(cur);
         if (SPLIT) {
@@ -694,7 +725,6 @@ __global__ __launch_bounds__(T::kThreads) void product_kernel(ProductArgs a, int
             interleave();
         }
     }
-
     finish_tile<T, OP, EPI>(a, w, acc, lds);
 }
 

@@ -18,7 +18,7 @@ struct TileCost {
 constexpr TileCost kCost[3] = {
     {256, 1, 10.0, {1.50}, 1.39},
     {128, 2, 5.0, {0.74, 1.06}, 1.25},
-    {64, 5, 3.0, {0.38, 0.52, 0.66, 0.78, 1.05}, 1.1},
+    {64, 5, 3.0, {0.38, 0.47, 0.63, 0.77, 1.03}, 1.1},
 };
 constexpr int kUnits = 256;
 constexpr double kJoin = 4.0;              // the join's launch
