@@ -27,16 +27,22 @@ using s16x4 = short __attribute__((ext_vector_type(4)));
 // one exponential, one reciprocal and seven multiply-adds, where the
 // library's erff costs about forty instructions and would take a quarter
 // of the time of a large layer's product.
-__device__ __forceinline__ void normal_cdf_pdf(float z, float &cdf, float &pdf)
+__device__ __forceinline__ void normal_tail(float z, float &tail, float &e)
 {
-    const float e = __builtin_amdgcn_exp2f(z * z * -0.72134752044448170f);
+    e = __builtin_amdgcn_exp2f(z * z * -0.72134752044448170f);
     const float t = __builtin_amdgcn_rcpf(1.0f + 0.23164189f * fabsf(z));
     float q = 0.53070271f;                      // half of the table's a_5 .. a_1
     q = q * t - 0.72657601f;
     q = q * t + 0.71070687f;
     q = q * t - 0.14224837f;
     q = q * t + 0.12741480f;
-    const float tail = q * t * e;               // Phi(-|z|)
+    tail = q * t * e;                           // Phi(-|z|)
+}
+
+__device__ __forceinline__ void normal_cdf_pdf(float z, float &cdf, float &pdf)
+{
+    float tail, e;
+    normal_tail(z, tail, e);
     cdf = z > 0.0f ? 1.0f - tail : tail;
     pdf = 0.39894228040143268f * e;
 }
@@ -53,12 +59,14 @@ __device__ __forceinline__ float activate(float z, int act)
     if (act == GPIC_ACT_RELU)
         return z > 0.0f || z != z ? z : 0.0f;
     if (act == GPIC_ACT_GELU) {
-        float c, p;
-        normal_cdf_pdf(z, c, p);
-        return z < -14.0f ? 0.0f : z * c;
+        // z Phi(z) = max(z, 0) - |z| Phi(-|z|); the bound keeps infinity times
+        // the tail's zero out, and is past where the tail is one
+        float tail, e;
+        normal_tail(z, tail, e);
+        return fmaxf(z, 0.0f) - fminf(fabsf(z), 14.5f) * tail;
     }
     if (act == GPIC_ACT_SILU)
-        return z < -104.0f ? 0.0f : z * sigmoidf(z);
+        return fmaxf(z, -104.0f) * sigmoidf(z);
     return z;
 }
 
@@ -258,10 +266,11 @@ hipError_t run_layer_backward(const Shape &s, bool gated, const void *dY, const 
                               void *ws, hipStream_t st);
 
 // ---------------------------------------------------------------- rows.hip
-// The forward layer of few rows, straight from the operands as they lie
-// (any pitch and alignment, no workspace).
+// The forward layer of few rows or a short contraction (as_rows), straight
+// from the operands as they lie (any pitch and alignment, no workspace).
 constexpr int kFewRows = 32;
-hipError_t run_few_rows(const Shape &s, bool gated, const void *X, const void *W,
+bool as_rows(const Shape &s);
+hipError_t run_rows(const Shape &s, bool gated, const void *X, const void *W,
                         const void *bias, const void *res, void *Y, void *Z, hipStream_t st);
 
 // ------------------------------------------------------ orthogonalize.hip

@@ -481,7 +481,7 @@ struct Forward {
     float *part = nullptr;
     Forward(const Shape &s, bool gated, const void *x, const void *w, Cursor &c)
     {
-        if (s.n <= kFewRows)
+        if (as_rows(s))
             return;
         const int64_t rows = gated ? 2 * s.m : s.m;
         X = Source{x, s.n, s.k, s.ldx, must_pack(s.dtype, s.k, s.ldx, s.aligned16)};
@@ -567,8 +567,8 @@ hipError_t run_layer(const Shape &s, bool gated, const void *X, const void *W, c
 {
     if (s.n == 0)
         return hipSuccess;
-    if (s.n <= kFewRows)
-        return run_few_rows(s, gated, X, W, bias, res, Y, Z, st);
+    if (as_rows(s))
+        return run_rows(s, gated, X, W, bias, res, Y, Z, st);
     Cursor c{static_cast<char *>(ws)};
     Forward f(s, gated, X, W, c);
     const Source *list[2] = {&f.X, &f.W};

@@ -65,7 +65,7 @@ def test_layer_buffers_are_refused(g):
     assert L.gpic_gated_backward(p, d, d, d, None, d, d, *ws, None) == 1
     # few rows are read as they lie; more rows of float32 need packed copies
     assert L.gpic_layer_workspace_bytes(0, C.byref(_layer(g, dtype=0))) == 0
-    f = _layer(g, dtype=0, n=100)
+    f = _layer(g, dtype=0, n=100, k=80, ldx=80, ldw=80)
     need = L.gpic_layer_workspace_bytes(0, C.byref(f))
     assert need > 0
     assert L.gpic_linear(C.byref(f), d, d, None, None, d, None, d, need - 1, None) == 2
@@ -85,7 +85,7 @@ def test_layer_workspaces(g):
     for op in range(4):
         for dt in range(3):
             def size(n, **kw):
-                w = dict(ldx=16, ldw=16, ldy=24, ldz=48)
+                w = dict(k=80, ldx=80, ldw=80, ldy=24, ldz=48)
                 w.update(kw)
                 return L.gpic_layer_workspace_bytes(op, C.byref(_layer(g, n=n, dtype=dt, **w)))
             if dt == 0 or op in (1, 3):
@@ -94,6 +94,12 @@ def test_layer_workspaces(g):
                 assert size(1000) == size(10 ** 6) == 0          # read as they lie
             # operands that may start anywhere are copied
             assert size(10 ** 6, aligned16=0) >= 10 ** 6 * 2 * 16
+            # short contractions are read as they lie: float32 up to 32 values
+            # or 2^23 results, 16 bits up to 64
+            if op in (0, 2):
+                assert size(10 ** 6, k=32, aligned16=0) == 0
+                assert size(2 ** 23 // 24, k=64, aligned16=0) == 0
+                assert (size(10 ** 6, k=64) > 0) == (dt == 0)
     assert L.gpic_layer_workspace_bytes(4, C.byref(_layer(g))) == 0
     assert L.gpic_layer_workspace_bytes(0, None) == 0
 

@@ -148,6 +148,60 @@ def test_gated_and_gradients(g, shape, dtype):
                dtype, "dW")
 
 
+# up to 64 values of k (read as they lie, in pieces of 16 bytes): every number
+# of pieces, ends inside one, and k shorter than one
+@pytest.mark.parametrize("dtype", list(T))
+@pytest.mark.parametrize("k", [1, 3, 4, 7, 8, 11, 16, 17, 31, 32, 33, 40, 47, 49, 63, 64])
+def test_short_contractions(g, k, dtype):
+    for n, m, act in ((33, 1, "silu"), (100, 5, "none"), (50, 70, "gelu"), (1000, 128, "relu"),
+                      (70, 8200, "gelu"), (9000, 37, "silu")):
+        print(f"short n={n} k={k} m={m} {dtype} {act}", flush=True)
+        # rows of a wider matrix, starting anywhere
+        X = _randn((n, k + 3), dtype, 1)[:, 2:k + 2]
+        W = _randn((2 * m, k + 1), dtype, 2, k ** -0.5)[:, 1:]
+        b, R = _randn((m,), dtype, 3), _randn((n, m), dtype, 4)
+        x, w = X.double(), W.double()
+        Y, Z = g.gpic_linear(X, W[:m], b, act, R, want_pre=True)
+        assert torch.equal(Y, g.gpic_linear(X, W[:m], b, act, R, Y=R.clone()))
+        z = x @ w[:m].t() + b.double()
+        pe = _product_error(x, w[:m], dtype) + 2 * E * z.abs()
+        a, _ = _act(z, act)
+        ref = a + R.double()
+        _close(Z, z, pe, dtype, "Z")
+        _close(Y, ref, 1.13 * pe + 2e-7 * z.abs() + 4 * E * (a.abs() + ref.abs()), dtype, "Y")
+        H, Z = g.gpic_gated(X, W, "silu", want_pre=True)
+        assert torch.equal(H, g.gpic_gated(X, W, "silu"))
+        z = x @ w.t()
+        pe = _product_error(x, w, dtype)
+        _close(Z, z, pe, dtype, "gated Z")
+        a, _ = _act(z[:, :m], "silu")
+        u = z[:, m:]
+        _close(H, a * u, (1.13 * pe[:, :m] + 2e-7 * z[:, :m].abs()) * (u.abs() + pe[:, m:])
+               + a.abs() * pe[:, m:] + 4 * E * (a * u).abs(), dtype, "H")
+
+
+def test_short_contraction_of_a_large_float32_result(g):
+    """Beyond 32 values of k and 2^23 results float32 goes through the tiles."""
+    for n, k, m in ((4100, 48, 2100), (4100, 64, 2100)):
+        X, W = _randn((n, k), "f32", 1), _randn((m, k), "f32", 2, k ** -0.5)
+        x, w = X.double(), W.double()
+        _close(g.gpic_linear(X, W), x @ w.t(), _product_error(x, w, "f32"), "f32", "Y")
+
+
+@pytest.mark.parametrize("dtype", list(T))
+def test_short_contractions_keep_non_finite_values(g, dtype):
+    """What a fragment reads twice at the end of k is not counted twice."""
+    for k in (5, 9, 33):
+        X, W = _randn((40, k), dtype, 1), _randn((20, k), dtype, 2)
+        X[3, k - 1], X[4, k - 2], X[5, 0] = math.inf, -math.inf, math.nan
+        Y = g.gpic_linear(X, W).float()
+        keep = torch.tensor([i for i in range(40) if i not in (3, 4, 5)], device=DEV)
+        assert bool(torch.isfinite(Y[keep]).all())
+        assert torch.equal(Y[3], W[:, k - 1].float() * math.inf)
+        assert torch.equal(Y[4], W[:, k - 2].float() * -math.inf)
+        assert bool(Y[5].isnan().all())
+
+
 @pytest.mark.parametrize("act", ["gelu", "silu"])
 def test_gradients_against_differences(g, act):
     """Directional derivatives of sum(c * Y) by central differences of the
