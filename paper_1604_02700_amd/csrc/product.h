@@ -588,6 +588,14 @@ __device__ __forceinline__ void finish_tile(const ProductArgs &a, const Work &w,
     }
 }
 
+// The middle and the small tile.  Several workgroups share a compute unit (2
+// of the middle, 5 of the small), so that one's barriers and epilogue lie
+// under another's products.  Middle: 4,096 squared times its transpose, upper
+// triangle (528 tiles, 71 GFLOP), 89 us, matrix pipe busy 35 %, a quarter of
+// the waves' cycles spent waiting; small: 10,007 x 1,000 -> 777 in float32 (2,041
+// tiles, 47 GFLOP of half products) 81 us, pipe busy 28 %: bound by the reads
+// of fragments (a fragment feeds 4 instructions, 2 in the small tile) and by
+// the last round's idle units.
 template <class T, bool ASTR, bool BSTR, int OP, int EPI>
 __global__ __launch_bounds__(T::kThreads) void product_kernel(ProductArgs a, int tm, int tn)
 {
@@ -740,8 +748,11 @@ __global__ __launch_bounds__(T::kThreads) void product_kernel(ProductArgs a, int
 // has been read by every wave: copies run two steps ahead, into that place.
 // 8,192 cubed in bfloat16: 930 to 1,020 us, box to box (1.08 to 1.18
 // PFLOP/s), matrix pipe busy 64 % at the 1.6 to 1.85 GHz that the card's power
-// leaves; leaving the barriers or the waits out (a timing copy) gains 2 %,
-// the copies or the fragment reads 20 % each.  Four waves of 128 x 128 gave 956, waves
+// leaves; the copies and the fragment reads cost about 20 % each (timed by
+// what is left without them).  16,384 x 8,192 -> 2,048 (the gradient of a layer's
+// inputs) 433 to 480 us, 1.15 to 1.27 PFLOP/s; 16,384 x 2,048 -> 8,192 with bias, gelu
+// and both results written 530 to 630 us, of which a tile's epilogue, during
+// which the unit's matrix pipe idles, is a quarter.  Four waves of 128 x 128 gave 956, waves
 // one barrier apart with reads before the products 1.06, one buffer step ahead
 // with all copies at its start 1.04.
 //   phase     multiplies   reads        copies (step t + 2)
