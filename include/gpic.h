@@ -445,9 +445,13 @@ gpic_status gpic_read_stream(const float *x, int64_t n, double *sink, void *stre
  * have one type.  Sums are float32 or wider.  float32 matrices are
  * multiplied as two half-precision parts (22 significant bits, one power of
  * two per matrix from its largest finite magnitude, so entries down to 2^-17
- * of it keep all 22).  Forward layers of up to 32 rows or of up to 64 inputs
- * (float32: up to 32, or up to 64 and 2^23 results) are multiplied as they
- * lie, float32 in float32, without a workspace.  A NaN or an infinity in a row of X (a column's
+ * of it keep all 22).  Small calls read the
+ * matrices as they lie, without a workspace, and multiply float32 in float32:
+ * forward layers of up to 32 rows, of up to 64 inputs (float32: up to 32, or
+ * up to 64 and 2^23 results), or of up to 2,048 rows with n k m (gated: twice
+ * that) up to 2^27 (float32: 2^28); gradients with n and m (gated: 2 m) up to
+ * 2,048 and n k m (gated: twice that) up to 2^28 in float32, and in 16 bits up
+ * to 2^26 with n and m (gated: 2 m) up to 1,024, else 2^22.  A NaN or an infinity in a row of X (a column's
  * weights) makes that row (column) of the result non-finite and no other.
  * Results are bitwise reproducible.  Asynchronous. */
 
@@ -500,7 +504,7 @@ gpic_status gpic_linear(const gpic_layer_params *p, const void *X, const void *W
  * may be null (not wanted).  Z may be null without an activation.  dZ is
  * rounded to the matrices' type for the products (float16: times a power of
  * two from the largest finite |dY|, so that small gradients keep their bits;
- * db sums it unrounded).
+ * db sums it unrounded; small calls do not round it).
  * With n = 0, dW and db are zeros.
  * ws: gpic_layer_workspace_bytes(GPIC_LAYER_BACKWARD, p). */
 gpic_status gpic_linear_backward(const gpic_layer_params *p, const void *dY, const void *X,

@@ -266,12 +266,20 @@ hipError_t run_layer_backward(const Shape &s, bool gated, const void *dY, const 
                               void *ws, hipStream_t st);
 
 // ---------------------------------------------------------------- rows.hip
-// The forward layer of few rows or a short contraction (as_rows), straight
+// The forward layer of few rows, a short contraction or little work (as_rows), straight
 // from the operands as they lie (any pitch and alignment, no workspace).
 constexpr int kFewRows = 32;
-bool as_rows(const Shape &s);
+bool as_rows(const Shape &s, bool gated);
 hipError_t run_rows(const Shape &s, bool gated, const void *X, const void *W,
                         const void *bias, const void *res, void *Y, void *Z, hipStream_t st);
+
+// ------------------------------------------------------ small_gradients.hip
+// The gradients of a small layer (small_gradients) in one launch, straight
+// from the operands as they lie, without a workspace.
+bool small_gradients(const Shape &s, bool gated);
+hipError_t run_small_gradients(const Shape &s, bool gated, const void *dY, const void *X,
+                               const void *W, const void *Z, void *dX, void *dW, void *db,
+                               hipStream_t st);
 
 // ------------------------------------------------------ orthogonalize.hip
 struct Polar {

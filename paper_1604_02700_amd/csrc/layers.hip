@@ -489,7 +489,7 @@ struct Forward {
     float *part = nullptr;
     Forward(const Shape &s, bool gated, const void *x, const void *w, Cursor &c)
     {
-        if (as_rows(s))
+        if (as_rows(s, gated))
             return;
         const int64_t rows = gated ? 2 * s.m : s.m;
         X = Source{x, s.n, s.k, s.ldx, must_pack(s.dtype, s.k, s.ldx, s.aligned16)};
@@ -563,6 +563,8 @@ struct Backward {
 size_t layer_ws(const Shape &s, bool gated, bool backward)
 {
     Cursor c{nullptr};
+    if (backward && small_gradients(s, gated))
+        return 0;
     if (backward)
         Backward b(s, gated, nullptr, nullptr, nullptr, c);
     else
@@ -575,7 +577,7 @@ hipError_t run_layer(const Shape &s, bool gated, const void *X, const void *W, c
 {
     if (s.n == 0)
         return hipSuccess;
-    if (as_rows(s))
+    if (as_rows(s, gated))
         return run_rows(s, gated, X, W, bias, res, Y, Z, st);
     Cursor c{static_cast<char *>(ws)};
     Forward f(s, gated, X, W, c);
@@ -616,6 +618,8 @@ hipError_t run_layer_backward(const Shape &s, bool gated, const void *dY, const 
                               const void *W, const void *Z, void *dX, void *dW, void *db, void *ws,
                               hipStream_t st)
 {
+    if (small_gradients(s, gated))
+        return run_small_gradients(s, gated, dY, X, W, Z, dX, dW, db, st);
     Cursor c{static_cast<char *>(ws)};
     Backward b(s, gated, dY, X, W, c);
     const int op = kind_of(s.dtype);

@@ -1,5 +1,6 @@
 // The layers' forward pass where a tiled product would not pay: few rows
-// (few_rows_kernel), and many rows of a short contraction (short_kernel).
+// (few_rows_kernel; small layers too), and many rows of a short contraction
+// (short_kernel).
 //
 // Few rows (serving single points) are bound by reading W once.  A workgroup takes 16 columns of the output (gated: 16 of
 // the gate's and the same 16 of the up projection's); its waves share the
@@ -82,7 +83,7 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(RowArgs a)
     constexpr int kUnroll = 4, kTurn = 4 * kValues * kUnroll;
     constexpr int kG = GATED ? 2 : 1;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, r = lane & 15;
-    const int64_t col0 = (int64_t)blockIdx.x * 16;
+    const int64_t col0 = (int64_t)blockIdx.x * 16, row0 = (int64_t)blockIdx.y * (16 * NB);
     // rows beyond the last are read as the last one and not stored
     const char *w[kG], *x[NB];
     constexpr int kSize = DT == GPIC_F32 ? 4 : 2;
@@ -93,7 +94,7 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(RowArgs a)
     }
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
-        const int row = b * 16 + r < a.n ? b * 16 + r : a.n - 1;
+        const int64_t row = row0 + b * 16 + r < a.n ? row0 + b * 16 + r : a.n - 1;
         x[b] = static_cast<const char *>(a.X) + row * a.ldx * kSize;
     }
     f32x4 acc[kG][NB];
@@ -145,7 +146,7 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(RowArgs a)
     // wave b finishes rows 16 b .. 16 b + 15: a lane four columns of one row
     if (wave >= NB)
         return;
-    const int row = wave * 16 + r;
+    const int64_t row = row0 + wave * 16 + r;
     f32x4 v[kG];
 #pragma unroll
     for (int i = 0; i < kG; ++i) {
@@ -185,17 +186,15 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(RowArgs a)
 template <int DT, bool GATED, int NB>
 hipError_t launch_waves(const RowArgs &a, hipStream_t st)
 {
-    const int64_t blocks = (a.m + 15) / 16;
-    if (blocks > 0x7fffffffll)
-        return hipErrorInvalidValue;
+    const dim3 blocks((unsigned)((a.m + 15) / 16), (unsigned)((a.n + 16 * NB - 1) / (16 * NB)));
     // as many waves as there are turns: then all of W is on its way at once
     const int64_t turns = (a.k + (DT == GPIC_F32 ? 63 : 127)) / (DT == GPIC_F32 ? 64 : 128);
     if (turns <= 4)
-        few_rows_kernel<DT, GATED, NB, 4><<<(unsigned)blocks, 256, 0, st>>>(a);
+        few_rows_kernel<DT, GATED, NB, 4><<<blocks, 256, 0, st>>>(a);
     else if (turns <= 8 || (GATED && NB == 2))
-        few_rows_kernel<DT, GATED, NB, 8><<<(unsigned)blocks, 512, 0, st>>>(a);
+        few_rows_kernel<DT, GATED, NB, 8><<<blocks, 512, 0, st>>>(a);
     else
-        few_rows_kernel<DT, GATED, NB, 16><<<(unsigned)blocks, 1024, 0, st>>>(a);
+        few_rows_kernel<DT, GATED, NB, 16><<<blocks, 1024, 0, st>>>(a);
     return hipGetLastError();
 }
 
@@ -440,23 +439,29 @@ hipError_t launch_short(RowArgs a, hipStream_t st)
 template <int DT>
 hipError_t launch_either(const RowArgs &a, bool gated, hipStream_t st)
 {
-    if (a.n > kFewRows)
+    if (a.n > kFewRows && a.k <= 64)
         return gated ? launch_short<DT, true>(a, st) : launch_short<DT, false>(a, st);
     return launch_rows<DT>(a, gated, st);
 }
 
 } // namespace
 
-// Few rows, or up to 64 values of k: the layer's results outweigh its
-// products.  float32 beyond 32 values: only small results, for the float32
-// matrix instruction then costs more than packed operands' two launches
-// (gelu, us, here and as a tiled product: 1,003 x 64 -> 700 6.9 and 12.6, 50,000
-// x 64 -> 256 38 and 38, 16,384 x 64 -> 8,192 240 and 194; 16,384 x 32 -> 8,192 177 and
-// 176; bfloat16 107 and 150).
-bool as_rows(const Shape &s)
+// Few rows, or up to 64 values of k, where a layer's results outweigh its
+// products, or little work, where launches do (32 rows at a time then).
+// float32 beyond 32 values of k only for small results: the float32 matrix
+// instruction then costs more than packed operands' two launches.  gelu, us,
+// here and as a tiled product: 1,003 x 64 -> 700 6.9 and 12.6, 50,000 x 64 -> 256 38
+// and 38, 16,384 x 64 -> 8,192 240 and 194, 16,384 x 32 -> 8,192 177 and 176 (bfloat16
+// 107 and 150); 52 x 512 -> 123 5.4 and 16, 200 x 300 -> 700 5.8 and 16.2 (bfloat16 5.9
+// and 9.7), 100 x 1,000 -> 1,000 7.7 and 21 (4.9 and 10), 1,003 x 300 -> 700 14 and 17.3
+// (12.4 and 10.3), 2,000 x 700 -> 700 47 and 28 (34 and 16).
+bool as_rows(const Shape &s, bool gated)
 {
-    return s.n <= kFewRows || s.k <= 32 ||
-           (s.k <= 64 && (s.dtype != GPIC_F32 || s.n * s.m <= (1 << 23)));
+    const bool f32 = s.dtype == GPIC_F32;
+    const int64_t rows = gated ? 2 * s.m : s.m;
+    if (s.n <= kFewRows || s.k <= 32 || (s.k <= 64 && (!f32 || s.n * rows <= (1 << 23))))
+        return true;
+    return s.n <= 2048 && s.n * rows <= ((int64_t)1 << (f32 ? 28 : 27)) / s.k;
 }
 
 hipError_t run_rows(const Shape &s, bool gated, const void *X, const void *W,

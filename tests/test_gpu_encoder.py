@@ -202,6 +202,70 @@ def test_short_contractions_keep_non_finite_values(g, dtype):
         assert bool(Y[5].isnan().all())
 
 
+# small gradients (one launch, dZ unrounded): ends of tiles of 16 and 64, one row, one
+# column, contractions of one turn and of many, waves with nothing to do
+SMALL = [(1, 1, 1), (2, 58, 588), (3, 65, 17), (16, 64, 16), (33, 100, 5), (50, 512, 123),
+         (100, 1, 130), (130, 7, 500), (257, 80, 33), (1000, 33, 16), (1024, 20, 300),
+         (200, 300, 512)]
+
+
+@pytest.mark.parametrize("dtype", list(T))
+@pytest.mark.parametrize("shape", SMALL, ids=str)
+def test_small_gradients(g, shape, dtype):
+    n, k, m = shape
+    X = _randn((n, k + 3), dtype, 1)[:, 2:k + 2]
+    W = _randn((2 * m, k + 1), dtype, 2, k ** -0.5)[:, 1:]
+    dY = _randn((n, m + 5), dtype, 3)[:, 3:m + 3]
+    x, w, dy = X.double(), W.double(), dY.double()
+    for act in ("none", "relu", "gelu", "silu"):
+        print(f"small n={n} k={k} m={m} {dtype} {act}", flush=True)
+        Z = g.gpic_linear(X, W[:m], None, act, want_pre=True)[1]
+        gr = g.gpic_linear_backward(dY, X, W[:m], Z if act != "none" else None, act)
+        da = _act(Z.double(), act)[1]
+        dz = dy * da
+        off = 1e-6 * dy.abs() * (1 + Z.double().abs() * (act != "none"))
+        # sums in float32 of what is in hand, nothing else rounded
+        _close(gr.dX, dz @ w[:m], off @ w[:m].abs() + (m + 16) * E * (dz.abs() @ w[:m].abs()),
+               dtype, "dX")
+        _close(gr.dW, dz.t() @ x, off.t() @ x.abs() + (n + 16) * E * (dz.abs().t() @ x.abs()),
+               dtype, "dW")
+        _close(gr.db, dz.sum(0), off.sum(0) + (n + 16) * E * dz.abs().sum(0), dtype, "db")
+        for want in ((True, False, False), (False, True, False), (False, False, True)):
+            one = g.gpic_linear_backward(dY, X, W[:m], Z if act != "none" else None, act, *want)
+            for name, asked in zip(("dX", "dW", "db"), want):
+                got = getattr(one, name)
+                assert torch.equal(got, getattr(gr, name)) if asked else got is None
+    for act in ("silu", "relu"):
+        Z = g.gpic_gated(X, W, act, want_pre=True)[1]
+        gr = g.gpic_gated_backward(dY, X, W, Z, act)
+        z = Z.double()
+        a, da = _act(z[:, :m], act)
+        dz = torch.cat([dy * z[:, m:] * da, dy * a], 1)
+        off = 1e-6 * torch.cat([dy * z[:, m:], dy * z[:, :m]], 1).abs() \
+            * (1 + torch.cat([z[:, :m], z[:, :m]], 1).abs())
+        _close(gr.dX, dz @ w, off @ w.abs() + (2 * m + 16) * E * (dz.abs() @ w.abs()), dtype,
+               "gated dX")
+        _close(gr.dW, dz.t() @ x, off.t() @ x.abs() + (n + 16) * E * (dz.abs().t() @ x.abs()),
+               dtype, "gated dW")
+
+
+@pytest.mark.parametrize("dtype", list(T))
+def test_small_forward_of_many_rows(g, dtype):
+    """Rows in blocks of 32 through the few-row kernel."""
+    for n, k, m in ((33, 100, 17), (64, 65, 33), (500, 300, 100), (2048, 129, 70)):
+        X = _randn((n, k + 3), dtype, 1)[:, 2:k + 2]
+        W = _randn((2 * m, k + 1), dtype, 2, k ** -0.5)[:, 1:]
+        x, w = X.double(), W.double()
+        _close(g.gpic_linear(X, W), x @ w.t(), _product_error(x, w, dtype), dtype, "Y")
+        H, Z = g.gpic_gated(X, W, "relu", want_pre=True)
+        z = x @ w.t()
+        pe = _product_error(x, w, dtype)
+        _close(Z, z, pe, dtype, "Z")
+        a, u = z[:, :m].clamp(min=0), z[:, m:]
+        _close(H, a * u, pe[:, :m] * (u.abs() + pe[:, m:]) + a * pe[:, m:] + 4 * E * (a * u).abs(),
+               dtype, "H")
+
+
 @pytest.mark.parametrize("act", ["gelu", "silu"])
 def test_gradients_against_differences(g, act):
     """Directional derivatives of sum(c * Y) by central differences of the
