@@ -550,8 +550,9 @@ size_t gpic_polar_workspace_bytes(const gpic_polar_params *p);
  * then `steps` times X <- a X + (b A + c A^2) X with A = X X^T (X^T X on the
  * right for m > n): the singular vectors of G with its singular values
  * taken near 1.  O may be G.  A zero matrix gives zeros (with eps > 0).
- * float32 and float16 matrices in split halves; bfloat16 matrices with
- * half-precision products, to about 2e-3 of |O|.
+ * float32 and float16 matrices, and bfloat16 ones whose smaller side is up to
+ * 64, in split halves; other bfloat16 matrices with half-precision products,
+ * to about 2e-3 of |O|.
  * ws: gpic_polar_workspace_bytes(p).  Asynchronous. */
 gpic_status gpic_orthogonalize(const gpic_polar_params *p, const void *G, void *O, void *ws,
                                size_t ws_bytes, void *stream);

@@ -20,6 +20,10 @@
 //   there too, a gradient of low rank over noise comes out 1.4e-2 off, with
 //   8 bits 1.1e-1, so 1.1e-4 (512 x 2048, float64 reference); for Gaussian
 //   matrices the result is 1.2e-3 to 1.7e-3 off, below its final rounding.
+//   Up to 64 rows (columns) they are split as the others are: the fewer
+//   directions, the less the roundings average out (2.1e-3 off at 31 x
+//   7,489, 1.3e-3 at 64 x 7,489, the final rounding apart), and it costs 8 to
+//   14 us of 133 there, 23 us of 136 at 256 x 4,096.
 // The norm is summed in float64.
 #include "encoder.h"
 
@@ -28,6 +32,7 @@ namespace gpic {
 namespace {
 
 constexpr int kParts = 1024;           // partial sums of squares per matrix
+constexpr int64_t kSplitSide = 64;     // bfloat16: split operands up to this smaller side
 constexpr float kStore = 1024.0f;      // X, A, P are stored times this: entries of
                                        // X are <= 1.3, of P <= 64 for any coefficients
                                        // the entry points accept
@@ -179,7 +184,7 @@ struct Layout {
             at += up(b);
             return q;
         };
-        split = p.dtype != GPIC_BF16;
+        split = p.dtype != GPIC_BF16 || p.m <= kSplitSide || p.n <= kSplitSide;
         tall = p.m > p.n;
         r = tall ? p.n : p.m;
         len = tall ? p.m : p.n;

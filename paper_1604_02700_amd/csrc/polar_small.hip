@@ -1,5 +1,5 @@
 // Orthogonalised updates of small matrices in one launch (the larger ones:
-// orthogonalize.hip, same formulas, same parts): a workgroup holds its
+// orthogonalize.hip, same formulas, X, A and P in two parts whatever the type): a workgroup holds its
 // matrix in LDS as half-precision parts, X [R x LEN] on the smaller side (a
 // tall matrix is transposed on the way in and out), and does every step
 // there.  Bound by the LDS round trips between the barriers, 5.3 us a step at 64 x
@@ -63,27 +63,23 @@ __device__ __forceinline__ f32x4 halves_at(const _Float16 *p)
     return __builtin_convertvector(*reinterpret_cast<const half4 *>(p), f32x4);
 }
 
-// the parts of v (scaled already); LOW: the low one too
-template <bool LOW>
+// the parts of v (scaled already)
 __device__ __forceinline__ void put_parts(_Float16 *hi, _Float16 *lo, f32x4 v)
 {
     const half4 h = __builtin_convertvector(v, half4);
     *reinterpret_cast<half4 *>(hi) = h;
-    if (LOW)
-        *reinterpret_cast<half4 *>(lo) =
-            __builtin_convertvector(v - __builtin_convertvector(h, f32x4), half4);
+    *reinterpret_cast<half4 *>(lo) =
+        __builtin_convertvector(v - __builtin_convertvector(h, f32x4), half4);
 }
 
 template <int DT, bool STEP, int R, int LEN>
 __global__ __launch_bounds__(kThreads) void polar_small_kernel(SmallArgs a)
 {
-    // bfloat16: products of the high halves alone, the low ones of X beside
-    constexpr bool SPLIT = DT != GPIC_BF16;
     constexpr int kLd = LEN + 8, kLdr = R + 8, kTiles = (R / 16) * (R / 16);
     constexpr int kShare = R == 64 ? 2 : 4;      // waves per 32 x 32 block of A
     constexpr int kSumBytes = (kShare - 1) * R * R * 4, kPolyBytes = 2 * R * kLdr * 2;
     __shared__ __attribute__((aligned(16))) _Float16 xh[R * kLd], xl[R * kLd];
-    __shared__ __attribute__((aligned(16))) _Float16 ah[R * kLdr], al[SPLIT ? R * kLdr : 8];
+    __shared__ __attribute__((aligned(16))) _Float16 ah[R * kLdr], al[R * kLdr];
     __shared__ __attribute__((aligned(16))) char both[kSumBytes > kPolyBytes ? kSumBytes : kPolyBytes];
     __shared__ double norm[kWaves];
     float *sums = reinterpret_cast<float *>(both);
@@ -150,7 +146,7 @@ __global__ __launch_bounds__(kThreads) void polar_small_kernel(SmallArgs a)
         // four of one row, on their place
         const bool four = !tall && i + 4 <= size && (a.n & 3) == 0;
         if (four)
-            put_parts<true>(xh + i0 * kLd + i1, xl + i0 * kLd + i1, u[q] * inv);
+            put_parts(xh + i0 * kLd + i1, xl + i0 * kLd + i1, u[q] * inv);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             if (i + j < size && !four) {
@@ -188,19 +184,15 @@ __global__ __launch_bounds__(kThreads) void polar_small_kernel(SmallArgs a)
                 for (int e = 0; e < 2; ++e) {
                     hi[e] = rows_at(xh, kLd, ti + 16 * e, c);
                     hj[e] = rows_at(xh, kLd, tj + 16 * e, c);
-                    if (SPLIT) {
-                        li[e] = rows_at(xl, kLd, ti + 16 * e, c);
-                        lj[e] = rows_at(xl, kLd, tj + 16 * e, c);
-                    }
+                    li[e] = rows_at(xl, kLd, ti + 16 * e, c);
+                    lj[e] = rows_at(xl, kLd, tj + 16 * e, c);
                 }
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int x = e >> 1, y = e & 1;
                     acc[x][y] = mma_f16(hj[y], hi[x], acc[x][y]);
-                    if (SPLIT) {
-                        low[x][y] = mma_f16(lj[y], hi[x], low[x][y]);
-                        low[x][y] = mma_f16(hj[y], li[x], low[x][y]);
-                    }
+                    low[x][y] = mma_f16(lj[y], hi[x], low[x][y]);
+                    low[x][y] = mma_f16(hj[y], li[x], low[x][y]);
                 }
             }
 #pragma unroll
@@ -221,7 +213,7 @@ __global__ __launch_bounds__(kThreads) void polar_small_kernel(SmallArgs a)
                     for (int w = 0; w < kShare - 1; ++w)
                         acc[x][y] += *reinterpret_cast<const f32x4 *>(sums + (w * R + row) * R + col);
                     const int at = row * kLdr + col;
-                    put_parts<SPLIT>(ah + at, al + (SPLIT ? at : 0), acc[x][y] * (inv2 * kStore));
+                    put_parts(ah + at, al + at, acc[x][y] * (inv2 * kStore));
                 }
             }
             __syncthreads();
@@ -234,16 +226,12 @@ __global__ __launch_bounds__(kThreads) void polar_small_kernel(SmallArgs a)
             for (int c = 0; c < R; c += 32) {
                 const u32x4 bj = rows_at(ah, kLdr, tj, c), bi = rows_at(ah, kLdr, ti, c);
                 acc = mma_f16(bj, bi, acc);
-                if (SPLIT) {
-                    acc = mma_f16(rows_at(al, kLdr, tj, c), bi, acc);
-                    acc = mma_f16(bj, rows_at(al, kLdr, ti, c), acc);
-                }
+                acc = mma_f16(rows_at(al, kLdr, tj, c), bi, acc);
+                acc = mma_f16(bj, rows_at(al, kLdr, ti, c), acc);
             }
             const int at = (ti + m16) * kLdr + tj + n4;
-            f32x4 v = halves_at(ah + at);
-            if (SPLIT)
-                v += halves_at(al + at);
-            put_parts<SPLIT>(ph + at, pl + at, a.b * v + acc * (a.c * inv2 * kStore));
+            const f32x4 v = halves_at(ah + at) + halves_at(al + at);
+            put_parts(ph + at, pl + at, a.b * v + acc * (a.c * inv2 * kStore));
         }
         __syncthreads();
         // X <- a X + P X
@@ -253,8 +241,7 @@ __global__ __launch_bounds__(kThreads) void polar_small_kernel(SmallArgs a)
 #pragma unroll
             for (int c = 0; c < R / 32; ++c) {
                 bh[c] = columns_at(xh, kLd, col, 32 * c);
-                if (SPLIT)
-                    bl[c] = columns_at(xl, kLd, col, 32 * c);
+                bl[c] = columns_at(xl, kLd, col, 32 * c);
             }
             f32x4 v[R / 16];
 #pragma unroll
@@ -264,10 +251,8 @@ __global__ __launch_bounds__(kThreads) void polar_small_kernel(SmallArgs a)
                 for (int c = 0; c < R / 32; ++c) {
                     const u32x4 p = rows_at(ph, kLdr, 16 * i, 32 * c);
                     acc = mma_f16(bh[c], p, acc);
-                    if (SPLIT) {
-                        acc = mma_f16(bl[c], p, acc);
-                        acc = mma_f16(bh[c], rows_at(pl, kLdr, 16 * i, 32 * c), acc);
-                    }
+                    acc = mma_f16(bl[c], p, acc);
+                    acc = mma_f16(bh[c], rows_at(pl, kLdr, 16 * i, 32 * c), acc);
                 }
                 const int at = (16 * i + m16) * kLd + col + n4;
                 v[i] = a.a * (halves_at(xh + at) + halves_at(xl + at)) + acc * (inv2 * kStore);
@@ -276,7 +261,7 @@ __global__ __launch_bounds__(kThreads) void polar_small_kernel(SmallArgs a)
             for (int i = 0; i < R / 16; ++i) {
                 const int row = 16 * i + m16, at = row * kLd + col + n4;
                 if (!last) {
-                    put_parts<true>(xh + at, xl + at, v[i]);
+                    put_parts(xh + at, xl + at, v[i]);
                     continue;
                 }
                 if (row >= r)

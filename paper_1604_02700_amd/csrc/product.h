@@ -322,7 +322,9 @@ template <int OP, int EPI>
 __device__ __forceinline__ int out_type(const Epilogue &e)
 {
     if (EPI == kEpiResult)
-        return OP == kOpF16 ? GPIC_BF16 : (e.dtype == GPIC_F32 ? GPIC_F32 : GPIC_F16);
+        return OP == kOpF16 ? GPIC_BF16
+                            : (e.dtype == GPIC_F32 ? GPIC_F32
+                                                   : (e.dtype == GPIC_F16 ? GPIC_F16 : GPIC_BF16));
     return OP == kOpSplit ? GPIC_F32 : (OP == kOpF16 ? GPIC_F16 : GPIC_BF16);
 }
 

@@ -516,6 +516,15 @@ def test_orthogonalize(g, shape, dtype):
         assert _rel(g.gpic_orthogonalize(G[1])[None], _polar(G[1:2])) <= _polar_tolerance(dtype)
 
 
+@pytest.mark.parametrize("shape", [(2, 58, 45), (3, 64, 256), (2, 31, 1000), (2, 2489, 31),
+                                   (1, 64, 4000)], ids=str)
+def test_orthogonalize_few_directions_bf16(g, shape):
+    """A smaller side of up to 64: split operands, so the result's own rounding
+    (at most 2^-9 of an entry) and float32's 4e-5 are all."""
+    G = _gradient(shape, 11).to(torch.bfloat16)
+    assert _rel(g.gpic_orthogonalize(G), _polar(G)) <= 2.0 ** -9 + 4e-5
+
+
 @pytest.mark.parametrize("dtype", list(T))
 def test_orthogonalize_other_polynomials_and_ranks(g, dtype):
     G = _gradient((2, 96, 160), 5, floor=0.02).to(T[dtype])
