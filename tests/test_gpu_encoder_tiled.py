@@ -1,0 +1,309 @@
+"""The layers where they go through packed operands and the tiled product:
+the same questions as test_gpu_encoder.py asks of small calls (views,
+alignment, in-place results, non-finite rows, no rows, workspaces, streams,
+graphs, offsets past 32 bits), at sizes that the one-launch kernels do not
+take.  `_tiled` asserts that, so that a change of the rules that choose a
+kernel cannot take the sizes away.  Tolerances as there."""
+import ctypes as C
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+from test_gpu_encoder import DEV, E, T, U, _act, _close, _product_error, _randn  # noqa: E402
+
+N, K, M = 2100, 100, 140
+
+
+@pytest.fixture(scope="module")
+def g():
+    import paper_1604_02700_amd as g
+    g.lib()
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    return g
+
+
+def _tiled(g, op, n, k, m, dtype):
+    """Operands that may start anywhere are copied on the tiled path, and
+    read as they lie on the others: there is a workspace on that path only."""
+    rows = 2 * m if "gated" in op else m
+    p = g.LayerParams(n=n, k=k, m=m, ldx=k, ldw=k, ldy=m, ldr=m, ldz=rows,
+                      dtype=g.DTYPES[T[dtype]], activation=2, aligned16=0, reserved=0)
+    assert g.lib().gpic_layer_workspace_bytes(g.LAYER_OP[op], C.byref(p)) > 0, (op, n, k, m)
+
+
+def _all_tiled(g, n, k, m, dtype):
+    for op in g.LAYER_OP:
+        _tiled(g, op, n, k, m, dtype)
+
+
+def _wide(t, pad, first):
+    """t as columns of a wider table of NaN, with a row of it before and after."""
+    big = torch.full((t.shape[0] + 2, t.shape[1] + pad), float("nan"), dtype=t.dtype, device=DEV)
+    v = big[1:1 + t.shape[0], first:first + t.shape[1]]
+    v.copy_(t)
+    return v
+
+
+def _late(t):
+    """t in a buffer of NaN that starts one value before it."""
+    flat = torch.full((t.numel() + 1,), float("nan"), dtype=t.dtype, device=DEV)
+    v = flat[1:].view(t.shape)
+    v.copy_(t)
+    return v
+
+
+@pytest.mark.parametrize("dtype", list(T))
+@pytest.mark.parametrize("shape", [(2100, 96, 1800), (2101, 101, 137)], ids=str)
+def test_every_activation(g, shape, dtype):
+    n, k, m = shape
+    _all_tiled(g, n, k, m, dtype)
+    for act in ("none", "relu", "gelu", "silu"):
+        print(f"tiled n={n} k={k} m={m} {dtype} {act}", flush=True)
+        X, W = _randn((n, k), dtype, 1), _randn((2 * m, k), dtype, 2, k ** -0.5)
+        b, R, dY = _randn((m,), dtype, 3), _randn((n, m), dtype, 4), _randn((n, m), dtype, 5, 0.01)
+        x, w, dy = X.double(), W.double(), dY.double()
+        Y, Z = g.gpic_linear(X, W[:m], b, act, R, want_pre=True)
+        z = x @ w[:m].t() + b.double()
+        pe = _product_error(x, w[:m], dtype) + 2 * E * z.abs()
+        a = _act(z, act)[0]
+        ref = a + R.double()
+        _close(Z, z, pe, dtype, "Z")
+        _close(Y, ref, 1.13 * pe + 2e-7 * z.abs() + 4 * E * (a.abs() + ref.abs()), dtype, "Y")
+        gr = g.gpic_linear_backward(dY, X, W[:m], Z if act != "none" else None, act)
+        zz = Z.double()
+        dz = dy * _act(zz, act)[1]
+        off = (U[dtype] if act != "none" and dtype != "f32" else 0.0) * dz.abs() \
+            + 1e-6 * dy.abs() * (1 + zz.abs() * (act != "none"))
+        _close(gr.dX, dz @ w[:m], off @ w[:m].abs() + _product_error(dz, w[:m].t(), dtype), dtype,
+               "dX")
+        _close(gr.dW, dz.t() @ x, off.t() @ x.abs() + _product_error(dz.t(), x.t(), dtype), dtype,
+               "dW")
+        _close(gr.db, dz.sum(0), (1e-6 + 70 * E) * (dy.abs() * (1 + zz.abs())).sum(0), dtype, "db")
+
+        H, Z = g.gpic_gated(X, W, act, want_pre=True)
+        z = x @ w.t()
+        pe = _product_error(x, w, dtype)
+        _close(Z, z, pe, dtype, "gated Z")
+        a, u = _act(z[:, :m], act)[0], z[:, m:]
+        _close(H, a * u, (1.13 * pe[:, :m] + 2e-7 * z[:, :m].abs()) * (u.abs() + pe[:, m:])
+               + a.abs() * pe[:, m:] + 4 * E * (a * u).abs(), dtype, "H")
+        gr = g.gpic_gated_backward(dY, X, W, Z, act)
+        zz = Z.double()
+        a, da = _act(zz[:, :m], act)
+        dz = torch.cat([dy * zz[:, m:] * da, dy * a], 1)
+        off = (U[dtype] if dtype != "f32" else 0.0) * dz.abs() + 1e-6 * torch.cat(
+            [(dy * zz[:, m:]).abs() * (1 + zz[:, :m].abs()), (dy * zz[:, :m]).abs()], 1)
+        _close(gr.dX, dz @ w, off @ w.abs() + _product_error(dz, w.t(), dtype), dtype, "gated dX")
+        _close(gr.dW, dz.t() @ x, off.t() @ x.abs() + _product_error(dz.t(), x.t(), dtype), dtype,
+               "gated dW")
+
+
+@pytest.mark.parametrize("dtype", list(T))
+def test_views_and_alignment(g, dtype):
+    """Column and row slices, transposed operands, buffers that start one
+    value late: the same bits as the contiguous tensors."""
+    n, k, m = N, 104, 136
+    _all_tiled(g, n, k, m, dtype)
+    X, W, b, R = (_randn(s, dtype, i) for i, s in enumerate(((n, k), (2 * m, k), (m,), (n, m))))
+    W *= 0.1
+    Y, Z = g.gpic_linear(X, W[:m], b, "gelu", R, want_pre=True)
+    gr = g.gpic_linear_backward(R, X, W[:m], Z, "gelu")
+    plain = g.gpic_linear_backward(R, X, W[:m])
+    H, ZZ = g.gpic_gated(X, W, want_pre=True)
+    gg = g.gpic_gated_backward(R, X, W, ZZ)
+    for i, make in enumerate((lambda t: _wide(t, 24, 8), lambda t: _wide(t, 5, 3), _late,
+                              lambda t: t.t().contiguous().t())):
+        print(f"views {dtype} {i}", flush=True)
+        x, w, w2, r, z, zz = (make(t) for t in (X, W[:m], W, R, Z, ZZ))
+        out = torch.empty_like(R)
+        assert torch.equal(g.gpic_linear(x, w, _late(b[None])[0], "gelu", r, Y=out), Y)
+        for got, want in ((g.gpic_linear_backward(r, x, w, z, "gelu"), gr),
+                          (g.gpic_linear_backward(r, x, w), plain),
+                          (g.gpic_gated_backward(r, x, w2, zz), gg)):
+            assert torch.equal(got.dX, want.dX) and torch.equal(got.dW, want.dW)
+            assert want.db is None or torch.equal(got.db, want.db)
+        assert torch.equal(g.gpic_gated(x, w2), H)
+    # results in place of a strided residual, and among other columns
+    out = _wide(R, 7, 3)
+    table = out._base.clone()
+    assert torch.equal(g.gpic_linear(X, W[:m], b, "gelu", out, Y=out), Y)
+    after = out._base.clone()
+    after[1:1 + n, 3:3 + m] = table[1:1 + n, 3:3 + m]
+    assert torch.equal(after.isnan(), table.isnan())          # nothing beside it was written
+    out = _wide(torch.zeros_like(H), 3, 1)
+    assert torch.equal(g.gpic_gated(X, W, H=out), H)
+    assert bool(out._base[:, 0].isnan().all()) and bool(out._base[:, m + 1:].isnan().all())
+    # gradients one at a time
+    for want in ((True, False, False), (False, True, False), (False, False, True)):
+        one = g.gpic_linear_backward(R, X, W[:m], Z, "gelu", *want)
+        for name, asked in zip(("dX", "dW", "db"), want):
+            got = getattr(one, name)
+            assert torch.equal(got, getattr(gr, name)) if asked else got is None
+
+
+@pytest.mark.parametrize("dtype", list(T))
+def test_no_rows(g, dtype):
+    k, m = K, 2100
+    _tiled(g, "linear_backward", 0, k, m, dtype)
+    _tiled(g, "gated_backward", 0, k, m, dtype)
+    X, W = _randn((0, k), dtype, 1), _randn((2 * m, k), dtype, 2)
+    Y, Z = g.gpic_linear(X, W[:m], None, "gelu", want_pre=True)
+    gr = g.gpic_linear_backward(Y, X, W[:m], Z, "gelu")
+    assert gr.dX.shape == (0, k) and gr.dW.shape == (m, k)
+    assert not bool(gr.dW.any()) and not bool(gr.db.any())
+    H, Z = g.gpic_gated(X, W, want_pre=True)
+    gr = g.gpic_gated_backward(H, X, W, Z)
+    assert gr.dW.shape == (2 * m, k) and not bool(gr.dW.any())
+
+
+@pytest.mark.parametrize("dtype", list(T))
+def test_non_finite_values_stay_in_their_rows(g, dtype):
+    _all_tiled(g, N, K, M, dtype)
+    X, W = _randn((N, K), dtype, 1), _randn((2 * M, K), dtype, 2, 0.1)
+    dY = _randn((N, M), dtype, 3, 0.1)
+    clean, pre = g.gpic_linear(X, W[:M], None, "gelu", want_pre=True)
+    H, ZZ = g.gpic_gated(X, W, want_pre=True)
+    back = g.gpic_linear_backward(dY, X, W[:M], pre, "gelu")
+    keep = torch.arange(N, device=DEV) != 1
+    cols = torch.arange(K, device=DEV) != 37
+    outs = torch.arange(M, device=DEV) != 5
+    for bad in (float("nan"), float("inf"), -float("inf")):
+        print(f"non-finite {dtype} {bad}", flush=True)
+        x = X.clone()
+        x[1, 37] = bad
+        y = g.gpic_linear(x, W[:M])
+        assert not bool(torch.isfinite(y[1]).any()) and bool(torch.isfinite(y[keep]).all())
+        # the other rows keep their bits
+        assert torch.equal(g.gpic_linear(x, W[:M], None, "gelu")[keep], clean[keep])
+        assert torch.equal(g.gpic_gated(x, W)[keep], H[keep])
+        gr = g.gpic_linear_backward(dY, x, W[:M], pre, "gelu")
+        assert torch.equal(gr.dX, back.dX) and torch.equal(gr.db, back.db)
+        assert not bool(torch.isfinite(gr.dW[:, 37]).any())
+        assert torch.equal(gr.dW[:, cols], back.dW[:, cols])
+        # a weight: its column of the result
+        w = W.clone()
+        w[5, 37] = bad
+        y = g.gpic_linear(X, w[:M], None, "gelu")
+        assert torch.equal(y[:, outs], clean[:, outs])
+        assert torch.equal(g.gpic_gated(X, w)[:, outs], H[:, outs])
+        gr = g.gpic_linear_backward(dY, X, w[:M], pre, "gelu")
+        assert not bool(torch.isfinite(gr.dX[:, 37]).any())
+        assert torch.equal(gr.dX[:, cols], back.dX[:, cols]) and torch.equal(gr.dW, back.dW)
+        # an entry of the gradient: its row of dX, its row of dW
+        dy = dY.clone()
+        dy[1, 5] = bad
+        gr = g.gpic_linear_backward(dy, X, W[:M], pre, "gelu")
+        assert torch.equal(gr.dX[keep], back.dX[keep]) and torch.equal(gr.dW[outs], back.dW[outs])
+        assert not bool(torch.isfinite(gr.dX[1]).any() | torch.isfinite(gr.dW[5]).any())
+        assert torch.equal(gr.db[outs], back.db[outs]) and not bool(torch.isfinite(gr.db[5]))
+
+
+def test_infinite_and_large_arguments(g):
+    """Z of a wide layer at large arguments: activations at their limits."""
+    z = torch.tensor([0.0, 5.0, -5.0, 13.9, -13.9, 14.1, -14.1, 90.0, -90.0, 120.0, -120.0, 1e4,
+                      -1e4], device=DEV)
+    X = torch.zeros((N, K), device=DEV)
+    X[:, 0] = z.repeat(-(-N // len(z)))[:N]
+    W = torch.zeros((M, K), device=DEV)
+    W[:, 0] = 1.0
+    _tiled(g, "linear", N, K, M, "f32")
+    ref = X[:, :1].double().expand(N, M)
+    for act in ("relu", "gelu", "silu"):
+        a = _act(ref, act)[0]
+        y = g.gpic_linear(X, W, None, act).double()
+        tol = 3e-7 * (a.abs() + ref.abs().clamp(max=20)) + 2.0 ** -21 * ref.abs() * (a != 0)
+        assert bool(((y - a).abs() <= tol).all()), act
+
+
+def _everything(g, dtype, X=None):
+    n, k, m = N, K, M
+    X = _randn((n, k), dtype, 1) if X is None else X
+    W, V = _randn((m, k), dtype, 2, 0.2), _randn((k, m), dtype, 3, 0.1)
+    W2 = _randn((2 * m, k), dtype, 4, 0.2)
+    Y, Z = g.gpic_linear(X, W, _randn((m,), dtype, 5), "gelu", want_pre=True)
+    out = g.gpic_linear(Y, V, None, "none", X)
+    gr = g.gpic_linear_backward(Y, X, W, Z, "gelu")
+    H, ZZ = g.gpic_gated(X, W2, want_pre=True)
+    gg = g.gpic_gated_backward(H, X, W2, ZZ)
+    lin = g.gpic_linear_backward(Y, X, W)
+    O = g.gpic_orthogonalize(gg.dW)
+    mom, weights = torch.ones_like(W2, dtype=torch.float32), W2.clone()
+    g.gpic_muon_step(weights, gg.dW, mom, 0.1)
+    return [Y, Z, out, gr.dX, gr.dW, gr.db, H, ZZ, gg.dX, gg.dW, lin.dX, lin.dW, lin.db, O,
+            weights, mom]
+
+
+@pytest.mark.parametrize("dtype", list(T))
+def test_results_do_not_depend_on_the_buffers(g, monkeypatch, dtype):
+    from gpu_helpers import Filled
+    _all_tiled(g, N, K, M, dtype)
+    runs = []
+    for x in (0.0, 1e300):
+        print(f"scratch {x} {dtype}", flush=True)
+        with monkeypatch.context() as mp:
+            mp.setattr(g, "torch", Filled(x))
+            runs.append(_everything(g, dtype))
+        torch.cuda.synchronize()
+    for a, b in zip(*runs):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", list(T))
+def test_another_stream_and_graph_replays(g, dtype):
+    eager = [t.clone() for t in _everything(g, dtype)]
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        on = _everything(g, dtype)
+    s.synchronize()
+    for a, b in zip(on, eager):
+        assert torch.equal(a, b)
+    X = _randn((N, K), dtype, 1)
+    W, W2 = _randn((M, K), dtype, 2, 0.2), _randn((2 * M, K), dtype, 4, 0.2)
+
+    def step():
+        Y, Z = g.gpic_linear(X, W, None, "gelu", want_pre=True)
+        gr = g.gpic_linear_backward(Y, X, W, Z, "gelu")
+        H, ZZ = g.gpic_gated(X, W2, want_pre=True)
+        return [Y, gr.dX, gr.dW, gr.db, H, g.gpic_gated_backward(H, X, W2, ZZ).dW,
+                g.gpic_orthogonalize(gr.dW)]
+
+    with torch.cuda.stream(s):
+        step()
+    s.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        out = step()
+    for i in range(4):
+        X.copy_(_randn((N, K), dtype, 20 + i))
+        want = step()
+        for t in out:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(out, want):
+            assert torch.equal(a, b), i
+
+
+def test_offsets_beyond_32_bits(g):
+    """n m > 2^32 values of Y, Z and the residual through the tiles."""
+    n, k, m = 525000, 72, 8200
+    _tiled(g, "linear", n, k, m, "bf16")
+    print(f"linear n={n} k={k} m={m} ({n * m} values)", flush=True)
+    X, W, b = _randn((n, k), "bf16", 1), _randn((m, k), "bf16", 2, k ** -0.5), _randn((m,), "bf16", 3)
+    R = torch.zeros((n, m), dtype=torch.bfloat16, device=DEV)
+    rows = sorted({r for p in range(30, 33) for d in (-1, 0, 1) for r in [2 ** p // m + d] if r < n}
+                  | {0, 1, n - 2, n - 1})
+    R[rows] = _randn((len(rows), m), "bf16", 4)
+    Y, Z = g.gpic_linear(X, W, b, "gelu", R, want_pre=True)
+    z = X[rows].double() @ W.double().t() + b.double()
+    pe = _product_error(X[rows].double(), W.double(), "bf16") + 2 * E * z.abs()
+    a = _act(z, "gelu")[0]
+    ref = a + R[rows].double()
+    _close(Z[rows], z, pe, "bf16", "Z")
+    _close(Y[rows], ref, 1.13 * pe + 2e-7 * z.abs() + 4 * E * (a.abs() + ref.abs()), "bf16", "Y")
+    # every row was written: none is left at what the allocator held
+    assert bool(torch.isfinite(Y.view(-1)[::4097]).all())
