@@ -193,9 +193,9 @@ enum { kEpiLayer = 0, kEpiGated = 1, kEpiGram = 2, kEpiPoly = 3, kEpiUpdate = 4,
 __host__ __device__ constexpr bool symmetric(int epi) { return epi == kEpiGram || epi == kEpiPoly; }
 
 struct Epilogue {
-    // operand scales: acc is divided by their product (device pointers to
-    // the scales, null = 1), then multiplied by alpha
-    const float *sa, *sb;
+    // layers: the powers of two that the operands were multiplied by, their
+    // exponents (device pointers, null = 0); the others multiply acc by alpha
+    const int *pa, *pb;
     float alpha;
     // kEpiLayer, kEpiGated: z = acc (+ bias); y = act(z) (+ residual)
     const void *bias, *res;

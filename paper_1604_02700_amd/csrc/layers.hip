@@ -99,18 +99,17 @@ __device__ __forceinline__ float join_max(const float *part)
     return fmaxf(fmaxf(w[0], w[1]), fmaxf(w[2], w[3]));
 }
 
-// The power of two that brings `most` into [2^14, 2^15): half-precision
-// parts of the scaled values neither overflow nor, down to 2^-17 of the
-// largest, lose bits.
-__device__ __forceinline__ float scale_for(float most)
+// The exponent of the power of two that brings `most` into [2^14, 2^15):
+// half-precision parts of the scaled values neither overflow nor, down to
+// 2^-17 of the largest, lose bits.  (-113 .. 164: the power itself may be no
+// float, so it is applied by ldexp.)
+__device__ __forceinline__ int power_for(float most)
 {
     if (!(most > 0.0f))
-        return 1.0f;
+        return 0;
     int e;
     frexpf(most, &e);                 // most = f 2^e, f in [1/2, 1)
-    int p = 15 - e;
-    p = p > 120 ? 120 : (p < -120 ? -120 : p);
-    return ldexpf(1.0f, p);
+    return 15 - e;
 }
 
 __device__ __forceinline__ void split2(float x, _Float16 &hi, _Float16 &lo)
@@ -126,7 +125,7 @@ struct PackJob {
     int64_t rows, cols, ld;
     void *to;              // split matrix (float32) or rows of up64(cols)
     const float *part;     // float32: the partial maxima
-    float *scale;          // float32: receives the scale
+    int *power;            // float32: receives the exponent of its power of two
 };
 struct PackJobs {
     PackJob j[3];
@@ -142,11 +141,11 @@ template <bool SPLIT>
 __global__ __launch_bounds__(256) void pack_kernel(PackJobs jobs)
 {
     const PackJob m = jobs.j[blockIdx.y];
-    float s = 1.0f;
+    int power = 0;
     if (SPLIT) {
-        s = scale_for(join_max(m.part));
+        power = power_for(join_max(m.part));
         if (blockIdx.x == 0 && threadIdx.x == 0)
-            *m.scale = s;
+            *m.power = power;
     }
     const int64_t width = SPLIT ? (m.cols + 31) / 32 * 32 : up64(m.cols);
     const int64_t groups = width / 8, total = m.rows * groups;
@@ -172,7 +171,7 @@ __global__ __launch_bounds__(256) void pack_kernel(PackJobs jobs)
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 _Float16 a, b;
-                split2(v[k] * s, a, b);
+                split2(ldexpf(v[k], power), a, b);
                 h[k] = a;
                 l[k] = b;
             }
@@ -208,7 +207,7 @@ struct GradArgs {
     int rows;              // of a workgroup
     float *sums;           // [ceil(n / rows)][m] partial column sums, or null
     const float *max_dy, *max_z;     // partial maxima (Z: gated only)
-    float *scale;          // dZ is stored times this; null: 1
+    int *power;            // dZ is stored times two to this; null: 0
 };
 
 __device__ __forceinline__ f32x4 read4(const void *p, int64_t row_at, int64_t col, int64_t cols,
@@ -228,16 +227,21 @@ __device__ __forceinline__ f32x4 read4(const void *p, int64_t row_at, int64_t co
 // at or beyond it)
 template <int DT>
 __device__ __forceinline__ void write4(const GradArgs &a, int64_t row, int64_t col, int64_t end,
-                                       f32x4 v, float s)
+                                       f32x4 v, int power)
 {
     const bool split = DT == GPIC_F32;
+    if (DT != GPIC_BF16) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            v[j] = ldexpf(v[j], power);
+    }
     if (split) {
         _Float16 *d = static_cast<_Float16 *>(a.dZ) + row * a.ldd;
         half4 h, l;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             _Float16 x, y;
-            split2(v[j] * s, x, y);
+            split2(v[j], x, y);
             h[j] = x;
             l[j] = y;
         }
@@ -255,12 +259,12 @@ __device__ __forceinline__ void write4(const GradArgs &a, int64_t row, int64_t c
         return;
     }
     if ((col & 3) == 0 && col + 4 <= end) {
-        store4(a.dZ, row * a.ldd + col, v * s, DT);
+        store4(a.dZ, row * a.ldd + col, v, DT);
     } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
             if (col + j < end)
-                store1(a.dZ, row * a.ldd + col + j, v[j] * s, DT);
+                store1(a.dZ, row * a.ldd + col + j, v[j], DT);
     }
 }
 
@@ -274,15 +278,15 @@ template <int DT, int ACT, bool GATED>
 __global__ __launch_bounds__(256) void grad_kernel(GradArgs a)
 {
     constexpr int ZT = GATED ? GPIC_F32 : DT;      // the type of Z
-    float s = 1.0f;
-    if (a.scale) {
+    int power = 0;
+    if (a.power) {
         // |act'| <= 1.13, and the gated forms multiply by |Z| or |act(Z)| <= |Z|
         float most = 1.25f * join_max(a.max_dy);
         if (a.max_z)
             most *= fmaxf(1.0f, join_max(a.max_z));
-        s = scale_for(most < INFINITY ? most : 3.0e38f);
+        power = power_for(most < INFINITY ? most : 3.0e38f);
         if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0)
-            *a.scale = s;
+            *a.power = power;
     }
     const int64_t col = (int64_t)blockIdx.y * 256 + (threadIdx.x & 63) * 4;
     const int64_t r0 = (int64_t)blockIdx.x * a.rows;
@@ -308,8 +312,8 @@ __global__ __launch_bounds__(256) void grad_kernel(GradArgs a)
                     d[j] = dy[j] * u[j] * dy1;
                     du[j] = dy[j] * y;
                 }
-                write4<DT>(a, r, col, a.m, d, s);
-                write4<DT>(a, r, a.m + col, 2 * a.m, du, s);
+                write4<DT>(a, r, col, a.m, d, power);
+                write4<DT>(a, r, a.m + col, 2 * a.m, du, power);
             } else {
                 if (ACT != GPIC_ACT_NONE) {
                     const f32x4 z = read4(a.Z, r * a.ldz, col, a.m, ZT);
@@ -322,11 +326,11 @@ __global__ __launch_bounds__(256) void grad_kernel(GradArgs a)
                     // beyond the last column z and dy are 0, and d too
                 }
                 if (a.dZ)
-                    write4<DT>(a, r, col, end, d, s);
+                    write4<DT>(a, r, col, end, d, power);
                 sum += d;
             }
         } else if (a.dZ && !GATED && col < end) {
-            write4<DT>(a, r, col, end, f32x4{0.0f, 0.0f, 0.0f, 0.0f}, s);
+            write4<DT>(a, r, col, end, f32x4{0.0f, 0.0f, 0.0f, 0.0f}, power);
         }
         // the thread at the gate's last column also writes the padding
         if (GATED && col < a.m && col + 4 >= a.m)
@@ -392,7 +396,8 @@ struct Source {
     int64_t rows, cols, ld;
     bool pack;
     void *to = nullptr;
-    float *part = nullptr, *scale = nullptr;
+    float *part = nullptr;
+    int *power = nullptr;
     Operand operand(int dtype) const
     {
         if (!pack)
@@ -418,7 +423,7 @@ void place(Source &s, int dtype, Cursor &c)
     s.to = c.take((size_t)s.rows * p * 2);
     if (dtype == GPIC_F32) {
         s.part = static_cast<float *>(c.take(kMaxParts * 4));
-        s.scale = static_cast<float *>(c.take(4));
+        s.power = static_cast<int *>(c.take(4));
     }
 }
 
@@ -439,7 +444,7 @@ hipError_t launch_pack(const Source *const *list, int count, int dtype, hipStrea
     for (int i = 0; i < count; ++i)
         if (list[i]->pack && list[i]->rows > 0) {
             const Source &s = *list[i];
-            j.j[used++] = PackJob{s.x, s.rows, s.cols, s.ld, s.to, s.part, s.scale};
+            j.j[used++] = PackJob{s.x, s.rows, s.cols, s.ld, s.to, s.part, s.power};
             const int64_t groups = s.rows * ((s.cols + 63) / 64 * 8);
             most = groups > most ? groups : most;
         }
@@ -518,7 +523,8 @@ struct Backward {
     bool form;             // dZ is formed by grad_kernel (else dY is read)
     float *sums;
     int rows_each;         // rows of a workgroup of grad_kernel
-    float *max_dy, *max_z, *scale;
+    float *max_dy, *max_z;
+    int *power;
     float *part;
     int64_t rows;
     Backward(const Shape &s, bool gated, const void *dy, const void *x, const void *w, Cursor &c)
@@ -536,11 +542,11 @@ struct Backward {
         // times act' soon fall below 6e-5, where halves lose bits
         if (form && s.dtype == GPIC_F16) {
             dZ.part = static_cast<float *>(c.take(kMaxParts * 4));
-            dZ.scale = static_cast<float *>(c.take(4));
+            dZ.power = static_cast<int *>(c.take(4));
         }
         max_dy = dZ.part;
-        scale = dZ.scale;
-        max_z = scale && gated ? static_cast<float *>(c.take(kMaxParts * 4)) : nullptr;
+        power = dZ.power;
+        max_z = power && gated ? static_cast<float *>(c.take(kMaxParts * 4)) : nullptr;
         rows_each = grad_rows(s.n, s.m);
         sums = static_cast<float *>(
             c.take((size_t)((s.n + rows_each - 1) / rows_each) * s.m * 4));
@@ -598,9 +604,8 @@ hipError_t run_layer(const Shape &s, bool gated, const void *X, const void *W, c
     a.batch = 1;
     a.part = f.part;
     Epilogue &e = a.e;
-    e.sa = f.X.scale;
-    e.sb = f.W.scale;
-    e.alpha = 1.0f;
+    e.pa = f.X.power;
+    e.pb = f.W.power;
     e.bias = bias;
     e.res = res;
     e.out = Y;
@@ -630,7 +635,7 @@ hipError_t run_layer_backward(const Shape &s, bool gated, const void *dY, const 
     if (!dX)
         b.W.pack = false;
     const bool need_dz = dX || dW;
-    if (b.scale) {
+    if (b.power) {
         MaxJob jobs[4];
         int count = 0;
         if (need_dz)
@@ -665,7 +670,7 @@ hipError_t run_layer_backward(const Shape &s, bool gated, const void *dY, const 
         if (need_dz) {
             g.max_dy = b.max_dy;
             g.max_z = b.max_z;
-            g.scale = b.scale;
+            g.power = b.power;
         }
         const int64_t width = gated ? s.m : up64(s.m);
         g.rows = b.rows_each;
@@ -683,7 +688,6 @@ hipError_t run_layer_backward(const Shape &s, bool gated, const void *dY, const 
     ProductArgs a{};
     a.batch = 1;
     a.part = b.part;
-    a.e.alpha = 1.0f;
     a.e.dtype = s.dtype;
     a.e.act = GPIC_ACT_NONE;
     a.e.ldo = s.k;
@@ -694,8 +698,8 @@ hipError_t run_layer_backward(const Shape &s, bool gated, const void *dY, const 
         a.M = (int)s.n;
         a.N = (int)s.k;
         a.K = b.rows;
-        a.e.sa = b.scale;
-        a.e.sb = b.W.scale;
+        a.e.pa = b.power;
+        a.e.pb = b.W.power;
         a.e.out = dX;
         RUN(launch_product(kKM, op, kEpiLayer, a, st));
     }
@@ -705,8 +709,8 @@ hipError_t run_layer_backward(const Shape &s, bool gated, const void *dY, const 
         a.M = (int)b.rows;
         a.N = (int)s.k;
         a.K = s.n;
-        a.e.sa = s.n > 0 ? b.scale : nullptr;      // no rows: dW = 0, no scales
-        a.e.sb = s.n > 0 ? b.X.scale : nullptr;
+        a.e.pa = s.n > 0 ? b.power : nullptr;      // no rows: dW = 0, no powers
+        a.e.pb = s.n > 0 ? b.X.power : nullptr;
         a.e.out = dW;
         RUN(launch_product(kMM, op, kEpiLayer, a, st));
     }

@@ -300,19 +300,33 @@ struct Parts {
     }
 };
 
-// What the accumulators are multiplied by: the operands' scales are powers
-// of two, taken off one after the other so that neither step overflows.
+// What the accumulators are multiplied by: in layers 2^power, both operands'
+// powers of two taken off at once (one after the other could overflow or
+// underflow on the way to a result that does neither), elsewhere alpha.
 struct Factor {
-    float a, b;
+    int power;
+    float alpha;
 };
+template <int OP, int EPI>
 __device__ __forceinline__ Factor factor_of(const Epilogue &e)
 {
-    return Factor{e.sa ? 1.0f / *e.sa : 1.0f, (e.sb ? 1.0f / *e.sb : 1.0f) * e.alpha};
+    if (OP != kOpBf16 && (EPI == kEpiLayer || EPI == kEpiGated))
+        return Factor{-((e.pa ? *e.pa : 0) + (e.pb ? *e.pb : 0)), 1.0f};
+    return Factor{0, e.alpha};
 }
 
+template <int OP, int EPI>
 __device__ __forceinline__ f32x8 staged(const float *p, Factor f)
 {
-    return *reinterpret_cast<const f32x8 *>(p) * f.a * f.b;
+    f32x8 v = *reinterpret_cast<const f32x8 *>(p);
+    if (EPI != kEpiLayer && EPI != kEpiGated)
+        return v * f.alpha;
+    if (OP != kOpBf16) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            v[j] = ldexpf(v[j], f.power);
+    }
+    return v;
 }
 
 // The type of what an epilogue reads and writes, known from the operands
@@ -349,7 +363,7 @@ __device__ __forceinline__ void finish_block(const Epilogue &e, int64_t z, int64
     static_assert(kPasses * kRowsPass == ROWS && kPasses % kGroup == 0, "passes");
     const int lane = threadIdx.x & 63, q = lane % kLanes, r0 = lane / kLanes;
     const bool idle = kLanes * kRowsPass < 64 && r0 >= kRowsPass;
-    const Factor f = factor_of(e);
+    const Factor f = factor_of<OP, EPI>(e);
     if (EPI == kEpiGated) {
         const int64_t col = col0 / 2 + q * 8, half = e.half;
         const int valid = half - col < 8 ? (int)(half - col) : 8;
@@ -359,8 +373,8 @@ __device__ __forceinline__ void finish_block(const Epilogue &e, int64_t z, int64
             const int64_t row = row0 + r;
             if (valid <= 0 || row >= M || idle)
                 continue;
-            f32x8 g = staged(src + r * kPitch, f);
-            const f32x8 u = staged(src + r * kPitch + 16, f);
+            f32x8 g = staged<OP, EPI>(src + r * kPitch, f);
+            const f32x8 u = staged<OP, EPI>(src + r * kPitch + 16, f);
             if (e.pre) {
                 store8(e.pre, row * e.ldz + col, g, GPIC_F32, valid);
                 store8(e.pre, row * e.ldz + half + col, u, GPIC_F32, valid);
@@ -383,7 +397,7 @@ __device__ __forceinline__ void finish_block(const Epilogue &e, int64_t z, int64
         for (int p = 0; p < kGroup; ++p) {
             const int r = (p0 + p) * kRowsPass + r0;
             const int64_t row = row0 + r;
-            v[p] = staged(st + (idle ? 0 : r) * kPitch + q * 8, f);
+            v[p] = staged<OP, EPI>(st + (idle ? 0 : r) * kPitch + q * 8, f);
             c[p] = 0.0f;
             if (EPI == kEpiPoly || EPI == kEpiUpdate || EPI == kEpiResult) {
                 // lanes that finish nothing load the first entry

@@ -307,3 +307,24 @@ def test_offsets_beyond_32_bits(g):
     _close(Y[rows], ref, 1.13 * pe + 2e-7 * z.abs() + 4 * E * (a.abs() + ref.abs()), "bf16", "Y")
     # every row was written: none is left at what the allocator held
     assert bool(torch.isfinite(Y.view(-1)[::4097]).all())
+
+
+@pytest.mark.parametrize("x, w", [(1e34, 1e-30), (1e-30, 1e34), (1e-36, 1e36), (1e30, 1e-20)],
+                         ids=str)
+def test_magnitudes_at_the_ends_of_float32(g, x, w):
+    """Operands whose powers of two, one after the other, would leave
+    float32's range on the way to a result inside it."""
+    X, W = _randn((N, K), "f32", 1) * x, _randn((2 * M, K), "f32", 2, 0.1) * w
+    dY = _randn((N, M), "f32", 3) * (1.0 if x < 1 else 1e-10)
+    _all_tiled(g, N, K, M, "f32")
+    a, b, d = X.double(), W.double(), dY.double()
+    _close(g.gpic_linear(X, W[:M]), a @ b[:M].t(), _product_error(a, b[:M], "f32"), "f32", "Y")
+    z = a @ b.t()
+    pe = _product_error(a, b, "f32")
+    H, Z = g.gpic_gated(X, W, "none", want_pre=True)
+    _close(Z, z, pe, "f32", "gated Z")
+    _close(H, z[:, :M] * z[:, M:], pe[:, :M] * (z[:, M:].abs() + pe[:, M:])
+           + z[:, :M].abs() * pe[:, M:] + 4 * E * (z[:, :M] * z[:, M:]).abs(), "f32", "H")
+    gr = g.gpic_linear_backward(dY, X, W[:M])
+    _close(gr.dX, d @ b[:M], _product_error(d, b[:M].t(), "f32"), "f32", "dX")
+    _close(gr.dW, d.t() @ a, _product_error(d.t(), a.t(), "f32"), "f32", "dW")
