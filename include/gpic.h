@@ -443,9 +443,11 @@ gpic_status gpic_read_stream(const float *x, int64_t n, double *sink, void *stre
  *
  * Matrices are row-major with a pitch in elements; all matrices of a call
  * have one type.  Sums are float32 or wider.  float32 matrices are
- * multiplied as two half-precision parts (22 significant bits, one power of
- * two per matrix from its largest finite magnitude, so entries down to 2^-17
- * of it keep all 22).  Small calls read the
+ * multiplied as two half-precision parts under a power of two from a largest
+ * finite magnitude: 22 significant bits for entries down to 2^-17 of that
+ * largest, 2^-40 of it below.  Forward that is the largest of the entry's own
+ * row of X or of W, so that no point's result depends on another point;
+ * backward the largest of the matrix.  Small calls read the
  * matrices as they lie, without a workspace, and multiply float32 in float32:
  * forward layers of up to 32 rows, of up to 64 inputs (float32: up to 32, or
  * up to 64 and 2^23 results), or of up to 2,048 rows with n k m (gated: twice

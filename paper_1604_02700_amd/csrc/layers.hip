@@ -3,8 +3,9 @@
 // matrix products (product.h): packing of operands that the product cannot
 // read as they lie, dZ = dY act'(Z), and the column sums of the bias.
 //
-// float32 operands are multiplied as split halves (encoder.h); each matrix
-// has one power of two as its scale, from its largest finite magnitude.
+// float32 operands are multiplied as split halves (encoder.h).  Forward,
+// every row of X and of W has a power of two of its own, from its largest
+// finite magnitude; backward, each matrix has one.
 #include "encoder.h"
 
 namespace gpic {
@@ -193,6 +194,108 @@ __global__ __launch_bounds__(256) void pack_kernel(PackJobs jobs)
                     u.h[k] = c + k < m.cols ? x[k] : (unsigned short)0;
             }
             *reinterpret_cast<u32x4 *>(static_cast<unsigned short *>(m.to) + r * width + c) = u.v;
+        }
+    }
+}
+
+// largest finite |v| and what was there
+__device__ __forceinline__ float finite_max(float best, f32x4 v)
+{
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        const float a = fabsf(v[c]);
+        best = a < INFINITY && a > best ? a : best;
+    }
+    return best;
+}
+
+struct RowJob {
+    const float *x;
+    int64_t rows, cols, ld;
+    _Float16 *to;
+    int *power;            // [rows]
+};
+struct RowJobs {
+    RowJob j[2];
+};
+
+// Split copies of X and W (grid.y) whose rows have a power of two each: WAVES
+// waves (one: four rows a workgroup) read a row into registers, find its
+// largest finite magnitude and write its parts, so that the matrix is read
+// once; of rows longer than 2,048 values a wave the rest is read again.
+template <int WAVES>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void split_rows_kernel(RowJobs jobs)
+{
+    constexpr int kRows = WAVES == 1 ? 4 : 1, kHold = 4, kStride = 64 * WAVES;
+    const RowJob m = jobs.j[blockIdx.y];
+    const int wave = threadIdx.x >> 6, at = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
+    const int64_t width = (m.cols + 31) / 32 * 32, groups = width / 8;
+    __shared__ float most[8];
+    for (int64_t r = (int64_t)blockIdx.x * kRows + (WAVES == 1 ? wave : 0); r < m.rows;
+         r += (int64_t)gridDim.x * kRows) {
+        const float *x = m.x + r * m.ld;
+        f32x4 v[kHold][2];
+        float best = 0.0f;
+        auto read = [&](int64_t g, f32x4 (&u)[2]) {
+            u[0] = u[1] = 0.0f;
+            if (g * 8 + 8 <= m.cols) {
+                u[0] = load4(x, g * 8, GPIC_F32);
+                u[1] = load4(x, g * 8 + 4, GPIC_F32);
+            } else if (g < groups) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (g * 8 + k < m.cols)
+                        u[k / 4][k % 4] = x[g * 8 + k];
+            }
+        };
+#pragma unroll
+        for (int h = 0; h < kHold; ++h)
+            read(at + h * kStride, v[h]);
+#pragma unroll
+        for (int h = 0; h < kHold; ++h)
+            best = finite_max(finite_max(best, v[h][0]), v[h][1]);
+        for (int64_t g = at + kHold * kStride; g < groups; g += kStride) {
+            f32x4 u[2];
+            read(g, u);
+            best = finite_max(finite_max(best, u[0]), u[1]);
+        }
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1)
+            best = fmaxf(best, __shfl_xor(best, o, 64));
+        if (WAVES > 1) {
+            __syncthreads();             // the row before has been read
+            if ((threadIdx.x & 63) == 0)
+                most[wave] = best;
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w)
+                best = fmaxf(best, most[w]);
+        }
+        const int power = power_for(best);
+        if (at == 0)
+            m.power[r] = power;
+        auto write = [&](int64_t g, const f32x4 (&u)[2]) {
+            if (g >= groups)
+                return;
+            half8 h, l;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                _Float16 a, b;
+                split2(ldexpf(u[k / 4][k % 4], power), a, b);
+                h[k] = a;
+                l[k] = b;
+            }
+            _Float16 *to = m.to + r * 2 * width + split_at(g * 8);
+            *reinterpret_cast<half8 *>(to) = h;
+            *reinterpret_cast<half8 *>(to + 32) = l;
+        };
+#pragma unroll
+        for (int h = 0; h < kHold; ++h)
+            write(at + h * kStride, v[h]);
+        for (int64_t g = at + kHold * kStride; g < groups; g += kStride) {
+            f32x4 u[2];
+            read(g, u);
+            write(g, u);
         }
     }
 }
@@ -415,13 +518,16 @@ bool must_pack(int dtype, int64_t cols, int64_t ld, bool aligned16)
     return dtype == GPIC_F32 || !aligned16 || cols % 8 || ld % 8;
 }
 
-void place(Source &s, int dtype, Cursor &c)
+// rows_each: a power of two for every row (float32)
+void place(Source &s, int dtype, Cursor &c, bool rows_each = false)
 {
     if (!s.pack)
         return;
     const int64_t p = dtype == GPIC_F32 ? split_ld(s.cols) : up64(s.cols);
     s.to = c.take((size_t)s.rows * p * 2);
-    if (dtype == GPIC_F32) {
+    if (dtype == GPIC_F32 && rows_each) {
+        s.power = static_cast<int *>(c.take((size_t)s.rows * 4));
+    } else if (dtype == GPIC_F32) {
         s.part = static_cast<float *>(c.take(kMaxParts * 4));
         s.power = static_cast<int *>(c.take(4));
     }
@@ -433,6 +539,25 @@ hipError_t launch_absmax(const MaxJob *jobs, int count, hipStream_t st)
     for (int i = 0; i < count; ++i)
         j.j[i] = jobs[i];
     absmax_kernel<<<dim3(kMaxParts, (unsigned)count), 256, 0, st>>>(j);
+    return hipGetLastError();
+}
+
+// X and W of a float32 layer, a power of two for every row
+hipError_t launch_split_rows(const Source &x, const Source &w, hipStream_t st)
+{
+    RowJobs j{};
+    const Source *list[2] = {&x, &w};
+    for (int i = 0; i < 2; ++i)
+        j.j[i] = RowJob{static_cast<const float *>(list[i]->x), list[i]->rows, list[i]->cols,
+                        list[i]->ld, static_cast<_Float16 *>(list[i]->to), list[i]->power};
+    const int64_t rows = x.rows > w.rows ? x.rows : w.rows;
+    const bool one = x.cols <= 2048;
+    int64_t blocks = one ? (rows + 3) / 4 : rows;
+    blocks = blocks > (1 << 20) ? 1 << 20 : blocks;
+    if (one)
+        split_rows_kernel<1><<<dim3((unsigned)blocks, 2), 256, 0, st>>>(j);
+    else
+        split_rows_kernel<8><<<dim3((unsigned)blocks, 2), 512, 0, st>>>(j);
     return hipGetLastError();
 }
 
@@ -499,8 +624,8 @@ struct Forward {
         const int64_t rows = gated ? 2 * s.m : s.m;
         X = Source{x, s.n, s.k, s.ldx, must_pack(s.dtype, s.k, s.ldx, s.aligned16)};
         W = Source{w, rows, s.k, s.ldw, must_pack(s.dtype, s.k, s.ldw, s.aligned16)};
-        place(X, s.dtype, c);
-        place(W, s.dtype, c);
+        place(X, s.dtype, c, true);
+        place(W, s.dtype, c, true);
         part = static_cast<float *>(c.take(
             product_plan(s.n, rows, s.k, 1, kind_of(s.dtype), gated ? kEpiGated : kEpiLayer)
                 .part_bytes));
@@ -588,13 +713,10 @@ hipError_t run_layer(const Shape &s, bool gated, const void *X, const void *W, c
     Cursor c{static_cast<char *>(ws)};
     Forward f(s, gated, X, W, c);
     const Source *list[2] = {&f.X, &f.W};
-    if (s.dtype == GPIC_F32) {
-        const MaxJob jobs[2] = {
-            {X, f.X.rows, s.k, s.ldx, s.dtype, f.X.part},
-            {W, f.W.rows, s.k, s.ldw, s.dtype, f.W.part}};
-        RUN(launch_absmax(jobs, 2, st));
-    }
-    RUN(launch_pack(list, 2, s.dtype, st));
+    if (s.dtype == GPIC_F32)
+        RUN(launch_split_rows(f.X, f.W, st));
+    else
+        RUN(launch_pack(list, 2, s.dtype, st));
     ProductArgs a{};
     a.A = f.X.operand(s.dtype);
     a.B = f.W.operand(s.dtype);
@@ -606,6 +728,7 @@ hipError_t run_layer(const Shape &s, bool gated, const void *X, const void *W, c
     Epilogue &e = a.e;
     e.pa = f.X.power;
     e.pb = f.W.power;
+    e.rows_each = e.columns_each = 1;
     e.bias = bias;
     e.res = res;
     e.out = Y;

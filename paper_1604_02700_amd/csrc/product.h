@@ -300,31 +300,51 @@ struct Parts {
     }
 };
 
-// What the accumulators are multiplied by: in layers 2^power, both operands'
-// powers of two taken off at once (one after the other could overflow or
-// underflow on the way to a result that does neither), elsewhere alpha.
-struct Factor {
-    int power;
-    float alpha;
-};
-template <int OP, int EPI>
-__device__ __forceinline__ Factor factor_of(const Epilogue &e)
+// What the accumulators are multiplied by: in layers 2^-(row's power +
+// column's), both operands' powers of two taken off at once (one after the
+// other could overflow or underflow on the way to a result that does
+// neither), elsewhere alpha.
+using i32x8 = int __attribute__((ext_vector_type(8), aligned(4)));
+
+// the powers of ROWS rows from row0 on, one a lane
+template <int ROWS, int OP, int EPI>
+__device__ __forceinline__ int row_powers(const Epilogue &e, int64_t row0, int64_t M)
 {
-    if (OP != kOpBf16 && (EPI == kEpiLayer || EPI == kEpiGated))
-        return Factor{-((e.pa ? *e.pa : 0) + (e.pb ? *e.pb : 0)), 1.0f};
-    return Factor{0, e.alpha};
+    if (OP == kOpBf16 || (EPI != kEpiLayer && EPI != kEpiGated) || !e.pa)
+        return 0;
+    static_assert(ROWS <= 64, "a row a lane");
+    const int64_t row = row0 + (threadIdx.x & 63);
+    return e.pa[OP == kOpSplit && e.rows_each ? (row < M ? row : M - 1) : 0];
+}
+
+// the powers of eight columns, of which `valid` exist
+template <int OP, int EPI>
+__device__ __forceinline__ i32x8 column_powers(const Epilogue &e, int64_t col, int valid)
+{
+    i32x8 p = 0;
+    if (OP == kOpBf16 || (EPI != kEpiLayer && EPI != kEpiGated) || !e.pb || valid <= 0)
+        return p;
+    if (OP != kOpSplit || !e.columns_each)
+        return p + *e.pb;
+    if (valid >= 8)
+        return *reinterpret_cast<const i32x8 *>(e.pb + col);
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (j < valid)
+            p[j] = e.pb[col + j];
+    return p;
 }
 
 template <int OP, int EPI>
-__device__ __forceinline__ f32x8 staged(const float *p, Factor f)
+__device__ __forceinline__ f32x8 staged(const float *p, const Epilogue &e, int row, i32x8 columns)
 {
     f32x8 v = *reinterpret_cast<const f32x8 *>(p);
     if (EPI != kEpiLayer && EPI != kEpiGated)
-        return v * f.alpha;
+        return v * e.alpha;
     if (OP != kOpBf16) {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            v[j] = ldexpf(v[j], f.power);
+            v[j] = ldexpf(v[j], -(row + columns[j]));
     }
     return v;
 }
@@ -363,18 +383,21 @@ __device__ __forceinline__ void finish_block(const Epilogue &e, int64_t z, int64
     static_assert(kPasses * kRowsPass == ROWS && kPasses % kGroup == 0, "passes");
     const int lane = threadIdx.x & 63, q = lane % kLanes, r0 = lane / kLanes;
     const bool idle = kLanes * kRowsPass < 64 && r0 >= kRowsPass;
-    const Factor f = factor_of<OP, EPI>(e);
+    const int powers = row_powers<ROWS, OP, EPI>(e, row0, M);
     if (EPI == kEpiGated) {
         const int64_t col = col0 / 2 + q * 8, half = e.half;
         const int valid = half - col < 8 ? (int)(half - col) : 8;
         const float *src = st + (q >> 1) * 32 + (q & 1) * 8;
+        const i32x8 pg = column_powers<OP, EPI>(e, col, valid);
+        const i32x8 pu = column_powers<OP, EPI>(e, half + col, valid);
         for (int p = 0; p < kPasses; ++p) {
             const int r = p * kRowsPass + r0;
             const int64_t row = row0 + r;
+            const int pr = OP == kOpBf16 ? 0 : __shfl(powers, r & 63, 64);
             if (valid <= 0 || row >= M || idle)
                 continue;
-            f32x8 g = staged<OP, EPI>(src + r * kPitch, f);
-            const f32x8 u = staged<OP, EPI>(src + r * kPitch + 16, f);
+            f32x8 g = staged<OP, EPI>(src + r * kPitch, e, pr, pg);
+            const f32x8 u = staged<OP, EPI>(src + r * kPitch + 16, e, pr, pu);
             if (e.pre) {
                 store8(e.pre, row * e.ldz + col, g, GPIC_F32, valid);
                 store8(e.pre, row * e.ldz + half + col, u, GPIC_F32, valid);
@@ -388,6 +411,7 @@ __device__ __forceinline__ void finish_block(const Epilogue &e, int64_t z, int64
     const int64_t end = symmetric(EPI) ? (N + 63) / 64 * 64 : N;
     const int64_t here = end - col;
     const int valid = here < 0 ? 0 : (here < 8 ? (int)here : 8);
+    const i32x8 pc = column_powers<OP, EPI>(e, col, valid);
     f32x8 bias = 0.0f;
     if (EPI == kEpiLayer && e.bias && valid > 0)
         bias = load8(e.bias, col, dtype, valid);
@@ -397,7 +421,8 @@ __device__ __forceinline__ void finish_block(const Epilogue &e, int64_t z, int64
         for (int p = 0; p < kGroup; ++p) {
             const int r = (p0 + p) * kRowsPass + r0;
             const int64_t row = row0 + r;
-            v[p] = staged<OP, EPI>(st + (idle ? 0 : r) * kPitch + q * 8, f);
+            const int pr = OP == kOpBf16 || EPI != kEpiLayer ? 0 : __shfl(powers, r & 63, 64);
+            v[p] = staged<OP, EPI>(st + (idle ? 0 : r) * kPitch + q * 8, e, pr, pc);
             c[p] = 0.0f;
             if (EPI == kEpiPoly || EPI == kEpiUpdate || EPI == kEpiResult) {
                 // lanes that finish nothing load the first entry

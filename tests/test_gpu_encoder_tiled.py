@@ -328,3 +328,33 @@ def test_magnitudes_at_the_ends_of_float32(g, x, w):
     gr = g.gpic_linear_backward(dY, X, W[:M])
     _close(gr.dX, d @ b[:M], _product_error(d, b[:M].t(), "f32"), "f32", "dX")
     _close(gr.dW, d.t() @ a, _product_error(d.t(), a.t(), "f32"), "f32", "dW")
+
+
+def _forward_bound(x, w, dtype="f32"):
+    """As _product_error, with each row's own largest entry: what a row of X
+    (of W) loses does not depend on the others."""
+    b = ((x.shape[1] + 16) * E + 2.0 ** -21) * (x.abs() @ w.abs().t())
+    return b + 2.0 ** -38 * (x.abs().amax(1)[:, None] * w.abs().sum(1)[None, :]
+                             + w.abs().amax(1)[None, :] * x.abs().sum(1)[:, None])
+
+
+@pytest.mark.parametrize("k", [K, 2500, 17000])
+@pytest.mark.parametrize("size", [1e6, 1e13, 1e30])
+def test_outlier_leaves_the_other_rows_alone(g, size, k):
+    """One huge finite entry in X (in W): the other points (outputs) keep
+    the bits that they have without it."""
+    X, W = _randn((N, k), "f32", 1), _randn((2 * M, k), "f32", 2, k ** -0.5)
+    for op in ("linear", "gated"):
+        _tiled(g, op, N, k, M, "f32")
+    Y, H = g.gpic_linear(X, W[:M]), g.gpic_gated(X, W)
+    x, w = X.clone(), W.clone()
+    x[17, 3] = size
+    keep = torch.arange(N, device=DEV) != 17
+    assert torch.equal(g.gpic_linear(x, W[:M])[keep], Y[keep])
+    assert torch.equal(g.gpic_gated(x, W)[keep], H[keep])
+    xd, wd = x.double(), W.double()
+    _close(g.gpic_linear(x, W[:M]), xd @ wd[:M].t(), _forward_bound(xd, wd[:M]), "f32", "Y")
+    w[17, 3] = size
+    outs = torch.arange(M, device=DEV) != 17
+    assert torch.equal(g.gpic_linear(X, w[:M])[:, outs], Y[:, outs])
+    assert torch.equal(g.gpic_gated(X, w)[:, outs], H[:, outs])
