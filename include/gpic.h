@@ -445,9 +445,10 @@ gpic_status gpic_read_stream(const float *x, int64_t n, double *sink, void *stre
  * have one type.  Sums are float32 or wider.  float32 matrices are
  * multiplied as two half-precision parts under a power of two from a largest
  * finite magnitude: 22 significant bits for entries down to 2^-17 of that
- * largest, 2^-40 of it below.  Forward that is the largest of the entry's own
- * row of X or of W, so that no point's result depends on another point;
- * backward the largest of the matrix.  Small calls read the
+ * largest, errors of 2^-39 of it below.  It is the largest of what one entry of the
+ * result sums over: a row of X and a row of W forward, a row of dZ and a
+ * column of W for dX, a column of dZ and a column of X for dW; so no point's
+ * result depends on another point.  Small calls read the
  * matrices as they lie, without a workspace, and multiply float32 in float32:
  * forward layers of up to 32 rows, of up to 64 inputs (float32: up to 32, or
  * up to 64 and 2^23 results), or of up to 2,048 rows with n k m (gated: twice

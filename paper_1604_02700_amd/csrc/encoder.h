@@ -16,6 +16,7 @@ using half4 = _Float16 __attribute__((ext_vector_type(4)));
 using bf4 = __bf16 __attribute__((ext_vector_type(4)));
 using f32x4 = float __attribute__((ext_vector_type(4)));
 using f32x8 = float __attribute__((ext_vector_type(8), aligned(16)));
+using i32x4 = int __attribute__((ext_vector_type(4)));
 using u32x4 = unsigned int __attribute__((ext_vector_type(4)));
 using s16x4 = short __attribute__((ext_vector_type(4)));
 
@@ -161,7 +162,7 @@ __device__ __forceinline__ void store4(void *p, int64_t i, f32x4 v, int dtype)
 // ---------------------------------------------------------- split matrices
 // A float32 matrix as 16-bit parts: x = (hi + lo) / s, s a power of two,
 // hi = half(s x), lo = half(s x - hi), 22 significant bits together for
-// entries down to 2^-17 of the largest under the same s (below it, 2^-40 of
+// entries down to 2^-17 of the largest under the same s (below it, to 2^-39 of
 // that largest).  s belongs to what the product does not sum over, a row of
 // its operand, so that no row's bits depend on another row.  The
 // columns come in groups of 32, each as 32 hi and then 32 lo values, so a
@@ -197,11 +198,10 @@ __host__ __device__ constexpr bool symmetric(int epi) { return epi == kEpiGram |
 
 struct Epilogue {
     // layers: the powers of two that the operands were multiplied by, their
-    // exponents (device pointers, null = 0); of split operands one each for
-    // every row i and every column j (rows_each, columns_each: 1) or one
-    // for all (0); the others multiply acc by alpha
+    // exponents (device pointers, null = 0): of split operands one for every
+    // row i of A and every row j of B, of float16 ones one for all of A; the
+    // others multiply acc by alpha
     const int *pa, *pb;
-    int rows_each, columns_each;
     float alpha;
     // kEpiLayer, kEpiGated: z = acc (+ bias); y = act(z) (+ residual)
     const void *bias, *res;

@@ -3,9 +3,11 @@
 // matrix products (product.h): packing of operands that the product cannot
 // read as they lie, dZ = dY act'(Z), and the column sums of the bias.
 //
-// float32 operands are multiplied as split halves (encoder.h).  Forward,
-// every row of X and of W has a power of two of its own, from its largest
-// finite magnitude; backward, each matrix has one.
+// float32 operands are multiplied as split halves (encoder.h) under powers
+// of two from the largest finite magnitude of what a result's entry sums
+// over: forward of each row of X and of W; for dX of each row of dZ and each
+// column of W; for dW of each column of dZ and of X.  dZ is written twice
+// then, once for each product.
 #include "encoder.h"
 
 namespace gpic {
@@ -125,15 +127,15 @@ struct PackJob {
     const void *x;
     int64_t rows, cols, ld;
     void *to;              // split matrix (float32) or rows of up64(cols)
-    const float *part;     // float32: the partial maxima
-    int *power;            // float32: receives the exponent of its power of two
+    const int *power;      // float32: of every column
 };
 struct PackJobs {
     PackJob j[3];
 };
 
 // Copies of operands in the form that the product reads (grid.y: which).
-// Eight columns a thread.  float32: split parts; 16 bits: zero-padded rows.
+// Eight columns a thread.  float32: split parts, every column under its power
+// of two; 16 bits: zero-padded rows.
 // Bound by memory: 10,007 x 1,000 and 777 x 1,000 in float32, read and
 // written (86 MB), 15.8 us, 5.4 TB/s with what the maxima's pass left in the
 // caches.  Splitting inside the product instead would do it once per tile
@@ -142,12 +144,6 @@ template <bool SPLIT>
 __global__ __launch_bounds__(256) void pack_kernel(PackJobs jobs)
 {
     const PackJob m = jobs.j[blockIdx.y];
-    int power = 0;
-    if (SPLIT) {
-        power = power_for(join_max(m.part));
-        if (blockIdx.x == 0 && threadIdx.x == 0)
-            *m.power = power;
-    }
     const int64_t width = SPLIT ? (m.cols + 31) / 32 * 32 : up64(m.cols);
     const int64_t groups = width / 8, total = m.rows * groups;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total;
@@ -156,6 +152,7 @@ __global__ __launch_bounds__(256) void pack_kernel(PackJobs jobs)
         if (SPLIT) {
             const float *x = static_cast<const float *>(m.x) + r * m.ld + c;
             float v[8];
+            int power[8];
             if (c + 8 <= m.cols) {
                 const f32x4 a = load4(x, 0, GPIC_F32), b = load4(x, 4, GPIC_F32);
 #pragma unroll
@@ -163,16 +160,21 @@ __global__ __launch_bounds__(256) void pack_kernel(PackJobs jobs)
                     v[k] = a[k];
                     v[4 + k] = b[k];
                 }
-            } else {
 #pragma unroll
                 for (int k = 0; k < 8; ++k)
+                    power[k] = m.power[c + k];
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
                     v[k] = c + k < m.cols ? x[k] : 0.0f;
+                    power[k] = c + k < m.cols ? m.power[c + k] : 0;
+                }
             }
             half8 h, l;
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 _Float16 a, b;
-                split2(ldexpf(v[k], power), a, b);
+                split2(ldexpf(v[k], power[k]), a, b);
                 h[k] = a;
                 l[k] = b;
             }
@@ -305,12 +307,15 @@ struct GradArgs {
     const void *dY, *Z;
     int64_t ldy, ldz, n, m;
     int act;
-    void *dZ;              // null: only the column sums
-    int64_t ldd;           // row pitch of dZ in 16-bit values
+    void *dZ;              // as dX's product reads it (16 bits: dW's too), or null
+    void *dZ_columns;      // float32: as dW's product reads it, or null
+    int64_t ldd;           // row pitch of both in 16-bit values
     int rows;              // of a workgroup
     float *sums;           // [ceil(n / rows)][m] partial column sums, or null
-    const float *max_dy, *max_z;     // partial maxima (Z: gated only)
-    int *power;            // dZ is stored times two to this; null: 0
+    const float *max_dy, *max_z;     // float16: partial maxima (Z: gated only)
+    int *power;            // float16: dZ is stored times two to this; null: 0
+    // float32: the powers of dZ's rows and of its columns
+    const int *row_power, *column_power;
 };
 
 __device__ __forceinline__ f32x4 read4(const void *p, int64_t row_at, int64_t col, int64_t cols,
@@ -327,19 +332,19 @@ __device__ __forceinline__ f32x4 read4(const void *p, int64_t row_at, int64_t co
 }
 
 // four values of dZ from column col on (`end`: no column of this half lies
-// at or beyond it)
+// at or beyond it), under their powers
 template <int DT>
-__device__ __forceinline__ void write4(const GradArgs &a, int64_t row, int64_t col, int64_t end,
-                                       f32x4 v, int power)
+__device__ __forceinline__ void write4(void *dZ, int64_t at, int64_t col, int64_t end, f32x4 v,
+                                       i32x4 power)
 {
     const bool split = DT == GPIC_F32;
     if (DT != GPIC_BF16) {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            v[j] = ldexpf(v[j], power);
+            v[j] = ldexpf(v[j], power[j]);
     }
     if (split) {
-        _Float16 *d = static_cast<_Float16 *>(a.dZ) + row * a.ldd;
+        _Float16 *d = static_cast<_Float16 *>(dZ) + at;
         half4 h, l;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -362,13 +367,169 @@ __device__ __forceinline__ void write4(const GradArgs &a, int64_t row, int64_t c
         return;
     }
     if ((col & 3) == 0 && col + 4 <= end) {
-        store4(a.dZ, row * a.ldd + col, v, DT);
+        store4(dZ, at + col, v, DT);
     } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
             if (col + j < end)
-                store1(a.dZ, row * a.ldd + col + j, v[j], DT);
+                store1(dZ, at + col + j, v[j], DT);
     }
+}
+
+// d (gated: and du) of four entries of dZ from dY and Z
+template <int ACT, bool GATED>
+__device__ __forceinline__ void form4(f32x4 dy, f32x4 g, f32x4 u, f32x4 &d, f32x4 &du)
+{
+    d = dy;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (GATED || ACT != GPIC_ACT_NONE) {
+            float y, dy1;
+            activate_grad(g[j], ACT, y, dy1);
+            d[j] = GATED ? dy[j] * u[j] * dy1 : dy[j] * dy1;
+            du[j] = dy[j] * y;
+        }
+}
+
+// Partial maxima of a float32 matrix's columns, or of dZ's columns and rows:
+// `parts` runs of `each` rows by strips of 256 columns.
+struct Maxima {
+    const float *x;        // null: dZ
+    int64_t rows, cols, ld;
+    float *part;           // [parts][cols]
+    int64_t strips, parts, each;
+    __host__ __device__ int64_t blocks() const { return strips * parts; }
+};
+struct MaximaArgs {
+    Maxima j[3];
+    int count;
+    // dZ from these; its rows' maxima go to row_part [strips][rows]
+    const float *dY, *Z;
+    int64_t ldy, ldz, m;
+    float *row_part;
+};
+
+// Largest finite magnitudes of the columns of X, W and dZ and of the rows of
+// dZ, which is formed for it and not kept: one more pass over dY and Z (the
+// second one finds them in the caches where they fit), and no product of
+// bounds stands in for a maximum.  Bound by memory and by the activation: dY
+// and Z of 10,007 x 777 with gelu, X of 10,007 x 1,000 and W (96 MB) 23 us, 4.2
+// TB/s; the powers from the partial maxima 6 us.
+template <int ACT, bool GATED>
+__global__ __launch_bounds__(256) void maxima_kernel(MaximaArgs a)
+{
+    int64_t id = blockIdx.x;
+    int job = 0;
+    while (job + 1 < a.count && id >= a.j[job].blocks())
+        id -= a.j[job++].blocks();
+    const Maxima m = a.j[job];
+    const int64_t strip = id % m.strips, part = id / m.strips;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t cols = m.x ? m.cols : a.m, col = strip * 256 + lane * 4;
+    const int64_t r0 = part * m.each, r1 = r0 + m.each < m.rows ? r0 + m.each : m.rows;
+    f32x4 best = 0.0f, best_u = 0.0f;
+    constexpr int kRows = 2;               // of a wave in flight
+    for (int64_t r = r0 + wave; r < r1; r += 4 * kRows) {
+        f32x4 x[kRows], g[kRows], u[kRows];
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            x[i] = g[i] = u[i] = 0.0f;
+            const int64_t row = r + 4 * i;
+            if (row < r1 && col < cols) {
+                x[i] = m.x ? read4(m.x, row * m.ld, col, cols, GPIC_F32)
+                           : read4(a.dY, row * a.ldy, col, cols, GPIC_F32);
+                if (!m.x && (GATED || ACT != GPIC_ACT_NONE))
+                    g[i] = read4(a.Z, row * a.ldz, col, cols, GPIC_F32);
+                if (!m.x && GATED)
+                    u[i] = read4(a.Z, row * a.ldz + a.m, col, cols, GPIC_F32);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            f32x4 d = x[i], du = 0.0f;
+            if (!m.x)
+                form4<ACT, GATED>(x[i], g[i], u[i], d, du);
+            float most = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float v = fabsf(d[j]), w = GATED ? fabsf(du[j]) : 0.0f;
+                best[j] = v < INFINITY && v > best[j] ? v : best[j];
+                best_u[j] = w < INFINITY && w > best_u[j] ? w : best_u[j];
+                most = v < INFINITY && v > most ? v : most;
+                most = w < INFINITY && w > most ? w : most;
+            }
+            if (m.x)
+                continue;
+#pragma unroll
+            for (int o = 32; o > 0; o >>= 1)
+                most = fmaxf(most, __shfl_xor(most, o, 64));
+            const int64_t row = r + 4 * i;
+            if (lane == 0 && row < r1)
+                a.row_part[strip * m.rows + row] = most;
+        }
+    }
+    __shared__ f32x4 all[2][256];
+    all[0][threadIdx.x] = best;
+    all[1][threadIdx.x] = best_u;
+    __syncthreads();
+    // wave 0 the columns, wave 1 the up projection's
+    if (wave > (GATED && !m.x ? 1 : 0))
+        return;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        float v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+            v = fmaxf(v, all[wave][w * 64 + lane][j]);
+        if (col + j < cols)
+            m.part[part * m.cols + (wave ? a.m : 0) + col + j] = v;
+    }
+}
+
+// Powers of two from partial maxima [parts][len]: a thread an entry, or
+// sixteen where there are many parts.
+struct PowerJob {
+    const float *part;
+    int64_t len, parts;
+    int *power;
+    __host__ __device__ bool many() const { return parts > 16; }
+    __host__ __device__ int64_t blocks() const
+    {
+        return many() ? (len + 63) / 64 : (len + 1023) / 1024;
+    }
+};
+struct PowerJobs {
+    PowerJob j[4];
+    int count;
+};
+
+__global__ __launch_bounds__(1024) void powers_kernel(PowerJobs a)
+{
+    int64_t id = blockIdx.x;
+    int job = 0;
+    while (job + 1 < a.count && id >= a.j[job].blocks())
+        id -= a.j[job++].blocks();
+    const PowerJob m = a.j[job];
+    const bool many = m.many();
+    const int first = many ? threadIdx.x >> 6 : 0, step = many ? 16 : 1;
+    const int64_t i = many ? id * 64 + (threadIdx.x & 63) : id * 1024 + threadIdx.x;
+    float best = 0.0f;
+    if (i < m.len) {
+#pragma unroll 8
+        for (int64_t p = first; p < m.parts; p += step)
+            best = fmaxf(best, m.part[p * m.len + i]);
+    }
+    __shared__ float all[1024];
+    if (many) {
+        all[threadIdx.x] = best;
+        __syncthreads();
+        if (threadIdx.x >= 64)
+            return;
+        for (int w = 1; w < 16; ++w)
+            best = fmaxf(best, all[w * 64 + threadIdx.x]);
+    }
+    if (i < m.len)
+        m.power[i] = power_for(best);
 }
 
 // dZ of `rows` rows x 256 columns a workgroup (four rows at a time, four
@@ -382,7 +543,7 @@ __global__ __launch_bounds__(256) void grad_kernel(GradArgs a)
 {
     constexpr int ZT = GATED ? GPIC_F32 : DT;      // the type of Z
     int power = 0;
-    if (a.power) {
+    if (DT == GPIC_F16 && a.power) {
         // |act'| <= 1.13, and the gated forms multiply by |Z| or |act(Z)| <= |Z|
         float most = 1.25f * join_max(a.max_dy);
         if (a.max_z)
@@ -400,7 +561,26 @@ __global__ __launch_bounds__(256) void grad_kernel(GradArgs a)
     const int64_t all = GATED ? 2 * a.m : a.m;
     const int64_t width = DT == GPIC_F32 ? (all + 31) / 32 * 32 : up64(all);
     const int64_t end = GATED ? a.m : width;
+    i32x4 columns = 0, columns_u = 0;
+    if (DT == GPIC_F32 && a.dZ_columns) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (col + j < a.m) {
+                columns[j] = a.column_power[col + j];
+                if (GATED)
+                    columns_u[j] = a.column_power[a.m + col + j];
+            }
+    }
+    // dZ from column c on, for the products that read it
+    auto put = [&](int64_t r, int64_t c, int64_t last, f32x4 v, i32x4 each) {
+        if (a.dZ)
+            write4<DT>(a.dZ, r * a.ldd, c, last, v, i32x4{power, power, power, power});
+        if (DT == GPIC_F32 && a.dZ_columns)
+            write4<DT>(a.dZ_columns, r * a.ldd, c, last, v, each);
+    };
     for (int64_t r = r0 + (threadIdx.x >> 6); r < r1; r += 4) {
+        if (DT == GPIC_F32 && a.dZ)
+            power = a.row_power[r];
         if (col < a.m) {
             const f32x4 dy = read4(a.dY, r * a.ldy, col, a.m, DT);
             f32x4 d = dy;
@@ -415,8 +595,8 @@ __global__ __launch_bounds__(256) void grad_kernel(GradArgs a)
                     d[j] = dy[j] * u[j] * dy1;
                     du[j] = dy[j] * y;
                 }
-                write4<DT>(a, r, col, a.m, d, power);
-                write4<DT>(a, r, a.m + col, 2 * a.m, du, power);
+                put(r, col, a.m, d, columns);
+                put(r, a.m + col, 2 * a.m, du, columns_u);
             } else {
                 if (ACT != GPIC_ACT_NONE) {
                     const f32x4 z = read4(a.Z, r * a.ldz, col, a.m, ZT);
@@ -428,19 +608,21 @@ __global__ __launch_bounds__(256) void grad_kernel(GradArgs a)
                     }
                     // beyond the last column z and dy are 0, and d too
                 }
-                if (a.dZ)
-                    write4<DT>(a, r, col, end, d, power);
+                put(r, col, end, d, columns);
                 sum += d;
             }
-        } else if (a.dZ && !GATED && col < end) {
-            write4<DT>(a, r, col, end, f32x4{0.0f, 0.0f, 0.0f, 0.0f}, power);
+        } else if (!GATED && col < end) {
+            put(r, col, end, f32x4{0.0f, 0.0f, 0.0f, 0.0f}, columns);
         }
         // the thread at the gate's last column also writes the padding
         if (GATED && col < a.m && col + 4 >= a.m)
             for (int64_t c = all; c < width; ++c) {
                 if (DT == GPIC_F32) {
-                    _Float16 *d = static_cast<_Float16 *>(a.dZ) + r * a.ldd + split_at(c);
-                    d[0] = d[32] = (_Float16)0.0f;
+                    for (void *to : {a.dZ, a.dZ_columns})
+                        if (to) {
+                            _Float16 *d = static_cast<_Float16 *>(to) + r * a.ldd + split_at(c);
+                            d[0] = d[32] = (_Float16)0.0f;
+                        }
                 } else {
                     store1(a.dZ, r * a.ldd + c, 0.0f, DT);
                 }
@@ -499,8 +681,7 @@ struct Source {
     int64_t rows, cols, ld;
     bool pack;
     void *to = nullptr;
-    float *part = nullptr;
-    int *power = nullptr;
+    int *power = nullptr;  // float32: of its rows (backward: columns)
     Operand operand(int dtype) const
     {
         if (!pack)
@@ -518,19 +699,15 @@ bool must_pack(int dtype, int64_t cols, int64_t ld, bool aligned16)
     return dtype == GPIC_F32 || !aligned16 || cols % 8 || ld % 8;
 }
 
-// rows_each: a power of two for every row (float32)
-void place(Source &s, int dtype, Cursor &c, bool rows_each = false)
+// `powers`: how many powers of two the copy has (float32)
+void place(Source &s, int dtype, Cursor &c, int64_t powers)
 {
     if (!s.pack)
         return;
     const int64_t p = dtype == GPIC_F32 ? split_ld(s.cols) : up64(s.cols);
     s.to = c.take((size_t)s.rows * p * 2);
-    if (dtype == GPIC_F32 && rows_each) {
-        s.power = static_cast<int *>(c.take((size_t)s.rows * 4));
-    } else if (dtype == GPIC_F32) {
-        s.part = static_cast<float *>(c.take(kMaxParts * 4));
-        s.power = static_cast<int *>(c.take(4));
-    }
+    if (dtype == GPIC_F32)
+        s.power = static_cast<int *>(c.take((size_t)powers * 4));
 }
 
 hipError_t launch_absmax(const MaxJob *jobs, int count, hipStream_t st)
@@ -569,7 +746,7 @@ hipError_t launch_pack(const Source *const *list, int count, int dtype, hipStrea
     for (int i = 0; i < count; ++i)
         if (list[i]->pack && list[i]->rows > 0) {
             const Source &s = *list[i];
-            j.j[used++] = PackJob{s.x, s.rows, s.cols, s.ld, s.to, s.part, s.power};
+            j.j[used++] = PackJob{s.x, s.rows, s.cols, s.ld, s.to, s.power};
             const int64_t groups = s.rows * ((s.cols + 63) / 64 * 8);
             most = groups > most ? groups : most;
         }
@@ -624,8 +801,8 @@ struct Forward {
         const int64_t rows = gated ? 2 * s.m : s.m;
         X = Source{x, s.n, s.k, s.ldx, must_pack(s.dtype, s.k, s.ldx, s.aligned16)};
         W = Source{w, rows, s.k, s.ldw, must_pack(s.dtype, s.k, s.ldw, s.aligned16)};
-        place(X, s.dtype, c, true);
-        place(W, s.dtype, c, true);
+        place(X, s.dtype, c, X.rows);
+        place(W, s.dtype, c, W.rows);
         part = static_cast<float *>(c.take(
             product_plan(s.n, rows, s.k, 1, kind_of(s.dtype), gated ? kEpiGated : kEpiLayer)
                 .part_bytes));
@@ -642,9 +819,26 @@ int grad_rows(int64_t n, int64_t m)
     return rows;
 }
 
+// How the maxima of a matrix's columns are cut: about 1,536 workgroups, none
+// of fewer than 16 rows (768: 27 us for 23 at 10,007 rows).
+Maxima maxima_of(const void *x, int64_t rows, int64_t cols, int64_t ld, int64_t across)
+{
+    Maxima m{static_cast<const float *>(x), rows, cols, ld, nullptr, (across + 255) / 256, 0, 0};
+    int64_t parts = 1536 / m.strips;
+    parts = parts < (rows + 15) / 16 ? parts : (rows + 15) / 16;
+    parts = parts < 1 ? 1 : parts;
+    m.each = (rows + parts - 1) / parts;
+    m.parts = m.each ? (rows + m.each - 1) / m.each : 0;
+    return m;
+}
+
 // What a backward call keeps in its workspace.
 struct Backward {
     Source dZ, X, W;
+    void *dZ_columns = nullptr;      // float32: dW's copy of dZ, the powers of its columns
+    int *column_power = nullptr;
+    Maxima mz{}, mx{}, mw{};         // float32
+    float *row_part = nullptr;       // [mz.strips][n]
     bool form;             // dZ is formed by grad_kernel (else dY is read)
     float *sums;
     int rows_each;         // rows of a workgroup of grad_kernel
@@ -660,18 +854,25 @@ struct Backward {
                     form || must_pack(s.dtype, rows, s.ldy, s.aligned16)};
         X = Source{x, s.n, s.k, s.ldx, must_pack(s.dtype, s.k, s.ldx, s.aligned16)};
         W = Source{w, rows, s.k, s.ldw, must_pack(s.dtype, s.k, s.ldw, s.aligned16)};
-        place(dZ, s.dtype, c);
-        place(X, s.dtype, c);
-        place(W, s.dtype, c);
+        place(dZ, s.dtype, c, s.n);
+        place(X, s.dtype, c, s.k);
+        place(W, s.dtype, c, s.k);
+        if (s.dtype == GPIC_F32) {
+            dZ_columns = c.take((size_t)s.n * split_ld(rows) * 2);
+            column_power = static_cast<int *>(c.take((size_t)rows * 4));
+            mz = maxima_of(nullptr, s.n, rows, 0, s.m);
+            mx = maxima_of(x, s.n, s.k, s.ldx, s.k);
+            mw = maxima_of(w, rows, s.k, s.ldw, s.k);
+            for (Maxima *m : {&mz, &mx, &mw})
+                m->part = static_cast<float *>(c.take((size_t)(m->parts * m->cols) * 4));
+            row_part = static_cast<float *>(c.take((size_t)(mz.strips * s.n) * 4));
+        }
         // a dZ that is formed in half precision has a scale too: gradients
         // times act' soon fall below 6e-5, where halves lose bits
-        if (form && s.dtype == GPIC_F16) {
-            dZ.part = static_cast<float *>(c.take(kMaxParts * 4));
-            dZ.power = static_cast<int *>(c.take(4));
-        }
-        max_dy = dZ.part;
-        power = dZ.power;
-        max_z = power && gated ? static_cast<float *>(c.take(kMaxParts * 4)) : nullptr;
+        const bool scaled = form && s.dtype == GPIC_F16;
+        max_dy = scaled ? static_cast<float *>(c.take(kMaxParts * 4)) : nullptr;
+        max_z = scaled && gated ? static_cast<float *>(c.take(kMaxParts * 4)) : nullptr;
+        power = scaled ? static_cast<int *>(c.take(4)) : nullptr;
         rows_each = grad_rows(s.n, s.m);
         sums = static_cast<float *>(
             c.take((size_t)((s.n + rows_each - 1) / rows_each) * s.m * 4));
@@ -688,6 +889,63 @@ struct Backward {
         if (e_ != hipSuccess)                                                  \
             return e_;                                                         \
     } while (0)
+
+// The powers of two of a float32 backward call: of W's columns and dZ's rows
+// for dX, of X's and dZ's columns for dW.
+template <bool GATED>
+void launch_maxima(const MaximaArgs &a, int act, unsigned blocks, hipStream_t st)
+{
+    switch (act) {
+    case GPIC_ACT_NONE:
+        maxima_kernel<GPIC_ACT_NONE, GATED><<<blocks, 256, 0, st>>>(a);
+        break;
+    case GPIC_ACT_RELU:
+        maxima_kernel<GPIC_ACT_RELU, GATED><<<blocks, 256, 0, st>>>(a);
+        break;
+    case GPIC_ACT_GELU:
+        maxima_kernel<GPIC_ACT_GELU, GATED><<<blocks, 256, 0, st>>>(a);
+        break;
+    default:
+        maxima_kernel<GPIC_ACT_SILU, GATED><<<blocks, 256, 0, st>>>(a);
+    }
+}
+
+hipError_t launch_powers(const Shape &s, bool gated, const Backward &b, const void *dY,
+                         const void *Z, bool dX, bool dW, hipStream_t st)
+{
+    MaximaArgs a{};
+    PowerJobs p{};
+    a.j[a.count++] = b.mz;
+    if (dX) {
+        a.j[a.count++] = b.mw;
+        p.j[p.count++] = PowerJob{b.mw.part, s.k, b.mw.parts, b.W.power};
+        p.j[p.count++] = PowerJob{b.row_part, s.n, b.mz.strips, b.dZ.power};
+    }
+    if (dW) {
+        a.j[a.count++] = b.mx;
+        p.j[p.count++] = PowerJob{b.mx.part, s.k, b.mx.parts, b.X.power};
+        p.j[p.count++] = PowerJob{b.mz.part, b.rows, b.mz.parts, b.column_power};
+    }
+    a.dY = static_cast<const float *>(dY);
+    a.Z = static_cast<const float *>(Z);
+    a.ldy = s.ldy;
+    a.ldz = s.ldz;
+    a.m = s.m;
+    a.row_part = b.row_part;
+    int64_t blocks = 0;
+    for (int i = 0; i < a.count; ++i)
+        blocks += a.j[i].blocks();
+    if (gated)
+        launch_maxima<true>(a, s.act, (unsigned)blocks, st);
+    else
+        launch_maxima<false>(a, s.act, (unsigned)blocks, st);
+    RUN(hipGetLastError());
+    blocks = 0;
+    for (int i = 0; i < p.count; ++i)
+        blocks += p.j[i].blocks();
+    powers_kernel<<<(unsigned)blocks, 1024, 0, st>>>(p);
+    return hipGetLastError();
+}
 
 } // namespace
 
@@ -728,7 +986,6 @@ hipError_t run_layer(const Shape &s, bool gated, const void *X, const void *W, c
     Epilogue &e = a.e;
     e.pa = f.X.power;
     e.pb = f.W.power;
-    e.rows_each = e.columns_each = 1;
     e.bias = bias;
     e.res = res;
     e.out = Y;
@@ -751,27 +1008,19 @@ hipError_t run_layer_backward(const Shape &s, bool gated, const void *dY, const 
     Cursor c{static_cast<char *>(ws)};
     Backward b(s, gated, dY, X, W, c);
     const int op = kind_of(s.dtype);
-    const int ztype = gated ? GPIC_F32 : s.dtype;
-    // operands: what the wanted gradients read
-    if (!dW)
+    // operands: what the wanted gradients read (of no rows: nothing)
+    if (!dW || s.n == 0)
         b.X.pack = false;
-    if (!dX)
+    if (!dX || s.n == 0)
         b.W.pack = false;
     const bool need_dz = dX || dW;
-    if (b.power) {
-        MaxJob jobs[4];
-        int count = 0;
-        if (need_dz)
-            jobs[count++] = {dY, s.n, s.m, s.ldy, s.dtype, b.max_dy};
-        if (need_dz && b.max_z)
-            jobs[count++] = {Z, s.n, b.rows, s.ldz, ztype, b.max_z};
-        if (dW && b.X.part)
-            jobs[count++] = {X, s.n, s.k, s.ldx, s.dtype, b.X.part};
-        if (dX && b.W.part)
-            jobs[count++] = {W, b.rows, s.k, s.ldw, s.dtype, b.W.part};
-        if (count)
-            RUN(launch_absmax(jobs, count, st));
+    if (need_dz && b.power && s.n > 0) {
+        const MaxJob jobs[2] = {{dY, s.n, s.m, s.ldy, s.dtype, b.max_dy},
+                                {Z, s.n, b.rows, s.ldz, GPIC_F32, b.max_z}};
+        RUN(launch_absmax(jobs, b.max_z ? 2 : 1, st));
     }
+    if (need_dz && s.dtype == GPIC_F32 && s.n > 0)
+        RUN(launch_powers(s, gated, b, dY, Z, dX != nullptr, dW != nullptr, st));
     {
         Source plain = b.dZ;
         plain.pack = b.dZ.pack && !b.form && need_dz;
@@ -787,7 +1036,10 @@ hipError_t run_layer_backward(const Shape &s, bool gated, const void *dY, const 
         g.n = s.n;
         g.m = s.m;
         g.act = s.act;
-        g.dZ = b.form && need_dz ? b.dZ.to : nullptr;
+        g.dZ = b.form && (dX || (dW && s.dtype != GPIC_F32)) ? b.dZ.to : nullptr;
+        g.dZ_columns = dW ? b.dZ_columns : nullptr;
+        g.row_power = b.dZ.power;
+        g.column_power = b.column_power;
         g.ldd = s.dtype == GPIC_F32 ? split_ld(b.rows) : up64(b.rows);
         g.sums = db ? b.sums : nullptr;
         if (need_dz) {
@@ -821,19 +1073,23 @@ hipError_t run_layer_backward(const Shape &s, bool gated, const void *dY, const 
         a.M = (int)s.n;
         a.N = (int)s.k;
         a.K = b.rows;
-        a.e.pa = b.power;
+        a.e.pa = b.power ? b.power : b.dZ.power;
         a.e.pb = b.W.power;
         a.e.out = dX;
         RUN(launch_product(kKM, op, kEpiLayer, a, st));
     }
     if (dW) {
         a.A = dz;
+        if (b.dZ_columns)
+            a.A.p = b.dZ_columns;
         a.B = b.X.operand(s.dtype);
         a.M = (int)b.rows;
         a.N = (int)s.k;
         a.K = s.n;
-        a.e.pa = s.n > 0 ? b.power : nullptr;      // no rows: dW = 0, no powers
-        a.e.pb = s.n > 0 ? b.X.power : nullptr;
+        a.e.pa = b.power ? b.power : b.column_power;
+        a.e.pb = b.X.power;
+        if (s.n == 0)                              // no rows: dW = 0, no powers
+            a.e.pa = a.e.pb = nullptr;
         a.e.out = dW;
         RUN(launch_product(kMM, op, kEpiLayer, a, st));
     }

@@ -314,7 +314,7 @@ __device__ __forceinline__ int row_powers(const Epilogue &e, int64_t row0, int64
         return 0;
     static_assert(ROWS <= 64, "a row a lane");
     const int64_t row = row0 + (threadIdx.x & 63);
-    return e.pa[OP == kOpSplit && e.rows_each ? (row < M ? row : M - 1) : 0];
+    return e.pa[OP == kOpSplit ? (row < M ? row : M - 1) : 0];
 }
 
 // the powers of eight columns, of which `valid` exist
@@ -322,10 +322,8 @@ template <int OP, int EPI>
 __device__ __forceinline__ i32x8 column_powers(const Epilogue &e, int64_t col, int valid)
 {
     i32x8 p = 0;
-    if (OP == kOpBf16 || (EPI != kEpiLayer && EPI != kEpiGated) || !e.pb || valid <= 0)
+    if (OP != kOpSplit || (EPI != kEpiLayer && EPI != kEpiGated) || !e.pb || valid <= 0)
         return p;
-    if (OP != kOpSplit || !e.columns_each)
-        return p + *e.pb;
     if (valid >= 8)
         return *reinterpret_cast<const i32x8 *>(e.pb + col);
 #pragma unroll

@@ -358,3 +358,79 @@ def test_outlier_leaves_the_other_rows_alone(g, size, k):
     outs = torch.arange(M, device=DEV) != 17
     assert torch.equal(g.gpic_linear(X, w[:M])[:, outs], Y[:, outs])
     assert torch.equal(g.gpic_gated(X, w)[:, outs], H[:, outs])
+
+
+@pytest.mark.parametrize("size", [1e6, 1e13, 1e28])
+def test_outlier_leaves_the_other_gradients_alone(g, size):
+    """One huge finite entry of dY, X, W or Z: the rows and columns of the
+    gradients that do not sum over it keep their bits."""
+    _all_tiled(g, N, K, M, "f32")
+    X, W = _randn((N, K), "f32", 1), _randn((2 * M, K), "f32", 2, K ** -0.5)
+    dY, Z = _randn((N, M), "f32", 3, 0.01), _randn((N, 2 * M), "f32", 4)
+    rows = torch.arange(N, device=DEV) != 17
+    ins = torch.arange(K, device=DEV) != 3
+    outs = torch.arange(M, device=DEV) != 5
+    both = torch.cat([outs, outs])
+
+    def lin(dy, x, w):
+        return g.gpic_linear_backward(dy, x, w[:M], Z[:, :M], "gelu")
+
+    def gat(dy, x, w, z=Z):
+        return g.gpic_gated_backward(dy, x, w, z)
+
+    dy, x, w = dY.clone(), X.clone(), W.clone()
+    dy[17, 5] = x[17, 3] = w[5, 3] = size
+    for f, keep in ((lin, outs), (gat, both)):
+        want = f(dY, X, W)
+        got = f(dy, X, W)
+        assert torch.equal(got.dX[rows], want.dX[rows])
+        assert torch.equal(got.dW[keep], want.dW[keep])
+        got = f(dY, x, W)
+        assert torch.equal(got.dX, want.dX) and torch.equal(got.dW[:, ins], want.dW[:, ins])
+        got = f(dY, X, w)
+        assert torch.equal(got.dX[:, ins], want.dX[:, ins]) and torch.equal(got.dW, want.dW)
+    # what does sum over it, to the bound of its own rows and columns
+    dz = dy.double() * _act(Z[:, :M].double(), "gelu")[1]
+    off = 1e-6 * dy.double().abs() * (1 + Z[:, :M].double().abs())
+    xd, wd = x.double(), W[:M].double()
+    gr = lin(dy, x, W)
+    for got, ref, bound, what in (
+            (gr.dX, dz @ wd, off @ wd.abs() + _forward_bound(dz, wd.t()), "dX"),
+            (gr.dW, dz.t() @ xd, off.t() @ xd.abs() + _forward_bound(dz.t(), xd.t()), "dW")):
+        over = ref.abs() > torch.finfo(torch.float32).max        # infinite in float32
+        assert torch.equal(got[over], ref[over].float()), what
+        _close(got[~over], ref[~over], bound[~over], "f32", what)
+    # a point with a huge Z that no gradient reaches
+    dy, z = dY.clone(), Z.clone()
+    dy[17] = 0.0
+    want = gat(dy, X, W)
+    z[17] = size
+    got = gat(dy, X, W, z)
+    assert torch.equal(got.dX, want.dX) and torch.equal(got.dW, want.dW)
+
+
+@pytest.mark.parametrize("shape", [(2100, 70, 270), (5000, 300, 66), (40, 1100, 4300),
+                                   (70000, 33, 20)], ids=str)
+def test_float32_gradients_of_uneven_shapes(g, shape):
+    """Every strip and part of the maxima: a scale that is off by a row or a
+    column shows where rows and columns differ by powers of two."""
+    n, k, m = shape
+    _tiled(g, "linear_backward", n, k, m, "f32")
+    _tiled(g, "gated_backward", n, k, m, "f32")
+    up = lambda s, i: 2.0 ** (_randn((s,), "f32", i, 8.0).round())  # noqa: E731
+    X, W = _randn((n, k), "f32", 1) * up(k, 10), _randn((2 * m, k), "f32", 2, k ** -0.5) * up(k, 11)
+    dY = _randn((n, m), "f32", 3) * up(n, 12)[:, None]
+    Z = _randn((n, 2 * m), "f32", 4)
+    x, w, dy, zz = X.double(), W.double(), dY.double(), Z.double()
+    gr = g.gpic_linear_backward(dY, X, W[:m], Z[:, :m], "silu")
+    dz = dy * _act(zz[:, :m], "silu")[1]
+    off = 1e-6 * dy.abs() * (1 + zz[:, :m].abs())
+    _close(gr.dX, dz @ w[:m], off @ w[:m].abs() + _forward_bound(dz, w[:m].t()), "f32", "dX")
+    _close(gr.dW, dz.t() @ x, off.t() @ x.abs() + _forward_bound(dz.t(), x.t()), "f32", "dW")
+    gr = g.gpic_gated_backward(dY, X, W, Z)
+    a, da = _act(zz[:, :m], "silu")
+    dz = torch.cat([dy * zz[:, m:] * da, dy * a], 1)
+    off = 1e-6 * torch.cat([(dy * zz[:, m:]).abs() * (1 + zz[:, :m].abs()),
+                            (dy * zz[:, :m]).abs()], 1)
+    _close(gr.dX, dz @ w, off @ w.abs() + _forward_bound(dz, w.t()), "f32", "gated dX")
+    _close(gr.dW, dz.t() @ x, off.t() @ x.abs() + _forward_bound(dz.t(), x.t()), "f32", "gated dW")
