@@ -525,7 +525,8 @@ gpic_status gpic_gated(const gpic_layer_params *p, const void *X, const void *W,
                        void *Z, void *ws, size_t ws_bytes, void *stream);
 
 /* Gradients of the same: dZg = dH * Zu * act'(Zg), dZu = dH * act(Zg), dX =
- * dZ W, dW = dZ^T X.  As gpic_linear_backward.
+ * dZ W, dW = dZ^T X.  As gpic_linear_backward (float16's power of two is
+ * from the largest finite |dZ|).
  * ws: gpic_layer_workspace_bytes(GPIC_GATED_BACKWARD, p). */
 gpic_status gpic_gated_backward(const gpic_layer_params *p, const void *dH, const void *X,
                                 const void *W, const void *Z, void *dX, void *dW, void *ws,

@@ -14,7 +14,6 @@ namespace gpic {
 
 namespace {
 
-constexpr int kMaxParts = 1024;       // partial maxima per matrix
 constexpr int kSumRows = 64;          // most rows of a partial column sum
 
 inline size_t up(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -33,64 +32,13 @@ struct Cursor {
 };
 
 // ---------------------------------------------------------------- maxima
-struct MaxJob {
-    const void *x;
-    int64_t rows, cols, ld;
-    int dtype;
-    float *part;           // [kMaxParts]
-};
-struct MaxJobs {
-    MaxJob j[4];
-};
-
-// Largest finite |x| of up to four matrices (grid.y), one partial a
-// workgroup.  Reads the matrices once: 10,007 x 777, 10,007 x 1,000 and
-// 777 x 1,000 in float32 (74 MB) in 12.4 us, 6.0 TB/s with what the caches
-// still hold of them; 1,003 x 300 in 3.6 us, a launch's time.
-__global__ __launch_bounds__(256) void absmax_kernel(MaxJobs jobs)
-{
-    const MaxJob m = jobs.j[blockIdx.y];
-    const int64_t total = m.rows * m.cols, stride = (int64_t)gridDim.x * 256;
-    float best = 0.0f;
-    if (m.ld == m.cols) {
-        const int64_t quads = total / 4;
-        for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < quads; i += stride) {
-            const f32x4 v = load4(m.x, i * 4, m.dtype);
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const float a = fabsf(v[c]);
-                best = a < INFINITY && a > best ? a : best;
-            }
-        }
-        for (int64_t i = quads * 4 + (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += stride) {
-            const float a = fabsf(load1(m.x, i, m.dtype));
-            best = a < INFINITY && a > best ? a : best;
-        }
-    } else {
-        for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += stride) {
-            const int64_t r = i / m.cols;
-            const float a = fabsf(load1(m.x, r * m.ld + (i - r * m.cols), m.dtype));
-            best = a < INFINITY && a > best ? a : best;
-        }
-    }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1)
-        best = fmaxf(best, __shfl_xor(best, o, 64));
-    __shared__ float w[4];
-    if ((threadIdx.x & 63) == 0)
-        w[threadIdx.x >> 6] = best;
-    __syncthreads();
-    if (threadIdx.x == 0)
-        m.part[blockIdx.x] = fmaxf(fmaxf(w[0], w[1]), fmaxf(w[2], w[3]));
-}
-
-// The block's largest of the kMaxParts partial maxima (256 threads).
-__device__ __forceinline__ float join_max(const float *part)
+// The largest of `count` values, by a block of 256 threads.
+__device__ __forceinline__ float join_max(const float *part, int count)
 {
     float best = 0.0f;
-#pragma unroll
-    for (int i = 0; i < kMaxParts / 256; ++i)
-        best = fmaxf(best, part[i * 256 + threadIdx.x]);
+#pragma unroll 4
+    for (int i = threadIdx.x; i < count; i += 256)
+        best = fmaxf(best, part[i]);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1)
         best = fmaxf(best, __shfl_xor(best, o, 64));
@@ -312,7 +260,8 @@ struct GradArgs {
     int64_t ldd;           // row pitch of both in 16-bit values
     int rows;              // of a workgroup
     float *sums;           // [ceil(n / rows)][m] partial column sums, or null
-    const float *max_dy, *max_z;     // float16: partial maxima (Z: gated only)
+    const float *part;     // float16: partial maxima of dZ
+    int parts;
     int *power;            // float16: dZ is stored times two to this; null: 0
     // float32: the powers of dZ's rows and of its columns
     const int *row_power, *column_power;
@@ -391,8 +340,9 @@ __device__ __forceinline__ void form4(f32x4 dy, f32x4 g, f32x4 u, f32x4 &d, f32x
         }
 }
 
-// Partial maxima of a float32 matrix's columns, or of dZ's columns and rows:
-// `parts` runs of `each` rows by strips of 256 columns.
+// Partial maxima of a float32 matrix's columns, or of dZ's columns and rows
+// (float16: of dZ as a whole): `parts` runs of `each` rows by strips of 256
+// columns.
 struct Maxima {
     const float *x;        // null: dZ
     int64_t rows, cols, ld;
@@ -403,8 +353,9 @@ struct Maxima {
 struct MaximaArgs {
     Maxima j[3];
     int count;
-    // dZ from these; its rows' maxima go to row_part [strips][rows]
-    const float *dY, *Z;
+    // dZ from these; its rows' maxima go to row_part [strips][rows], float16: its
+    // own, one a workgroup, to row_part [parts strips]
+    const void *dY, *Z;
     int64_t ldy, ldz, m;
     float *row_part;
 };
@@ -415,9 +366,10 @@ struct MaximaArgs {
 // bounds stands in for a maximum.  Bound by memory and by the activation: dY
 // and Z of 10,007 x 777 with gelu, X of 10,007 x 1,000 and W (96 MB) 23 us, 4.2
 // TB/s; the powers from the partial maxima 6 us.
-template <int ACT, bool GATED>
+template <int DT, int ACT, bool GATED>
 __global__ __launch_bounds__(256) void maxima_kernel(MaximaArgs a)
 {
+    constexpr int ZT = GATED ? GPIC_F32 : DT;      // the type of Z
     int64_t id = blockIdx.x;
     int job = 0;
     while (job + 1 < a.count && id >= a.j[job].blocks())
@@ -437,11 +389,11 @@ __global__ __launch_bounds__(256) void maxima_kernel(MaximaArgs a)
             const int64_t row = r + 4 * i;
             if (row < r1 && col < cols) {
                 x[i] = m.x ? read4(m.x, row * m.ld, col, cols, GPIC_F32)
-                           : read4(a.dY, row * a.ldy, col, cols, GPIC_F32);
+                           : read4(a.dY, row * a.ldy, col, cols, DT);
                 if (!m.x && (GATED || ACT != GPIC_ACT_NONE))
-                    g[i] = read4(a.Z, row * a.ldz, col, cols, GPIC_F32);
+                    g[i] = read4(a.Z, row * a.ldz, col, cols, ZT);
                 if (!m.x && GATED)
-                    u[i] = read4(a.Z, row * a.ldz + a.m, col, cols, GPIC_F32);
+                    u[i] = read4(a.Z, row * a.ldz + a.m, col, cols, ZT);
             }
         }
 #pragma unroll
@@ -458,7 +410,7 @@ __global__ __launch_bounds__(256) void maxima_kernel(MaximaArgs a)
                 most = v < INFINITY && v > most ? v : most;
                 most = w < INFINITY && w > most ? w : most;
             }
-            if (m.x)
+            if (m.x || DT == GPIC_F16)
                 continue;
 #pragma unroll
             for (int o = 32; o > 0; o >>= 1)
@@ -467,6 +419,19 @@ __global__ __launch_bounds__(256) void maxima_kernel(MaximaArgs a)
             if (lane == 0 && row < r1)
                 a.row_part[strip * m.rows + row] = most;
         }
+    }
+    if (DT == GPIC_F16) {
+        float most = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            most = fmaxf(most, fmaxf(best[j], best_u[j]));
+        __shared__ float each[256];
+        each[threadIdx.x] = most;
+        __syncthreads();
+        most = join_max(each, 256);
+        if (threadIdx.x == 0)
+            a.row_part[blockIdx.x] = most;
+        return;
     }
     __shared__ f32x4 all[2][256];
     all[0][threadIdx.x] = best;
@@ -544,11 +509,7 @@ __global__ __launch_bounds__(256) void grad_kernel(GradArgs a)
     constexpr int ZT = GATED ? GPIC_F32 : DT;      // the type of Z
     int power = 0;
     if (DT == GPIC_F16 && a.power) {
-        // |act'| <= 1.13, and the gated forms multiply by |Z| or |act(Z)| <= |Z|
-        float most = 1.25f * join_max(a.max_dy);
-        if (a.max_z)
-            most *= fmaxf(1.0f, join_max(a.max_z));
-        power = power_for(most < INFINITY ? most : 3.0e38f);
+        power = power_for(join_max(a.part, a.parts));
         if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0)
             *a.power = power;
     }
@@ -710,15 +671,6 @@ void place(Source &s, int dtype, Cursor &c, int64_t powers)
         s.power = static_cast<int *>(c.take((size_t)powers * 4));
 }
 
-hipError_t launch_absmax(const MaxJob *jobs, int count, hipStream_t st)
-{
-    MaxJobs j{};
-    for (int i = 0; i < count; ++i)
-        j.j[i] = jobs[i];
-    absmax_kernel<<<dim3(kMaxParts, (unsigned)count), 256, 0, st>>>(j);
-    return hipGetLastError();
-}
-
 // X and W of a float32 layer, a power of two for every row
 hipError_t launch_split_rows(const Source &x, const Source &w, hipStream_t st)
 {
@@ -837,13 +789,12 @@ struct Backward {
     Source dZ, X, W;
     void *dZ_columns = nullptr;      // float32: dW's copy of dZ, the powers of its columns
     int *column_power = nullptr;
-    Maxima mz{}, mx{}, mw{};         // float32
-    float *row_part = nullptr;       // [mz.strips][n]
+    Maxima mz{}, mx{}, mw{};         // float32 (mz: float16 too)
+    float *row_part = nullptr;       // [mz.strips][n], float16: [mz.blocks()]
     bool form;             // dZ is formed by grad_kernel (else dY is read)
     float *sums;
     int rows_each;         // rows of a workgroup of grad_kernel
-    float *max_dy, *max_z;
-    int *power;
+    int *power;            // float16: of all of dZ
     float *part;
     int64_t rows;
     Backward(const Shape &s, bool gated, const void *dy, const void *x, const void *w, Cursor &c)
@@ -867,12 +818,15 @@ struct Backward {
                 m->part = static_cast<float *>(c.take((size_t)(m->parts * m->cols) * 4));
             row_part = static_cast<float *>(c.take((size_t)(mz.strips * s.n) * 4));
         }
-        // a dZ that is formed in half precision has a scale too: gradients
-        // times act' soon fall below 6e-5, where halves lose bits
-        const bool scaled = form && s.dtype == GPIC_F16;
-        max_dy = scaled ? static_cast<float *>(c.take(kMaxParts * 4)) : nullptr;
-        max_z = scaled && gated ? static_cast<float *>(c.take(kMaxParts * 4)) : nullptr;
-        power = scaled ? static_cast<int *>(c.take(4)) : nullptr;
+        // a dZ that is formed in half precision has a power too, from its own
+        // largest magnitude (not gated: dY's): gradients times act' soon fall
+        // below 6e-5, where halves lose bits
+        power = nullptr;
+        if (form && s.dtype == GPIC_F16) {
+            mz = maxima_of(nullptr, s.n, rows, 0, s.m);
+            row_part = static_cast<float *>(c.take((size_t)mz.blocks() * 4));
+            power = static_cast<int *>(c.take(4));
+        }
         rows_each = grad_rows(s.n, s.m);
         sums = static_cast<float *>(
             c.take((size_t)((s.n + rows_each - 1) / rows_each) * s.m * 4));
@@ -891,22 +845,22 @@ struct Backward {
     } while (0)
 
 // The powers of two of a float32 backward call: of W's columns and dZ's rows
-// for dX, of X's and dZ's columns for dW.
-template <bool GATED>
+// for dX, of X's and dZ's columns for dW.  float16: dZ's partial maxima.
+template <int DT, bool GATED>
 void launch_maxima(const MaximaArgs &a, int act, unsigned blocks, hipStream_t st)
 {
     switch (act) {
     case GPIC_ACT_NONE:
-        maxima_kernel<GPIC_ACT_NONE, GATED><<<blocks, 256, 0, st>>>(a);
+        maxima_kernel<DT, GPIC_ACT_NONE, GATED><<<blocks, 256, 0, st>>>(a);
         break;
     case GPIC_ACT_RELU:
-        maxima_kernel<GPIC_ACT_RELU, GATED><<<blocks, 256, 0, st>>>(a);
+        maxima_kernel<DT, GPIC_ACT_RELU, GATED><<<blocks, 256, 0, st>>>(a);
         break;
     case GPIC_ACT_GELU:
-        maxima_kernel<GPIC_ACT_GELU, GATED><<<blocks, 256, 0, st>>>(a);
+        maxima_kernel<DT, GPIC_ACT_GELU, GATED><<<blocks, 256, 0, st>>>(a);
         break;
     default:
-        maxima_kernel<GPIC_ACT_SILU, GATED><<<blocks, 256, 0, st>>>(a);
+        maxima_kernel<DT, GPIC_ACT_SILU, GATED><<<blocks, 256, 0, st>>>(a);
     }
 }
 
@@ -915,19 +869,20 @@ hipError_t launch_powers(const Shape &s, bool gated, const Backward &b, const vo
 {
     MaximaArgs a{};
     PowerJobs p{};
+    const bool f32 = s.dtype == GPIC_F32;
     a.j[a.count++] = b.mz;
-    if (dX) {
+    if (dX && f32) {
         a.j[a.count++] = b.mw;
         p.j[p.count++] = PowerJob{b.mw.part, s.k, b.mw.parts, b.W.power};
         p.j[p.count++] = PowerJob{b.row_part, s.n, b.mz.strips, b.dZ.power};
     }
-    if (dW) {
+    if (dW && f32) {
         a.j[a.count++] = b.mx;
         p.j[p.count++] = PowerJob{b.mx.part, s.k, b.mx.parts, b.X.power};
         p.j[p.count++] = PowerJob{b.mz.part, b.rows, b.mz.parts, b.column_power};
     }
-    a.dY = static_cast<const float *>(dY);
-    a.Z = static_cast<const float *>(Z);
+    a.dY = dY;
+    a.Z = Z;
     a.ldy = s.ldy;
     a.ldz = s.ldz;
     a.m = s.m;
@@ -935,11 +890,17 @@ hipError_t launch_powers(const Shape &s, bool gated, const Backward &b, const vo
     int64_t blocks = 0;
     for (int i = 0; i < a.count; ++i)
         blocks += a.j[i].blocks();
-    if (gated)
-        launch_maxima<true>(a, s.act, (unsigned)blocks, st);
-    else
-        launch_maxima<false>(a, s.act, (unsigned)blocks, st);
+    if (f32 && gated)
+        launch_maxima<GPIC_F32, true>(a, s.act, (unsigned)blocks, st);
+    else if (f32)
+        launch_maxima<GPIC_F32, false>(a, s.act, (unsigned)blocks, st);
+    else if (gated)
+        launch_maxima<GPIC_F16, true>(a, s.act, (unsigned)blocks, st);
+    else               // |dZ| <= 1.13 |dY|: the maxima of dY, without reading Z
+        maxima_kernel<GPIC_F16, GPIC_ACT_NONE, false><<<(unsigned)blocks, 256, 0, st>>>(a);
     RUN(hipGetLastError());
+    if (!f32)
+        return hipSuccess;
     blocks = 0;
     for (int i = 0; i < p.count; ++i)
         blocks += p.j[i].blocks();
@@ -1014,12 +975,7 @@ hipError_t run_layer_backward(const Shape &s, bool gated, const void *dY, const 
     if (!dX || s.n == 0)
         b.W.pack = false;
     const bool need_dz = dX || dW;
-    if (need_dz && b.power && s.n > 0) {
-        const MaxJob jobs[2] = {{dY, s.n, s.m, s.ldy, s.dtype, b.max_dy},
-                                {Z, s.n, b.rows, s.ldz, GPIC_F32, b.max_z}};
-        RUN(launch_absmax(jobs, b.max_z ? 2 : 1, st));
-    }
-    if (need_dz && s.dtype == GPIC_F32 && s.n > 0)
+    if (need_dz && b.mz.parts > 0)
         RUN(launch_powers(s, gated, b, dY, Z, dX != nullptr, dW != nullptr, st));
     {
         Source plain = b.dZ;
@@ -1043,8 +999,8 @@ hipError_t run_layer_backward(const Shape &s, bool gated, const void *dY, const 
         g.ldd = s.dtype == GPIC_F32 ? split_ld(b.rows) : up64(b.rows);
         g.sums = db ? b.sums : nullptr;
         if (need_dz) {
-            g.max_dy = b.max_dy;
-            g.max_z = b.max_z;
+            g.part = b.row_part;
+            g.parts = (int)b.mz.blocks();
             g.power = b.power;
         }
         const int64_t width = gated ? s.m : up64(s.m);

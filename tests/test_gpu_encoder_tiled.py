@@ -434,3 +434,18 @@ def test_float32_gradients_of_uneven_shapes(g, shape):
                             (dy * zz[:, :m]).abs()], 1)
     _close(gr.dX, dz @ w, off @ w.abs() + _forward_bound(dz, w.t()), "f32", "gated dX")
     _close(gr.dW, dz.t() @ x, off.t() @ x.abs() + _forward_bound(dz.t(), x.t()), "f32", "gated dW")
+
+
+@pytest.mark.parametrize("size", [1e6, 1e13, 1e30])
+def test_float16_gradients_beside_a_huge_z(g, size):
+    """A point with a huge Z that no gradient reaches takes no bits of dZ:
+    its power of two comes from dZ itself, not from dH's and Z's largest."""
+    _tiled(g, "gated_backward", N, K, M, "f16")
+    X, W = _randn((N, K), "f16", 1), _randn((2 * M, K), "f16", 2, K ** -0.5)
+    dH, Z = _randn((N, M), "f16", 3, 1e-3), _randn((N, 2 * M), "f32", 4)
+    dH[17] = 0.0
+    want = g.gpic_gated_backward(dH, X, W, Z)
+    z = Z.clone()
+    z[17] = size
+    got = g.gpic_gated_backward(dH, X, W, z)
+    assert torch.equal(got.dX, want.dX) and torch.equal(got.dW, want.dW)
