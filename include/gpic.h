@@ -537,10 +537,12 @@ typedef struct gpic_polar_params {
                             65535; m, n 1 .. 2^20)                                */
     int32_t dtype;       /* GPIC_F32, GPIC_F16 or GPIC_BF16                       */
     int32_t steps;       /* 1 .. 64                                               */
-    float a, b, c;       /* the polynomial a x + b x^3 + c x^5; each at most 16 in
-                            magnitude.  It has to keep [0, 1] below 2 (as the
-                            usual 3.4445, -4.7750, 2.0315 and the quintic 15/8,
-                            -10/8, 3/8 do)                                        */
+    float a, b, c;       /* the polynomial q(x) = a x + b x^3 + c x^5; each at most
+                            16 in magnitude.  Let B_1 = 1, B_{i+1} the largest
+                            |q| over [0, B_i] times 257/256: with every B_i^2 up
+                            to B_steps, and |b x^2 + c x^4| on [0, B_i], at most
+                            60 (the usual 3.4445, -4.7750, 2.0315 and the quintic
+                            15/8, -10/8, 3/8 stay below 3); else INVALID_ARG      */
     int32_t reserved;    /* must be 0                                             */
     double eps;          /* >= 0; added to the Frobenius norm                     */
 } gpic_polar_params;

@@ -85,6 +85,49 @@ Shape shape_of(const gpic_layer_params *p)
     return s;
 }
 
+// Largest |c1 s + c3 s^3 + c5 s^5| over [0, top]: the end or where the
+// derivative c1 + 3 c3 s^2 + 5 c5 s^4 is zero.
+double largest_odd(double c1, double c3, double c5, double top)
+{
+    auto at = [&](double s) { return fabs(s * (c1 + s * s * (c3 + s * s * c5))); };
+    double most = at(top);
+    auto consider = [&](double t) {
+        if (t > 0.0 && t < top * top)
+            most = fmax(most, at(sqrt(t)));
+    };
+    if (c5 == 0.0) {
+        consider(c3 != 0.0 ? -c1 / (3.0 * c3) : 0.0);
+        return most;
+    }
+    const double root = 9.0 * c3 * c3 - 20.0 * c5 * c1;
+    if (root >= 0.0) {
+        consider((-3.0 * c3 + sqrt(root)) / (10.0 * c5));
+        consider((-3.0 * c3 - sqrt(root)) / (10.0 * c5));
+    }
+    return most;
+}
+
+// The iterates are held in halves times 1,024 (orthogonalize.hip): entries of
+// A = X X^T are at most the square of X's largest singular value, those of
+// b A + c A^2 at most |b s^2 + c s^4| there.  From 1 at the start, the bound of
+// a step's singular values is the polynomial's largest over the step's before,
+// and 1/256 for what is rounded.  The last step's result is no iterate.
+gpic_status check_polynomial(const gpic_polar_params *p)
+{
+    const double a = p->a, b = p->b, c = p->c, limit = 60.0;     // 65,504 / 1,024 is 63.97
+    double top = 1.0;
+    for (int k = 0; k < p->steps; ++k) {
+        double poly = fabs(top * top * (b + c * top * top));
+        if (c != 0.0 && -b / (2.0 * c) > 0.0 && -b / (2.0 * c) < top * top)
+            poly = fmax(poly, b * b / (4.0 * fabs(c)));
+        CHECK_ARG(top * top <= limit && poly <= limit,
+                  "the polynomial takes singular values up to %g at step %d of %d: they must stay "
+                  "below 7.7, and |b s^2 + c s^4| below 60 on them", top, k + 1, p->steps);
+        top = largest_odd(a, b, c, top) * (1.0 + 1.0 / 256.0);
+    }
+    return GPIC_OK;
+}
+
 gpic_status check_polar(const gpic_polar_params *p)
 {
     CHECK_ARG(p != nullptr, "params is null");
@@ -99,7 +142,7 @@ gpic_status check_polar(const gpic_polar_params *p)
               "coefficients must be finite and at most 16 in magnitude");
     CHECK_ARG(isfinite(p->eps) && p->eps >= 0.0, "eps must be finite and >= 0");
     CHECK_ARG(p->reserved == 0, "reserved must be 0");
-    return GPIC_OK;
+    return check_polynomial(p);
 }
 
 Polar polar_of(const gpic_polar_params *p)

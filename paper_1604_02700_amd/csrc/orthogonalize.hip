@@ -34,8 +34,9 @@ namespace {
 constexpr int kParts = 1024;           // partial sums of squares per matrix
 constexpr int64_t kSplitSide = 64;     // bfloat16: split operands up to this smaller side
 constexpr float kStore = 1024.0f;      // X, A, P are stored times this: entries of
-                                       // X are <= 1.3, of P <= 64 for any coefficients
-                                       // the entry points accept
+                                       // each are at most 60 for the coefficients and
+                                       // steps that the entry points accept (1.3 and
+                                       // 2.8 for the usual ones)
 
 inline size_t up(size_t x) { return (x + 255) & ~(size_t)255; }
 __host__ __device__ inline int64_t up64(int64_t x) { return (x + 63) & ~(int64_t)63; }

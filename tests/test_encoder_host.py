@@ -157,3 +157,32 @@ def test_binding_refuses_host_tensors(g):
                  lambda: g.gpic_muon_step(x, x, x, 0.1)):
         with pytest.raises(TypeError):
             call()
+
+
+@pytest.mark.parametrize("steps, a, b, c, ok", [
+    (64, 3.4445, -4.775, 2.0315, True), (64, 15 / 8, -10 / 8, 3 / 8, True), (64, 1.5, -0.5, 0.0, True),
+    (1, 16.0, 0.0, 0.0, True), (1, 16.0, -16.0, 16.0, True), (64, 0.0, 0.0, 0.0, True),
+    # singular values that grow from step to step: 1.9^3 = 6.9, 1.9^4 = 13
+    (4, 1.9, 0.0, 0.0, True), (5, 1.9, 0.0, 0.0, False), (2, 16.0, 0.0, 0.0, False),
+    # below 4 after a step, but b x^2 + c x^4 is not there
+    (1, 1.0, 15.0, -15.0, True), (2, 1.0, 15.0, -15.0, False),
+    # the largest value is inside the interval: 2.3 for a polynomial that is 0 at 1
+    (2, 6.0, -6.0, 0.0, True), (3, 6.0, -6.0, 0.0, False)], ids=str)
+def test_polynomials_that_leave_the_halves_are_refused(g, steps, a, b, c, ok):
+    """Against the same bound by dense sampling; a refused step advances nothing."""
+    import numpy as np
+    top, fits = 1.0, True
+    a32, b32, c32 = (float(np.float32(v)) for v in (a, b, c))
+    for _ in range(steps):
+        s = np.linspace(0.0, top, 200001)
+        fits = fits and top * top <= 60 and float(np.abs(b32 * s ** 2 + c32 * s ** 4).max()) <= 60
+        top = float(np.abs(a32 * s + b32 * s ** 3 + c32 * s ** 5).max()) * 257 / 256
+    assert fits == ok
+    L, d = g.lib(), C.c_void_p(4096)            # never dereferenced: refused, or no workspace
+    p = C.byref(_polar(g, steps=steps, a=a, b=b, c=c, m=640, n=960))
+    h = C.byref(g.MuonParams(lr=0.1, momentum=0.9, weight_decay=0.0, scale=1.0, nesterov=1,
+                             reserved=0))
+    assert (L.gpic_polar_workspace_bytes(p) > 0) == ok
+    assert L.gpic_orthogonalize(p, d, d, None, 0, None) == (2 if ok else 1)
+    assert L.gpic_muon_step(p, h, d, d, d, None, 0, None) == (2 if ok else 1)
+    assert ok or b"singular values" in L.gpic_last_error()

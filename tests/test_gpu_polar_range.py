@@ -1,0 +1,50 @@
+"""Orthogonalised updates at the ends of what the polynomial may do: the
+iterates are held in half precision, so what the entry points accept must
+stay finite and right there, and the rest must be refused."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+from test_gpu_encoder import DEV, T, U, _gradient, _polar, _rel  # noqa: E402
+
+
+@pytest.fixture(scope="module")
+def g():
+    import paper_1604_02700_amd as g
+    g.lib()
+    return g
+
+
+@pytest.mark.parametrize("dtype", list(T))
+@pytest.mark.parametrize("shape", [(60, 90), (300, 200), (130, 520)], ids=str)
+def test_growing_singular_values(g, shape, dtype):
+    """A matrix of rank one has the singular value 1 at the start.  1.9 x takes
+    it to 1.9^3 = 6.9 before the fourth step, where A's entries reach 47; 6 x -
+    3 x^3 to 3, where b A is 27; x + 15 x^3 - 15 x^5 cancels to 1.  Halves are
+    off by 2^-12, A by 2^-11; the steepest of the three, the last, takes that
+    to 15 (2^-11) of the result, twice that with the other roundings."""
+    m, n = shape
+    u = torch.where(torch.arange(m, device=DEV) % 3 == 0, -1.0, 1.0)[:, None]
+    v = torch.zeros((1, n), device=DEV)
+    v[0, 5] = 1.0                                   # one column: A's entries are 1 / m ..
+    one = torch.zeros((m, n), device=DEV)
+    one[3, 5] = 1.0                                 # .. and one entry: A has a 1
+    for G in ((u @ v).to(T[dtype]), one.to(T[dtype])):
+        for steps, coef in ((4, (1.9, 0.0, 0.0)), (1, (1.0, 15.0, -15.0)), (2, (6.0, -3.0, 0.0))):
+            print(f"polar {shape} {dtype} {steps} {coef}", flush=True)
+            O = g.gpic_orthogonalize(G, steps, coef)
+            assert bool(torch.isfinite(O).all())
+            ref = _polar(G[None], steps, coef)
+            assert _rel(O[None], ref) <= 2.0 ** -6 + U[dtype]
+    with pytest.raises(g.GpicError, match="singular values"):
+        g.gpic_orthogonalize(one.to(T[dtype]), 5, (1.9, 0.0, 0.0))
+
+
+def test_a_refused_step_changes_nothing(g):
+    W, G = _gradient((1, 130, 520), 1), _gradient((1, 130, 520), 2)
+    M = torch.ones_like(W)
+    w = W.clone()
+    with pytest.raises(g.GpicError, match="singular values"):
+        g.gpic_muon_step(W, G, M, 0.1, coefficients=(1.9, 0.0, 0.0))
+    assert torch.equal(W, w) and bool((M == 1).all())
