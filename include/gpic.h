@@ -456,7 +456,9 @@ gpic_status gpic_read_stream(const float *x, int64_t n, double *sink, void *stre
  * 2,048 and n k m (gated: twice that) up to 2^28 in float32, and in 16 bits up
  * to 2^26 with n and m (gated: 2 m) up to 1,024, else 2^22.  A NaN or an infinity in a row of X (a column's
  * weights) makes that row (column) of the result non-finite and no other.
- * Results are bitwise reproducible.  Asynchronous. */
+ * Results are bitwise reproducible.  A product of more workgroups than a
+ * launch takes (more than 2^31 - 128 rows, beyond small calls) is UNSUPPORTED.
+ * Asynchronous. */
 
 /* Element types. */
 enum { GPIC_F32 = 0, GPIC_F16 = 1, GPIC_BF16 = 2 };
@@ -496,7 +498,7 @@ size_t gpic_layer_workspace_bytes(int32_t op, const gpic_layer_params *p);
  * receives X W^T + bias, which the gradient needs.  Y may be the residual's
  * own buffer (same pitch); no other overlap.  n = 0 does nothing.
  * ws: gpic_layer_workspace_bytes(GPIC_LAYER_FORWARD, p).  Errors:
- * INVALID_ARG, WORKSPACE. */
+ * INVALID_ARG, WORKSPACE, UNSUPPORTED. */
 gpic_status gpic_linear(const gpic_layer_params *p, const void *X, const void *W,
                         const void *bias, const void *residual, void *Y, void *Z,
                         void *ws, size_t ws_bytes, void *stream);

@@ -85,6 +85,15 @@ Shape shape_of(const gpic_layer_params *p)
     return s;
 }
 
+gpic_status check_fits(const gpic_layer_params *p, bool gated, bool backward)
+{
+    if (!layer_fits(shape_of(p), gated, backward))
+        return fail(GPIC_ERR_UNSUPPORTED, "n = %lld, k = %lld, m = %lld: a product of more "
+                    "workgroups than a launch takes", (long long)p->n, (long long)p->k,
+                    (long long)p->m);
+    return GPIC_OK;
+}
+
 // Largest |c1 s + c3 s^3 + c5 s^5| over [0, top]: the end or where the
 // derivative c1 + 3 c3 s^2 + 5 c5 s^4 is zero.
 double largest_odd(double c1, double c3, double c5, double top)
@@ -176,9 +185,10 @@ size_t gpic_layer_workspace_bytes(int32_t op, const gpic_layer_params *p)
     if (op < GPIC_LAYER_FORWARD || op > GPIC_GATED_BACKWARD)
         return 0;
     const bool gated = op >= GPIC_GATED_FORWARD;
-    if (check_layer(p, gated) != GPIC_OK)
+    const bool backward = op == GPIC_LAYER_BACKWARD || op == GPIC_GATED_BACKWARD;
+    if (check_layer(p, gated) != GPIC_OK || check_fits(p, gated, backward) != GPIC_OK)
         return 0;
-    return layer_ws(shape_of(p), gated, op == GPIC_LAYER_BACKWARD || op == GPIC_GATED_BACKWARD);
+    return layer_ws(shape_of(p), gated, backward);
 }
 
 gpic_status gpic_linear(const gpic_layer_params *p, const void *X, const void *W,
@@ -197,6 +207,7 @@ gpic_status gpic_linear(const gpic_layer_params *p, const void *X, const void *W
               "ldr = %lld not in [m, 2^22]", (long long)p->ldr);
     if (Z != nullptr)
         CHECK(check_pre(p, false));
+    CHECK(check_fits(p, false, false));
     CHECK(check_ws(ws, ws_bytes, layer_ws(shape_of(p), false, false)));
     CHECK_HIP(run_layer(shape_of(p), false, X, W, bias, residual, Y, Z, ws,
                         (hipStream_t)stream),
@@ -220,6 +231,7 @@ gpic_status gpic_linear_backward(const gpic_layer_params *p, const void *dY, con
     CHECK(check_matrix(db, "db", p->dtype, true));
     if (act)
         CHECK(check_pre(p, false));
+    CHECK(check_fits(p, false, true));
     CHECK(check_ws(ws, ws_bytes, layer_ws(shape_of(p), false, true)));
     CHECK_HIP(run_layer_backward(shape_of(p), false, dY, X, W, Z, dX, dW, db, ws,
                                  (hipStream_t)stream),
@@ -238,6 +250,7 @@ gpic_status gpic_gated(const gpic_layer_params *p, const void *X, const void *W,
     CHECK(check_matrix(Z, "Z", GPIC_F32, true));
     if (Z != nullptr)
         CHECK(check_pre(p, true));
+    CHECK(check_fits(p, true, false));
     CHECK(check_ws(ws, ws_bytes, layer_ws(shape_of(p), true, false)));
     CHECK_HIP(run_layer(shape_of(p), true, X, W, nullptr, nullptr, H, Z, ws,
                         (hipStream_t)stream),
@@ -258,6 +271,7 @@ gpic_status gpic_gated_backward(const gpic_layer_params *p, const void *dH, cons
     CHECK(check_matrix(dX, "dX", p->dtype, true));
     CHECK(check_matrix(dW, "dW", p->dtype, true));
     CHECK(check_pre(p, true));
+    CHECK(check_fits(p, true, true));
     CHECK(check_ws(ws, ws_bytes, layer_ws(shape_of(p), true, true)));
     CHECK_HIP(run_layer_backward(shape_of(p), true, dH, X, W, Z, dX, dW, nullptr, ws,
                                  (hipStream_t)stream),

@@ -239,6 +239,7 @@ enum { kKK = 0, kKM = 1, kMM = 2 };                // A, B k-contiguous (K) or k
 // How a product is cut: `whole` tiles over the full contraction, then
 // `tail` tiles in `splits` parts each, joined by a second launch.
 struct Plan {
+    bool fits;         // false: more threads than a launch takes with every tile
     int tile;          // 0: 256 x 256, 1: 128 x 128, 2: 64 x 64
     int tm, tn;        // tiles down and across
     int64_t whole, tail;
@@ -264,6 +265,8 @@ struct Shape {         // a layer: n rows, k inputs, m outputs
     bool aligned16;    // every matrix starts on 16 bytes
 };
 size_t layer_ws(const Shape &s, bool gated, bool backward);
+// Whether every launch of a call stays below a grid's 2^32 threads.
+bool layer_fits(const Shape &s, bool gated, bool backward);
 hipError_t run_layer(const Shape &s, bool gated, const void *X, const void *W,
                      const void *bias, const void *res, void *Y, void *Z, void *ws,
                      hipStream_t st);

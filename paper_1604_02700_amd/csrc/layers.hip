@@ -762,10 +762,13 @@ struct Forward {
 };
 
 // Rows of a workgroup of grad_kernel: 64, fewer where that would leave the
-// card half empty (1,003 rows of 700: 48 workgroups of 16 turns, 25 us).
+// card half empty (1,003 rows of 700: 48 workgroups of 16 turns, 25 us), more
+// from 2^29 rows on, where the grid would come to 2^31 threads.
 int grad_rows(int64_t n, int64_t m)
 {
     int rows = kSumRows;
+    while ((n + rows - 1) / rows > (1 << 23))
+        rows *= 2;
     while (rows > 8 && (n + rows - 1) / rows * ((m + 255) / 256) < 1024)
         rows /= 2;
     return rows;
@@ -920,6 +923,18 @@ size_t layer_ws(const Shape &s, bool gated, bool backward)
     else
         Forward f(s, gated, nullptr, nullptr, c);
     return c.at;
+}
+
+bool layer_fits(const Shape &s, bool gated, bool backward)
+{
+    if (s.n == 0 || (backward ? small_gradients(s, gated) : as_rows(s, gated)))
+        return true;
+    const int64_t rows = gated ? 2 * s.m : s.m;
+    const int op = kind_of(s.dtype);
+    if (!backward)
+        return product_plan(s.n, rows, s.k, 1, op, gated ? kEpiGated : kEpiLayer).fits;
+    return product_plan(s.n, s.k, rows, 1, op, kEpiLayer).fits &&
+           product_plan(rows, s.k, s.n, 1, op, kEpiLayer).fits;
 }
 
 hipError_t run_layer(const Shape &s, bool gated, const void *X, const void *W, const void *bias,

@@ -45,7 +45,8 @@ Plan product_plan(int64_t M, int64_t N, int64_t K, int64_t batch, int op, int ep
 {
     Plan best{};
     best.splits = 1;
-    if (M <= 0 || N <= 0 || batch <= 0)
+    best.fits = M <= 0 || N <= 0 || batch <= 0;
+    if (best.fits)
         return best;
     const bool sym = symmetric(epi), split = op == kOpSplit;
     const int64_t step = split ? 32 : 64, steps = (K + step - 1) / step;
@@ -57,6 +58,9 @@ Plan product_plan(int64_t M, int64_t N, int64_t K, int64_t batch, int op, int ep
         const int64_t tiles = (sym ? tn * (tn + 1) / 2 : tm * tn) * batch;
         auto consider = [&](int64_t whole, int parts) {
             const int64_t tail = tiles - whole;
+            // a grid of 2^32 threads or more is refused (2^30 rows of a narrow matrix)
+            if ((whole + tail * parts) * (c.edge == 256 ? 512 : 256) >= (int64_t)1 << 32)
+                return;
             double time = time_of(c, split, whole, (double)steps);
             size_t bytes = 0;
             if (tail) {
@@ -67,7 +71,7 @@ Plan product_plan(int64_t M, int64_t N, int64_t K, int64_t batch, int op, int ep
             if (least != 0.0 && time >= least)
                 return;
             least = time;
-            best = Plan{t, (int)tm, (int)tn, whole, tail, tail ? parts : 1, bytes};
+            best = Plan{true, t, (int)tm, (int)tn, whole, tail, tail ? parts : 1, bytes};
         };
         consider(tiles, 1);
         const int64_t slots = (int64_t)kUnits * c.resident, round = tiles / slots * slots;
@@ -85,10 +89,10 @@ Plan product_plan(int64_t M, int64_t N, int64_t K, int64_t batch, int op, int ep
 hipError_t launch_product(int modes, int op, int epi, const ProductArgs &a, hipStream_t s)
 {
     const Plan p = product_plan(a.M, epi == kEpiGated ? 2 * a.e.half : a.N, a.K, a.batch, op, epi);
+    if (!p.fits)
+        return hipErrorInvalidValue;
     if (p.whole + p.tail == 0)
         return hipSuccess;
-    if (p.whole + p.tail * p.splits > 0x7fffffffll)
-        return hipErrorInvalidValue;
     if (modes == kKK)
         return launch_product_kk(op, epi, p, a, s);
     if (modes == kKM)

@@ -186,3 +186,26 @@ def test_polynomials_that_leave_the_halves_are_refused(g, steps, a, b, c, ok):
     assert L.gpic_orthogonalize(p, d, d, None, 0, None) == (2 if ok else 1)
     assert L.gpic_muon_step(p, h, d, d, d, None, 0, None) == (2 if ok else 1)
     assert ok or b"singular values" in L.gpic_last_error()
+
+
+def test_rows_up_to_the_limit_of_a_launch(g):
+    """A launch has fewer than 2^32 threads: narrow layers of 2^30 rows and
+    more take larger tiles, and the last 127 row counts are refused before
+    anything runs."""
+    L, d = g.lib(), C.c_void_p(4096)            # never dereferenced: no workspace is given
+    for dt in range(3):
+        for n, ok in ((2 ** 30, True), (2 ** 31 - 128, True), (2 ** 31 - 127, False),
+                      (2 ** 31 - 1, False)):
+            p = _layer(g, n=n, k=80, m=8, ldx=80, ldw=80, ldy=8, ldr=8, ldz=16, dtype=dt,
+                       aligned16=0)
+            ref = C.byref(p)
+            for op in range(4):
+                assert (L.gpic_layer_workspace_bytes(op, ref) > 0) == ok
+            want = 2 if ok else 5
+            assert L.gpic_linear(ref, d, d, None, None, d, d, None, 0, None) == want
+            assert L.gpic_linear_backward(ref, d, d, d, d, d, d, d, None, 0, None) == want
+            assert L.gpic_gated(ref, d, d, d, d, None, 0, None) == want
+            assert L.gpic_gated_backward(ref, d, d, d, d, d, d, None, 0, None) == want
+    # rows that are read as they lie have no such limit
+    p = _layer(g, n=2 ** 31 - 1)
+    assert L.gpic_layer_workspace_bytes(0, C.byref(p)) == 0

@@ -449,3 +449,26 @@ def test_float16_gradients_beside_a_huge_z(g, size):
     z[17] = size
     got = g.gpic_gated_backward(dH, X, W, z)
     assert torch.equal(got.dX, want.dX) and torch.equal(got.dW, want.dW)
+
+
+def test_more_than_2_30_rows(g):
+    """The gradients of a narrow layer at 2^30 + 77 rows, more than a launch
+    of 64 rows a workgroup would take: zero but for rows at the ends of tiles
+    and of powers of two, so that every sum is short."""
+    n, k, m = 2 ** 30 + 77, 8, 8
+    _tiled(g, "linear_backward", n, k, m, "bf16")
+    print(f"linear backward n={n} k={k} m={m}", flush=True)
+    X = torch.zeros((n, k), dtype=torch.bfloat16, device=DEV)
+    dY = torch.zeros((n, m), dtype=torch.bfloat16, device=DEV)
+    rows = sorted({0, 1, 63, 64, 255, 256, n - 1, n - 2, 2 ** 30, 2 ** 30 - 1, 2 ** 29, 2 ** 29 - 1,
+                   2 ** 28 + 3, 3 * 2 ** 28 + 129})
+    X[rows], dY[rows] = _randn((len(rows), k), "bf16", 1), _randn((len(rows), m), "bf16", 2)
+    W = _randn((m, k), "bf16", 3)
+    gr = g.gpic_linear_backward(dY, X, W)
+    x, d, w = X[rows].double(), dY[rows].double(), W.double()
+    _close(gr.dX[rows], d @ w, _product_error(d, w.t(), "bf16"), "bf16", "dX")
+    _close(gr.dW, d.t() @ x, _product_error(d.t(), x.t(), "bf16"), "bf16", "dW")
+    _close(gr.db, d.sum(0), 70 * E * d.abs().sum(0), "bf16", "db")
+    gr.dX[rows] = 0
+    for part in gr.dX.split(2 ** 27):           # no other row has a gradient
+        assert not bool(part.any())
