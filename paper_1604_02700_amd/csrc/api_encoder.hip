@@ -186,7 +186,11 @@ size_t gpic_layer_workspace_bytes(int32_t op, const gpic_layer_params *p)
         return 0;
     const bool gated = op >= GPIC_GATED_FORWARD;
     const bool backward = op == GPIC_LAYER_BACKWARD || op == GPIC_GATED_BACKWARD;
-    if (check_layer(p, gated) != GPIC_OK || check_fits(p, gated, backward) != GPIC_OK)
+    if (check_layer(p, gated) != GPIC_OK)
+        return 0;
+    if (backward && (gated || p->activation != GPIC_ACT_NONE) && check_pre(p, gated) != GPIC_OK)
+        return 0;
+    if (check_fits(p, gated, backward) != GPIC_OK)
         return 0;
     return layer_ws(shape_of(p), gated, backward);
 }

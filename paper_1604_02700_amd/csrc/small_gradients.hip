@@ -241,7 +241,8 @@ int64_t rows_of(const Shape &s, bool gated) { return gated ? 2 * s.m : s.m; }
 bool small_gradients(const Shape &s, bool gated)
 {
     const int64_t rows = rows_of(s, gated), far = (int64_t)1 << 28;
-    if (s.n * s.ldy > far || s.n * s.ldx > far || s.n * s.ldz > far || rows * s.ldw > far)
+    const int64_t ldz = gated || s.act != GPIC_ACT_NONE ? s.ldz : 0;     // else Z is not read
+    if (s.n * s.ldy > far || s.n * s.ldx > far || s.n * ldz > far || rows * s.ldw > far)
         return false;
     if (s.n > 2048 || rows > 2048)
         return false;

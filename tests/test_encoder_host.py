@@ -209,3 +209,22 @@ def test_rows_up_to_the_limit_of_a_launch(g):
     # rows that are read as they lie have no such limit
     p = _layer(g, n=2 ** 31 - 1)
     assert L.gpic_layer_workspace_bytes(0, C.byref(p)) == 0
+
+
+@pytest.mark.parametrize("ldz", [0, -7, 2 ** 40, 2 ** 62, -2 ** 63])
+def test_a_pitch_that_is_not_used_changes_nothing(g, ldz):
+    """ldz without a Z that is read: no part in the choice of a kernel."""
+    L, d = g.lib(), C.c_void_p(4096)
+    for n in (50, 5000):
+        for dt in range(3):
+            p = _layer(g, n=n, activation=0, dtype=dt, aligned16=0, ldz=ldz)
+            q = _layer(g, n=n, activation=0, dtype=dt, aligned16=0)
+            for op in (0, 1):
+                assert L.gpic_layer_workspace_bytes(op, C.byref(p)) \
+                    == L.gpic_layer_workspace_bytes(op, C.byref(q))
+            # where Z is read the call refuses it, and there is no workspace for it
+            p = _layer(g, n=n, dtype=dt, aligned16=0, ldz=ldz)
+            assert L.gpic_layer_workspace_bytes(1, C.byref(p)) == 0
+            assert L.gpic_layer_workspace_bytes(3, C.byref(p)) == 0
+            assert L.gpic_linear_backward(C.byref(p), d, d, d, d, d, d, d, None, 0, None) == 1
+            assert L.gpic_gated_backward(C.byref(p), d, d, d, d, d, d, None, 0, None) == 1
