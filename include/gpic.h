@@ -469,7 +469,8 @@ enum { GPIC_ACT_NONE = 0, GPIC_ACT_RELU = 1, GPIC_ACT_GELU = 2, GPIC_ACT_SILU = 
 
 typedef struct gpic_layer_params {
     int64_t n, k, m;     /* rows (0 .. 2^31 - 1), inputs, outputs (1 .. 2^20 each;
-                            gated: 2 m <= 2^20)                                   */
+                            gated: 2 m <= 2^20, and UNSUPPORTED where m + 256 rows
+                            of W in 16 bits come to 4 GiB)                        */
     int64_t ldx, ldw;    /* pitches of X [n x k] and W [m x k] (gated [2 m x k])  */
     int64_t ldy;         /* of Y, H [n x m] (backward: of dY, dH)                 */
     int64_t ldr;         /* of the residual [n x m] (ignored without one)         */

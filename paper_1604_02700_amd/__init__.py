@@ -51,6 +51,7 @@ EXPORTS = (
 )
 DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
+MAX_PITCH = 1 << 22        # of a layer's matrices (include/gpic.h)
 LAYER_OP = {"linear": 0, "linear_backward": 1, "gated": 2, "gated_backward": 3}
 
 # the static scratch of gpic_power_iterate_dense_noalloc (include/gpic.h)
@@ -653,7 +654,8 @@ class LayerGrads:
 
 def _matrix(t, rows, cols, like, name):
     """t as a [rows, cols] tensor of like's type and device with unit column
-    stride (copied only when its columns are strided or its rows overlap)."""
+    stride (copied only when its columns are strided, its rows overlap or lie
+    further apart than the C calls' pitches reach)."""
     _dev(t, like.dtype, name)
     return _matrix_of(t, rows, cols, like, name)
 
@@ -666,7 +668,7 @@ def _matrix_of(t, rows, cols, like, name):
     if t.is_contiguous():
         return t
     sr, sc = t.stride()
-    if (cols > 1 and sc != 1) or (rows > 1 and sr < cols):
+    if (cols > 1 and sc != 1) or (rows > 1 and not cols <= sr <= MAX_PITCH):
         return t.contiguous()
     return t
 
@@ -716,7 +718,8 @@ def _output(t, rows, cols, X, name):
     if t is None:
         return torch.empty((rows, cols), dtype=X.dtype, device=X.device)
     if _matrix(t, rows, cols, X, name) is not t:
-        raise ValueError(f"{name} must have unit column stride and rows that do not overlap")
+        raise ValueError(f"{name} must have unit column stride and rows that do not overlap, "
+                         f"at most {MAX_PITCH} values apart")
     return t
 
 

@@ -472,3 +472,20 @@ def test_more_than_2_30_rows(g):
     gr.dX[rows] = 0
     for part in gr.dX.split(2 ** 27):           # no other row has a gradient
         assert not bool(part.any())
+
+
+@pytest.mark.parametrize("n", [7, N])
+def test_rows_far_apart_are_copied(g, n):
+    """Rows further apart than a pitch may be (2^22 values): the binding
+    copies them, and refuses results that would lie so."""
+    pitch, k, m = 2 ** 22 + 8, 100, 20
+    far = torch.zeros((n - 1) * pitch + k, dtype=torch.bfloat16, device=DEV).as_strided(
+        (n, k), (pitch, 1))
+    X, W = _randn((n, k), "bf16", 1), _randn((m, k), "bf16", 2)
+    far.copy_(X)
+    assert torch.equal(g.gpic_linear(far, W), g.gpic_linear(X, W))
+    dY = _randn((n, m), "bf16", 3)
+    got, want = g.gpic_linear_backward(dY, far, W), g.gpic_linear_backward(dY, X, W)
+    assert torch.equal(got.dX, want.dX) and torch.equal(got.dW, want.dW)
+    with pytest.raises(ValueError, match="apart"):
+        g.gpic_linear(X, W, Y=far[:, :m])
