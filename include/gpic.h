@@ -456,7 +456,9 @@ gpic_status gpic_read_stream(const float *x, int64_t n, double *sink, void *stre
  * 2,048 and n k m (gated: twice that) up to 2^28 in float32, and in 16 bits up
  * to 2^26 with n and m (gated: 2 m) up to 1,024, else 2^22.  A NaN or an infinity in a row of X (a column's
  * weights) makes that row (column) of the result non-finite and no other.
- * Results are bitwise reproducible.  A product of more workgroups than a
+ * Results are bitwise reproducible.  Results that overlap what a call reads,
+ * or each other, are refused (INVALID_ARG) but where stated; columns of one
+ * table may be read and written side by side.  A product of more workgroups than a
  * launch takes (more than 2^31 - 128 rows, beyond small calls) is UNSUPPORTED.
  * Asynchronous. */
 
@@ -497,7 +499,7 @@ size_t gpic_layer_workspace_bytes(int32_t op, const gpic_layer_params *p);
 
 /* Y = act(X W^T + bias) + residual.  bias [m], residual and Z nullable; Z
  * receives X W^T + bias, which the gradient needs.  Y may be the residual's
- * own buffer (same pitch); no other overlap.  n = 0 does nothing.
+ * own buffer (same pitch).  n = 0 does nothing.
  * ws: gpic_layer_workspace_bytes(GPIC_LAYER_FORWARD, p).  Errors:
  * INVALID_ARG, WORKSPACE, UNSUPPORTED. */
 gpic_status gpic_linear(const gpic_layer_params *p, const void *X, const void *W,
@@ -558,7 +560,7 @@ size_t gpic_polar_workspace_bytes(const gpic_polar_params *p);
 /* O = the Newton-Schulz iterate of each matrix: X_0 = G / (|G|_F + eps),
  * then `steps` times X <- a X + (b A + c A^2) X with A = X X^T (X^T X on the
  * right for m > n): the singular vectors of G with its singular values
- * taken near 1.  O may be G.  A zero matrix gives zeros (with eps > 0).
+ * taken near 1.  O may be G itself.  A zero matrix gives zeros (with eps > 0).
  * float32 and float16 matrices, and bfloat16 ones whose smaller side is up to
  * 64, in split halves; other bfloat16 matrices with half-precision products,
  * to about 2e-3 of |O|.

@@ -68,6 +68,60 @@ gpic_status check_pre(const gpic_layer_params *p, bool gated)
     return GPIC_OK;
 }
 
+// A matrix in memory: `rows` runs of `width` bytes, `pitch` bytes apart.
+struct Extent {
+    const char *name;
+    const void *p;
+    int64_t rows, width, pitch;
+};
+
+Extent matrix(const char *name, const void *p, int64_t rows, int64_t cols, int64_t ld, size_t size)
+{
+    return Extent{name, p, rows, cols * (int64_t)size, ld * (int64_t)size};
+}
+
+Extent packed(const char *name, const void *p, int64_t values, size_t size)
+{
+    return matrix(name, p, 1, values, values, size);
+}
+
+// Whether two matrices share a byte.  Columns of one table do not.
+bool overlap(Extent a, Extent b)
+{
+    if (!a.p || !b.p || a.rows <= 0 || b.rows <= 0 || a.width <= 0 || b.width <= 0)
+        return false;
+    const int64_t at = (int64_t)(uintptr_t)a.p, bt = (int64_t)(uintptr_t)b.p;
+    if (at + (a.rows - 1) * a.pitch + a.width <= bt || bt + (b.rows - 1) * b.pitch + b.width <= at)
+        return false;
+    if (a.rows > 1 && b.rows > 1 && a.pitch == b.pitch) {
+        int64_t d = (bt - at) % a.pitch;
+        d = d < 0 ? d + a.pitch : d;
+        return d < a.width || d + b.width > a.pitch;
+    }
+    if (a.rows > b.rows)
+        return overlap(b, a);
+    for (int64_t i = 0; i < a.rows; ++i) {
+        // the first row of b that ends beyond this row's start
+        const int64_t s = at + i * a.pitch, before = s - bt - b.width;
+        const int64_t j = before < 0 ? 0 : (b.rows > 1 ? before / b.pitch + 1 : 1);
+        if (j < b.rows && bt + j * b.pitch < s + a.width)
+            return true;
+    }
+    return false;
+}
+
+// Results lie apart from what a call reads and from each other.
+gpic_status check_apart(const Extent *out, int outs, const Extent *in, int ins)
+{
+    for (int i = 0; i < outs; ++i) {
+        for (int j = 0; j < ins; ++j)
+            CHECK_ARG(!overlap(out[i], in[j]), "%s overlaps %s", out[i].name, in[j].name);
+        for (int j = 0; j < i; ++j)
+            CHECK_ARG(!overlap(out[i], out[j]), "%s overlaps %s", out[i].name, out[j].name);
+    }
+    return GPIC_OK;
+}
+
 Shape shape_of(const gpic_layer_params *p)
 {
     Shape s;
@@ -213,6 +267,18 @@ gpic_status gpic_linear(const gpic_layer_params *p, const void *X, const void *W
         CHECK(check_pre(p, false));
     CHECK(check_fits(p, false, false));
     CHECK(check_ws(ws, ws_bytes, layer_ws(shape_of(p), false, false)));
+    {
+        const size_t e = size_of(p->dtype);
+        // Y may be the residual itself
+        const bool in_place = residual == Y && (p->ldr == p->ldy || p->n == 1);
+        const Extent out[] = {matrix("Y", Y, p->n, p->m, p->ldy, e),
+                              matrix("Z", Z, p->n, p->m, p->ldz, e)};
+        const Extent in[] = {matrix("X", X, p->n, p->k, p->ldx, e),
+                             matrix("W", W, p->m, p->k, p->ldw, e), packed("bias", bias, p->m, e),
+                             matrix("the residual", in_place ? nullptr : residual, p->n, p->m,
+                                    p->ldr, e)};
+        CHECK(check_apart(out, 2, in, 4));
+    }
     CHECK_HIP(run_layer(shape_of(p), false, X, W, bias, residual, Y, Z, ws,
                         (hipStream_t)stream),
               "linear");
@@ -237,6 +303,16 @@ gpic_status gpic_linear_backward(const gpic_layer_params *p, const void *dY, con
         CHECK(check_pre(p, false));
     CHECK(check_fits(p, false, true));
     CHECK(check_ws(ws, ws_bytes, layer_ws(shape_of(p), false, true)));
+    {
+        const size_t e = size_of(p->dtype);
+        const Extent out[] = {packed("dX", dX, p->n * p->k, e), packed("dW", dW, p->m * p->k, e),
+                              packed("db", db, p->m, e)};
+        const Extent in[] = {matrix("dY", dY, p->n, p->m, p->ldy, e),
+                             matrix("X", dW ? X : nullptr, p->n, p->k, p->ldx, e),
+                             matrix("W", dX ? W : nullptr, p->m, p->k, p->ldw, e),
+                             matrix("Z", act ? Z : nullptr, p->n, p->m, p->ldz, e)};
+        CHECK(check_apart(out, 3, in, 4));
+    }
     CHECK_HIP(run_layer_backward(shape_of(p), false, dY, X, W, Z, dX, dW, db, ws,
                                  (hipStream_t)stream),
               "linear backward");
@@ -256,6 +332,14 @@ gpic_status gpic_gated(const gpic_layer_params *p, const void *X, const void *W,
         CHECK(check_pre(p, true));
     CHECK(check_fits(p, true, false));
     CHECK(check_ws(ws, ws_bytes, layer_ws(shape_of(p), true, false)));
+    {
+        const size_t e = size_of(p->dtype);
+        const Extent out[] = {matrix("H", H, p->n, p->m, p->ldy, e),
+                              matrix("Z", Z, p->n, 2 * p->m, p->ldz, 4)};
+        const Extent in[] = {matrix("X", X, p->n, p->k, p->ldx, e),
+                             matrix("W", W, 2 * p->m, p->k, p->ldw, e)};
+        CHECK(check_apart(out, 2, in, 2));
+    }
     CHECK_HIP(run_layer(shape_of(p), true, X, W, nullptr, nullptr, H, Z, ws,
                         (hipStream_t)stream),
               "gated");
@@ -277,6 +361,16 @@ gpic_status gpic_gated_backward(const gpic_layer_params *p, const void *dH, cons
     CHECK(check_pre(p, true));
     CHECK(check_fits(p, true, true));
     CHECK(check_ws(ws, ws_bytes, layer_ws(shape_of(p), true, true)));
+    {
+        const size_t e = size_of(p->dtype);
+        const Extent out[] = {packed("dX", dX, p->n * p->k, e),
+                              packed("dW", dW, 2 * p->m * p->k, e)};
+        const Extent in[] = {matrix("dH", dH, p->n, p->m, p->ldy, e),
+                             matrix("X", dW ? X : nullptr, p->n, p->k, p->ldx, e),
+                             matrix("W", dX ? W : nullptr, 2 * p->m, p->k, p->ldw, e),
+                             matrix("Z", Z, p->n, 2 * p->m, p->ldz, 4)};
+        CHECK(check_apart(out, 2, in, 4));
+    }
     CHECK_HIP(run_layer_backward(shape_of(p), true, dH, X, W, Z, dX, dW, nullptr, ws,
                                  (hipStream_t)stream),
               "gated backward");
@@ -296,6 +390,12 @@ gpic_status gpic_orthogonalize(const gpic_polar_params *p, const void *G, void *
     CHECK(check_matrix(G, "G", p->dtype, empty));
     CHECK(check_matrix(O, "O", p->dtype, empty));
     CHECK(check_ws(ws, ws_bytes, polar_ws(polar_of(p))));
+    {
+        const int64_t values = p->batch * p->m * p->n;
+        const Extent out = packed("O", O, values, size_of(p->dtype));
+        const Extent in = packed("G", O == G ? nullptr : G, values, size_of(p->dtype));
+        CHECK(check_apart(&out, 1, &in, 1));
+    }
     CHECK_HIP(run_orthogonalize(polar_of(p), G, O, ws, (hipStream_t)stream), "orthogonalize");
     return GPIC_OK;
 }
@@ -315,6 +415,13 @@ gpic_status gpic_muon_step(const gpic_polar_params *p, const gpic_muon_params *h
     CHECK(check_matrix(G, "G", p->dtype, empty));
     CHECK(check_matrix(M, "M", GPIC_F32, empty));
     CHECK(check_ws(ws, ws_bytes, polar_ws(polar_of(p))));
+    {
+        const int64_t values = p->batch * p->m * p->n;
+        const Extent out[] = {packed("W", W, values, size_of(p->dtype)), packed("M", M, values, 4)};
+        // (G is read before W is written)
+        const Extent in = packed("G", G == W ? nullptr : G, values, size_of(p->dtype));
+        CHECK(check_apart(out, 2, &in, 1));
+    }
     MuonStep m;
     m.lr = h->lr;
     m.momentum = h->momentum;

@@ -228,3 +228,57 @@ def test_a_pitch_that_is_not_used_changes_nothing(g, ldz):
             assert L.gpic_layer_workspace_bytes(3, C.byref(p)) == 0
             assert L.gpic_linear_backward(C.byref(p), d, d, d, d, d, d, d, None, 0, None) == 1
             assert L.gpic_gated_backward(C.byref(p), d, d, d, d, d, d, None, 0, None) == 1
+
+
+def _at(address):
+    return C.c_void_p(address)                  # never dereferenced
+
+
+def test_results_over_operands_are_refused(g):
+    """Shared bytes are refused before any launch (what shares none is called
+    with memory of its own in the tests on the GPU)."""
+    L = g.lib()
+    base, far = 1 << 30, 1 << 34
+
+    def linear(Y, X=base, W=far, R=None, Z=None, ldx=16, ldy=24, ldr=24, n=10):
+        p = _layer(g, n=n, ldx=ldx, ldy=ldy, ldr=ldr, ldz=24, aligned16=0)
+        st = L.gpic_linear(C.byref(p), _at(X), _at(W), None, R and _at(R), _at(Y), Z and _at(Z),
+                           None, 0, None)
+        return st, L.gpic_last_error()
+
+    for Y in (base, base + 2, base + 10 * 32 - 2, base - 10 * 48 + 2):
+        assert linear(Y) == (1, b"Y overlaps X")
+    assert linear(far + 24 * 32 - 2) == (1, b"Y overlaps W")
+    assert linear(2 * far, R=2 * far + 2)[1] == b"Y overlaps the residual"
+    assert linear(2 * far, R=2 * far, ldr=26)[1] == b"Y overlaps the residual"
+    assert linear(2 * far, Z=2 * far + 100)[1] == b"Z overlaps Y"
+    # one table of 48 columns, X in 0 .. 15: Y a column early, Y past its row's end
+    assert linear(base + 30, ldx=48, ldy=48) == (1, b"Y overlaps X")
+    assert linear(base + 2 * (48 * 4 + 25), ldx=48, ldy=48) == (1, b"Y overlaps X")
+    # pitches that differ: rows of Y in the gaps of a table of X but the last
+    assert linear(base + 2 * 16, ldx=100, ldy=199, n=10) == (1, b"Y overlaps X")
+    assert linear(base + 2 * 90, ldx=100, n=2, ldy=24) == (1, b"Y overlaps X")
+
+
+def test_gradients_and_steps_over_operands_are_refused(g):
+    L, f = g.lib(), 1 << 34
+    p = C.byref(_layer(g, n=10, aligned16=0, ldz=48))
+    a = [_at(f * i) for i in range(1, 9)]
+    for bad in (dict(dX=a[0]), dict(dX=a[1]), dict(dX=a[2]), dict(dX=a[3]), dict(dW=a[4]),
+                dict(db=a[5]), dict(dW=a[0])):
+        o = {**dict(dX=a[4], dW=a[5], db=a[6]), **bad}
+        assert L.gpic_linear_backward(p, a[0], a[1], a[2], a[3], o["dX"], o["dW"], o["db"], None, 0,
+                                      None) == 1
+        assert b"overlaps" in L.gpic_last_error()
+        if "db" not in bad:
+            assert L.gpic_gated_backward(p, a[0], a[1], a[2], a[3], o["dX"], o["dW"], None, 0,
+                                         None) == 1
+    for H, Z in ((a[0], a[2]), (a[1], a[2]), (a[2], a[2]), (a[2], a[0])):
+        assert L.gpic_gated(p, a[0], a[1], H, Z, None, 0, None) == 1
+    q = C.byref(_polar(g))
+    h = C.byref(g.MuonParams(lr=0.1, momentum=0.9, weight_decay=0.0, scale=1.0, nesterov=1,
+                             reserved=0))
+    assert L.gpic_orthogonalize(q, a[0], _at(f + 4), None, 0, None) == 1
+    for W, G, M in ((a[0], a[1], a[1]), (a[0], a[1], a[0]),
+                    (a[0], _at(f + 64), a[1])):
+        assert L.gpic_muon_step(q, h, W, G, M, None, 0, None) == 1

@@ -489,3 +489,48 @@ def test_rows_far_apart_are_copied(g, n):
     assert torch.equal(got.dX, want.dX) and torch.equal(got.dW, want.dW)
     with pytest.raises(ValueError, match="apart"):
         g.gpic_linear(X, W, Y=far[:, :m])
+
+
+@pytest.mark.parametrize("n", [10, N])
+def test_results_beside_their_operands(g, n):
+    """X, the residual and Y as columns of one table, and of tables of two
+    pitches in one buffer: no byte is shared, so the calls run.  Where bytes
+    are shared, and the call would race, it is refused."""
+    k, m = 100, 60
+    X, W, R = _randn((n, k), "f32", 1), _randn((m, k), "f32", 2, 0.1), _randn((n, m), "f32", 3)
+    Y, H = g.gpic_linear(X, W, None, "silu", R), g.gpic_gated(X, W)
+    table = torch.full((n, k + 2 * m + 3), float("nan"), device=DEV)
+    x, r, y = table[:, :k], table[:, k:k + m], table[:, k + m + 2:k + 2 * m + 2]
+    x.copy_(X), r.copy_(R)
+    assert torch.equal(g.gpic_linear(x, W, None, "silu", r, Y=y), Y) and torch.equal(x, X)
+    assert bool(table[:, k + m:k + m + 2].isnan().all() & table[:, k + 2 * m + 2].isnan().all())
+    assert torch.equal(g.gpic_linear(x, W, None, "silu", r, Y=r), Y)          # in place
+    assert torch.equal(g.gpic_gated(x, W, H=y[:, :m // 2]), H) and torch.equal(x, X)
+    # rows of Y in the gaps of every second row of X's table
+    buf = torch.full((2 * n, 400), float("nan"), device=DEV)
+    x, y = buf.view(-1).as_strided((n, k), (400, 1)), buf.view(-1).as_strided((n, m), (800, 1), 200)
+    x.copy_(X)
+    assert torch.equal(g.gpic_linear(x, W, Y=y), g.gpic_linear(X, W)) and torch.equal(x, X)
+    V = _randn((k, k), "f32", 4)
+    table = torch.zeros((n, k + m), device=DEV)
+    table[:, :k] = X
+    for call in (lambda: g.gpic_linear(X, V, Y=X), lambda: g.gpic_linear(X, V, Y=V[:n]) if n <= k else
+                 g.gpic_linear(X, V, Y=X), lambda: g.gpic_linear(table[:, :k], W, Y=table[:, k - 1:-1]),
+                 lambda: g.gpic_linear(X, W, None, "none", table[:, k:], Y=table[:, k - 1:-1]),
+                 lambda: g.gpic_gated(X, V, H=X[:, :k // 2])):
+        with pytest.raises(g.GpicError, match="overlaps"):
+            call()
+    G = _randn((65, 300), "f32", 5)
+    O = g.gpic_orthogonalize(G)
+    big = torch.zeros(65 * 300 + 4, device=DEV)
+    big[:65 * 300] = G.view(-1)
+    with pytest.raises(g.GpicError, match="overlaps"):
+        g.gpic_orthogonalize(big[:-4].view(65, 300), O=big[4:].view(65, 300))
+    assert torch.equal(g.gpic_orthogonalize(G, O=G), O)
+    w, M = _randn((65, 300), "f32", 6), torch.zeros((65, 300), device=DEV)
+    w2, M2 = w.clone(), M.clone()
+    g.gpic_muon_step(w, w.clone(), M, 0.1)
+    g.gpic_muon_step(w2, w2, M2, 0.1)           # G is read before W is written
+    assert torch.equal(w, w2) and torch.equal(M, M2)
+    with pytest.raises(g.GpicError, match="overlaps"):
+        g.gpic_muon_step(w, M, M, 0.1)
