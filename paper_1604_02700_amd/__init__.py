@@ -652,6 +652,25 @@ class LayerGrads:
     db: Optional[torch.Tensor] = None
 
 
+def _no_graph(names, *tensors):
+    """The calls record nothing for autograd: a tensor that would expect it is
+    refused rather than its graph cut."""
+    if not torch.is_grad_enabled():
+        return
+    for i, t in enumerate(tensors):
+        if getattr(t, "requires_grad", False):
+            name = names.split()[i]
+            raise ValueError(f"{name} requires gradients, and this call records none: use the "
+                             f"package's gradients, under torch.no_grad() or on {name}.detach()")
+
+
+def _written(*tensors):
+    """Tells autograd that these were written in place."""
+    for t in tensors:
+        if not t.is_inference():
+            torch.autograd.graph.increment_version(t)
+
+
 def _matrix(t, rows, cols, like, name):
     """t as a [rows, cols] tensor of like's type and device with unit column
     stride (copied only when its columns are strided, its rows overlap or lie
@@ -736,7 +755,8 @@ def gpic_linear(X: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] =
     gpic_linear_backward reads.  Y (optional) may be the residual itself.
     float32 beyond small calls: 22 significant bits of each entry of X (W)
     down to 2^-17 of the largest finite one of its row, errors of 2^-39 of that
-    largest below."""
+    largest below.  Records nothing for autograd (as every call of this
+    section): operands that require gradients are refused outside no_grad()."""
     X = _layer_type(X)
     W = _weights(X, W, False)
     n, m = X.shape[0], W.shape[0]
@@ -748,11 +768,17 @@ def gpic_linear(X: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] =
         bias = bias.contiguous()
     if residual is not None:
         residual = _matrix(residual, n, m, X, "residual")
-    Y = _output(Y, n, m, X, "Y")
+    given, Y = Y, _output(Y, n, m, X, "Y")
     Z = torch.empty((n, m), dtype=X.dtype, device=X.device) if want_pre else None
+    if (X.requires_grad or W.requires_grad or (bias is not None and bias.requires_grad)
+            or (residual is not None and residual.requires_grad)
+            or Y.requires_grad):
+        _no_graph("X W bias residual Y", X, W, bias, residual, Y)
     ref, xp, wp, yp, ws, nb = _layer("linear", X, W, Y, Z, residual, act, m)
     _check(lib().gpic_linear(ref, xp, wp, _at(bias), _at(residual), yp, _at(Z), _at(ws), nb,
                              _stream(X.device)))
+    if given is not None:
+        _written(given)
     return (Y, Z) if want_pre else Y
 
 
@@ -777,6 +803,9 @@ def gpic_linear_backward(dY: torch.Tensor, X: torch.Tensor, W: torch.Tensor,
     dX = torch.empty((n, k), dtype=X.dtype, device=dev) if want_x else None
     dW = torch.empty((m, k), dtype=X.dtype, device=dev) if want_w else None
     db = torch.empty(m, dtype=X.dtype, device=dev) if want_bias else None
+    if (dY.requires_grad or X.requires_grad or W.requires_grad
+            or (Z is not None and Z.requires_grad)):
+        _no_graph("dY X W Z", dY, X, W, Z)
     ref, xp, wp, yp, ws, nb = _layer("linear_backward", X, W, dY, Z, None, act, m)
     _check(lib().gpic_linear_backward(ref, yp, xp, wp, _at(Z), _at(dX), _at(dW), _at(db), _at(ws),
                                       nb, _stream(dev)))
@@ -792,10 +821,14 @@ def gpic_gated(X: torch.Tensor, W: torch.Tensor, activation: str = "silu",
     W = _weights(X, W, True)
     n, m = X.shape[0], W.shape[0] // 2
     act = _activation(activation)
-    H = _output(H, n, m, X, "H")
+    given, H = H, _output(H, n, m, X, "H")
     Z = torch.empty((n, 2 * m), dtype=torch.float32, device=X.device) if want_pre else None
+    if X.requires_grad or W.requires_grad or H.requires_grad:
+        _no_graph("X W H", X, W, H)
     ref, xp, wp, hp, ws, nb = _layer("gated", X, W, H, Z, None, act, m)
     _check(lib().gpic_gated(ref, xp, wp, hp, _at(Z), _at(ws), nb, _stream(X.device)))
+    if given is not None:
+        _written(given)
     return (H, Z) if want_pre else H
 
 
@@ -812,6 +845,8 @@ def gpic_gated_backward(dH: torch.Tensor, X: torch.Tensor, W: torch.Tensor, Z: t
     Z = _matrix_of(Z, n, 2 * m, X, "Z")
     dX = torch.empty((n, k), dtype=X.dtype, device=dev) if want_x else None
     dW = torch.empty((2 * m, k), dtype=X.dtype, device=dev) if want_w else None
+    if dH.requires_grad or X.requires_grad or W.requires_grad or Z.requires_grad:
+        _no_graph("dH X W Z", dH, X, W, Z)
     ref, xp, wp, hp, ws, nb = _layer("gated_backward", X, W, dH, Z, None, act, m)
     _check(lib().gpic_gated_backward(ref, hp, xp, wp, _at(Z), _at(dX), _at(dW), _at(ws), nb,
                                      _stream(dev)))
@@ -858,9 +893,13 @@ def gpic_orthogonalize(G: torch.Tensor, steps: int = 5, coefficients=POLAR_COEFF
         if out.shape != G.shape or out.device != G.device or not out.is_contiguous():
             raise ValueError("O must be contiguous, of G's shape and on its device")
     G = G.contiguous()
+    if G.requires_grad or (O is not None and O.requires_grad):
+        _no_graph("G O", G, O)
     ref, ws, nb = _polar(G, steps, coefficients, eps)
     _check(lib().gpic_orthogonalize(ref, G.data_ptr(), out.data_ptr(), _at(ws), nb,
                                     _stream(G.device)))
+    if O is not None:
+        _written(O)
     return out
 
 
@@ -871,7 +910,8 @@ def gpic_muon_step(W: torch.Tensor, G: torch.Tensor, M: torch.Tensor, lr: float,
     """One optimiser step in place: M <- momentum M + G, U = G + momentum M
     (nesterov) or M, W <- (1 - lr weight_decay) W - lr scale O(U) with O as
     gpic_orthogonalize.  W and G of one type, M float32; [m, n] or stacks.
-    scale: by default sqrt(max(1, m / n))."""
+    scale: by default sqrt(max(1, m / n)).  Parameters that require gradients
+    are stepped under torch.no_grad()."""
     _stack(W, None, "W")
     _stack(G, W.dtype, "G")
     _stack(M, torch.float32, "M")
@@ -885,11 +925,14 @@ def gpic_muon_step(W: torch.Tensor, G: torch.Tensor, M: torch.Tensor, lr: float,
     m, n = W.shape[-2:]
     if scale is None:
         scale = max(1.0, m / max(n, 1)) ** 0.5
+    if W.requires_grad or G.requires_grad or M.requires_grad:
+        _no_graph("W G M", W, G, M)
     ref, ws, nb = _polar(W, steps, coefficients, eps)
     h = MuonParams(float(lr), float(momentum), float(weight_decay), float(scale),
                    int(bool(nesterov)), 0)
     _check(lib().gpic_muon_step(ref, C.byref(h), W.data_ptr(), G.data_ptr(), M.data_ptr(), _at(ws),
                                 nb, _stream(W.device)))
+    _written(W, M)
 
 
 # ----------------------------------------------- whole paths (call chains)
