@@ -291,6 +291,17 @@ hipError_t run_small_gradients(const Shape &s, bool gated, const void *dY, const
                                hipStream_t st);
 
 // ------------------------------------------------------ orthogonalize.hip
+// x times a positive factor whose float may overflow or vanish (1 / norm over
+// float32's range of matrices): as a mantissa in [1/2, 1) and a power of two
+struct Wide {
+    float mantissa;
+    int power;
+    __device__ __forceinline__ Wide(double factor)
+    {
+        mantissa = (float)frexp(factor, &power);
+    }
+    __device__ __forceinline__ float times(float x) const { return ldexpf(x, power) * mantissa; }
+};
 struct Polar {
     int64_t batch, m, n;
     int dtype, steps;

@@ -128,7 +128,7 @@ __global__ __launch_bounds__(256) void start_kernel(Input in, const double *part
     if ((threadIdx.x & 63) == 0)
         w[threadIdx.x >> 6] = t;
     __syncthreads();
-    const float inv = (float)((double)kStore / (sqrt(((w[0] + w[1]) + w[2]) + w[3]) + eps));
+    const Wide inv((double)kStore / (sqrt(((w[0] + w[1]) + w[2]) + w[3]) + eps));
     const int64_t z = blockIdx.y, z0 = z * in.m * in.n;
     const int64_t quads = up64(in.n) / 4, total = in.m * quads;
     const bool split = x0.lo == nullptr;
@@ -154,7 +154,9 @@ __global__ __launch_bounds__(256) void start_kernel(Input in, const double *part
                         u[j] = u_of(u[j], in.M[at + j], in);
                 }
         }
-        u *= inv;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            u[j] = inv.times(u[j]);
         const half4 h = __builtin_convertvector(u, half4);
         const half4 l = __builtin_convertvector(u - __builtin_convertvector(h, f32x4), half4);
         const int64_t o = z * x0.batch + r * x0.ld + (split ? split_at(c) : c);

@@ -138,20 +138,23 @@ __global__ __launch_bounds__(kThreads) void polar_small_kernel(SmallArgs a)
 #pragma unroll
     for (int w = 1; w < kWaves; ++w)
         t += norm[w];
-    const float inv = (float)((double)kStore / (sqrt(t) + a.eps));
+    const Wide inv((double)kStore / (sqrt(t) + a.eps));
 #pragma unroll
     for (int q = 0; q < kQuads; ++q) {
         const int i = (q * kThreads + (int)threadIdx.x) * 4;
         int i0 = i / a.n, i1 = i - i0 * a.n;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            u[q][j] = inv.times(u[q][j]);
         // four of one row, on their place
         const bool four = !tall && i + 4 <= size && (a.n & 3) == 0;
         if (four)
-            put_parts(xh + i0 * kLd + i1, xl + i0 * kLd + i1, u[q] * inv);
+            put_parts(xh + i0 * kLd + i1, xl + i0 * kLd + i1, u[q]);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             if (i + j < size && !four) {
                 const int at = tall ? i1 * kLd + i0 : i0 * kLd + i1;
-                const float v = u[q][j] * inv;
+                const float v = u[q][j];
                 const _Float16 h = (_Float16)v;
                 xh[at] = h;
                 xl[at] = (_Float16)(v - (float)h);

@@ -6,7 +6,7 @@ import pytest
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
 
-from test_gpu_encoder import DEV, T, U, _gradient, _polar, _rel  # noqa: E402
+from test_gpu_encoder import DEV, T, U, _gradient, _polar, _polar_tolerance, _rel  # noqa: E402
 
 
 @pytest.fixture(scope="module")
@@ -48,3 +48,20 @@ def test_a_refused_step_changes_nothing(g):
     with pytest.raises(g.GpicError, match="singular values"):
         g.gpic_muon_step(W, G, M, 0.1, coefficients=(1.9, 0.0, 0.0))
     assert torch.equal(W, w) and bool((M == 1).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(2, 60, 90), (2, 130, 520)], ids=str)
+def test_magnitudes_at_the_ends_of_the_type(g, shape, dtype):
+    """1 / |G|_F is no float32 below 2.9e-39 and above 3.4e38, and times 1,024
+    from 3.0e-36 on; the matrices are.  With eps = 0 only the direction counts."""
+    for s in (1e-39, 1e-37, 1e-35, 1e34, 1e37):
+        G = (_gradient(shape, 7) * s).to(T[dtype])
+        assert bool(torch.isfinite(G).all() & (G != 0).any())
+        O = g.gpic_orthogonalize(G, eps=0.0)
+        assert _rel(O, _polar(G, eps=0.0)) <= _polar_tolerance(dtype), s
+    # the zero matrix of a stack stays what it was, 0 / 0
+    G[1] = 0
+    O = g.gpic_orthogonalize(G, eps=0.0)
+    assert bool(O[1].isnan().all()) and bool(torch.isfinite(O[0]).all())
+    assert not bool(g.gpic_orthogonalize(torch.zeros_like(G)).any())
