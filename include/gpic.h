@@ -562,8 +562,8 @@ size_t gpic_polar_workspace_bytes(const gpic_polar_params *p);
  * right for m > n): the singular vectors of G with its singular values
  * taken near 1.  O may be G itself.  A zero matrix gives zeros (with eps > 0).
  * float32 and float16 matrices, and bfloat16 ones whose smaller side is up to
- * 64, in split halves; other bfloat16 matrices with half-precision products,
- * to about 2e-3 of |O|.
+ * 128, in split halves; other bfloat16 matrices with half-precision products,
+ * to about 2e-3 of |O| (the rounding of O to bfloat16 is 1.7e-3).
  * ws: gpic_polar_workspace_bytes(p).  Asynchronous. */
 gpic_status gpic_orthogonalize(const gpic_polar_params *p, const void *G, void *O, void *ws,
                                size_t ws_bytes, void *stream);

@@ -18,12 +18,14 @@
 //   range and carry 3 more bits), and X keeps the low half beside it for the
 //   term a X, which carries the small directions: with X rounded to 11 bits
 //   there too, a gradient of low rank over noise comes out 1.4e-2 off, with
-//   8 bits 1.1e-1, so 1.1e-4 (512 x 2048, float64 reference); for Gaussian
-//   matrices the result is 1.2e-3 to 1.7e-3 off, below its final rounding.
-//   Up to 64 rows (columns) they are split as the others are: the fewer
-//   directions, the less the roundings average out (2.1e-3 off at 31 x
-//   7,489, 1.3e-3 at 64 x 7,489, the final rounding apart), and it costs 8 to
-//   14 us of 133 there, 23 us of 136 at 256 x 4,096.
+//   8 bits 1.1e-1, so 1.1e-4 (512 x 2048, float64 reference).  The final
+//   rounding (1.7e-3) apart, Gaussian matrices are 1.9e-3 off at 160 x 700, 1.7e-3
+//   at 512 x 2,048, 1.3e-3 at 1,024 x 4,096, 1.2e-3 at 2,048 squared, gradients of
+//   a decaying spectrum 1.4e-3 to 0.6e-3: the fewer directions, the less the
+//   roundings average out.  Up to 128 rows (columns) they are split as the others
+//   are (2.1e-3 off in halves at 65 x 300, 1.9e-3 at 128 x 300, 1e-6 split), for
+//   99 us instead of 84 and 105 instead of 87; at 512 x 2,048 it would be 192
+//   instead of 156, at 1,024 x 4,096 434 instead of 281.
 // The norm is summed in float64.
 #include "encoder.h"
 
@@ -32,7 +34,7 @@ namespace gpic {
 namespace {
 
 constexpr int kParts = 1024;           // partial sums of squares per matrix
-constexpr int64_t kSplitSide = 64;     // bfloat16: split operands up to this smaller side
+constexpr int64_t kSplitSide = 128;    // bfloat16: split operands up to this smaller side
 constexpr float kStore = 1024.0f;      // X, A, P are stored times this: entries of
                                        // each are at most 60 for the coefficients and
                                        // steps that the entry points accept (1.3 and

@@ -65,3 +65,19 @@ def test_magnitudes_at_the_ends_of_the_type(g, shape, dtype):
     O = g.gpic_orthogonalize(G, eps=0.0)
     assert bool(O[1].isnan().all()) and bool(torch.isfinite(O[0]).all())
     assert not bool(g.gpic_orthogonalize(torch.zeros_like(G)).any())
+
+
+# The rounding of the result to 8 bits: half a unit, uniform, of values of which
+# all mantissas are as likely, 2^-7 / sqrt(12) / 1.35 = 1.7e-3 in the 2-norm.  Each
+# of five steps rounds X, A and b A + c A^2 to 11 bits, 1.7e-3 / 8 of them each,
+# against terms three times the result's size, and p'(1) = -0.7 takes half of
+# the square of it on to the next: sqrt(3) 3 (2.1e-4) sqrt(2) = 1.6e-3, a quarter more
+# for entries that are not independent.  Two bits less in the iterates would be
+# 6e-3 and more.
+@pytest.mark.parametrize("shape", [(1, 65, 300), (2, 100, 1000), (1, 300, 300), (1, 1500, 513),
+                                   (1, 1024, 4096)], ids=str)
+def test_bf16_iterates_keep_eleven_bits(g, shape):
+    gen = torch.Generator(device=DEV).manual_seed(5)
+    for G in (torch.randn(shape, device=DEV, generator=gen), _gradient(shape, 9)):
+        G = G.to(torch.bfloat16)
+        assert _rel(g.gpic_orthogonalize(G), _polar(G)) <= (1.7e-3 ** 2 + 2.0e-3 ** 2) ** 0.5
