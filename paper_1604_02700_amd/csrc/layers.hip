@@ -169,18 +169,20 @@ struct RowJobs {
     RowJob j[2];
 };
 
-// Split copies of X and W (grid.y) whose rows have a power of two each: WAVES
-// waves (one: four rows a workgroup) read a row into registers, find its
+// Split copies of X and W (grid.y) whose rows have a power of two each: one
+// wave or all four of a workgroup read a row into registers, find its
 // largest finite magnitude and write its parts, so that the matrix is read
-// once; of rows longer than 2,048 values a wave the rest is read again.
+// once; of rows longer than 2,048 values a wave the rest is read again.  Bound
+// by memory: 10,007 x 1,000 and 777 x 1,000, read and written (86 MB), 18.5 us,
+// 4.7 TB/s.
 template <int WAVES>
-__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void split_rows_kernel(RowJobs jobs)
+__global__ __launch_bounds__(256) void split_rows_kernel(RowJobs jobs)
 {
-    constexpr int kRows = WAVES == 1 ? 4 : 1, kHold = 4, kStride = 64 * WAVES;
+    constexpr int kRows = 4 / WAVES, kHold = 4, kStride = 64 * WAVES;
     const RowJob m = jobs.j[blockIdx.y];
     const int wave = threadIdx.x >> 6, at = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
     const int64_t width = (m.cols + 31) / 32 * 32, groups = width / 8;
-    __shared__ float most[8];
+    __shared__ float most[WAVES];
     for (int64_t r = (int64_t)blockIdx.x * kRows + (WAVES == 1 ? wave : 0); r < m.rows;
          r += (int64_t)gridDim.x * kRows) {
         const float *x = m.x + r * m.ld;
@@ -364,7 +366,7 @@ struct MaximaArgs {
 // dZ, which is formed for it and not kept: one more pass over dY and Z (the
 // second one finds them in the caches where they fit), and no product of
 // bounds stands in for a maximum.  Bound by memory and by the activation: dY
-// and Z of 10,007 x 777 with gelu, X of 10,007 x 1,000 and W (96 MB) 23 us, 4.2
+// and Z of 10,007 x 777 with gelu, X of 10,007 x 1,000 and W (105 MB) 22.5 us, 4.7
 // TB/s; the powers from the partial maxima 6 us.
 template <int DT, int ACT, bool GATED>
 __global__ __launch_bounds__(256) void maxima_kernel(MaximaArgs a)
@@ -498,10 +500,15 @@ __global__ __launch_bounds__(1024) void powers_kernel(PowerJobs a)
 }
 
 // dZ of `rows` rows x 256 columns a workgroup (four rows at a time, four
-// columns a thread) and their column sums, in float32 in a fixed order.
+// columns a thread) and their column sums, in float32 in a fixed order.  For
+// the products dZ is rounded as their operands are: to the matrices' type
+// (float32: to two halves).  In bfloat16 that is what the gradients lose beside
+// their own rounding (16,384 x 2,048 -> 8,192: 2.4e-3 off in the 2-norm, 1.7e-3
+// if only the result were rounded); two parts of it would double the products.
 // Bound by memory: reads dY and Z, writes dZ once.  16,384 x 8,192 in
 // bfloat16 with gelu 184 us (805 MB, 4.4 TB/s); gated 8,192 x 5,504 with silu
-// 171 us (631 MB, 3.7 TB/s).  Inside the products it would be formed once
+// 171 us (631 MB, 3.7 TB/s); float32 10,007 x 777 with gelu, both copies, 30 us
+// (124 MB, 4.1 TB/s).  Inside the products it would be formed once
 // per tile row and column, and twice (dX and dW read it in different orders).
 template <int DT, int ACT, bool GATED>
 __global__ __launch_bounds__(256) void grad_kernel(GradArgs a)
@@ -653,7 +660,7 @@ struct Source {
 };
 
 // 16-bit matrices are read as they lie when rows start on 16 bytes and
-// hold whole chunks of 8 values; float32 ones are always split.  `vec16`:
+// hold whole chunks of 8 values; float32 ones are always split.  `aligned16`:
 // every matrix starts on 16 bytes.
 bool must_pack(int dtype, int64_t cols, int64_t ld, bool aligned16)
 {
@@ -680,13 +687,15 @@ hipError_t launch_split_rows(const Source &x, const Source &w, hipStream_t st)
         j.j[i] = RowJob{static_cast<const float *>(list[i]->x), list[i]->rows, list[i]->cols,
                         list[i]->ld, static_cast<_Float16 *>(list[i]->to), list[i]->power};
     const int64_t rows = x.rows > w.rows ? x.rows : w.rows;
-    const bool one = x.cols <= 2048;
+    // one wave a row or four: 3,200 rows of 2,143 values 14 and 17 us, of 4,096 23
+    // and 20, of 8,000 56 and 43 (eight waves 24, 25 and 42)
+    const bool one = x.cols <= 3000;
     int64_t blocks = one ? (rows + 3) / 4 : rows;
     blocks = blocks > (1 << 20) ? 1 << 20 : blocks;
     if (one)
         split_rows_kernel<1><<<dim3((unsigned)blocks, 2), 256, 0, st>>>(j);
     else
-        split_rows_kernel<8><<<dim3((unsigned)blocks, 2), 512, 0, st>>>(j);
+        split_rows_kernel<4><<<dim3((unsigned)blocks, 2), 256, 0, st>>>(j);
     return hipGetLastError();
 }
 
