@@ -169,21 +169,20 @@ struct RowJobs {
     RowJob j[2];
 };
 
-// Split copies of X and W (grid.y) whose rows have a power of two each: one
-// wave or all four of a workgroup read a row into registers, find its
-// largest finite magnitude and write its parts, so that the matrix is read
-// once; of rows longer than 2,048 values a wave the rest is read again.  Bound
-// by memory: 10,007 x 1,000 and 777 x 1,000, read and written (86 MB), 18.5 us,
-// 4.7 TB/s.
-template <int WAVES>
+// Split copies of X and W (grid.y) whose rows have a power of two each: LANES
+// lanes of a workgroup read a row into registers, find its largest finite
+// magnitude and write its parts, so that the matrix is read once; what a row has
+// beyond four groups of eight values a lane is read again.  Bound by memory:
+// 10,007 x 1,000 and 777 x 1,000, read and written (86 MB), 15 us, 5.7 TB/s.
+template <int LANES>
 __global__ __launch_bounds__(256) void split_rows_kernel(RowJobs jobs)
 {
-    constexpr int kRows = 4 / WAVES, kHold = 4, kStride = 64 * WAVES;
+    constexpr int kRows = 256 / LANES, kHold = 4, kStride = LANES;
     const RowJob m = jobs.j[blockIdx.y];
-    const int wave = threadIdx.x >> 6, at = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
+    const int wave = threadIdx.x >> 6, at = threadIdx.x % LANES;
     const int64_t width = (m.cols + 31) / 32 * 32, groups = width / 8;
-    __shared__ float most[WAVES];
-    for (int64_t r = (int64_t)blockIdx.x * kRows + (WAVES == 1 ? wave : 0); r < m.rows;
+    __shared__ float most[4];
+    for (int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES; r < m.rows;
          r += (int64_t)gridDim.x * kRows) {
         const float *x = m.x + r * m.ld;
         f32x4 v[kHold][2];
@@ -212,15 +211,15 @@ __global__ __launch_bounds__(256) void split_rows_kernel(RowJobs jobs)
             best = finite_max(finite_max(best, u[0]), u[1]);
         }
 #pragma unroll
-        for (int o = 32; o > 0; o >>= 1)
+        for (int o = LANES < 64 ? LANES / 2 : 32; o > 0; o >>= 1)
             best = fmaxf(best, __shfl_xor(best, o, 64));
-        if (WAVES > 1) {
+        if (LANES > 64) {
             __syncthreads();             // the row before has been read
             if ((threadIdx.x & 63) == 0)
                 most[wave] = best;
             __syncthreads();
 #pragma unroll
-            for (int w = 0; w < WAVES; ++w)
+            for (int w = 0; w < 4; ++w)
                 best = fmaxf(best, most[w]);
         }
         const int power = power_for(best);
@@ -687,15 +686,23 @@ hipError_t launch_split_rows(const Source &x, const Source &w, hipStream_t st)
         j.j[i] = RowJob{static_cast<const float *>(list[i]->x), list[i]->rows, list[i]->cols,
                         list[i]->ld, static_cast<_Float16 *>(list[i]->to), list[i]->power};
     const int64_t rows = x.rows > w.rows ? x.rows : w.rows;
-    // one wave a row or four: 3,200 rows of 2,143 values 14 and 17 us, of 4,096 23
-    // and 20, of 8,000 56 and 43 (eight waves 24, 25 and 42)
-    const bool one = x.cols <= 3000;
-    int64_t blocks = one ? (rows + 3) / 4 : rows;
+    // Few lanes a row keep all of them at work and more loads in flight.  us, X's
+    // rows by 8, 32, 64 and 256 lanes: 50,000 x 72 13, 24, 42 and 130; 20,000 x 256
+    // 14, 15, 20, 54; 10,000 x 512 12, 15, 16, 31; 10,007 x 1,000 25, 14, 17, 30;
+    // 10,007 x 2,000 42, 32, 27, 32; 3,200 x 3,000 48, 19, 17, 17; 3,200 x 4,096 58,
+    // 26, 23, 20
+    const int lanes = x.cols <= 512 ? 8 : (x.cols <= 1024 ? 32 : (x.cols <= 3000 ? 64 : 256));
+    int64_t blocks = (rows * lanes + 255) / 256;
     blocks = blocks > (1 << 20) ? 1 << 20 : blocks;
-    if (one)
-        split_rows_kernel<1><<<dim3((unsigned)blocks, 2), 256, 0, st>>>(j);
+    const dim3 grid((unsigned)blocks, 2);
+    if (lanes == 8)
+        split_rows_kernel<8><<<grid, 256, 0, st>>>(j);
+    else if (lanes == 32)
+        split_rows_kernel<32><<<grid, 256, 0, st>>>(j);
+    else if (lanes == 64)
+        split_rows_kernel<64><<<grid, 256, 0, st>>>(j);
     else
-        split_rows_kernel<4><<<dim3((unsigned)blocks, 2), 256, 0, st>>>(j);
+        split_rows_kernel<256><<<grid, 256, 0, st>>>(j);
     return hipGetLastError();
 }
 
