@@ -342,13 +342,14 @@ __device__ __forceinline__ void form4(f32x4 dy, f32x4 g, f32x4 u, f32x4 &d, f32x
 }
 
 // Partial maxima of a float32 matrix's columns, or of dZ's columns and rows
-// (float16: of dZ as a whole): `parts` runs of `each` rows by strips of 256
-// columns.
+// (float16: of dZ as a whole): `parts` runs of `each` rows by strips of 4
+// `lanes` columns.
 struct Maxima {
     const float *x;        // null: dZ
     int64_t rows, cols, ld;
     float *part;           // [parts][cols]
     int64_t strips, parts, each;
+    int lanes;             // 16 or 32
     __host__ __device__ int64_t blocks() const { return strips * parts; }
 };
 struct MaximaArgs {
@@ -361,66 +362,83 @@ struct MaximaArgs {
     float *row_part;
 };
 
-// Largest finite magnitudes of the columns of X, W and dZ and of the rows of
-// dZ, which is formed for it and not kept: one more pass over dY and Z (the
-// second one finds them in the caches where they fit), and no product of
-// bounds stands in for a maximum.  Bound by memory and by the activation: dY
-// and Z of 10,007 x 777 with gelu, X of 10,007 x 1,000 and W (105 MB) 22.5 us, 4.7
-// TB/s; the powers from the partial maxima 6 us.
-template <int DT, int ACT, bool GATED>
-__global__ __launch_bounds__(256) void maxima_kernel(MaximaArgs a)
+// largest finite magnitudes of four columns of a strip (dZ: and of the up
+// projection's) over rows r0 .. r1 - 1; of dZ's rows in row_part, float16: only
+// the largest of all, in best
+template <int DT, int ACT, bool GATED, bool DZ>
+__device__ __forceinline__ void scan_maxima(const MaximaArgs &a, const Maxima &m, int64_t strip,
+                                            int64_t r0, int64_t r1, f32x4 &best,
+                                            f32x4 &best_u)
 {
     constexpr int ZT = GATED ? GPIC_F32 : DT;      // the type of Z
-    int64_t id = blockIdx.x;
-    int job = 0;
-    while (job + 1 < a.count && id >= a.j[job].blocks())
-        id -= a.j[job++].blocks();
-    const Maxima m = a.j[job];
-    const int64_t strip = id % m.strips, part = id / m.strips;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t cols = m.x ? m.cols : a.m, col = strip * 256 + lane * 4;
-    const int64_t r0 = part * m.each, r1 = r0 + m.each < m.rows ? r0 + m.each : m.rows;
-    f32x4 best = 0.0f, best_u = 0.0f;
-    constexpr int kRows = 2;               // of a wave in flight
-    for (int64_t r = r0 + wave; r < r1; r += 4 * kRows) {
+    constexpr int kRows = DZ ? 2 : 4;              // of a lane in flight
+    const int lanes = m.lanes, at = threadIdx.x & (lanes - 1), abreast = 256 / lanes;
+    const int64_t cols = DZ ? a.m : m.cols, col = (strip * lanes + at) * 4;
+    for (int64_t r = r0 + threadIdx.x / lanes; r < r1; r += abreast * kRows) {
         f32x4 x[kRows], g[kRows], u[kRows];
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
             x[i] = g[i] = u[i] = 0.0f;
-            const int64_t row = r + 4 * i;
+            const int64_t row = r + (int64_t)abreast * i;
             if (row < r1 && col < cols) {
-                x[i] = m.x ? read4(m.x, row * m.ld, col, cols, GPIC_F32)
-                           : read4(a.dY, row * a.ldy, col, cols, DT);
-                if (!m.x && (GATED || ACT != GPIC_ACT_NONE))
+                x[i] = DZ ? read4(a.dY, row * a.ldy, col, cols, DT)
+                          : read4(m.x, row * m.ld, col, cols, GPIC_F32);
+                if (DZ && (GATED || ACT != GPIC_ACT_NONE))
                     g[i] = read4(a.Z, row * a.ldz, col, cols, ZT);
-                if (!m.x && GATED)
+                if (DZ && GATED)
                     u[i] = read4(a.Z, row * a.ldz + a.m, col, cols, ZT);
             }
         }
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
             f32x4 d = x[i], du = 0.0f;
-            if (!m.x)
+            if (DZ)
                 form4<ACT, GATED>(x[i], g[i], u[i], d, du);
             float most = 0.0f;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const float v = fabsf(d[j]), w = GATED ? fabsf(du[j]) : 0.0f;
-                best[j] = v < INFINITY && v > best[j] ? v : best[j];
-                best_u[j] = w < INFINITY && w > best_u[j] ? w : best_u[j];
-                most = v < INFINITY && v > most ? v : most;
-                most = w < INFINITY && w > most ? w : most;
+                const float v = fabsf(d[j]), w = fabsf(du[j]);
+                const float fv = v < INFINITY ? v : 0.0f, fw = w < INFINITY ? w : 0.0f;
+                best[j] = fmaxf(best[j], fv);
+                if (DZ && GATED)
+                    best_u[j] = fmaxf(best_u[j], fw);
+                most = fmaxf(most, DZ && GATED ? fmaxf(fv, fw) : fv);
             }
-            if (m.x || DT == GPIC_F16)
+            if (!DZ || DT == GPIC_F16)
                 continue;
-#pragma unroll
-            for (int o = 32; o > 0; o >>= 1)
+            for (int o = lanes / 2; o > 0; o >>= 1)
                 most = fmaxf(most, __shfl_xor(most, o, 64));
-            const int64_t row = r + 4 * i;
-            if (lane == 0 && row < r1)
+            const int64_t row = r + (int64_t)abreast * i;
+            if (at == 0 && row < r1)
                 a.row_part[strip * m.rows + row] = most;
         }
     }
+}
+
+// Largest finite magnitudes of the columns of X, W and dZ and of the rows of
+// dZ, which is formed for it and not kept: one more pass over dY and Z (the
+// second one finds them in the caches where they fit), and no product of
+// bounds stands in for a maximum.  Strips are narrow, so that little of the
+// last one is beyond the columns.  Bound by memory and by the activation: dY and
+// Z of 10,007 x 777 with gelu, X of 10,007 x 1,000 and W (105 MB) 24 us, 4.4 TB/s;
+// the powers from the partial maxima 5.5 us.
+template <int DT, int ACT, bool GATED>
+__global__ __launch_bounds__(256) void maxima_kernel(MaximaArgs a)
+{
+    int64_t id = blockIdx.x;
+    int job = 0;
+    while (job + 1 < a.count && id >= a.j[job].blocks())
+        id -= a.j[job++].blocks();
+    const Maxima m = a.j[job];
+    const bool dz = m.x == nullptr;
+    const int64_t strip = id % m.strips, part = id / m.strips;
+    const int64_t cols = dz ? a.m : m.cols;
+    const int64_t r0 = part * m.each, r1 = r0 + m.each < m.rows ? r0 + m.each : m.rows;
+    f32x4 best = 0.0f, best_u = 0.0f;
+    if (dz)
+        scan_maxima<DT, ACT, GATED, true>(a, m, strip, r0, r1, best, best_u);
+    else
+        scan_maxima<DT, ACT, GATED, false>(a, m, strip, r0, r1, best, best_u);
     if (DT == GPIC_F16) {
         float most = 0.0f;
 #pragma unroll
@@ -438,18 +456,20 @@ __global__ __launch_bounds__(256) void maxima_kernel(MaximaArgs a)
     all[0][threadIdx.x] = best;
     all[1][threadIdx.x] = best_u;
     __syncthreads();
-    // wave 0 the columns, wave 1 the up projection's
-    if (wave > (GATED && !m.x ? 1 : 0))
+    // the first `lanes` threads the columns, the next ones the up projection's
+    const int lanes = m.lanes, half = threadIdx.x / lanes, at = threadIdx.x & (lanes - 1);
+    if (half > (GATED && dz ? 1 : 0))
         return;
+    f32x4 v = 0.0f;
+    for (int k = at; k < 256; k += lanes)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        float v = 0.0f;
+        for (int j = 0; j < 4; ++j)
+            v[j] = fmaxf(v[j], all[half][k][j]);
+    const int64_t col = (strip * lanes + at) * 4;
 #pragma unroll
-        for (int w = 0; w < 4; ++w)
-            v = fmaxf(v, all[wave][w * 64 + lane][j]);
+    for (int j = 0; j < 4; ++j)
         if (col + j < cols)
-            m.part[part * m.cols + (wave ? a.m : 0) + col + j] = v;
-    }
+            m.part[part * m.cols + (half ? a.m : 0) + col + j] = v[j];
 }
 
 // Powers of two from partial maxima [parts][len]: a thread an entry, or
@@ -790,14 +810,17 @@ int grad_rows(int64_t n, int64_t m)
     return rows;
 }
 
-// How the maxima of a matrix's columns are cut: about 1,536 workgroups, none
-// of fewer than 16 rows (768: 27 us for 23 at 10,007 rows).
+// How the maxima of a matrix's columns are cut: strips of 128 columns (of 64,
+// where that is all: 100,000 x 16 -> 64 14 us instead of 21), about 1,536
+// workgroups, none of fewer than 16 rows and no more than 512 runs of rows,
+// which the powers are then found from.
 Maxima maxima_of(const void *x, int64_t rows, int64_t cols, int64_t ld, int64_t across)
 {
-    Maxima m{static_cast<const float *>(x), rows, cols, ld, nullptr, (across + 255) / 256, 0, 0};
+    Maxima m{static_cast<const float *>(x), rows, cols, ld, nullptr, 0, 0, 0, across <= 64 ? 16 : 32};
+    m.strips = (across + 4 * m.lanes - 1) / (4 * m.lanes);
     int64_t parts = 1536 / m.strips;
     parts = parts < (rows + 15) / 16 ? parts : (rows + 15) / 16;
-    parts = parts < 1 ? 1 : parts;
+    parts = parts < 1 ? 1 : (parts > 512 ? 512 : parts);
     m.each = (rows + parts - 1) / parts;
     m.parts = m.each ? (rows + m.each - 1) / m.each : 0;
     return m;
