@@ -173,7 +173,7 @@ struct RowJobs {
 // lanes of a workgroup read a row into registers, find its largest finite
 // magnitude and write its parts, so that the matrix is read once; what a row has
 // beyond four groups of eight values a lane is read again.  Bound by memory:
-// 10,007 x 1,000 and 777 x 1,000, read and written (86 MB), 15 us, 5.7 TB/s.
+// 10,007 x 1,000 and 777 x 1,000, read and written (86 MB), 18 us, 4.8 TB/s.
 template <int LANES>
 __global__ __launch_bounds__(256) void split_rows_kernel(RowJobs jobs)
 {
@@ -710,8 +710,10 @@ hipError_t launch_split_rows(const Source &x, const Source &w, hipStream_t st)
     // rows by 8, 32, 64 and 256 lanes: 50,000 x 72 13, 24, 42 and 130; 20,000 x 256
     // 14, 15, 20, 54; 10,000 x 512 12, 15, 16, 31; 10,007 x 1,000 25, 14, 17, 30;
     // 10,007 x 2,000 42, 32, 27, 32; 3,200 x 3,000 48, 19, 17, 17; 3,200 x 4,096 58,
-    // 26, 23, 20
-    const int lanes = x.cols <= 512 ? 8 : (x.cols <= 1024 ? 32 : (x.cols <= 3000 ? 64 : 256));
+    // 26, 23, 20.  Few rows by 64 lanes fill the card better (1,400 x 300 5.4 for
+    // 6.8 by 8).
+    int lanes = x.cols <= 512 ? 8 : (x.cols <= 1024 ? 32 : (x.cols <= 3000 ? 64 : 256));
+    lanes = rows * lanes < 65536 && lanes < 64 ? 64 : lanes;
     int64_t blocks = (rows * lanes + 255) / 256;
     blocks = blocks > (1 << 20) ? 1 << 20 : blocks;
     const dim3 grid((unsigned)blocks, 2);

@@ -450,11 +450,11 @@ hipError_t launch_either(const RowArgs &a, bool gated, hipStream_t st)
 // products, or little work, where launches do (32 rows at a time then).
 // float32 beyond 32 values of k only for small results: the float32 matrix
 // instruction then costs more than packed operands' two launches.  gelu, us,
-// here and as a tiled product: 1,003 x 64 -> 700 6.9 and 12.6, 50,000 x 64 -> 256 38
-// and 38, 16,384 x 64 -> 8,192 240 and 194, 16,384 x 32 -> 8,192 177 and 176 (bfloat16
-// 107 and 150); 52 x 512 -> 123 5.4 and 16, 200 x 300 -> 700 5.8 and 16.2 (bfloat16 5.9
-// and 9.7), 100 x 1,000 -> 1,000 7.7 and 21 (4.9 and 10), 1,003 x 300 -> 700 14 and 17.3
-// (12.4 and 10.3), 2,000 x 700 -> 700 47 and 28 (34 and 16).
+// here and as a tiled product: 1,003 x 64 -> 700 6.9 and 9.7, 50,000 x 64 -> 256 42
+// and 40, 16,384 x 64 -> 8,192 251 and 192, 16,384 x 32 -> 8,192 179 and 170 (bfloat16
+// 107 and 150); 52 x 512 -> 123 5.5 and 15, 200 x 300 -> 700 5.8 and 14.5 (bfloat16 5.9
+// and 9.7), 100 x 1,000 -> 1,000 7.9 and 19 (4.9 and 10), 1,003 x 300 -> 700 14 and 16
+// (12.4 and 10.3), 2,000 x 700 -> 700 48 and 26 (34 and 16).
 bool as_rows(const Shape &s, bool gated)
 {
     const bool f32 = s.dtype == GPIC_F32;

@@ -232,12 +232,12 @@ int64_t rows_of(const Shape &s, bool gated) { return gated ? 2 * s.m : s.m; }
 
 // Where this beats the tiled products' six to eight launches: short
 // contractions (a workgroup goes through all of one) and little work.  us, here
-// and tiled, gelu and gated silu: float32 52 x 512 -> 123 4.5 and 24.5, 200 x 300
-// -> 700 10.2 and 32.3, gated 18 and 35, 1,003 x 300 -> 700 33 and 45, gated 53 and
-// 46, 100 x 1,000 -> 2 x 1,000 41 and 40, 16 x 2,048 -> 2,048 43 and 42; bfloat16 52 x 512 ->
-// 123 5.1 and 15.1, 200 x 300 -> 700 10.7 and 23.5, 100 x 1,000 -> 1,000 24 and 22,
-// 1,003 x 300 -> 700 33 and 32, 2 x 58 -> 2 x 588 14 and 19, 16 x 2,048 -> 2,048 51 and
-// 23 (16 bits: contractions beyond 1,024 for very little work only).
+// and tiled, gelu and gated silu: float32 52 x 512 -> 123 4.5 and 26.5, 200 x 300
+// -> 700 10.3 and 36, gated 18 and 40, 1,003 x 300 -> 700 33 and 51, gated 54 and
+// 52, 100 x 1,000 -> 2 x 1,000 40 and 46, 16 x 2,048 -> 2,048 43 and 46; bfloat16 52 x 512 ->
+// 123 5.0 and 13.9, 200 x 300 -> 700 11 and 22, 100 x 1,000 -> 1,000 22 and 21,
+// 1,003 x 300 -> 700 33 and 31, 2 x 58 -> 2 x 588 14 and 18, 16 x 2,048 -> 2,048 50 and
+// 22 (16 bits: contractions beyond 1,024 for very little work only).
 bool small_gradients(const Shape &s, bool gated)
 {
     const int64_t rows = rows_of(s, gated), far = (int64_t)1 << 28;
