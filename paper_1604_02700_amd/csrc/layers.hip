@@ -14,7 +14,7 @@ namespace gpic {
 
 namespace {
 
-constexpr int kSumRows = 64;          // most rows of a partial column sum
+constexpr int kSumRows = 64;          // most rows of a partial column sum (below 2^29 in all)
 
 inline size_t up(size_t x) { return (x + 255) & ~(size_t)255; }
 __host__ __device__ inline int64_t up64(int64_t x) { return (x + 63) & ~(int64_t)63; }
