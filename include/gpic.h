@@ -582,6 +582,91 @@ typedef struct gpic_muon_params {
 gpic_status gpic_muon_step(const gpic_polar_params *p, const gpic_muon_params *h, void *W,
                            const void *G, float *M, void *ws, size_t ws_bytes, void *stream);
 
+/* ------------------------------ 8. what surrounds an encoder's layers in training
+ *
+ * The table that tokens enter an encoder through, the norm and the dropout
+ * between its blocks, and a loss over a vocabulary.  Types, pitches, overlap and
+ * reproducibility as in section 7: all matrices of a call have one type, sums
+ * are float32 or wider in a fixed order, results that overlap what a call reads
+ * are refused but where stated.  Asynchronous. */
+
+typedef struct gpic_norm_params {
+    int64_t n, k;        /* rows (0 .. 2^31 - 1), columns (1 .. 2^20)             */
+    int64_t ldx, ldy;    /* pitches of X and of Y (backward: of dY), up to 2^22   */
+    float eps;           /* >= 0, finite                                          */
+    int32_t dtype;       /* GPIC_F32, GPIC_F16 or GPIC_BF16                       */
+} gpic_norm_params;
+
+/* Y = (X - mean) r w + b, row by row, with r = 1 / sqrt(var + eps) and the
+ * variance over k.  weight and bias [k] nullable (ones, zeros); stats (float32
+ * [n x 2], 8-byte aligned, nullable) receives mean and r, which the gradients
+ * need.  A row that holds a NaN or an infinity gives a row of NaN and no other.
+ * Y may be X itself (same pitch).  Errors: INVALID_ARG. */
+gpic_status gpic_layer_norm(const gpic_norm_params *p, const void *X, const void *weight,
+                            const void *bias, void *Y, float *stats, void *stream);
+
+/* Workspace bytes of the gradients (0 also for parameters that they refuse). */
+size_t gpic_layer_norm_workspace_bytes(const gpic_norm_params *p);
+
+/* Gradients of the same: with g = dY w and h = (X - mean) r, dX [n x k] =
+ * r (g - mean(g) - h mean(g h)), dW [k] = column sums of dY h, db [k] = column
+ * sums of dY.  dX, dW and db are contiguous, any may be null (not wanted).  With
+ * n = 0, dW and db are zeros.  ws: gpic_layer_norm_workspace_bytes(p). */
+gpic_status gpic_layer_norm_backward(const gpic_norm_params *p, const void *dY, const void *X,
+                                     const void *weight, const float *stats, void *dX, void *dW,
+                                     void *db, void *ws, size_t ws_bytes, void *stream);
+
+typedef struct gpic_dropout_params {
+    int64_t n, m;             /* rows (0 .. 2^31 - 1), columns (1 .. 2^20)        */
+    int64_t ldx, ldr, ldy;    /* pitches of X, the residual (ignored without one)
+                                 and Y, up to 2^22                                */
+    uint64_t seed, offset;
+    double p;                 /* 0 <= p, round(2^16 p) < 2^16                     */
+    int32_t dtype;            /* GPIC_F32, GPIC_F16 or GPIC_BF16                  */
+    int32_t reserved;         /* must be 0                                        */
+} gpic_dropout_params;
+
+/* Y = residual + keep X / (1 - p').  p' is p in steps of 2^-16, L = round(2^16
+ * p) of them.  Value i = row m + column stays where its 16 bits are at least L:
+ * bits 16 (i mod 2) and on of word (i mod 8) / 2 of the block that Philox4x32-10
+ * gives for the counter (i / 8, offset + *step), each as two words, low first,
+ * under the key `seed`.  So the mask depends on nothing else (not on the type,
+ * pitches or launch) and is not stored: the gradient with respect to X is the
+ * same call on dY without the residual.  residual and step (device, int64 [1]:
+ * what a captured graph counts its replays with) nullable.  What is dropped
+ * gives 0, infinities and NaN too.  Y may be X or the residual itself (same
+ * pitch).  Errors: INVALID_ARG. */
+gpic_status gpic_dropout(const gpic_dropout_params *p, const void *X, const void *residual,
+                         const int64_t *step, void *Y, void *stream);
+
+typedef struct gpic_embedding_params {
+    int64_t n, k, rows;  /* ids (0 .. 2^31 - 1), columns (1 .. 2^20), the table's
+                            rows (1 .. 2^31 - 1)                                  */
+    int64_t ldt, ldy;    /* pitches of T (backward: of dT) and of Y (dY), up to
+                            2^22                                                  */
+    float scale;         /* finite                                                */
+    int32_t dtype;       /* GPIC_F32, GPIC_F16 or GPIC_BF16                       */
+    int32_t id_bytes;    /* 4 (int32) or 8 (int64)                                */
+    int32_t accumulate;  /* backward: 1 adds to what dT holds, 0 writes all of it */
+} gpic_embedding_params;
+
+/* Y [n x k] = scale T[ids].  An id outside 0 .. rows - 1 (padding) gives a row
+ * of zeros.  Errors: INVALID_ARG. */
+gpic_status gpic_embedding(const gpic_embedding_params *p, const void *ids, const void *T, void *Y,
+                           void *stream);
+
+/* Workspace bytes of the gradient (0 for up to 1,024 ids, which are not sorted,
+ * and for parameters that the call refuses). */
+size_t gpic_embedding_workspace_bytes(const gpic_embedding_params *p);
+
+/* dT [rows x k] = scale times the sum of the rows of dY with that id (accumulate:
+ * plus what dT holds, rounded once more; other rows are not touched), in float32
+ * in a fixed order.  Padding has no part in it.
+ * ws: gpic_embedding_workspace_bytes(p). */
+gpic_status gpic_embedding_backward(const gpic_embedding_params *p, const void *dY,
+                                    const void *ids, void *dT, void *ws, size_t ws_bytes,
+                                    void *stream);
+
 #ifdef __cplusplus
 }
 #endif

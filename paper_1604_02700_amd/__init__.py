@@ -47,7 +47,9 @@ EXPORTS = (
     "gpic_power_iterate_dense_noalloc", "gpic_knn_graph_local",
     "gpic_layer_workspace_bytes", "gpic_linear", "gpic_linear_backward", "gpic_gated",
     "gpic_gated_backward", "gpic_polar_workspace_bytes", "gpic_orthogonalize",
-    "gpic_muon_step",
+    "gpic_muon_step", "gpic_layer_norm", "gpic_layer_norm_workspace_bytes",
+    "gpic_layer_norm_backward", "gpic_dropout", "gpic_embedding",
+    "gpic_embedding_workspace_bytes", "gpic_embedding_backward",
 )
 DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
@@ -95,6 +97,23 @@ class MuonParams(C.Structure):
                 ("scale", C.c_float), ("nesterov", C.c_int32), ("reserved", C.c_int32)]
 
 
+class NormParams(C.Structure):
+    _fields_ = [("n", C.c_int64), ("k", C.c_int64), ("ldx", C.c_int64), ("ldy", C.c_int64),
+                ("eps", C.c_float), ("dtype", C.c_int32)]
+
+
+class DropoutParams(C.Structure):
+    _fields_ = [("n", C.c_int64), ("m", C.c_int64), ("ldx", C.c_int64), ("ldr", C.c_int64),
+                ("ldy", C.c_int64), ("seed", C.c_uint64), ("offset", C.c_uint64),
+                ("p", C.c_double), ("dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
+class EmbeddingParams(C.Structure):
+    _fields_ = [("n", C.c_int64), ("k", C.c_int64), ("rows", C.c_int64), ("ldt", C.c_int64),
+                ("ldy", C.c_int64), ("scale", C.c_float), ("dtype", C.c_int32),
+                ("id_bytes", C.c_int32), ("accumulate", C.c_int32)]
+
+
 _lib = None
 
 
@@ -117,6 +136,10 @@ def lib() -> C.CDLL:
         L.gpic_layer_workspace_bytes.argtypes = [i32, C.POINTER(LayerParams)]
         L.gpic_polar_workspace_bytes.restype = sz
         L.gpic_polar_workspace_bytes.argtypes = [C.POINTER(PolarParams)]
+        L.gpic_layer_norm_workspace_bytes.restype = sz
+        L.gpic_layer_norm_workspace_bytes.argtypes = [C.POINTER(NormParams)]
+        L.gpic_embedding_workspace_bytes.restype = sz
+        L.gpic_embedding_workspace_bytes.argtypes = [C.POINTER(EmbeddingParams)]
         L.gpic_sym_bytes.restype = sz
         L.gpic_sym_bytes.argtypes = [i64]
         sigs = {
@@ -156,6 +179,11 @@ def lib() -> C.CDLL:
             "gpic_gated_backward": [C.POINTER(LayerParams), p, p, p, p, p, p, p, sz, p],
             "gpic_orthogonalize": [C.POINTER(PolarParams), p, p, p, sz, p],
             "gpic_muon_step": [C.POINTER(PolarParams), C.POINTER(MuonParams), p, p, p, p, sz, p],
+            "gpic_layer_norm": [C.POINTER(NormParams), p, p, p, p, p, p],
+            "gpic_layer_norm_backward": [C.POINTER(NormParams)] + [p] * 8 + [sz, p],
+            "gpic_dropout": [C.POINTER(DropoutParams), p, p, p, p, p],
+            "gpic_embedding": [C.POINTER(EmbeddingParams), p, p, p, p],
+            "gpic_embedding_backward": [C.POINTER(EmbeddingParams), p, p, p, p, sz, p],
         }
         for name, args in sigs.items():
             fn = getattr(L, name)
@@ -933,6 +961,169 @@ def gpic_muon_step(W: torch.Tensor, G: torch.Tensor, M: torch.Tensor, lr: float,
     _check(lib().gpic_muon_step(ref, C.byref(h), W.data_ptr(), G.data_ptr(), M.data_ptr(), _at(ws),
                                 nb, _stream(W.device)))
     _written(W, M)
+
+
+# ------------------- 8. what surrounds an encoder's layers in training
+def _run(fn, device, *args):
+    """fn(*args, the current stream of `device`), with that device current."""
+    if device.index == torch.cuda.current_device():
+        _check(fn(*args, _stream(device)))
+    else:
+        with torch.cuda.device(device):
+            _check(fn(*args, _stream(device)))
+
+
+def _columns(t, k, like, name):
+    """A contiguous vector of k values of like's type and device, or None."""
+    if t is None:
+        return None
+    _dev(t, like.dtype, name)
+    if t.shape != (k,) or t.device != like.device:
+        raise ValueError(f"{name} must be [{k}] on {like.device}")
+    return t.contiguous()
+
+
+def _stats(t, n, like):
+    _dev(t, torch.float32, "stats")
+    if t.shape != (n, 2) or t.device != like.device:
+        raise ValueError(f"stats must be {(n, 2)} on {like.device}")
+    return t.contiguous()
+
+
+def _ids(t, n, device, name):
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA (HIP) tensor")
+    if t.dtype not in (torch.int32, torch.int64):
+        raise TypeError(f"{name} must be int32 or int64, got {t.dtype}")
+    if t.dim() != 1 or (n is not None and t.shape[0] != n):
+        raise ValueError(f"{name} must be [{'n' if n is None else n}], got {tuple(t.shape)}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not on {device}")
+    return t.contiguous()
+
+
+def gpic_layer_norm(X: torch.Tensor, weight: Optional[torch.Tensor] = None,
+                    bias: Optional[torch.Tensor] = None, eps: float = 1e-5,
+                    want_stats: bool = False, Y: Optional[torch.Tensor] = None):
+    """Y = (X - mean) / sqrt(var + eps) * weight + bias over the columns of X
+    [n, k] (float32, float16 or bfloat16, weight and bias [k] too).
+    want_stats: returns (Y, stats) with stats float32 [n, 2] (the mean and 1 /
+    sqrt(var + eps)), which gpic_layer_norm_backward reads.  Y (optional) may
+    be X itself.  Records nothing for autograd (as every call of this
+    section): operands that require gradients are refused outside no_grad()."""
+    X = _layer_type(X)
+    n, k = X.shape
+    weight, bias = _columns(weight, k, X, "weight"), _columns(bias, k, X, "bias")
+    given, Y = Y, _output(Y, n, k, X, "Y")
+    stats = torch.empty((n, 2), dtype=torch.float32, device=X.device) if want_stats else None
+    _no_graph("X weight bias Y", X, weight, bias, Y)
+    p = NormParams(n, k, _pitch(X, n, k), _pitch(Y, n, k), float(eps), DTYPES[X.dtype])
+    _run(lib().gpic_layer_norm, X.device, C.byref(p), _at(X), _at(weight), _at(bias), _at(Y),
+         _at(stats))
+    if given is not None:
+        _written(given)
+    return (Y, stats) if want_stats else Y
+
+
+def gpic_layer_norm_backward(dY: torch.Tensor, X: torch.Tensor, weight: Optional[torch.Tensor],
+                             stats: torch.Tensor, want_x: bool = True, want_w: bool = True,
+                             want_bias: bool = True) -> LayerGrads:
+    """Gradients of gpic_layer_norm: dX, dW (of the weight) and db (those
+    wanted).  stats as gpic_layer_norm gave them."""
+    X = _layer_type(X)
+    (n, k), dev = X.shape, X.device
+    dY = _matrix(dY, n, k, X, "dY")
+    weight, stats = _columns(weight, k, X, "weight"), _stats(stats, n, X)
+    dX = torch.empty((n, k), dtype=X.dtype, device=dev) if want_x else None
+    dW = torch.empty(k, dtype=X.dtype, device=dev) if want_w else None
+    db = torch.empty(k, dtype=X.dtype, device=dev) if want_bias else None
+    _no_graph("dY X weight stats", dY, X, weight, stats)
+    p = NormParams(n, k, _pitch(X, n, k), _pitch(dY, n, k), 0.0, DTYPES[X.dtype])
+    ref = C.byref(p)
+    ws, nb = _workspace(lib().gpic_layer_norm_workspace_bytes(ref), dev)
+    _run(lib().gpic_layer_norm_backward, dev, ref, _at(dY), _at(X), _at(weight), _at(stats),
+         _at(dX), _at(dW), _at(db), _at(ws), nb)
+    return LayerGrads(dX, dW, db)
+
+
+def gpic_dropout(X: torch.Tensor, p: float, seed: int, offset: int = 0,
+                 residual: Optional[torch.Tensor] = None, step: Optional[torch.Tensor] = None,
+                 Y: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Y = residual + keep * X / (1 - p) for X [n, m]: the mask is a function
+    of (seed, offset + step, index) and never stored, so the gradient with
+    respect to X is this call on dY without the residual.  p counts in steps of
+    2^-16.  seed and offset: 0 .. 2^64 - 1; step (optional, int64 [1] on X's
+    device) is read when the call runs, for captured graphs to count their
+    replays with.  Y (optional) may be X or the residual."""
+    X = _layer_type(X)
+    n, m = X.shape
+    if residual is not None:
+        residual = _matrix(residual, n, m, X, "residual")
+    if step is not None:
+        _dev(step, torch.int64, "step")
+        if step.numel() != 1 or step.device != X.device:
+            raise ValueError(f"step must be one value on {X.device}")
+    for name, v in (("seed", seed), ("offset", offset)):
+        if not 0 <= int(v) < 1 << 64:
+            raise ValueError(f"{name} must be in 0 .. 2^64 - 1")
+    given, Y = Y, _output(Y, n, m, X, "Y")
+    _no_graph("X residual Y", X, residual, Y)
+    d = DropoutParams(n, m, _pitch(X, n, m), _pitch(residual, n, m), _pitch(Y, n, m), int(seed),
+                      int(offset), float(p), DTYPES[X.dtype], 0)
+    _run(lib().gpic_dropout, X.device, C.byref(d), _at(X), _at(residual), _at(step), _at(Y))
+    if given is not None:
+        _written(given)
+    return Y
+
+
+def gpic_embedding(ids: torch.Tensor, T: torch.Tensor, scale: float = 1.0,
+                   Y: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Y = scale * T[ids] for ids [n] (int32 or int64) and a table T [rows, k]
+    (float32, float16 or bfloat16).  An id outside the table is padding: its
+    row of Y is zeros."""
+    if not isinstance(T, torch.Tensor) or not T.is_cuda:
+        raise TypeError("T must be a CUDA (HIP) tensor")
+    if T.dtype not in DTYPES:
+        raise TypeError(f"T must be float32, float16 or bfloat16, got {T.dtype}")
+    if T.dim() != 2:
+        raise ValueError("T must be [rows, k]")
+    rows, k = T.shape
+    T = _matrix_of(T, rows, k, T, "T")
+    ids = _ids(ids, None, T.device, "ids")
+    n = ids.shape[0]
+    given, Y = Y, _output(Y, n, k, T, "Y")
+    _no_graph("T Y", T, Y)
+    p = EmbeddingParams(n, k, rows, _pitch(T, rows, k), _pitch(Y, n, k), float(scale),
+                        DTYPES[T.dtype], ids.element_size(), 0)
+    _run(lib().gpic_embedding, T.device, C.byref(p), _at(ids), _at(T), _at(Y))
+    if given is not None:
+        _written(given)
+    return Y
+
+
+def gpic_embedding_backward(dY: torch.Tensor, ids: torch.Tensor, rows: int, scale: float = 1.0,
+                            dT: Optional[torch.Tensor] = None,
+                            accumulate: bool = False) -> torch.Tensor:
+    """The gradient of gpic_embedding with respect to its table of `rows`
+    rows: dT[v] = scale * sum of the rows of dY whose id is v, in a fixed
+    order.  accumulate: dT (given) is added to, and its other rows stay, as a
+    table that is also the weights of gpic_cross_entropy wants it."""
+    dY = _layer_type(dY)
+    n, k = dY.shape
+    rows = int(rows)
+    ids = _ids(ids, n, dY.device, "ids")
+    if accumulate and dT is None:
+        raise ValueError("accumulate adds to a given dT")
+    given, dT = dT, _output(dT, rows, k, dY, "dT")
+    _no_graph("dY dT", dY, dT)
+    p = EmbeddingParams(n, k, rows, _pitch(dT, rows, k), _pitch(dY, n, k), float(scale),
+                        DTYPES[dY.dtype], ids.element_size(), int(bool(accumulate)))
+    ref = C.byref(p)
+    ws, nb = _workspace(lib().gpic_embedding_workspace_bytes(ref), dY.device)
+    _run(lib().gpic_embedding_backward, dY.device, ref, _at(dY), _at(ids), _at(dT), _at(ws), nb)
+    if given is not None:
+        _written(given)
+    return dT
 
 
 # ----------------------------------------------- whole paths (call chains)

@@ -159,6 +159,51 @@ __device__ __forceinline__ void store4(void *p, int64_t i, f32x4 v, int dtype)
             __builtin_convertvector(v, bf4);
 }
 
+// Eight values p[i .. i + 7], of which `valid` exist, at any alignment (the
+// card's 16-byte accesses need none; where a row starts on 16 bytes they
+// cover whole lines).
+using f32x8_any = float __attribute__((ext_vector_type(8), aligned(4)));
+using half8_any = _Float16 __attribute__((ext_vector_type(8), aligned(2)));
+using bfrag8_any = __bf16 __attribute__((ext_vector_type(8), aligned(2)));
+
+__device__ __forceinline__ f32x8 load8(const void *p, int64_t i, int dtype, int valid)
+{
+    if (valid >= 8) {
+        if (dtype == GPIC_F32)
+            return *reinterpret_cast<const f32x8_any *>(static_cast<const float *>(p) + i);
+        if (dtype == GPIC_F16)
+            return __builtin_convertvector(
+                *reinterpret_cast<const half8_any *>(static_cast<const _Float16 *>(p) + i), f32x8);
+        return __builtin_convertvector(
+            *reinterpret_cast<const bfrag8_any *>(static_cast<const __bf16 *>(p) + i), f32x8);
+    }
+    f32x8 v = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (j < valid)
+            v[j] = load1(p, i + j, dtype);
+    return v;
+}
+
+__device__ __forceinline__ void store8(void *p, int64_t i, f32x8 v, int dtype, int valid)
+{
+    if (valid >= 8) {
+        if (dtype == GPIC_F32)
+            *reinterpret_cast<f32x8_any *>(static_cast<float *>(p) + i) = v;
+        else if (dtype == GPIC_F16)
+            *reinterpret_cast<half8_any *>(static_cast<_Float16 *>(p) + i) =
+                __builtin_convertvector(v, half8);
+        else
+            *reinterpret_cast<bfrag8_any *>(static_cast<__bf16 *>(p) + i) =
+                __builtin_convertvector(v, bfrag8);
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (j < valid)
+            store1(p, i + j, v[j], dtype);
+}
+
 // ---------------------------------------------------------- split matrices
 // A float32 matrix as 16-bit parts: x = (hi + lo) / s, s a power of two,
 // hi = half(s x), lo = half(s x - hi), 22 significant bits together for
@@ -176,6 +221,42 @@ __host__ __device__ __forceinline__ int64_t split_at(int64_t col)
 {
     return (col >> 5) * 64 + (col & 31);
 }
+
+// The exponent of the power of two that brings `most` into [2^14, 2^15):
+// half-precision parts of the scaled values neither overflow nor, down to
+// 2^-17 of the largest, lose bits.  (-113 .. 164: the power itself may be no
+// float, so it is applied by ldexp.)
+__device__ __forceinline__ int power_for(float most)
+{
+    if (!(most > 0.0f))
+        return 0;
+    int e;
+    frexpf(most, &e);                 // most = f 2^e, f in [1/2, 1)
+    return 15 - e;
+}
+
+__device__ __forceinline__ void split2(float x, _Float16 &hi, _Float16 &lo)
+{
+    hi = (_Float16)x;
+    const float r = x - (float)hi;
+    lo = fabsf((float)hi) < INFINITY ? (_Float16)r : (_Float16)0.0f;
+}
+
+// ----------------------------------------------------- workspaces' layout
+inline size_t up(size_t x) { return (x + 255) & ~(size_t)255; }
+__host__ __device__ inline int64_t up64(int64_t x) { return (x + 63) & ~(int64_t)63; }
+
+// Lays a workspace out; with a null base it only counts.
+struct Cursor {
+    char *base;
+    size_t at = 0;
+    void *take(size_t bytes)
+    {
+        void *p = base ? base + at : nullptr;
+        at += up(bytes);
+        return p;
+    }
+};
 
 // -------------------------------------------------------- matrix product
 // out[M x N] = epilogue(sum_k A(i, k) B(j, k)) over 16-bit operands on the

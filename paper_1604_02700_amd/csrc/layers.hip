@@ -16,21 +16,6 @@ namespace {
 
 constexpr int kSumRows = 64;          // most rows of a partial column sum (below 2^29 in all)
 
-inline size_t up(size_t x) { return (x + 255) & ~(size_t)255; }
-__host__ __device__ inline int64_t up64(int64_t x) { return (x + 63) & ~(int64_t)63; }
-
-// Lays a workspace out; with a null base it only counts.
-struct Cursor {
-    char *base;
-    size_t at = 0;
-    void *take(size_t bytes)
-    {
-        void *p = base ? base + at : nullptr;
-        at += up(bytes);
-        return p;
-    }
-};
-
 // ---------------------------------------------------------------- maxima
 // The largest of `count` values, by a block of 256 threads.
 __device__ __forceinline__ float join_max(const float *part, int count)
@@ -48,26 +33,6 @@ __device__ __forceinline__ float join_max(const float *part, int count)
         w[threadIdx.x >> 6] = best;
     __syncthreads();
     return fmaxf(fmaxf(w[0], w[1]), fmaxf(w[2], w[3]));
-}
-
-// The exponent of the power of two that brings `most` into [2^14, 2^15):
-// half-precision parts of the scaled values neither overflow nor, down to
-// 2^-17 of the largest, lose bits.  (-113 .. 164: the power itself may be no
-// float, so it is applied by ldexp.)
-__device__ __forceinline__ int power_for(float most)
-{
-    if (!(most > 0.0f))
-        return 0;
-    int e;
-    frexpf(most, &e);                 // most = f 2^e, f in [1/2, 1)
-    return 15 - e;
-}
-
-__device__ __forceinline__ void split2(float x, _Float16 &hi, _Float16 &lo)
-{
-    hi = (_Float16)x;
-    const float r = x - (float)hi;
-    lo = fabsf((float)hi) < INFINITY ? (_Float16)r : (_Float16)0.0f;
 }
 
 // --------------------------------------------------------------- packing

@@ -1,0 +1,348 @@
+// Layer norm and its gradients: y = (x - mean) r w + b with r = 1 / sqrt(var
+// + eps); with g = dy w and h = (x - mean) r,
+//   dx = r (g - mean(g) - h mean(g h)),  dw = sum_rows dy h,  db = sum_rows dy.
+// Sums are float32, over rows float64 at the end, in a fixed order.
+#include "training.h"
+
+namespace gpic {
+namespace {
+
+struct NormArgs {
+    const void *X, *w, *b;
+    void *Y;
+    float *stats;              // [n][2]: mean, r
+    int64_t n, k, ldx, ldy;
+    float eps;
+};
+
+// The sum over the LANES lanes that share a row, the same in all of them
+// (LANES > 64: the whole workgroup; `part` is its scratch, LANES / 64 pairs).
+template <int LANES>
+__device__ __forceinline__ void row_sums(float &s, float &t, float2 *part)
+{
+#pragma unroll
+    for (int o = (LANES < 64 ? LANES : 64) / 2; o > 0; o >>= 1) {
+        s += __shfl_xor(s, o, 64);
+        t += __shfl_xor(t, o, 64);
+    }
+    if (LANES <= 64)
+        return;
+    __syncthreads();                     // what was here before has been read
+    if ((threadIdx.x & 63) == 0)
+        part[threadIdx.x >> 6] = make_float2(s, t);
+    __syncthreads();
+    s = t = 0.0f;
+#pragma unroll
+    for (int i = 0; i < LANES / 64; ++i) {
+        s += part[i].x;
+        t += part[i].y;
+    }
+}
+
+template <int DT>
+__device__ __forceinline__ f32x8 read8(const void *p, int64_t row_at, int64_t col, int64_t cols)
+{
+    const int64_t left = cols - col;
+    if (left <= 0)
+        return f32x8(0.0f);
+    return load8(p, row_at + col, DT, left < 8 ? (int)left : 8);
+}
+
+// LANES lanes a row, eight columns at a time; up to kHold groups of them stay
+// in registers, what a row has beyond is read again.  The mean is found first
+// and corrected by the deviations' own sum, so that rows far from zero lose
+// nothing.
+template <int DT, int LANES>
+__global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_kernel(NormArgs a)
+{
+    constexpr int kHold = 4, kThreads = LANES > 256 ? LANES : 256, kRows = kThreads / LANES;
+    __shared__ float2 part[LANES > 64 ? LANES / 64 : 1];
+    const int at = threadIdx.x % LANES;
+    const int64_t groups = (a.k + 7) / 8;
+    const float inv = 1.0f / (float)a.k;
+    for (int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES; r < a.n;
+         r += (int64_t)gridDim.x * kRows) {
+        f32x8 v[kHold];
+        float s = 0.0f, t = 0.0f;
+#pragma unroll
+        for (int h = 0; h < kHold; ++h) {
+            v[h] = read8<DT>(a.X, r * a.ldx, (int64_t)(at + h * LANES) * 8, a.k);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                s += v[h][j];
+        }
+        for (int64_t g = at + kHold * LANES; g < groups; g += LANES) {
+            const f32x8 u = read8<DT>(a.X, r * a.ldx, g * 8, a.k);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                s += u[j];
+        }
+        row_sums<LANES>(s, t, part);
+        float mean = s * inv;
+        s = t = 0.0f;
+        auto deviate = [&](const f32x8 &u, int64_t g) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float d = g * 8 + j < a.k ? u[j] - mean : 0.0f;
+                s += d;
+                t += d * d;
+            }
+        };
+#pragma unroll
+        for (int h = 0; h < kHold; ++h)
+            deviate(v[h], at + h * LANES);
+        for (int64_t g = at + kHold * LANES; g < groups; g += LANES)
+            deviate(read8<DT>(a.X, r * a.ldx, g * 8, a.k), g);
+        row_sums<LANES>(s, t, part);
+        const float off = s * inv;
+        mean += off;
+        const float var = fmaxf(t * inv - off * off, 0.0f);
+        const float rs = 1.0f / sqrtf((t != t ? t : var) + a.eps);
+        if (a.stats && at == 0)
+            reinterpret_cast<float2 *>(a.stats)[r] = make_float2(mean, rs);
+        auto write = [&](const f32x8 &u, int64_t g) {
+            const int64_t left = a.k - g * 8;
+            if (left <= 0)
+                return;
+            const int valid = left < 8 ? (int)left : 8;
+            f32x8 y = (u - mean) * rs;
+            if (a.w)
+                y = y * load8(a.w, g * 8, DT, valid);
+            if (a.b)
+                y = y + load8(a.b, g * 8, DT, valid);
+            store8(a.Y, r * a.ldy + g * 8, y, DT, valid);
+        };
+#pragma unroll
+        for (int h = 0; h < kHold; ++h)
+            write(v[h], at + h * LANES);
+        for (int64_t g = at + kHold * LANES; g < groups; g += LANES)
+            write(read8<DT>(a.X, r * a.ldx, g * 8, a.k), g);
+    }
+}
+
+struct NormGradArgs {
+    const void *dY, *X, *w;
+    const float *stats;
+    void *dX;
+    float *dots;               // [n][2]: mean(g), mean(g h)
+    float *sums;               // [parts][2][k]: of dy h, of dy
+    int64_t n, k, ldx, ldy;
+    int64_t strips, each;
+};
+
+// mean(g) and mean(g h) of every row
+template <int DT, int LANES>
+__global__ __launch_bounds__(256) void norm_dots_kernel(NormGradArgs a)
+{
+    constexpr int kRows = 256 / LANES;
+    __shared__ float2 part[LANES > 64 ? LANES / 64 : 1];
+    const int at = threadIdx.x % LANES;
+    const int64_t groups = (a.k + 7) / 8;
+    const float inv = 1.0f / (float)a.k;
+    for (int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES; r < a.n;
+         r += (int64_t)gridDim.x * kRows) {
+        const float2 st = reinterpret_cast<const float2 *>(a.stats)[r];
+        float s = 0.0f, t = 0.0f;
+        for (int64_t g = at; g < groups; g += LANES) {
+            const int valid = a.k - g * 8 < 8 ? (int)(a.k - g * 8) : 8;
+            f32x8 d = load8(a.dY, r * a.ldy + g * 8, DT, valid);
+            const f32x8 x = load8(a.X, r * a.ldx + g * 8, DT, valid);
+            if (a.w)
+                d = d * load8(a.w, g * 8, DT, valid);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (j < valid) {
+                    s += d[j];
+                    t += d[j] * ((x[j] - st.x) * st.y);
+                }
+        }
+        row_sums<LANES>(s, t, part);
+        if (at == 0)
+            reinterpret_cast<float2 *>(a.dots)[r] = make_float2(s * inv, t * inv);
+    }
+}
+
+// dX and the partial sums of a strip of 512 columns over `each` rows, four
+// rows at a time
+template <int DT>
+__global__ __launch_bounds__(256) void norm_strip_kernel(NormGradArgs a)
+{
+    const int64_t strip = blockIdx.x % a.strips, part = blockIdx.x / a.strips;
+    const int64_t col = (strip * 64 + (threadIdx.x & 63)) * 8;
+    const int64_t r0 = part * a.each, r1 = r0 + a.each < a.n ? r0 + a.each : a.n;
+    const int64_t left = a.k - col;
+    const int valid = left <= 0 ? 0 : (left < 8 ? (int)left : 8);
+    f32x8 sw = 0.0f, sb = 0.0f, w = 1.0f;
+    if (a.w && valid)
+        w = load8(a.w, col, DT, valid);
+    if (valid)
+        for (int64_t r = r0 + (threadIdx.x >> 6); r < r1; r += 4) {
+            const float2 st = reinterpret_cast<const float2 *>(a.stats)[r];
+            const f32x8 d = load8(a.dY, r * a.ldy + col, DT, valid);
+            const f32x8 x = load8(a.X, r * a.ldx + col, DT, valid);
+            const f32x8 h = (x - st.x) * st.y;
+            sw += d * h;
+            sb += d;
+            if (a.dX) {
+                const float2 m = reinterpret_cast<const float2 *>(a.dots)[r];
+                store8(a.dX, r * a.k + col, (d * w - m.x - h * m.y) * st.y, DT, valid);
+            }
+        }
+    if (!a.sums)
+        return;
+    __shared__ f32x8 all[2][4][64];
+    all[0][threadIdx.x >> 6][threadIdx.x & 63] = sw;
+    all[1][threadIdx.x >> 6][threadIdx.x & 63] = sb;
+    __syncthreads();
+    const int which = threadIdx.x >> 6, l = threadIdx.x & 63;
+    if (which < 2 && valid) {
+        const f32x8 s = ((all[which][0][l] + all[which][1][l]) + all[which][2][l]) +
+                        all[which][3][l];
+        store8(a.sums + (part * 2 + which) * a.k, col, s, GPIC_F32, valid);
+    }
+}
+
+// dW and db (grid.y) from the partial sums, in float64 in a fixed order: 64
+// columns a workgroup, sixteen runs of parts
+__global__ __launch_bounds__(1024) void norm_join_kernel(const float *sums, int64_t parts,
+                                                         int64_t k, void *dW, void *db, int dtype)
+{
+    void *out = blockIdx.y ? db : dW;
+    if (!out)
+        return;
+    const int lane = threadIdx.x & 63, run = threadIdx.x >> 6;
+    const int64_t col = (int64_t)blockIdx.x * 64 + lane;
+    double t = 0.0;
+    if (col < k) {
+#pragma unroll 8
+        for (int64_t p = run; p < parts; p += 16)
+            t += (double)sums[(p * 2 + blockIdx.y) * k + col];
+    }
+    __shared__ double all[16][64];
+    all[run][lane] = t;
+    __syncthreads();
+    if (run == 0 && col < k) {
+        for (int i = 1; i < 16; ++i)
+            t += all[i][lane];
+        store1(out, col, (float)t, dtype);
+    }
+}
+
+// ------------------------------------------------------------------- host
+constexpr int64_t kMostBlocks = 1 << 20;
+
+unsigned capped(int64_t blocks)
+{
+    return (unsigned)(blocks < 1 ? 1 : (blocks > kMostBlocks ? kMostBlocks : blocks));
+}
+
+// How the strips' rows are cut: about 2,048 workgroups, none of fewer than 16
+// rows.
+struct Strips {
+    int64_t strips, each, parts;
+    explicit Strips(const Norm &p)
+    {
+        strips = (p.k + 511) / 512;
+        int64_t want = 2048 / strips;
+        want = want < (p.n + 15) / 16 ? want : (p.n + 15) / 16;
+        want = want < 1 ? 1 : want;
+        each = (p.n + want - 1) / want;
+        parts = each ? (p.n + each - 1) / each : 0;
+    }
+};
+
+struct Backward {
+    float *dots, *sums;
+    Backward(const Norm &p, Cursor &c)
+    {
+        const Strips s(p);
+        dots = static_cast<float *>(c.take((size_t)p.n * 8));
+        sums = static_cast<float *>(c.take((size_t)s.parts * 2 * p.k * 4));
+    }
+};
+
+template <int DT>
+hipError_t launch_norm(const NormArgs &a, hipStream_t st)
+{
+    // lanes that hold a row in registers, more of them where rows are few
+    int lanes = a.k <= 512 ? 16 : (a.k <= 2048 ? 64 : (a.k <= 8192 ? 256 : 1024));
+    if (lanes == 16 && a.n < 4096 && a.k > 128)
+        lanes = 64;
+    if (lanes == 64 && a.n < 1024 && a.k > 512)
+        lanes = 256;
+    const int rows = lanes > 256 ? 1 : 256 / lanes;
+    const unsigned blocks = capped((a.n + rows - 1) / rows);
+    if (lanes == 16)
+        norm_kernel<DT, 16><<<blocks, 256, 0, st>>>(a);
+    else if (lanes == 64)
+        norm_kernel<DT, 64><<<blocks, 256, 0, st>>>(a);
+    else if (lanes == 256)
+        norm_kernel<DT, 256><<<blocks, 256, 0, st>>>(a);
+    else
+        norm_kernel<DT, 1024><<<blocks, 1024, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+template <int DT>
+hipError_t launch_gradients(const NormGradArgs &a, int64_t parts, hipStream_t st)
+{
+    if (a.dX) {
+        if (a.k <= 512)
+            norm_dots_kernel<DT, 16><<<capped((a.n + 15) / 16), 256, 0, st>>>(a);
+        else if (a.k <= 4096)
+            norm_dots_kernel<DT, 64><<<capped((a.n + 3) / 4), 256, 0, st>>>(a);
+        else
+            norm_dots_kernel<DT, 256><<<capped(a.n), 256, 0, st>>>(a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess)
+            return e;
+    }
+    norm_strip_kernel<DT><<<(unsigned)(parts * a.strips), 256, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+} // namespace
+
+size_t norm_ws(const Norm &p)
+{
+    Cursor c{nullptr};
+    Backward b(p, c);
+    return c.at;
+}
+
+hipError_t run_norm(const Norm &p, const void *X, const void *w, const void *b, void *Y,
+                    float *stats, hipStream_t st)
+{
+    if (p.n == 0)
+        return hipSuccess;
+    const NormArgs a{X, w, b, Y, stats, p.n, p.k, p.ldx, p.ldy, p.eps};
+    return p.dtype == GPIC_F32    ? launch_norm<GPIC_F32>(a, st)
+           : p.dtype == GPIC_F16 ? launch_norm<GPIC_F16>(a, st)
+                                 : launch_norm<GPIC_BF16>(a, st);
+}
+
+hipError_t run_norm_backward(const Norm &p, const void *dY, const void *X, const void *w,
+                             const float *stats, void *dX, void *dW, void *db, void *ws,
+                             hipStream_t st)
+{
+    Cursor c{static_cast<char *>(ws)};
+    const Backward b(p, c);
+    const Strips s(p);
+    if (p.n > 0 && (dX || dW || db)) {
+        const NormGradArgs a{dY, X, w, stats, dX, b.dots, dW || db ? b.sums : nullptr, p.n, p.k,
+                             p.ldx, p.ldy, s.strips, s.each};
+        const hipError_t e = p.dtype == GPIC_F32    ? launch_gradients<GPIC_F32>(a, s.parts, st)
+                             : p.dtype == GPIC_F16 ? launch_gradients<GPIC_F16>(a, s.parts, st)
+                                                   : launch_gradients<GPIC_BF16>(a, s.parts, st);
+        if (e != hipSuccess)
+            return e;
+    }
+    if (dW || db) {
+        norm_join_kernel<<<dim3((unsigned)((p.k + 63) / 64), 2), 1024, 0, st>>>(
+            b.sums, s.parts, p.k, dW, db, p.dtype);
+        return hipGetLastError();
+    }
+    return hipSuccess;
+}
+
+} // namespace gpic

@@ -218,51 +218,6 @@ __device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 c)
 // A wave's accumulators go through LDS (its own piece, no barrier) so that
 // a lane finishes eight consecutive columns of a row: 16-byte loads and
 // stores that cover whole lines.
-// Eight values p[i .. i + 7], of which `valid` exist, at any alignment (the
-// card's 16-byte accesses need none; where a row starts on 16 bytes they
-// cover whole lines).
-using f32x8_any = float __attribute__((ext_vector_type(8), aligned(4)));
-using half8_any = _Float16 __attribute__((ext_vector_type(8), aligned(2)));
-using bfrag8_any = __bf16 __attribute__((ext_vector_type(8), aligned(2)));
-
-__device__ __forceinline__ f32x8 load8(const void *p, int64_t i, int dtype, int valid)
-{
-    if (valid >= 8) {
-        if (dtype == GPIC_F32)
-            return *reinterpret_cast<const f32x8_any *>(static_cast<const float *>(p) + i);
-        if (dtype == GPIC_F16)
-            return __builtin_convertvector(
-                *reinterpret_cast<const half8_any *>(static_cast<const _Float16 *>(p) + i), f32x8);
-        return __builtin_convertvector(
-            *reinterpret_cast<const bfrag8_any *>(static_cast<const __bf16 *>(p) + i), f32x8);
-    }
-    f32x8 v = 0.0f;
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-        if (j < valid)
-            v[j] = load1(p, i + j, dtype);
-    return v;
-}
-
-__device__ __forceinline__ void store8(void *p, int64_t i, f32x8 v, int dtype, int valid)
-{
-    if (valid >= 8) {
-        if (dtype == GPIC_F32)
-            *reinterpret_cast<f32x8_any *>(static_cast<float *>(p) + i) = v;
-        else if (dtype == GPIC_F16)
-            *reinterpret_cast<half8_any *>(static_cast<_Float16 *>(p) + i) =
-                __builtin_convertvector(v, half8);
-        else
-            *reinterpret_cast<bfrag8_any *>(static_cast<__bf16 *>(p) + i) =
-                __builtin_convertvector(v, bfrag8);
-        return;
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-        if (j < valid)
-            store1(p, i + j, v[j], dtype);
-}
-
 // 16-bit parts of iterates: of split operands one split matrix; of single
 // ones a matrix of high halves and, for X (kEpiUpdate, kEpiResult), one of low
 // halves beside it.

@@ -1,0 +1,46 @@
+// Internal declarations of what surrounds an encoder's layers in training
+// (layer norm, embedding table, dropout, cross entropy): host launchers.
+#pragma once
+
+#include "encoder.h"
+
+namespace gpic {
+
+// --------------------------------------------------------------- norm.hip
+struct Norm {
+    int64_t n, k, ldx, ldy;    // ldy: of Y (backward: of dY)
+    float eps;
+    int dtype;
+};
+size_t norm_ws(const Norm &p);             // of the backward pass
+hipError_t run_norm(const Norm &p, const void *X, const void *w, const void *b, void *Y,
+                    float *stats, hipStream_t st);
+hipError_t run_norm_backward(const Norm &p, const void *dY, const void *X, const void *w,
+                             const float *stats, void *dX, void *dW, void *db, void *ws,
+                             hipStream_t st);
+
+// ------------------------------------------------------------ dropout.hip
+struct Dropout {
+    int64_t n, m, ldx, ldr, ldy;
+    uint64_t seed, offset;
+    uint32_t limit;            // of 2^16: a value stays from here on
+    int dtype;
+};
+hipError_t run_dropout(const Dropout &p, const void *X, const void *R, const int64_t *step,
+                       void *Y, hipStream_t st);
+
+// ---------------------------------------------------------- embedding.hip
+struct Embedding {
+    int64_t n, k, rows, ldt, ldy;
+    float scale;
+    int dtype;
+    bool wide;                 // 64-bit ids
+    bool accumulate;
+};
+size_t embedding_ws(const Embedding &p);   // of the backward pass
+hipError_t run_embedding(const Embedding &p, const void *ids, const void *T, void *Y,
+                         hipStream_t st);
+hipError_t run_embedding_backward(const Embedding &p, const void *dY, const void *ids, void *dT,
+                                  void *ws, hipStream_t st);
+
+} // namespace gpic
