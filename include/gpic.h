@@ -667,6 +667,51 @@ gpic_status gpic_embedding_backward(const gpic_embedding_params *p, const void *
                                     const void *ids, void *dT, void *ws, size_t ws_bytes,
                                     void *stream);
 
+typedef struct gpic_loss_params {
+    int64_t n, k, v;     /* rows (0 .. 2^31 - 1), inputs, the vocabulary (1 .. 2^20
+                            each)                                                 */
+    int64_t ldx, ldw;    /* pitches of X [n x k] and W [v x k], up to 2^22        */
+    int32_t dtype;       /* GPIC_F32, GPIC_F16 or GPIC_BF16                       */
+    int32_t id_bytes;    /* of a target: 4 (int32) or 8 (int64)                   */
+    int32_t aligned16;   /* as gpic_layer_params, of X and W                      */
+    int32_t reserved;    /* must be 0                                             */
+} gpic_loss_params;
+
+/* Workspace bytes of gpic_cross_entropy (backward 0) or its gradients (1); 0 also
+ * for parameters that the call refuses. */
+size_t gpic_cross_entropy_workspace_bytes(int32_t backward, const gpic_loss_params *p);
+
+/* loss_i = lse_i - z_i,t(i) with the logits z = X W^T + bias and lse_i = log
+ * sum_v exp z_iv, natural logarithms; no logit is kept.  targets [n]; one outside
+ * 0 .. v - 1 (padding) gives loss 0 and no gradient.  loss and lse (nullable,
+ * which the gradients need) are float32 [n].  bias [v] nullable; a bias of
+ * -infinity takes an entry out.  A small loss keeps its digits (it is summed from
+ * the other entries).  A row with a NaN or a logit of +infinity gives NaN, and so
+ * does one whose entries are all out; a target whose logit is -infinity gives
+ * +infinity.  n = 0 does nothing.
+ * ws: gpic_cross_entropy_workspace_bytes(0, p): split or padded copies of operands
+ * that cannot be read as they lie, and 8 bytes for each row and tile (64 to 256
+ * columns; up to 32 rows and small calls: 16) of the vocabulary.
+ * Errors: INVALID_ARG, WORKSPACE, UNSUPPORTED. */
+gpic_status gpic_cross_entropy(const gpic_loss_params *p, const void *X, const void *W,
+                               const void *bias, const void *targets, float *loss, float *lse,
+                               void *ws, size_t ws_bytes, void *stream);
+
+/* Gradients of sum_i dloss_i loss_i: dZ = dloss (exp(z - lse) - [v = t]), dX
+ * [n x k] = dZ W, dW [v x k] = dZ^T X, db [v] = column sums of dZ.  dX, dW and db
+ * are contiguous, any may be null (not wanted).  loss and lse as
+ * gpic_cross_entropy gave them.  The logits are computed once more, in pieces of
+ * the vocabulary whose dZ takes about 256 MB, rounded to the matrices' type for
+ * the products (float16: times a power of two from the largest finite |dloss|;
+ * float32: 22 bits down to 2^-17 of the row's |dloss|, errors of 2^-39 of it
+ * below); db sums it unrounded.  With n = 0, dW and db are zeros.
+ * ws: gpic_cross_entropy_workspace_bytes(1, p). */
+gpic_status gpic_cross_entropy_backward(const gpic_loss_params *p, const float *dloss,
+                                        const void *X, const void *W, const void *bias,
+                                        const void *targets, const float *loss, const float *lse,
+                                        void *dX, void *dW, void *db, void *ws, size_t ws_bytes,
+                                        void *stream);
+
 #ifdef __cplusplus
 }
 #endif

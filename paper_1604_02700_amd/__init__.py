@@ -50,6 +50,7 @@ EXPORTS = (
     "gpic_muon_step", "gpic_layer_norm", "gpic_layer_norm_workspace_bytes",
     "gpic_layer_norm_backward", "gpic_dropout", "gpic_embedding",
     "gpic_embedding_workspace_bytes", "gpic_embedding_backward",
+    "gpic_cross_entropy_workspace_bytes", "gpic_cross_entropy", "gpic_cross_entropy_backward",
 )
 DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
@@ -114,6 +115,12 @@ class EmbeddingParams(C.Structure):
                 ("id_bytes", C.c_int32), ("accumulate", C.c_int32)]
 
 
+class LossParams(C.Structure):
+    _fields_ = [("n", C.c_int64), ("k", C.c_int64), ("v", C.c_int64), ("ldx", C.c_int64),
+                ("ldw", C.c_int64), ("dtype", C.c_int32), ("id_bytes", C.c_int32),
+                ("aligned16", C.c_int32), ("reserved", C.c_int32)]
+
+
 _lib = None
 
 
@@ -140,6 +147,8 @@ def lib() -> C.CDLL:
         L.gpic_layer_norm_workspace_bytes.argtypes = [C.POINTER(NormParams)]
         L.gpic_embedding_workspace_bytes.restype = sz
         L.gpic_embedding_workspace_bytes.argtypes = [C.POINTER(EmbeddingParams)]
+        L.gpic_cross_entropy_workspace_bytes.restype = sz
+        L.gpic_cross_entropy_workspace_bytes.argtypes = [i32, C.POINTER(LossParams)]
         L.gpic_sym_bytes.restype = sz
         L.gpic_sym_bytes.argtypes = [i64]
         sigs = {
@@ -184,6 +193,8 @@ def lib() -> C.CDLL:
             "gpic_dropout": [C.POINTER(DropoutParams), p, p, p, p, p],
             "gpic_embedding": [C.POINTER(EmbeddingParams), p, p, p, p],
             "gpic_embedding_backward": [C.POINTER(EmbeddingParams), p, p, p, p, sz, p],
+            "gpic_cross_entropy": [C.POINTER(LossParams)] + [p] * 7 + [sz, p],
+            "gpic_cross_entropy_backward": [C.POINTER(LossParams)] + [p] * 11 + [sz, p],
         }
         for name, args in sigs.items():
             fn = getattr(L, name)
@@ -1124,6 +1135,72 @@ def gpic_embedding_backward(dY: torch.Tensor, ids: torch.Tensor, rows: int, scal
     if given is not None:
         _written(given)
     return dT
+
+
+def _row_floats(t, n, device, name):
+    """A contiguous float32 [n] on `device`."""
+    _dev(t, torch.float32, name)
+    if t.shape != (n,) or t.device != device:
+        raise ValueError(f"{name} must be [{n}] on {device}")
+    return t.contiguous()
+
+
+def _loss(backward, X, W, targets):
+    """LossParams for these tensors and a workspace."""
+    n, k = X.shape
+    v = W.shape[0]
+    p = LossParams(n, k, v, _pitch(X, n, k), _pitch(W, v, k), DTYPES[X.dtype],
+                   targets.element_size(), int((X.data_ptr() | W.data_ptr()) % 16 == 0), 0)
+    ref = C.byref(p)
+    ws, nb = _workspace(lib().gpic_cross_entropy_workspace_bytes(backward, ref), X.device)
+    return ref, ws, nb
+
+
+def gpic_cross_entropy(X: torch.Tensor, W: torch.Tensor, targets: torch.Tensor,
+                       bias: Optional[torch.Tensor] = None, want_lse: bool = False):
+    """loss (float32 [n]) of the logits X W^T + bias for X [n, k], W [v, k]
+    (float32, float16 or bfloat16) and targets [n] (int32 or int64): the
+    logarithm of the sum of the logits' exponentials minus the target's logit.
+    The logits are never kept.  A target outside 0 .. v - 1 is padding: loss 0,
+    no gradient.  want_lse: returns (loss, lse), which
+    gpic_cross_entropy_backward reads."""
+    X = _layer_type(X)
+    W = _weights(X, W, False)
+    n = X.shape[0]
+    targets = _ids(targets, n, X.device, "targets")
+    bias = _columns(bias, W.shape[0], X, "bias")
+    loss = torch.empty(n, dtype=torch.float32, device=X.device)
+    lse = torch.empty(n, dtype=torch.float32, device=X.device) if want_lse else None
+    _no_graph("X W bias", X, W, bias)
+    ref, ws, nb = _loss(0, X, W, targets)
+    _run(lib().gpic_cross_entropy, X.device, ref, _at(X), _at(W), _at(bias), _at(targets),
+         _at(loss), _at(lse), _at(ws), nb)
+    return (loss, lse) if want_lse else loss
+
+
+def gpic_cross_entropy_backward(dloss: torch.Tensor, X: torch.Tensor, W: torch.Tensor,
+                                targets: torch.Tensor, loss: torch.Tensor, lse: torch.Tensor,
+                                bias: Optional[torch.Tensor] = None, want_x: bool = True,
+                                want_w: bool = True, want_bias: bool = True) -> LayerGrads:
+    """Gradients of sum(dloss * gpic_cross_entropy(...)): dX, dW and db (those
+    wanted).  dloss float32 [n] (1 / n of the mean, say); loss and lse as
+    gpic_cross_entropy gave them.  The vocabulary goes by in pieces, whose
+    logits are computed once more."""
+    X = _layer_type(X)
+    W = _weights(X, W, False)
+    (n, k), v, dev = X.shape, W.shape[0], X.device
+    targets = _ids(targets, n, dev, "targets")
+    bias = _columns(bias, v, X, "bias")
+    dloss, loss, lse = (_row_floats(t, n, dev, name) for t, name in
+                        ((dloss, "dloss"), (loss, "loss"), (lse, "lse")))
+    dX = torch.empty((n, k), dtype=X.dtype, device=dev) if want_x else None
+    dW = torch.empty((v, k), dtype=X.dtype, device=dev) if want_w else None
+    db = torch.empty(v, dtype=X.dtype, device=dev) if want_bias else None
+    _no_graph("dloss X W loss lse bias", dloss, X, W, loss, lse, bias)
+    ref, ws, nb = _loss(1, X, W, targets)
+    _run(lib().gpic_cross_entropy_backward, dev, ref, _at(dloss), _at(X), _at(W), _at(bias),
+         _at(targets), _at(loss), _at(lse), _at(dX), _at(dW), _at(db), _at(ws), nb)
+    return LayerGrads(dX, dW, db)
 
 
 # ----------------------------------------------- whole paths (call chains)

@@ -1,6 +1,6 @@
 // C entry points of what surrounds an encoder's layers in training: argument
-// checks on the host, then the launchers of norm.hip, dropout.hip and
-// embedding.hip.
+// checks on the host, then the launchers of norm.hip, dropout.hip, embedding.hip
+// and loss.hip.
 #include <math.h>
 
 #include "extents.h"
@@ -94,6 +94,34 @@ gpic_status check_ids(const void *ids, const char *name, int32_t bytes, bool nul
     CHECK_ARG(ids != nullptr || nullable, "%s is null", name);
     CHECK_ARG(aligned(ids, bytes), "%s is misaligned", name);
     return GPIC_OK;
+}
+
+Loss loss_of(const gpic_loss_params *p)
+{
+    return Loss{p->n,   p->k,     p->v,             p->ldx,
+                p->ldw, p->dtype, p->id_bytes == 8, p->aligned16 != 0};
+}
+
+gpic_status check_loss(const gpic_loss_params *p, bool backward)
+{
+    CHECK_ARG(p != nullptr, "params is null");
+    CHECK(check_sides(p->n, p->k, "k", p->dtype));
+    CHECK_ARG(p->v >= 1 && p->v <= kMaxSide, "v = %lld out of range [1, 2^20]", (long long)p->v);
+    CHECK(check_pitch(p->ldx, p->k, "ldx"));
+    CHECK(check_pitch(p->ldw, p->k, "ldw"));
+    CHECK_ARG(p->id_bytes == 4 || p->id_bytes == 8, "id_bytes must be 4 or 8");
+    CHECK_ARG(p->aligned16 == 0 || p->aligned16 == 1, "aligned16 must be 0 or 1");
+    CHECK_ARG(p->reserved == 0, "reserved must be 0");
+    if (!loss_fits(loss_of(p), backward))
+        return fail(GPIC_ERR_UNSUPPORTED, "n = %lld, k = %lld, v = %lld: a product of more "
+                    "workgroups than a launch takes", (long long)p->n, (long long)p->k,
+                    (long long)p->v);
+    return GPIC_OK;
+}
+
+gpic_status check_floats(const float *x, const char *name, bool nullable)
+{
+    return check_matrix(x, name, GPIC_F32, nullable);
 }
 
 } // namespace
@@ -214,6 +242,70 @@ gpic_status gpic_embedding_backward(const gpic_embedding_params *p, const void *
     CHECK(check_apart(&out, 1, in, 2));
     CHECK_HIP(run_embedding_backward(embedding_of(p), dY, ids, dT, ws, (hipStream_t)stream),
               "embedding backward");
+    return GPIC_OK;
+}
+
+size_t gpic_cross_entropy_workspace_bytes(int32_t backward, const gpic_loss_params *p)
+{
+    if (backward != 0 && backward != 1)
+        return 0;
+    return check_loss(p, backward != 0) == GPIC_OK ? loss_ws(loss_of(p), backward != 0) : 0;
+}
+
+gpic_status gpic_cross_entropy(const gpic_loss_params *p, const void *X, const void *W,
+                               const void *bias, const void *targets, float *loss, float *lse,
+                               void *ws, size_t ws_bytes, void *stream)
+{
+    CHECK(check_loss(p, false));
+    const bool empty = p->n == 0, a16 = p->aligned16 != 0;
+    CHECK(check_matrix(X, "X", p->dtype, empty, a16));
+    CHECK(check_matrix(W, "W", p->dtype, false, a16));
+    CHECK(check_matrix(bias, "bias", p->dtype, true));
+    CHECK(check_ids(targets, "targets", p->id_bytes, empty));
+    CHECK(check_floats(loss, "loss", empty));
+    CHECK(check_floats(lse, "lse", true));
+    CHECK(check_ws(ws, ws_bytes, loss_ws(loss_of(p), false)));
+    const size_t e = size_of(p->dtype);
+    const Extent out[] = {packed("loss", loss, p->n, 4), packed("lse", lse, p->n, 4)};
+    const Extent in[] = {matrix("X", X, p->n, p->k, p->ldx, e),
+                         matrix("W", W, p->v, p->k, p->ldw, e), packed("bias", bias, p->v, e),
+                         packed("targets", targets, p->n, p->id_bytes)};
+    CHECK(check_apart(out, 2, in, 4));
+    CHECK_HIP(run_loss(loss_of(p), X, W, bias, targets, loss, lse, ws, (hipStream_t)stream),
+              "cross entropy");
+    return GPIC_OK;
+}
+
+gpic_status gpic_cross_entropy_backward(const gpic_loss_params *p, const float *dloss,
+                                        const void *X, const void *W, const void *bias,
+                                        const void *targets, const float *loss, const float *lse,
+                                        void *dX, void *dW, void *db, void *ws, size_t ws_bytes,
+                                        void *stream)
+{
+    CHECK(check_loss(p, true));
+    const bool empty = p->n == 0, a16 = p->aligned16 != 0;
+    CHECK(check_floats(dloss, "dloss", empty));
+    CHECK(check_matrix(X, "X", p->dtype, empty, a16));
+    CHECK(check_matrix(W, "W", p->dtype, empty, a16));
+    CHECK(check_matrix(bias, "bias", p->dtype, true));
+    CHECK(check_ids(targets, "targets", p->id_bytes, empty));
+    CHECK(check_floats(loss, "loss", empty));
+    CHECK(check_floats(lse, "lse", empty));
+    CHECK(check_matrix(dX, "dX", p->dtype, true));
+    CHECK(check_matrix(dW, "dW", p->dtype, true));
+    CHECK(check_matrix(db, "db", p->dtype, true));
+    CHECK(check_ws(ws, ws_bytes, loss_ws(loss_of(p), true)));
+    const size_t e = size_of(p->dtype);
+    const Extent out[] = {packed("dX", dX, p->n * p->k, e), packed("dW", dW, p->v * p->k, e),
+                          packed("db", db, p->v, e)};
+    const Extent in[] = {packed("dloss", dloss, p->n, 4), matrix("X", X, p->n, p->k, p->ldx, e),
+                         matrix("W", W, p->v, p->k, p->ldw, e), packed("bias", bias, p->v, e),
+                         packed("targets", targets, p->n, p->id_bytes),
+                         packed("loss", loss, p->n, 4), packed("lse", lse, p->n, 4)};
+    CHECK(check_apart(out, 3, in, 7));
+    CHECK_HIP(run_loss_backward(loss_of(p), dloss, X, W, bias, targets, loss, lse, dX, dW, db, ws,
+                                (hipStream_t)stream),
+              "cross entropy backward");
     return GPIC_OK;
 }
 

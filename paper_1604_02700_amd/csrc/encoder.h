@@ -273,9 +273,30 @@ struct Operand {
 
 // kEpiGram: P = acc; kEpiPoly: P = beta C + acc, both over the upper triangle
 // of tiles and mirrored, C and P symmetric; kEpiUpdate: X' = beta X + acc;
-// kEpiResult: the same as a result (or, is_step, weights moved by it)
-enum { kEpiLayer = 0, kEpiGated = 1, kEpiGram = 2, kEpiPoly = 3, kEpiUpdate = 4, kEpiResult = 5 };
+// kEpiResult: the same as a result (or, is_step, weights moved by it);
+// kEpiLse: logits z = acc + bias, of which each row's largest and sum of
+// exponentials over the tile's columns are kept (but the target's, which is
+// kept itself); kEpiSoft: the logits' gradients g (exp(z - lse) - [target]) as
+// an operand of further products; kEpiSum: acc added to float32 sums
+enum {
+    kEpiLayer = 0, kEpiGated = 1, kEpiGram = 2, kEpiPoly = 3, kEpiUpdate = 4, kEpiResult = 5,
+    kEpiLse = 6, kEpiSoft = 7, kEpiSum = 8
+};
 __host__ __device__ constexpr bool symmetric(int epi) { return epi == kEpiGram || epi == kEpiPoly; }
+// whose operands may be under powers of two
+__host__ __device__ constexpr bool powered(int epi)
+{
+    return epi == kEpiLayer || epi == kEpiGated || epi >= kEpiLse;
+}
+// whose tiles are not cut along the contraction
+__host__ __device__ constexpr bool uncut(int epi) { return epi == kEpiLse || epi == kEpiSoft; }
+
+// What kEpiSoft knows of a row.
+struct LossRow {
+    float lse, g;      // g: the loss's gradient
+    float picked;      // the gradient of the target's logit
+    int target;        // its column; -1: none, no gradient
+};
 
 struct Epilogue {
     // layers: the powers of two that the operands were multiplied by, their
@@ -302,6 +323,23 @@ struct Epilogue {
     int is_step;
     float decay, step;
     int64_t batch_o;
+    // kEpiLse: targets (32 or 64 bits), [tiles across][M] largest logit and
+    // sum of exponentials, [M] target's logit
+    const void *targets;
+    int wide;
+    float2 *strip;
+    float *picked;
+    // kEpiSoft: rows, the column that the piece starts at, the powers of two
+    // that dZ (p_hi, ldp) is stored under (one for all rows: power_step 0),
+    // [row blocks][N] column sums of dZ or null
+    const LossRow *rows;
+    int64_t first;
+    const int *power;
+    int power_step;
+    float *sums;
+    // kEpiSum: float32 sums so far (of pitch ldr, in res) or null; out is
+    // float32, or (last) of the operands' type
+    int last;
 };
 
 struct ProductArgs {
@@ -337,6 +375,60 @@ hipError_t launch_product(int modes, int op, int epi, const ProductArgs &a, hipS
 hipError_t launch_product_kk(int op, int epi, const Plan &p, const ProductArgs &a, hipStream_t s);
 hipError_t launch_product_km(int op, int epi, const Plan &p, const ProductArgs &a, hipStream_t s);
 hipError_t launch_product_mm(int op, int epi, const Plan &p, const ProductArgs &a, hipStream_t s);
+hipError_t launch_product_loss(int op, int epi, const Plan &p, const ProductArgs &a,
+                               hipStream_t s);
+
+// ---------------------------------------------------- operands' copies (layers.hip)
+inline int kind_of(int dtype)
+{
+    return dtype == GPIC_F32 ? kOpSplit : (dtype == GPIC_F16 ? kOpF16 : kOpBf16);
+}
+
+// A matrix that a product reads: as it lies where it can, else a packed
+// copy in the workspace.
+struct Source {
+    const void *x;
+    int64_t rows, cols, ld;
+    bool pack;
+    void *to = nullptr;
+    int *power = nullptr;  // float32: of its rows (backward: columns)
+    const int *row = nullptr;  // float32 backward: packed over two to this, by row
+    Operand operand(int dtype) const
+    {
+        if (!pack)
+            return Operand{x, ld, 0, cols};
+        const int64_t p = dtype == GPIC_F32 ? split_ld(cols) : up64(cols);
+        return Operand{to, p, 0, p};
+    }
+};
+
+// 16-bit matrices are read as they lie when rows start on 16 bytes and
+// hold whole chunks of 8 values; float32 ones are always split.  `aligned16`:
+// every matrix starts on 16 bytes.
+inline bool must_pack(int dtype, int64_t cols, int64_t ld, bool aligned16)
+{
+    return dtype == GPIC_F32 || !aligned16 || cols % 8 || ld % 8;
+}
+
+// `powers`: how many powers of two the copy has (float32)
+inline void place(Source &s, int dtype, Cursor &c, int64_t powers)
+{
+    if (!s.pack)
+        return;
+    const int64_t p = dtype == GPIC_F32 ? split_ld(s.cols) : up64(s.cols);
+    s.to = c.take((size_t)s.rows * p * 2);
+    if (dtype == GPIC_F32)
+        s.power = static_cast<int *>(c.take((size_t)powers * 4));
+}
+
+// X and W of a float32 layer, split under a power of two for every row
+hipError_t launch_split_rows(const Source &x, const Source &w, hipStream_t st);
+// copies of up to three operands (those to be packed); float32: split under a
+// power of two for every column
+hipError_t launch_pack(const Source *const *list, int count, int dtype, hipStream_t st);
+// db [m] = sums of `parts` partial column sums [parts][m]
+hipError_t launch_sum_parts(const float *sums, int64_t parts, int64_t m, void *db, int dtype,
+                            hipStream_t st);
 
 // ------------------------------------------------------------- layers.hip
 struct Shape {         // a layer: n rows, k inputs, m outputs

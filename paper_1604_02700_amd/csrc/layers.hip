@@ -41,6 +41,7 @@ struct PackJob {
     int64_t rows, cols, ld;
     void *to;              // split matrix (float32) or rows of up64(cols)
     const int *power;      // float32: of every column
+    const int *row;        // float32: over two to this, of every row (or null)
 };
 struct PackJobs {
     PackJob j[3];
@@ -66,6 +67,7 @@ __global__ __launch_bounds__(256) void pack_kernel(PackJobs jobs)
             const float *x = static_cast<const float *>(m.x) + r * m.ld + c;
             float v[8];
             int power[8];
+            const int over = m.row ? m.row[r] : 0;
             if (c + 8 <= m.cols) {
                 const f32x4 a = load4(x, 0, GPIC_F32), b = load4(x, 4, GPIC_F32);
 #pragma unroll
@@ -87,7 +89,7 @@ __global__ __launch_bounds__(256) void pack_kernel(PackJobs jobs)
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 _Float16 a, b;
-                split2(ldexpf(v[k], power[k]), a, b);
+                split2(ldexpf(v[k], power[k] - over), a, b);
                 h[k] = a;
                 l[k] = b;
             }
@@ -626,95 +628,6 @@ unsigned blocks_for(int64_t items)
     return (unsigned)(b < 1 ? 1 : (b > 4096 ? 4096 : b));
 }
 
-// A matrix that a product reads: as it lies where it can, else a packed
-// copy in the workspace.
-struct Source {
-    const void *x;
-    int64_t rows, cols, ld;
-    bool pack;
-    void *to = nullptr;
-    int *power = nullptr;  // float32: of its rows (backward: columns)
-    Operand operand(int dtype) const
-    {
-        if (!pack)
-            return Operand{x, ld, 0, cols};
-        const int64_t p = dtype == GPIC_F32 ? split_ld(cols) : up64(cols);
-        return Operand{to, p, 0, p};
-    }
-};
-
-// 16-bit matrices are read as they lie when rows start on 16 bytes and
-// hold whole chunks of 8 values; float32 ones are always split.  `aligned16`:
-// every matrix starts on 16 bytes.
-bool must_pack(int dtype, int64_t cols, int64_t ld, bool aligned16)
-{
-    return dtype == GPIC_F32 || !aligned16 || cols % 8 || ld % 8;
-}
-
-// `powers`: how many powers of two the copy has (float32)
-void place(Source &s, int dtype, Cursor &c, int64_t powers)
-{
-    if (!s.pack)
-        return;
-    const int64_t p = dtype == GPIC_F32 ? split_ld(s.cols) : up64(s.cols);
-    s.to = c.take((size_t)s.rows * p * 2);
-    if (dtype == GPIC_F32)
-        s.power = static_cast<int *>(c.take((size_t)powers * 4));
-}
-
-// X and W of a float32 layer, a power of two for every row
-hipError_t launch_split_rows(const Source &x, const Source &w, hipStream_t st)
-{
-    RowJobs j{};
-    const Source *list[2] = {&x, &w};
-    for (int i = 0; i < 2; ++i)
-        j.j[i] = RowJob{static_cast<const float *>(list[i]->x), list[i]->rows, list[i]->cols,
-                        list[i]->ld, static_cast<_Float16 *>(list[i]->to), list[i]->power};
-    const int64_t rows = x.rows > w.rows ? x.rows : w.rows;
-    // Few lanes a row keep all of them at work and more loads in flight.  us, X's
-    // rows by 8, 32, 64 and 256 lanes: 50,000 x 72 13, 24, 42 and 130; 20,000 x 256
-    // 14, 15, 20, 54; 10,000 x 512 12, 15, 16, 31; 10,007 x 1,000 25, 14, 17, 30;
-    // 10,007 x 2,000 42, 32, 27, 32; 3,200 x 3,000 48, 19, 17, 17; 3,200 x 4,096 58,
-    // 26, 23, 20.  Few rows by 64 lanes fill the card better (1,400 x 300 5.4 for
-    // 6.8 by 8).
-    int lanes = x.cols <= 512 ? 8 : (x.cols <= 1024 ? 32 : (x.cols <= 3000 ? 64 : 256));
-    lanes = rows * lanes < 65536 && lanes < 64 ? 64 : lanes;
-    int64_t blocks = (rows * lanes + 255) / 256;
-    blocks = blocks > (1 << 20) ? 1 << 20 : blocks;
-    const dim3 grid((unsigned)blocks, 2);
-    if (lanes == 8)
-        split_rows_kernel<8><<<grid, 256, 0, st>>>(j);
-    else if (lanes == 32)
-        split_rows_kernel<32><<<grid, 256, 0, st>>>(j);
-    else if (lanes == 64)
-        split_rows_kernel<64><<<grid, 256, 0, st>>>(j);
-    else
-        split_rows_kernel<256><<<grid, 256, 0, st>>>(j);
-    return hipGetLastError();
-}
-
-hipError_t launch_pack(const Source *const *list, int count, int dtype, hipStream_t st)
-{
-    PackJobs j{};
-    int used = 0;
-    int64_t most = 0;
-    for (int i = 0; i < count; ++i)
-        if (list[i]->pack && list[i]->rows > 0) {
-            const Source &s = *list[i];
-            j.j[used++] = PackJob{s.x, s.rows, s.cols, s.ld, s.to, s.power};
-            const int64_t groups = s.rows * ((s.cols + 63) / 64 * 8);
-            most = groups > most ? groups : most;
-        }
-    if (used == 0)
-        return hipSuccess;
-    const dim3 grid(blocks_for(most), (unsigned)used);
-    if (dtype == GPIC_F32)
-        pack_kernel<true><<<grid, 256, 0, st>>>(j);
-    else
-        pack_kernel<false><<<grid, 256, 0, st>>>(j);
-    return hipGetLastError();
-}
-
 template <int DT, bool GATED>
 hipError_t launch_grad_act(const GradArgs &g, dim3 grid, hipStream_t st)
 {
@@ -738,11 +651,6 @@ template <int DT>
 hipError_t launch_grad(const GradArgs &g, bool gated, dim3 grid, hipStream_t st)
 {
     return gated ? launch_grad_act<DT, true>(g, grid, st) : launch_grad_act<DT, false>(g, grid, st);
-}
-
-int kind_of(int dtype)
-{
-    return dtype == GPIC_F32 ? kOpSplit : (dtype == GPIC_F16 ? kOpF16 : kOpBf16);
 }
 
 // What a forward call keeps in its workspace.
@@ -919,6 +827,66 @@ hipError_t launch_powers(const Shape &s, bool gated, const Backward &b, const vo
 
 } // namespace
 
+// X and W of a float32 layer, a power of two for every row
+hipError_t launch_split_rows(const Source &x, const Source &w, hipStream_t st)
+{
+    RowJobs j{};
+    const Source *list[2] = {&x, &w};
+    for (int i = 0; i < 2; ++i)
+        j.j[i] = RowJob{static_cast<const float *>(list[i]->x), list[i]->rows, list[i]->cols,
+                        list[i]->ld, static_cast<_Float16 *>(list[i]->to), list[i]->power};
+    const int64_t rows = x.rows > w.rows ? x.rows : w.rows;
+    // Few lanes a row keep all of them at work and more loads in flight.  us, X's
+    // rows by 8, 32, 64 and 256 lanes: 50,000 x 72 13, 24, 42 and 130; 20,000 x 256
+    // 14, 15, 20, 54; 10,000 x 512 12, 15, 16, 31; 10,007 x 1,000 25, 14, 17, 30;
+    // 10,007 x 2,000 42, 32, 27, 32; 3,200 x 3,000 48, 19, 17, 17; 3,200 x 4,096 58,
+    // 26, 23, 20.  Few rows by 64 lanes fill the card better (1,400 x 300 5.4 for
+    // 6.8 by 8).
+    int lanes = x.cols <= 512 ? 8 : (x.cols <= 1024 ? 32 : (x.cols <= 3000 ? 64 : 256));
+    lanes = rows * lanes < 65536 && lanes < 64 ? 64 : lanes;
+    int64_t blocks = (rows * lanes + 255) / 256;
+    blocks = blocks > (1 << 20) ? 1 << 20 : blocks;
+    const dim3 grid((unsigned)blocks, 2);
+    if (lanes == 8)
+        split_rows_kernel<8><<<grid, 256, 0, st>>>(j);
+    else if (lanes == 32)
+        split_rows_kernel<32><<<grid, 256, 0, st>>>(j);
+    else if (lanes == 64)
+        split_rows_kernel<64><<<grid, 256, 0, st>>>(j);
+    else
+        split_rows_kernel<256><<<grid, 256, 0, st>>>(j);
+    return hipGetLastError();
+}
+
+hipError_t launch_pack(const Source *const *list, int count, int dtype, hipStream_t st)
+{
+    PackJobs j{};
+    int used = 0;
+    int64_t most = 0;
+    for (int i = 0; i < count; ++i)
+        if (list[i]->pack && list[i]->rows > 0) {
+            const Source &s = *list[i];
+            j.j[used++] = PackJob{s.x, s.rows, s.cols, s.ld, s.to, s.power, s.row};
+            const int64_t groups = s.rows * ((s.cols + 63) / 64 * 8);
+            most = groups > most ? groups : most;
+        }
+    if (used == 0)
+        return hipSuccess;
+    const dim3 grid(blocks_for(most), (unsigned)used);
+    if (dtype == GPIC_F32)
+        pack_kernel<true><<<grid, 256, 0, st>>>(j);
+    else
+        pack_kernel<false><<<grid, 256, 0, st>>>(j);
+    return hipGetLastError();
+}
+
+hipError_t launch_sum_parts(const float *sums, int64_t parts, int64_t m, void *db, int dtype,
+                            hipStream_t st)
+{
+    sum_parts_kernel<<<(unsigned)((m + 63) / 64), 1024, 0, st>>>(sums, parts, m, db, dtype);
+    return hipGetLastError();
+}
+
 size_t layer_ws(const Shape &s, bool gated, bool backward)
 {
     Cursor c{nullptr};
@@ -1033,9 +1001,8 @@ hipError_t run_layer_backward(const Shape &s, bool gated, const void *dY, const 
                                   : launch_grad<GPIC_BF16>(g, gated, grid, st));
     }
     if (db) {
-        sum_parts_kernel<<<(unsigned)((s.m + 63) / 64), 1024, 0, st>>>(
-            b.sums, (s.n + b.rows_each - 1) / b.rows_each, s.m, db, s.dtype);
-        RUN(hipGetLastError());
+        RUN(launch_sum_parts(b.sums, (s.n + b.rows_each - 1) / b.rows_each, s.m, db, s.dtype,
+                             st));
     }
     ProductArgs a{};
     a.batch = 1;

@@ -1,0 +1,676 @@
+// Cross entropy over a vocabulary whose logits are never kept: z = X W^T + b,
+//   loss_i = log sum_v exp z_iv - z_i,t(i),
+//   dZ = g_i (exp(z - lse_i) - [v = t(i)]), dX = dZ W, dW = dZ^T X, db = column sums.
+//
+// Forward, a tile of logits leaves only each row's largest and sum of
+// exponentials (product.h, kEpiLse), the target's logit set aside: from the
+// others' lse' = log sum_{v != t} exp z_v the loss is softplus(lse' - z_t),
+// which keeps its digits where the target's probability is near one, and the
+// gradient of the target's logit is g (exp(-loss) - 1).  Backward, the
+// vocabulary goes by in pieces: the piece's logits once more, their gradients
+// into one buffer (product.h, kEpiSoft), from there into the sum dX and into
+// the piece's rows of dW.
+//
+// Few rows, or little work, read W once as it lies (few_lse_kernel).
+//
+// float32 operands are split halves (encoder.h).  A row of dZ is at most |g_i|,
+// and is stored under that bound's power of two, for both products: dX takes
+// it off, and dW = sum_i (dZ_i 2^p_i) (x_i 2^-p_i) takes X over the same powers,
+// under its own by column.  float16's dZ is under one power, from the largest
+// |g|.
+#include <type_traits>
+
+#include "row_chunks.h"
+#include "training.h"
+
+namespace gpic {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+__device__ __forceinline__ float2 merge(float2 a, float2 b)
+{
+    const float m = fmaxf(a.x, b.x), at = m == -INFINITY ? 0.0f : m;
+    return make_float2(m, a.y * __builtin_amdgcn_exp2f((a.x - at) * kLog2e) +
+                              b.y * __builtin_amdgcn_exp2f((b.x - at) * kLog2e));
+}
+
+__device__ __forceinline__ int64_t target_at(const void *t, int wide, int64_t row)
+{
+    return wide ? static_cast<const int64_t *>(t)[row]
+                : (int64_t)static_cast<const int32_t *>(t)[row];
+}
+
+// ------------------------------------------------------------- few rows
+struct FewArgs {
+    const void *X, *W, *bias, *targets;
+    float2 *strip;             // [blocks of 16 columns][n]
+    float *picked;
+    int64_t ldx, ldw, n, k, v;
+    int wide;
+};
+
+// The logits of 16 columns and up to 16 NB rows a workgroup, whose waves share
+// the contraction in turns.
+template <int DT, int NB, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void few_lse_kernel(FewArgs a)
+{
+    constexpr int kValues = DT == GPIC_F32 ? 4 : 8;       // of k a lane loads at once
+    constexpr int kSize = DT == GPIC_F32 ? 4 : 2;
+    constexpr int kUnroll = 4, kTurn = 4 * kValues * kUnroll;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, r = lane & 15;
+    const int64_t col0 = (int64_t)blockIdx.x * 16, row0 = (int64_t)blockIdx.y * (16 * NB);
+    // rows beyond the last are read as the last one and not kept
+    const int64_t wrow = col0 + r < a.v ? col0 + r : a.v - 1;
+    const char *w = static_cast<const char *>(a.W) + wrow * a.ldw * kSize;
+    const char *x[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        const int64_t row = row0 + b * 16 + r < a.n ? row0 + b * 16 + r : a.n - 1;
+        x[b] = static_cast<const char *>(a.X) + row * a.ldx * kSize;
+    }
+    f32x4 acc[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+        acc[b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    auto turn = [&](int64_t k0, auto last) {
+        constexpr bool kLast = decltype(last)::value;
+        u32x4 fw[kUnroll], fx[NB][kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int64_t k = k0 + u * 4 * kValues + g * kValues;
+            fw[u] = chunk_at<DT, kLast>(w, k, a.k);
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+                fx[b][u] = chunk_at<DT, kLast>(x[b], k, a.k);
+        }
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+                acc[b] = mma16<DT>(fw[u], fx[b][u], acc[b]);
+    };
+    int64_t k0 = (int64_t)wave * kTurn;
+#pragma unroll 2
+    for (; k0 + kTurn <= a.k; k0 += (int64_t)WAVES * kTurn)
+        turn(k0, std::false_type{});
+    if (k0 < a.k)                      // the turn that the contraction ends in
+        turn(k0, std::true_type{});
+    __shared__ f32x4 part[WAVES][NB][64];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+        part[wave][b][lane] = acc[b];
+    __syncthreads();
+    // wave b finishes rows 16 b .. 16 b + 15: a lane four columns of one row
+    if (wave >= NB)
+        return;
+    const int64_t row = row0 + wave * 16 + r;
+    f32x4 v = part[0][wave][lane];
+#pragma unroll
+    for (int s = 1; s < WAVES; ++s)
+        v += part[s][wave][lane];
+    const bool live = row < a.n;
+    const int64_t t = live ? target_at(a.targets, a.wide, row) : -1;
+    float m = -INFINITY, s = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int64_t col = col0 + g * 4 + j;
+        float z = -INFINITY;
+        if (col < a.v) {
+            const float bias = a.bias ? load1(a.bias, col, DT) : 0.0f;
+            z = bias == -INFINITY ? bias : v[j] + bias;
+            if (col == t) {
+                a.picked[row] = z;
+                z = -INFINITY;
+            }
+        }
+        v[j] = z;
+        m = fmaxf(m, z);
+    }
+    m = fmaxf(m, __shfl_xor(m, 16, 64));
+    m = fmaxf(m, __shfl_xor(m, 32, 64));
+    const float at = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        s += __builtin_amdgcn_exp2f((v[j] - at) * kLog2e);
+    s += __shfl_xor(s, 16, 64);
+    s += __shfl_xor(s, 32, 64);
+    if (live && g == 0)
+        a.strip[(int64_t)blockIdx.x * a.n + row] = make_float2(m, s);
+}
+
+// ------------------------------------------------------------------ join
+struct JoinArgs {
+    const float2 *strip;       // [strips][n]
+    const float *picked;
+    const void *targets;
+    float *loss, *lse;
+    int64_t n, strips, v;
+    int wide;
+};
+
+// The loss of ROWS rows a workgroup from their strips.
+template <int ROWS>
+__global__ __launch_bounds__(256) void join_kernel(JoinArgs a)
+{
+    constexpr int kLanes = 256 / ROWS;
+    const int r = threadIdx.x % ROWS, l = threadIdx.x / ROWS;
+    const int64_t row = (int64_t)blockIdx.x * ROWS + r;
+    float2 v = make_float2(-INFINITY, 0.0f);
+    if (row < a.n) {
+#pragma unroll 8
+        for (int64_t s = l; s < a.strips; s += kLanes)
+            v = merge(v, a.strip[s * a.n + row]);
+    }
+    __shared__ float2 all[256];
+    all[threadIdx.x] = v;
+    for (int o = kLanes / 2; o > 0; o >>= 1) {
+        __syncthreads();
+        if (l < o)
+            all[threadIdx.x] = merge(all[threadIdx.x], all[threadIdx.x + o * ROWS]);
+    }
+    if (l > 0 || row >= a.n)
+        return;
+    v = all[threadIdx.x];
+    // (no other entry: -inf)
+    const float others = v.x + logf(v.y);
+    const int64_t t = target_at(a.targets, a.wide, row);
+    float loss = 0.0f, lse = others;
+    if (t >= 0 && t < a.v) {
+        const float z = a.picked[row], d = others - z;
+        // softplus(d), the larger of both logits apart; an infinite or NaN
+        // logit makes it NaN, a target without probability infinite
+        const float tail = log1pf(expf(-fabsf(d)));
+        loss = z == INFINITY ? NAN : (d > 0.0f ? d + tail : tail);
+        lse = z == -INFINITY ? others : fmaxf(others, z) + tail;
+        if (d != d)
+            loss = lse = NAN;
+    }
+    a.loss[row] = loss;
+    if (a.lse)
+        a.lse[row] = lse;
+}
+
+// -------------------------------------------------------------- backward
+constexpr int kNoGradient = 400;       // beyond any power, and their sums an int
+
+struct RowsArgs {
+    const float *dloss, *loss, *lse;
+    const void *targets;
+    int wide;
+    int64_t n, v;
+    LossRow *rows;
+    float *most;               // of each workgroup's |g|, or null
+    int *power;                // float32: of each row, or null
+};
+
+__global__ __launch_bounds__(256) void rows_kernel(RowsArgs a)
+{
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    float size = 0.0f;
+    if (i < a.n) {
+        const int64_t t = target_at(a.targets, a.wide, i);
+        LossRow r{0.0f, 0.0f, 0.0f, -1};
+        if (t >= 0 && t < a.v) {
+            const float g = a.dloss[i];
+            r = LossRow{a.lse[i], g, g * expm1f(-a.loss[i]), (int)t};
+            size = fabsf(g) < INFINITY ? fabsf(g) : 0.0f;
+        }
+        a.rows[i] = r;
+        // (rows without a gradient take no part in the columns' maxima)
+        if (a.power)
+            a.power[i] = size > 0.0f ? power_for(size) : kNoGradient;
+    }
+    if (!a.most)
+        return;
+    __shared__ float w[4];
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1)
+        size = fmaxf(size, __shfl_xor(size, o, 64));
+    if ((threadIdx.x & 63) == 0)
+        w[threadIdx.x >> 6] = size;
+    __syncthreads();
+    if (threadIdx.x == 0)
+        a.most[blockIdx.x] = fmaxf(fmaxf(w[0], w[1]), fmaxf(w[2], w[3]));
+}
+
+// the power of the largest |g|
+__global__ __launch_bounds__(1024) void largest_kernel(const float *most, int64_t count, int *power)
+{
+    float best = 0.0f;
+    for (int64_t i = threadIdx.x; i < count; i += 1024)
+        best = fmaxf(best, most[i]);
+    __shared__ float all[1024];
+    all[threadIdx.x] = best;
+    for (int o = 512; o > 0; o >>= 1) {
+        __syncthreads();
+        if (threadIdx.x < o)
+            all[threadIdx.x] = fmaxf(all[threadIdx.x], all[threadIdx.x + o]);
+    }
+    if (threadIdx.x == 0)
+        *power = power_for(all[0]);
+}
+
+// Partial maxima [parts][cols] of the finite |x| 2^(base - row) of a float32
+// matrix's columns.
+struct ColumnArgs {
+    const float *x;
+    int64_t rows, cols, ld, each;
+    const int *row, *base;     // or null: |x|
+    float *part;
+};
+
+__global__ __launch_bounds__(256) void column_max_kernel(ColumnArgs a)
+{
+    const int64_t col = ((int64_t)blockIdx.x * 64 + (threadIdx.x & 63)) * 4;
+    const int64_t r0 = blockIdx.y * a.each, r1 = r0 + a.each < a.rows ? r0 + a.each : a.rows;
+    const int base = a.base ? *a.base : 0;
+    f32x4 best = 0.0f;
+    if (col < a.cols)
+#pragma unroll 4
+        for (int64_t r = r0 + (threadIdx.x >> 6); r < r1; r += 4) {
+            const int over = a.row ? base - a.row[r] : 0;
+            f32x4 x = 0.0f;
+            if (col + 4 <= a.cols)
+                x = load4(a.x, r * a.ld + col, GPIC_F32);
+            else
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (col + j < a.cols)
+                        x[j] = a.x[r * a.ld + col + j];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float v = fabsf(x[j]);
+                best[j] = v < INFINITY ? fmaxf(best[j], ldexpf(v, over)) : best[j];
+            }
+        }
+    __shared__ f32x4 all[4][64];
+    all[threadIdx.x >> 6][threadIdx.x & 63] = best;
+    __syncthreads();
+    if (threadIdx.x >= 64)
+        return;
+    for (int w = 1; w < 4; ++w)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            best[j] = fmaxf(best[j], all[w][threadIdx.x][j]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (col + j < a.cols)
+            a.part[blockIdx.y * a.cols + col + j] = best[j];
+}
+
+__global__ __launch_bounds__(256) void column_power_kernel(const float *part, int64_t parts,
+                                                           int64_t cols, const int *base,
+                                                           int *power)
+{
+    const int64_t col = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
+    float best = 0.0f;
+    if (col < cols) {
+#pragma unroll 8
+        for (int64_t p = threadIdx.x >> 6; p < parts; p += 4)
+            best = fmaxf(best, part[p * cols + col]);
+    }
+    __shared__ float all[4][64];
+    all[threadIdx.x >> 6][threadIdx.x & 63] = best;
+    __syncthreads();
+    if (threadIdx.x < 64 && col < cols) {
+        for (int w = 1; w < 4; ++w)
+            best = fmaxf(best, all[w][threadIdx.x]);
+        power[col] = power_for(best) + (base ? *base : 0);
+    }
+}
+
+__global__ __launch_bounds__(256) void zero_kernel(void *p, int64_t values, int dtype)
+{
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < values;
+         i += (int64_t)gridDim.x * 256)
+        store1(p, i, 0.0f, dtype);
+}
+
+// ------------------------------------------------------------------- host
+#define RUN(expr)                                                              \
+    do {                                                                       \
+        hipError_t e_ = (expr);                                                \
+        if (e_ != hipSuccess)                                                  \
+            return e_;                                                         \
+    } while (0)
+
+constexpr int kFew = 32;
+
+// Few rows, or little work, where launches count.
+bool few(const Loss &p)
+{
+    if (p.n <= kFew)
+        return true;
+    const bool f32 = p.dtype == GPIC_F32;
+    return p.n <= 2048 && p.n * p.v <= ((int64_t)1 << (f32 ? 28 : 27)) / p.k;
+}
+
+int64_t edge_of(const Plan &p) { return p.tile == 0 ? 256 : (p.tile == 1 ? 128 : 64); }
+
+// What a forward call keeps in its workspace.
+struct Forward {
+    Source X{}, W{};
+    int64_t strips;
+    float2 *strip;
+    float *picked;
+    Forward(const Loss &p, const void *x, const void *w, Cursor &c)
+    {
+        picked = static_cast<float *>(c.take((size_t)p.n * 4));
+        if (few(p)) {
+            strips = (p.v + 15) / 16;
+        } else {
+            const Plan plan = product_plan(p.n, p.v, p.k, 1, kind_of(p.dtype), kEpiLse);
+            strips = (p.v + edge_of(plan) - 1) / edge_of(plan);
+            X = Source{x, p.n, p.k, p.ldx, must_pack(p.dtype, p.k, p.ldx, p.aligned16)};
+            W = Source{w, p.v, p.k, p.ldw, must_pack(p.dtype, p.k, p.ldw, p.aligned16)};
+            place(X, p.dtype, c, X.rows);
+            place(W, p.dtype, c, W.rows);
+        }
+        strip = static_cast<float2 *>(c.take((size_t)strips * p.n * 8));
+    }
+};
+
+// How the vocabulary is cut: pieces of whole tiles, of which dZ takes up to
+// 256 MB (what the last-level cache holds), of 2,048 columns at least.
+int64_t piece_of(const Loss &p)
+{
+    const int64_t size = p.dtype == GPIC_F32 ? 4 : 2, n = p.n < 1 ? 1 : p.n;
+    int64_t most = ((int64_t)256 << 20) / (size * n) / 256 * 256;
+    most = most < 2048 ? 2048 : most;
+    const int64_t pieces = (p.v + most - 1) / most;
+    return ((p.v + pieces - 1) / pieces + 255) / 256 * 256;
+}
+
+int64_t max_parts(int64_t rows, int64_t cols)
+{
+    const int64_t strips = (cols + 255) / 256;
+    int64_t parts = 1024 / strips;
+    parts = parts < (rows + 15) / 16 ? parts : (rows + 15) / 16;
+    return parts < 1 ? 1 : (parts > 512 ? 512 : parts);
+}
+
+// What a backward call keeps in its workspace.
+struct Backward {
+    int64_t piece, pitch;      // columns of a piece, 16-bit values of a row of dZ
+    LossRow *rows;
+    float *most = nullptr;
+    int *power = nullptr;      // of the largest |g|
+    int *row_power = nullptr;  // float32: of dZ's rows
+    Source X, W;               // as the logits' product reads them (W: a piece)
+    Source Xc{}, Wc{};         // float32: as dW's and dX's do
+    float *column_part = nullptr;
+    void *dZ;
+    float *sum_x, *sum_b;      // dX over the pieces, partial column sums of dZ
+    float *part;
+    Backward(const Loss &p, const void *x, const void *w, Cursor &c)
+    {
+        const bool f32 = p.dtype == GPIC_F32;
+        piece = piece_of(p);
+        const int64_t cols = piece < p.v ? piece : p.v;
+        pitch = f32 ? split_ld(up64(cols)) : up64(cols);
+        rows = static_cast<LossRow *>(c.take((size_t)p.n * sizeof(LossRow)));
+        if (p.dtype != GPIC_BF16) {
+            most = static_cast<float *>(c.take((size_t)((p.n + 255) / 256) * 4));
+            power = static_cast<int *>(c.take(4));
+        }
+        X = Source{x, p.n, p.k, p.ldx, must_pack(p.dtype, p.k, p.ldx, p.aligned16)};
+        W = Source{w, cols, p.k, p.ldw, must_pack(p.dtype, p.k, p.ldw, p.aligned16)};
+        place(X, p.dtype, c, p.n);
+        place(W, p.dtype, c, cols);
+        if (f32) {
+            row_power = static_cast<int *>(c.take((size_t)p.n * 4));
+            Xc = Source{x, p.n, p.k, p.ldx, true};
+            Xc.row = row_power;
+            Wc = Source{w, cols, p.k, p.ldw, true};
+            place(Xc, p.dtype, c, p.k);
+            place(Wc, p.dtype, c, p.k);
+            const int64_t px = max_parts(p.n, p.k), pw = max_parts(p.v, p.k);
+            column_part = static_cast<float *>(c.take((size_t)(px > pw ? px : pw) * p.k * 4));
+        }
+        dZ = c.take((size_t)p.n * pitch * 2);
+        sum_x = piece < p.v ? static_cast<float *>(c.take((size_t)p.n * p.k * 4)) : nullptr;
+        sum_b = static_cast<float *>(c.take((size_t)((p.n + 31) / 32) * cols * 4));
+        size_t bytes = 0;
+        const int op = kind_of(p.dtype);
+        for (int64_t len : {cols, p.v - (p.v - 1) / piece * piece}) {
+            const size_t bx = product_plan(p.n, p.k, len, 1, op, kEpiSum).part_bytes;
+            const size_t bw = product_plan(len, p.k, p.n, 1, op, kEpiLayer).part_bytes;
+            bytes = bytes > bx ? bytes : bx;
+            bytes = bytes > bw ? bytes : bw;
+        }
+        part = static_cast<float *>(c.take(bytes));
+    }
+};
+
+template <int DT, int NB>
+void launch_waves(const FewArgs &a, hipStream_t st)
+{
+    const dim3 blocks((unsigned)((a.v + 15) / 16), (unsigned)((a.n + 16 * NB - 1) / (16 * NB)));
+    const int64_t turns = (a.k + (DT == GPIC_F32 ? 63 : 127)) / (DT == GPIC_F32 ? 64 : 128);
+    if (turns <= 4)
+        few_lse_kernel<DT, NB, 4><<<blocks, 256, 0, st>>>(a);
+    else if (turns <= 8)
+        few_lse_kernel<DT, NB, 8><<<blocks, 512, 0, st>>>(a);
+    else
+        few_lse_kernel<DT, NB, 16><<<blocks, 1024, 0, st>>>(a);
+}
+
+template <int DT>
+hipError_t launch_few(const FewArgs &a, hipStream_t st)
+{
+    if (a.n <= 16)
+        launch_waves<DT, 1>(a, st);
+    else
+        launch_waves<DT, 2>(a, st);
+    return hipGetLastError();
+}
+
+hipError_t launch_columns(const Source &s, const int *row, const int *base, float *part,
+                          hipStream_t st)
+{
+    const int64_t parts = max_parts(s.rows, s.cols), each = (s.rows + parts - 1) / parts;
+    const ColumnArgs a{static_cast<const float *>(s.x), s.rows, s.cols, s.ld, each, row, base,
+                       part};
+    const int64_t used = (s.rows + each - 1) / each;
+    column_max_kernel<<<dim3((unsigned)((s.cols + 255) / 256), (unsigned)used), 256, 0, st>>>(a);
+    RUN(hipGetLastError());
+    column_power_kernel<<<(unsigned)((s.cols + 63) / 64), 256, 0, st>>>(part, used, s.cols, base,
+                                                                      s.power);
+    return hipGetLastError();
+}
+
+} // namespace
+
+size_t loss_ws(const Loss &p, bool backward)
+{
+    Cursor c{nullptr};
+    if (backward)
+        Backward b(p, nullptr, nullptr, c);
+    else
+        Forward f(p, nullptr, nullptr, c);
+    return c.at;
+}
+
+bool loss_fits(const Loss &p, bool backward)
+{
+    if (p.n == 0 || (!backward && few(p)))
+        return true;
+    const int op = kind_of(p.dtype);
+    if (!backward)
+        return product_plan(p.n, p.v, p.k, 1, op, kEpiLse).fits;
+    const int64_t piece = piece_of(p) < p.v ? piece_of(p) : p.v;
+    return product_plan(p.n, piece, p.k, 1, op, kEpiSoft).fits &&
+           product_plan(p.n, p.k, piece, 1, op, kEpiSum).fits &&
+           product_plan(piece, p.k, p.n, 1, op, kEpiLayer).fits;
+}
+
+hipError_t run_loss(const Loss &p, const void *X, const void *W, const void *bias,
+                    const void *targets, float *loss, float *lse, void *ws, hipStream_t st)
+{
+    if (p.n == 0)
+        return hipSuccess;
+    Cursor c{static_cast<char *>(ws)};
+    Forward f(p, X, W, c);
+    if (few(p)) {
+        const FewArgs a{X, W, bias, targets, f.strip, f.picked, p.ldx, p.ldw, p.n, p.k, p.v, p.wide};
+        RUN(p.dtype == GPIC_F32    ? launch_few<GPIC_F32>(a, st)
+            : p.dtype == GPIC_F16 ? launch_few<GPIC_F16>(a, st)
+                                  : launch_few<GPIC_BF16>(a, st));
+    } else {
+        const Source *list[2] = {&f.X, &f.W};
+        if (p.dtype == GPIC_F32)
+            RUN(launch_split_rows(f.X, f.W, st));
+        else
+            RUN(launch_pack(list, 2, p.dtype, st));
+        ProductArgs a{};
+        a.A = f.X.operand(p.dtype);
+        a.B = f.W.operand(p.dtype);
+        a.M = (int)p.n;
+        a.N = (int)p.v;
+        a.K = p.k;
+        a.batch = 1;
+        a.e.pa = f.X.power;
+        a.e.pb = f.W.power;
+        a.e.bias = bias;
+        a.e.targets = targets;
+        a.e.wide = p.wide;
+        a.e.strip = f.strip;
+        a.e.picked = f.picked;
+        RUN(launch_product(kKK, kind_of(p.dtype), kEpiLse, a, st));
+    }
+    const JoinArgs j{f.strip, f.picked, targets, loss, lse, p.n, f.strips, p.v, p.wide};
+    if (p.n < 64)
+        join_kernel<1><<<(unsigned)p.n, 256, 0, st>>>(j);
+    else
+        join_kernel<16><<<(unsigned)((p.n + 15) / 16), 256, 0, st>>>(j);
+    return hipGetLastError();
+}
+
+hipError_t run_loss_backward(const Loss &p, const float *dloss, const void *X, const void *W,
+                             const void *bias, const void *targets, const float *loss,
+                             const float *lse, void *dX, void *dW, void *db, void *ws,
+                             hipStream_t st)
+{
+    const size_t size = p.dtype == GPIC_F32 ? 4 : 2;
+    if (p.n == 0) {
+        if (dW)
+            zero_kernel<<<4096, 256, 0, st>>>(dW, p.v * p.k, p.dtype);
+        if (db)
+            zero_kernel<<<64, 256, 0, st>>>(db, p.v, p.dtype);
+        return hipGetLastError();
+    }
+    if (!dX && !dW && !db)
+        return hipSuccess;
+    Cursor c{static_cast<char *>(ws)};
+    Backward b(p, X, W, c);
+    const bool f32 = p.dtype == GPIC_F32;
+    const int op = kind_of(p.dtype);
+    {
+        const RowsArgs a{dloss, loss, lse, targets, p.wide, p.n, p.v, b.rows, b.most, b.row_power};
+        rows_kernel<<<(unsigned)((p.n + 255) / 256), 256, 0, st>>>(a);
+        RUN(hipGetLastError());
+    }
+    if (b.power) {
+        largest_kernel<<<1, 1024, 0, st>>>(b.most, (p.n + 255) / 256, b.power);
+        RUN(hipGetLastError());
+    }
+    if (f32) {
+        if (dW) {
+            RUN(launch_columns(b.Xc, b.row_power, b.power, b.column_part, st));
+            const Source *list[1] = {&b.Xc};
+            RUN(launch_pack(list, 1, p.dtype, st));
+        }
+        if (dX) {
+            Source all = b.Wc;
+            all.rows = p.v;
+            RUN(launch_columns(all, nullptr, nullptr, b.column_part, st));
+        }
+    } else {
+        const Source *list[1] = {&b.X};
+        RUN(launch_pack(list, 1, p.dtype, st));
+    }
+    for (int64_t first = 0; first < p.v; first += b.piece) {
+        const int64_t len = p.v - first < b.piece ? p.v - first : b.piece;
+        const void *w = static_cast<const char *>(W) + (size_t)first * p.ldw * size;
+        b.W.x = b.Wc.x = w;
+        b.W.rows = b.Wc.rows = len;
+        if (f32) {
+            Source x = b.X;
+            if (first > 0)
+                x.rows = 0;                       // X is split with the first piece
+            RUN(launch_split_rows(x, b.W, st));
+            if (dX) {
+                const Source *list[1] = {&b.Wc};
+                RUN(launch_pack(list, 1, p.dtype, st));
+            }
+        } else {
+            const Source *list[1] = {&b.W};
+            RUN(launch_pack(list, 1, p.dtype, st));
+        }
+        ProductArgs a{};
+        a.A = b.X.operand(p.dtype);
+        a.B = b.W.operand(p.dtype);
+        a.M = (int)p.n;
+        a.N = (int)len;
+        a.K = p.k;
+        a.batch = 1;
+        a.part = b.part;
+        a.e.pa = f32 ? b.X.power : nullptr;
+        a.e.pb = b.W.power;
+        a.e.bias = bias;
+        a.e.rows = b.rows;
+        a.e.first = first;
+        a.e.power = f32 ? b.row_power : b.power;
+        a.e.power_step = f32 ? 1 : 0;
+        a.e.p_hi = b.dZ;
+        a.e.ldp = b.pitch;
+        a.e.sums = db ? b.sum_b : nullptr;
+        RUN(launch_product(kKK, op, kEpiSoft, a, st));
+        if (db) {
+            const Plan plan = product_plan(p.n, len, p.k, 1, op, kEpiSoft);
+            const int64_t each = plan.tile == 2 ? 32 : 64;
+            RUN(launch_sum_parts(b.sum_b, (p.n + each - 1) / each, len,
+                                 static_cast<char *>(db) + (size_t)first * size, p.dtype, st));
+        }
+        const int64_t width = f32 ? split_ld(up64(len)) : up64(len);
+        if (dX) {
+            ProductArgs x{};
+            x.A = Operand{b.dZ, b.pitch, 0, width};
+            x.B = f32 ? b.Wc.operand(p.dtype) : b.W.operand(p.dtype);
+            x.M = (int)p.n;
+            x.N = (int)p.k;
+            x.K = len;
+            x.batch = 1;
+            x.part = b.part;
+            x.e.dtype = p.dtype;
+            x.e.pa = f32 ? b.row_power : b.power;
+            x.e.pb = b.Wc.power;
+            x.e.res = first > 0 ? b.sum_x : nullptr;
+            x.e.ldr = x.e.ldo = p.k;
+            x.e.last = first + len >= p.v;
+            x.e.out = x.e.last ? dX : b.sum_x;
+            RUN(launch_product(kKM, op, kEpiSum, x, st));
+        }
+        if (dW) {
+            ProductArgs d{};
+            d.A = Operand{b.dZ, b.pitch, 0, width};
+            d.B = f32 ? b.Xc.operand(p.dtype) : b.X.operand(p.dtype);
+            d.M = (int)len;
+            d.N = (int)p.k;
+            d.K = p.n;
+            d.batch = 1;
+            d.part = b.part;
+            d.e.dtype = p.dtype;
+            d.e.act = GPIC_ACT_NONE;
+            d.e.pa = f32 ? nullptr : b.power;
+            d.e.pb = b.Xc.power;
+            d.e.ldo = p.k;
+            d.e.out = static_cast<char *>(dW) + (size_t)first * p.k * size;
+            RUN(launch_product(kMM, op, kEpiLayer, d, st));
+        }
+    }
+    return hipSuccess;
+}
+
+} // namespace gpic

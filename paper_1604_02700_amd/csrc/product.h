@@ -265,7 +265,7 @@ using i32x8 = int __attribute__((ext_vector_type(8), aligned(4)));
 template <int ROWS, int OP, int EPI>
 __device__ __forceinline__ int row_powers(const Epilogue &e, int64_t row0, int64_t M)
 {
-    if (OP == kOpBf16 || (EPI != kEpiLayer && EPI != kEpiGated) || !e.pa)
+    if (OP == kOpBf16 || !powered(EPI) || !e.pa)
         return 0;
     static_assert(ROWS <= 64, "a row a lane");
     const int64_t row = row0 + (threadIdx.x & 63);
@@ -277,7 +277,7 @@ template <int OP, int EPI>
 __device__ __forceinline__ i32x8 column_powers(const Epilogue &e, int64_t col, int valid)
 {
     i32x8 p = 0;
-    if (OP != kOpSplit || (EPI != kEpiLayer && EPI != kEpiGated) || !e.pb || valid <= 0)
+    if (OP != kOpSplit || !powered(EPI) || !e.pb || valid <= 0)
         return p;
     if (valid >= 8)
         return *reinterpret_cast<const i32x8 *>(e.pb + col);
@@ -292,7 +292,7 @@ template <int OP, int EPI>
 __device__ __forceinline__ f32x8 staged(const float *p, const Epilogue &e, int row, i32x8 columns)
 {
     f32x8 v = *reinterpret_cast<const f32x8 *>(p);
-    if (EPI != kEpiLayer && EPI != kEpiGated)
+    if (!powered(EPI))
         return v * e.alpha;
     if (OP != kOpBf16) {
 #pragma unroll
@@ -374,7 +374,7 @@ __device__ __forceinline__ void finish_block(const Epilogue &e, int64_t z, int64
         for (int p = 0; p < kGroup; ++p) {
             const int r = (p0 + p) * kRowsPass + r0;
             const int64_t row = row0 + r;
-            const int pr = OP == kOpBf16 || EPI != kEpiLayer ? 0 : __shfl(powers, r & 63, 64);
+            const int pr = OP == kOpBf16 || !powered(EPI) ? 0 : __shfl(powers, r & 63, 64);
             v[p] = staged<OP, EPI>(st + (idle ? 0 : r) * kPitch + q * 8, e, pr, pc);
             c[p] = 0.0f;
             if (EPI == kEpiPoly || EPI == kEpiUpdate || EPI == kEpiResult) {
@@ -386,6 +386,8 @@ __device__ __forceinline__ void finish_block(const Epilogue &e, int64_t z, int64
                 continue;
             if (EPI == kEpiLayer && e.res)
                 c[p] = load8(e.res, row * e.ldr + col, dtype, valid);
+            if (EPI == kEpiSum && e.res)
+                c[p] = load8(e.res, row * e.ldr + col, GPIC_F32, valid);
             if (EPI == kEpiResult && e.is_step) {
                 // decay W - step (beta X + acc)
                 const f32x8 old = load8(e.out, z * e.batch_o + row * e.ldo + col, dtype, valid);
@@ -409,6 +411,12 @@ __device__ __forceinline__ void finish_block(const Epilogue &e, int64_t z, int64
                 if (e.res)
                     x = x + c[p];
                 store8(e.out, row * e.ldo + col, x, dtype, valid);
+            } else if (EPI == kEpiSum) {
+                x = x + c[p];
+                if (e.last)
+                    store8(e.out, row * e.ldo + col, x, dtype, valid);
+                else
+                    store8(e.out, row * e.ldo + col, x, GPIC_F32, valid);
             } else if (kSym) {
                 x = (EPI == kEpiPoly ? x + c[p] : x) * e.store_scale;
                 P::store(e, P::at(e, z, row, col), x);
@@ -542,6 +550,181 @@ struct Staging {
     static constexpr int kBytes = kFloats * 4 * (T::kThreads / 64);
 };
 
+// ------------------------------------------------- epilogues of the loss
+constexpr float kLog2e = 1.4426950408889634f;
+
+// (largest, sum of exponentials) of two sets together; no members: (-inf, 0).
+// A NaN or an infinite logit makes the sum NaN.
+__device__ __forceinline__ float2 merge_lse(float2 a, float2 b)
+{
+    const float m = fmaxf(a.x, b.x), at = m == -INFINITY ? 0.0f : m;
+    return make_float2(m, a.y * __builtin_amdgcn_exp2f((a.x - at) * kLog2e) +
+                              b.y * __builtin_amdgcn_exp2f((b.x - at) * kLog2e));
+}
+
+__device__ __forceinline__ int64_t target_of(const void *t, int wide, int64_t row)
+{
+    return wide ? static_cast<const int64_t *>(t)[row]
+                : (int64_t)static_cast<const int32_t *>(t)[row];
+}
+
+// Each row's (largest, sum of exponentials) over the tile's columns, straight
+// from the accumulators: a lane holds 4 RN of a row's logits, four lanes the
+// wave's share of it, and the waves side by side meet in LDS.
+template <class T, int OP>
+__device__ __forceinline__ void finish_lse(const ProductArgs &a, const Work &w,
+                                           f32x4 (&acc)[T::kRM][T::kRN], char *lds)
+{
+    constexpr int kDt = OP == kOpSplit ? GPIC_F32 : (OP == kOpF16 ? GPIC_F16 : GPIC_BF16);
+    const Epilogue &e = a.e;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4;
+    const int wm = (wave / T::kWN) * (16 * T::kRM), wn = wave % T::kWN;
+    const int64_t col0 = (int64_t)w.tj * T::kBN + wn * (16 * T::kRN) + 4 * g;
+    float bias[T::kRN][4];
+    int pc[T::kRN][4];
+#pragma unroll
+    for (int j = 0; j < T::kRN; ++j)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const int64_t col = col0 + 16 * j + c;
+            // columns beyond the last are no logits
+            bias[j][c] = col < a.N ? (e.bias ? load1(e.bias, col, kDt) : 0.0f) : -INFINITY;
+            pc[j][c] = OP == kOpSplit && col < a.N ? e.pb[col] : 0;
+        }
+    float2 *all = reinterpret_cast<float2 *>(lds);             // [WN][BM]
+#pragma unroll
+    for (int i = 0; i < T::kRM; ++i) {
+        const int r = wm + 16 * i + (lane & 15);
+        const int64_t row = (int64_t)w.ti * T::kBM + r;
+        const bool live = row < a.M;
+        const int pr = OP == kOpSplit && live ? e.pa[row] : 0;
+        float z[T::kRN][4];
+#pragma unroll
+        for (int j = 0; j < T::kRN; ++j)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                float v = acc[i][j][c];
+                if (OP == kOpSplit)
+                    v = ldexpf(v, -(pr + pc[j][c]));
+                z[j][c] = bias[j][c] == -INFINITY ? -INFINITY : v + bias[j][c];
+            }
+        const int64_t t = live ? target_of(e.targets, e.wide, row) : -1;
+        const int64_t at = t - col0;
+        const bool mine = t >= 0 && t < a.N && at >= 0 && at < 16 * T::kRN && (at & 15) < 4;
+        if (__any(mine)) {
+#pragma unroll
+            for (int j = 0; j < T::kRN; ++j)
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    if (mine && at == 16 * j + c) {
+                        e.picked[row] = z[j][c];
+                        z[j][c] = -INFINITY;
+                    }
+        }
+        float m = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < T::kRN; ++j)
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                m = fmaxf(m, z[j][c]);
+        m = fmaxf(m, __shfl_xor(m, 16, 64));
+        m = fmaxf(m, __shfl_xor(m, 32, 64));
+        const float base = m == -INFINITY ? 0.0f : m;
+        float s = 0.0f;
+#pragma unroll
+        for (int j = 0; j < T::kRN; ++j)
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                s += __builtin_amdgcn_exp2f((z[j][c] - base) * kLog2e);
+        s += __shfl_xor(s, 16, 64);
+        s += __shfl_xor(s, 32, 64);
+        if (g == 0)
+            all[wn * T::kBM + r] = make_float2(m, s);
+    }
+    __syncthreads();
+    for (int r = threadIdx.x; r < T::kBM; r += T::kThreads) {
+        const int64_t row = (int64_t)w.ti * T::kBM + r;
+        if (row >= a.M)
+            break;
+        float2 v = all[r];
+#pragma unroll
+        for (int n = 1; n < T::kWN; ++n)
+            v = merge_lse(v, all[n * T::kBM + r]);
+        e.strip[(int64_t)w.tj * a.M + row] = v;
+    }
+}
+
+// dZ = g (exp(z - lse) - [target]) of ROWS x COLS logits that the wave has
+// staged at `st`, as the products that follow read it (a row's padding up to
+// 64 columns zeros), and its column sums, unrounded.
+template <int ROWS, int COLS, int OP>
+__device__ __forceinline__ void finish_soft(const Epilogue &e, int64_t row0, int64_t col0,
+                                            int64_t M, int64_t N, const float *st)
+{
+    constexpr int kDt = OP == kOpSplit ? GPIC_F32 : (OP == kOpF16 ? GPIC_F16 : GPIC_BF16);
+    constexpr int kPitch = COLS + 4, kLanes = COLS / 8, kRowsPass = 64 / kLanes;
+    constexpr int kPasses = ROWS / kRowsPass;
+    static_assert(kPasses * kRowsPass == ROWS, "passes");
+    const int lane = threadIdx.x & 63, q = lane % kLanes, r0 = lane / kLanes;
+    const int64_t col = col0 + q * 8, end = (N + 63) / 64 * 64;
+    const int real = N - col < 0 ? 0 : (N - col < 8 ? (int)(N - col) : 8);
+    const bool written = col < end;
+    const int powers = row_powers<ROWS, OP, kEpiSoft>(e, row0, M);
+    const i32x8 pc = column_powers<OP, kEpiSoft>(e, col, real);
+    f32x8 bias = 0.0f, sum = 0.0f;
+    if (e.bias && real > 0)
+        bias = load8(e.bias, e.first + col, kDt, real);
+#pragma unroll 2
+    for (int p = 0; p < kPasses; ++p) {
+        const int r = p * kRowsPass + r0;
+        const int64_t row = row0 + r;
+        const int pr = OP == kOpBf16 ? 0 : __shfl(powers, r & 63, 64);
+        f32x8 z = staged<OP, kEpiSoft>(st + r * kPitch + q * 8, e, pr, pc);
+        if (row >= M || !written)
+            continue;
+        const LossRow info = e.rows[row];
+        const int at = info.target - (int)(e.first + col);
+        f32x8 d;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            d[j] = info.g * __builtin_amdgcn_exp2f((z[j] + bias[j] - info.lse) * kLog2e);
+            d[j] = at == j ? info.picked : (bias[j] == -INFINITY ? 0.0f : d[j]);
+            d[j] = j < real && info.target >= 0 ? d[j] : 0.0f;
+        }
+        sum += d;
+        if (OP != kOpBf16) {
+            const int power = e.power[row * e.power_step];
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                d[j] = ldexpf(d[j], power);
+        }
+        if (OP == kOpSplit) {
+            _Float16 *to = static_cast<_Float16 *>(e.p_hi) + row * e.ldp + split_at(col);
+            half8 h, l;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                _Float16 x, y;
+                split2(d[j], x, y);
+                h[j] = x;
+                l[j] = y;
+            }
+            *reinterpret_cast<half8 *>(to) = h;
+            *reinterpret_cast<half8 *>(to + 32) = l;
+        } else {
+            store8(e.p_hi, row * e.ldp + col, d, kDt, 8);
+        }
+    }
+    if (!e.sums)
+        return;
+#pragma unroll
+    for (int o = kLanes; o < 64; o <<= 1)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            sum[j] += __shfl_xor(sum[j], o, 64);
+    if (r0 == 0 && real > 0 && row0 < M)
+        store8(e.sums + row0 / ROWS * N, col, sum, GPIC_F32, real);
+}
+
 // A wave's accumulators to their place: the epilogue, or the partial sums.
 template <class T, int OP, int EPI>
 __device__ __forceinline__ void finish_tile(const ProductArgs &a, const Work &w,
@@ -554,6 +737,10 @@ __device__ __forceinline__ void finish_tile(const ProductArgs &a, const Work &w,
     copies_done();
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
+    if constexpr (EPI == kEpiLse) {
+        finish_lse<T, OP>(a, w, acc, lds);
+        return;
+    }
     float *st = reinterpret_cast<float *>(lds) + wave * St::kFloats;
     float *to = st + (lane & 15) * St::kPitch + (lane >> 4) * 4;
     float *part = a.part + ((int64_t)w.split * (((int)gridDim.x - a.whole) / w.parts) +
@@ -575,7 +762,11 @@ __device__ __forceinline__ void finish_tile(const ProductArgs &a, const Work &w,
         } else {
             const int64_t r0 = (int64_t)w.ti * T::kBM + wm + 16 * i0, c0 = (int64_t)w.tj * T::kBN + wn;
             const bool mirror = symmetric(EPI) && w.ti != w.tj;
-            finish_block<St::kRows, St::kCols, OP, EPI>(a.e, w.z, r0, c0, a.M, a.N, st, mirror);
+            if constexpr (EPI == kEpiSoft)
+                finish_soft<St::kRows, St::kCols, OP>(a.e, r0, c0, a.M, a.N, st);
+            else
+                finish_block<St::kRows, St::kCols, OP, EPI>(a.e, w.z, r0, c0, a.M, a.N, st,
+                                                            mirror);
             if (mirror)
                 mirror_block<St::kRows, St::kCols, OP, EPI>(a.e, w.z, r0, c0, a.N, st, 0, 1);
         }
@@ -967,14 +1158,18 @@ hipError_t launch_tile(const Plan &p, ProductArgs a, hipStream_t s)
         product_kernel<T, ASTR, BSTR, OP, EPI>
             <<<(unsigned)blocks, T::kThreads, 0, s>>>(a, p.tm, p.tn);
     hipError_t e = hipGetLastError();
-    if (e == hipSuccess && p.tail > 0) {
-        using St = Staging<T>;
-        constexpr int kPieces = T::kBM / St::kRows * (T::kBN / St::kCols);
-        product_join_kernel<T, OP, EPI>
-            <<<(unsigned)(p.tail * kPieces), 256, 0, s>>>(a, p.tm, p.tn, (int)p.tail);
-        e = hipGetLastError();
+    if constexpr (uncut(EPI)) {
+        return e;
+    } else {
+        if (e == hipSuccess && p.tail > 0) {
+            using St = Staging<T>;
+            constexpr int kPieces = T::kBM / St::kRows * (T::kBN / St::kCols);
+            product_join_kernel<T, OP, EPI>
+                <<<(unsigned)(p.tail * kPieces), 256, 0, s>>>(a, p.tm, p.tn, (int)p.tail);
+            e = hipGetLastError();
+        }
+        return e;
     }
-    return e;
 }
 
 template <bool ASTR, bool BSTR, int OP, int EPI>

@@ -74,6 +74,8 @@ Plan product_plan(int64_t M, int64_t N, int64_t K, int64_t batch, int op, int ep
             best = Plan{true, t, (int)tm, (int)tn, whole, tail, tail ? parts : 1, bytes};
         };
         consider(tiles, 1);
+        if (uncut(epi))
+            continue;
         const int64_t slots = (int64_t)kUnits * c.resident, round = tiles / slots * slots;
         for (int parts : kParts)
             if (parts * 2 <= steps) {
@@ -93,6 +95,8 @@ hipError_t launch_product(int modes, int op, int epi, const ProductArgs &a, hipS
         return hipErrorInvalidValue;
     if (p.whole + p.tail == 0)
         return hipSuccess;
+    if (epi >= kEpiLse)
+        return launch_product_loss(op, epi, p, a, s);
     if (modes == kKK)
         return launch_product_kk(op, epi, p, a, s);
     if (modes == kKM)

@@ -43,4 +43,21 @@ hipError_t run_embedding(const Embedding &p, const void *ids, const void *T, voi
 hipError_t run_embedding_backward(const Embedding &p, const void *dY, const void *ids, void *dT,
                                   void *ws, hipStream_t st);
 
+// --------------------------------------------------------------- loss.hip
+struct Loss {
+    int64_t n, k, v, ldx, ldw;
+    int dtype;
+    bool wide;                 // 64-bit targets
+    bool aligned16;            // X and W start on 16 bytes
+};
+size_t loss_ws(const Loss &p, bool backward);
+// Whether every launch of a call stays below a grid's 2^32 threads.
+bool loss_fits(const Loss &p, bool backward);
+hipError_t run_loss(const Loss &p, const void *X, const void *W, const void *bias,
+                    const void *targets, float *loss, float *lse, void *ws, hipStream_t st);
+hipError_t run_loss_backward(const Loss &p, const float *dloss, const void *X, const void *W,
+                             const void *bias, const void *targets, const float *loss,
+                             const float *lse, void *dX, void *dW, void *db, void *ws,
+                             hipStream_t st);
+
 } // namespace gpic
