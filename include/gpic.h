@@ -701,10 +701,12 @@ gpic_status gpic_cross_entropy(const gpic_loss_params *p, const void *X, const v
  * [n x k] = dZ W, dW [v x k] = dZ^T X, db [v] = column sums of dZ.  dX, dW and db
  * are contiguous, any may be null (not wanted).  loss and lse as
  * gpic_cross_entropy gave them.  The logits are computed once more, in pieces of
- * the vocabulary whose dZ takes about 256 MB, rounded to the matrices' type for
- * the products (float16: times a power of two from the largest finite |dloss|;
- * float32: 22 bits down to 2^-17 of the row's |dloss|, errors of 2^-39 of it
- * below); db sums it unrounded.  With n = 0, dW and db are zeros.
+ * the vocabulary whose dZ takes about 256 MB.  For the products dZ / dloss is
+ * rounded to the matrices' type (float16: nothing finer than 2^-39; float32: 22
+ * bits down to 2^-17, errors of 2^-39 below), and for dW so is X times dloss over
+ * the largest finite |dloss| (no rounding where all are alike); db sums it
+ * unrounded.  X's rows of padding, and those whose dloss is 0, may hold anything.
+ * With n = 0, dW and db are zeros.
  * ws: gpic_cross_entropy_workspace_bytes(1, p). */
 gpic_status gpic_cross_entropy_backward(const gpic_loss_params *p, const float *dloss,
                                         const void *X, const void *W, const void *bias,

@@ -276,8 +276,8 @@ struct Operand {
 // kEpiResult: the same as a result (or, is_step, weights moved by it);
 // kEpiLse: logits z = acc + bias, of which each row's largest and sum of
 // exponentials over the tile's columns are kept (but the target's, which is
-// kept itself); kEpiSoft: the logits' gradients g (exp(z - lse) - [target]) as
-// an operand of further products; kEpiSum: acc added to float32 sums
+// kept itself); kEpiSoft: exp(z - lse) - [target] as an operand of further
+// products; kEpiSum: acc times a factor (of its row), added to float32 sums
 enum {
     kEpiLayer = 0, kEpiGated = 1, kEpiGram = 2, kEpiPoly = 3, kEpiUpdate = 4, kEpiResult = 5,
     kEpiLse = 6, kEpiSoft = 7, kEpiSum = 8
@@ -291,10 +291,13 @@ __host__ __device__ constexpr bool powered(int epi)
 // whose tiles are not cut along the contraction
 __host__ __device__ constexpr bool uncut(int epi) { return epi == kEpiLse || epi == kEpiSoft; }
 
+// Brings exp(z - lse) - [target], at most 1, next to the largest half.
+constexpr int kSoftPower = 15;
+
 // What kEpiSoft knows of a row.
 struct LossRow {
     float lse, g;      // g: the loss's gradient
-    float picked;      // the gradient of the target's logit
+    float picked;      // exp(z - lse) - 1 of the target
     int target;        // its column; -1: none, no gradient
 };
 
@@ -329,16 +332,17 @@ struct Epilogue {
     int wide;
     float2 *strip;
     float *picked;
-    // kEpiSoft: rows, the column that the piece starts at, the powers of two
-    // that dZ (p_hi, ldp) is stored under (one for all rows: power_step 0),
-    // [row blocks][N] column sums of dZ or null
+    // kEpiSoft: rows, the column that the piece starts at, where exp(z - lse) -
+    // [target] goes (p_hi, ldp; times 2^kSoftPower but in bfloat16), [row blocks][N]
+    // column sums of it times g, or null
     const LossRow *rows;
     int64_t first;
-    const int *power;
-    int power_step;
     float *sums;
-    // kEpiSum: float32 sums so far (of pitch ldr, in res) or null; out is
-    // float32, or (last) of the operands' type
+    // kEpiSum: operand A is under 2^kSoftPower (but in bfloat16); factors, one a
+    // row or (factor_step 0) for all; sums so far (float32, res and ldr) or null;
+    // out is float32, or (last) of the operands' type
+    const float *factor;
+    int factor_step;
     int last;
 };
 
@@ -375,7 +379,7 @@ hipError_t launch_product(int modes, int op, int epi, const ProductArgs &a, hipS
 hipError_t launch_product_kk(int op, int epi, const Plan &p, const ProductArgs &a, hipStream_t s);
 hipError_t launch_product_km(int op, int epi, const Plan &p, const ProductArgs &a, hipStream_t s);
 hipError_t launch_product_mm(int op, int epi, const Plan &p, const ProductArgs &a, hipStream_t s);
-hipError_t launch_product_loss(int op, int epi, const Plan &p, const ProductArgs &a,
+hipError_t launch_product_loss(int modes, int op, int epi, const Plan &p, const ProductArgs &a,
                                hipStream_t s);
 
 // ---------------------------------------------------- operands' copies (layers.hip)
@@ -392,7 +396,7 @@ struct Source {
     bool pack;
     void *to = nullptr;
     int *power = nullptr;  // float32: of its rows (backward: columns)
-    const int *row = nullptr;  // float32 backward: packed over two to this, by row
+    const float *row = nullptr;    // packed times this, by row (0: zeros)
     Operand operand(int dtype) const
     {
         if (!pack)

@@ -41,7 +41,8 @@ struct PackJob {
     int64_t rows, cols, ld;
     void *to;              // split matrix (float32) or rows of up64(cols)
     const int *power;      // float32: of every column
-    const int *row;        // float32: over two to this, of every row (or null)
+    const float *row;      // every row times this (or null); 0: zeros whatever it holds
+    bool f16;
 };
 struct PackJobs {
     PackJob j[3];
@@ -67,7 +68,6 @@ __global__ __launch_bounds__(256) void pack_kernel(PackJobs jobs)
             const float *x = static_cast<const float *>(m.x) + r * m.ld + c;
             float v[8];
             int power[8];
-            const int over = m.row ? m.row[r] : 0;
             if (c + 8 <= m.cols) {
                 const f32x4 a = load4(x, 0, GPIC_F32), b = load4(x, 4, GPIC_F32);
 #pragma unroll
@@ -85,11 +85,17 @@ __global__ __launch_bounds__(256) void pack_kernel(PackJobs jobs)
                     power[k] = c + k < m.cols ? m.power[c + k] : 0;
                 }
             }
+            if (m.row) {
+                const float f = m.row[r];
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    v[k] = f == 0.0f ? 0.0f : v[k] * f;
+            }
             half8 h, l;
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 _Float16 a, b;
-                split2(ldexpf(v[k], power[k] - over), a, b);
+                split2(ldexpf(v[k], power[k]), a, b);
                 h[k] = a;
                 l[k] = b;
             }
@@ -109,6 +115,21 @@ __global__ __launch_bounds__(256) void pack_kernel(PackJobs jobs)
 #pragma unroll
                 for (int k = 0; k < 8; ++k)
                     u.h[k] = c + k < m.cols ? x[k] : (unsigned short)0;
+            }
+            if (m.row) {
+                const float f = m.row[r];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    if (m.f16)
+                        u.h[k] = __builtin_bit_cast(
+                            unsigned short,
+                            (_Float16)((float)__builtin_bit_cast(_Float16, u.h[k]) * f));
+                    else
+                        u.h[k] = __builtin_bit_cast(
+                            unsigned short, (__bf16)((float)__builtin_bit_cast(__bf16, u.h[k]) * f));
+                    if (f == 0.0f)
+                        u.h[k] = 0;
+                }
             }
             *reinterpret_cast<u32x4 *>(static_cast<unsigned short *>(m.to) + r * width + c) = u.v;
         }
@@ -866,7 +887,7 @@ hipError_t launch_pack(const Source *const *list, int count, int dtype, hipStrea
     for (int i = 0; i < count; ++i)
         if (list[i]->pack && list[i]->rows > 0) {
             const Source &s = *list[i];
-            j.j[used++] = PackJob{s.x, s.rows, s.cols, s.ld, s.to, s.power, s.row};
+            j.j[used++] = PackJob{s.x, s.rows, s.cols, s.ld, s.to, s.power, s.row, dtype == GPIC_F16};
             const int64_t groups = s.rows * ((s.cols + 63) / 64 * 8);
             most = groups > most ? groups : most;
         }

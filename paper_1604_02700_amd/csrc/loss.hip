@@ -13,11 +13,10 @@
 //
 // Few rows, or little work, read W once as it lies (few_lse_kernel).
 //
-// float32 operands are split halves (encoder.h).  A row of dZ is at most |g_i|,
-// and is stored under that bound's power of two, for both products: dX takes
-// it off, and dW = sum_i (dZ_i 2^p_i) (x_i 2^-p_i) takes X over the same powers,
-// under its own by column.  float16's dZ is under one power, from the largest
-// |g|.
+// What is rounded to the products' operands is D = exp(z - lse) - [target], at
+// most 1, without g: dX_i = g_i sum_v D_iv W_v, and dW_v = G sum_i D_iv (g_i / G x_i)
+// with the largest |g| G, so that the usual g, one for all rows, costs nothing.
+// float32 operands are split halves (encoder.h).
 #include <type_traits>
 
 #include "row_chunks.h"
@@ -192,16 +191,13 @@ __global__ __launch_bounds__(256) void join_kernel(JoinArgs a)
 }
 
 // -------------------------------------------------------------- backward
-constexpr int kNoGradient = 400;       // beyond any power, and their sums an int
-
 struct RowsArgs {
     const float *dloss, *loss, *lse;
     const void *targets;
     int wide;
     int64_t n, v;
     LossRow *rows;
-    float *most;               // of each workgroup's |g|, or null
-    int *power;                // float32: of each row, or null
+    float *most;               // of each workgroup's finite |g|
 };
 
 __global__ __launch_bounds__(256) void rows_kernel(RowsArgs a)
@@ -211,18 +207,13 @@ __global__ __launch_bounds__(256) void rows_kernel(RowsArgs a)
     if (i < a.n) {
         const int64_t t = target_at(a.targets, a.wide, i);
         LossRow r{0.0f, 0.0f, 0.0f, -1};
-        if (t >= 0 && t < a.v) {
-            const float g = a.dloss[i];
-            r = LossRow{a.lse[i], g, g * expm1f(-a.loss[i]), (int)t};
+        const float g = a.dloss[i];
+        if (t >= 0 && t < a.v && g != 0.0f) {
+            r = LossRow{a.lse[i], g, expm1f(-a.loss[i]), (int)t};
             size = fabsf(g) < INFINITY ? fabsf(g) : 0.0f;
         }
         a.rows[i] = r;
-        // (rows without a gradient take no part in the columns' maxima)
-        if (a.power)
-            a.power[i] = size > 0.0f ? power_for(size) : kNoGradient;
     }
-    if (!a.most)
-        return;
     __shared__ float w[4];
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1)
@@ -234,8 +225,10 @@ __global__ __launch_bounds__(256) void rows_kernel(RowsArgs a)
         a.most[blockIdx.x] = fmaxf(fmaxf(w[0], w[1]), fmaxf(w[2], w[3]));
 }
 
-// the power of the largest |g|
-__global__ __launch_bounds__(1024) void largest_kernel(const float *most, int64_t count, int *power)
+// G, the largest |g|, and each row's g / G
+__global__ __launch_bounds__(1024) void shares_kernel(const float *most, int64_t count,
+                                                      const LossRow *rows, int64_t n,
+                                                      float *largest, float *share)
 {
     float best = 0.0f;
     for (int64_t i = threadIdx.x; i < count; i += 1024)
@@ -247,16 +240,21 @@ __global__ __launch_bounds__(1024) void largest_kernel(const float *most, int64_
         if (threadIdx.x < o)
             all[threadIdx.x] = fmaxf(all[threadIdx.x], all[threadIdx.x + o]);
     }
+    __syncthreads();
+    best = all[0] > 0.0f ? all[0] : 1.0f;
     if (threadIdx.x == 0)
-        *power = power_for(all[0]);
+        *largest = best;
+#pragma unroll 4
+    for (int64_t i = threadIdx.x; i < n; i += 1024)
+        share[i] = rows[i].g / best;
 }
 
-// Partial maxima [parts][cols] of the finite |x| 2^(base - row) of a float32
-// matrix's columns.
+// Partial maxima [parts][cols] of the finite magnitudes of a float32 matrix's
+// columns, its rows times a factor each.
 struct ColumnArgs {
     const float *x;
     int64_t rows, cols, ld, each;
-    const int *row, *base;     // or null: |x|
+    const float *row;          // or null
     float *part;
 };
 
@@ -264,12 +262,11 @@ __global__ __launch_bounds__(256) void column_max_kernel(ColumnArgs a)
 {
     const int64_t col = ((int64_t)blockIdx.x * 64 + (threadIdx.x & 63)) * 4;
     const int64_t r0 = blockIdx.y * a.each, r1 = r0 + a.each < a.rows ? r0 + a.each : a.rows;
-    const int base = a.base ? *a.base : 0;
     f32x4 best = 0.0f;
     if (col < a.cols)
 #pragma unroll 4
         for (int64_t r = r0 + (threadIdx.x >> 6); r < r1; r += 4) {
-            const int over = a.row ? base - a.row[r] : 0;
+            const float f = a.row ? a.row[r] : 1.0f;
             f32x4 x = 0.0f;
             if (col + 4 <= a.cols)
                 x = load4(a.x, r * a.ld + col, GPIC_F32);
@@ -280,8 +277,8 @@ __global__ __launch_bounds__(256) void column_max_kernel(ColumnArgs a)
                         x[j] = a.x[r * a.ld + col + j];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const float v = fabsf(x[j]);
-                best[j] = v < INFINITY ? fmaxf(best[j], ldexpf(v, over)) : best[j];
+                const float v = fabsf(x[j] * f);
+                best[j] = v < INFINITY ? fmaxf(best[j], v) : best[j];
             }
         }
     __shared__ f32x4 all[4][64];
@@ -300,8 +297,7 @@ __global__ __launch_bounds__(256) void column_max_kernel(ColumnArgs a)
 }
 
 __global__ __launch_bounds__(256) void column_power_kernel(const float *part, int64_t parts,
-                                                           int64_t cols, const int *base,
-                                                           int *power)
+                                                           int64_t cols, int *power)
 {
     const int64_t col = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
     float best = 0.0f;
@@ -316,7 +312,7 @@ __global__ __launch_bounds__(256) void column_power_kernel(const float *part, in
     if (threadIdx.x < 64 && col < cols) {
         for (int w = 1; w < 4; ++w)
             best = fmaxf(best, all[w][threadIdx.x]);
-        power[col] = power_for(best) + (base ? *base : 0);
+        power[col] = power_for(best);
     }
 }
 
@@ -394,11 +390,9 @@ int64_t max_parts(int64_t rows, int64_t cols)
 struct Backward {
     int64_t piece, pitch;      // columns of a piece, 16-bit values of a row of dZ
     LossRow *rows;
-    float *most = nullptr;
-    int *power = nullptr;      // of the largest |g|
-    int *row_power = nullptr;  // float32: of dZ's rows
+    float *most, *largest, *share;
     Source X, W;               // as the logits' product reads them (W: a piece)
-    Source Xc{}, Wc{};         // float32: as dW's and dX's do
+    Source Xg, Wc{};           // as dW's does, rows times their shares; float32: as dX's
     float *column_part = nullptr;
     void *dZ;
     float *sum_x, *sum_b;      // dX over the pieces, partial column sums of dZ
@@ -410,20 +404,18 @@ struct Backward {
         const int64_t cols = piece < p.v ? piece : p.v;
         pitch = f32 ? split_ld(up64(cols)) : up64(cols);
         rows = static_cast<LossRow *>(c.take((size_t)p.n * sizeof(LossRow)));
-        if (p.dtype != GPIC_BF16) {
-            most = static_cast<float *>(c.take((size_t)((p.n + 255) / 256) * 4));
-            power = static_cast<int *>(c.take(4));
-        }
+        most = static_cast<float *>(c.take((size_t)((p.n + 255) / 256) * 4));
+        largest = static_cast<float *>(c.take(4));
+        share = static_cast<float *>(c.take((size_t)p.n * 4));
         X = Source{x, p.n, p.k, p.ldx, must_pack(p.dtype, p.k, p.ldx, p.aligned16)};
         W = Source{w, cols, p.k, p.ldw, must_pack(p.dtype, p.k, p.ldw, p.aligned16)};
         place(X, p.dtype, c, p.n);
         place(W, p.dtype, c, cols);
+        Xg = Source{x, p.n, p.k, p.ldx, true};
+        Xg.row = share;
+        place(Xg, p.dtype, c, p.k);
         if (f32) {
-            row_power = static_cast<int *>(c.take((size_t)p.n * 4));
-            Xc = Source{x, p.n, p.k, p.ldx, true};
-            Xc.row = row_power;
             Wc = Source{w, cols, p.k, p.ldw, true};
-            place(Xc, p.dtype, c, p.k);
             place(Wc, p.dtype, c, p.k);
             const int64_t px = max_parts(p.n, p.k), pw = max_parts(p.v, p.k);
             column_part = static_cast<float *>(c.take((size_t)(px > pw ? px : pw) * p.k * 4));
@@ -435,7 +427,7 @@ struct Backward {
         const int op = kind_of(p.dtype);
         for (int64_t len : {cols, p.v - (p.v - 1) / piece * piece}) {
             const size_t bx = product_plan(p.n, p.k, len, 1, op, kEpiSum).part_bytes;
-            const size_t bw = product_plan(len, p.k, p.n, 1, op, kEpiLayer).part_bytes;
+            const size_t bw = product_plan(len, p.k, p.n, 1, op, kEpiSum).part_bytes;
             bytes = bytes > bx ? bytes : bx;
             bytes = bytes > bw ? bytes : bw;
         }
@@ -466,16 +458,14 @@ hipError_t launch_few(const FewArgs &a, hipStream_t st)
     return hipGetLastError();
 }
 
-hipError_t launch_columns(const Source &s, const int *row, const int *base, float *part,
-                          hipStream_t st)
+hipError_t launch_columns(const Source &s, float *part, hipStream_t st)
 {
     const int64_t parts = max_parts(s.rows, s.cols), each = (s.rows + parts - 1) / parts;
-    const ColumnArgs a{static_cast<const float *>(s.x), s.rows, s.cols, s.ld, each, row, base,
-                       part};
+    const ColumnArgs a{static_cast<const float *>(s.x), s.rows, s.cols, s.ld, each, s.row, part};
     const int64_t used = (s.rows + each - 1) / each;
     column_max_kernel<<<dim3((unsigned)((s.cols + 255) / 256), (unsigned)used), 256, 0, st>>>(a);
     RUN(hipGetLastError());
-    column_power_kernel<<<(unsigned)((s.cols + 63) / 64), 256, 0, st>>>(part, used, s.cols, base,
+    column_power_kernel<<<(unsigned)((s.cols + 63) / 64), 256, 0, st>>>(part, used, s.cols,
                                                                       s.power);
     return hipGetLastError();
 }
@@ -502,7 +492,7 @@ bool loss_fits(const Loss &p, bool backward)
     const int64_t piece = piece_of(p) < p.v ? piece_of(p) : p.v;
     return product_plan(p.n, piece, p.k, 1, op, kEpiSoft).fits &&
            product_plan(p.n, p.k, piece, 1, op, kEpiSum).fits &&
-           product_plan(piece, p.k, p.n, 1, op, kEpiLayer).fits;
+           product_plan(piece, p.k, p.n, 1, op, kEpiSum).fits;
 }
 
 hipError_t run_loss(const Loss &p, const void *X, const void *W, const void *bias,
@@ -567,28 +557,27 @@ hipError_t run_loss_backward(const Loss &p, const float *dloss, const void *X, c
     const bool f32 = p.dtype == GPIC_F32;
     const int op = kind_of(p.dtype);
     {
-        const RowsArgs a{dloss, loss, lse, targets, p.wide, p.n, p.v, b.rows, b.most, b.row_power};
-        rows_kernel<<<(unsigned)((p.n + 255) / 256), 256, 0, st>>>(a);
+        const RowsArgs a{dloss, loss, lse, targets, p.wide, p.n, p.v, b.rows, b.most};
+        const int64_t blocks = (p.n + 255) / 256;
+        rows_kernel<<<(unsigned)blocks, 256, 0, st>>>(a);
+        RUN(hipGetLastError());
+        shares_kernel<<<1, 1024, 0, st>>>(b.most, blocks, b.rows, p.n, b.largest, b.share);
         RUN(hipGetLastError());
     }
-    if (b.power) {
-        largest_kernel<<<1, 1024, 0, st>>>(b.most, (p.n + 255) / 256, b.power);
-        RUN(hipGetLastError());
+    {
+        b.Xg.pack = dW != nullptr;
+        b.X.pack = b.X.pack && !f32;
+        const Source *list[2] = {&b.X, &b.Xg};
+        if (f32 && dW)
+            RUN(launch_columns(b.Xg, b.column_part, st));
+        RUN(launch_pack(list, 2, p.dtype, st));
+        b.Xg.pack = true;
+        b.X.pack = b.X.pack || f32;
     }
-    if (f32) {
-        if (dW) {
-            RUN(launch_columns(b.Xc, b.row_power, b.power, b.column_part, st));
-            const Source *list[1] = {&b.Xc};
-            RUN(launch_pack(list, 1, p.dtype, st));
-        }
-        if (dX) {
-            Source all = b.Wc;
-            all.rows = p.v;
-            RUN(launch_columns(all, nullptr, nullptr, b.column_part, st));
-        }
-    } else {
-        const Source *list[1] = {&b.X};
-        RUN(launch_pack(list, 1, p.dtype, st));
+    if (f32 && dX) {
+        Source all = b.Wc;
+        all.rows = p.v;
+        RUN(launch_columns(all, b.column_part, st));
     }
     for (int64_t first = 0; first < p.v; first += b.piece) {
         const int64_t len = p.v - first < b.piece ? p.v - first : b.piece;
@@ -621,8 +610,6 @@ hipError_t run_loss_backward(const Loss &p, const float *dloss, const void *X, c
         a.e.bias = bias;
         a.e.rows = b.rows;
         a.e.first = first;
-        a.e.power = f32 ? b.row_power : b.power;
-        a.e.power_step = f32 ? 1 : 0;
         a.e.p_hi = b.dZ;
         a.e.ldp = b.pitch;
         a.e.sums = db ? b.sum_b : nullptr;
@@ -644,8 +631,9 @@ hipError_t run_loss_backward(const Loss &p, const float *dloss, const void *X, c
             x.batch = 1;
             x.part = b.part;
             x.e.dtype = p.dtype;
-            x.e.pa = f32 ? b.row_power : b.power;
             x.e.pb = b.Wc.power;
+            x.e.factor = &b.rows->g;
+            x.e.factor_step = sizeof(LossRow) / sizeof(float);
             x.e.res = first > 0 ? b.sum_x : nullptr;
             x.e.ldr = x.e.ldo = p.k;
             x.e.last = first + len >= p.v;
@@ -655,19 +643,20 @@ hipError_t run_loss_backward(const Loss &p, const float *dloss, const void *X, c
         if (dW) {
             ProductArgs d{};
             d.A = Operand{b.dZ, b.pitch, 0, width};
-            d.B = f32 ? b.Xc.operand(p.dtype) : b.X.operand(p.dtype);
+            d.B = b.Xg.operand(p.dtype);
             d.M = (int)len;
             d.N = (int)p.k;
             d.K = p.n;
             d.batch = 1;
             d.part = b.part;
             d.e.dtype = p.dtype;
-            d.e.act = GPIC_ACT_NONE;
-            d.e.pa = f32 ? nullptr : b.power;
-            d.e.pb = b.Xc.power;
+            d.e.pb = b.Xg.power;
+            d.e.factor = b.largest;
+            d.e.factor_step = 0;
             d.e.ldo = p.k;
+            d.e.last = 1;
             d.e.out = static_cast<char *>(dW) + (size_t)first * p.k * size;
-            RUN(launch_product(kMM, op, kEpiLayer, d, st));
+            RUN(launch_product(kMM, op, kEpiSum, d, st));
         }
     }
     return hipSuccess;

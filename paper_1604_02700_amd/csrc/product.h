@@ -265,6 +265,8 @@ using i32x8 = int __attribute__((ext_vector_type(8), aligned(4)));
 template <int ROWS, int OP, int EPI>
 __device__ __forceinline__ int row_powers(const Epilogue &e, int64_t row0, int64_t M)
 {
+    if (OP != kOpBf16 && EPI == kEpiSum)
+        return kSoftPower;
     if (OP == kOpBf16 || !powered(EPI) || !e.pa)
         return 0;
     static_assert(ROWS <= 64, "a row a lane");
@@ -386,8 +388,11 @@ __device__ __forceinline__ void finish_block(const Epilogue &e, int64_t z, int64
                 continue;
             if (EPI == kEpiLayer && e.res)
                 c[p] = load8(e.res, row * e.ldr + col, dtype, valid);
-            if (EPI == kEpiSum && e.res)
-                c[p] = load8(e.res, row * e.ldr + col, GPIC_F32, valid);
+            if (EPI == kEpiSum) {
+                v[p] = v[p] * e.factor[row * e.factor_step];
+                if (e.res)
+                    c[p] = load8(e.res, row * e.ldr + col, GPIC_F32, valid);
+            }
             if (EPI == kEpiResult && e.is_step) {
                 // decay W - step (beta X + acc)
                 const f32x8 old = load8(e.out, z * e.batch_o + row * e.ldo + col, dtype, valid);
@@ -654,9 +659,11 @@ __device__ __forceinline__ void finish_lse(const ProductArgs &a, const Work &w,
     }
 }
 
-// dZ = g (exp(z - lse) - [target]) of ROWS x COLS logits that the wave has
-// staged at `st`, as the products that follow read it (a row's padding up to
-// 64 columns zeros), and its column sums, unrounded.
+// D = exp(z - lse) - [target] of ROWS x COLS logits that the wave has staged at
+// `st`, as the products that follow read it (a row's padding up to 64 columns
+// zeros), and its column sums times g, unrounded.  The loss's gradient g is left
+// out of what is rounded: it is the same for every row as a rule (1 / n), and its
+// own rounding to 16 bits would be every entry's, up to 2^-8 of the gradients.
 template <int ROWS, int COLS, int OP>
 __device__ __forceinline__ void finish_soft(const Epilogue &e, int64_t row0, int64_t col0,
                                             int64_t M, int64_t N, const float *st)
@@ -687,17 +694,14 @@ __device__ __forceinline__ void finish_soft(const Epilogue &e, int64_t row0, int
         f32x8 d;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            d[j] = info.g * __builtin_amdgcn_exp2f((z[j] + bias[j] - info.lse) * kLog2e);
+            d[j] = __builtin_amdgcn_exp2f((z[j] + bias[j] - info.lse) * kLog2e);
             d[j] = at == j ? info.picked : (bias[j] == -INFINITY ? 0.0f : d[j]);
             d[j] = j < real && info.target >= 0 ? d[j] : 0.0f;
         }
-        sum += d;
-        if (OP != kOpBf16) {
-            const int power = e.power[row * e.power_step];
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                d[j] = ldexpf(d[j], power);
-        }
+        if (info.target >= 0)
+            sum += d * info.g;
+        if (OP != kOpBf16)
+            d = d * (float)(1 << kSoftPower);
         if (OP == kOpSplit) {
             _Float16 *to = static_cast<_Float16 *>(e.p_hi) + row * e.ldp + split_at(col);
             half8 h, l;

@@ -96,7 +96,7 @@ hipError_t launch_product(int modes, int op, int epi, const ProductArgs &a, hipS
     if (p.whole + p.tail == 0)
         return hipSuccess;
     if (epi >= kEpiLse)
-        return launch_product_loss(op, epi, p, a, s);
+        return launch_product_loss(modes, op, epi, p, a, s);
     if (modes == kKK)
         return launch_product_kk(op, epi, p, a, s);
     if (modes == kKM)

@@ -11,8 +11,9 @@ An exponential is off by the error of its argument, 2 e of it and 4 e; sums of
 them pass through at most v / 256 + 40 joins of 4 e; so the others' lse is off
 by dl = max over their probabilities of dz, weighted, and that.  The loss
 softplus(lse' - z_t) has the slope 1 - p_t.  dZ then is off by that times p,
-and is rounded as the products' operand: to the type, float16 no finer than
-2^-39 of the largest |dloss|, float32 to 2^-22 and 2^-39 of the row's |dloss|."""
+and is rounded as the products' operand: to the type, float16 and float32 no
+finer than 2^-39 of the row's |dloss|, float32 to 2^-22.  dW's other operand is X
+times dloss over its largest, rounded to the type where that is not 1."""
 import math
 
 import pytest
@@ -112,13 +113,18 @@ def _check(g, X, W, b, t, dloss, dtype, what):
     rel = dz + lse_err[:, None] + 2 * E * (z - full[:, None]).abs().nan_to_num(posinf=0.0) + 6 * E
     off = gl.abs() * torch.where(one > 0, (pt * dloss_err)[:, None] + 6 * E * rest[:, None], p * rel)
     _close(gr.db, d.sum(0), off.sum(0) + (n / 64 + 32) * E * d.abs().sum(0), dtype, "db")
-    big = float(gl.abs().max())
     if dtype == "f32":
         off = off + 2.0 ** -22 * d.abs() + 2.0 ** -39 * gl.abs()
     else:
-        off = off + U[dtype] * d.abs() + (2.0 ** -39 * big if dtype == "f16" else 0.0)
+        off = off + U[dtype] * d.abs() + (2.0 ** -39 * gl.abs() if dtype == "f16" else 0.0)
     ex = off @ w.abs() + (v + 48) * E * (d.abs() @ w.abs())
     ew = off.t() @ x.abs() + (n + 16) * E * (d.abs().t() @ x.abs())
+    # X times its share of the largest dloss, as dW's operand: a float32 division and
+    # product, rounded to the type (float16: 2^-25 of the largest dloss at least)
+    unlike = bool((gl[gl != 0].abs() != gl.abs().max()).any()) if bool(gl.any()) else False
+    ew += (3 * E + (U[dtype] if unlike else 0.0)) * (d.abs().t() @ x.abs())
+    if dtype == "f16" and unlike:
+        ew += 2.0 ** -25 * gl.abs().max() * (d.abs() / gl.abs().clamp(min=1e-300)).sum(0)[:, None]
     if dtype == "f32":
         ex += 2.0 ** -21 * (d.abs() @ w.abs()) + 2.0 ** -38 * d.abs().sum(1)[:, None] * w.abs().amax(0)
         share = (d.abs() / gl.abs().clamp(min=1e-300)).sum(0)
@@ -225,8 +231,18 @@ def test_non_finite_rows_and_certain_targets(g, n, dtype):
     pad[[1, 4]] = -1
     loss, lse = g.gpic_cross_entropy(bad, W, pad, b, want_lse=True)
     assert not loss[[1, 4]].any()
-    dX = g.gpic_cross_entropy_backward(torch.ones(n, device=DEV), bad, W, pad, loss, lse, b).dX
-    assert not dX[[1, 4]].any() and torch.equal(dX[keep], clean[keep])
+    gr = g.gpic_cross_entropy_backward(torch.ones(n, device=DEV), bad, W, pad, loss, lse, b)
+    assert not gr.dX[[1, 4]].any() and torch.equal(gr.dX[keep], clean[keep])
+    few = g.gpic_cross_entropy(X, W, pad, b, want_lse=True)
+    want = g.gpic_cross_entropy_backward(torch.ones(n, device=DEV), X, W, pad, *few, b)
+    assert torch.equal(gr.dW, want.dW) and torch.equal(gr.db, want.db)
+    # so may rows whose dloss is 0
+    some = torch.ones(n, device=DEV)
+    some[[1, 4]] = 0.0
+    loss, lse = g.gpic_cross_entropy(bad, W, t, b, want_lse=True)
+    gr = g.gpic_cross_entropy_backward(some, bad, W, t, loss, lse, b)
+    assert not gr.dX[[1, 4]].any() and torch.equal(gr.dX[keep], clean[keep])
+    assert torch.equal(gr.dW, want.dW) and torch.equal(gr.db, want.db)
     # a loss far below a float32 rounding of its logits
     b2 = torch.zeros_like(b)
     b2[7] = 60.0
