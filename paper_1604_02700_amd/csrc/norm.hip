@@ -162,7 +162,8 @@ __global__ __launch_bounds__(256) void norm_dots_kernel(NormGradArgs a)
     }
 }
 
-// dX and the partial sums of a strip of 512 columns over `each` rows, four
+// Longer rows: mean(g) and mean(g h) first, then dX and the partial sums of a
+// strip of 512 columns over `each` rows, four
 // rows at a time
 template <int DT>
 __global__ __launch_bounds__(256) void norm_strip_kernel(NormGradArgs a)
@@ -202,6 +203,171 @@ __global__ __launch_bounds__(256) void norm_strip_kernel(NormGradArgs a)
     }
 }
 
+// Eight values of a row as they lie in memory.
+template <int DT>
+struct Chunk {
+    static constexpr int kQuads = DT == GPIC_F32 ? 2 : 1;
+    u32x4 q[kQuads];
+    __device__ __forceinline__ void load(const void *p, int64_t i, int valid)
+    {
+        constexpr int kSize = DT == GPIC_F32 ? 4 : 2;
+        using loose = u32x4 __attribute__((aligned(kSize)));
+        const char *at = static_cast<const char *>(p) + i * kSize;
+        if (valid >= 8) {
+#pragma unroll
+            for (int j = 0; j < kQuads; ++j)
+                q[j] = *reinterpret_cast<const loose *>(at + 16 * j);
+            return;
+        }
+#pragma unroll
+        for (int j = 0; j < kQuads; ++j)
+            q[j] = u32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < valid) {
+                if (DT == GPIC_F32)
+                    q[j / 4 % kQuads][j % 4] = reinterpret_cast<const uint32_t *>(at)[j];
+                else
+                    q[0][j / 2] |= (uint32_t)reinterpret_cast<const uint16_t *>(at)[j]
+                                   << (16 * (j & 1));
+            }
+    }
+    __device__ __forceinline__ f32x8 floats() const
+    {
+        if constexpr (DT == GPIC_F32) {
+            const f32x4 a = __builtin_bit_cast(f32x4, q[0]), b = __builtin_bit_cast(f32x4, q[1]);
+            return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+        } else if constexpr (DT == GPIC_F16) {
+            return __builtin_convertvector(__builtin_bit_cast(half8, q[0]), f32x8);
+        } else {
+            return __builtin_convertvector(__builtin_bit_cast(bfrag8, q[0]), f32x8);
+        }
+    }
+};
+
+// The same in one pass over X and dY, for rows that LANES lanes hold in HOLD
+// groups of eight columns each: the next row is on its way while one is
+// finished, and the columns' sums stay in registers until the rows are through,
+// then meet in LDS.  Groups of lanes take rows in turn over the whole grid.
+template <int DT, int LANES, int HOLD, int THREADS>
+__global__ __launch_bounds__(THREADS) void norm_grad_kernel(NormGradArgs a)
+{
+    constexpr int kRows = THREADS / LANES, kWaves = THREADS / 64;
+    constexpr bool kWide = LANES > 64;
+    // sums of rows across waves (two sets in turn), or of columns
+    __shared__ float2 part[kWide ? 2 : 1][kWide ? LANES / 64 : 1];
+    __shared__ f32x8 cols[kWide ? 1 : kWaves][kWide ? 1 : 64];
+    const int at = threadIdx.x % LANES;
+    const float inv = 1.0f / (float)a.k;
+    int valid[HOLD];
+#pragma unroll
+    for (int h = 0; h < HOLD; ++h) {
+        const int64_t left = a.k - (int64_t)(at + h * LANES) * 8;
+        valid[h] = left <= 0 ? 0 : (left < 8 ? (int)left : 8);
+    }
+    Chunk<DT> w[HOLD], x[HOLD], d[HOLD], nx[HOLD], nd[HOLD];
+    f32x8 sw[HOLD], sb[HOLD];
+#pragma unroll
+    for (int h = 0; h < HOLD; ++h) {
+        sw[h] = sb[h] = 0.0f;
+        if (a.w)
+            w[h].load(a.w, (at + h * LANES) * 8, valid[h]);
+    }
+    float2 st, nst;
+    auto fetch = [&](int64_t r) {
+        nst = reinterpret_cast<const float2 *>(a.stats)[r];
+#pragma unroll
+        for (int h = 0; h < HOLD; ++h) {
+            nx[h].load(a.X, r * a.ldx + (at + h * LANES) * 8, valid[h]);
+            nd[h].load(a.dY, r * a.ldy + (at + h * LANES) * 8, valid[h]);
+        }
+    };
+    const int64_t step = (int64_t)gridDim.x * kRows;
+    int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES;
+    if (r < a.n)
+        fetch(r);
+    for (int turn = 0; r < a.n; r += step, turn ^= 1) {
+        st = nst;
+#pragma unroll
+        for (int h = 0; h < HOLD; ++h) {
+            x[h] = nx[h];
+            d[h] = nd[h];
+        }
+        if (r + step < a.n)
+            fetch(r + step);
+        float s = 0.0f, t = 0.0f;
+#pragma unroll
+        for (int h = 0; h < HOLD; ++h) {
+            const f32x8 dy = d[h].floats(), hx = (x[h].floats() - st.x) * st.y;
+            const f32x8 g = a.w ? dy * w[h].floats() : dy;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (j < valid[h]) {
+                    s += g[j];
+                    t += g[j] * hx[j];
+                    sw[h][j] += dy[j] * hx[j];
+                    sb[h][j] += dy[j];
+                }
+        }
+        if (a.dX) {
+#pragma unroll
+            for (int o = (kWide ? 64 : LANES) / 2; o > 0; o >>= 1) {
+                s += __shfl_xor(s, o, 64);
+                t += __shfl_xor(t, o, 64);
+            }
+            if (kWide) {
+                if ((threadIdx.x & 63) == 0)
+                    part[turn & (kWide ? 1 : 0)][threadIdx.x >> 6] = make_float2(s, t);
+                __syncthreads();
+                s = t = 0.0f;
+#pragma unroll
+                for (int i = 0; i < (kWide ? LANES / 64 : 1); ++i) {
+                    s += part[turn & (kWide ? 1 : 0)][i].x;
+                    t += part[turn & (kWide ? 1 : 0)][i].y;
+                }
+            }
+            s *= inv;
+            t *= inv;
+#pragma unroll
+            for (int h = 0; h < HOLD; ++h) {
+                if (!valid[h])
+                    continue;
+                const f32x8 dy = d[h].floats(), hx = (x[h].floats() - st.x) * st.y;
+                const f32x8 g = a.w ? dy * w[h].floats() : dy;
+                store8(a.dX, r * a.k + (at + h * LANES) * 8, (g - s - hx * t) * st.y, DT,
+                       valid[h]);
+            }
+        }
+    }
+    if (!a.sums)
+        return;
+#pragma unroll
+    for (int i = 0; i < 2 * HOLD; ++i) {
+        const int h = i >> 1;
+        f32x8 v = i & 1 ? sb[h] : sw[h];
+        float *to = a.sums + ((int64_t)blockIdx.x * 2 + (i & 1)) * a.k;
+        if (kWide) {                     // a workgroup's rows are one after another
+            if (valid[h])
+                store8(to, (at + h * LANES) * 8, v, GPIC_F32, valid[h]);
+            continue;
+        }
+#pragma unroll
+        for (int o = LANES; o < 64; o <<= 1)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                v[j] += __shfl_xor(v[j], o, 64);
+        __syncthreads();
+        cols[kWide ? 0 : threadIdx.x >> 6][kWide ? 0 : threadIdx.x & 63] = v;
+        __syncthreads();
+        if (threadIdx.x < LANES && valid[h]) {
+#pragma unroll
+            for (int o = 1; o < kWaves; ++o)
+                v += cols[kWide ? 0 : o][kWide ? 0 : threadIdx.x];
+            store8(to, (at + h * LANES) * 8, v, GPIC_F32, valid[h]);
+        }
+    }
+}
+
 // dW and db (grid.y) from the partial sums, in float64 in a fixed order: 64
 // columns a workgroup, sixteen runs of parts
 __global__ __launch_bounds__(1024) void norm_join_kernel(const float *sums, int64_t parts,
@@ -236,13 +402,33 @@ unsigned capped(int64_t blocks)
     return (unsigned)(blocks < 1 ? 1 : (blocks > kMostBlocks ? kMostBlocks : blocks));
 }
 
-// How the strips' rows are cut: about 2,048 workgroups, none of fewer than 16
-// rows.
-struct Strips {
+// How the gradients' rows are cut: one pass by groups of lanes that hold a row
+// (up to 8,192 columns), or strips of 512 columns.
+struct Cut {
+    int lanes, hold;           // 0: strips
     int64_t strips, each, parts;
-    explicit Strips(const Norm &p)
+    explicit Cut(const Norm &p)
     {
         strips = (p.k + 511) / 512;
+        lanes = hold = 0;
+        each = 0;
+        static const int kFit[][2] = {{16, 1}, {16, 2}, {64, 1}, {64, 2},
+                                      {64, 4}, {256, 2}, {256, 4}};
+        for (auto &f : kFit)
+            if (p.k <= f[0] * f[1] * 8) {
+                lanes = f[0];
+                hold = f[1];
+                break;
+            }
+        if (lanes) {
+            // two waves to each of the card's 1,024 vector units, fewer where
+            // rows are
+            const int rows = lanes > 64 ? 1 : 512 / lanes;
+            parts = (p.n + rows - 1) / rows;
+            const int64_t most = lanes > 64 ? 512 : 256;
+            parts = parts < most ? parts : most;
+            return;
+        }
         int64_t want = 2048 / strips;
         want = want < (p.n + 15) / 16 ? want : (p.n + 15) / 16;
         want = want < 1 ? 1 : want;
@@ -255,8 +441,8 @@ struct Backward {
     float *dots, *sums;
     Backward(const Norm &p, Cursor &c)
     {
-        const Strips s(p);
-        dots = static_cast<float *>(c.take((size_t)p.n * 8));
+        const Cut s(p);
+        dots = s.lanes ? nullptr : static_cast<float *>(c.take((size_t)p.n * 8));
         sums = static_cast<float *>(c.take((size_t)s.parts * 2 * p.k * 4));
     }
 };
@@ -284,20 +470,39 @@ hipError_t launch_norm(const NormArgs &a, hipStream_t st)
 }
 
 template <int DT>
-hipError_t launch_gradients(const NormGradArgs &a, int64_t parts, hipStream_t st)
+hipError_t launch_gradients(const NormGradArgs &a, const Cut &cut, hipStream_t st)
 {
+    const unsigned blocks = (unsigned)cut.parts;
+    switch (cut.lanes * 8 + cut.hold) {
+    case 16 * 8 + 1:
+        norm_grad_kernel<DT, 16, 1, 512><<<blocks, 512, 0, st>>>(a);
+        return hipGetLastError();
+    case 16 * 8 + 2:
+        norm_grad_kernel<DT, 16, 2, 512><<<blocks, 512, 0, st>>>(a);
+        return hipGetLastError();
+    case 64 * 8 + 1:
+        norm_grad_kernel<DT, 64, 1, 512><<<blocks, 512, 0, st>>>(a);
+        return hipGetLastError();
+    case 64 * 8 + 2:
+        norm_grad_kernel<DT, 64, 2, 512><<<blocks, 512, 0, st>>>(a);
+        return hipGetLastError();
+    case 64 * 8 + 4:
+        norm_grad_kernel<DT, 64, 4, 512><<<blocks, 512, 0, st>>>(a);
+        return hipGetLastError();
+    case 256 * 8 + 2:
+        norm_grad_kernel<DT, 256, 2, 256><<<blocks, 256, 0, st>>>(a);
+        return hipGetLastError();
+    case 256 * 8 + 4:
+        norm_grad_kernel<DT, 256, 4, 256><<<blocks, 256, 0, st>>>(a);
+        return hipGetLastError();
+    }
     if (a.dX) {
-        if (a.k <= 512)
-            norm_dots_kernel<DT, 16><<<capped((a.n + 15) / 16), 256, 0, st>>>(a);
-        else if (a.k <= 4096)
-            norm_dots_kernel<DT, 64><<<capped((a.n + 3) / 4), 256, 0, st>>>(a);
-        else
-            norm_dots_kernel<DT, 256><<<capped(a.n), 256, 0, st>>>(a);
+        norm_dots_kernel<DT, 256><<<capped(a.n), 256, 0, st>>>(a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess)
             return e;
     }
-    norm_strip_kernel<DT><<<(unsigned)(parts * a.strips), 256, 0, st>>>(a);
+    norm_strip_kernel<DT><<<(unsigned)(cut.parts * a.strips), 256, 0, st>>>(a);
     return hipGetLastError();
 }
 
@@ -327,13 +532,13 @@ hipError_t run_norm_backward(const Norm &p, const void *dY, const void *X, const
 {
     Cursor c{static_cast<char *>(ws)};
     const Backward b(p, c);
-    const Strips s(p);
+    const Cut s(p);
     if (p.n > 0 && (dX || dW || db)) {
         const NormGradArgs a{dY, X, w, stats, dX, b.dots, dW || db ? b.sums : nullptr, p.n, p.k,
                              p.ldx, p.ldy, s.strips, s.each};
-        const hipError_t e = p.dtype == GPIC_F32    ? launch_gradients<GPIC_F32>(a, s.parts, st)
-                             : p.dtype == GPIC_F16 ? launch_gradients<GPIC_F16>(a, s.parts, st)
-                                                   : launch_gradients<GPIC_BF16>(a, s.parts, st);
+        const hipError_t e = p.dtype == GPIC_F32    ? launch_gradients<GPIC_F32>(a, s, st)
+                             : p.dtype == GPIC_F16 ? launch_gradients<GPIC_F16>(a, s, st)
+                                                   : launch_gradients<GPIC_BF16>(a, s, st);
         if (e != hipSuccess)
             return e;
     }
