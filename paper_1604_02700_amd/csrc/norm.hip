@@ -48,10 +48,132 @@ __device__ __forceinline__ f32x8 read8(const void *p, int64_t row_at, int64_t co
     return load8(p, row_at + col, DT, left < 8 ? (int)left : 8);
 }
 
-// LANES lanes a row, eight columns at a time; up to kHold groups of them stay
-// in registers, what a row has beyond is read again.  The mean is found first
-// and corrected by the deviations' own sum, so that rows far from zero lose
-// nothing.
+// Eight values of a row as they lie in memory.
+template <int DT>
+struct Chunk {
+    static constexpr int kQuads = DT == GPIC_F32 ? 2 : 1;
+    u32x4 q[kQuads];
+    __device__ __forceinline__ void load(const void *p, int64_t i, int valid)
+    {
+        constexpr int kSize = DT == GPIC_F32 ? 4 : 2;
+        using loose = u32x4 __attribute__((aligned(kSize)));
+        const char *at = static_cast<const char *>(p) + i * kSize;
+        if (valid >= 8) {
+#pragma unroll
+            for (int j = 0; j < kQuads; ++j)
+                q[j] = *reinterpret_cast<const loose *>(at + 16 * j);
+            return;
+        }
+#pragma unroll
+        for (int j = 0; j < kQuads; ++j)
+            q[j] = u32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < valid) {
+                if (DT == GPIC_F32)
+                    q[j / 4 % kQuads][j % 4] = reinterpret_cast<const uint32_t *>(at)[j];
+                else
+                    q[0][j / 2] |= (uint32_t)reinterpret_cast<const uint16_t *>(at)[j]
+                                   << (16 * (j & 1));
+            }
+    }
+    __device__ __forceinline__ f32x8 floats() const
+    {
+        if constexpr (DT == GPIC_F32) {
+            const f32x4 a = __builtin_bit_cast(f32x4, q[0]), b = __builtin_bit_cast(f32x4, q[1]);
+            return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+        } else if constexpr (DT == GPIC_F16) {
+            return __builtin_convertvector(__builtin_bit_cast(half8, q[0]), f32x8);
+        } else {
+            return __builtin_convertvector(__builtin_bit_cast(bfrag8, q[0]), f32x8);
+        }
+    }
+};
+
+// Rows that LANES lanes hold in HOLD groups of eight columns each, with the next
+// row on its way while one is finished: the mean, then the deviations from it,
+// whose own sum corrects it, so that rows far from zero lose nothing.  Groups of
+// lanes take rows in turn over the whole grid.
+template <int DT, int LANES, int HOLD>
+__global__ __launch_bounds__(256) void norm_rows_kernel(NormArgs a)
+{
+    constexpr int kRows = 256 / LANES;
+    __shared__ float2 part[LANES > 64 ? LANES / 64 : 1];
+    const int at = threadIdx.x % LANES;
+    const float inv = 1.0f / (float)a.k;
+    int valid[HOLD];
+#pragma unroll
+    for (int h = 0; h < HOLD; ++h) {
+        const int64_t left = a.k - (int64_t)(at + h * LANES) * 8;
+        valid[h] = left <= 0 ? 0 : (left < 8 ? (int)left : 8);
+    }
+    Chunk<DT> w[HOLD], b[HOLD], x[HOLD], next[HOLD];
+    auto fetch = [&](int64_t r) {
+#pragma unroll
+        for (int h = 0; h < HOLD; ++h)
+            next[h].load(a.X, r * a.ldx + (at + h * LANES) * 8, valid[h]);
+    };
+    const int64_t step = (int64_t)gridDim.x * kRows;
+    int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES;
+    if (r < a.n)
+        fetch(r);
+#pragma unroll
+    for (int h = 0; h < HOLD; ++h) {
+        if (a.w)
+            w[h].load(a.w, (at + h * LANES) * 8, valid[h]);
+        if (a.b)
+            b[h].load(a.b, (at + h * LANES) * 8, valid[h]);
+    }
+    for (; r < a.n; r += step) {
+#pragma unroll
+        for (int h = 0; h < HOLD; ++h)
+            x[h] = next[h];
+        if (r + step < a.n)
+            fetch(r + step);
+        float s = 0.0f, t = 0.0f;
+#pragma unroll
+        for (int h = 0; h < HOLD; ++h) {
+            const f32x8 v = x[h].floats();
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                s += v[j];                   // (zeros beyond the row)
+        }
+        row_sums<LANES>(s, t, part);
+        float mean = s * inv;
+        s = t = 0.0f;
+#pragma unroll
+        for (int h = 0; h < HOLD; ++h) {
+            const f32x8 v = x[h].floats();
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float d = j < valid[h] ? v[j] - mean : 0.0f;
+                s += d;
+                t += d * d;
+            }
+        }
+        row_sums<LANES>(s, t, part);
+        const float off = s * inv;
+        mean += off;
+        const float var = fmaxf(t * inv - off * off, 0.0f);
+        const float rs = 1.0f / sqrtf((t != t ? t : var) + a.eps);
+        if (a.stats && at == 0)
+            reinterpret_cast<float2 *>(a.stats)[r] = make_float2(mean, rs);
+#pragma unroll
+        for (int h = 0; h < HOLD; ++h) {
+            if (!valid[h])
+                continue;
+            f32x8 y = (x[h].floats() - mean) * rs;
+            if (a.w)
+                y = y * w[h].floats();
+            if (a.b)
+                y = y + b[h].floats();
+            store8(a.Y, r * a.ldy + (at + h * LANES) * 8, y, DT, valid[h]);
+        }
+    }
+}
+
+// Longer rows: a workgroup a row, eight columns at a time a lane; up to kHold
+// groups of them stay in registers, what a row has beyond is read again.
 template <int DT, int LANES>
 __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_kernel(NormArgs a)
 {
@@ -202,48 +324,6 @@ __global__ __launch_bounds__(256) void norm_strip_kernel(NormGradArgs a)
         store8(a.sums + (part * 2 + which) * a.k, col, s, GPIC_F32, valid);
     }
 }
-
-// Eight values of a row as they lie in memory.
-template <int DT>
-struct Chunk {
-    static constexpr int kQuads = DT == GPIC_F32 ? 2 : 1;
-    u32x4 q[kQuads];
-    __device__ __forceinline__ void load(const void *p, int64_t i, int valid)
-    {
-        constexpr int kSize = DT == GPIC_F32 ? 4 : 2;
-        using loose = u32x4 __attribute__((aligned(kSize)));
-        const char *at = static_cast<const char *>(p) + i * kSize;
-        if (valid >= 8) {
-#pragma unroll
-            for (int j = 0; j < kQuads; ++j)
-                q[j] = *reinterpret_cast<const loose *>(at + 16 * j);
-            return;
-        }
-#pragma unroll
-        for (int j = 0; j < kQuads; ++j)
-            q[j] = u32x4{0, 0, 0, 0};
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (j < valid) {
-                if (DT == GPIC_F32)
-                    q[j / 4 % kQuads][j % 4] = reinterpret_cast<const uint32_t *>(at)[j];
-                else
-                    q[0][j / 2] |= (uint32_t)reinterpret_cast<const uint16_t *>(at)[j]
-                                   << (16 * (j & 1));
-            }
-    }
-    __device__ __forceinline__ f32x8 floats() const
-    {
-        if constexpr (DT == GPIC_F32) {
-            const f32x4 a = __builtin_bit_cast(f32x4, q[0]), b = __builtin_bit_cast(f32x4, q[1]);
-            return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
-        } else if constexpr (DT == GPIC_F16) {
-            return __builtin_convertvector(__builtin_bit_cast(half8, q[0]), f32x8);
-        } else {
-            return __builtin_convertvector(__builtin_bit_cast(bfrag8, q[0]), f32x8);
-        }
-    }
-};
 
 // The same in one pass over X and dY, for rows that LANES lanes hold in HOLD
 // groups of eight columns each: the next row is on its way while one is
@@ -396,6 +476,7 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(const float *sums, int6
 
 // ------------------------------------------------------------------- host
 constexpr int64_t kMostBlocks = 1 << 20;
+constexpr int64_t kNormBlocks = 1024;
 
 unsigned capped(int64_t blocks)
 {
@@ -447,25 +528,36 @@ struct Backward {
     }
 };
 
+template <int DT, int LANES, int HOLD>
+void launch_rows(const NormArgs &a, hipStream_t st)
+{
+    constexpr int kRows = 256 / LANES;
+    const int64_t blocks = (a.n + kRows - 1) / kRows;
+    norm_rows_kernel<DT, LANES, HOLD>
+        <<<(unsigned)(blocks < kNormBlocks ? blocks : kNormBlocks), 256, 0, st>>>(a);
+}
+
 template <int DT>
 hipError_t launch_norm(const NormArgs &a, hipStream_t st)
 {
-    // lanes that hold a row in registers, more of them where rows are few
-    int lanes = a.k <= 512 ? 16 : (a.k <= 2048 ? 64 : (a.k <= 8192 ? 256 : 1024));
-    if (lanes == 16 && a.n < 4096 && a.k > 128)
-        lanes = 64;
-    if (lanes == 64 && a.n < 1024 && a.k > 512)
-        lanes = 256;
-    const int rows = lanes > 256 ? 1 : 256 / lanes;
-    const unsigned blocks = capped((a.n + rows - 1) / rows);
-    if (lanes == 16)
-        norm_kernel<DT, 16><<<blocks, 256, 0, st>>>(a);
-    else if (lanes == 64)
-        norm_kernel<DT, 64><<<blocks, 256, 0, st>>>(a);
-    else if (lanes == 256)
-        norm_kernel<DT, 256><<<blocks, 256, 0, st>>>(a);
+    if (a.k > 8192)
+        norm_kernel<DT, 1024><<<capped(a.n), 1024, 0, st>>>(a);
+    else if (a.k > 4096)
+        launch_rows<DT, 256, 4>(a, st);
+    else if (a.k > 2048)
+        launch_rows<DT, 256, 2>(a, st);
+    else if (a.k > 512 && a.n < 1024)
+        launch_rows<DT, 256, 1>(a, st);
+    else if (a.k > 1024)
+        launch_rows<DT, 64, 4>(a, st);
+    else if (a.k > 512)
+        launch_rows<DT, 64, 2>(a, st);
+    else if (a.k > 256)
+        launch_rows<DT, 64, 1>(a, st);
+    else if (a.k > 128)
+        launch_rows<DT, 16, 2>(a, st);
     else
-        norm_kernel<DT, 1024><<<blocks, 1024, 0, st>>>(a);
+        launch_rows<DT, 16, 1>(a, st);
     return hipGetLastError();
 }
 
