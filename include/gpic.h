@@ -655,7 +655,7 @@ typedef struct gpic_embedding_params {
 gpic_status gpic_embedding(const gpic_embedding_params *p, const void *ids, const void *T, void *Y,
                            void *stream);
 
-/* Workspace bytes of the gradient (0 for up to 1,024 ids, which are not sorted,
+/* Workspace bytes of the gradient (0 for up to 2,048 ids, which are not sorted,
  * and for parameters that the call refuses). */
 size_t gpic_embedding_workspace_bytes(const gpic_embedding_params *p);
 

@@ -4,18 +4,17 @@
 //
 // The gradient adds in float32 in a fixed order: the ids are sorted with
 // their positions (stable), every row of the table finds its run, and a wave
-// adds a run of up to 64 rows of dY, eight columns a lane.  Longer runs
+// adds a run of up to 16 rows of dY, eight columns a lane.  Longer runs
 // (tokens as frequent as words are) are cut where the sorted positions pass
-// multiples of 64; the cuts' sums are added by a workgroup in a second launch.
+// multiples of 16; the cuts' sums are added by a workgroup in a second launch.
 // A few ids are not sorted: each position compares itself with all of them.
-#include "common.h"
 #include "training.h"
 
 namespace gpic {
 namespace {
 
-constexpr int kRun = 64;               // longest run that one wave adds
-constexpr int64_t kFewIds = 1024;      // compared one by one
+constexpr int kRun = 16;               // longest run that one wave adds
+constexpr int64_t kFewIds = 2048;      // compared one by one
 
 struct TableArgs {
     const void *ids, *T, *dY;
@@ -24,7 +23,7 @@ struct TableArgs {
     float scale;
     int accumulate;
     // sorted: keys, positions, where each row's run starts, cut runs' sums
-    const uint64_t *key;
+    const uint32_t *key;
     const int32_t *pos;
     uint32_t *start;
     float *part;
@@ -45,6 +44,45 @@ __device__ __forceinline__ int valid8(int64_t col, int64_t cols)
     const int64_t left = cols - col;
     return left <= 0 ? 0 : (left < 8 ? (int)left : 8);
 }
+
+// Eight columns that a lane adds: its own, or, where a row ends within them, the
+// row's last eight, of which it keeps those from `skip` on; beyond the row the
+// first eight, of which it keeps none.  So no load of a run depends on a branch.
+// TINY: rows of fewer than eight columns.
+template <int DT, bool TINY>
+struct Window {
+    int64_t col;
+    int skip, tiny;
+    __device__ __forceinline__ Window(int64_t c, int64_t k)
+    {
+        tiny = TINY ? (int)k : 8;
+        skip = c >= k ? 8 : 0;
+        col = c >= k ? 0 : c;
+        if (!TINY && c < k && c + 8 > k) {
+            col = k - 8;
+            skip = (int)(c - col);
+        }
+    }
+    __device__ __forceinline__ f32x8 load(const void *p, int64_t row_at) const
+    {
+        return load8(p, row_at + col, DT, TINY ? tiny : 8);
+    }
+    __device__ __forceinline__ f32x8 load_sum(const float *p, int64_t row_at) const
+    {
+        return load8(p, row_at + col, GPIC_F32, TINY ? tiny : 8);
+    }
+    __device__ __forceinline__ void store(void *p, int64_t row_at, f32x8 v, int dtype) const
+    {
+        if (skip == 0) {
+            store8(p, row_at + col, v, dtype, TINY ? tiny : 8);
+            return;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j >= skip)
+                store1(p, row_at + col + j, v[j], dtype);
+    }
+};
 
 template <int DT, bool WIDE>
 __global__ __launch_bounds__(256) void lookup_kernel(TableArgs a)
@@ -73,20 +111,72 @@ __global__ __launch_bounds__(256) void zero_rows_kernel(TableArgs a)
     }
 }
 
-// dT's row v from column col on, or what it held and that
-template <int DT>
-__device__ __forceinline__ void put(const TableArgs &a, int64_t v, int64_t col, f32x8 sum,
-                                    int valid)
+// dT's row v, or what it held and that
+template <int DT, bool TINY>
+__device__ __forceinline__ void put(const TableArgs &a, int64_t v, const Window<DT, TINY> &w,
+                                    f32x8 sum)
 {
+    if (w.skip == 8)
+        return;
     sum = sum * a.scale;
     if (a.accumulate)
-        sum = sum + load8(a.dT, v * a.ldt + col, DT, valid);
-    store8(a.dT, v * a.ldt + col, sum, DT, valid);
+        sum = sum + w.load(a.dT, v * a.ldt);
+    w.store(a.dT, v * a.ldt, sum, DT);
+}
+
+// What earlier launches wrote, at an index that the wave shares: through the
+// scalar cache, whose loads return sooner than a vector's.
+template <class T>
+__device__ __forceinline__ T shared_load(const T *p, int64_t i)
+{
+    return *(const __attribute__((address_space(4))) T *)(uintptr_t)(p + i);
+}
+__device__ __forceinline__ int64_t wave_index()
+{
+    return (int64_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+}
+
+// sum[h] += load(item, h) for item = get(j0 .. j1 - 1), in order.  A batch's loads
+// are all under way before the first is added; the last one loads its last item
+// again in place of what it lacks.
+template <int COUNT, int HOLD, class Get, class Load>
+__device__ __forceinline__ void add_batch(int64_t j, int64_t j1, Get get, Load load,
+                                          f32x8 (&sum)[HOLD])
+{
+    f32x8 v[COUNT][HOLD];
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) {
+        const int64_t item = get(j + i < j1 ? j + i : j1 - 1);
+#pragma unroll
+        for (int h = 0; h < HOLD; ++h)
+            v[i][h] = load(item, h);
+    }
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i)
+        if (j + i < j1)
+#pragma unroll
+            for (int h = 0; h < HOLD; ++h)
+                sum[h] += v[i][h];
+}
+
+template <int HOLD, class Get, class Load>
+__device__ __forceinline__ void add_batches(int64_t j0, int64_t j1, Get get, Load load,
+                                            f32x8 (&sum)[HOLD])
+{
+    constexpr int kMost = HOLD > 1 ? 4 : 8;
+    int64_t j = j0;
+    for (; j1 - j > 2; j += kMost)
+        add_batch<kMost>(j, j1, get, load, sum);
+    if (j1 - j == 2)
+        add_batch<2>(j, j1, get, load, sum);
+    else if (j1 - j == 1)
+        add_batch<1>(j, j1, get, load, sum);
 }
 
 // A workgroup for every position and strip of 512 columns: where no earlier
-// position has the same id, the waves add a quarter each of the ones that do.
-template <int DT, bool WIDE>
+// position has the same id, its waves list the ones that do and add a quarter
+// each.
+template <int DT, bool WIDE, bool TINY>
 __global__ __launch_bounds__(256) void few_ids_kernel(TableArgs a)
 {
     const int64_t i = blockIdx.x / a.strips, strip = blockIdx.x % a.strips;
@@ -98,38 +188,144 @@ __global__ __launch_bounds__(256) void few_ids_kernel(TableArgs a)
         earlier |= id_at<WIDE>(a.ids, j, a.rows) == id;
     if (__syncthreads_or(earlier))
         return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t col = (strip * 64 + lane) * 8;
-    const int valid = valid8(col, a.k);
+    __shared__ int list[4][kFewIds / 4 + 64], found[4];
+    const int lane = threadIdx.x & 63, wave = (int)wave_index();
     const int64_t each = (a.n - i + 255) / 256 * 64;
     const int64_t j0 = i + wave * each, j1 = j0 + each < a.n ? j0 + each : a.n;
-    f32x8 sum = 0.0f;
+    int count = 0;
     for (int64_t j = j0; j < j1; j += 64) {
-        uint64_t same = __ballot(j + lane < j1 && id_at<WIDE>(a.ids, j + lane, a.rows) == id);
-        while (same) {
-            const int64_t row = j + __builtin_ctzll(same);
-            same &= same - 1;
-            if (valid)
-                sum += load8(a.dY, row * a.ldy + col, DT, valid);
-        }
+        const bool same = j + lane < j1 && id_at<WIDE>(a.ids, j + lane, a.rows) == id;
+        const uint64_t all = __ballot(same);
+        if (same)
+            list[wave][count + __popcll(all & ~(~0ull << lane))] = (int)(j + lane);
+        count += __popcll(all);
     }
-    __shared__ f32x8 part[4][64];
-    part[wave][lane] = sum;
+    if (lane == 0)
+        found[wave] = count;
     __syncthreads();
-    if (wave == 0 && valid)
-        put<DT>(a, id, col, ((part[0][lane] + part[1][lane]) + part[2][lane]) + part[3][lane],
-                valid);
+    const int e1 = found[0], e2 = e1 + found[1], e3 = e2 + found[2], total = e3 + found[3];
+    const Window<DT, TINY> window((strip * 64 + lane) * 8, a.k);
+    f32x8 sum[1];
+    sum[0] = 0.0f;
+    add_batches(total * wave / 4, total * (wave + 1) / 4,
+                [&](int64_t e) {
+                    const int w = (e >= e1) + (e >= e2) + (e >= e3);
+                    return (int64_t)list[w][e - (w == 0 ? 0 : (w == 1 ? e1 : (w == 2 ? e2 : e3)))];
+                },
+                [&](int64_t row, int) { return window.load(a.dY, row * a.ldy); }, sum);
+    __shared__ f32x8 part[4][64];
+    part[wave][lane] = sum[0];
+    __syncthreads();
+    if (wave == 0)
+        put(a, id, window, ((part[0][lane] + part[1][lane]) + part[2][lane]) + part[3][lane]);
+}
+
+// ------------------------------------------------------------------- sort
+// Stable sort of (id, position) by 8-bit digits, two launches a digit: a
+// workgroup counts its tile's digits; then every workgroup finds its tile's
+// places from all tiles' counts (at most 256, so no launch scans them) and
+// scatters, its keys ranked within their wave by ballots over the digit's bits.
+// 32,768 ids below 50,000: 2 x (4 + 6) us, where a scan of the counts by one
+// workgroup between them took another 12 each.
+constexpr int kMostTiles = 256;
+
+struct SortArgs {
+    const void *ids;           // of the first digit's pass, else null
+    int64_t n, rows;
+    const uint32_t *key_in;
+    const int32_t *pos_in;
+    uint32_t *key;
+    int32_t *pos;
+    uint32_t *counts;          // [tiles][256]
+    int64_t tile;              // keys, a multiple of 256
+    int shift;
+};
+
+template <bool WIDE>
+__device__ __forceinline__ uint32_t key_at(const SortArgs &a, int64_t i)
+{
+    if (!a.ids)
+        return a.key_in[i];
+    const int64_t id = id_at<WIDE>(a.ids, i, a.rows);
+    return (uint32_t)(id < 0 ? a.rows : id);             // padding sorts last
 }
 
 template <bool WIDE>
-__global__ __launch_bounds__(256) void keys_kernel(const void *ids, int64_t n, int64_t rows,
-                                                   uint64_t *key, int32_t *pos)
+__global__ __launch_bounds__(256) void count_digits_kernel(SortArgs a)
 {
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n;
-         i += (int64_t)gridDim.x * 256) {
-        const int64_t id = id_at<WIDE>(ids, i, rows);
-        key[i] = (uint64_t)(id < 0 ? rows : id);       // padding sorts last
-        pos[i] = (int32_t)i;
+    __shared__ uint32_t count[256];
+    count[threadIdx.x] = 0;
+    __syncthreads();
+    const int64_t i0 = blockIdx.x * a.tile, i1 = i0 + a.tile < a.n ? i0 + a.tile : a.n;
+#pragma unroll 4
+    for (int64_t i = i0 + threadIdx.x; i < i1; i += 256)
+        atomicAdd(&count[(key_at<WIDE>(a, i) >> a.shift) & 255u], 1u);
+    __syncthreads();
+    a.counts[(int64_t)blockIdx.x * 256 + threadIdx.x] = count[threadIdx.x];
+}
+
+template <bool WIDE>
+__global__ __launch_bounds__(256) void scatter_digits_kernel(SortArgs a)
+{
+    __shared__ uint32_t base[256], total[256], wave_count[4][256];
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    uint32_t before = 0, all = 0;
+#pragma unroll 8
+    for (int i = 0; i < (int)gridDim.x; ++i) {
+        const uint32_t c = a.counts[(int64_t)i * 256 + t];
+        before += i < (int)blockIdx.x ? c : 0;
+        all += c;
+    }
+    total[t] = all;
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+        wave_count[w][t] = 0;
+    __syncthreads();
+    for (int o = 1; o < 256; o <<= 1) {
+        const uint32_t x = t >= o ? total[t - o] : 0;
+        __syncthreads();
+        total[t] += x;
+        __syncthreads();
+    }
+    base[t] = total[t] - all + before;
+    __syncthreads();
+    const int64_t i0 = blockIdx.x * a.tile, i1 = i0 + a.tile < a.n ? i0 + a.tile : a.n;
+    const uint64_t lower = lane == 0 ? 0 : ~0ull >> (64 - lane);
+    for (int64_t first = i0; first < i1; first += 256) {
+        const int64_t i = first + t;
+        const bool live = i < i1;
+        uint32_t key = 0;
+        int32_t pos = 0;
+        if (live) {
+            key = key_at<WIDE>(a, i);
+            pos = a.ids ? (int32_t)i : a.pos_in[i];
+        }
+        const uint32_t digit = (key >> a.shift) & 255u;
+        uint64_t peers = __ballot(live);
+#pragma unroll
+        for (int bit = 0; bit < 8; ++bit) {
+            const uint64_t set = __ballot((digit >> bit) & 1u);
+            peers &= (digit >> bit) & 1u ? set : ~set;
+        }
+        if (live && (peers & lower) == 0)
+            wave_count[wave][digit] = (uint32_t)__popcll(peers);
+        __syncthreads();
+        if (live) {
+            uint32_t to = base[digit] + (uint32_t)__popcll(peers & lower);
+            for (int w = 0; w < wave; ++w)
+                to += wave_count[w][digit];
+            a.key[to] = key;
+            a.pos[to] = pos;
+        }
+        __syncthreads();
+        uint32_t add = 0;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            add += wave_count[w][t];
+            wave_count[w][t] = 0;
+        }
+        base[t] += add;
+        __syncthreads();
     }
 }
 
@@ -150,94 +346,108 @@ __global__ __launch_bounds__(256) void starts_kernel(TableArgs a)
     }
 }
 
+// ------------------------------------------------------------ sums of runs
 // the sum of dY's rows at sorted positions j0 .. j1 - 1
-template <int DT>
-__device__ __forceinline__ f32x8 add_rows(const TableArgs &a, int64_t j0, int64_t j1, int64_t col,
-                                          int valid)
+template <int DT, bool TINY, int HOLD>
+__device__ __forceinline__ void add_rows(const TableArgs &a, int64_t j0, int64_t j1,
+                                         const Window<DT, TINY> (&w)[HOLD], f32x8 (&sum)[HOLD])
 {
-    f32x8 sum = 0.0f;
-    if (valid) {
-#pragma unroll 8
-        for (int64_t j = j0; j < j1; ++j)
-            sum += load8(a.dY, (int64_t)a.pos[j] * a.ldy + col, DT, valid);
-    }
-    return sum;
+#pragma unroll
+    for (int h = 0; h < HOLD; ++h)
+        sum[h] = 0.0f;
+    add_batches(j0, j1, [&](int64_t j) { return (int64_t)shared_load(a.pos, j); },
+                [&](int64_t row, int h) { return w[h].load(a.dY, row * a.ldy); }, sum);
 }
 
-// A wave for every row of the table and strip of 512 columns.
-template <int DT>
+// A wave for every row of the table and 1,024 (TINY: 512) columns.
+template <int DT, bool TINY, bool ONE>
 __global__ __launch_bounds__(256) void rows_kernel(TableArgs a)
 {
-    const int64_t tasks = a.rows * a.strips;
-    for (int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); t < tasks;
+    using W = Window<DT, TINY>;
+    constexpr int kHold = ONE ? 1 : 2;
+    const int64_t strips = (a.strips + kHold - 1) / kHold, tasks = a.rows * strips;
+    for (int64_t t = (int64_t)blockIdx.x * 4 + wave_index(); t < tasks;
          t += (int64_t)gridDim.x * 4) {
-        const int64_t v = t / a.strips, col = (t % a.strips * 64 + (threadIdx.x & 63)) * 8;
-        const int64_t j0 = a.start[v], j1 = a.start[v + 1];
-        const int valid = valid8(col, a.k);
-        if (!valid || j1 - j0 > kRun || (a.accumulate && j0 == j1))
+        const int64_t v = strips == 1 ? t : t / strips;
+        const int64_t col = ((t - v * strips) * kHold * 64 + (threadIdx.x & 63)) * 8;
+        const int64_t j0 = shared_load(a.start, v), j1 = shared_load(a.start, v + 1);
+        if (j1 - j0 > kRun || (a.accumulate && j0 == j1))
             continue;
-        put<DT>(a, v, col, add_rows<DT>(a, j0, j1, col, valid), valid);
+        if constexpr (ONE) {
+            const W w[1] = {W(col, a.k)};
+            f32x8 sum[1];
+            add_rows(a, j0, j1, w, sum);
+            put(a, v, w[0], sum[0]);
+        } else {
+            const W w[2] = {W(col, a.k), W(col + 512, a.k)};
+            f32x8 sum[2];
+            add_rows(a, j0, j1, w, sum);
+            put(a, v, w[0], sum[0]);
+            put(a, v, w[1], sum[1]);
+        }
     }
 }
 
-// Of the runs longer than 64, what lies in a chunk of 64 sorted positions:
-// the run that the chunk begins in (slot 0) and the one that it ends in
-// (slot 1).
-template <int DT>
+// Of the runs longer than 16, what lies in a chunk of 16 sorted positions: the
+// run that the chunk begins in (slot 0) and the one that it ends in (slot 1).
+template <int DT, bool TINY>
 __global__ __launch_bounds__(256) void cuts_kernel(TableArgs a)
 {
     const int64_t chunks = (a.n + kRun - 1) / kRun, tasks = chunks * a.strips;
-    for (int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); t < tasks;
+    for (int64_t t = (int64_t)blockIdx.x * 4 + wave_index(); t < tasks;
          t += (int64_t)gridDim.x * 4) {
-        const int64_t c = t / a.strips, col = (t % a.strips * 64 + (threadIdx.x & 63)) * 8;
+        const int64_t c = a.strips == 1 ? t : t / a.strips;
+        const Window<DT, TINY> w[1] = {
+            Window<DT, TINY>(((t - c * a.strips) * 64 + (threadIdx.x & 63)) * 8, a.k)};
         const int64_t first = c * kRun, end = first + kRun < a.n ? first + kRun : a.n;
-        const int valid = valid8(col, a.k);
-        const int64_t head = (int64_t)a.key[first], tail = (int64_t)a.key[end - 1];
-        if (head >= a.rows)
-            continue;
-        float *to = a.part + c * 2 * a.k + col;
-        if (a.start[head + 1] - a.start[head] > kRun) {
-            const int64_t j1 = a.start[head + 1] < end ? a.start[head + 1] : end;
-            store8(to, 0, add_rows<DT>(a, first, j1, col, valid), GPIC_F32, valid);
+        const int64_t head = shared_load(a.key, first), tail = shared_load(a.key, end - 1);
+#pragma unroll
+        for (int slot = 0; slot < 2; ++slot) {
+            const int64_t v = slot ? tail : head;
+            if (v >= a.rows || (slot && tail == head))
+                break;
+            const int64_t s0 = shared_load(a.start, v), s1 = shared_load(a.start, v + 1);
+            if (s1 - s0 <= kRun)
+                continue;
+            f32x8 sum[1];
+            add_rows(a, s0 > first ? s0 : first, s1 < end ? s1 : end, w, sum);
+            if (w[0].skip < 8)
+                w[0].store(a.part, (c * 2 + slot) * a.k, sum[0], GPIC_F32);
         }
-        if (tail != head && tail < a.rows && a.start[tail + 1] - a.start[tail] > kRun)
-            store8(to, a.k, add_rows<DT>(a, a.start[tail], end, col, valid), GPIC_F32, valid);
     }
 }
 
-// The cuts' sums of the run that starts in a chunk, by the sixteen waves of a
+// The cuts' sums of the run that starts in a chunk, by the eight waves of a
 // workgroup.
-template <int DT>
-__global__ __launch_bounds__(1024) void join_cuts_kernel(TableArgs a)
+template <int DT, bool TINY>
+__global__ __launch_bounds__(512) void join_cuts_kernel(TableArgs a)
 {
-    __shared__ f32x8 all[16][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    __shared__ f32x8 all[8][64];
+    const int lane = threadIdx.x & 63;
+    const int64_t wave = wave_index();
     const int64_t tasks = (a.n + kRun - 1) / kRun * a.strips;
     for (int64_t t = blockIdx.x; t < tasks; t += gridDim.x) {
         const int64_t c = t / a.strips, first = c * kRun;
         const int64_t end = first + kRun < a.n ? first + kRun : a.n;
-        const int64_t v = (int64_t)a.key[end - 1];
+        const int64_t v = shared_load(a.key, end - 1);
         if (v >= a.rows)
             continue;
-        const int64_t j0 = a.start[v], j1 = a.start[v + 1];
+        const int64_t j0 = shared_load(a.start, v), j1 = shared_load(a.start, v + 1);
         if (j0 < first || j1 - j0 <= kRun)
             continue;
-        const int64_t col = (t % a.strips * 64 + lane) * 8;
-        const int valid = valid8(col, a.k);
-        const int64_t cuts = (j1 - 1) / kRun - c + 1, each = (cuts + 15) / 16;
+        const Window<DT, TINY> w((t % a.strips * 64 + lane) * 8, a.k);
+        const int64_t cuts = (j1 - 1) / kRun - c + 1, each = (cuts + 7) / 8;
         const int64_t c0 = c + wave * each, c1 = c0 + each < c + cuts ? c0 + each : c + cuts;
-        f32x8 sum = 0.0f;
-        if (valid) {
-#pragma unroll 4
-            for (int64_t i = c0; i < c1; ++i)
-                sum += load8(a.part, (i * 2 + (i == c && j0 > first)) * a.k + col, GPIC_F32, valid);
-        }
-        all[wave][lane] = sum;
+        f32x8 sum[1];
+        sum[0] = 0.0f;
+        add_batches(c0, c1, [&](int64_t i) { return i * 2 + (i == c && j0 > first); },
+                    [&](int64_t slot, int) { return w.load_sum(a.part, slot * a.k); }, sum);
+        all[wave][lane] = sum[0];
         __syncthreads();
-        if (wave == 0 && valid) {
-            for (int i = 1; i < 16; ++i)
-                sum += all[i][lane];
-            put<DT>(a, v, col, sum, valid);
+        if (wave == 0) {
+            for (int i = 1; i < 8; ++i)
+                sum[0] += all[i][lane];
+            put(a, v, w, sum[0]);
         }
         __syncthreads();
     }
@@ -250,20 +460,17 @@ unsigned capped(int64_t blocks)
 }
 
 struct Sorted {
-    uint64_t *key[2];
+    uint32_t *key[2], *counts, *start;
     int32_t *pos[2];
-    uint32_t *hist, *hsum, *start;
     float *part;
     Sorted(const Embedding &p, Cursor &c)
     {
-        const size_t n = (size_t)p.n, most = n > 4096 ? n : 4096;
-        auto larger = [&](size_t bytes) { return bytes > 2 * most ? bytes : 2 * most; };
+        const size_t n = (size_t)p.n;
         for (int i = 0; i < 2; ++i) {
-            key[i] = static_cast<uint64_t *>(c.take(n * 8));
+            key[i] = static_cast<uint32_t *>(c.take(n * 4));
             pos[i] = static_cast<int32_t *>(c.take(n * 4));
         }
-        hist = static_cast<uint32_t *>(c.take(larger(radix_hist_bytes(p.n))));
-        hsum = static_cast<uint32_t *>(c.take(larger(radix_hsum_bytes(p.n))));
+        counts = static_cast<uint32_t *>(c.take((size_t)kMostTiles * 256 * 4));
         start = static_cast<uint32_t *>(c.take(((size_t)p.rows + 1) * 4));
         part = static_cast<float *>(c.take((n + kRun - 1) / kRun * 2 * (size_t)p.k * 4));
     }
@@ -286,10 +493,58 @@ hipError_t few_ids(const Embedding &p, const TableArgs &a, hipStream_t st)
     if (p.n == 0)
         return hipSuccess;
     const unsigned blocks = (unsigned)(p.n * a.strips);
-    if (p.wide)
-        few_ids_kernel<DT, true><<<blocks, 256, 0, st>>>(a);
+    if (p.k < 8 && p.wide)
+        few_ids_kernel<DT, true, true><<<blocks, 256, 0, st>>>(a);
+    else if (p.k < 8)
+        few_ids_kernel<DT, false, true><<<blocks, 256, 0, st>>>(a);
+    else if (p.wide)
+        few_ids_kernel<DT, true, false><<<blocks, 256, 0, st>>>(a);
     else
-        few_ids_kernel<DT, false><<<blocks, 256, 0, st>>>(a);
+        few_ids_kernel<DT, false, false><<<blocks, 256, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+template <bool WIDE>
+hipError_t sort_ids(const Embedding &p, const void *ids, const Sorted &s, int &at, hipStream_t st)
+{
+    SortArgs a{};
+    a.ids = ids;
+    a.n = p.n;
+    a.rows = p.rows;
+    a.counts = s.counts;
+    a.tile = (p.n + kMostTiles - 1) / kMostTiles;
+    a.tile = a.tile < 1024 ? 1024 : (a.tile + 255) / 256 * 256;
+    const unsigned tiles = (unsigned)((p.n + a.tile - 1) / a.tile);
+    at = 0;
+    for (int shift = 0; shift < 32 && (shift == 0 || (p.rows >> shift) != 0); shift += 8) {
+        a.shift = shift;
+        a.key = s.key[at];
+        a.pos = s.pos[at];
+        count_digits_kernel<WIDE><<<tiles, 256, 0, st>>>(a);
+        RUN(hipGetLastError());
+        scatter_digits_kernel<WIDE><<<tiles, 256, 0, st>>>(a);
+        RUN(hipGetLastError());
+        a.ids = nullptr;
+        a.key_in = s.key[at];
+        a.pos_in = s.pos[at];
+        at ^= 1;
+    }
+    at ^= 1;
+    return hipSuccess;
+}
+
+template <int DT, bool TINY>
+hipError_t add_runs(const Embedding &p, const TableArgs &a, hipStream_t st)
+{
+    const int64_t chunks = (p.n + kRun - 1) / kRun, pairs = (a.strips + 1) / 2;
+    if (a.strips == 1)
+        rows_kernel<DT, TINY, true><<<capped((p.rows + 3) / 4), 256, 0, st>>>(a);
+    else
+        rows_kernel<DT, TINY, false><<<capped((p.rows * pairs + 3) / 4), 256, 0, st>>>(a);
+    RUN(hipGetLastError());
+    cuts_kernel<DT, TINY><<<capped((chunks * a.strips + 3) / 4), 256, 0, st>>>(a);
+    RUN(hipGetLastError());
+    join_cuts_kernel<DT, TINY><<<capped(chunks * a.strips), 512, 0, st>>>(a);
     return hipGetLastError();
 }
 
@@ -297,31 +552,16 @@ template <int DT>
 hipError_t sorted_ids(const Embedding &p, TableArgs a, void *ws, hipStream_t st)
 {
     Cursor c{static_cast<char *>(ws)};
-    Sorted s(p, c);
-    const unsigned blocks = capped((p.n + 255) / 256);
-    if (p.wide)
-        keys_kernel<true><<<blocks, 256, 0, st>>>(a.ids, p.n, p.rows, s.key[0], s.pos[0]);
-    else
-        keys_kernel<false><<<blocks, 256, 0, st>>>(a.ids, p.n, p.rows, s.key[0], s.pos[0]);
-    RUN(hipGetLastError());
-    int bits = 8;
-    while (bits < 32 && (p.rows >> bits) != 0)
-        bits += 8;
-    RUN(radix_sort_u64(s.key[0], s.pos[0], s.key[1], s.pos[1], p.n, bits, s.hist, s.hsum, st,
-                       true));
-    a.key = s.key[0];
-    a.pos = s.pos[0];
+    const Sorted s(p, c);
+    int at = 0;
+    RUN(p.wide ? sort_ids<true>(p, a.ids, s, at, st) : sort_ids<false>(p, a.ids, s, at, st));
+    a.key = s.key[at];
+    a.pos = s.pos[at];
     a.start = s.start;
     a.part = s.part;
     starts_kernel<<<capped((p.rows + 256) / 256), 256, 0, st>>>(a);
     RUN(hipGetLastError());
-    const int64_t chunks = (p.n + kRun - 1) / kRun;
-    rows_kernel<DT><<<capped((p.rows * a.strips + 3) / 4), 256, 0, st>>>(a);
-    RUN(hipGetLastError());
-    cuts_kernel<DT><<<capped((chunks * a.strips + 3) / 4), 256, 0, st>>>(a);
-    RUN(hipGetLastError());
-    join_cuts_kernel<DT><<<capped(chunks * a.strips), 1024, 0, st>>>(a);
-    return hipGetLastError();
+    return p.k < 8 ? add_runs<DT, true>(p, a, st) : add_runs<DT, false>(p, a, st);
 }
 
 template <int DT>
