@@ -89,6 +89,14 @@ Embedding embedding_of(const gpic_embedding_params *p)
                      p->accumulate != 0};
 }
 
+gpic_status check_gradient_fits(const gpic_embedding_params *p)
+{
+    if (!embedding_fits(embedding_of(p)))
+        return fail(GPIC_ERR_UNSUPPORTED, "n = %lld, k = %lld: a gradient of more workgroups than "
+                    "a launch takes", (long long)p->n, (long long)p->k);
+    return GPIC_OK;
+}
+
 gpic_status check_ids(const void *ids, const char *name, int32_t bytes, bool nullable)
 {
     CHECK_ARG(ids != nullptr || nullable, "%s is null", name);
@@ -222,7 +230,9 @@ gpic_status gpic_embedding(const gpic_embedding_params *p, const void *ids, cons
 
 size_t gpic_embedding_workspace_bytes(const gpic_embedding_params *p)
 {
-    return check_embedding(p) == GPIC_OK ? embedding_ws(embedding_of(p)) : 0;
+    if (check_embedding(p) != GPIC_OK || check_gradient_fits(p) != GPIC_OK)
+        return 0;
+    return embedding_ws(embedding_of(p));
 }
 
 gpic_status gpic_embedding_backward(const gpic_embedding_params *p, const void *dY,
@@ -230,6 +240,7 @@ gpic_status gpic_embedding_backward(const gpic_embedding_params *p, const void *
                                     void *stream)
 {
     CHECK(check_embedding(p));
+    CHECK(check_gradient_fits(p));
     const bool empty = p->n == 0;
     CHECK(check_matrix(dY, "dY", p->dtype, empty));
     CHECK(check_ids(ids, "ids", p->id_bytes, empty));

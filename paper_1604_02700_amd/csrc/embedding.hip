@@ -225,8 +225,6 @@ __global__ __launch_bounds__(256) void few_ids_kernel(TableArgs a)
 // workgroup counts its tile's digits; then every workgroup finds its tile's
 // places from all tiles' counts (at most 256, so no launch scans them) and
 // scatters, its keys ranked within their wave by ballots over the digit's bits.
-// 32,768 ids below 50,000: 2 x (4 + 6) us, where a scan of the counts by one
-// workgroup between them took another 12 each.
 constexpr int kMostTiles = 256;
 
 struct SortArgs {
@@ -237,7 +235,7 @@ struct SortArgs {
     uint32_t *key;
     int32_t *pos;
     uint32_t *counts;          // [tiles][256]
-    int64_t tile;              // keys, a multiple of 256
+    int64_t tile;              // keys, a multiple of 1,024
     int shift;
 };
 
@@ -265,33 +263,50 @@ __global__ __launch_bounds__(256) void count_digits_kernel(SortArgs a)
 }
 
 template <bool WIDE>
-__global__ __launch_bounds__(256) void scatter_digits_kernel(SortArgs a)
+__global__ __launch_bounds__(1024) void scatter_digits_kernel(SortArgs a)
 {
-    __shared__ uint32_t base[256], total[256], wave_count[4][256];
+    __shared__ uint32_t base[256], part[2][4][256], in_wave[16][256], wave_sum[4];
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
     uint32_t before = 0, all = 0;
+    const int tiles = (int)gridDim.x;
 #pragma unroll 8
-    for (int i = 0; i < (int)gridDim.x; ++i) {
-        const uint32_t c = a.counts[(int64_t)i * 256 + t];
+    for (int i = t >> 8; i < tiles; i += 4) {
+        const uint32_t c = a.counts[(int64_t)i * 256 + (t & 255)];
         before += i < (int)blockIdx.x ? c : 0;
         all += c;
     }
-    total[t] = all;
+    part[0][t >> 8][t & 255] = before;
+    part[1][t >> 8][t & 255] = all;
 #pragma unroll
-    for (int w = 0; w < 4; ++w)
-        wave_count[w][t] = 0;
+    for (int i = 0; i < 4; ++i)
+        in_wave[4 * i + (t >> 8)][t & 255] = 0;
     __syncthreads();
-    for (int o = 1; o < 256; o <<= 1) {
-        const uint32_t x = t >= o ? total[t - o] : 0;
-        __syncthreads();
-        total[t] += x;
-        __syncthreads();
+    uint32_t sum = 0;
+    if (t < 256) {
+        before = all = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            before += part[0][i][t];
+            all += part[1][i][t];
+        }
+        sum = all;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const uint32_t x = __shfl_up(sum, o, 64);
+            sum += lane >= o ? x : 0;
+        }
+        if (lane == 63)
+            wave_sum[wave] = sum;
     }
-    base[t] = total[t] - all + before;
     __syncthreads();
+    if (t < 256) {
+        for (int w = 0; w < wave; ++w)
+            sum += wave_sum[w];
+        base[t] = sum - all + before;
+    }
     const int64_t i0 = blockIdx.x * a.tile, i1 = i0 + a.tile < a.n ? i0 + a.tile : a.n;
     const uint64_t lower = lane == 0 ? 0 : ~0ull >> (64 - lane);
-    for (int64_t first = i0; first < i1; first += 256) {
+    for (int64_t first = i0; first < i1; first += 1024) {
         const int64_t i = first + t;
         const bool live = i < i1;
         uint32_t key = 0;
@@ -308,23 +323,29 @@ __global__ __launch_bounds__(256) void scatter_digits_kernel(SortArgs a)
             peers &= (digit >> bit) & 1u ? set : ~set;
         }
         if (live && (peers & lower) == 0)
-            wave_count[wave][digit] = (uint32_t)__popcll(peers);
+            in_wave[wave][digit] = (uint32_t)__popcll(peers);
+        __syncthreads();
+        // each wave's first place for a digit
+        if (t < 256) {
+            uint32_t at = base[t];
+#pragma unroll
+            for (int w = 0; w < 16; ++w) {
+                const uint32_t c = in_wave[w][t];
+                in_wave[w][t] = at;
+                at += c;
+            }
+            base[t] = at;
+        }
         __syncthreads();
         if (live) {
-            uint32_t to = base[digit] + (uint32_t)__popcll(peers & lower);
-            for (int w = 0; w < wave; ++w)
-                to += wave_count[w][digit];
+            const uint32_t to = in_wave[wave][digit] + (uint32_t)__popcll(peers & lower);
             a.key[to] = key;
             a.pos[to] = pos;
         }
         __syncthreads();
-        uint32_t add = 0;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            add += wave_count[w][t];
-            wave_count[w][t] = 0;
-        }
-        base[t] += add;
+        for (int k = 0; k < 4; ++k)
+            in_wave[4 * k + (t >> 8)][t & 255] = 0;
         __syncthreads();
     }
 }
@@ -359,35 +380,6 @@ __device__ __forceinline__ void add_rows(const TableArgs &a, int64_t j0, int64_t
                 [&](int64_t row, int h) { return w[h].load(a.dY, row * a.ldy); }, sum);
 }
 
-// A wave for every row of the table and 1,024 (TINY: 512) columns.
-template <int DT, bool TINY, bool ONE>
-__global__ __launch_bounds__(256) void rows_kernel(TableArgs a)
-{
-    using W = Window<DT, TINY>;
-    constexpr int kHold = ONE ? 1 : 2;
-    const int64_t strips = (a.strips + kHold - 1) / kHold, tasks = a.rows * strips;
-    for (int64_t t = (int64_t)blockIdx.x * 4 + wave_index(); t < tasks;
-         t += (int64_t)gridDim.x * 4) {
-        const int64_t v = strips == 1 ? t : t / strips;
-        const int64_t col = ((t - v * strips) * kHold * 64 + (threadIdx.x & 63)) * 8;
-        const int64_t j0 = shared_load(a.start, v), j1 = shared_load(a.start, v + 1);
-        if (j1 - j0 > kRun || (a.accumulate && j0 == j1))
-            continue;
-        if constexpr (ONE) {
-            const W w[1] = {W(col, a.k)};
-            f32x8 sum[1];
-            add_rows(a, j0, j1, w, sum);
-            put(a, v, w[0], sum[0]);
-        } else {
-            const W w[2] = {W(col, a.k), W(col + 512, a.k)};
-            f32x8 sum[2];
-            add_rows(a, j0, j1, w, sum);
-            put(a, v, w[0], sum[0]);
-            put(a, v, w[1], sum[1]);
-        }
-    }
-}
-
 // Of the runs longer than 16, what lies in a chunk of 16 sorted positions: the
 // run that the chunk begins in (slot 0) and the one that it ends in (slot 1).
 template <int DT, bool TINY>
@@ -417,39 +409,104 @@ __global__ __launch_bounds__(256) void cuts_kernel(TableArgs a)
     }
 }
 
-// The cuts' sums of the run that starts in a chunk, by the eight waves of a
-// workgroup.
+// The cuts' sums of the runs that start in eight chunks, a wave a chunk; of a
+// run of more than eight cuts (no two can start within eight chunks) by all
+// waves of the workgroup.
+constexpr int kJoinWaves = 8;
+
 template <int DT, bool TINY>
-__global__ __launch_bounds__(512) void join_cuts_kernel(TableArgs a)
+__device__ __forceinline__ void join_cuts(const TableArgs &a, int64_t t)
 {
-    __shared__ f32x8 all[8][64];
+    __shared__ f32x8 all[kJoinWaves][64];
+    __shared__ int long_run;
     const int lane = threadIdx.x & 63;
-    const int64_t wave = wave_index();
-    const int64_t tasks = (a.n + kRun - 1) / kRun * a.strips;
-    for (int64_t t = blockIdx.x; t < tasks; t += gridDim.x) {
-        const int64_t c = t / a.strips, first = c * kRun;
-        const int64_t end = first + kRun < a.n ? first + kRun : a.n;
-        const int64_t v = shared_load(a.key, end - 1);
+    const int64_t wave = wave_index(), chunks = (a.n + kRun - 1) / kRun;
+    const int64_t block = t / a.strips, mine = block * kJoinWaves + wave;
+    const Window<DT, TINY> w(((t - block * a.strips) * 64 + lane) * 8, a.k);
+    // chunk c's last run: its row of the table, and the cut after its last (c
+    // where it does not start there or is not cut); the sum over cuts c0 .. c1 - 1
+    auto row_of = [&](int64_t c) {
+        const int64_t end = (c + 1) * kRun < a.n ? (c + 1) * kRun : a.n;
+        return (int64_t)shared_load(a.key, end - 1);
+    };
+    auto cuts_of = [&](int64_t c, int64_t v) {
         if (v >= a.rows)
-            continue;
+            return c;
         const int64_t j0 = shared_load(a.start, v), j1 = shared_load(a.start, v + 1);
-        if (j0 < first || j1 - j0 <= kRun)
-            continue;
-        const Window<DT, TINY> w((t % a.strips * 64 + lane) * 8, a.k);
-        const int64_t cuts = (j1 - 1) / kRun - c + 1, each = (cuts + 7) / 8;
-        const int64_t c0 = c + wave * each, c1 = c0 + each < c + cuts ? c0 + each : c + cuts;
-        f32x8 sum[1];
+        return j0 < c * kRun || j1 - j0 <= kRun ? c : (j1 - 1) / kRun + 1;
+    };
+    auto add = [&](int64_t c, int64_t v, int64_t c0, int64_t c1, f32x8 (&sum)[1]) {
+        const bool within = (int64_t)shared_load(a.start, v) > c * kRun;
         sum[0] = 0.0f;
-        add_batches(c0, c1, [&](int64_t i) { return i * 2 + (i == c && j0 > first); },
+        add_batches(c0, c1, [&](int64_t i) { return i * 2 + (i == c && within); },
                     [&](int64_t slot, int) { return w.load_sum(a.part, slot * a.k); }, sum);
-        all[wave][lane] = sum[0];
-        __syncthreads();
-        if (wave == 0) {
-            for (int i = 1; i < 8; ++i)
-                sum[0] += all[i][lane];
+    };
+    if (threadIdx.x == 0)
+        long_run = -1;
+    __syncthreads();
+    f32x8 sum[1];
+    if (mine < chunks) {
+        const int64_t v = row_of(mine), c1 = cuts_of(mine, v);
+        if (c1 - mine > kJoinWaves) {
+            if (lane == 0)
+                long_run = (int)wave;
+        } else if (c1 > mine) {
+            add(mine, v, mine, c1, sum);
             put(a, v, w, sum[0]);
         }
-        __syncthreads();
+    }
+    __syncthreads();
+    const int found = __builtin_amdgcn_readfirstlane(long_run);
+    if (found < 0)
+        return;
+    const int64_t c = block * kJoinWaves + found, v = row_of(c), cuts = cuts_of(c, v) - c;
+    const int64_t each = (cuts + kJoinWaves - 1) / kJoinWaves, c0 = c + wave * each;
+    add(c, v, c0, c0 + each < c + cuts ? c0 + each : c + cuts, sum);
+    all[wave][lane] = sum[0];
+    __syncthreads();
+    if (wave == 0) {
+        for (int i = 1; i < kJoinWaves; ++i)
+            sum[0] += all[i][lane];
+        put(a, v, w, sum[0]);
+    }
+}
+
+// (In one launch with the rows they would hide behind them, but both then run at
+// the registers of the larger: 43 us for 24.5 and 17.7.)
+template <int DT, bool TINY>
+__global__ __launch_bounds__(64 * kJoinWaves) void join_cuts_kernel(TableArgs a)
+{
+    join_cuts<DT, TINY>(a, blockIdx.x);
+}
+
+// A wave for every row of the table and 1,024 (ONE: 512) columns.  Bound by
+// memory: 32,768 x 1,024 -> 50,000 in bfloat16, ids as frequent as words, 24.5 us
+// (102 MB written, 43 MB read: 5.9 TB/s).
+template <int DT, bool TINY, bool ONE>
+__global__ __launch_bounds__(256) void rows_kernel(TableArgs a)
+{
+    using W = Window<DT, TINY>;
+    constexpr int kHold = ONE ? 1 : 2;
+    const int64_t strips = (a.strips + kHold - 1) / kHold, tasks = a.rows * strips;
+    for (int64_t t = (int64_t)blockIdx.x * 4 + wave_index(); t < tasks;
+         t += (int64_t)gridDim.x * 4) {
+        const int64_t v = strips == 1 ? t : t / strips;
+        const int64_t col = ((t - v * strips) * kHold * 64 + (threadIdx.x & 63)) * 8;
+        const int64_t j0 = shared_load(a.start, v), j1 = shared_load(a.start, v + 1);
+        if (j1 - j0 > kRun || (a.accumulate && j0 == j1))
+            continue;
+        if constexpr (ONE) {
+            const W w[1] = {W(col, a.k)};
+            f32x8 sum[1];
+            add_rows(a, j0, j1, w, sum);
+            put(a, v, w[0], sum[0]);
+        } else {
+            const W w[2] = {W(col, a.k), W(col + 512, a.k)};
+            f32x8 sum[2];
+            add_rows(a, j0, j1, w, sum);
+            put(a, v, w[0], sum[0]);
+            put(a, v, w[1], sum[1]);
+        }
     }
 }
 
@@ -513,7 +570,7 @@ hipError_t sort_ids(const Embedding &p, const void *ids, const Sorted &s, int &a
     a.rows = p.rows;
     a.counts = s.counts;
     a.tile = (p.n + kMostTiles - 1) / kMostTiles;
-    a.tile = a.tile < 1024 ? 1024 : (a.tile + 255) / 256 * 256;
+    a.tile = (a.tile + 1023) / 1024 * 1024;
     const unsigned tiles = (unsigned)((p.n + a.tile - 1) / a.tile);
     at = 0;
     for (int shift = 0; shift < 32 && (shift == 0 || (p.rows >> shift) != 0); shift += 8) {
@@ -522,7 +579,7 @@ hipError_t sort_ids(const Embedding &p, const void *ids, const Sorted &s, int &a
         a.pos = s.pos[at];
         count_digits_kernel<WIDE><<<tiles, 256, 0, st>>>(a);
         RUN(hipGetLastError());
-        scatter_digits_kernel<WIDE><<<tiles, 256, 0, st>>>(a);
+        scatter_digits_kernel<WIDE><<<tiles, 1024, 0, st>>>(a);
         RUN(hipGetLastError());
         a.ids = nullptr;
         a.key_in = s.key[at];
@@ -536,15 +593,17 @@ hipError_t sort_ids(const Embedding &p, const void *ids, const Sorted &s, int &a
 template <int DT, bool TINY>
 hipError_t add_runs(const Embedding &p, const TableArgs &a, hipStream_t st)
 {
-    const int64_t chunks = (p.n + kRun - 1) / kRun, pairs = (a.strips + 1) / 2;
+    const int64_t chunks = (p.n + kRun - 1) / kRun;
+    const int64_t joins = (chunks + kJoinWaves - 1) / kJoinWaves * a.strips;
+    cuts_kernel<DT, TINY><<<capped((chunks * a.strips + 3) / 4), 256, 0, st>>>(a);
+    RUN(hipGetLastError());
+    const int64_t pairs = (a.strips + 1) / 2;
     if (a.strips == 1)
         rows_kernel<DT, TINY, true><<<capped((p.rows + 3) / 4), 256, 0, st>>>(a);
     else
         rows_kernel<DT, TINY, false><<<capped((p.rows * pairs + 3) / 4), 256, 0, st>>>(a);
     RUN(hipGetLastError());
-    cuts_kernel<DT, TINY><<<capped((chunks * a.strips + 3) / 4), 256, 0, st>>>(a);
-    RUN(hipGetLastError());
-    join_cuts_kernel<DT, TINY><<<capped(chunks * a.strips), 512, 0, st>>>(a);
+    join_cuts_kernel<DT, TINY><<<(unsigned)joins, 64 * kJoinWaves, 0, st>>>(a);
     return hipGetLastError();
 }
 
@@ -597,6 +656,12 @@ TableArgs args_of(const Embedding &p, const void *ids)
 }
 
 } // namespace
+
+bool embedding_fits(const Embedding &p)
+{
+    const int64_t chunks = (p.n + kRun - 1) / kRun, strips = (p.k + 511) / 512;
+    return p.n <= kFewIds || (chunks / kJoinWaves + 1) * strips <= (int64_t)3 << 20;
+}
 
 size_t embedding_ws(const Embedding &p)
 {

@@ -38,6 +38,8 @@ struct Embedding {
     bool accumulate;
 };
 size_t embedding_ws(const Embedding &p);   // of the backward pass
+// Whether every launch of the backward pass stays below a grid's 2^32 threads.
+bool embedding_fits(const Embedding &p);
 hipError_t run_embedding(const Embedding &p, const void *ids, const void *T, void *Y,
                          hipStream_t st);
 hipError_t run_embedding_backward(const Embedding &p, const void *dY, const void *ids, void *dT,

@@ -210,6 +210,9 @@ def test_loss_workspaces(g):
 
 def test_too_many_workgroups_are_refused(g):
     L = g.lib()
+    e = _embed(g, n=2 ** 31 - 1)
+    assert L.gpic_embedding_backward(e, *AT[:3], *WS, None) == 5
+    assert L.gpic_embedding_workspace_bytes(e) == 0
     p = _loss(g, n=2 ** 31 - 1, v=1 << 20)
     assert L.gpic_cross_entropy(p, *AT[:6], *WS, None) == 5
     assert L.gpic_cross_entropy_workspace_bytes(0, p) == 0
