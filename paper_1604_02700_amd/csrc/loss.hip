@@ -616,7 +616,7 @@ hipError_t run_loss_backward(const Loss &p, const float *dloss, const void *X, c
         RUN(launch_product(kKK, op, kEpiSoft, a, st));
         if (db) {
             const Plan plan = product_plan(p.n, len, p.k, 1, op, kEpiSoft);
-            const int64_t each = plan.tile == 2 ? 32 : 64;
+            const int64_t each = edge_of(plan) / 2;      // rows of a wave
             RUN(launch_sum_parts(b.sum_b, (p.n + each - 1) / each, len,
                                  static_cast<char *>(db) + (size_t)first * size, p.dtype, st));
         }

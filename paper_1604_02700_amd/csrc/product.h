@@ -659,74 +659,129 @@ __device__ __forceinline__ void finish_lse(const ProductArgs &a, const Work &w,
     }
 }
 
-// D = exp(z - lse) - [target] of ROWS x COLS logits that the wave has staged at
-// `st`, as the products that follow read it (a row's padding up to 64 columns
-// zeros), and its column sums times g, unrounded.  The loss's gradient g is left
-// out of what is rounded: it is the same for every row as a rule (1 / n), and its
-// own rounding to 16 bits would be every entry's, up to 2^-8 of the gradients.
-template <int ROWS, int COLS, int OP>
-__device__ __forceinline__ void finish_soft(const Epilogue &e, int64_t row0, int64_t col0,
-                                            int64_t M, int64_t N, const float *st)
+// D = exp(z - lse) - [target] straight from the accumulators, rounded as the
+// products that follow read it and only then staged in LDS (its own piece, no
+// barrier), so that whole lines go out (a row's padding up to 64 columns zeros);
+// and its column sums times g, unrounded.  The loss's gradient g is left out of
+// what is rounded: it is the same for every row as a rule (1 / n), and its own
+// rounding to 16 bits would be every entry's, up to 2^-8 of the gradients.
+// 8,192 x 2,048 -> 12,544 in bfloat16 (1,568 tiles): 422 us with logits staged in
+// float32.
+template <class T, int OP>
+__device__ __forceinline__ void finish_soft(const ProductArgs &a, const Work &w,
+                                            f32x4 (&acc)[T::kRM][T::kRN], char *lds)
 {
-    constexpr int kDt = OP == kOpSplit ? GPIC_F32 : (OP == kOpF16 ? GPIC_F16 : GPIC_BF16);
-    constexpr int kPitch = COLS + 4, kLanes = COLS / 8, kRowsPass = 64 / kLanes;
-    constexpr int kPasses = ROWS / kRowsPass;
-    static_assert(kPasses * kRowsPass == ROWS, "passes");
-    const int lane = threadIdx.x & 63, q = lane % kLanes, r0 = lane / kLanes;
-    const int64_t col = col0 + q * 8, end = (N + 63) / 64 * 64;
-    const int real = N - col < 0 ? 0 : (N - col < 8 ? (int)(N - col) : 8);
-    const bool written = col < end;
-    const int powers = row_powers<ROWS, OP, kEpiSoft>(e, row0, M);
-    const i32x8 pc = column_powers<OP, kEpiSoft>(e, col, real);
-    f32x8 bias = 0.0f, sum = 0.0f;
-    if (e.bias && real > 0)
-        bias = load8(e.bias, e.first + col, kDt, real);
-#pragma unroll 2
-    for (int p = 0; p < kPasses; ++p) {
-        const int r = p * kRowsPass + r0;
-        const int64_t row = row0 + r;
-        const int pr = OP == kOpBf16 ? 0 : __shfl(powers, r & 63, 64);
-        f32x8 z = staged<OP, kEpiSoft>(st + r * kPitch + q * 8, e, pr, pc);
-        if (row >= M || !written)
-            continue;
-        const LossRow info = e.rows[row];
-        const int at = info.target - (int)(e.first + col);
-        f32x8 d;
+    constexpr bool kSplit = OP == kOpSplit;
+    constexpr int kDt = kSplit ? GPIC_F32 : (OP == kOpF16 ? GPIC_F16 : GPIC_BF16);
+    constexpr int kFrags = Staging<T>::kFrags, kRows = Staging<T>::kRows;
+    constexpr int kWidth = 16 * T::kRN * (kSplit ? 4 : 2);       // bytes of a row
+    constexpr int kPitch = kWidth + 16, kLanes = kWidth / 16, kRowsPass = 64 / kLanes;
+    static_assert(kRows * kPitch <= Staging<T>::kFloats * 4, "a wave's piece");
+    static_assert(kRows % kRowsPass == 0, "passes");
+    const Epilogue &e = a.e;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4;
+    const int64_t row0 = (int64_t)w.ti * T::kBM + (wave / T::kWN) * (16 * T::kRM);
+    const int64_t col0 = (int64_t)w.tj * T::kBN + (wave % T::kWN) * (16 * T::kRN);
+    const int64_t end = ((int64_t)a.N + 63) / 64 * 64;
+    char *st = lds + wave * (Staging<T>::kFloats * 4);
+    float bias[T::kRN][4], sum[T::kRN][4];
+    int pc[T::kRN][4];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            d[j] = __builtin_amdgcn_exp2f((z[j] + bias[j] - info.lse) * kLog2e);
-            d[j] = at == j ? info.picked : (bias[j] == -INFINITY ? 0.0f : d[j]);
-            d[j] = j < real && info.target >= 0 ? d[j] : 0.0f;
+    for (int j = 0; j < T::kRN; ++j)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const int64_t col = col0 + 16 * j + 4 * g + c;
+            // columns beyond the last, as those that the bias takes out, are zeros
+            bias[j][c] = col < a.N ? (e.bias ? load1(e.bias, e.first + col, kDt) : 0.0f)
+                                   : -INFINITY;
+            pc[j][c] = kSplit && col < a.N ? e.pb[col] : 0;
+            sum[j][c] = 0.0f;
         }
-        if (info.target >= 0)
-            sum += d * info.g;
-        if (OP != kOpBf16)
-            d = d * (float)(1 << kSoftPower);
-        if (OP == kOpSplit) {
-            _Float16 *to = static_cast<_Float16 *>(e.p_hi) + row * e.ldp + split_at(col);
-            half8 h, l;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                _Float16 x, y;
-                split2(d[j], x, y);
-                h[j] = x;
-                l[j] = y;
+    for (int i0 = 0; i0 < T::kRM; i0 += kFrags) {
+#pragma unroll
+        for (int i = 0; i < kFrags; ++i) {
+            const int64_t row = row0 + 16 * (i0 + i) + (lane & 15);
+            LossRow info{0.0f, 0.0f, 0.0f, -1};
+            if (row < a.M)
+                info = e.rows[row];
+            const int pr = kSplit && row < a.M ? e.pa[row] : 0;
+            float d[T::kRN][4];
+#pragma unroll
+            for (int j = 0; j < T::kRN; ++j)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    float z = acc[i0 + i][j][c];
+                    if (kSplit)
+                        z = ldexpf(z, -(pr + pc[j][c]));
+                    z = __builtin_amdgcn_exp2f((z + bias[j][c] - info.lse) * kLog2e);
+                    d[j][c] = info.target < 0 || bias[j][c] == -INFINITY ? 0.0f : z;
+                }
+            const int at = info.target < 0 ? -1 : info.target - (int)(e.first + col0) - 4 * g;
+            const bool mine = at >= 0 && at < 16 * T::kRN && (at & 15) < 4;
+            if (__any(mine)) {
+#pragma unroll
+                for (int j = 0; j < T::kRN; ++j)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        if (mine && at == 16 * j + c)
+                            d[j][c] = info.picked;
             }
-            *reinterpret_cast<half8 *>(to) = h;
-            *reinterpret_cast<half8 *>(to + 32) = l;
-        } else {
-            store8(e.p_hi, row * e.ldp + col, d, kDt, 8);
+            char *to = st + (16 * i + (lane & 15)) * kPitch;
+#pragma unroll
+            for (int j = 0; j < T::kRN; ++j) {
+                f32x4 v;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    sum[j][c] += d[j][c] * info.g;
+                    v[c] = OP == kOpBf16 ? d[j][c] : d[j][c] * (float)(1 << kSoftPower);
+                }
+                if (kSplit) {
+                    half4 hi, lo;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        _Float16 x, y;
+                        split2(v[c], x, y);
+                        hi[c] = x;
+                        lo[c] = y;
+                    }
+                    char *p = to + (j >> 1) * 128 + (j & 1) * 32 + g * 8;
+                    *reinterpret_cast<half4 *>(p) = hi;
+                    *reinterpret_cast<half4 *>(p + 64) = lo;
+                } else if (OP == kOpF16) {
+                    *reinterpret_cast<half4 *>(to + j * 32 + g * 8) =
+                        __builtin_convertvector(v, half4);
+                } else {
+                    *reinterpret_cast<bf4 *>(to + j * 32 + g * 8) = __builtin_convertvector(v, bf4);
+                }
+            }
+        }
+        const int q = lane % kLanes, r0 = lane / kLanes;
+        const int64_t col = col0 + (kSplit ? (q >> 3) * 32 + (q & 3) * 8 : q * 8);
+#pragma unroll 4
+        for (int r = r0; r < kRows; r += kRowsPass) {
+            const int64_t row = row0 + 16 * i0 + r;
+            if (row < a.M && col < end)
+                *reinterpret_cast<u32x4 *>(static_cast<char *>(e.p_hi) +
+                                           (row * e.ldp + (kSplit ? 2 : 1) * col0) * 2 + q * 16) =
+                    *reinterpret_cast<const u32x4 *>(st + r * kPitch + q * 16);
         }
     }
-    if (!e.sums)
+    if (!e.sums || row0 >= a.M)
         return;
+    float *to = e.sums + row0 / (16 * T::kRM) * a.N;
 #pragma unroll
-    for (int o = kLanes; o < 64; o <<= 1)
+    for (int j = 0; j < T::kRN; ++j)
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            sum[j] += __shfl_xor(sum[j], o, 64);
-    if (r0 == 0 && real > 0 && row0 < M)
-        store8(e.sums + row0 / ROWS * N, col, sum, GPIC_F32, real);
+        for (int c = 0; c < 4; ++c) {
+            float s = sum[j][c];
+#pragma unroll
+            for (int o = 1; o < 16; o <<= 1)
+                s += __shfl_xor(s, o, 64);
+            const int64_t col = col0 + 16 * j + 4 * g + c;
+            if ((lane & 15) == 0 && col < a.N)
+                to[col] = s;
+        }
 }
 
 // A wave's accumulators to their place: the epilogue, or the partial sums.
@@ -743,6 +798,10 @@ __device__ __forceinline__ void finish_tile(const ProductArgs &a, const Work &w,
     asm volatile("" ::: "memory");
     if constexpr (EPI == kEpiLse) {
         finish_lse<T, OP>(a, w, acc, lds);
+        return;
+    }
+    if constexpr (EPI == kEpiSoft) {
+        finish_soft<T, OP>(a, w, acc, lds);
         return;
     }
     float *st = reinterpret_cast<float *>(lds) + wave * St::kFloats;
@@ -766,11 +825,7 @@ __device__ __forceinline__ void finish_tile(const ProductArgs &a, const Work &w,
         } else {
             const int64_t r0 = (int64_t)w.ti * T::kBM + wm + 16 * i0, c0 = (int64_t)w.tj * T::kBN + wn;
             const bool mirror = symmetric(EPI) && w.ti != w.tj;
-            if constexpr (EPI == kEpiSoft)
-                finish_soft<St::kRows, St::kCols, OP>(a.e, r0, c0, a.M, a.N, st);
-            else
-                finish_block<St::kRows, St::kCols, OP, EPI>(a.e, w.z, r0, c0, a.M, a.N, st,
-                                                            mirror);
+            finish_block<St::kRows, St::kCols, OP, EPI>(a.e, w.z, r0, c0, a.M, a.N, st, mirror);
             if (mirror)
                 mirror_block<St::kRows, St::kCols, OP, EPI>(a.e, w.z, r0, c0, a.N, st, 0, 1);
         }
