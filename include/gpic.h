@@ -702,7 +702,7 @@ gpic_status gpic_cross_entropy(const gpic_loss_params *p, const void *X, const v
  * [n x k] = dZ W, dW [v x k] = dZ^T X, db [v] = column sums of dZ.  dX, dW and db
  * are contiguous, any may be null (not wanted).  loss and lse as
  * gpic_cross_entropy gave them.  The logits are computed once more, in pieces of
- * the vocabulary whose dZ takes about 256 MB.  For the products dZ / dloss is
+ * the vocabulary whose dZ takes up to 512 MB, or 2,048 columns.  For the products dZ / dloss is
  * rounded to the matrices' type (float16: nothing finer than 2^-39; float32: 22
  * bits down to 2^-17, errors of 2^-39 below), and for dW so is X times dloss over
  * the largest finite |dloss| (no rounding where all are alike); db sums it

@@ -49,10 +49,11 @@ struct FewArgs {
     int wide;
 };
 
-// The logits of 16 columns and up to 16 NB rows a workgroup, whose waves share
-// the contraction in turns.
+// The products of 16 columns and up to 16 NB rows a workgroup, whose waves share
+// the contraction in turns; wave b < NB ends with rows 16 b .. 16 b + 15 (true), a
+// lane with four columns (4 (lane / 16) on) of `row`.
 template <int DT, int NB, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void few_lse_kernel(FewArgs a)
+__device__ __forceinline__ bool few_logits(const FewArgs &a, f32x4 &v, int64_t &row)
 {
     constexpr int kValues = DT == GPIC_F32 ? 4 : 8;       // of k a lane loads at once
     constexpr int kSize = DT == GPIC_F32 ? 4 : 2;
@@ -100,14 +101,26 @@ __global__ __launch_bounds__(64 * WAVES) void few_lse_kernel(FewArgs a)
     for (int b = 0; b < NB; ++b)
         part[wave][b][lane] = acc[b];
     __syncthreads();
-    // wave b finishes rows 16 b .. 16 b + 15: a lane four columns of one row
     if (wave >= NB)
-        return;
-    const int64_t row = row0 + wave * 16 + r;
-    f32x4 v = part[0][wave][lane];
+        return false;
+    row = row0 + wave * 16 + r;
+    v = part[0][wave][lane];
 #pragma unroll
     for (int s = 1; s < WAVES; ++s)
         v += part[s][wave][lane];
+    return true;
+}
+
+// Each row's largest and sum of exponentials over 16 columns.
+template <int DT, int NB, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void few_lse_kernel(FewArgs a)
+{
+    f32x4 v;
+    int64_t row;
+    if (!few_logits<DT, NB, WAVES>(a, v, row))
+        return;
+    const int g = (threadIdx.x & 63) >> 4;
+    const int64_t col0 = (int64_t)blockIdx.x * 16;
     const bool live = row < a.n;
     const int64_t t = live ? target_at(a.targets, a.wide, row) : -1;
     float m = -INFINITY, s = 0.0f;
@@ -136,6 +149,52 @@ __global__ __launch_bounds__(64 * WAVES) void few_lse_kernel(FewArgs a)
     s += __shfl_xor(s, 32, 64);
     if (live && g == 0)
         a.strip[(int64_t)blockIdx.x * a.n + row] = make_float2(m, s);
+}
+
+// The same logits to D = g (exp(z - lse) - [target]) in float32, for the gradients
+// of a small layer (small_gradients.hip), and a copy of X whose rows without a
+// gradient are zeros.
+struct SmallArgs {
+    FewArgs f;
+    const float *dloss, *loss, *lse;
+    float *D, *X;              // [n][v], [n][k]
+};
+
+template <int NB, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void small_soft_kernel(SmallArgs s)
+{
+    const FewArgs &a = s.f;
+    f32x4 v;
+    int64_t row;
+    const int g = (threadIdx.x & 63) >> 4;
+    {
+        const int64_t total = a.n * a.k, each = (total + gridDim.x * gridDim.y - 1) /
+                                                (gridDim.x * gridDim.y);
+        const int64_t i0 = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * each;
+        const int64_t i1 = i0 + each < total ? i0 + each : total;
+        for (int64_t i = i0 + threadIdx.x; i < i1; i += 64 * WAVES) {
+            const int64_t r = i / a.k, t = target_at(a.targets, a.wide, r);
+            const bool live = t >= 0 && t < a.v && s.dloss[r] != 0.0f;
+            s.X[i] = live ? static_cast<const float *>(a.X)[r * a.ldx + (i - r * a.k)] : 0.0f;
+        }
+    }
+    if (!few_logits<GPIC_F32, NB, WAVES>(a, v, row) || row >= a.n)
+        return;
+    const int64_t t = target_at(a.targets, a.wide, row);
+    const float gl = s.dloss[row];
+    const bool live = t >= 0 && t < a.v && gl != 0.0f;
+    const float lse = s.lse[row], loss = s.loss[row];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int64_t col = (int64_t)blockIdx.x * 16 + g * 4 + j;
+        if (col >= a.v)
+            break;
+        const float bias = a.bias ? load1(a.bias, col, GPIC_F32) : 0.0f;
+        float d = col == t ? expm1f(-loss)
+                           : __builtin_amdgcn_exp2f((v[j] + bias - lse) * kLog2e);
+        d = bias == -INFINITY && col != t ? 0.0f : d;
+        s.D[row * a.v + col] = live ? d * gl : 0.0f;
+    }
 }
 
 // ------------------------------------------------------------------ join
@@ -200,24 +259,36 @@ struct RowsArgs {
     float *most;               // of each workgroup's finite |g|
 };
 
+// A row's LossRow; its finite |g|
+__device__ __forceinline__ float row_of(const RowsArgs &a, int64_t i, LossRow &r)
+{
+    const int64_t t = target_at(a.targets, a.wide, i);
+    const float g = a.dloss[i];
+    r = LossRow{0.0f, 0.0f, 0.0f, -1};
+    if (t >= 0 && t < a.v && g != 0.0f)
+        r = LossRow{a.lse[i], g, expm1f(-a.loss[i]), (int)t};
+    return fabsf(r.g) < INFINITY ? fabsf(r.g) : 0.0f;
+}
+
+__device__ __forceinline__ float wave_max(float x)
+{
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1)
+        x = fmaxf(x, __shfl_xor(x, o, 64));
+    return x;
+}
+
 __global__ __launch_bounds__(256) void rows_kernel(RowsArgs a)
 {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     float size = 0.0f;
     if (i < a.n) {
-        const int64_t t = target_at(a.targets, a.wide, i);
-        LossRow r{0.0f, 0.0f, 0.0f, -1};
-        const float g = a.dloss[i];
-        if (t >= 0 && t < a.v && g != 0.0f) {
-            r = LossRow{a.lse[i], g, expm1f(-a.loss[i]), (int)t};
-            size = fabsf(g) < INFINITY ? fabsf(g) : 0.0f;
-        }
+        LossRow r;
+        size = row_of(a, i, r);
         a.rows[i] = r;
     }
     __shared__ float w[4];
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1)
-        size = fmaxf(size, __shfl_xor(size, o, 64));
+    size = wave_max(size);
     if ((threadIdx.x & 63) == 0)
         w[threadIdx.x >> 6] = size;
     __syncthreads();
@@ -225,41 +296,61 @@ __global__ __launch_bounds__(256) void rows_kernel(RowsArgs a)
         a.most[blockIdx.x] = fmaxf(fmaxf(w[0], w[1]), fmaxf(w[2], w[3]));
 }
 
-// G, the largest |g|, and each row's g / G
-__global__ __launch_bounds__(1024) void shares_kernel(const float *most, int64_t count,
-                                                      const LossRow *rows, int64_t n,
-                                                      float *largest, float *share)
+// G, the largest |g|, and each row's g / G; up to kRowsAtOnce rows' LossRow too
+// (else `most` holds `count` workgroups' largest).
+constexpr int64_t kRowsAtOnce = 16384;
+
+__global__ __launch_bounds__(1024) void shares_kernel(RowsArgs a, int64_t count, float *largest,
+                                                      float *share)
 {
+    const bool here = a.n <= kRowsAtOnce;
     float best = 0.0f;
-    for (int64_t i = threadIdx.x; i < count; i += 1024)
-        best = fmaxf(best, most[i]);
-    __shared__ float all[1024];
-    all[threadIdx.x] = best;
-    for (int o = 512; o > 0; o >>= 1) {
-        __syncthreads();
-        if (threadIdx.x < o)
-            all[threadIdx.x] = fmaxf(all[threadIdx.x], all[threadIdx.x + o]);
+    if (here) {
+#pragma unroll 2
+        for (int64_t i = threadIdx.x; i < a.n; i += 1024) {
+            LossRow r;
+            best = fmaxf(best, row_of(a, i, r));
+            a.rows[i] = r;
+        }
+    } else {
+        for (int64_t i = threadIdx.x; i < count; i += 1024)
+            best = fmaxf(best, a.most[i]);
     }
+    __shared__ float w[16];
+    best = wave_max(best);
+    if ((threadIdx.x & 63) == 0)
+        w[threadIdx.x >> 6] = best;
     __syncthreads();
-    best = all[0] > 0.0f ? all[0] : 1.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        best = fmaxf(best, w[i]);
+    best = best > 0.0f ? best : 1.0f;
     if (threadIdx.x == 0)
         *largest = best;
+    // (each thread reads the rows that it wrote)
 #pragma unroll 4
-    for (int64_t i = threadIdx.x; i < n; i += 1024)
-        share[i] = rows[i].g / best;
+    for (int64_t i = threadIdx.x; i < a.n; i += 1024)
+        share[i] = a.rows[i].g / best;
 }
 
 // Partial maxima [parts][cols] of the finite magnitudes of a float32 matrix's
 // columns, its rows times a factor each.
 struct ColumnArgs {
     const float *x;
-    int64_t rows, cols, ld, each;
+    int64_t rows, cols, ld, each, parts;
     const float *row;          // or null
     float *part;
+    int *power;
+};
+struct ColumnJobs {
+    ColumnArgs j[2];
 };
 
-__global__ __launch_bounds__(256) void column_max_kernel(ColumnArgs a)
+__global__ __launch_bounds__(256) void column_max_kernel(ColumnJobs jobs)
 {
+    const ColumnArgs a = jobs.j[blockIdx.z];
+    if ((int64_t)blockIdx.y >= a.parts)
+        return;
     const int64_t col = ((int64_t)blockIdx.x * 64 + (threadIdx.x & 63)) * 4;
     const int64_t r0 = blockIdx.y * a.each, r1 = r0 + a.each < a.rows ? r0 + a.each : a.rows;
     f32x4 best = 0.0f;
@@ -296,15 +387,16 @@ __global__ __launch_bounds__(256) void column_max_kernel(ColumnArgs a)
             a.part[blockIdx.y * a.cols + col + j] = best[j];
 }
 
-__global__ __launch_bounds__(256) void column_power_kernel(const float *part, int64_t parts,
-                                                           int64_t cols, int *power)
+__global__ __launch_bounds__(256) void column_power_kernel(ColumnJobs jobs)
 {
-    const int64_t col = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
+    const ColumnArgs a = jobs.j[blockIdx.y];
+    const int64_t col = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63), cols = a.cols;
+    int *power = a.power;
     float best = 0.0f;
     if (col < cols) {
 #pragma unroll 8
-        for (int64_t p = threadIdx.x >> 6; p < parts; p += 4)
-            best = fmaxf(best, part[p * cols + col]);
+        for (int64_t p = threadIdx.x >> 6; p < a.parts; p += 4)
+            best = fmaxf(best, a.part[p * cols + col]);
     }
     __shared__ float all[4][64];
     all[threadIdx.x >> 6][threadIdx.x & 63] = best;
@@ -342,6 +434,26 @@ bool few(const Loss &p)
     return p.n <= 2048 && p.n * p.v <= ((int64_t)1 << (f32 ? 28 : 27)) / p.k;
 }
 
+// The gradients of little work: float32, in two launches.
+Shape layer_of(const Loss &p)
+{
+    Shape s{};
+    s.n = p.n;
+    s.k = p.k;
+    s.m = p.v;
+    s.dtype = p.dtype;
+    s.act = GPIC_ACT_NONE;
+    s.ldx = p.k;
+    s.ldw = p.ldw;
+    s.ldy = p.v;
+    return s;
+}
+
+bool small(const Loss &p)
+{
+    return p.n > 0 && p.dtype == GPIC_F32 && small_gradients(layer_of(p), false);
+}
+
 int64_t edge_of(const Plan &p) { return p.tile == 0 ? 256 : (p.tile == 1 ? 128 : 64); }
 
 // What a forward call keeps in its workspace.
@@ -367,12 +479,23 @@ struct Forward {
     }
 };
 
-// How the vocabulary is cut: pieces of whole tiles, of which dZ takes up to
-// 256 MB (what the last-level cache holds), of 2,048 columns at least.
+struct Small {
+    float *D, *X;
+    Small(const Loss &p, Cursor &c)
+    {
+        D = static_cast<float *>(c.take((size_t)p.n * p.v * 4));
+        X = static_cast<float *>(c.take((size_t)p.n * p.k * 4));
+    }
+};
+
+// How the vocabulary is cut: pieces of whole tiles, of which dZ takes up to 512
+// MB, of 2,048 columns at least.  Gradients in us with 112, 256, 400, 512 and 1,024
+// MB: 8,192 x 2,048 -> 50,000 in bfloat16 4,370, 4,429, 4,244, 4,254 and 4,219 (one
+// piece), 8,192 x 512 in float32 4,510, 3,780, 3,614, 3,599 and 3,503.
 int64_t piece_of(const Loss &p)
 {
     const int64_t size = p.dtype == GPIC_F32 ? 4 : 2, n = p.n < 1 ? 1 : p.n;
-    int64_t most = ((int64_t)256 << 20) / (size * n) / 256 * 256;
+    int64_t most = ((int64_t)512 << 20) / (size * n) / 256 * 256;
     most = most < 2048 ? 2048 : most;
     const int64_t pieces = (p.v + most - 1) / most;
     return ((p.v + pieces - 1) / pieces + 255) / 256 * 256;
@@ -393,7 +516,7 @@ struct Backward {
     float *most, *largest, *share;
     Source X, W;               // as the logits' product reads them (W: a piece)
     Source Xg, Wc{};           // as dW's does, rows times their shares; float32: as dX's
-    float *column_part = nullptr;
+    float *column_part[2] = {nullptr, nullptr};
     void *dZ;
     float *sum_x, *sum_b;      // dX over the pieces, partial column sums of dZ
     float *part;
@@ -417,8 +540,9 @@ struct Backward {
         if (f32) {
             Wc = Source{w, cols, p.k, p.ldw, true};
             place(Wc, p.dtype, c, p.k);
-            const int64_t px = max_parts(p.n, p.k), pw = max_parts(p.v, p.k);
-            column_part = static_cast<float *>(c.take((size_t)(px > pw ? px : pw) * p.k * 4));
+            for (int i = 0; i < 2; ++i)
+                column_part[i] = static_cast<float *>(
+                    c.take((size_t)max_parts(i ? p.v : p.n, p.k) * p.k * 4));
         }
         dZ = c.take((size_t)p.n * pitch * 2);
         sum_x = piece < p.v ? static_cast<float *>(c.take((size_t)p.n * p.k * 4)) : nullptr;
@@ -458,15 +582,24 @@ hipError_t launch_few(const FewArgs &a, hipStream_t st)
     return hipGetLastError();
 }
 
-hipError_t launch_columns(const Source &s, float *part, hipStream_t st)
+// The powers of the columns of up to two matrices of the same width.
+hipError_t launch_columns(const Source *const *list, float *const *part, int count, hipStream_t st)
 {
-    const int64_t parts = max_parts(s.rows, s.cols), each = (s.rows + parts - 1) / parts;
-    const ColumnArgs a{static_cast<const float *>(s.x), s.rows, s.cols, s.ld, each, s.row, part};
-    const int64_t used = (s.rows + each - 1) / each;
-    column_max_kernel<<<dim3((unsigned)((s.cols + 255) / 256), (unsigned)used), 256, 0, st>>>(a);
+    ColumnJobs jobs{};
+    int64_t most = 0;
+    for (int i = 0; i < count; ++i) {
+        const Source &s = *list[i];
+        const int64_t parts = max_parts(s.rows, s.cols), each = (s.rows + parts - 1) / parts;
+        const int64_t used = (s.rows + each - 1) / each;
+        jobs.j[i] = ColumnArgs{static_cast<const float *>(s.x), s.rows, s.cols, s.ld, each, used,
+                               s.row, part[i], s.power};
+        most = used > most ? used : most;
+    }
+    const int64_t cols = list[0]->cols;
+    column_max_kernel<<<dim3((unsigned)((cols + 255) / 256), (unsigned)most, (unsigned)count), 256,
+                        0, st>>>(jobs);
     RUN(hipGetLastError());
-    column_power_kernel<<<(unsigned)((s.cols + 63) / 64), 256, 0, st>>>(part, used, s.cols,
-                                                                      s.power);
+    column_power_kernel<<<dim3((unsigned)((cols + 63) / 64), (unsigned)count), 256, 0, st>>>(jobs);
     return hipGetLastError();
 }
 
@@ -475,7 +608,9 @@ hipError_t launch_columns(const Source &s, float *part, hipStream_t st)
 size_t loss_ws(const Loss &p, bool backward)
 {
     Cursor c{nullptr};
-    if (backward)
+    if (backward && small(p))
+        Small m(p, c);
+    else if (backward)
         Backward b(p, nullptr, nullptr, c);
     else
         Forward f(p, nullptr, nullptr, c);
@@ -484,7 +619,7 @@ size_t loss_ws(const Loss &p, bool backward)
 
 bool loss_fits(const Loss &p, bool backward)
 {
-    if (p.n == 0 || (!backward && few(p)))
+    if (p.n == 0 || (backward ? small(p) : few(p)))
         return true;
     const int op = kind_of(p.dtype);
     if (!backward)
@@ -537,6 +672,21 @@ hipError_t run_loss(const Loss &p, const void *X, const void *W, const void *bia
     return hipGetLastError();
 }
 
+template <int NB>
+hipError_t launch_small(const SmallArgs &a, hipStream_t st)
+{
+    const FewArgs &f = a.f;
+    const dim3 blocks((unsigned)((f.v + 15) / 16), (unsigned)((f.n + 16 * NB - 1) / (16 * NB)));
+    const int64_t turns = (f.k + 63) / 64;
+    if (turns <= 4)
+        small_soft_kernel<NB, 4><<<blocks, 256, 0, st>>>(a);
+    else if (turns <= 8)
+        small_soft_kernel<NB, 8><<<blocks, 512, 0, st>>>(a);
+    else
+        small_soft_kernel<NB, 16><<<blocks, 1024, 0, st>>>(a);
+    return hipGetLastError();
+}
+
 hipError_t run_loss_backward(const Loss &p, const float *dloss, const void *X, const void *W,
                              const void *bias, const void *targets, const float *loss,
                              const float *lse, void *dX, void *dW, void *db, void *ws,
@@ -553,50 +703,62 @@ hipError_t run_loss_backward(const Loss &p, const float *dloss, const void *X, c
     if (!dX && !dW && !db)
         return hipSuccess;
     Cursor c{static_cast<char *>(ws)};
+    if (small(p)) {
+        const Small m(p, c);
+        SmallArgs a{};
+        a.f = FewArgs{X, W, bias, targets, nullptr, nullptr, p.ldx, p.ldw, p.n, p.k, p.v, p.wide};
+        a.dloss = dloss;
+        a.loss = loss;
+        a.lse = lse;
+        a.D = m.D;
+        a.X = m.X;
+        RUN(p.n <= 16 ? launch_small<1>(a, st) : launch_small<2>(a, st));
+        return run_small_gradients(layer_of(p), false, m.D, m.X, W, nullptr, dX, dW, db, st);
+    }
     Backward b(p, X, W, c);
     const bool f32 = p.dtype == GPIC_F32;
     const int op = kind_of(p.dtype);
     {
         const RowsArgs a{dloss, loss, lse, targets, p.wide, p.n, p.v, b.rows, b.most};
         const int64_t blocks = (p.n + 255) / 256;
-        rows_kernel<<<(unsigned)blocks, 256, 0, st>>>(a);
-        RUN(hipGetLastError());
-        shares_kernel<<<1, 1024, 0, st>>>(b.most, blocks, b.rows, p.n, b.largest, b.share);
+        if (p.n > kRowsAtOnce) {
+            rows_kernel<<<(unsigned)blocks, 256, 0, st>>>(a);
+            RUN(hipGetLastError());
+        }
+        shares_kernel<<<1, 1024, 0, st>>>(a, blocks, b.largest, b.share);
         RUN(hipGetLastError());
     }
-    {
-        b.Xg.pack = dW != nullptr;
-        b.X.pack = b.X.pack && !f32;
-        const Source *list[2] = {&b.X, &b.Xg};
-        if (f32 && dW)
-            RUN(launch_columns(b.Xg, b.column_part, st));
-        RUN(launch_pack(list, 2, p.dtype, st));
-        b.Xg.pack = true;
-        b.X.pack = b.X.pack || f32;
-    }
-    if (f32 && dX) {
+    if (f32 && (dX || dW)) {
         Source all = b.Wc;
         all.rows = p.v;
-        RUN(launch_columns(all, b.column_part, st));
+        const Source *list[2];
+        float *part[2];
+        int count = 0;
+        if (dW) {
+            list[count] = &b.Xg;
+            part[count++] = b.column_part[0];
+        }
+        if (dX) {
+            list[count] = &all;
+            part[count++] = b.column_part[1];
+        }
+        RUN(launch_columns(list, part, count, st));
     }
     for (int64_t first = 0; first < p.v; first += b.piece) {
         const int64_t len = p.v - first < b.piece ? p.v - first : b.piece;
         const void *w = static_cast<const char *>(W) + (size_t)first * p.ldw * size;
         b.W.x = b.Wc.x = w;
         b.W.rows = b.Wc.rows = len;
-        if (f32) {
-            Source x = b.X;
-            if (first > 0)
-                x.rows = 0;                       // X is split with the first piece
+        // X is packed with the first piece
+        Source x = b.X, xg = b.Xg, wc = b.Wc;
+        if (first > 0)
+            x.rows = xg.rows = 0;
+        xg.pack = dW != nullptr;
+        wc.pack = f32 && dX;
+        const Source *list[3] = {&xg, f32 ? &wc : &x, &b.W};
+        if (f32)
             RUN(launch_split_rows(x, b.W, st));
-            if (dX) {
-                const Source *list[1] = {&b.Wc};
-                RUN(launch_pack(list, 1, p.dtype, st));
-            }
-        } else {
-            const Source *list[1] = {&b.W};
-            RUN(launch_pack(list, 1, p.dtype, st));
-        }
+        RUN(launch_pack(list, f32 ? 2 : 3, p.dtype, st));
         ProductArgs a{};
         a.A = b.X.operand(p.dtype);
         a.B = b.W.operand(p.dtype);

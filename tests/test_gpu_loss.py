@@ -156,7 +156,7 @@ def test_loss_and_gradients(g, shape, dtype):
 
 @pytest.mark.parametrize("dtype", list(T))
 def test_pieces_of_the_vocabulary(g, dtype):
-    """dZ beyond 256 MB: several pieces, the last of them short."""
+    """dZ beyond 512 MB: several pieces, the last of them short."""
     n, k, v = (9001, 72, 33003)
     X, W, b, t = _inputs(n, k, v, dtype)
     _check(g, X, W, b, t, torch.full((n,), 1.0 if dtype == "f16" else 1.0 / n, device=DEV), dtype,

@@ -193,7 +193,7 @@ def test_loss_buffers_are_refused(g):
 
 def test_loss_workspaces(g):
     """No logits: the forward call keeps 8 bytes a row and tile, the gradients
-    a piece of about 256 MB whatever the vocabulary."""
+    a piece of up to 512 MB whatever the vocabulary."""
     L = g.lib()
 
     def size(back, **kw):
@@ -203,8 +203,9 @@ def test_loss_workspaces(g):
 
     for v in (50000, 100000, 1 << 20):
         assert size(0, v=v) <= 8192 * 8 * (v // 64 + 2) + 8192 * 16
-        assert size(1, v=v) <= (256 << 20) + 8192 * 512 * 4 + 8192 * 64 + 8192 // 32 * 32768 * 4 + \
-            (256 << 20)
+        # dZ, dX's sum, X under its shares, sums of the bias, parts of split tiles
+        assert size(1, v=v) <= (512 << 20) + 8192 * 512 * 6 + 8192 * 64 + 8192 // 32 * 32768 * 4 + \
+            (64 << 20)
     assert size(0, v=50000, aligned16=0) >= size(0, v=50000) + (8192 + 50000) * 512 * 2
 
 
