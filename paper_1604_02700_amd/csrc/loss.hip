@@ -50,7 +50,9 @@ struct FewArgs {
 };
 
 // The products of 16 columns and up to 16 NB rows a workgroup, whose waves share
-// the contraction in turns; wave b < NB ends with rows 16 b .. 16 b + 15 (true), a
+// the contraction in turns (bound by reading W: one bfloat16 row, 4,096 -> 65,000,
+// 109 us with the join, 4.9 TB/s; 2,048 -> 32,000 30 us and 5 for the join;
+// workgroups that stay and read a block ahead spilled at 16 waves, 45 for 38); wave b < NB ends with rows 16 b .. 16 b + 15 (true), a
 // lane with four columns (4 (lane / 16) on) of `row`.
 template <int DT, int NB, int WAVES>
 __device__ __forceinline__ bool few_logits(const FewArgs &a, f32x4 &v, int64_t &row)
@@ -220,16 +222,18 @@ __global__ __launch_bounds__(256) void join_kernel(JoinArgs a)
         for (int64_t s = l; s < a.strips; s += kLanes)
             v = merge(v, a.strip[s * a.n + row]);
     }
-    __shared__ float2 all[256];
-    all[threadIdx.x] = v;
-    for (int o = kLanes / 2; o > 0; o >>= 1) {
-        __syncthreads();
-        if (l < o)
-            all[threadIdx.x] = merge(all[threadIdx.x], all[threadIdx.x + o * ROWS]);
-    }
+#pragma unroll
+    for (int o = ROWS; o < 64; o <<= 1)
+        v = merge(v, make_float2(__shfl_xor(v.x, o, 64), __shfl_xor(v.y, o, 64)));
+    __shared__ float2 all[4][ROWS];
+    if ((threadIdx.x & 63) < ROWS)
+        all[threadIdx.x >> 6][threadIdx.x & 63] = v;
+    __syncthreads();
     if (l > 0 || row >= a.n)
         return;
-    v = all[threadIdx.x];
+#pragma unroll
+    for (int w = 1; w < 4; ++w)
+        v = merge(v, all[w][r]);
     // (no other entry: -inf)
     const float others = v.x + logf(v.y);
     const int64_t t = target_at(a.targets, a.wide, row);
@@ -298,7 +302,7 @@ __global__ __launch_bounds__(256) void rows_kernel(RowsArgs a)
 
 // G, the largest |g|, and each row's g / G; up to kRowsAtOnce rows' LossRow too
 // (else `most` holds `count` workgroups' largest).
-constexpr int64_t kRowsAtOnce = 16384;
+constexpr int64_t kRowsAtOnce = 4096;
 
 __global__ __launch_bounds__(1024) void shares_kernel(RowsArgs a, int64_t count, float *largest,
                                                       float *share)
