@@ -331,7 +331,7 @@ struct Epilogue {
     const void *targets;
     int wide;
     float2 *strip;
-    float *picked;
+    double *picked;
     // kEpiSoft: rows, the column that the piece starts at, where exp(z - lse) -
     // [target] goes (p_hi, ldp; times 2^kSoftPower but in bfloat16), [row blocks][N]
     // column sums of it times g, or null

@@ -44,7 +44,7 @@ __device__ __forceinline__ int64_t target_at(const void *t, int wide, int64_t ro
 struct FewArgs {
     const void *X, *W, *bias, *targets;
     float2 *strip;             // [blocks of 16 columns][n]
-    float *picked;
+    double *picked;
     int64_t ldx, ldw, n, k, v;
     int wide;
 };
@@ -55,7 +55,7 @@ struct FewArgs {
 // workgroups that stay and read a block ahead spilled at 16 waves, 45 for 38); wave b < NB ends with rows 16 b .. 16 b + 15 (true), a
 // lane with four columns (4 (lane / 16) on) of `row`.
 template <int DT, int NB, int WAVES>
-__device__ __forceinline__ bool few_logits(const FewArgs &a, f32x4 &v, int64_t &row)
+__device__ __forceinline__ bool few_logits(const FewArgs &a, double (&v)[4], int64_t &row)
 {
     constexpr int kValues = DT == GPIC_F32 ? 4 : 8;       // of k a lane loads at once
     constexpr int kSize = DT == GPIC_F32 ? 4 : 2;
@@ -106,18 +106,24 @@ __device__ __forceinline__ bool few_logits(const FewArgs &a, f32x4 &v, int64_t &
     if (wave >= NB)
         return false;
     row = row0 + wave * 16 + r;
-    v = part[0][wave][lane];
 #pragma unroll
-    for (int s = 1; s < WAVES; ++s)
-        v += part[s][wave][lane];
+    for (int j = 0; j < 4; ++j)
+        v[j] = 0.0;
+#pragma unroll
+    for (int s = 0; s < WAVES; ++s)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            v[j] += (double)part[s][wave][lane][j];
     return true;
 }
 
-// Each row's largest and sum of exponentials over 16 columns.
+// Each row's largest and sum of exponentials over 16 columns.  The waves' sums of
+// a logit meet in float64, and so do the target's and the others' later: a loss
+// is the small difference of both, a float32 of 18 is 10^-6 off.
 template <int DT, int NB, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void few_lse_kernel(FewArgs a)
 {
-    f32x4 v;
+    double v[4];
     int64_t row;
     if (!few_logits<DT, NB, WAVES>(a, v, row))
         return;
@@ -129,24 +135,24 @@ __global__ __launch_bounds__(64 * WAVES) void few_lse_kernel(FewArgs a)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const int64_t col = col0 + g * 4 + j;
-        float z = -INFINITY;
+        double z = -INFINITY;
         if (col < a.v) {
             const float bias = a.bias ? load1(a.bias, col, DT) : 0.0f;
-            z = bias == -INFINITY ? bias : v[j] + bias;
+            z = bias == -INFINITY ? (double)bias : v[j] + (double)bias;
             if (col == t) {
                 a.picked[row] = z;
                 z = -INFINITY;
             }
         }
         v[j] = z;
-        m = fmaxf(m, z);
+        m = fmaxf(m, (float)z);
     }
     m = fmaxf(m, __shfl_xor(m, 16, 64));
     m = fmaxf(m, __shfl_xor(m, 32, 64));
-    const float at = m == -INFINITY ? 0.0f : m;
+    const double at = m == -INFINITY ? 0.0 : (double)m;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-        s += __builtin_amdgcn_exp2f((v[j] - at) * kLog2e);
+        s += __builtin_amdgcn_exp2f((float)(v[j] - at) * kLog2e);
     s += __shfl_xor(s, 16, 64);
     s += __shfl_xor(s, 32, 64);
     if (live && g == 0)
@@ -166,7 +172,7 @@ template <int NB, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void small_soft_kernel(SmallArgs s)
 {
     const FewArgs &a = s.f;
-    f32x4 v;
+    double v[4];
     int64_t row;
     const int g = (threadIdx.x & 63) >> 4;
     {
@@ -193,7 +199,7 @@ __global__ __launch_bounds__(64 * WAVES) void small_soft_kernel(SmallArgs s)
             break;
         const float bias = a.bias ? load1(a.bias, col, GPIC_F32) : 0.0f;
         float d = col == t ? expm1f(-loss)
-                           : __builtin_amdgcn_exp2f((v[j] + bias - lse) * kLog2e);
+                           : __builtin_amdgcn_exp2f((float)(v[j] + bias - lse) * kLog2e);
         d = bias == -INFINITY && col != t ? 0.0f : d;
         s.D[row * a.v + col] = live ? d * gl : 0.0f;
     }
@@ -202,7 +208,7 @@ __global__ __launch_bounds__(64 * WAVES) void small_soft_kernel(SmallArgs s)
 // ------------------------------------------------------------------ join
 struct JoinArgs {
     const float2 *strip;       // [strips][n]
-    const float *picked;
+    const double *picked;
     const void *targets;
     float *loss, *lse;
     int64_t n, strips, v;
@@ -235,22 +241,22 @@ __global__ __launch_bounds__(256) void join_kernel(JoinArgs a)
     for (int w = 1; w < 4; ++w)
         v = merge(v, all[w][r]);
     // (no other entry: -inf)
-    const float others = v.x + logf(v.y);
+    const double others = (double)v.x + (double)logf(v.y);
     const int64_t t = target_at(a.targets, a.wide, row);
-    float loss = 0.0f, lse = others;
+    double loss = 0.0, lse = others;
     if (t >= 0 && t < a.v) {
-        const float z = a.picked[row], d = others - z;
+        const double z = a.picked[row], d = others - z;
         // softplus(d), the larger of both logits apart; an infinite or NaN
         // logit makes it NaN, a target without probability infinite
-        const float tail = log1pf(expf(-fabsf(d)));
-        loss = z == INFINITY ? NAN : (d > 0.0f ? d + tail : tail);
-        lse = z == -INFINITY ? others : fmaxf(others, z) + tail;
+        const double tail = (double)log1pf(expf(-fabsf((float)d)));
+        loss = z == INFINITY ? NAN : (d > 0.0 ? d + tail : tail);
+        lse = z == -INFINITY ? others : fmax(others, z) + tail;
         if (d != d)
             loss = lse = NAN;
     }
-    a.loss[row] = loss;
+    a.loss[row] = (float)loss;
     if (a.lse)
-        a.lse[row] = lse;
+        a.lse[row] = (float)lse;
 }
 
 // -------------------------------------------------------------- backward
@@ -465,10 +471,10 @@ struct Forward {
     Source X{}, W{};
     int64_t strips;
     float2 *strip;
-    float *picked;
+    double *picked;
     Forward(const Loss &p, const void *x, const void *w, Cursor &c)
     {
-        picked = static_cast<float *>(c.take((size_t)p.n * 4));
+        picked = static_cast<double *>(c.take((size_t)p.n * 8));
         if (few(p)) {
             strips = (p.v + 15) / 16;
         } else {
