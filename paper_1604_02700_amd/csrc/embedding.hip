@@ -176,21 +176,24 @@ __device__ __forceinline__ void add_batches(int64_t j0, int64_t j1, Get get, Loa
 // A workgroup for every position and strip of 512 columns: where no earlier
 // position has the same id, its waves list the ones that do and add a quarter
 // each.
+constexpr int kFewWaves = 4;
+
 template <int DT, bool WIDE, bool TINY>
-__global__ __launch_bounds__(256) void few_ids_kernel(TableArgs a)
+__global__ __launch_bounds__(64 * kFewWaves) void few_ids_kernel(TableArgs a)
 {
     const int64_t i = blockIdx.x / a.strips, strip = blockIdx.x % a.strips;
     const int64_t id = id_at<WIDE>(a.ids, i, a.rows);
     if (id < 0)
         return;
     int earlier = 0;
-    for (int64_t j = threadIdx.x; j < i; j += 256)
+    for (int64_t j = threadIdx.x; j < i; j += 64 * kFewWaves)
         earlier |= id_at<WIDE>(a.ids, j, a.rows) == id;
     if (__syncthreads_or(earlier))
         return;
-    __shared__ int list[4][kFewIds / 4 + 64], found[4];
+    // each wave lists its run of positions; together they are in order
+    __shared__ int list[kFewWaves][kFewIds / kFewWaves + 64], found[kFewWaves];
     const int lane = threadIdx.x & 63, wave = (int)wave_index();
-    const int64_t each = (a.n - i + 255) / 256 * 64;
+    const int64_t each = (a.n - i + 64 * kFewWaves - 1) / (64 * kFewWaves) * 64;
     const int64_t j0 = i + wave * each, j1 = j0 + each < a.n ? j0 + each : a.n;
     int count = 0;
     for (int64_t j = j0; j < j1; j += 64) {
@@ -203,21 +206,35 @@ __global__ __launch_bounds__(256) void few_ids_kernel(TableArgs a)
     if (lane == 0)
         found[wave] = count;
     __syncthreads();
-    const int e1 = found[0], e2 = e1 + found[1], e3 = e2 + found[2], total = e3 + found[3];
+    int end[kFewWaves];
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w)
+        end[w] = found[w] + (w ? end[w - 1] : 0);
+    const int total = end[kFewWaves - 1];
     const Window<DT, TINY> window((strip * 64 + lane) * 8, a.k);
     f32x8 sum[1];
     sum[0] = 0.0f;
-    add_batches(total * wave / 4, total * (wave + 1) / 4,
+    add_batches(total * wave / kFewWaves, total * (wave + 1) / kFewWaves,
                 [&](int64_t e) {
-                    const int w = (e >= e1) + (e >= e2) + (e >= e3);
-                    return (int64_t)list[w][e - (w == 0 ? 0 : (w == 1 ? e1 : (w == 2 ? e2 : e3)))];
+                    int w = 0, before = 0;
+#pragma unroll
+                    for (int k = 0; k + 1 < kFewWaves; ++k)
+                        if (e >= end[k]) {
+                            w = k + 1;
+                            before = end[k];
+                        }
+                    return (int64_t)list[w][e - before];
                 },
                 [&](int64_t row, int) { return window.load(a.dY, row * a.ldy); }, sum);
-    __shared__ f32x8 part[4][64];
+    __shared__ f32x8 part[kFewWaves][64];
     part[wave][lane] = sum[0];
     __syncthreads();
-    if (wave == 0)
-        put(a, id, window, ((part[0][lane] + part[1][lane]) + part[2][lane]) + part[3][lane]);
+    if (wave > 0)
+        return;
+#pragma unroll
+    for (int w = 1; w < kFewWaves; ++w)
+        sum[0] += part[w][lane];
+    put(a, id, window, sum[0]);
 }
 
 // ------------------------------------------------------------------- sort
@@ -551,13 +568,13 @@ hipError_t few_ids(const Embedding &p, const TableArgs &a, hipStream_t st)
         return hipSuccess;
     const unsigned blocks = (unsigned)(p.n * a.strips);
     if (p.k < 8 && p.wide)
-        few_ids_kernel<DT, true, true><<<blocks, 256, 0, st>>>(a);
+        few_ids_kernel<DT, true, true><<<blocks, 64 * kFewWaves, 0, st>>>(a);
     else if (p.k < 8)
-        few_ids_kernel<DT, false, true><<<blocks, 256, 0, st>>>(a);
+        few_ids_kernel<DT, false, true><<<blocks, 64 * kFewWaves, 0, st>>>(a);
     else if (p.wide)
-        few_ids_kernel<DT, true, false><<<blocks, 256, 0, st>>>(a);
+        few_ids_kernel<DT, true, false><<<blocks, 64 * kFewWaves, 0, st>>>(a);
     else
-        few_ids_kernel<DT, false, false><<<blocks, 256, 0, st>>>(a);
+        few_ids_kernel<DT, false, false><<<blocks, 64 * kFewWaves, 0, st>>>(a);
     return hipGetLastError();
 }
 
