@@ -732,14 +732,14 @@ def _matrix_of(t, rows, cols, like, name):
     return t
 
 
-def _layer_type(X):
+def _layer_type(X, name="X", shape="[n, k]"):
     if not isinstance(X, torch.Tensor) or not X.is_cuda:
-        raise TypeError("X must be a CUDA (HIP) tensor")
+        raise TypeError(f"{name} must be a CUDA (HIP) tensor")
     if X.dtype not in DTYPES:
-        raise TypeError(f"X must be float32, float16 or bfloat16, got {X.dtype}")
+        raise TypeError(f"{name} must be float32, float16 or bfloat16, got {X.dtype}")
     if X.dim() != 2:
-        raise ValueError("X must be [n, k]")
-    return _matrix_of(X, X.shape[0], X.shape[1], X, "X")
+        raise ValueError(f"{name} must be {shape}")
+    return _matrix_of(X, X.shape[0], X.shape[1], X, name)
 
 
 def _activation(name):
@@ -1093,14 +1093,8 @@ def gpic_embedding(ids: torch.Tensor, T: torch.Tensor, scale: float = 1.0,
     """Y = scale * T[ids] for ids [n] (int32 or int64) and a table T [rows, k]
     (float32, float16 or bfloat16).  An id outside the table is padding: its
     row of Y is zeros."""
-    if not isinstance(T, torch.Tensor) or not T.is_cuda:
-        raise TypeError("T must be a CUDA (HIP) tensor")
-    if T.dtype not in DTYPES:
-        raise TypeError(f"T must be float32, float16 or bfloat16, got {T.dtype}")
-    if T.dim() != 2:
-        raise ValueError("T must be [rows, k]")
+    T = _layer_type(T, "T", "[rows, k]")
     rows, k = T.shape
-    T = _matrix_of(T, rows, k, T, "T")
     ids = _ids(ids, None, T.device, "ids")
     n = ids.shape[0]
     given, Y = Y, _output(Y, n, k, T, "Y")
@@ -1120,7 +1114,7 @@ def gpic_embedding_backward(dY: torch.Tensor, ids: torch.Tensor, rows: int, scal
     rows: dT[v] = scale * sum of the rows of dY whose id is v, in a fixed
     order.  accumulate: dT (given) is added to, and its other rows stay, as a
     table that is also the weights of gpic_cross_entropy wants it."""
-    dY = _layer_type(dY)
+    dY = _layer_type(dY, "dY")
     n, k = dY.shape
     rows = int(rows)
     ids = _ids(ids, n, dY.device, "ids")

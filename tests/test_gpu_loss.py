@@ -326,3 +326,72 @@ def test_gradients_against_differences(g):
         # most, and the losses' float32 error (2e-6 each) over 2 h
         tol = h * h * float(dloss.abs().sum()) + 2e-6 * float(dloss.abs().sum()) / h
         assert abs(slope - want) <= tol, (which, slope, want, tol)
+
+
+@pytest.mark.parametrize("n", [2, 40])
+def test_weights_beyond_32_bits(g, n):
+    """v k > 2^32 values of W and dW."""
+    v, k = 1 << 20, 4120
+    print(f"loss n={n} k={k} v={v}", flush=True)
+    W = torch.empty((v, k), dtype=T["bf16"], device=DEV)
+    for i in range(0, v, 65536):
+        W[i:i + 65536] = _randn((65536, k), "bf16", i, k ** -0.5)
+    X = _randn((n, k), "bf16", 1)
+    t = torch.tensor([v - 1, 2 ** 32 // k + 1] * (n // 2), device=DEV)
+    loss, lse = g.gpic_cross_entropy(X, W, t, want_lse=True)
+    z = torch.cat([X.double() @ W[i:i + 65536].double().t() for i in range(0, v, 65536)], 1)
+    full = z.logsumexp(1)
+    # logits of size one: (K + 16) e of sum |x||w| (at most 70) each, weighted; 8,192 joins of
+    # strips by 256 lanes (n = 2: 256 a lane) or 16 lanes, 4 e each
+    tol = (k + 16) * E * 70 + 4 * (v / 256 / 16 + 40) * E + 4 * E * float(full.abs().max())
+    _within(lse, full, torch.full_like(full, tol), "lse")
+    _within(loss, full - z.gather(1, t[:, None])[:, 0], torch.full_like(full, 2 * tol), "loss")
+    if n == 2:
+        return
+    gr = g.gpic_cross_entropy_backward(torch.ones(n, device=DEV), X, W, t, loss, lse)
+    rows = torch.tensor([0, 1, 2 ** 31 // k, 2 ** 32 // k - 1, 2 ** 32 // k, 2 ** 32 // k + 1, v - 2,
+                         v - 1], device=DEV)
+    d = (z - full[:, None]).exp()
+    d[torch.arange(n, device=DEV), t] -= 1.0
+    x = X.double()
+    off = (U["bf16"] + 2 * tol) * d.abs()
+    _close(gr.dW[rows], d[:, rows].t() @ x, (off[:, rows].t() + 60 * E * d[:, rows].abs().t()) @ x.abs(),
+           "bf16", "dW")
+    dX, size = torch.zeros((n, k), dtype=torch.float64, device=DEV), 0.0
+    for i in range(0, v, 65536):
+        w = W[i:i + 65536].double()
+        dX += d[:, i:i + 65536] @ w
+        size = size + d[:, i:i + 65536].abs() @ w.abs()
+    # float32 sums of v products, of random sign: 4 sqrt(v) of their roundings at the most
+    # likely worst, and one rounding of dZ each
+    _close(gr.dX, dX, (U["bf16"] + 2 * tol + 4 * math.sqrt(v) * E) * size, "bf16", "dX")
+    del W, gr, z, d
+    torch.cuda.empty_cache()
+
+
+def test_gradients_of_logits_beyond_32_bits(g):
+    """A piece's dZ of more than 2^32 values: the rows on both sides of 2^31 and
+    2^32, and the weights' gradient in chunks."""
+    n, k, v = 2 ** 21 + 300, 24, 2100
+    print(f"loss n={n} k={k} v={v}", flush=True)
+    X, W = _randn((n, k), "bf16", 1), _randn((v, k), "bf16", 2, k ** -0.5)
+    t = torch.arange(n, device=DEV) % v
+    loss, lse = g.gpic_cross_entropy(X, W, t, want_lse=True)
+    gr = g.gpic_cross_entropy_backward(torch.ones(n, device=DEV), X, W, t, loss, lse)
+    w = W.double()
+    rows = sorted({2 ** p // 2304 + d for p in (31, 32) for d in (-1, 0, 1)}
+                  | {2 ** p // 2112 + d for p in (31, 32) for d in (-1, 0, 1) if 2 ** p // 2112 + d < n}
+                  | {0, 1, n - 2, n - 1})
+    z = X[rows].double() @ w.t()
+    d = (z - z.logsumexp(1, keepdim=True)).exp()
+    d[torch.arange(len(rows), device=DEV), t[rows]] -= 1.0
+    _close(gr.dX[rows], d @ w, (U["bf16"] + 1e-5 + (v + 48) * E) * (d.abs() @ w.abs()), "bf16", "dX")
+    dW, size = torch.zeros((v, k), dtype=torch.float64, device=DEV), 0.0
+    for i in range(0, n, 100000):
+        x = X[i:i + 100000].double()
+        z = x @ w.t()
+        d = (z - z.logsumexp(1, keepdim=True)).exp()
+        d[torch.arange(len(x), device=DEV), t[i:i + 100000]] -= 1.0
+        dW += d.t() @ x
+        size = size + d.abs().t() @ x.abs()
+    _close(gr.dW, dW, (U["bf16"] + 1e-5 + 4 * math.sqrt(n) * E) * size, "bf16", "dW")

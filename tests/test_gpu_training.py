@@ -350,3 +350,81 @@ def test_dropout_beyond_32_bits(g, pitched):
     assert bool((tail[torch.from_numpy(want)] == 2).all())
     del X, Y
     torch.cuda.empty_cache()
+
+
+# ------------------------------------------------- beyond 32 bits of values
+def _filled(shape, dtype, seed):
+    t = torch.empty(shape, dtype=T[dtype], device=DEV)
+    gen = torch.Generator(device=DEV).manual_seed(seed)
+    for i in range(0, shape[0], 16384):
+        t[i:i + 16384] = torch.randn((min(16384, shape[0] - i), shape[1]), device=DEV,
+                                     generator=gen).to(t.dtype)
+    return t
+
+
+def test_norm_beyond_32_bits(g):
+    """n k > 2^32: the rows on both sides of 2^31 and 2^32 values, and the last."""
+    n, k = 1050000, 4100
+    print(f"norm n={n} k={k}", flush=True)
+    X, dY = _filled((n, k), "bf16", 1), _filled((n, k), "bf16", 2)
+    w, b = (1 + _randn((k,), "f32", 3, 0.2)).to(T["bf16"]), _randn((k,), "bf16", 4)
+    Y, stats = g.gpic_layer_norm(X, w, b, want_stats=True)
+    gr = g.gpic_layer_norm_backward(dY, X, w, stats)
+    rows = [0, 1, 2 ** 31 // k - 1, 2 ** 31 // k, 2 ** 31 // k + 1, 2 ** 32 // k - 1, 2 ** 32 // k,
+            2 ** 32 // k + 1, n - 2, n - 1]
+    x, dy = X[rows].contiguous(), dY[rows].contiguous()
+    ref, s = g.gpic_layer_norm(x, w, b, want_stats=True)
+    assert torch.equal(Y[rows], ref) and torch.equal(stats[rows], s)
+    assert torch.equal(gr.dX[rows], g.gpic_layer_norm_backward(dy, x, w, s).dX)
+    db, size = (torch.zeros(k, dtype=torch.float64, device=DEV) for _ in range(2))
+    for i in range(0, n, 50000):
+        d = dY[i:i + 50000].double()
+        db, size = db + d.sum(0), size + d.abs().sum(0)
+    # (rows of a wave: n / 512 one after another at most)
+    _close(gr.db, db, (n / 512 + 32) * E * size, "bf16", "db")
+    del X, dY, Y, gr
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("n", [100, 5000])
+def test_embedding_beyond_32_bits(g, n):
+    """A table and its gradient of more than 2^32 values."""
+    rows, k = 140000, 32768
+    print(f"embedding n={n} rows={rows} k={k}", flush=True)
+    Tb = torch.zeros((rows, k), dtype=T["bf16"], device=DEV)
+    some = torch.tensor([0, 1, 2 ** 31 // k - 1, 2 ** 31 // k, 2 ** 32 // k - 1, 2 ** 32 // k,
+                         2 ** 32 // k + 1, rows - 2, rows - 1], device=DEV)
+    Tb[some] = _randn((len(some), k), "bf16", 1)
+    ids = some[torch.arange(n, device=DEV) % len(some)]
+    assert torch.equal(g.gpic_embedding(ids[:20], Tb), Tb[ids[:20]])
+    dY = _randn((n, k), "bf16", 2)
+    dT = Tb                            # every row is written
+    dT.fill_(5.0)
+    g.gpic_embedding_backward(dY, ids, rows, dT=dT)
+    for i, v in enumerate(some.tolist()):
+        d = dY[i::len(some)].double()
+        _close(dT[v], d.sum(0), (min(len(d), 512) + 64) * E * d.abs().sum(0), "bf16", f"row {v}")
+    total = sum(float(dT[i:i + 10000].abs().sum(dtype=torch.float64)) for i in range(0, rows, 10000))
+    kept = float(dT[some].abs().sum(dtype=torch.float64))
+    assert abs(total - kept) <= 1e-9 * kept          # the other rows are zeros
+    del Tb, dT
+    torch.cuda.empty_cache()
+
+
+def test_embedding_of_many_ids_beyond_32_bits(g):
+    """n k > 2^32 values of Y and dY."""
+    n, k, rows = 2 ** 23 + 4099, 512, 3000
+    print(f"embedding n={n} k={k}", flush=True)
+    Tb = _randn((rows, k), "bf16", 1)
+    ids = torch.arange(n, device=DEV, dtype=torch.int32) % rows
+    Y = g.gpic_embedding(ids, Tb)
+    at = [0, 2 ** 22 - 1, 2 ** 22, 2 ** 23 - 1, 2 ** 23, n - 1]
+    assert torch.equal(Y[at], Tb[[i % rows for i in at]])
+    # every row of dY one value: sums of up to 2,798 whole numbers are exact
+    Y.copy_(((torch.arange(n, device=DEV) // rows) % 2).to(Y.dtype)[:, None].expand(n, k))
+    dT = g.gpic_embedding_backward(Y, ids, rows)
+    count = torch.bincount(ids.long(), weights=((torch.arange(n, device=DEV) // rows) % 2).double(),
+                           minlength=rows)
+    assert torch.equal(dT.double(), count.to(T["bf16"]).double()[:, None].expand(rows, k))
+    del Y
+    torch.cuda.empty_cache()
