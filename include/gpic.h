@@ -655,14 +655,14 @@ typedef struct gpic_embedding_params {
 gpic_status gpic_embedding(const gpic_embedding_params *p, const void *ids, const void *T, void *Y,
                            void *stream);
 
-/* Workspace bytes of the gradient (0 for up to 2,048 ids, which are not sorted,
+/* Workspace bytes of the gradient (0 for up to 1,024 ids, which are not sorted,
  * and for parameters that the call refuses). */
 size_t gpic_embedding_workspace_bytes(const gpic_embedding_params *p);
 
 /* dT [rows x k] = scale times the sum of the rows of dY with that id (accumulate:
  * plus what dT holds, rounded once more; other rows are not touched), in float32
- * in a fixed order.  Padding has no part in it.  More than 2^28 ids of up to 512
- * columns (n ceil(k / 512) beyond 3 * 2^27) are UNSUPPORTED.
+ * in a fixed order.  Padding has no part in it.  n ceil(k / 512) beyond 3 * 2^28
+ * is UNSUPPORTED.
  * ws: gpic_embedding_workspace_bytes(p). */
 gpic_status gpic_embedding_backward(const gpic_embedding_params *p, const void *dY,
                                     const void *ids, void *dT, void *ws, size_t ws_bytes,

@@ -6,7 +6,7 @@
 // their positions (stable), every row of the table finds its run, and a wave
 // adds a run of up to 16 rows of dY, eight columns a lane.  Longer runs
 // (tokens as frequent as words are) are cut where the sorted positions pass
-// multiples of 16; the cuts' sums are added by a workgroup in a second launch.
+// multiples of 16; the cuts' sums are added by a second launch.
 // A few ids are not sorted: each position compares itself with all of them.
 #include "training.h"
 
@@ -14,7 +14,7 @@ namespace gpic {
 namespace {
 
 constexpr int kRun = 16;               // longest run that one wave adds
-constexpr int64_t kFewIds = 2048;      // compared one by one
+constexpr int64_t kFewIds = 1024;      // compared one by one
 
 struct TableArgs {
     const void *ids, *T, *dY;
@@ -27,7 +27,14 @@ struct TableArgs {
     const int32_t *pos;
     uint32_t *start;
     float *part;
+    struct CutRun *run;
     int64_t strips;
+};
+
+// The run longer than 16 that starts in a chunk: its row of the table, the chunk
+// after its last (the chunk itself: there is none), its first sum's slot.
+struct CutRun {
+    uint32_t row, end, slot, unused;
 };
 
 // id i, or -1 where it is outside the table
@@ -174,9 +181,9 @@ __device__ __forceinline__ void add_batches(int64_t j0, int64_t j1, Get get, Loa
 }
 
 // A workgroup for every position and strip of 512 columns: where no earlier
-// position has the same id, its waves list the ones that do and add a quarter
+// position has the same id, its waves list the ones that do and add an eighth
 // each.
-constexpr int kFewWaves = 4;
+constexpr int kFewWaves = 8;
 
 template <int DT, bool WIDE, bool TINY>
 __global__ __launch_bounds__(64 * kFewWaves) void few_ids_kernel(TableArgs a)
@@ -398,115 +405,110 @@ __device__ __forceinline__ void add_rows(const TableArgs &a, int64_t j0, int64_t
 }
 
 // Of the runs longer than 16, what lies in a chunk of 16 sorted positions: the
-// run that the chunk begins in (slot 0) and the one that it ends in (slot 1).
+// run that the chunk begins in (slot 0) and the one that it ends in (slot 1); and
+// which of them starts here.
 template <int DT, bool TINY>
-__global__ __launch_bounds__(256) void cuts_kernel(TableArgs a)
+__device__ __forceinline__ void cut_runs(const TableArgs &a, int64_t t)
 {
-    const int64_t chunks = (a.n + kRun - 1) / kRun, tasks = chunks * a.strips;
-    for (int64_t t = (int64_t)blockIdx.x * 4 + wave_index(); t < tasks;
-         t += (int64_t)gridDim.x * 4) {
-        const int64_t c = a.strips == 1 ? t : t / a.strips;
-        const Window<DT, TINY> w[1] = {
-            Window<DT, TINY>(((t - c * a.strips) * 64 + (threadIdx.x & 63)) * 8, a.k)};
-        const int64_t first = c * kRun, end = first + kRun < a.n ? first + kRun : a.n;
-        const int64_t head = shared_load(a.key, first), tail = shared_load(a.key, end - 1);
-#pragma unroll
-        for (int slot = 0; slot < 2; ++slot) {
-            const int64_t v = slot ? tail : head;
-            if (v >= a.rows || (slot && tail == head))
-                break;
-            const int64_t s0 = shared_load(a.start, v), s1 = shared_load(a.start, v + 1);
-            if (s1 - s0 <= kRun)
-                continue;
-            f32x8 sum[1];
-            add_rows(a, s0 > first ? s0 : first, s1 < end ? s1 : end, w, sum);
-            if (w[0].skip < 8)
-                w[0].store(a.part, (c * 2 + slot) * a.k, sum[0], GPIC_F32);
-        }
+    const int64_t c = a.strips == 1 ? t : t / a.strips, strip = t - c * a.strips;
+    const Window<DT, TINY> w[1] = {Window<DT, TINY>((strip * 64 + (threadIdx.x & 63)) * 8, a.k)};
+    const int64_t first = c * kRun, end = first + kRun < a.n ? first + kRun : a.n;
+    const int64_t head = shared_load(a.key, first), tail = shared_load(a.key, end - 1);
+    CutRun run{0, (uint32_t)c, 0, 0};
+    // (not unrolled: one copy of the sums' code)
+#pragma unroll 1
+    for (int slot = 0; slot < 2; ++slot) {
+        const int64_t v = slot ? tail : head;
+        if (v >= a.rows || (slot && tail == head))
+            break;
+        const int64_t s0 = shared_load(a.start, v), s1 = shared_load(a.start, v + 1);
+        if (s1 - s0 <= kRun)
+            continue;
+        if (s0 >= first)
+            run = CutRun{(uint32_t)v, (uint32_t)((s1 - 1) / kRun + 1), (uint32_t)slot, 0};
+        f32x8 sum[1];
+        add_rows(a, s0 > first ? s0 : first, s1 < end ? s1 : end, w, sum);
+        if (w[0].skip < 8)
+            w[0].store(a.part, (c * 2 + slot) * a.k, sum[0], GPIC_F32);
     }
+    if (strip == 0 && (threadIdx.x & 63) == 0)
+        a.run[c] = run;
 }
 
-// The cuts' sums of the runs that start in eight chunks, a wave a chunk; of a
-// run of more than eight cuts (no two can start within eight chunks) by all
-// waves of the workgroup.
-constexpr int kJoinWaves = 8;
+// The cuts' sums of the runs that start in sixteen chunks, a wave a chunk; of a
+// run of more than sixteen cuts (no two can start within sixteen chunks) by all
+// waves of the workgroup.  Bound by latency: where a run is, then its cuts' sums.
+constexpr int kJoinWaves = 16;
 
 template <int DT, bool TINY>
-__device__ __forceinline__ void join_cuts(const TableArgs &a, int64_t t)
+__global__ __launch_bounds__(64 * kJoinWaves) void join_cuts_kernel(TableArgs a)
 {
     __shared__ f32x8 all[kJoinWaves][64];
-    __shared__ int long_run;
     const int lane = threadIdx.x & 63;
     const int64_t wave = wave_index(), chunks = (a.n + kRun - 1) / kRun;
-    const int64_t block = t / a.strips, mine = block * kJoinWaves + wave;
-    const Window<DT, TINY> w(((t - block * a.strips) * 64 + lane) * 8, a.k);
-    // chunk c's last run: its row of the table, and the cut after its last (c
-    // where it does not start there or is not cut); the sum over cuts c0 .. c1 - 1
-    auto row_of = [&](int64_t c) {
-        const int64_t end = (c + 1) * kRun < a.n ? (c + 1) * kRun : a.n;
-        return (int64_t)shared_load(a.key, end - 1);
-    };
-    auto cuts_of = [&](int64_t c, int64_t v) {
-        if (v >= a.rows)
-            return c;
-        const int64_t j0 = shared_load(a.start, v), j1 = shared_load(a.start, v + 1);
-        return j0 < c * kRun || j1 - j0 <= kRun ? c : (j1 - 1) / kRun + 1;
-    };
-    auto add = [&](int64_t c, int64_t v, int64_t c0, int64_t c1, f32x8 (&sum)[1]) {
-        const bool within = (int64_t)shared_load(a.start, v) > c * kRun;
-        sum[0] = 0.0f;
-        add_batches(c0, c1, [&](int64_t i) { return i * 2 + (i == c && within); },
-                    [&](int64_t slot, int) { return w.load_sum(a.part, slot * a.k); }, sum);
-    };
-    if (threadIdx.x == 0)
-        long_run = -1;
-    __syncthreads();
-    f32x8 sum[1];
-    if (mine < chunks) {
-        const int64_t v = row_of(mine), c1 = cuts_of(mine, v);
-        if (c1 - mine > kJoinWaves) {
-            if (lane == 0)
-                long_run = (int)wave;
-        } else if (c1 > mine) {
-            add(mine, v, mine, c1, sum);
-            put(a, v, w, sum[0]);
+    const int64_t block = a.strips == 1 ? (int64_t)blockIdx.x : blockIdx.x / a.strips;
+    const int64_t strip = blockIdx.x - block * a.strips;
+    const Window<DT, TINY> w((strip * 64 + lane) * 8, a.k);
+    // the runs of the workgroup's chunks, one a lane
+    const int64_t c0 = block * kJoinWaves, its = c0 + (lane < kJoinWaves ? lane : 0);
+    CutRun run{0, (uint32_t)its, 0, 0};
+    if (lane < kJoinWaves && its < chunks)
+        run = a.run[its];
+    const int cuts = (int)((int64_t)run.end - its);
+    const uint64_t large = __ballot(lane < kJoinWaves && cuts > kJoinWaves);
+    // first this wave's own run, if it is short, then its share of the long one
+    for (int pass = 0; pass < 2; ++pass) {
+        const int which = pass == 0 ? (int)wave : (large ? __builtin_ctzll(large) : 0);
+        const int64_t c = c0 + which;
+        const int64_t count = __builtin_amdgcn_readlane(cuts, which);
+        const int64_t v = (uint32_t)__builtin_amdgcn_readlane((int)run.row, which);
+        const int slot = __builtin_amdgcn_readlane((int)run.slot, which);
+        int64_t i0 = c, i1 = c + count;
+        if (pass == 0 && count > kJoinWaves)
+            continue;
+        if (pass == 1) {
+            if (!large)
+                break;
+            const int64_t each = (count + kJoinWaves - 1) / kJoinWaves;
+            i0 = c + wave * each;
+            i1 = i0 + each < c + count ? i0 + each : c + count;
         }
-    }
-    __syncthreads();
-    const int found = __builtin_amdgcn_readfirstlane(long_run);
-    if (found < 0)
-        return;
-    const int64_t c = block * kJoinWaves + found, v = row_of(c), cuts = cuts_of(c, v) - c;
-    const int64_t each = (cuts + kJoinWaves - 1) / kJoinWaves, c0 = c + wave * each;
-    add(c, v, c0, c0 + each < c + cuts ? c0 + each : c + cuts, sum);
-    all[wave][lane] = sum[0];
-    __syncthreads();
-    if (wave == 0) {
+        f32x8 sum[1];
+        sum[0] = 0.0f;
+        add_batches(i0, i1, [&](int64_t i) { return i * 2 + (i == c ? slot : 0); },
+                    [&](int64_t at, int) { return w.load_sum(a.part, at * a.k); }, sum);
+        if (pass == 0) {
+            if (count > 0)
+                put(a, v, w, sum[0]);
+            continue;
+        }
+        all[wave][lane] = sum[0];
+        __syncthreads();
+        if (wave > 0)
+            break;
         for (int i = 1; i < kJoinWaves; ++i)
             sum[0] += all[i][lane];
         put(a, v, w, sum[0]);
     }
 }
 
-// (In one launch with the rows they would hide behind them, but both then run at
-// the registers of the larger: 43 us for 24.5 and 17.7.)
-template <int DT, bool TINY>
-__global__ __launch_bounds__(64 * kJoinWaves) void join_cuts_kernel(TableArgs a)
-{
-    join_cuts<DT, TINY>(a, blockIdx.x);
-}
-
-// A wave for every row of the table and 1,024 (ONE: 512) columns.  Bound by
-// memory: 32,768 x 1,024 -> 50,000 in bfloat16, ids as frequent as words, 24.5 us
-// (102 MB written, 43 MB read: 5.9 TB/s).
+// The first workgroups cut the long runs, whose chain of loads is hidden behind
+// the others, whose waves take a row of the table and 1,024 (ONE: 512) columns
+// each.
 template <int DT, bool TINY, bool ONE>
-__global__ __launch_bounds__(256) void rows_kernel(TableArgs a)
+__global__ __launch_bounds__(256) void rows_kernel(TableArgs a, int64_t cuts)
 {
+    if ((int64_t)blockIdx.x < cuts) {
+        const int64_t chunks = (a.n + kRun - 1) / kRun;
+        for (int64_t t = (int64_t)blockIdx.x * 4 + wave_index(); t < chunks * a.strips; t += cuts * 4)
+            cut_runs<DT, TINY>(a, t);
+        return;
+    }
     using W = Window<DT, TINY>;
     constexpr int kHold = ONE ? 1 : 2;
     const int64_t strips = (a.strips + kHold - 1) / kHold, tasks = a.rows * strips;
-    for (int64_t t = (int64_t)blockIdx.x * 4 + wave_index(); t < tasks;
-         t += (int64_t)gridDim.x * 4) {
+    for (int64_t t = ((int64_t)blockIdx.x - cuts) * 4 + wave_index(); t < tasks;
+         t += ((int64_t)gridDim.x - cuts) * 4) {
         const int64_t v = strips == 1 ? t : t / strips;
         const int64_t col = ((t - v * strips) * kHold * 64 + (threadIdx.x & 63)) * 8;
         const int64_t j0 = shared_load(a.start, v), j1 = shared_load(a.start, v + 1);
@@ -537,6 +539,7 @@ struct Sorted {
     uint32_t *key[2], *counts, *start;
     int32_t *pos[2];
     float *part;
+    CutRun *run;
     Sorted(const Embedding &p, Cursor &c)
     {
         const size_t n = (size_t)p.n;
@@ -547,6 +550,7 @@ struct Sorted {
         counts = static_cast<uint32_t *>(c.take((size_t)kMostTiles * 256 * 4));
         start = static_cast<uint32_t *>(c.take(((size_t)p.rows + 1) * 4));
         part = static_cast<float *>(c.take((n + kRun - 1) / kRun * 2 * (size_t)p.k * 4));
+        run = static_cast<CutRun *>(c.take((n + kRun - 1) / kRun * sizeof(CutRun)));
     }
 };
 
@@ -612,13 +616,12 @@ hipError_t add_runs(const Embedding &p, const TableArgs &a, hipStream_t st)
 {
     const int64_t chunks = (p.n + kRun - 1) / kRun;
     const int64_t joins = (chunks + kJoinWaves - 1) / kJoinWaves * a.strips;
-    cuts_kernel<DT, TINY><<<capped((chunks * a.strips + 3) / 4), 256, 0, st>>>(a);
-    RUN(hipGetLastError());
-    const int64_t pairs = (a.strips + 1) / 2;
+    const int64_t pairs = (a.strips + 1) / 2, cuts = capped((chunks * a.strips + 3) / 4);
+    const unsigned rows = capped((p.rows * (a.strips == 1 ? 1 : pairs) + 3) / 4);
     if (a.strips == 1)
-        rows_kernel<DT, TINY, true><<<capped((p.rows + 3) / 4), 256, 0, st>>>(a);
+        rows_kernel<DT, TINY, true><<<(unsigned)cuts + rows, 256, 0, st>>>(a, cuts);
     else
-        rows_kernel<DT, TINY, false><<<capped((p.rows * pairs + 3) / 4), 256, 0, st>>>(a);
+        rows_kernel<DT, TINY, false><<<(unsigned)cuts + rows, 256, 0, st>>>(a, cuts);
     RUN(hipGetLastError());
     join_cuts_kernel<DT, TINY><<<(unsigned)joins, 64 * kJoinWaves, 0, st>>>(a);
     return hipGetLastError();
@@ -635,6 +638,7 @@ hipError_t sorted_ids(const Embedding &p, TableArgs a, void *ws, hipStream_t st)
     a.pos = s.pos[at];
     a.start = s.start;
     a.part = s.part;
+    a.run = s.run;
     starts_kernel<<<capped((p.rows + 256) / 256), 256, 0, st>>>(a);
     RUN(hipGetLastError());
     return p.k < 8 ? add_runs<DT, true>(p, a, st) : add_runs<DT, false>(p, a, st);

@@ -397,24 +397,24 @@ __global__ __launch_bounds__(256) void column_max_kernel(ColumnJobs jobs)
             a.part[blockIdx.y * a.cols + col + j] = best[j];
 }
 
-__global__ __launch_bounds__(256) void column_power_kernel(ColumnJobs jobs)
+__global__ __launch_bounds__(1024) void column_power_kernel(ColumnJobs jobs)
 {
     const ColumnArgs a = jobs.j[blockIdx.y];
-    const int64_t col = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63), cols = a.cols;
-    int *power = a.power;
+    const int lane = threadIdx.x & 63, run = threadIdx.x >> 6;
+    const int64_t col = (int64_t)blockIdx.x * 64 + lane;
     float best = 0.0f;
-    if (col < cols) {
+    if (col < a.cols) {
 #pragma unroll 8
-        for (int64_t p = threadIdx.x >> 6; p < a.parts; p += 4)
-            best = fmaxf(best, a.part[p * cols + col]);
+        for (int64_t p = run; p < a.parts; p += 16)
+            best = fmaxf(best, a.part[p * a.cols + col]);
     }
-    __shared__ float all[4][64];
-    all[threadIdx.x >> 6][threadIdx.x & 63] = best;
+    __shared__ float all[16][64];
+    all[run][lane] = best;
     __syncthreads();
-    if (threadIdx.x < 64 && col < cols) {
-        for (int w = 1; w < 4; ++w)
-            best = fmaxf(best, all[w][threadIdx.x]);
-        power[col] = power_for(best);
+    if (run == 0 && col < a.cols) {
+        for (int w = 1; w < 16; ++w)
+            best = fmaxf(best, all[w][lane]);
+        a.power[col] = power_for(best);
     }
 }
 
@@ -609,7 +609,7 @@ hipError_t launch_columns(const Source *const *list, float *const *part, int cou
     column_max_kernel<<<dim3((unsigned)((cols + 255) / 256), (unsigned)most, (unsigned)count), 256,
                         0, st>>>(jobs);
     RUN(hipGetLastError());
-    column_power_kernel<<<dim3((unsigned)((cols + 63) / 64), (unsigned)count), 256, 0, st>>>(jobs);
+    column_power_kernel<<<dim3((unsigned)((cols + 63) / 64), (unsigned)count), 1024, 0, st>>>(jobs);
     return hipGetLastError();
 }
 

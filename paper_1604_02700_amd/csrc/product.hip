@@ -24,13 +24,18 @@ constexpr int kUnits = 256;
 constexpr double kJoin = 4.0;              // the join's launch
 constexpr double kJoinBytes = 3.0e6;       // partial sums written and read, bytes per us
 
-// `n` workgroups of `steps` steps each
-double time_of(const TileCost &c, bool split, int64_t n, double steps)
+// of `fixed` where a tile's results are kept as sums or halves (uncut), by size:
+// the small tiles' start and end weigh more (float32, 1,003 x 700 -> 10,007, us by
+// size: logits 56, 63 and 62, their gradients 66, 73 and 72)
+constexpr double kUncut[3] = {1.0, 1.3, 2.0};
+
+// `n` workgroups of `steps` steps each; `results`: what `fixed` takes times
+double time_of(const TileCost &c, bool split, double results, int64_t n, double steps)
 {
     if (n <= 0)
         return 0.0;
     const int64_t slots = (int64_t)kUnits * c.resident, full = n / slots, rest = n % slots;
-    const double f = split ? c.split : 1.0, fixed = c.fixed * (split ? 1.8 : 1.0);
+    const double f = split ? c.split : 1.0, fixed = c.fixed * (split ? results : 1.0);
     double t = (double)full * (fixed + steps * c.step[c.resident - 1] * f);
     if (rest)
         t += fixed + steps * c.step[(rest - 1) / kUnits] * f;
@@ -61,11 +66,13 @@ Plan product_plan(int64_t M, int64_t N, int64_t K, int64_t batch, int op, int ep
             // a grid of 2^32 threads or more is refused (2^30 rows of a narrow matrix)
             if ((whole + tail * parts) * (c.edge == 256 ? 512 : 256) >= (int64_t)1 << 32)
                 return;
-            double time = time_of(c, split, whole, (double)steps);
+            const double results = uncut(epi) ? kUncut[t] : 1.8;
+            double time = time_of(c, split, results, whole, (double)steps);
             size_t bytes = 0;
             if (tail) {
                 bytes = (size_t)parts * tail * c.edge * c.edge * sizeof(float);
-                time += time_of(c, split, tail * parts, (double)((steps + parts - 1) / parts)) +
+                time += time_of(c, split, results, tail * parts,
+                                (double)((steps + parts - 1) / parts)) +
                         kJoin + 2.0 * (double)bytes / kJoinBytes;
             }
             if (least != 0.0 && time >= least)
