@@ -49,39 +49,48 @@ struct FewArgs {
     int wide;
 };
 
-// The products of 16 columns and up to 16 NB rows a workgroup, whose waves share
-// the contraction in turns (bound by reading W: one bfloat16 row, 4,096 -> 65,000,
-// 109 us with the join, 4.9 TB/s; 2,048 -> 32,000 30 us and 5 for the join;
-// workgroups that stay and read a block ahead spilled at 16 waves, 45 for 38); wave b < NB ends with rows 16 b .. 16 b + 15 (true), a
-// lane with four columns (4 (lane / 16) on) of `row`.
-template <int DT, int NB, int WAVES>
-__device__ __forceinline__ bool few_logits(const FewArgs &a, double (&v)[4], int64_t &row)
+// The products of CB blocks of 16 columns and up to 16 NB rows a workgroup, whose
+// waves share the contraction in turns; wave w < NB CB ends (true) with rows
+// 16 (w mod NB) on and block w / NB, a lane with four columns, from `col` on, of
+// `row`.  Bound by reading W: one bfloat16 row, 4,096 -> 65,000, 109 us with the
+// join, 4.9 TB/s.  (Workgroups that stay and read a block ahead spilled at 16 waves,
+// 45 us for 38.)
+template <int DT, int NB, int CB, int WAVES>
+__device__ __forceinline__ bool few_logits(const FewArgs &a, double (&v)[4], int64_t &row,
+                                           int64_t &col)
 {
     constexpr int kValues = DT == GPIC_F32 ? 4 : 8;       // of k a lane loads at once
     constexpr int kSize = DT == GPIC_F32 ? 4 : 2;
     constexpr int kUnroll = 4, kTurn = 4 * kValues * kUnroll;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, r = lane & 15;
-    const int64_t col0 = (int64_t)blockIdx.x * 16, row0 = (int64_t)blockIdx.y * (16 * NB);
-    // rows beyond the last are read as the last one and not kept
-    const int64_t wrow = col0 + r < a.v ? col0 + r : a.v - 1;
-    const char *w = static_cast<const char *>(a.W) + wrow * a.ldw * kSize;
-    const char *x[NB];
+    const int64_t col0 = (int64_t)blockIdx.x * (16 * CB), row0 = (int64_t)blockIdx.y * (16 * NB);
+    // rows and columns beyond the last are read as the last ones and not kept
+    const char *w[CB], *x[NB];
+#pragma unroll
+    for (int c = 0; c < CB; ++c) {
+        const int64_t at = col0 + c * 16 + r < a.v ? col0 + c * 16 + r : a.v - 1;
+        w[c] = static_cast<const char *>(a.W) + at * a.ldw * kSize;
+    }
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
-        const int64_t row = row0 + b * 16 + r < a.n ? row0 + b * 16 + r : a.n - 1;
-        x[b] = static_cast<const char *>(a.X) + row * a.ldx * kSize;
+        const int64_t at = row0 + b * 16 + r < a.n ? row0 + b * 16 + r : a.n - 1;
+        x[b] = static_cast<const char *>(a.X) + at * a.ldx * kSize;
     }
-    f32x4 acc[NB];
+    f32x4 acc[CB][NB];
 #pragma unroll
-    for (int b = 0; b < NB; ++b)
-        acc[b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int c = 0; c < CB; ++c)
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+            acc[c][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     auto turn = [&](int64_t k0, auto last) {
         constexpr bool kLast = decltype(last)::value;
-        u32x4 fw[kUnroll], fx[NB][kUnroll];
+        u32x4 fw[CB][kUnroll], fx[NB][kUnroll];
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
             const int64_t k = k0 + u * 4 * kValues + g * kValues;
-            fw[u] = chunk_at<DT, kLast>(w, k, a.k);
+#pragma unroll
+            for (int c = 0; c < CB; ++c)
+                fw[c][u] = chunk_at<DT, kLast>(w[c], k, a.k);
 #pragma unroll
             for (int b = 0; b < NB; ++b)
                 fx[b][u] = chunk_at<DT, kLast>(x[b], k, a.k);
@@ -89,8 +98,10 @@ __device__ __forceinline__ bool few_logits(const FewArgs &a, double (&v)[4], int
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u)
 #pragma unroll
-            for (int b = 0; b < NB; ++b)
-                acc[b] = mma16<DT>(fw[u], fx[b][u], acc[b]);
+            for (int c = 0; c < CB; ++c)
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+                    acc[c][b] = mma16<DT>(fw[c][u], fx[b][u], acc[c][b]);
     };
     int64_t k0 = (int64_t)wave * kTurn;
 #pragma unroll 2
@@ -98,14 +109,17 @@ __device__ __forceinline__ bool few_logits(const FewArgs &a, double (&v)[4], int
         turn(k0, std::false_type{});
     if (k0 < a.k)                      // the turn that the contraction ends in
         turn(k0, std::true_type{});
-    __shared__ f32x4 part[WAVES][NB][64];
+    __shared__ f32x4 part[WAVES][CB * NB][64];
 #pragma unroll
-    for (int b = 0; b < NB; ++b)
-        part[wave][b][lane] = acc[b];
+    for (int c = 0; c < CB; ++c)
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+            part[wave][c * NB + b][lane] = acc[c][b];
     __syncthreads();
-    if (wave >= NB)
+    if (wave >= NB * CB)
         return false;
-    row = row0 + wave * 16 + r;
+    row = row0 + wave % NB * 16 + r;
+    col = col0 + wave / NB * 16 + g * 4;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
         v[j] = 0.0;
@@ -120,21 +134,19 @@ __device__ __forceinline__ bool few_logits(const FewArgs &a, double (&v)[4], int
 // Each row's largest and sum of exponentials over 16 columns.  The waves' sums of
 // a logit meet in float64, and so do the target's and the others' later: a loss
 // is the small difference of both, a float32 of 18 is 10^-6 off.
-template <int DT, int NB, int WAVES>
+template <int DT, int NB, int CB, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void few_lse_kernel(FewArgs a)
 {
     double v[4];
-    int64_t row;
-    if (!few_logits<DT, NB, WAVES>(a, v, row))
+    int64_t row, col0;
+    if (!few_logits<DT, NB, CB, WAVES>(a, v, row, col0))
         return;
-    const int g = (threadIdx.x & 63) >> 4;
-    const int64_t col0 = (int64_t)blockIdx.x * 16;
     const bool live = row < a.n;
     const int64_t t = live ? target_at(a.targets, a.wide, row) : -1;
     float m = -INFINITY, s = 0.0f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const int64_t col = col0 + g * 4 + j;
+        const int64_t col = col0 + j;
         double z = -INFINITY;
         if (col < a.v) {
             const float bias = a.bias ? load1(a.bias, col, DT) : 0.0f;
@@ -155,8 +167,8 @@ __global__ __launch_bounds__(64 * WAVES) void few_lse_kernel(FewArgs a)
         s += __builtin_amdgcn_exp2f((float)(v[j] - at) * kLog2e);
     s += __shfl_xor(s, 16, 64);
     s += __shfl_xor(s, 32, 64);
-    if (live && g == 0)
-        a.strip[(int64_t)blockIdx.x * a.n + row] = make_float2(m, s);
+    if (live && (threadIdx.x & 63) < 16)
+        a.strip[(col0 >> 4) * a.n + row] = make_float2(m, s);
 }
 
 // The same logits to D = g (exp(z - lse) - [target]) in float32, for the gradients
@@ -173,8 +185,7 @@ __global__ __launch_bounds__(64 * WAVES) void small_soft_kernel(SmallArgs s)
 {
     const FewArgs &a = s.f;
     double v[4];
-    int64_t row;
-    const int g = (threadIdx.x & 63) >> 4;
+    int64_t row, col0;
     {
         const int64_t total = a.n * a.k, each = (total + gridDim.x * gridDim.y - 1) /
                                                 (gridDim.x * gridDim.y);
@@ -186,7 +197,7 @@ __global__ __launch_bounds__(64 * WAVES) void small_soft_kernel(SmallArgs s)
             s.X[i] = live ? static_cast<const float *>(a.X)[r * a.ldx + (i - r * a.k)] : 0.0f;
         }
     }
-    if (!few_logits<GPIC_F32, NB, WAVES>(a, v, row) || row >= a.n)
+    if (!few_logits<GPIC_F32, NB, 1, WAVES>(a, v, row, col0) || row >= a.n)
         return;
     const int64_t t = target_at(a.targets, a.wide, row);
     const float gl = s.dloss[row];
@@ -194,7 +205,7 @@ __global__ __launch_bounds__(64 * WAVES) void small_soft_kernel(SmallArgs s)
     const float lse = s.lse[row], loss = s.loss[row];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const int64_t col = (int64_t)blockIdx.x * 16 + g * 4 + j;
+        const int64_t col = col0 + j;
         if (col >= a.v)
             break;
         const float bias = a.bias ? load1(a.bias, col, GPIC_F32) : 0.0f;
@@ -434,6 +445,7 @@ __global__ __launch_bounds__(256) void zero_kernel(void *p, int64_t values, int 
     } while (0)
 
 constexpr int kFew = 32;
+constexpr int64_t kWideFew = 16384;     // columns that fill the card two blocks at a time
 
 // Few rows, or little work, where launches count.
 bool few(const Loss &p)
@@ -569,26 +581,44 @@ struct Backward {
     }
 };
 
-template <int DT, int NB>
-void launch_waves(const FewArgs &a, hipStream_t st)
+// Turns of a contraction that waves share.
+int64_t turns_of(const Loss &p)
 {
-    const dim3 blocks((unsigned)((a.v + 15) / 16), (unsigned)((a.n + 16 * NB - 1) / (16 * NB)));
-    const int64_t turns = (a.k + (DT == GPIC_F32 ? 63 : 127)) / (DT == GPIC_F32 ? 64 : 128);
+    const int64_t turn = p.dtype == GPIC_F32 ? 64 : 128;
+    return (p.k + turn - 1) / turn;
+}
+
+template <int DT, int NB, int CB>
+void launch_waves(const FewArgs &a, int64_t turns, hipStream_t st)
+{
+    const dim3 blocks((unsigned)((a.v + 16 * CB - 1) / (16 * CB)),
+                      (unsigned)((a.n + 16 * NB - 1) / (16 * NB)));
     if (turns <= 4)
-        few_lse_kernel<DT, NB, 4><<<blocks, 256, 0, st>>>(a);
+        few_lse_kernel<DT, NB, CB, 4><<<blocks, 256, 0, st>>>(a);
     else if (turns <= 8)
-        few_lse_kernel<DT, NB, 8><<<blocks, 512, 0, st>>>(a);
+        few_lse_kernel<DT, NB, CB, 8><<<blocks, 512, 0, st>>>(a);
     else
-        few_lse_kernel<DT, NB, 16><<<blocks, 1024, 0, st>>>(a);
+        few_lse_kernel<DT, NB, CB, 16><<<blocks, 1024, 0, st>>>(a);
 }
 
 template <int DT>
-hipError_t launch_few(const FewArgs &a, hipStream_t st)
+hipError_t launch_few(const FewArgs &a, const Loss &p, hipStream_t st)
 {
-    if (a.n <= 16)
-        launch_waves<DT, 1>(a, st);
+    // Two blocks of columns a workgroup read X half as often, and where the sixteen
+    // waves have one turn each they halve the ends of workgroups; else they leave
+    // fewer waves in flight.  us, one and two blocks: 1 x 2,048 -> 32,000 in bfloat16
+    // 38.8 and 35.1, 1 x 1,000 17.6 and 20.8, 4 x 4,096 62 and 72, 16 x 4,096 82 and 76,
+    // 16 x 2,048 50 and 41, 32 x 2,048 63 and 50, 32 x 1,500 -> 20,000 in float32 65 and 56.
+    const int64_t turns = turns_of(p);
+    const bool wide = a.v >= kWideFew && (a.n > 8 || (turns > 8 && turns <= 16));
+    if (a.n <= 16 && wide)
+        launch_waves<DT, 1, 2>(a, turns, st);
+    else if (a.n <= 16)
+        launch_waves<DT, 1, 1>(a, turns, st);
+    else if (wide)
+        launch_waves<DT, 2, 2>(a, turns, st);
     else
-        launch_waves<DT, 2>(a, st);
+        launch_waves<DT, 2, 1>(a, turns, st);
     return hipGetLastError();
 }
 
@@ -649,9 +679,9 @@ hipError_t run_loss(const Loss &p, const void *X, const void *W, const void *bia
     Forward f(p, X, W, c);
     if (few(p)) {
         const FewArgs a{X, W, bias, targets, f.strip, f.picked, p.ldx, p.ldw, p.n, p.k, p.v, p.wide};
-        RUN(p.dtype == GPIC_F32    ? launch_few<GPIC_F32>(a, st)
-            : p.dtype == GPIC_F16 ? launch_few<GPIC_F16>(a, st)
-                                  : launch_few<GPIC_BF16>(a, st));
+        RUN(p.dtype == GPIC_F32    ? launch_few<GPIC_F32>(a, p, st)
+            : p.dtype == GPIC_F16 ? launch_few<GPIC_F16>(a, p, st)
+                                  : launch_few<GPIC_BF16>(a, p, st));
     } else {
         const Source *list[2] = {&f.X, &f.W};
         if (p.dtype == GPIC_F32)
