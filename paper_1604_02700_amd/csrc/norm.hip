@@ -93,7 +93,10 @@ struct Chunk {
 // Rows that LANES lanes hold in HOLD groups of eight columns each, with the next
 // row on its way while one is finished: the mean, then the deviations from it,
 // whose own sum corrects it, so that rows far from zero lose nothing.  Groups of
-// lanes take rows in turn over the whole grid.
+// lanes take rows in turn over the whole grid.  Bound by memory: 16,384 x 2,048 in
+// bfloat16 24.5 us (5.5 TB/s), 31 with a row a wave and no next one on its way;
+// 10,007 x 1,000 in float32 17.1 (4.7); 1,024 workgroups, since 2,048 and more take
+// up to 30 % longer (16,384 x 2,048 in float32 45 us, 47, and 59 with 4,096).
 template <int DT, int LANES, int HOLD>
 __global__ __launch_bounds__(256) void norm_rows_kernel(NormArgs a)
 {
@@ -328,7 +331,10 @@ __global__ __launch_bounds__(256) void norm_strip_kernel(NormGradArgs a)
 // The same in one pass over X and dY, for rows that LANES lanes hold in HOLD
 // groups of eight columns each: the next row is on its way while one is
 // finished, and the columns' sums stay in registers until the rows are through,
-// then meet in LDS.  Groups of lanes take rows in turn over the whole grid.
+// then meet in LDS.  Groups of lanes take rows in turn over the whole grid.  Bound
+// by memory: 16,384 x 2,048 in bfloat16 40 us with the join (5.0 TB/s), 10,007 x
+// 1,000 in float32 27 (4.5); in two passes, rows' means and then strips of
+// columns, 63 and 40.
 template <int DT, int LANES, int HOLD, int THREADS>
 __global__ __launch_bounds__(THREADS) void norm_grad_kernel(NormGradArgs a)
 {

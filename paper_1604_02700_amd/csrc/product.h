@@ -665,8 +665,8 @@ __device__ __forceinline__ void finish_lse(const ProductArgs &a, const Work &w,
 // and its column sums times g, unrounded.  The loss's gradient g is left out of
 // what is rounded: it is the same for every row as a rule (1 / n), and its own
 // rounding to 16 bits would be every entry's, up to 2^-8 of the gradients.
-// 8,192 x 2,048 -> 12,544 in bfloat16 (1,568 tiles): 422 us with logits staged in
-// float32.
+// 8,192 x 2,048 -> 25,088 in bfloat16 775 to 791 us (1.07 PFLOP/s, matrix pipe busy
+// 52 %); with logits staged in float32 and finished from there 844.
 template <class T, int OP>
 __device__ __forceinline__ void finish_soft(const ProductArgs &a, const Work &w,
                                             f32x4 (&acc)[T::kRM][T::kRN], char *lds)
@@ -702,7 +702,7 @@ __device__ __forceinline__ void finish_soft(const ProductArgs &a, const Work &w,
 #pragma unroll
         for (int i = 0; i < kFrags; ++i) {
             const int64_t row = row0 + 16 * (i0 + i) + (lane & 15);
-            LossRow info{0.0f, 0.0f, 0.0f, -1};
+            LossRow info{0.0f, 0.0f, 0.0f, 0.0f, -1, {0, 0, 0}};
             if (row < a.M)
                 info = e.rows[row];
             const int pr = kSplit && row < a.M ? e.pa[row] : 0;
@@ -714,7 +714,7 @@ __device__ __forceinline__ void finish_soft(const ProductArgs &a, const Work &w,
                     float z = acc[i0 + i][j][c];
                     if (kSplit)
                         z = ldexpf(z, -(pr + pc[j][c]));
-                    z = __builtin_amdgcn_exp2f((z + bias[j][c] - info.lse) * kLog2e);
+                    z = __builtin_amdgcn_exp2f((z + bias[j][c] - info.at - info.off) * kLog2e);
                     d[j][c] = info.target < 0 || bias[j][c] == -INFINITY ? 0.0f : z;
                 }
             const int at = info.target < 0 ? -1 : info.target - (int)(e.first + col0) - 4 * g;

@@ -211,6 +211,43 @@ def test_entries_taken_out(g, n, dtype):
 
 
 @pytest.mark.parametrize("dtype", list(T))
+@pytest.mark.parametrize("n", [5, 300, 2100])
+def test_masks_of_the_lowest_value(g, n, dtype):
+    """Entries at the type's lowest value weigh nothing beside others, and as
+    much as each other where nothing else is left."""
+    X, W, b, t = _inputs(n, 48, 130 if n == 5 else 5000, dtype)
+    v = W.shape[0]
+    out = torch.rand(v, generator=torch.Generator().manual_seed(2)).to(DEV) < 0.5
+    live = (~out).nonzero()[:, 0]
+    t = torch.where((t >= 0) & (t < v), live[t.clamp(0, v - 1) % len(live)], t)
+    low = torch.finfo(T[dtype]).min
+    one = torch.ones(n, device=DEV)
+    got = []
+    for mask in (low, -math.inf):
+        loss, lse = g.gpic_cross_entropy(X, W, t, b.masked_fill(out, mask), want_lse=True)
+        gr = g.gpic_cross_entropy_backward(one, X, W, t, loss, lse, b.masked_fill(out, mask))
+        got.append((loss, lse, gr.dX, gr.dW, gr.db))
+    for a, c in zip(*got):
+        assert torch.equal(a, c)
+    # all of them: the products vanish beside 3.4e38 (not beside float16's lowest,
+    # whose share cancels), and every entry weighs the same
+    mask = torch.full_like(b, low)
+    loss, lse = g.gpic_cross_entropy(X, W, t, mask, want_lse=True)
+    gr = g.gpic_cross_entropy_backward(one, X, W, t, loss, lse, mask)
+    real = (t >= 0) & (t < v)
+    z = X.double() @ W.double().t() if dtype == "f16" else torch.zeros((n, v), device=DEV).double()
+    ref = z.logsumexp(1) - z.gather(1, t.clamp(0, v - 1)[:, None])[:, 0]
+    # float16: logits beside 65504 are off by 2^-8 in float32
+    tol = 2.0 ** -6 if dtype == "f16" else 4 * (v / 256 + 40) * E + 1e-6
+    assert float((loss.double() - ref)[real].abs().max()) <= tol and not loss[~real].any()
+    d = (z - z.logsumexp(1, keepdim=True)).exp()
+    d[torch.arange(n, device=DEV), t.clamp(0, v - 1)] -= 1.0
+    d = torch.where(real[:, None], d, 0.0)
+    size = d.abs() @ W.double().abs()
+    _close(gr.dX, d @ W.double(), (2 * tol + U[dtype] + (v + 48) * E) * size, dtype, "dX")
+
+
+@pytest.mark.parametrize("dtype", list(T))
 @pytest.mark.parametrize("n", [6, 300])
 def test_non_finite_rows_and_certain_targets(g, n, dtype):
     X, W, b, t = _inputs(n, 48, 900 if n == 6 else 5000, dtype)

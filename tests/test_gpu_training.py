@@ -167,6 +167,12 @@ def _table_check(g, n, k, rows, ids, dtype, scale, what):
     Y = g.gpic_embedding(ids, Tb, scale)
     y = torch.where(real[:, None], Tb.double()[at] * scale, 0.0)
     _close(Y, y, 2 * E * y.abs(), dtype, what + " Y")
+    wide = _randn((n, k + 4), dtype, 4)
+    kept = wide.clone()
+    table = torch.cat([Tb, Tb], 1)[:, :k] if k < 2000 else Tb          # a pitch of 2 k
+    g.gpic_embedding(ids, table, scale, Y=wide[:, 3:3 + k])
+    assert torch.equal(wide[:, 3:3 + k], Y) and torch.equal(wide[:, :3], kept[:, :3])
+    assert torch.equal(wide[:, 3 + k:], kept[:, 3 + k:])
     dT = g.gpic_embedding_backward(dY, ids, rows, scale)
     d = torch.where(real[:, None], dY.double(), 0.0)
     zero = torch.zeros((rows, k), device=DEV, dtype=torch.float64)
@@ -184,6 +190,10 @@ def _table_check(g, n, k, rows, ids, dtype, scale, what):
     _close(view, total, bound + 2 * E * (total.abs() + (ref * scale).abs()), dtype, what + " sum")
     empty = (count == 0).squeeze(1)
     assert torch.equal(acc[empty], old[empty])
+    into = old.clone()                       # every row written, nothing beside them
+    g.gpic_embedding_backward(dY, ids, rows, scale, dT=into[:, 1:1 + k])
+    assert torch.equal(into[:, 1:1 + k], dT)
+    assert torch.equal(into[:, :1], old[:, :1]) and torch.equal(into[:, 1 + k:], old[:, 1 + k:])
     assert torch.equal(acc[:, :2], old[:, :2]) and torch.equal(acc[:, 2 + k:], old[:, 2 + k:])
 
 
