@@ -733,6 +733,9 @@ def _matrix_of(t, rows, cols, like, name):
 
 
 def _layer_type(X, name="X", shape="[n, k]"):
+    if (isinstance(X, torch.Tensor) and X.is_cuda and X.dtype in DTYPES and X.dim() == 2
+            and X.is_contiguous()):
+        return X
     if not isinstance(X, torch.Tensor) or not X.is_cuda:
         raise TypeError(f"{name} must be a CUDA (HIP) tensor")
     if X.dtype not in DTYPES:
@@ -976,23 +979,30 @@ def gpic_muon_step(W: torch.Tensor, G: torch.Tensor, M: torch.Tensor, lr: float,
 
 
 # ------------------- 8. what surrounds an encoder's layers in training
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
 def _run(fn, device, *args):
     """fn(*args, the current stream of `device`), with that device current."""
-    if device.index == torch.cuda.current_device():
-        _check(fn(*args, _stream(device)))
+    index = device.index
+    if index == _current_device():
+        st = fn(*args, _raw_stream(index) if _raw_stream is not None else _stream(device))
     else:
         with torch.cuda.device(device):
-            _check(fn(*args, _stream(device)))
+            st = fn(*args, _stream(device))
+    if st != GPIC_OK:
+        _check(st)
 
 
 def _columns(t, k, like, name):
     """A contiguous vector of k values of like's type and device, or None."""
     if t is None:
         return None
-    _dev(t, like.dtype, name)
-    if t.shape != (k,) or t.device != like.device:
+    if not (isinstance(t, torch.Tensor) and t.dtype == like.dtype and t.device == like.device
+            and t.shape == (k,)):
+        _dev(t, like.dtype, name)
         raise ValueError(f"{name} must be [{k}] on {like.device}")
-    return t.contiguous()
+    return t if t.is_contiguous() else t.contiguous()
 
 
 def _stats(t, n, like):
@@ -1005,13 +1015,13 @@ def _stats(t, n, like):
 def _ids(t, n, device, name):
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA (HIP) tensor")
-    if t.dtype not in (torch.int32, torch.int64):
+    if t.dtype != torch.int64 and t.dtype != torch.int32:
         raise TypeError(f"{name} must be int32 or int64, got {t.dtype}")
     if t.dim() != 1 or (n is not None and t.shape[0] != n):
         raise ValueError(f"{name} must be [{'n' if n is None else n}], got {tuple(t.shape)}")
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, not on {device}")
-    return t.contiguous()
+    return t if t.is_contiguous() else t.contiguous()
 
 
 def gpic_layer_norm(X: torch.Tensor, weight: Optional[torch.Tensor] = None,
@@ -1028,10 +1038,12 @@ def gpic_layer_norm(X: torch.Tensor, weight: Optional[torch.Tensor] = None,
     weight, bias = _columns(weight, k, X, "weight"), _columns(bias, k, X, "bias")
     given, Y = Y, _output(Y, n, k, X, "Y")
     stats = torch.empty((n, 2), dtype=torch.float32, device=X.device) if want_stats else None
-    _no_graph("X weight bias Y", X, weight, bias, Y)
+    if (X.requires_grad or Y.requires_grad or (weight is not None and weight.requires_grad)
+            or (bias is not None and bias.requires_grad)):
+        _no_graph("X weight bias Y", X, weight, bias, Y)
     p = NormParams(n, k, _pitch(X, n, k), _pitch(Y, n, k), float(eps), DTYPES[X.dtype])
-    _run(lib().gpic_layer_norm, X.device, C.byref(p), _at(X), _at(weight), _at(bias), _at(Y),
-         _at(stats))
+    _run(lib().gpic_layer_norm, X.device, C.byref(p), X.data_ptr(), _at(weight), _at(bias),
+         Y.data_ptr(), _at(stats))
     if given is not None:
         _written(given)
     return (Y, stats) if want_stats else Y
@@ -1049,7 +1061,9 @@ def gpic_layer_norm_backward(dY: torch.Tensor, X: torch.Tensor, weight: Optional
     dX = torch.empty((n, k), dtype=X.dtype, device=dev) if want_x else None
     dW = torch.empty(k, dtype=X.dtype, device=dev) if want_w else None
     db = torch.empty(k, dtype=X.dtype, device=dev) if want_bias else None
-    _no_graph("dY X weight stats", dY, X, weight, stats)
+    if (dY.requires_grad or X.requires_grad or stats.requires_grad
+            or (weight is not None and weight.requires_grad)):
+        _no_graph("dY X weight stats", dY, X, weight, stats)
     p = NormParams(n, k, _pitch(X, n, k), _pitch(dY, n, k), 0.0, DTYPES[X.dtype])
     ref = C.byref(p)
     ws, nb = _workspace(lib().gpic_layer_norm_workspace_bytes(ref), dev)
@@ -1075,14 +1089,17 @@ def gpic_dropout(X: torch.Tensor, p: float, seed: int, offset: int = 0,
         _dev(step, torch.int64, "step")
         if step.numel() != 1 or step.device != X.device:
             raise ValueError(f"step must be one value on {X.device}")
-    for name, v in (("seed", seed), ("offset", offset)):
-        if not 0 <= int(v) < 1 << 64:
-            raise ValueError(f"{name} must be in 0 .. 2^64 - 1")
+    seed, offset = int(seed), int(offset)
+    if not (0 <= seed < 1 << 64 and 0 <= offset < 1 << 64):
+        raise ValueError("seed and offset must be in 0 .. 2^64 - 1")
     given, Y = Y, _output(Y, n, m, X, "Y")
-    _no_graph("X residual Y", X, residual, Y)
-    d = DropoutParams(n, m, _pitch(X, n, m), _pitch(residual, n, m), _pitch(Y, n, m), int(seed),
-                      int(offset), float(p), DTYPES[X.dtype], 0)
-    _run(lib().gpic_dropout, X.device, C.byref(d), _at(X), _at(residual), _at(step), _at(Y))
+    if (X.requires_grad or Y.requires_grad
+            or (residual is not None and residual.requires_grad)):
+        _no_graph("X residual Y", X, residual, Y)
+    d = DropoutParams(n, m, _pitch(X, n, m), _pitch(residual, n, m), _pitch(Y, n, m), seed, offset,
+                      float(p), DTYPES[X.dtype], 0)
+    _run(lib().gpic_dropout, X.device, C.byref(d), X.data_ptr(), _at(residual), _at(step),
+         Y.data_ptr())
     if given is not None:
         _written(given)
     return Y
@@ -1098,10 +1115,11 @@ def gpic_embedding(ids: torch.Tensor, T: torch.Tensor, scale: float = 1.0,
     ids = _ids(ids, None, T.device, "ids")
     n = ids.shape[0]
     given, Y = Y, _output(Y, n, k, T, "Y")
-    _no_graph("T Y", T, Y)
+    if T.requires_grad or Y.requires_grad:
+        _no_graph("T Y", T, Y)
     p = EmbeddingParams(n, k, rows, _pitch(T, rows, k), _pitch(Y, n, k), float(scale),
                         DTYPES[T.dtype], ids.element_size(), 0)
-    _run(lib().gpic_embedding, T.device, C.byref(p), _at(ids), _at(T), _at(Y))
+    _run(lib().gpic_embedding, T.device, C.byref(p), ids.data_ptr(), T.data_ptr(), Y.data_ptr())
     if given is not None:
         _written(given)
     return Y
@@ -1121,12 +1139,14 @@ def gpic_embedding_backward(dY: torch.Tensor, ids: torch.Tensor, rows: int, scal
     if accumulate and dT is None:
         raise ValueError("accumulate adds to a given dT")
     given, dT = dT, _output(dT, rows, k, dY, "dT")
-    _no_graph("dY dT", dY, dT)
+    if dY.requires_grad or dT.requires_grad:
+        _no_graph("dY dT", dY, dT)
     p = EmbeddingParams(n, k, rows, _pitch(dT, rows, k), _pitch(dY, n, k), float(scale),
                         DTYPES[dY.dtype], ids.element_size(), int(bool(accumulate)))
     ref = C.byref(p)
     ws, nb = _workspace(lib().gpic_embedding_workspace_bytes(ref), dY.device)
-    _run(lib().gpic_embedding_backward, dY.device, ref, _at(dY), _at(ids), _at(dT), _at(ws), nb)
+    _run(lib().gpic_embedding_backward, dY.device, ref, dY.data_ptr(), ids.data_ptr(),
+         dT.data_ptr(), _at(ws), nb)
     if given is not None:
         _written(given)
     return dT
@@ -1137,7 +1157,7 @@ def _row_floats(t, n, device, name):
     _dev(t, torch.float32, name)
     if t.shape != (n,) or t.device != device:
         raise ValueError(f"{name} must be [{n}] on {device}")
-    return t.contiguous()
+    return t if t.is_contiguous() else t.contiguous()
 
 
 def _loss(backward, X, W, targets):
@@ -1166,10 +1186,11 @@ def gpic_cross_entropy(X: torch.Tensor, W: torch.Tensor, targets: torch.Tensor,
     bias = _columns(bias, W.shape[0], X, "bias")
     loss = torch.empty(n, dtype=torch.float32, device=X.device)
     lse = torch.empty(n, dtype=torch.float32, device=X.device) if want_lse else None
-    _no_graph("X W bias", X, W, bias)
+    if X.requires_grad or W.requires_grad or (bias is not None and bias.requires_grad):
+        _no_graph("X W bias", X, W, bias)
     ref, ws, nb = _loss(0, X, W, targets)
-    _run(lib().gpic_cross_entropy, X.device, ref, _at(X), _at(W), _at(bias), _at(targets),
-         _at(loss), _at(lse), _at(ws), nb)
+    _run(lib().gpic_cross_entropy, X.device, ref, X.data_ptr(), W.data_ptr(), _at(bias),
+         targets.data_ptr(), loss.data_ptr(), _at(lse), _at(ws), nb)
     return (loss, lse) if want_lse else loss
 
 
@@ -1186,12 +1207,14 @@ def gpic_cross_entropy_backward(dloss: torch.Tensor, X: torch.Tensor, W: torch.T
     (n, k), v, dev = X.shape, W.shape[0], X.device
     targets = _ids(targets, n, dev, "targets")
     bias = _columns(bias, v, X, "bias")
-    dloss, loss, lse = (_row_floats(t, n, dev, name) for t, name in
-                        ((dloss, "dloss"), (loss, "loss"), (lse, "lse")))
+    dloss, loss = _row_floats(dloss, n, dev, "dloss"), _row_floats(loss, n, dev, "loss")
+    lse = _row_floats(lse, n, dev, "lse")
     dX = torch.empty((n, k), dtype=X.dtype, device=dev) if want_x else None
     dW = torch.empty((v, k), dtype=X.dtype, device=dev) if want_w else None
     db = torch.empty(v, dtype=X.dtype, device=dev) if want_bias else None
-    _no_graph("dloss X W loss lse bias", dloss, X, W, loss, lse, bias)
+    if (dloss.requires_grad or X.requires_grad or W.requires_grad or loss.requires_grad
+            or lse.requires_grad or (bias is not None and bias.requires_grad)):
+        _no_graph("dloss X W loss lse bias", dloss, X, W, loss, lse, bias)
     ref, ws, nb = _loss(1, X, W, targets)
     _run(lib().gpic_cross_entropy_backward, dev, ref, _at(dloss), _at(X), _at(W), _at(bias),
          _at(targets), _at(loss), _at(lse), _at(dX), _at(dW), _at(db), _at(ws), nb)
