@@ -463,16 +463,19 @@ __global__ __launch_bounds__(256) void zero_kernel(void *p, int64_t values, int 
 constexpr int kFew = 32;
 constexpr int64_t kWideFew = 16384;     // columns that fill the card two blocks at a time
 
-// Few rows, or little work, where launches count.
+// Few rows (float32's split copies of W cost more for up to 64), or little work,
+// where launches count; not many short rows (2,000 x 1 -> 50,000 380 us, 60 tiled).
 bool few(const Loss &p)
 {
-    if (p.n <= kFew)
-        return true;
     const bool f32 = p.dtype == GPIC_F32;
-    return p.n <= 2048 && p.n * p.v <= ((int64_t)1 << (f32 ? 28 : 27)) / p.k;
+    if (p.n <= (f32 ? kThinRows : kFew))
+        return true;
+    return p.n <= 2048 && p.n * p.v <= (1 << 23) &&
+           p.n * p.v <= ((int64_t)1 << (f32 ? 28 : 27)) / p.k;
 }
 
-// The gradients of little work: float32, in two launches.
+// The gradients of little work or few rows: float32, from D in float32
+// (small_gradients.hip, loss_thin.hip).
 Shape layer_of(const Loss &p)
 {
     Shape s{};
@@ -487,9 +490,11 @@ Shape layer_of(const Loss &p)
     return s;
 }
 
+bool little(const Loss &p) { return small_gradients(layer_of(p), false); }
+
 bool small(const Loss &p)
 {
-    return p.n > 0 && p.dtype == GPIC_F32 && small_gradients(layer_of(p), false);
+    return p.n > 0 && p.dtype == GPIC_F32 && (p.n <= kThinRows || little(p));
 }
 
 int64_t edge_of(const Plan &p) { return p.tile == 0 ? 256 : (p.tile == 1 ? 128 : 64); }
@@ -518,11 +523,12 @@ struct Forward {
 };
 
 struct Small {
-    float *D, *X;
+    float *D, *X, *part;
     Small(const Loss &p, Cursor &c)
     {
         D = static_cast<float *>(c.take((size_t)p.n * p.v * 4));
         X = static_cast<float *>(c.take((size_t)p.n * p.k * 4));
+        part = static_cast<float *>(c.take(little(p) ? 0 : thin_ws(p.n, p.k, p.v)));
     }
 };
 
@@ -769,7 +775,11 @@ hipError_t run_loss_backward(const Loss &p, const float *dloss, const void *X, c
         a.D = m.D;
         a.X = m.X;
         RUN(p.n <= 16 ? launch_small<1>(a, st) : launch_small<2>(a, st));
-        return run_small_gradients(layer_of(p), false, m.D, m.X, W, nullptr, dX, dW, db, st);
+        if (little(p))
+            return run_small_gradients(layer_of(p), false, m.D, m.X, W, nullptr, dX, dW, db, st);
+        return run_thin_gradients(m.D, m.X, static_cast<const float *>(W), p.n, p.k, p.v, p.ldw,
+                                  static_cast<float *>(dX), static_cast<float *>(dW),
+                                  static_cast<float *>(db), m.part, st);
     }
     Backward b(p, X, W, c);
     const bool f32 = p.dtype == GPIC_F32;

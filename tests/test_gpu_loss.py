@@ -138,6 +138,9 @@ def _check(g, X, W, b, t, dloss, dtype, what):
 SHAPES = [(1, 8, 1), (1, 2048, 500), (3, 5, 7), (17, 64, 300), (33, 40, 1000), (64, 64, 64),
           (130, 72, 257), (52, 512, 1013), (300, 136, 5000), (1003, 700, 10007), (2100, 96, 3001),
           (4100, 72, 5001), (2049, 520, 4099), (700, 1, 33), (20, 3001, 100), (5000, 24, 2),
+          # few float32 rows over a large vocabulary, odd widths and partial blocks
+          (1, 130, 5000), (16, 63, 3001), (17, 65, 2049), (33, 700, 4007), (64, 1, 2500), (48, 4099, 3000),
+          (65, 200, 3000),
           # tiles of the large size in every product
           (6000, 1100, 9000)]
 
