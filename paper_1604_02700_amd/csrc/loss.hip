@@ -774,7 +774,11 @@ hipError_t run_loss_backward(const Loss &p, const float *dloss, const void *X, c
         a.lse = lse;
         a.D = m.D;
         a.X = m.X;
-        RUN(p.n <= 16 ? launch_small<1>(a, st) : launch_small<2>(a, st));
+        // W once for all rows up to 64 (64 rows over 2,048 -> 32,000: 185 us with it
+        // read twice, 164 so; the forward kernel 133 and 160, which reads it twice)
+        RUN(p.n <= 16                      ? launch_small<1>(a, st)
+            : p.n <= 32 || p.n > kThinRows ? launch_small<2>(a, st)
+                                           : launch_small<4>(a, st));
         if (little(p))
             return run_small_gradients(layer_of(p), false, m.D, m.X, W, nullptr, dX, dW, db, st);
         return run_thin_gradients(m.D, m.X, static_cast<const float *>(W), p.n, p.k, p.v, p.ldw,

@@ -5,9 +5,14 @@
 //
 // mfma_f32_16x16x4: a lane (g = lane / 16, r = lane mod 16) holds one value of both
 // operands, k = g; of the result rows r of the second operand and columns 4 g +
-// q of the first.  The first operand's column r is taken as columns 4 r + c of
-// 64, one instruction for each c = 0 .. 3, so that a lane loads four consecutive
-// values and ends with sixteen: column 16 g + 4 q + c in acc[c][q].
+// q of the first.  A wave takes 64 columns in four instructions c = 0 .. 3.  Where
+// the first operand is W its column r is column 4 r + c of the 64, so that a lane
+// loads four consecutive values and ends with sixteen: column 16 g + 4 q + c in
+// acc[c][q].  X is read once and dW written throughout, so there it is 16 c + r.
+//
+// With 2,048 -> 32,000 (W 262 MB; D in float32 and all gradients, in us): 1 row 51
+// for D, 50 dW, 79 dX and its parts' sum 5; 33 rows 138, 96, 93, 5; 64 rows 164,
+// 118, 98, 5.  By the split copies 33 rows took 507.
 #include "training.h"
 
 namespace gpic {
@@ -52,7 +57,9 @@ __device__ __forceinline__ void put16(float *row, int64_t col, int64_t cols, con
 }
 
 // dW: a wave keeps 64 columns of X (4 STEPS rows) in registers and takes 16 rows
-// of dW after another.  Bound by writing dW.
+// of dW after another.  Column r of the first operand is column 16 c + r here, so
+// that four lanes store 64 bytes of a row (98 us with 16 bytes a lane at a pitch of
+// 64 and one row, 50 so).  Bound by writing dW, from 33 rows on also by its products.
 template <int STEPS>
 __global__ __launch_bounds__(256) void thin_weights_kernel(ThinArgs a)
 {
@@ -62,12 +69,14 @@ __global__ __launch_bounds__(256) void thin_weights_kernel(ThinArgs a)
     const int64_t b0 = id / a.strips * a.each, b1 = b0 + a.each < blocks ? b0 + a.each : blocks;
     if (b0 >= b1)
         return;
-    f32x4 x[STEPS];
+    float x[STEPS][4];
 #pragma unroll
-    for (int s = 0; s < STEPS; ++s) {
-        const int64_t i = 4 * s + g;
-        x[s] = i < a.n ? quad(a.X + i * a.k, j0 + 4 * r, a.k) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    }
+    for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const int64_t i = 4 * s + g, j = j0 + 16 * c + r;
+            x[s][c] = i < a.n && j < a.k ? a.X[i * a.k + j] : 0.0f;
+        }
     // rows beyond the last are computed as the last and not stored
     auto fetch = [&](int64_t b, float (&d)[STEPS]) {
         const int64_t v = b * 16 + r < a.v ? b * 16 + r : a.v - 1;
@@ -77,6 +86,7 @@ __global__ __launch_bounds__(256) void thin_weights_kernel(ThinArgs a)
             d[s] = i < a.n ? a.D[i * a.v + v] : 0.0f;
         }
     };
+    using any = f32x4 __attribute__((aligned(4)));
     float next[STEPS];
     fetch(b0, next);
     for (int64_t b = b0; b < b1; ++b) {
@@ -96,8 +106,21 @@ __global__ __launch_bounds__(256) void thin_weights_kernel(ThinArgs a)
             for (int c = 0; c < 4; ++c)
                 acc[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[s][c], d[s], acc[c], 0, 0, 0);
         const int64_t v = b * 16 + r;
-        if (v < a.v)
-            put16(a.dW + v * a.k, j0 + 16 * g, a.k, acc);
+        if (v >= a.v)
+            continue;
+        float *row = a.dW + v * a.k;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const int64_t j = j0 + 16 * c + 4 * g;
+            if (j + 4 <= a.k) {
+                *reinterpret_cast<any *>(row + j) = acc[c];
+            } else {
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    if (j + q < a.k)
+                        row[j + q] = acc[c][q];
+            }
+        }
     }
 }
 
@@ -230,6 +253,8 @@ hipError_t run_thin_gradients(const float *D, const float *X, const float *W, in
             thin_weights_kernel<4><<<grid, 256, 0, st>>>(a);
         else if (n <= 32)
             thin_weights_kernel<8><<<grid, 256, 0, st>>>(a);
+        else if (n <= 48)
+            thin_weights_kernel<12><<<grid, 256, 0, st>>>(a);
         else
             thin_weights_kernel<16><<<grid, 256, 0, st>>>(a);
         e = hipGetLastError();
@@ -241,6 +266,8 @@ hipError_t run_thin_gradients(const float *D, const float *X, const float *W, in
             thin_points_kernel<1><<<grid, 256, 0, st>>>(a);
         else if (n <= 32)
             thin_points_kernel<2><<<grid, 256, 0, st>>>(a);
+        else if (n <= 48)
+            thin_points_kernel<3><<<grid, 256, 0, st>>>(a);
         else
             thin_points_kernel<4><<<grid, 256, 0, st>>>(a);
         e = hipGetLastError();
