@@ -197,16 +197,20 @@ __global__ __launch_bounds__(64 * WAVES) void small_soft_kernel(SmallArgs s)
     double v[4];
     int64_t row, col0;
     {
-        const int64_t total = a.n * a.k, each = (total + gridDim.x * gridDim.y - 1) /
-                                                (gridDim.x * gridDim.y);
+        // (fewer than 2^31 values: small())
+        const uint32_t total = (uint32_t)(a.n * a.k), k = (uint32_t)a.k;
+        const uint32_t groups = gridDim.x * gridDim.y, each = (total + groups - 1) / groups;
         const int64_t i0 = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * each;
         const int64_t i1 = i0 + each < total ? i0 + each : total;
+#pragma unroll 2
         for (int64_t i = i0 + threadIdx.x; i < i1; i += 64 * WAVES) {
-            const int64_t r = i / a.k, t = target_at(a.targets, a.wide, r);
+            const int64_t r = (uint32_t)i / k, t = target_at(a.targets, a.wide, r);
             const bool live = t >= 0 && t < a.v && s.dloss[r] != 0.0f;
             s.X[i] = live ? static_cast<const float *>(a.X)[r * a.ldx + (i - r * a.k)] : 0.0f;
         }
     }
+    if ((int64_t)blockIdx.y * (16 * NB) >= a.n)      // here for the copy alone
+        return;
     if (!few_logits<GPIC_F32, NB, 1, WAVES>(a, v, row, col0) || row >= a.n)
         return;
     const int64_t t = target_at(a.targets, a.wide, row);
@@ -333,8 +337,9 @@ __global__ __launch_bounds__(256) void rows_kernel(RowsArgs a)
         a.most[blockIdx.x] = fmaxf(fmaxf(w[0], w[1]), fmaxf(w[2], w[3]));
 }
 
-// G, the largest |g|, and each row's g / G; up to kRowsAtOnce rows' LossRow too
-// (else `most` holds `count` workgroups' largest).
+// G, the largest |g|, and each row's g / G; up to kRowsAtOnce rows' LossRow too, by
+// one workgroup.  Else `most` holds `count` workgroups' largest, which each of up
+// to 128 goes through (1,000,000 rows: one workgroup 447 us, now 8).
 constexpr int64_t kRowsAtOnce = 4096;
 
 __global__ __launch_bounds__(1024) void shares_kernel(RowsArgs a, int64_t count, float *largest,
@@ -362,11 +367,11 @@ __global__ __launch_bounds__(1024) void shares_kernel(RowsArgs a, int64_t count,
     for (int i = 0; i < 16; ++i)
         best = fmaxf(best, w[i]);
     best = best > 0.0f ? best : 1.0f;
-    if (threadIdx.x == 0)
+    if (threadIdx.x == 0 && blockIdx.x == 0)
         *largest = best;
-    // (each thread reads the rows that it wrote)
+    // (one workgroup: each thread reads the rows that it wrote)
 #pragma unroll 4
-    for (int64_t i = threadIdx.x; i < a.n; i += 1024)
+    for (int64_t i = (int64_t)blockIdx.x * 1024 + threadIdx.x; i < a.n; i += gridDim.x * 1024)
         share[i] = a.rows[i].g / best;
 }
 
@@ -610,6 +615,12 @@ int64_t turns_of(const Loss &p)
     return (p.k + turn - 1) / turn;
 }
 
+// Fewer workgroups of 32 rows than half the compute units: of 16 rows then
+bool thin_grid(const FewArgs &a)
+{
+    return (a.v + 15) / 16 * ((a.n + 31) / 32) < 128;
+}
+
 template <int DT, int NB, int CB>
 void launch_waves(const FewArgs &a, int64_t turns, hipStream_t st)
 {
@@ -635,7 +646,7 @@ hipError_t launch_few(const FewArgs &a, const Loss &p, hipStream_t st)
     const bool wide = a.v >= kWideFew && (a.n > 8 || (turns > 8 && turns <= 16));
     if (a.n <= 16 && wide)
         launch_waves<DT, 1, 2>(a, turns, st);
-    else if (a.n <= 16)
+    else if (a.n <= 16 || thin_grid(a))
         launch_waves<DT, 1, 1>(a, turns, st);
     else if (wide)
         launch_waves<DT, 2, 2>(a, turns, st);
@@ -738,8 +749,12 @@ template <int NB>
 hipError_t launch_small(const SmallArgs &a, hipStream_t st)
 {
     const FewArgs &f = a.f;
-    const dim3 blocks((unsigned)((f.v + 15) / 16), (unsigned)((f.n + 16 * NB - 1) / (16 * NB)));
-    const int64_t turns = (f.k + 63) / 64;
+    const int64_t x = (f.v + 15) / 16, y = (f.n + 16 * NB - 1) / (16 * NB);
+    const int64_t turns = (f.k + 63) / 64, threads = turns <= 4 ? 256 : (turns <= 8 ? 512 : 1024);
+    // X's copy: up to eight values a thread on up to 1,024 workgroups
+    int64_t more = (f.n * f.k + 8 * threads - 1) / (8 * threads);
+    more = ((more < 1024 ? more : 1024) + x - 1) / x;
+    const dim3 blocks((unsigned)x, (unsigned)(y > more ? y : more));
     if (turns <= 4)
         small_soft_kernel<NB, 4><<<blocks, 256, 0, st>>>(a);
     else if (turns <= 8)
@@ -776,9 +791,9 @@ hipError_t run_loss_backward(const Loss &p, const float *dloss, const void *X, c
         a.X = m.X;
         // W once for all rows up to 64 (64 rows over 2,048 -> 32,000: 185 us with it
         // read twice, 164 so; the forward kernel 133 and 160, which reads it twice)
-        RUN(p.n <= 16                      ? launch_small<1>(a, st)
-            : p.n <= 32 || p.n > kThinRows ? launch_small<2>(a, st)
-                                           : launch_small<4>(a, st));
+        RUN(p.n <= 16 || thin_grid(a.f)                            ? launch_small<1>(a, st)
+            : p.n <= 32 || p.n > kThinRows || p.v < kWideFew / 4 ? launch_small<2>(a, st)
+                                                                 : launch_small<4>(a, st));
         if (little(p))
             return run_small_gradients(layer_of(p), false, m.D, m.X, W, nullptr, dX, dW, db, st);
         return run_thin_gradients(m.D, m.X, static_cast<const float *>(W), p.n, p.k, p.v, p.ldw,
@@ -791,11 +806,13 @@ hipError_t run_loss_backward(const Loss &p, const float *dloss, const void *X, c
     {
         const RowsArgs a{dloss, loss, lse, targets, p.wide, p.n, p.v, b.rows, b.most};
         const int64_t blocks = (p.n + 255) / 256;
+        unsigned groups = 1;
         if (p.n > kRowsAtOnce) {
             rows_kernel<<<(unsigned)blocks, 256, 0, st>>>(a);
             RUN(hipGetLastError());
+            groups = (unsigned)(p.n < 128 * 4096 ? (p.n + 4095) / 4096 : 128);
         }
-        shares_kernel<<<1, 1024, 0, st>>>(a, blocks, b.largest, b.share);
+        shares_kernel<<<groups, 1024, 0, st>>>(a, blocks, b.largest, b.share);
         RUN(hipGetLastError());
     }
     if (f32 && (dX || dW)) {
