@@ -443,7 +443,8 @@ __device__ __forceinline__ void cut_runs(const TableArgs &a, int64_t t)
 
 // The cuts' sums of the runs that start in sixteen chunks, a wave a chunk; of a
 // run of more than sixteen cuts (no two can start within sixteen chunks) by all
-// waves of the workgroup.  Bound by latency, where a run is and then its cuts' sums:
+// waves of the workgroup, a narrow row by as many groups of lanes as fit (300,000 x
+// 64 of two ids 150 us with one, 38 so).  Bound by latency, where a run is and then its cuts' sums:
 // 6 us (18 where ids and starts are read to find it).
 constexpr int kJoinWaves = 16;
 
@@ -463,6 +464,11 @@ __global__ __launch_bounds__(64 * kJoinWaves) void join_cuts_kernel(TableArgs a)
         run = a.run[its];
     const int cuts = (int)((int64_t)run.end - its);
     const uint64_t large = __ballot(lane < kJoinWaves && cuts > kJoinWaves);
+    // lanes that a narrow row takes, of as many groups as fit into a wave
+    int span = 64;
+    if (a.strips == 1)
+        while (span > 1 && span * 4 >= a.k)
+            span >>= 1;
     // first this wave's own run, if it is short, then its share of the long one
     for (int pass = 0; pass < 2; ++pass) {
         const int which = pass == 0 ? (int)wave : (large ? __builtin_ctzll(large) : 0);
@@ -470,25 +476,28 @@ __global__ __launch_bounds__(64 * kJoinWaves) void join_cuts_kernel(TableArgs a)
         const int64_t count = __builtin_amdgcn_readlane(cuts, which);
         const int64_t v = (uint32_t)__builtin_amdgcn_readlane((int)run.row, which);
         const int slot = __builtin_amdgcn_readlane((int)run.slot, which);
-        int64_t i0 = c, i1 = c + count;
-        if (pass == 0 && count > kJoinWaves)
-            continue;
-        if (pass == 1) {
-            if (!large)
-                break;
-            const int64_t each = (count + kJoinWaves - 1) / kJoinWaves;
-            i0 = c + wave * each;
-            i1 = i0 + each < c + count ? i0 + each : c + count;
-        }
         f32x8 sum[1];
         sum[0] = 0.0f;
-        add_batches(i0, i1, [&](int64_t i) { return i * 2 + (i == c ? slot : 0); },
-                    [&](int64_t at, int) { return w.load_sum(a.part, at * a.k); }, sum);
+        auto item = [&](int64_t i) { return i * 2 + (i == c ? slot : 0); };
         if (pass == 0) {
-            if (count > 0)
-                put(a, v, w, sum[0]);
+            if (count > kJoinWaves || count <= 0)
+                continue;
+            add_batches(c, c + count, item,
+                        [&](int64_t at, int) { return w.load_sum(a.part, at * a.k); }, sum);
+            put(a, v, w, sum[0]);
             continue;
         }
+        if (!large)
+            break;
+        // its groups of lanes take a run of cuts each
+        const int groups = kJoinWaves * (64 / span), group = (int)wave * (64 / span) + lane / span;
+        const Window<DT, TINY> own((strip * 64 + (lane & (span - 1))) * 8, a.k);
+        add_batches(c + count * group / groups, c + count * (group + 1) / groups, item,
+                    [&](int64_t at, int) { return own.load_sum(a.part, at * a.k); }, sum);
+        for (int o = span; o < 64; o <<= 1)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                sum[0][j] += __shfl_xor(sum[0][j], o, 64);
         all[wave][lane] = sum[0];
         __syncthreads();
         if (wave > 0)

@@ -199,7 +199,8 @@ def _table_check(g, n, k, rows, ids, dtype, scale, what):
 
 TABLES = [(1, 1, 1), (1, 2048, 50), (3, 7, 5), (64, 64, 3), (65, 8, 1000), (1000, 300, 77),
           (1024, 40, 30000), (1025, 40, 30000), (1100, 1, 2), (4096, 9, 255), (4097, 513, 256),
-          (5000, 1030, 700), (70000, 72, 9), (40000, 16, 70000), (70001, 520, 3001)]
+          (5000, 1030, 700), (70000, 72, 9), (40000, 16, 70000), (70001, 520, 3001),
+          (20000, 100, 2), (9000, 257, 3), (30000, 3, 4)]
 
 
 @pytest.mark.parametrize("dtype", list(T))
