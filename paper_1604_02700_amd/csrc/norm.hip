@@ -499,8 +499,8 @@ struct Cut {
         strips = (p.k + 511) / 512;
         lanes = hold = 0;
         each = 0;
-        static const int kFit[][2] = {{16, 1}, {16, 2}, {64, 1}, {64, 2},
-                                      {64, 4}, {256, 2}, {256, 4}};
+        static const int kFit[][2] = {{4, 1},  {8, 1},  {16, 1},  {16, 2}, {64, 1},
+                                      {64, 2}, {64, 4}, {256, 2}, {256, 4}};
         for (auto &f : kFit)
             if (p.k <= f[0] * f[1] * 8) {
                 lanes = f[0];
@@ -562,8 +562,12 @@ hipError_t launch_norm(const NormArgs &a, hipStream_t st)
         launch_rows<DT, 64, 1>(a, st);
     else if (a.k > 128)
         launch_rows<DT, 16, 2>(a, st);
-    else
+    else if (a.k > 64)
         launch_rows<DT, 16, 1>(a, st);
+    else if (a.k > 32)
+        launch_rows<DT, 8, 1>(a, st);
+    else                                 // 1,000,000 x 16 in bfloat16: 77 us by 16 lanes, 22 so
+        launch_rows<DT, 4, 1>(a, st);
     return hipGetLastError();
 }
 
@@ -572,6 +576,12 @@ hipError_t launch_gradients(const NormGradArgs &a, const Cut &cut, hipStream_t s
 {
     const unsigned blocks = (unsigned)cut.parts;
     switch (cut.lanes * 8 + cut.hold) {
+    case 4 * 8 + 1:                      // 1,000,000 x 16 in bfloat16: 129 us by 16 lanes, 37 so
+        norm_grad_kernel<DT, 4, 1, 512><<<blocks, 512, 0, st>>>(a);
+        return hipGetLastError();
+    case 8 * 8 + 1:
+        norm_grad_kernel<DT, 8, 1, 512><<<blocks, 512, 0, st>>>(a);
+        return hipGetLastError();
     case 16 * 8 + 1:
         norm_grad_kernel<DT, 16, 1, 512><<<blocks, 512, 0, st>>>(a);
         return hipGetLastError();

@@ -90,7 +90,8 @@ def _norm_check(g, X, w, b, dY, dtype, what, eps=1e-5):
 
 NORMS = [(1, 1), (1, 2048), (3, 7), (5, 64), (1, 8192), (17, 129), (300, 8), (1003, 300),
          (4100, 512), (5000, 40), (2100, 1000), (1030, 2048), (777, 2049), (513, 4100), (70, 8200),
-         (9, 33000), (3, 100001), (40000, 24)]
+         (9, 33000), (3, 100001), (40000, 24),
+         (140000, 30), (9001, 3), (70001, 33), (300, 64)]
 
 
 @pytest.mark.parametrize("dtype", list(T))
