@@ -190,7 +190,7 @@ struct SmallArgs {
     float *D, *X;              // [n][v], [n][k]
 };
 
-template <int NB, int WAVES>
+template <int DT, int NB, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void small_soft_kernel(SmallArgs s)
 {
     const FewArgs &a = s.f;
@@ -206,12 +206,12 @@ __global__ __launch_bounds__(64 * WAVES) void small_soft_kernel(SmallArgs s)
         for (int64_t i = i0 + threadIdx.x; i < i1; i += 64 * WAVES) {
             const int64_t r = (uint32_t)i / k, t = target_at(a.targets, a.wide, r);
             const bool live = t >= 0 && t < a.v && s.dloss[r] != 0.0f;
-            s.X[i] = live ? static_cast<const float *>(a.X)[r * a.ldx + (i - r * a.k)] : 0.0f;
+            s.X[i] = live ? load1(a.X, r * a.ldx + (i - r * a.k), DT) : 0.0f;
         }
     }
     if ((int64_t)blockIdx.y * (16 * NB) >= a.n)      // here for the copy alone
         return;
-    if (!few_logits<GPIC_F32, NB, 1, WAVES>(a, v, row, col0) || row >= a.n)
+    if (!few_logits<DT, NB, 1, WAVES>(a, v, row, col0) || row >= a.n)
         return;
     const int64_t t = target_at(a.targets, a.wide, row);
     const float gl = s.dloss[row];
@@ -224,7 +224,7 @@ __global__ __launch_bounds__(64 * WAVES) void small_soft_kernel(SmallArgs s)
         const int64_t col = col0 + j;
         if (col >= a.v)
             break;
-        const float bias = a.bias ? load1(a.bias, col, GPIC_F32) : 0.0f;
+        const float bias = a.bias ? load1(a.bias, col, DT) : 0.0f;
         float d = col == t ? expm1f(-loss)
                            : __builtin_amdgcn_exp2f((float)(v[j] + bias - at - off) * kLog2e);
         d = bias == -INFINITY && col != t ? 0.0f : d;
@@ -470,16 +470,18 @@ constexpr int64_t kWideFew = 16384;     // columns that fill the card two blocks
 
 // Few rows (float32's split copies of W cost more for up to 64), or little work,
 // where launches count; not many short rows (2,000 x 1 -> 50,000 380 us, 60 tiled).
+int64_t few_rows(const Loss &p) { return p.dtype == GPIC_F32 ? kThinRows : kFew; }
+
 bool few(const Loss &p)
 {
     const bool f32 = p.dtype == GPIC_F32;
-    if (p.n <= (f32 ? kThinRows : kFew))
+    if (p.n <= few_rows(p))
         return true;
     return p.n <= 2048 && p.n * p.v <= (1 << 23) &&
            p.n * p.v <= ((int64_t)1 << (f32 ? 28 : 27)) / p.k;
 }
 
-// The gradients of little work or few rows: float32, from D in float32
+// The gradients of little work in float32 or of few rows: from D in float32
 // (small_gradients.hip, loss_thin.hip).
 Shape layer_of(const Loss &p)
 {
@@ -495,11 +497,25 @@ Shape layer_of(const Loss &p)
     return s;
 }
 
-bool little(const Loss &p) { return small_gradients(layer_of(p), false); }
+bool little(const Loss &p)
+{
+    return p.dtype == GPIC_F32 && small_gradients(layer_of(p), false);
+}
+
+// 16 bits: up to 8 rows, whose roundings of D do not average out (one row of 39 ->
+// 3,840 in float16, dW off by 2.5e-4 in the 2-norm, 1.3e-4 from the result's own), and
+// up to 32 over a small W.  us, here and tiled: 1 x 2,048 -> 32,000 109 and 106, 8 rows
+// 115 and 107, 32 rows 185 and 108; 32 x 1,000 -> 1,000 24 and 32, 32 x 4,096 -> 100 25 and
+// 40, 8 x 65,000 -> 5 64 and 334.
+constexpr int kFewSoft = 8;
 
 bool small(const Loss &p)
 {
-    return p.n > 0 && p.dtype == GPIC_F32 && (p.n <= kThinRows || little(p));
+    if (p.n == 0 || little(p))
+        return p.n > 0;
+    if (p.dtype == GPIC_F32)
+        return p.n <= kThinRows;
+    return p.n <= kFewSoft || (p.n <= kFew && p.k * p.v <= 1 << 21);
 }
 
 int64_t edge_of(const Plan &p) { return p.tile == 0 ? 256 : (p.tile == 1 ? 128 : 64); }
@@ -745,23 +761,37 @@ hipError_t run_loss(const Loss &p, const void *X, const void *W, const void *bia
     return hipGetLastError();
 }
 
-template <int NB>
-hipError_t launch_small(const SmallArgs &a, hipStream_t st)
+template <int DT, int NB>
+hipError_t launch_small_of(const SmallArgs &a, int64_t turns, hipStream_t st)
 {
     const FewArgs &f = a.f;
     const int64_t x = (f.v + 15) / 16, y = (f.n + 16 * NB - 1) / (16 * NB);
-    const int64_t turns = (f.k + 63) / 64, threads = turns <= 4 ? 256 : (turns <= 8 ? 512 : 1024);
+    const int64_t threads = turns <= 4 ? 256 : (turns <= 8 ? 512 : 1024);
     // X's copy: up to eight values a thread on up to 1,024 workgroups
     int64_t more = (f.n * f.k + 8 * threads - 1) / (8 * threads);
     more = ((more < 1024 ? more : 1024) + x - 1) / x;
     const dim3 blocks((unsigned)x, (unsigned)(y > more ? y : more));
     if (turns <= 4)
-        small_soft_kernel<NB, 4><<<blocks, 256, 0, st>>>(a);
+        small_soft_kernel<DT, NB, 4><<<blocks, 256, 0, st>>>(a);
     else if (turns <= 8)
-        small_soft_kernel<NB, 8><<<blocks, 512, 0, st>>>(a);
+        small_soft_kernel<DT, NB, 8><<<blocks, 512, 0, st>>>(a);
     else
-        small_soft_kernel<NB, 16><<<blocks, 1024, 0, st>>>(a);
+        small_soft_kernel<DT, NB, 16><<<blocks, 1024, 0, st>>>(a);
     return hipGetLastError();
+}
+
+template <int DT>
+hipError_t launch_small(const SmallArgs &a, const Loss &p, hipStream_t st)
+{
+    const int64_t turns = turns_of(p);
+    if (p.n <= 16 || thin_grid(a.f))
+        return launch_small_of<DT, 1>(a, turns, st);
+    // W once for all rows up to 64 (64 rows over 2,048 -> 32,000: 185 us with it
+    // read twice, 164 so; the forward kernel 133 and 160, which reads it twice)
+    if constexpr (DT == GPIC_F32)
+        if (p.n > 32 && p.n <= kThinRows && p.v >= kWideFew / 4)
+            return launch_small_of<DT, 4>(a, turns, st);
+    return launch_small_of<DT, 2>(a, turns, st);
 }
 
 hipError_t run_loss_backward(const Loss &p, const float *dloss, const void *X, const void *W,
@@ -789,16 +819,12 @@ hipError_t run_loss_backward(const Loss &p, const float *dloss, const void *X, c
         a.lse = lse;
         a.D = m.D;
         a.X = m.X;
-        // W once for all rows up to 64 (64 rows over 2,048 -> 32,000: 185 us with it
-        // read twice, 164 so; the forward kernel 133 and 160, which reads it twice)
-        RUN(p.n <= 16 || thin_grid(a.f)                            ? launch_small<1>(a, st)
-            : p.n <= 32 || p.n > kThinRows || p.v < kWideFew / 4 ? launch_small<2>(a, st)
-                                                                 : launch_small<4>(a, st));
+        RUN(p.dtype == GPIC_F32    ? launch_small<GPIC_F32>(a, p, st)
+            : p.dtype == GPIC_F16 ? launch_small<GPIC_F16>(a, p, st)
+                                  : launch_small<GPIC_BF16>(a, p, st));
         if (little(p))
             return run_small_gradients(layer_of(p), false, m.D, m.X, W, nullptr, dX, dW, db, st);
-        return run_thin_gradients(m.D, m.X, static_cast<const float *>(W), p.n, p.k, p.v, p.ldw,
-                                  static_cast<float *>(dX), static_cast<float *>(dW),
-                                  static_cast<float *>(db), m.part, st);
+        return run_thin_gradients(m.D, m.X, W, p.n, p.k, p.v, p.ldw, p.dtype, dX, dW, db, m.part, st);
     }
     Backward b(p, X, W, c);
     const bool f32 = p.dtype == GPIC_F32;

@@ -1,7 +1,8 @@
-// Gradients of up to 64 float32 rows from D (n x v) in float32: dX = D W and
-// dW = D^T X on the float32 matrix instruction, W and dW read and written once
-// as they lie.  The tiled products' split copies of W (two of them, and its
-// columns' maxima) are five times its bytes, which is what few rows are bound by.
+// Gradients of up to 64 rows from D (n x v) in float32: dX = D W and dW = D^T X on
+// the float32 matrix instruction, W and dW read and written once as they lie.
+// float32: the tiled products' split copies of W (two of them, and its columns'
+// maxima) are five times its bytes, which is what few rows are bound by.  16 bits:
+// D is not rounded.
 //
 // mfma_f32_16x16x4: a lane (g = lane / 16, r = lane mod 16) holds one value of both
 // operands, k = g; of the result rows r of the second operand and columns 4 g +
@@ -19,21 +20,24 @@ namespace gpic {
 namespace {
 
 struct ThinArgs {
-    const float *D, *X, *W;    // [n][v], [n][k], [v] of pitch ldw
-    float *dX, *dW, *part;     // part: [parts][n][k]
+    const float *D, *X;        // [n][v], [n][k]
+    const void *W;             // [v] of pitch ldw, of the matrices' type, as dX and dW
+    void *dX, *dW;
+    float *part;               // [parts][n][k]
     int64_t n, k, v, ldw, strips, each, parts;
 };
 
-// Columns c .. c + 3 of a row of `cols`, zeros beyond
-__device__ __forceinline__ f32x4 quad(const float *row, int64_t c, int64_t cols)
+// Columns c .. c + 3 of a row of `cols` that starts at `row`, zeros beyond
+template <int DT>
+__device__ __forceinline__ f32x4 quad(const void *p, int64_t row, int64_t c, int64_t cols)
 {
     if (c + 4 <= cols)
-        return load4(row, c, GPIC_F32);
+        return load4(p, row + c, DT);
     f32x4 x = 0.0f;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
         if (c + j < cols)
-            x[j] = row[c + j];
+            x[j] = load1(p, row + c + j, DT);
     return x;
 }
 
@@ -57,10 +61,11 @@ __device__ __forceinline__ void put16(float *row, int64_t col, int64_t cols, con
 }
 
 // dW: a wave keeps 64 columns of X (4 STEPS rows) in registers and takes 16 rows
-// of dW after another.  Column r of the first operand is column 16 c + r here, so
-// that four lanes store 64 bytes of a row (98 us with 16 bytes a lane at a pitch of
-// 64 and one row, 50 so).  Bound by writing dW, from 33 rows on also by its products.
-template <int STEPS>
+// of dW after another.  Column r = 4 g + q of the first operand is column 16 c + r
+// here, of 16 bits 32 (c / 2) + 8 g + 4 (c mod 2) + q, so that four lanes store 64 bytes
+// of a row (one row in float32: 98 us with 16 bytes a lane 64 apart, 50 so).  Bound by
+// writing dW, from 33 rows on also by its products.
+template <int DT, int STEPS>
 __global__ __launch_bounds__(256) void thin_weights_kernel(ThinArgs a)
 {
     const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
@@ -74,7 +79,9 @@ __global__ __launch_bounds__(256) void thin_weights_kernel(ThinArgs a)
     for (int s = 0; s < STEPS; ++s)
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-            const int64_t i = 4 * s + g, j = j0 + 16 * c + r;
+            const int64_t i = 4 * s + g;
+            const int64_t j = j0 + (DT == GPIC_F32 ? 16 * c + r
+                                                   : 32 * (c / 2) + 8 * (r / 4) + 4 * (c % 2) + r % 4);
             x[s][c] = i < a.n && j < a.k ? a.X[i * a.k + j] : 0.0f;
         }
     // rows beyond the last are computed as the last and not stored
@@ -108,7 +115,18 @@ __global__ __launch_bounds__(256) void thin_weights_kernel(ThinArgs a)
         const int64_t v = b * 16 + r;
         if (v >= a.v)
             continue;
-        float *row = a.dW + v * a.k;
+        if constexpr (DT != GPIC_F32) {
+#pragma unroll
+            for (int c = 0; c < 4; c += 2) {
+                const int64_t j = j0 + 16 * c + 8 * g, left = a.k - j;
+                if (left > 0)
+                    store8(a.dW, v * a.k + j,
+                           __builtin_shufflevector(acc[c], acc[c + 1], 0, 1, 2, 3, 4, 5, 6, 7), DT,
+                           left < 8 ? (int)left : 8);
+            }
+            continue;
+        }
+        float *row = static_cast<float *>(a.dW) + v * a.k;
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
             const int64_t j = j0 + 16 * c + 4 * g;
@@ -127,7 +145,7 @@ __global__ __launch_bounds__(256) void thin_weights_kernel(ThinArgs a)
 // Partial dX: 64 columns by 16 NI rows a wave over a run of W's rows, 16 of them
 // (row 4 g + s in instruction s) at a time, the next on their way; the four waves
 // of a workgroup add up in LDS.  Bound by reading W.
-template <int NI>
+template <int DT, int NI>
 __global__ __launch_bounds__(256) void thin_points_kernel(ThinArgs a)
 {
     const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15, wave = threadIdx.x >> 6;
@@ -147,12 +165,13 @@ __global__ __launch_bounds__(256) void thin_points_kernel(ThinArgs a)
         for (int s = 0; s < 4; ++s) {
             // (beyond the last row D is zero)
             const int64_t v = v0 + s < a.v ? v0 + s : a.v - 1;
-            nw[s] = quad(a.W + v * a.ldw, j0 + 4 * r, a.k);
+            nw[s] = quad<DT>(a.W, v * a.ldw, j0 + 4 * r, a.k);
         }
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
             const int64_t row = 16 * i + r;
-            nd[i] = row < a.n ? quad(a.D + row * a.v, v0, a.v) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            nd[i] = row < a.n ? quad<GPIC_F32>(a.D, row * a.v, v0, a.v)
+                              : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         }
     };
     if (b0 < b1)
@@ -196,7 +215,7 @@ __global__ __launch_bounds__(256) void thin_points_kernel(ThinArgs a)
 }
 
 // dX from its parts, in float64 in a fixed order
-__global__ __launch_bounds__(256) void thin_join_kernel(ThinArgs a)
+__global__ __launch_bounds__(256) void thin_join_kernel(ThinArgs a, int dtype)
 {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, values = a.n * a.k;
     if (i >= values)
@@ -205,11 +224,12 @@ __global__ __launch_bounds__(256) void thin_join_kernel(ThinArgs a)
 #pragma unroll 8
     for (int64_t p = 0; p < a.parts; ++p)
         t += (double)a.part[p * values + i];
-    a.dX[i] = (float)t;
+    store1(a.dX, i, (float)t, dtype);
 }
 
 // db: column sums of D
-__global__ __launch_bounds__(256) void thin_bias_kernel(const float *D, int64_t n, int64_t v, float *db)
+__global__ __launch_bounds__(256) void thin_bias_kernel(const float *D, int64_t n, int64_t v, void *db,
+                                                        int dtype)
 {
     const int64_t col = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (col >= v)
@@ -218,7 +238,7 @@ __global__ __launch_bounds__(256) void thin_bias_kernel(const float *D, int64_t 
 #pragma unroll 8
     for (int64_t i = 0; i < n; ++i)
         t += (double)D[i * v + col];
-    db[col] = (float)t;
+    store1(db, col, (float)t, dtype);
 }
 
 // about four workgroups a compute unit, none of fewer than four turns a wave
@@ -237,50 +257,62 @@ size_t thin_ws(int64_t n, int64_t k, int64_t v)
     return (size_t)parts_of(k, v) * n * k * 4;
 }
 
-hipError_t run_thin_gradients(const float *D, const float *X, const float *W, int64_t n, int64_t k,
-                              int64_t v, int64_t ldw, float *dX, float *dW, float *db, float *part,
-                              hipStream_t st)
+namespace {
+
+template <int DT>
+hipError_t run(ThinArgs a, void *db, hipStream_t st)
 {
-    ThinArgs a{D, X, W, dX, dW, part, n, k, v, ldw, (k + 63) / 64, 0, parts_of(k, v)};
-    const int64_t blocks = (v + 15) / 16;
+    const int64_t n = a.n, blocks = (a.v + 15) / 16;
     hipError_t e = hipSuccess;
-    if (dW) {
+    if (a.dW) {
         // about eight waves for each of the card's 1,024 vector units
         a.each = (blocks * a.strips + 8191) / 8192;
         const int64_t waves = (blocks + a.each - 1) / a.each * a.strips;
         const unsigned grid = (unsigned)((waves + 3) / 4);
         if (n <= 16)
-            thin_weights_kernel<4><<<grid, 256, 0, st>>>(a);
+            thin_weights_kernel<DT, 4><<<grid, 256, 0, st>>>(a);
         else if (n <= 32)
-            thin_weights_kernel<8><<<grid, 256, 0, st>>>(a);
+            thin_weights_kernel<DT, 8><<<grid, 256, 0, st>>>(a);
         else if (n <= 48)
-            thin_weights_kernel<12><<<grid, 256, 0, st>>>(a);
+            thin_weights_kernel<DT, 12><<<grid, 256, 0, st>>>(a);
         else
-            thin_weights_kernel<16><<<grid, 256, 0, st>>>(a);
+            thin_weights_kernel<DT, 16><<<grid, 256, 0, st>>>(a);
         e = hipGetLastError();
     }
-    if (e == hipSuccess && dX) {
+    if (e == hipSuccess && a.dX) {
         a.each = (blocks + 4 * a.parts - 1) / (4 * a.parts);
         const unsigned grid = (unsigned)(a.strips * a.parts);
         if (n <= 16)
-            thin_points_kernel<1><<<grid, 256, 0, st>>>(a);
+            thin_points_kernel<DT, 1><<<grid, 256, 0, st>>>(a);
         else if (n <= 32)
-            thin_points_kernel<2><<<grid, 256, 0, st>>>(a);
+            thin_points_kernel<DT, 2><<<grid, 256, 0, st>>>(a);
         else if (n <= 48)
-            thin_points_kernel<3><<<grid, 256, 0, st>>>(a);
+            thin_points_kernel<DT, 3><<<grid, 256, 0, st>>>(a);
         else
-            thin_points_kernel<4><<<grid, 256, 0, st>>>(a);
+            thin_points_kernel<DT, 4><<<grid, 256, 0, st>>>(a);
         e = hipGetLastError();
         if (e != hipSuccess)
             return e;
-        thin_join_kernel<<<(unsigned)((n * k + 255) / 256), 256, 0, st>>>(a);
+        thin_join_kernel<<<(unsigned)((n * a.k + 255) / 256), 256, 0, st>>>(a, DT);
         e = hipGetLastError();
     }
     if (e == hipSuccess && db) {
-        thin_bias_kernel<<<(unsigned)((v + 255) / 256), 256, 0, st>>>(D, n, v, db);
+        thin_bias_kernel<<<(unsigned)((a.v + 255) / 256), 256, 0, st>>>(a.D, n, a.v, db, DT);
         e = hipGetLastError();
     }
     return e;
+}
+
+} // namespace
+
+hipError_t run_thin_gradients(const float *D, const float *X, const void *W, int64_t n, int64_t k,
+                              int64_t v, int64_t ldw, int dtype, void *dX, void *dW, void *db,
+                              float *part, hipStream_t st)
+{
+    const ThinArgs a{D, X, W, dX, dW, part, n, k, v, ldw, (k + 63) / 64, 0, parts_of(k, v)};
+    return dtype == GPIC_F32    ? run<GPIC_F32>(a, db, st)
+           : dtype == GPIC_F16 ? run<GPIC_F16>(a, db, st)
+                               : run<GPIC_BF16>(a, db, st);
 }
 
 } // namespace gpic

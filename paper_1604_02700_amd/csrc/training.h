@@ -46,13 +46,13 @@ hipError_t run_embedding_backward(const Embedding &p, const void *dY, const void
                                   void *ws, hipStream_t st);
 
 // ---------------------------------------------------------- loss_thin.hip
-// Gradients of up to kThinRows float32 rows from D [n][v] and a contiguous X;
-// part: thin_ws bytes.
+// Gradients of up to kThinRows rows from D [n][v] and a contiguous X, both float32
+// whatever the matrices' type; part: thin_ws bytes.
 constexpr int64_t kThinRows = 64;
 size_t thin_ws(int64_t n, int64_t k, int64_t v);
-hipError_t run_thin_gradients(const float *D, const float *X, const float *W, int64_t n, int64_t k,
-                              int64_t v, int64_t ldw, float *dX, float *dW, float *db, float *part,
-                              hipStream_t st);
+hipError_t run_thin_gradients(const float *D, const float *X, const void *W, int64_t n, int64_t k,
+                              int64_t v, int64_t ldw, int dtype, void *dX, void *dW, void *db,
+                              float *part, hipStream_t st);
 
 // --------------------------------------------------------------- loss.hip
 struct Loss {

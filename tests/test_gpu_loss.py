@@ -149,7 +149,7 @@ SHAPES = [(1, 8, 1), (1, 2048, 500), (3, 5, 7), (17, 64, 300), (33, 40, 1000), (
           (4100, 72, 5001), (2049, 520, 4099), (700, 1, 33), (20, 3001, 100), (5000, 24, 2),
           # few float32 rows over a large vocabulary, odd widths and partial blocks
           (1, 130, 5000), (16, 63, 3001), (17, 65, 2049), (33, 700, 4007), (64, 1, 2500), (48, 4099, 3000),
-          (65, 200, 3000), (64, 300, 5003),
+          (65, 200, 3000), (64, 300, 5003), (8, 203, 5001), (32, 129, 900),
           # tiles of the large size in every product
           (6000, 1100, 9000),
           # a handful of classes; rows beyond what 128 workgroups take at once
@@ -302,7 +302,8 @@ def test_non_finite_rows_and_certain_targets(g, n, dtype):
 
 
 @pytest.mark.parametrize("dtype", list(T))
-@pytest.mark.parametrize("shape", [(9, 100, 60), (1100, 104, 3000), (1100, 99, 3000)], ids=str)
+@pytest.mark.parametrize("shape", [(9, 100, 60), (1100, 104, 3000), (1100, 99, 3000),
+                                   (7, 99, 3000)], ids=str)
 def test_views_alignment_and_wanted_gradients(g, shape, dtype):
     n, k, v = shape
     X, W, b, t = _inputs(n, k, v, dtype)
