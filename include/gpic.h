@@ -693,7 +693,7 @@ size_t gpic_cross_entropy_workspace_bytes(int32_t backward, const gpic_loss_para
  * +infinity.  n = 0 does nothing.
  * ws: gpic_cross_entropy_workspace_bytes(0, p): split or padded copies of operands
  * that cannot be read as they lie, and 8 bytes for each row and tile (64 to 256
- * columns; up to 32 rows and small calls: 16) of the vocabulary.
+ * columns; up to 32 rows, float32 64, and small calls: 16) of the vocabulary.
  * Errors: INVALID_ARG, WORKSPACE, UNSUPPORTED. */
 gpic_status gpic_cross_entropy(const gpic_loss_params *p, const void *X, const void *W,
                                const void *bias, const void *targets, float *loss, float *lse,
@@ -707,8 +707,10 @@ gpic_status gpic_cross_entropy(const gpic_loss_params *p, const void *X, const v
  * rounded to the matrices' type (float16: nothing finer than 2^-39; float32: 22
  * bits down to 2^-17, errors of 2^-39 below), and for dW so is X times dloss over
  * the largest finite |dloss| (no rounding where all are alike); db sums it
- * unrounded.  X's rows of padding, and those whose dloss is 0, may hold anything.
- * With n = 0, dW and db are zeros.
+ * unrounded.  Few rows (float32 up to 64, 16 bits up to 8, and up to 32 over a small
+ * vocabulary) and little work in float32 keep dZ and X in float32, 4 n (v + k) bytes,
+ * and round nothing before the products.  X's rows of padding, and those whose dloss
+ * is 0, may hold anything.  With n = 0, dW and db are zeros.
  * ws: gpic_cross_entropy_workspace_bytes(1, p). */
 gpic_status gpic_cross_entropy_backward(const gpic_loss_params *p, const float *dloss,
                                         const void *X, const void *W, const void *bias,
