@@ -398,8 +398,6 @@ def test_weights_beyond_32_bits(g, n):
     tol = (k + 16) * E * 70 + 4 * (v / 256 / 16 + 40) * E + 4 * E * float(full.abs().max())
     _within(lse, full, torch.full_like(full, tol), "lse")
     _within(loss, full - z.gather(1, t[:, None])[:, 0], torch.full_like(full, 2 * tol), "loss")
-    if n == 2:
-        return
     gr = g.gpic_cross_entropy_backward(torch.ones(n, device=DEV), X, W, t, loss, lse)
     rows = torch.tensor([0, 1, 2 ** 31 // k, 2 ** 32 // k - 1, 2 ** 32 // k, 2 ** 32 // k + 1, v - 2,
                          v - 1], device=DEV)
