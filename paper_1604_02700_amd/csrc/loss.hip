@@ -167,7 +167,8 @@ __global__ __launch_bounds__(64 * WAVES) void few_lse_kernel(FewArgs a)
         s += __builtin_amdgcn_exp2f((float)(v[j] - at) * kLog2e);
     s += __shfl_xor(s, 16, 64);
     s += __shfl_xor(s, 32, 64);
-    if (live && (threadIdx.x & 63) < 16)
+    // (the last workgroup's second block may lie beyond the last column)
+    if (live && (threadIdx.x & 63) < 16 && col0 < a.v)
         a.strip[(col0 >> 4) * a.n + row] = make_float2(m, s);
 }
 

@@ -1,0 +1,103 @@
+"""Edges of the calls around an encoder's layers that their shapes elsewhere
+cross by luck or not at all: workspaces of exactly the bytes that a call asks
+for, with others' bytes on both sides.
+
+Tolerances as derived in test_gpu_loss and test_gpu_training."""
+import pytest
+
+from test_gpu_loss import DEV, T, _check, _inputs, _randn
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture(scope="module")
+def g():
+    import paper_1604_02700_amd as g
+    g.lib()
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    return g
+
+
+class Exact:
+    """The binding's workspaces, each between 4,096 bytes that have to stay."""
+
+    def __init__(self, monkeypatch, g):
+        self.given = []
+        monkeypatch.setattr(g, "_workspace", self.make)
+
+    def make(self, nbytes, device):
+        if nbytes == 0:
+            return None, 0
+        buf = torch.full((nbytes + 8448,), 0xA5, dtype=torch.uint8, device=device)
+        off = 4096 + (-buf.data_ptr()) % 256
+        self.given.append((buf, off, nbytes))
+        return buf[off:off + nbytes], nbytes
+
+    def check(self, least=1):
+        assert len(self.given) >= least
+        for buf, off, nbytes in self.given:
+            assert bool((buf[:off] == 0xA5).all()), "before the workspace"
+            assert bool((buf[off + nbytes:] == 0xA5).all()), "behind the workspace"
+        self.given.clear()
+
+
+# ------------------------------------------------------------------- loss
+@pytest.mark.parametrize("waves", [4, 8, 16])
+@pytest.mark.parametrize("n", [1, 9, 16, 17, 32, 43, 64])
+@pytest.mark.parametrize("v", [16385, 32001])
+@pytest.mark.parametrize("dtype", list(T))
+def test_losses_of_few_rows_stay_in_their_workspace(g, monkeypatch, dtype, v, n, waves):
+    """An odd number of blocks of 16 columns, taken two at a time; the
+    contraction's turns shared by 4, 8 and 16 waves."""
+    k = (64 if dtype == "f32" else 128) * waves - 3
+    X, W, b, t = _inputs(n, k, v, dtype)
+    t[0] = v - 1                           # in the last block
+    exact = Exact(monkeypatch, g)
+    _check(g, X, W, b, t, torch.full((n,), 64.0 if dtype == "f16" else 1.0 / n, device=DEV), dtype,
+           f"{waves} waves")
+    exact.check(4)
+
+
+LOSSES = [(1, 8, 1), (3, 5, 7), (33, 40, 1000), (130, 72, 257), (1003, 70, 4007), (33, 700, 4097),
+          (64, 1000, 4111), (300, 136, 5000), (4100, 72, 501), (5000, 24, 2)]
+
+
+@pytest.mark.parametrize("dtype", list(T))
+@pytest.mark.parametrize("shape", LOSSES, ids=str)
+def test_losses_stay_in_their_workspace(g, monkeypatch, shape, dtype):
+    n, k, v = shape
+    X, W, b, t = _inputs(n, k, v, dtype)
+    exact = Exact(monkeypatch, g)
+    _check(g, X, W, b, t, torch.full((n,), 64.0 if dtype == "f16" else 1.0 / n, device=DEV), dtype,
+           "exact")
+    exact.check(4)
+
+
+# --------------------------------------------------------- norm and table
+@pytest.mark.parametrize("dtype", list(T))
+@pytest.mark.parametrize("shape", [(1, 1), (3, 7), (300, 64), (70, 2049), (1003, 300), (9, 33000),
+                                   (70, 8200)], ids=str)
+def test_norms_stay_in_their_workspace(g, monkeypatch, shape, dtype):
+    n, k = shape
+    X, w, dY = _randn((n, k), dtype, 1), _randn((k,), dtype, 2), _randn((n, k), dtype, 3)
+    _, stats = g.gpic_layer_norm(X, w, want_stats=True)
+    want = g.gpic_layer_norm_backward(dY, X, w, stats)
+    exact = Exact(monkeypatch, g)
+    got = g.gpic_layer_norm_backward(dY, X, w, stats)
+    exact.check()
+    for name in ("dX", "dW", "db"):
+        assert torch.equal(getattr(got, name), getattr(want, name))
+
+
+@pytest.mark.parametrize("dtype", list(T))
+@pytest.mark.parametrize("shape", [(1025, 1, 3), (1039, 33, 70), (4097, 513, 256), (70001, 24, 9)],
+                         ids=str)
+def test_table_gradients_stay_in_their_workspace(g, monkeypatch, shape, dtype):
+    n, k, rows = shape
+    ids = torch.arange(n, device=DEV) * rows // n
+    dY = _randn((n, k), dtype, 1)
+    want = g.gpic_embedding_backward(dY, ids, rows)
+    exact = Exact(monkeypatch, g)
+    assert torch.equal(g.gpic_embedding_backward(dY, ids, rows), want)
+    exact.check()
