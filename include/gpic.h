@@ -706,7 +706,8 @@ gpic_status gpic_cross_entropy(const gpic_loss_params *p, const void *X, const v
  * the vocabulary whose dZ takes up to 512 MB, or 2,048 columns.  For the products dZ / dloss is
  * rounded to the matrices' type (float16: nothing finer than 2^-39; float32: 22
  * bits down to 2^-17, errors of 2^-39 below), and for dW so is X times dloss over
- * the largest finite |dloss| (no rounding where all are alike); db sums it
+ * the largest finite |dloss| (no rounding where all are alike; float16: nothing finer
+ * than 2^-39 of the largest such value, float32: of its column's); db sums dZ
  * unrounded.  Few rows (float32 up to 64, 16 bits up to 8, and up to 32 over a small
  * vocabulary) and little work in float32 keep dZ and X in float32, 4 n (v + k) bytes,
  * and round nothing before the products.  X's rows of padding, and those whose dloss

@@ -340,7 +340,8 @@ struct Epilogue {
     const LossRow *rows;
     int64_t first;
     float *sums;
-    // kEpiSum: operand A is under 2^kSoftPower (but in bfloat16); factors, one a
+    // kEpiSum: operand A is under 2^kSoftPower (but in bfloat16), float16 both
+    // together under 2^*pa more (if not null); factors, one a
     // row or (factor_step 0) for all; sums so far (float32, res and ldr) or null;
     // out is float32, or (last) of the operands' type
     const float *factor;
@@ -399,6 +400,9 @@ struct Source {
     void *to = nullptr;
     int *power = nullptr;  // float32: of its rows (backward: columns)
     const float *row = nullptr;    // packed times this, by row (0: zeros)
+    const float *most = nullptr;   // float16: `count` parts of the largest of that, for
+    int count = 0;                 // the power of two that goes to *scale
+    int *scale = nullptr;
     Operand operand(int dtype) const
     {
         if (!pack)

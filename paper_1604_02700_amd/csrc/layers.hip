@@ -43,6 +43,11 @@ struct PackJob {
     const int *power;      // float32: of every column
     const float *row;      // every row times this (or null); 0: zeros whatever it holds
     bool f16;
+    // float16 with factors: `count` parts of the largest of what is packed, which sets
+    // a power of two for all of it, not below 1; kept in *scale
+    const float *most;
+    int count;
+    int *scale;
 };
 struct PackJobs {
     PackJob j[3];
@@ -61,6 +66,13 @@ __global__ __launch_bounds__(256) void pack_kernel(PackJobs jobs)
     const PackJob m = jobs.j[blockIdx.y];
     const int64_t width = SPLIT ? (m.cols + 31) / 32 * 32 : up64(m.cols);
     const int64_t groups = width / 8, total = m.rows * groups;
+    int scale = 0;
+    if (!SPLIT && m.most) {
+        scale = power_for(join_max(m.most, m.count));
+        scale = scale < 0 ? 0 : scale;
+        if (blockIdx.x == 0 && threadIdx.x == 0)
+            *m.scale = scale;
+    }
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total;
          i += (int64_t)gridDim.x * 256) {
         const int64_t r = i / groups, c = (i - r * groups) * 8;
@@ -123,7 +135,7 @@ __global__ __launch_bounds__(256) void pack_kernel(PackJobs jobs)
                     if (m.f16)
                         u.h[k] = __builtin_bit_cast(
                             unsigned short,
-                            (_Float16)((float)__builtin_bit_cast(_Float16, u.h[k]) * f));
+                            (_Float16)ldexpf((float)__builtin_bit_cast(_Float16, u.h[k]) * f, scale));
                     else
                         u.h[k] = __builtin_bit_cast(
                             unsigned short, (__bf16)((float)__builtin_bit_cast(__bf16, u.h[k]) * f));
@@ -887,7 +899,8 @@ hipError_t launch_pack(const Source *const *list, int count, int dtype, hipStrea
     for (int i = 0; i < count; ++i)
         if (list[i]->pack && list[i]->rows > 0) {
             const Source &s = *list[i];
-            j.j[used++] = PackJob{s.x, s.rows, s.cols, s.ld, s.to, s.power, s.row, dtype == GPIC_F16};
+            j.j[used++] = PackJob{s.x, s.rows, s.cols, s.ld, s.to, s.power, s.row, dtype == GPIC_F16,
+                                  s.most, s.count, s.scale};
             const int64_t groups = s.rows * ((s.cols + 63) / 64 * 8);
             most = groups > most ? groups : most;
         }

@@ -266,7 +266,7 @@ template <int ROWS, int OP, int EPI>
 __device__ __forceinline__ int row_powers(const Epilogue &e, int64_t row0, int64_t M)
 {
     if (OP != kOpBf16 && EPI == kEpiSum)
-        return kSoftPower;
+        return kSoftPower + (OP == kOpF16 && e.pa ? e.pa[0] : 0);
     if (OP == kOpBf16 || !powered(EPI) || !e.pa)
         return 0;
     static_assert(ROWS <= 64, "a row a lane");

@@ -5,7 +5,7 @@ for, with others' bytes on both sides.
 Tolerances as derived in test_gpu_loss and test_gpu_training."""
 import pytest
 
-from test_gpu_loss import DEV, T, _check, _inputs, _randn
+from test_gpu_loss import DEV, E, T, U, _check, _close, _inputs, _randn
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
@@ -72,6 +72,49 @@ def test_losses_stay_in_their_workspace(g, monkeypatch, shape, dtype):
     _check(g, X, W, b, t, torch.full((n,), 64.0 if dtype == "f16" else 1.0 / n, device=DEV), dtype,
            "exact")
     exact.check(4)
+
+
+@pytest.mark.parametrize("scale", [1.0, 2.0 ** -9, 2.0 ** 13])
+@pytest.mark.parametrize("power", [16, 20, 22, 26])
+@pytest.mark.parametrize("dtype", list(T))
+def test_gradients_of_rows_with_small_shares(g, dtype, power, scale):
+    """Rows whose dloss is far below the largest keep their digits where they are
+    the only ones that an entry's weights learn from, whatever X's size is.
+
+    X's and W's first columns send half of the rows to half of the entries: the other
+    half's logits are 60 below.  The factor of such a row is 2^-power; X times it is an
+    operand of dW, rounded to U of it, float16 no finer than 2^-39 of the largest."""
+    n, k, v = 1100, 40, 700
+    X, W, t = _randn((n, k), dtype, 1), _randn((v, k), dtype, 2, 0.1), torch.arange(n, device=DEV) % v
+    low, far = torch.arange(n, device=DEV) % 2 == 1, torch.arange(v, device=DEV) % 2 == 1
+    X[:, 0] = torch.where(low, -2.0, 2.0).to(T[dtype])
+    W[:, 0] = torch.where(far, -15.0, 15.0).to(T[dtype])
+    X = X * scale                          # (powers of two: W makes up for them)
+    W = W / scale
+    big = 2.0 ** 11 / scale
+    dloss = torch.where(low, big * 2.0 ** -power, big)
+    print(f"shares {dtype} 2^-{power} scale {scale}", flush=True)
+    loss, lse = g.gpic_cross_entropy(X, W, t, want_lse=True)
+    dW = g.gpic_cross_entropy_backward(dloss, X, W, t, loss, lse).dW
+    x, w, gl = X.double(), W.double(), dloss.double()[:, None]
+    z = x @ w.t()
+    p = (z - z.logsumexp(1, keepdim=True)).exp()
+    p[torch.arange(n, device=DEV), t] -= 1.0
+    # a logit, its lse and the target's loss: each within (k + 16) e of the products' sizes,
+    # float32's halves 2^-21 of them; the exponential's argument, joins and rounding 60 e
+    size = (x.abs() @ w.abs().t()).amax()
+    rel = 3 * ((k + 16) * E + (2.0 ** -21 if dtype == "f32" else 0.0)) * size + 100 * E
+    d = gl * p
+    off = (rel + (2.0 ** -22 if dtype == "f32" else U[dtype])) * d.abs()
+    if dtype != "bf16":
+        off = off + torch.minimum(d.abs(), 2.0 ** -39 * gl)
+    ew = off.t() @ x.abs() + ((n + 19) * E + U[dtype]) * (d.abs().t() @ x.abs())
+    if dtype == "f16":
+        ew += 2.0 ** -39 * (gl * x.abs()).amax() * p.abs().sum(0)[:, None]
+    if dtype == "f32":
+        ew += 2.0 ** -21 * (d.abs().t() @ x.abs())
+        ew += 2.0 ** -38 * p.abs().sum(0)[:, None] * (gl * x.abs()).amax(0)
+    _close(dW[far], (d.t() @ x)[far], ew[far], dtype, "dW")
 
 
 # --------------------------------------------------------- norm and table
