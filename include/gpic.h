@@ -601,7 +601,8 @@ typedef struct gpic_norm_params {
  * variance over k.  weight and bias [k] nullable (ones, zeros); stats (float32
  * [n x 2], 8-byte aligned, nullable) receives mean and r, which the gradients
  * need.  A row that holds a NaN or an infinity gives a row of NaN and no other
- * does; deviations beyond 1.8e19 have no float32 square (r = 0).
+ * does (but, with eps 0, one whose deviations' squares, up to 1e-45, are all 0); rows
+ * up to the type's largest value are as any other (from 9e37 on, r is a subnormal).
  * Y may be X itself (same pitch).  Errors: INVALID_ARG. */
 gpic_status gpic_layer_norm(const gpic_norm_params *p, const void *X, const void *weight,
                             const void *bias, void *Y, float *stats, void *stream);

@@ -90,6 +90,85 @@ struct Chunk {
     }
 };
 
+// A row's values count as x c, their mean is m and their reciprocal spread r.
+struct RowStats {
+    float c, m, r;
+};
+
+// RowStats from the sums of the deviations from m, which correct it, and of their
+// squares.  Whether a sum or square is no float32.
+__device__ __forceinline__ bool settle(RowStats &q, float s, float t, float inv, float eps)
+{
+    const float off = s * inv, var = fmaxf(t * inv - off * off, 0.0f);
+    q.m += off;
+    q.r = 1.0f / sqrtf((t != t ? t : var) + eps);
+    return !(t < INFINITY);
+}
+
+// Such rows once more, from memory (a function of its own, which takes none of the
+// kernel's registers).  Values beyond 1e19 or so are scaled by 2^-100, which leaves
+// everything that matters beside the largest.
+template <int DT, int LANES>
+__device__ __noinline__ void norm_anew(const void *X, const void *w, const void *b, void *Y,
+                                       float *stats, int64_t k, float eps, float2 *part)
+{
+    constexpr float kMost = 0x1.fffffep127f;
+    const int at = threadIdx.x % LANES;
+    const float inv = 1.0f / (float)k;
+    RowStats q;
+    q.c = 1.0f;
+    for (int turn = 0; turn < 2; ++turn) {
+        float s = 0.0f, t = 0.0f;
+#pragma unroll 8
+        for (int64_t c = at; c < k; c += LANES)
+            s += load1(X, c, DT) * q.c;
+        row_sums<LANES>(s, t, part);
+        q.m = s * inv;
+        s = t = 0.0f;
+#pragma unroll 8
+        for (int64_t c = at; c < k; c += LANES) {
+            const float d = load1(X, c, DT) * q.c - q.m;
+            s += d;
+            t += d * d;
+        }
+        row_sums<LANES>(s, t, part);
+        if (!settle(q, s, t, inv, eps * q.c * q.c) || turn == 1)
+            break;
+        q.c = 0x1p-100f;
+    }
+    float mean = q.m, rs = q.r;
+    if (q.c != 1.0f) {
+        rs = q.r * q.c;
+        mean = q.m * 0x1p100f;
+        if (fabsf(mean) == INFINITY)         // of finite values: rounded so
+            mean = copysignf(kMost, mean);
+        if (q.r == INFINITY && eps > 0.0f) { // (rows of one value: eps vanishes beside 2^200)
+            rs = 1.0f / sqrtf(eps);
+            q.r = kMost;
+        }
+    }
+    if (stats && at == 0)
+        *reinterpret_cast<float2 *>(stats) = make_float2(mean, rs);
+#pragma unroll 4
+    for (int64_t c = at; c < k; c += LANES) {
+        float y = (load1(X, c, DT) * q.c - q.m) * q.r;
+        if (w)
+            y *= load1(w, c, DT);
+        if (b)
+            y += load1(b, c, DT);
+        store1(Y, c, y, DT);
+    }
+}
+
+template <int DT, int LANES>
+__device__ __forceinline__ void norm_anew(const NormArgs &a, int64_t r, float2 *part)
+{
+    constexpr int kSize = DT == GPIC_F32 ? 4 : 2;
+    norm_anew<DT, LANES>(static_cast<const char *>(a.X) + r * a.ldx * kSize, a.w, a.b,
+                         static_cast<char *>(a.Y) + r * a.ldy * kSize,
+                         a.stats ? a.stats + 2 * r : nullptr, a.k, a.eps, part);
+}
+
 // Rows that LANES lanes hold in HOLD groups of eight columns each, with the next
 // row on its way while one is finished: the mean, then the deviations from it,
 // whose own sum corrects it, so that rows far from zero lose nothing.  Groups of
@@ -118,6 +197,8 @@ __global__ __launch_bounds__(256) void norm_rows_kernel(NormArgs a)
     };
     const int64_t step = (int64_t)gridDim.x * kRows;
     int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES;
+    const int64_t first = r;
+    uint64_t again = 0;                  // which of up to 64 rows are not settled
     if (r < a.n)
         fetch(r);
 #pragma unroll
@@ -127,7 +208,7 @@ __global__ __launch_bounds__(256) void norm_rows_kernel(NormArgs a)
         if (a.b)
             b[h].load(a.b, (at + h * LANES) * 8, valid[h]);
     }
-    for (; r < a.n; r += step) {
+    for (int turn = 0; r < a.n; ++turn, r += step) {
 #pragma unroll
         for (int h = 0; h < HOLD; ++h)
             x[h] = next[h];
@@ -142,30 +223,29 @@ __global__ __launch_bounds__(256) void norm_rows_kernel(NormArgs a)
                 s += v[j];                   // (zeros beyond the row)
         }
         row_sums<LANES>(s, t, part);
-        float mean = s * inv;
+        RowStats q;
+        q.m = s * inv;
         s = t = 0.0f;
 #pragma unroll
         for (int h = 0; h < HOLD; ++h) {
             const f32x8 v = x[h].floats();
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float d = j < valid[h] ? v[j] - mean : 0.0f;
+                const float d = j < valid[h] ? v[j] - q.m : 0.0f;
                 s += d;
                 t += d * d;
             }
         }
         row_sums<LANES>(s, t, part);
-        const float off = s * inv;
-        mean += off;
-        const float var = fmaxf(t * inv - off * off, 0.0f);
-        const float rs = 1.0f / sqrtf((t != t ? t : var) + a.eps);
+        const bool open = settle(q, s, t, inv, a.eps);
+        again |= open ? 1ull << turn : 0;
         if (a.stats && at == 0)
-            reinterpret_cast<float2 *>(a.stats)[r] = make_float2(mean, rs);
+            reinterpret_cast<float2 *>(a.stats)[r] = make_float2(q.m, q.r);
 #pragma unroll
         for (int h = 0; h < HOLD; ++h) {
-            if (!valid[h])
+            if (!valid[h] || open)           // (Y may be X, which is read again)
                 continue;
-            f32x8 y = (x[h].floats() - mean) * rs;
+            f32x8 y = (x[h].floats() - q.m) * q.r;
             if (a.w)
                 y = y * w[h].floats();
             if (a.b)
@@ -173,6 +253,8 @@ __global__ __launch_bounds__(256) void norm_rows_kernel(NormArgs a)
             store8(a.Y, r * a.ldy + (at + h * LANES) * 8, y, DT, valid[h]);
         }
     }
+    for (; again; again &= again - 1)
+        norm_anew<DT, LANES>(a, first + __builtin_ctzll(again) * step, part);
 }
 
 // Longer rows: a workgroup a row, eight columns at a time a lane; up to kHold
@@ -203,12 +285,13 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_kernel(NormArg
                 s += u[j];
         }
         row_sums<LANES>(s, t, part);
-        float mean = s * inv;
+        RowStats q;
+        q.m = s * inv;
         s = t = 0.0f;
         auto deviate = [&](const f32x8 &u, int64_t g) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float d = g * 8 + j < a.k ? u[j] - mean : 0.0f;
+                const float d = g * 8 + j < a.k ? u[j] - q.m : 0.0f;
                 s += d;
                 t += d * d;
             }
@@ -219,18 +302,18 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_kernel(NormArg
         for (int64_t g = at + kHold * LANES; g < groups; g += LANES)
             deviate(read8<DT>(a.X, r * a.ldx, g * 8, a.k), g);
         row_sums<LANES>(s, t, part);
-        const float off = s * inv;
-        mean += off;
-        const float var = fmaxf(t * inv - off * off, 0.0f);
-        const float rs = 1.0f / sqrtf((t != t ? t : var) + a.eps);
+        if (settle(q, s, t, inv, a.eps)) {
+            norm_anew<DT, LANES>(a, r, part);
+            continue;
+        }
         if (a.stats && at == 0)
-            reinterpret_cast<float2 *>(a.stats)[r] = make_float2(mean, rs);
+            reinterpret_cast<float2 *>(a.stats)[r] = make_float2(q.m, q.r);
         auto write = [&](const f32x8 &u, int64_t g) {
             const int64_t left = a.k - g * 8;
             if (left <= 0)
                 return;
             const int valid = left < 8 ? (int)left : 8;
-            f32x8 y = (u - mean) * rs;
+            f32x8 y = (u - q.m) * q.r;
             if (a.w)
                 y = y * load8(a.w, g * 8, DT, valid);
             if (a.b)
@@ -244,6 +327,20 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_kernel(NormArg
             write(read8<DT>(a.X, r * a.ldx, g * 8, a.k), g);
     }
 }
+
+// h = (x - mean) r.  Rows of the largest values deviate by more than a float32
+// holds, and then r is next to nothing: both under a power of two.
+struct Deviation {
+    float c, m, r;
+    __device__ __forceinline__ explicit Deviation(float2 stats)
+    {
+        c = stats.y < 0x1p-100f ? 0x1p-10f : 1.0f;
+        m = stats.x * c;
+        r = stats.y < 0x1p-100f ? stats.y * 0x1p10f : stats.y;
+    }
+    template <class T>
+    __device__ __forceinline__ T of(T x) const { return (x * c - m) * r; }
+};
 
 struct NormGradArgs {
     const void *dY, *X, *w;
@@ -266,7 +363,7 @@ __global__ __launch_bounds__(256) void norm_dots_kernel(NormGradArgs a)
     const float inv = 1.0f / (float)a.k;
     for (int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES; r < a.n;
          r += (int64_t)gridDim.x * kRows) {
-        const float2 st = reinterpret_cast<const float2 *>(a.stats)[r];
+        const Deviation h(reinterpret_cast<const float2 *>(a.stats)[r]);
         float s = 0.0f, t = 0.0f;
         for (int64_t g = at; g < groups; g += LANES) {
             const int valid = a.k - g * 8 < 8 ? (int)(a.k - g * 8) : 8;
@@ -278,7 +375,7 @@ __global__ __launch_bounds__(256) void norm_dots_kernel(NormGradArgs a)
             for (int j = 0; j < 8; ++j)
                 if (j < valid) {
                     s += d[j];
-                    t += d[j] * ((x[j] - st.x) * st.y);
+                    t += d[j] * h.of(x[j]);
                 }
         }
         row_sums<LANES>(s, t, part);
@@ -306,7 +403,7 @@ __global__ __launch_bounds__(256) void norm_strip_kernel(NormGradArgs a)
             const float2 st = reinterpret_cast<const float2 *>(a.stats)[r];
             const f32x8 d = load8(a.dY, r * a.ldy + col, DT, valid);
             const f32x8 x = load8(a.X, r * a.ldx + col, DT, valid);
-            const f32x8 h = (x - st.x) * st.y;
+            const f32x8 h = Deviation(st).of(x);
             sw += d * h;
             sb += d;
             if (a.dX) {
@@ -382,9 +479,10 @@ __global__ __launch_bounds__(THREADS) void norm_grad_kernel(NormGradArgs a)
         if (r + step < a.n)
             fetch(r + step);
         float s = 0.0f, t = 0.0f;
+        const Deviation dev(st);
 #pragma unroll
         for (int h = 0; h < HOLD; ++h) {
-            const f32x8 dy = d[h].floats(), hx = (x[h].floats() - st.x) * st.y;
+            const f32x8 dy = d[h].floats(), hx = dev.of(x[h].floats());
             const f32x8 g = a.w ? dy * w[h].floats() : dy;
 #pragma unroll
             for (int j = 0; j < 8; ++j)
@@ -418,7 +516,7 @@ __global__ __launch_bounds__(THREADS) void norm_grad_kernel(NormGradArgs a)
             for (int h = 0; h < HOLD; ++h) {
                 if (!valid[h])
                     continue;
-                const f32x8 dy = d[h].floats(), hx = (x[h].floats() - st.x) * st.y;
+                const f32x8 dy = d[h].floats(), hx = dev.of(x[h].floats());
                 const f32x8 g = a.w ? dy * w[h].floats() : dy;
                 store8(a.dX, r * a.k + (at + h * LANES) * 8, (g - s - hx * t) * st.y, DT,
                        valid[h]);
@@ -537,10 +635,19 @@ struct Backward {
 template <int DT, int LANES, int HOLD>
 void launch_rows(const NormArgs &a, hipStream_t st)
 {
-    constexpr int kRows = 256 / LANES;
-    const int64_t blocks = (a.n + kRows - 1) / kRows;
-    norm_rows_kernel<DT, LANES, HOLD>
-        <<<(unsigned)(blocks < kNormBlocks ? blocks : kNormBlocks), 256, 0, st>>>(a);
+    constexpr int kSize = DT == GPIC_F32 ? 4 : 2;
+    // (64 rows a group of lanes at most)
+    constexpr int64_t kRows = 256 / LANES, kMost = kNormBlocks * kRows * 64;
+    for (int64_t first = 0; first < a.n; first += kMost) {
+        NormArgs p = a;
+        p.X = static_cast<const char *>(a.X) + first * a.ldx * kSize;
+        p.Y = static_cast<char *>(a.Y) + first * a.ldy * kSize;
+        p.stats = a.stats ? a.stats + first * 2 : nullptr;
+        p.n = a.n - first < kMost ? a.n - first : kMost;
+        const int64_t blocks = (p.n + kRows - 1) / kRows;
+        norm_rows_kernel<DT, LANES, HOLD>
+            <<<(unsigned)(blocks < kNormBlocks ? blocks : kNormBlocks), 256, 0, st>>>(p);
+    }
 }
 
 template <int DT>

@@ -144,3 +144,105 @@ def test_table_gradients_stay_in_their_workspace(g, monkeypatch, shape, dtype):
     exact = Exact(monkeypatch, g)
     assert torch.equal(g.gpic_embedding_backward(dY, ids, rows), want)
     exact.check()
+
+
+def _norm_rows(g, X, w, b, dY, dtype, what, far_mean, far_h, eps=1e-5):
+    """Y, statistics and gradients of rows near the ends of float32's range or far from
+    zero.  D as in test_gpu_training.  far_mean: what the mean in Y is off by, in mean
+    |x - m|'s place; far_h: the same in the gradients."""
+    n, k = X.shape
+    print(f"norm n={n} k={k} {dtype} {what}", flush=True)
+    Y, stats = g.gpic_layer_norm(X, w, b, eps, want_stats=True)
+    assert torch.equal(Y, g.gpic_layer_norm(X, w, b, eps))
+    inplace = X.clone()
+    assert torch.equal(Y, g.gpic_layer_norm(inplace, w, b, eps, Y=inplace))
+    x, dy, wd, bd = X.double(), dY.double(), w.double(), b.double()
+    mean = x.mean(1, keepdim=True)
+    # (float64 squares of 1e38 are fine)
+    r = 1.0 / ((x - mean).square().mean(1, keepdim=True) + eps).sqrt()
+    h = (x - mean) * r
+    D = (k / 16 + 32) * E
+    low = mean.abs() * r * E               # half a unit of the mean, in spreads
+    # the deviations' mean is off by (D + e) of the mean deviation, which is at most the
+    # spread and what they are counted from; r by D, squared terms included
+    hm = (D + E) * (1 + low) + (2 * low if far_mean else 0.0)
+    Dh = 2 * D * (1 + low.square())
+    _close(Y, h * wd + bd, (Dh * h.abs() + hm) * wd.abs() + 2 * E * bd.abs(), dtype, what + " Y")
+    assert bool(((stats[:, :1].double() - mean).abs() <= 2 * E * mean.abs() + (D + E) / r).all())
+    # (r may be a subnormal float32: its rounding)
+    sub = 2.0 ** -149 / r
+    assert bool(((stats[:, 1:].double() - r).abs() <= (Dh + sub) * r).all())
+
+    gr = g.gpic_layer_norm_backward(dY, X, w, stats)
+    hm = (D + E) * (1 + low) + (2 * low if far_h else 0.0)
+    Dh = Dh + sub
+    G = dy * wd
+    s1, s2 = G.mean(1, keepdim=True), (G * h).mean(1, keepdim=True)
+    a1, a2 = G.abs().mean(1, keepdim=True), (G * h).abs().mean(1, keepdim=True)
+    bound = r * (2 * Dh * (G.abs() + a1 + h.abs() * a2 * 2) + hm * a2 + (h.abs() + hm) * hm * a1)
+    _close(gr.dX, r * (G - s1 - h * s2), bound, dtype, what + " dX")
+    Dn = (n / 64 + 32) * E
+    _close(gr.dW, (dy * h).sum(0),
+           Dn * (dy * h).abs().sum(0) + (dy.abs() * (Dh * h.abs() + hm)).sum(0), dtype, what + " dW")
+    _close(gr.db, dy.sum(0), Dn * dy.abs().sum(0), dtype, what + " db")
+    for kw in (dict(want_x=False), dict(want_w=False), dict(want_bias=False)):
+        part = g.gpic_layer_norm_backward(dY, X, w, stats, **kw)
+        for name in ("dX", "dW", "db"):
+            if getattr(part, name) is not None:
+                assert torch.equal(getattr(part, name), getattr(gr, name))
+    return Y, stats
+
+
+WIDTHS = [8, 40, 100, 300, 1000, 2048, 4100, 9000, 33000]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("k", WIDTHS)
+def test_norm_of_large_rows(g, k, dtype):
+    """Finite rows whose sums or squares are no float32, up to the type's largest
+    value; such a row changes no other."""
+    most = torch.finfo(T[dtype]).max
+    base = _randn((40, k), "f32", 1).double()
+    for i in range(24):
+        base[i] *= 10.0 ** (15 + i)
+    base[24:28] = 1e36 * (1 + 0.05 * base[24:28])
+    base[28] = most * torch.where(torch.arange(k, device=DEV) % 2 == 0, 1.0, -1.0)
+    base[29, k // 2] = most
+    base[30] = 0.0
+    base[30, k - 1] = -most
+    base[31] = most
+    base[31, 3] = -most
+    X = base.clamp(-most, most).to(T[dtype])
+    assert bool(X.isfinite().all())
+    w, b = _randn((k,), dtype, 2), _randn((k,), dtype, 3)
+    dY = _randn((40, k), dtype, 4)
+    Y, _ = _norm_rows(g, X, w, b, dY, dtype, "large", True, True)
+    assert torch.equal(Y[32:], g.gpic_layer_norm(X[32:], w, b))
+    # rows of one large value are the bias
+    same = torch.tensor([1e19, 1e36, most, -most, most / 3], device=DEV)[:, None].expand(5, k)
+    same = same.to(T[dtype]).contiguous()
+    assert torch.equal(g.gpic_layer_norm(same, w, b), b.expand(5, k))
+    # what is not finite stays so
+    X[5, 1], X[7, k - 1] = float("inf"), float("nan")
+    Y, stats = g.gpic_layer_norm(X, w, b, want_stats=True)
+    assert bool(Y[[5, 7]].isnan().all() and stats[[5, 7]].isnan().all())
+    keep = [i for i in range(40) if i not in (5, 7)]
+    assert bool(Y[keep].isfinite().all())
+
+
+@pytest.mark.parametrize("shape", [(70000, 40), (300000, 12), (9000, 600), (68000, 2100)], ids=str)
+def test_norm_of_large_rows_among_many(g, shape):
+    """Rows in turn over a grid, some of them large, in several launches: each as alone."""
+    n, k = shape
+    X = _randn((n, k), "bf16", 1)
+    X[3::7] *= 1e25
+    X[n - 1] *= 1e30
+    w, b = _randn((k,), "bf16", 2), _randn((k,), "bf16", 3)
+    Y, stats = g.gpic_layer_norm(X, w, b, want_stats=True)
+    at = sorted({0, 3, 10, n // 2, n - 8, n - 1} | set(range(5, n, max(1, n // 40)))
+                | {min(n - 1, 65536 + d) for d in (-1, 0, 1)})
+    at = torch.tensor(at + [0] * (1100 - len(at)), device=DEV)       # (the same lanes a row)
+    ref, s = g.gpic_layer_norm(X[at], w, b, want_stats=True)
+    assert torch.equal(Y[at], ref) and torch.equal(stats[at], s)
+    assert bool(Y.isfinite().all() and stats.isfinite().all())
+    assert torch.equal(g.gpic_layer_norm(X, w, b, Y=X), Y)
