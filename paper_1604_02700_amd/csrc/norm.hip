@@ -90,24 +90,42 @@ struct Chunk {
     }
 };
 
-// A row's values count as x c, their mean is m and their reciprocal spread r.
+// A row's values count as x c, its deviations as (x c - m) - off, whose
+// reciprocal spread is r; the row's own mean, and the reciprocal of its spread.
 struct RowStats {
-    float c, m, r;
+    float c, m, off, r, mean, rs;
 };
 
-// RowStats from the sums of the deviations from m, which correct it, and of their
-// squares.  Whether a sum or square is no float32.
-__device__ __forceinline__ bool settle(RowStats &q, float s, float t, float inv, float eps)
+// (a product of its own: fused into some of the differences from it and not into
+// others, it would be two values)
+__device__ __forceinline__ float mean_of(float s, float inv)
 {
-    const float off = s * inv, var = fmaxf(t * inv - off * off, 0.0f);
-    q.m += off;
-    q.r = 1.0f / sqrtf((t != t ? t : var) + eps);
-    return !(t < INFINITY);
+#pragma clang fp contract(off)
+    return s * inv;
+}
+
+// RowStats from the sums of the deviations from m and of their squares.  The first
+// corrects m by `off`, which stays apart: a float32 mean holds little of it where
+// a row is far from zero.
+__device__ __forceinline__ void settle(RowStats &q, float s, float t, float inv, float eps)
+{
+    q.off = s * inv;
+    const float var = fmaxf(t * inv - q.off * q.off, 0.0f);
+    q.r = q.rs = 1.0f / sqrtf((t != t ? t : var) + eps);
+    q.mean = q.m + q.off;
+}
+
+// Whether that does not hold: a sum or square is no float32, or `off` is so large
+// beside the spread that its own rounding shows.
+__device__ __forceinline__ bool unsettled(const RowStats &q, float t, float inv)
+{
+    return !(t < INFINITY && fabsf(q.off) * q.r <= 0x1p-8f && 2.0f * q.off * q.off <= t * inv);
 }
 
 // Such rows once more, from memory (a function of its own, which takes none of the
 // kernel's registers).  Values beyond 1e19 or so are scaled by 2^-100, which leaves
-// everything that matters beside the largest.
+// everything that matters beside the largest.  Rows far from zero are counted again
+// from the corrected mean; rows of one value deviate by 0 then.
 template <int DT, int LANES>
 __device__ __noinline__ void norm_anew(const void *X, const void *w, const void *b, void *Y,
                                        float *stats, int64_t k, float eps, float2 *part)
@@ -117,13 +135,16 @@ __device__ __noinline__ void norm_anew(const void *X, const void *w, const void 
     const float inv = 1.0f / (float)k;
     RowStats q;
     q.c = 1.0f;
-    for (int turn = 0; turn < 2; ++turn) {
+    bool fresh = true, moved = false;
+    for (bool more = true; more;) {
         float s = 0.0f, t = 0.0f;
+        if (fresh) {
 #pragma unroll 8
-        for (int64_t c = at; c < k; c += LANES)
-            s += load1(X, c, DT) * q.c;
-        row_sums<LANES>(s, t, part);
-        q.m = s * inv;
+            for (int64_t c = at; c < k; c += LANES)
+                s += load1(X, c, DT) * q.c;
+            row_sums<LANES>(s, t, part);
+            q.m = mean_of(s, inv);
+        }
         s = t = 0.0f;
 #pragma unroll 8
         for (int64_t c = at; c < k; c += LANES) {
@@ -132,26 +153,29 @@ __device__ __noinline__ void norm_anew(const void *X, const void *w, const void 
             t += d * d;
         }
         row_sums<LANES>(s, t, part);
-        if (!settle(q, s, t, inv, eps * q.c * q.c) || turn == 1)
-            break;
-        q.c = 0x1p-100f;
+        settle(q, s, t, inv, eps * q.c * q.c);
+        more = unsettled(q, t, inv) && !moved;
+        fresh = q.c == 1.0f && !(t < INFINITY);
+        if (fresh)
+            q.c = 0x1p-100f;
+        moved = more && !fresh;
+        q.m = moved ? q.mean : q.m;
     }
-    float mean = q.m, rs = q.r;
     if (q.c != 1.0f) {
-        rs = q.r * q.c;
-        mean = q.m * 0x1p100f;
-        if (fabsf(mean) == INFINITY)         // of finite values: rounded so
-            mean = copysignf(kMost, mean);
+        q.rs = q.r * q.c;
+        q.mean = q.mean * 0x1p100f;
+        if (fabsf(q.mean) == INFINITY)       // of finite values: rounded so
+            q.mean = copysignf(kMost, q.mean);
         if (q.r == INFINITY && eps > 0.0f) { // (rows of one value: eps vanishes beside 2^200)
-            rs = 1.0f / sqrtf(eps);
+            q.rs = 1.0f / sqrtf(eps);
             q.r = kMost;
         }
     }
     if (stats && at == 0)
-        *reinterpret_cast<float2 *>(stats) = make_float2(mean, rs);
+        *reinterpret_cast<float2 *>(stats) = make_float2(q.mean, q.rs);
 #pragma unroll 4
     for (int64_t c = at; c < k; c += LANES) {
-        float y = (load1(X, c, DT) * q.c - q.m) * q.r;
+        float y = (load1(X, c, DT) * q.c - q.m - q.off) * q.r;
         if (w)
             y *= load1(w, c, DT);
         if (b)
@@ -224,7 +248,7 @@ __global__ __launch_bounds__(256) void norm_rows_kernel(NormArgs a)
         }
         row_sums<LANES>(s, t, part);
         RowStats q;
-        q.m = s * inv;
+        q.m = mean_of(s, inv);
         s = t = 0.0f;
 #pragma unroll
         for (int h = 0; h < HOLD; ++h) {
@@ -237,15 +261,17 @@ __global__ __launch_bounds__(256) void norm_rows_kernel(NormArgs a)
             }
         }
         row_sums<LANES>(s, t, part);
-        const bool open = settle(q, s, t, inv, a.eps);
+        settle(q, s, t, inv, a.eps);
+        const bool open = unsettled(q, t, inv);
         again |= open ? 1ull << turn : 0;
         if (a.stats && at == 0)
-            reinterpret_cast<float2 *>(a.stats)[r] = make_float2(q.m, q.r);
+            reinterpret_cast<float2 *>(a.stats)[r] = make_float2(q.mean, q.rs);
+        const float shift = -q.off * q.r;
 #pragma unroll
         for (int h = 0; h < HOLD; ++h) {
             if (!valid[h] || open)           // (Y may be X, which is read again)
                 continue;
-            f32x8 y = (x[h].floats() - q.m) * q.r;
+            f32x8 y = (x[h].floats() - q.m) * q.r + shift;
             if (a.w)
                 y = y * w[h].floats();
             if (a.b)
@@ -286,7 +312,7 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_kernel(NormArg
         }
         row_sums<LANES>(s, t, part);
         RowStats q;
-        q.m = s * inv;
+        q.m = mean_of(s, inv);
         s = t = 0.0f;
         auto deviate = [&](const f32x8 &u, int64_t g) {
 #pragma unroll
@@ -302,18 +328,20 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_kernel(NormArg
         for (int64_t g = at + kHold * LANES; g < groups; g += LANES)
             deviate(read8<DT>(a.X, r * a.ldx, g * 8, a.k), g);
         row_sums<LANES>(s, t, part);
-        if (settle(q, s, t, inv, a.eps)) {
+        settle(q, s, t, inv, a.eps);
+        if (unsettled(q, t, inv)) {
             norm_anew<DT, LANES>(a, r, part);
             continue;
         }
         if (a.stats && at == 0)
-            reinterpret_cast<float2 *>(a.stats)[r] = make_float2(q.m, q.r);
+            reinterpret_cast<float2 *>(a.stats)[r] = make_float2(q.mean, q.rs);
+        const float shift = -q.off * q.r;
         auto write = [&](const f32x8 &u, int64_t g) {
             const int64_t left = a.k - g * 8;
             if (left <= 0)
                 return;
             const int valid = left < 8 ? (int)left : 8;
-            f32x8 y = (u - q.m) * q.r;
+            f32x8 y = (u - q.m) * q.r + shift;
             if (a.w)
                 y = y * load8(a.w, g * 8, DT, valid);
             if (a.b)

@@ -246,3 +246,38 @@ def test_norm_of_large_rows_among_many(g, shape):
     assert torch.equal(Y[at], ref) and torch.equal(stats[at], s)
     assert bool(Y.isfinite().all() and stats.isfinite().all())
     assert torch.equal(g.gpic_layer_norm(X, w, b, Y=X), Y)
+
+
+@pytest.mark.parametrize("dtype", list(T))
+@pytest.mark.parametrize("k", WIDTHS)
+def test_norm_of_rows_far_from_zero(g, k, dtype):
+    """Rows 10 to 10^6 spreads from zero, or of one value but for one unit, keep their
+    digits: what Y is off by does not grow with the mean."""
+    n = 30
+    noise = _randn((n, k), "f32", 1)
+    far = torch.tensor([10.0 ** (1 + i % 6) * (-1) ** i for i in range(n)], device=DEV)[:, None]
+    X = (far * (1.0 if dtype == "f32" else 0.1) + noise).clamp(-60000, 60000)
+    if dtype == "f32":
+        X = (X.double() * 2.0 ** torch.arange(n, device=DEV)[:, None]).float()
+    X = X.to(T[dtype])
+    one = torch.tensor([3.0, 2001.0, -777.0, 60001.0], device=DEV).to(T[dtype])
+    X[:4] = one[:, None]
+    X[:4, k // 3] = (one.float() * (1 + 2.0 * U[dtype])).to(T[dtype])       # a unit away
+    w, b, dY = _randn((k,), dtype, 2), _randn((k,), dtype, 3), _randn((n, k), dtype, 4)
+    _norm_rows(g, X, w, b, dY, dtype, "far", False, True)
+    # rows of one value are the bias, and their spread is eps alone
+    same = torch.tensor([3.1, -2001.3, 59999.0, 1e-3, 12345.67], device=DEV)[:, None].expand(5, k)
+    same = same.to(T[dtype]).contiguous()
+    Y, stats = g.gpic_layer_norm(same, w, b, want_stats=True)
+    assert torch.equal(Y, b.expand(5, k)) and torch.equal(stats[:, 0], same[:, 0].float())
+    assert float((stats[:, 1].double() * 1e-5 ** 0.5 - 1).abs().max()) <= 8 * E
+
+
+@pytest.mark.parametrize("k", WIDTHS)
+def test_norm_of_float32_rows_a_million_spreads_away(g, k):
+    """The same for many rows in turn, in float32 as far as it resolves a spread."""
+    n = 3000 if k < 5000 else 100
+    X = _randn((n, k), "f32", 1) + torch.tensor([1e5, -1e6, 3e4, 0.0], device=DEV)[
+        torch.arange(n, device=DEV) % 4][:, None]
+    w, b, dY = _randn((k,), "f32", 2), _randn((k,), "f32", 3), _randn((n, k), "f32", 4)
+    _norm_rows(g, X, w, b, dY, "f32", "million", False, True)
