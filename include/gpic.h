@@ -612,8 +612,9 @@ size_t gpic_layer_norm_workspace_bytes(const gpic_norm_params *p);
 
 /* Gradients of the same: with g = dY w and h = (X - mean) r, dX [n x k] =
  * r (g - mean(g) - h mean(g h)), dW [k] = column sums of dY h, db [k] = column
- * sums of dY.  dX, dW and db are contiguous, any may be null (not wanted).  With
- * n = 0, dW and db are zeros.  ws: gpic_layer_norm_workspace_bytes(p). */
+ * sums of dY.  What the statistics' float32 mean is off by is found again: rows far
+ * from zero keep their digits.  dX, dW and db are contiguous, any may be null (not
+ * wanted).  With n = 0, dW and db are zeros.  ws: gpic_layer_norm_workspace_bytes(p). */
 gpic_status gpic_layer_norm_backward(const gpic_norm_params *p, const void *dY, const void *X,
                                      const void *weight, const float *stats, void *dX, void *dW,
                                      void *db, void *ws, size_t ws_bytes, void *stream);

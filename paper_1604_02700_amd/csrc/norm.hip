@@ -15,7 +15,7 @@ struct NormArgs {
     float eps;
 };
 
-// The sum over the LANES lanes that share a row, the same in all of them
+// The sums over the LANES lanes that share a row, the same in all of them
 // (LANES > 64: the whole workgroup; `part` is its scratch, LANES / 64 pairs).
 template <int LANES>
 __device__ __forceinline__ void row_sums(float &s, float &t, float2 *part)
@@ -76,6 +76,14 @@ struct Chunk {
                     q[0][j / 2] |= (uint32_t)reinterpret_cast<const uint16_t *>(at)[j]
                                    << (16 * (j & 1));
             }
+    }
+    // keeps the compiler from holding the floats it made of them (16,384 x 2,048 in
+    // bfloat16, gradients: 61 us and spilled, 41 so)
+    __device__ __forceinline__ void again()
+    {
+#pragma unroll
+        for (int j = 0; j < kQuads; ++j)
+            asm volatile("" : "+v"(q[j]));
     }
     __device__ __forceinline__ f32x8 floats() const
     {
@@ -356,8 +364,11 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_kernel(NormArg
     }
 }
 
-// h = (x - mean) r.  Rows of the largest values deviate by more than a float32
-// holds, and then r is next to nothing: both under a power of two.
+// h = (x - mean) r - mean of that: the statistics' mean is a float32, off by up to half
+// a unit, which is most of a spread where a row is far enough from zero.  What
+// is off is the mean of (x - mean) r, found along with the other two.  Rows of the
+// largest values deviate by more than a float32 holds, and then r is next to nothing:
+// both under a power of two.
 struct Deviation {
     float c, m, r;
     __device__ __forceinline__ explicit Deviation(float2 stats)
@@ -370,30 +381,39 @@ struct Deviation {
     __device__ __forceinline__ T of(T x) const { return (x * c - m) * r; }
 };
 
+// The sums over the first LANES lanes of a wave's groups
+template <int LANES>
+__device__ __forceinline__ void wave_sums(float &s, float &t, float &u)
+{
+#pragma unroll
+    for (int o = LANES / 2; o > 0; o >>= 1) {
+        s += __shfl_xor(s, o, 64);
+        t += __shfl_xor(t, o, 64);
+        u += __shfl_xor(u, o, 64);
+    }
+}
+
 struct NormGradArgs {
     const void *dY, *X, *w;
     const float *stats;
     void *dX;
-    float *dots;               // [n][2]: mean(g), mean(g h)
+    float *dots;               // [n][4]: mean(g), mean(g h), mean((x - mean) r)
     float *sums;               // [parts][2][k]: of dy h, of dy
     int64_t n, k, ldx, ldy;
     int64_t strips, each;
 };
 
-// mean(g) and mean(g h) of every row
-template <int DT, int LANES>
+// mean(g), mean(g h) and what the mean is off by, of every row
+template <int DT>
 __global__ __launch_bounds__(256) void norm_dots_kernel(NormGradArgs a)
 {
-    constexpr int kRows = 256 / LANES;
-    __shared__ float2 part[LANES > 64 ? LANES / 64 : 1];
-    const int at = threadIdx.x % LANES;
+    __shared__ float4 part[4];
     const int64_t groups = (a.k + 7) / 8;
     const float inv = 1.0f / (float)a.k;
-    for (int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES; r < a.n;
-         r += (int64_t)gridDim.x * kRows) {
-        const Deviation h(reinterpret_cast<const float2 *>(a.stats)[r]);
-        float s = 0.0f, t = 0.0f;
-        for (int64_t g = at; g < groups; g += LANES) {
+    for (int64_t r = blockIdx.x; r < a.n; r += gridDim.x) {
+        const Deviation dev(reinterpret_cast<const float2 *>(a.stats)[r]);
+        float s = 0.0f, t = 0.0f, u = 0.0f;
+        for (int64_t g = threadIdx.x; g < groups; g += 256) {
             const int valid = a.k - g * 8 < 8 ? (int)(a.k - g * 8) : 8;
             f32x8 d = load8(a.dY, r * a.ldy + g * 8, DT, valid);
             const f32x8 x = load8(a.X, r * a.ldx + g * 8, DT, valid);
@@ -402,13 +422,27 @@ __global__ __launch_bounds__(256) void norm_dots_kernel(NormGradArgs a)
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 if (j < valid) {
+                    const float h = dev.of(x[j]);
                     s += d[j];
-                    t += d[j] * h.of(x[j]);
+                    t += d[j] * h;
+                    u += h;
                 }
         }
-        row_sums<LANES>(s, t, part);
-        if (at == 0)
-            reinterpret_cast<float2 *>(a.dots)[r] = make_float2(s * inv, t * inv);
+        wave_sums<64>(s, t, u);
+        __syncthreads();                 // what was here before has been read
+        if ((threadIdx.x & 63) == 0)
+            part[threadIdx.x >> 6] = make_float4(s, t, u, 0.0f);
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            for (int i = 1; i < 4; ++i) {
+                s += part[i].x;
+                t += part[i].y;
+                u += part[i].z;
+            }
+            s *= inv;
+            u *= inv;
+            reinterpret_cast<float4 *>(a.dots)[r] = make_float4(s, t * inv - u * s, u, 0.0f);
+        }
     }
 }
 
@@ -431,13 +465,14 @@ __global__ __launch_bounds__(256) void norm_strip_kernel(NormGradArgs a)
             const float2 st = reinterpret_cast<const float2 *>(a.stats)[r];
             const f32x8 d = load8(a.dY, r * a.ldy + col, DT, valid);
             const f32x8 x = load8(a.X, r * a.ldx + col, DT, valid);
-            const f32x8 h = Deviation(st).of(x);
-            sw += d * h;
             sb += d;
-            if (a.dX) {
-                const float2 m = reinterpret_cast<const float2 *>(a.dots)[r];
+            if (!a.dots)                 // (db alone)
+                continue;
+            const float4 m = reinterpret_cast<const float4 *>(a.dots)[r];
+            const f32x8 h = Deviation(st).of(x) - m.z;
+            sw += d * h;
+            if (a.dX)
                 store8(a.dX, r * a.k + col, (d * w - m.x - h * m.y) * st.y, DT, valid);
-            }
         }
     if (!a.sums)
         return;
@@ -457,8 +492,8 @@ __global__ __launch_bounds__(256) void norm_strip_kernel(NormGradArgs a)
 // groups of eight columns each: the next row is on its way while one is
 // finished, and the columns' sums stay in registers until the rows are through,
 // then meet in LDS.  Groups of lanes take rows in turn over the whole grid.  Bound
-// by memory: 16,384 x 2,048 in bfloat16 40 us with the join (5.0 TB/s), 10,007 x
-// 1,000 in float32 27 (4.5); in two passes, rows' means and then strips of
+// by memory: 16,384 x 2,048 in bfloat16 41 us with the join (4.9 TB/s), 10,007 x
+// 1,000 in float32 26 (4.6); in two passes, rows' means and then strips of
 // columns, 63 and 40.
 template <int DT, int LANES, int HOLD, int THREADS>
 __global__ __launch_bounds__(THREADS) void norm_grad_kernel(NormGradArgs a)
@@ -466,7 +501,7 @@ __global__ __launch_bounds__(THREADS) void norm_grad_kernel(NormGradArgs a)
     constexpr int kRows = THREADS / LANES, kWaves = THREADS / 64;
     constexpr bool kWide = LANES > 64;
     // sums of rows across waves (two sets in turn), or of columns
-    __shared__ float2 part[kWide ? 2 : 1][kWide ? LANES / 64 : 1];
+    __shared__ float4 part[kWide ? 2 : 1][kWide ? LANES / 64 : 1];
     __shared__ f32x8 cols[kWide ? 1 : kWaves][kWide ? 1 : 64];
     const int at = threadIdx.x % LANES;
     const float inv = 1.0f / (float)a.k;
@@ -506,7 +541,7 @@ __global__ __launch_bounds__(THREADS) void norm_grad_kernel(NormGradArgs a)
         }
         if (r + step < a.n)
             fetch(r + step);
-        float s = 0.0f, t = 0.0f;
+        float s = 0.0f, t = 0.0f, u = 0.0f;
         const Deviation dev(st);
 #pragma unroll
         for (int h = 0; h < HOLD; ++h) {
@@ -517,34 +552,39 @@ __global__ __launch_bounds__(THREADS) void norm_grad_kernel(NormGradArgs a)
                 if (j < valid[h]) {
                     s += g[j];
                     t += g[j] * hx[j];
-                    sw[h][j] += dy[j] * hx[j];
+                    u += hx[j];
                     sb[h][j] += dy[j];
                 }
         }
-        if (a.dX) {
+        wave_sums<(kWide ? 64 : LANES)>(s, t, u);
+        if (kWide) {
+            if ((threadIdx.x & 63) == 0)
+                part[turn & (kWide ? 1 : 0)][threadIdx.x >> 6] = make_float4(s, t, u, 0.0f);
+            __syncthreads();
+            s = t = u = 0.0f;
 #pragma unroll
-            for (int o = (kWide ? 64 : LANES) / 2; o > 0; o >>= 1) {
-                s += __shfl_xor(s, o, 64);
-                t += __shfl_xor(t, o, 64);
+            for (int i = 0; i < (kWide ? LANES / 64 : 1); ++i) {
+                const float4 p = part[turn & (kWide ? 1 : 0)][i];
+                s += p.x;
+                t += p.y;
+                u += p.z;
             }
-            if (kWide) {
-                if ((threadIdx.x & 63) == 0)
-                    part[turn & (kWide ? 1 : 0)][threadIdx.x >> 6] = make_float2(s, t);
-                __syncthreads();
-                s = t = 0.0f;
+        }
+        s *= inv;
+        u *= inv;
+        t = t * inv - u * s;
 #pragma unroll
-                for (int i = 0; i < (kWide ? LANES / 64 : 1); ++i) {
-                    s += part[turn & (kWide ? 1 : 0)][i].x;
-                    t += part[turn & (kWide ? 1 : 0)][i].y;
-                }
-            }
-            s *= inv;
-            t *= inv;
+        for (int h = 0; HOLD > 2 && h < HOLD; ++h) {
+            x[h].again();
+            d[h].again();
+        }
 #pragma unroll
-            for (int h = 0; h < HOLD; ++h) {
-                if (!valid[h])
-                    continue;
-                const f32x8 dy = d[h].floats(), hx = dev.of(x[h].floats());
+        for (int h = 0; h < HOLD; ++h) {
+            if (!valid[h])
+                continue;
+            const f32x8 dy = d[h].floats(), hx = dev.of(x[h].floats()) - u;
+            sw[h] += dy * hx;
+            if (a.dX) {
                 const f32x8 g = a.w ? dy * w[h].floats() : dy;
                 store8(a.dX, r * a.k + (at + h * LANES) * 8, (g - s - hx * t) * st.y, DT,
                        valid[h]);
@@ -625,10 +665,12 @@ struct Cut {
         strips = (p.k + 511) / 512;
         lanes = hold = 0;
         each = 0;
+        // (float32 rows of 1,025 to 2,048 in a wave take more registers than it has: 16,384 x
+        // 2,048 128 us by 64 lanes, 76 by 256; in bfloat16 41 by 64)
         static const int kFit[][2] = {{4, 1},  {8, 1},  {16, 1},  {16, 2}, {64, 1},
-                                      {64, 2}, {64, 4}, {256, 2}, {256, 4}};
+                                      {64, 2}, {64, 4}, {256, 1}, {256, 2}, {256, 4}};
         for (auto &f : kFit)
-            if (p.k <= f[0] * f[1] * 8) {
+            if (p.k <= f[0] * f[1] * 8 && !(p.dtype == GPIC_F32 && f[0] == 64 && f[1] == 4)) {
                 lanes = f[0];
                 hold = f[1];
                 break;
@@ -655,7 +697,7 @@ struct Backward {
     Backward(const Norm &p, Cursor &c)
     {
         const Cut s(p);
-        dots = s.lanes ? nullptr : static_cast<float *>(c.take((size_t)p.n * 8));
+        dots = s.lanes ? nullptr : static_cast<float *>(c.take((size_t)p.n * 16));
         sums = static_cast<float *>(c.take((size_t)s.parts * 2 * p.k * 4));
     }
 };
@@ -730,7 +772,12 @@ hipError_t launch_gradients(const NormGradArgs &a, const Cut &cut, hipStream_t s
         norm_grad_kernel<DT, 64, 2, 512><<<blocks, 512, 0, st>>>(a);
         return hipGetLastError();
     case 64 * 8 + 4:
-        norm_grad_kernel<DT, 64, 4, 512><<<blocks, 512, 0, st>>>(a);
+        if constexpr (DT != GPIC_F32)
+            norm_grad_kernel<DT, 64, 4, 512><<<blocks, 512, 0, st>>>(a);
+        return hipGetLastError();
+    case 256 * 8 + 1:
+        if constexpr (DT == GPIC_F32)
+            norm_grad_kernel<DT, 256, 1, 256><<<blocks, 256, 0, st>>>(a);
         return hipGetLastError();
     case 256 * 8 + 2:
         norm_grad_kernel<DT, 256, 2, 256><<<blocks, 256, 0, st>>>(a);
@@ -739,8 +786,8 @@ hipError_t launch_gradients(const NormGradArgs &a, const Cut &cut, hipStream_t s
         norm_grad_kernel<DT, 256, 4, 256><<<blocks, 256, 0, st>>>(a);
         return hipGetLastError();
     }
-    if (a.dX) {
-        norm_dots_kernel<DT, 256><<<capped(a.n), 256, 0, st>>>(a);
+    if (a.dots) {
+        norm_dots_kernel<DT><<<capped(a.n), 256, 0, st>>>(a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess)
             return e;
@@ -777,7 +824,8 @@ hipError_t run_norm_backward(const Norm &p, const void *dY, const void *X, const
     const Backward b(p, c);
     const Cut s(p);
     if (p.n > 0 && (dX || dW || db)) {
-        const NormGradArgs a{dY, X, w, stats, dX, b.dots, dW || db ? b.sums : nullptr, p.n, p.k,
+        const NormGradArgs a{dY, X, w, stats, dX, dX || dW ? b.dots : nullptr,
+                             dW || db ? b.sums : nullptr, p.n, p.k,
                              p.ldx, p.ldy, s.strips, s.each};
         const hipError_t e = p.dtype == GPIC_F32    ? launch_gradients<GPIC_F32>(a, s, st)
                              : p.dtype == GPIC_F16 ? launch_gradients<GPIC_F16>(a, s, st)

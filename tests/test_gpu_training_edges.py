@@ -264,7 +264,7 @@ def test_norm_of_rows_far_from_zero(g, k, dtype):
     X[:4] = one[:, None]
     X[:4, k // 3] = (one.float() * (1 + 2.0 * U[dtype])).to(T[dtype])       # a unit away
     w, b, dY = _randn((k,), dtype, 2), _randn((k,), dtype, 3), _randn((n, k), dtype, 4)
-    _norm_rows(g, X, w, b, dY, dtype, "far", False, True)
+    _norm_rows(g, X, w, b, dY, dtype, "far", False, False)
     # rows of one value are the bias, and their spread is eps alone
     same = torch.tensor([3.1, -2001.3, 59999.0, 1e-3, 12345.67], device=DEV)[:, None].expand(5, k)
     same = same.to(T[dtype]).contiguous()
@@ -280,4 +280,4 @@ def test_norm_of_float32_rows_a_million_spreads_away(g, k):
     X = _randn((n, k), "f32", 1) + torch.tensor([1e5, -1e6, 3e4, 0.0], device=DEV)[
         torch.arange(n, device=DEV) % 4][:, None]
     w, b, dY = _randn((k,), "f32", 2), _randn((k,), "f32", 3), _randn((n, k), "f32", 4)
-    _norm_rows(g, X, w, b, dY, "f32", "million", False, True)
+    _norm_rows(g, X, w, b, dY, "f32", "million", False, False)
