@@ -681,8 +681,8 @@ typedef struct gpic_loss_params {
     int32_t reserved;    /* must be 0                                             */
 } gpic_loss_params;
 
-/* Workspace bytes of gpic_cross_entropy (backward 0) or its gradients (1); 0 also
- * for parameters that the call refuses. */
+/* Workspace bytes of gpic_cross_entropy (backward 0) or its gradients (1); 0 for
+ * n = 0, and for parameters that the call refuses. */
 size_t gpic_cross_entropy_workspace_bytes(int32_t backward, const gpic_loss_params *p);
 
 /* loss_i = lse_i - z_i,t(i) with the logits z = X W^T + bias and lse_i = log

@@ -752,6 +752,8 @@ hipError_t launch_columns(const Source *const *list, float *const *part, int cou
 size_t loss_ws(const Loss &p, bool backward)
 {
     Cursor c{nullptr};
+    if (p.n == 0)                        // (results of zeros at the most)
+        return 0;
     if (backward && small(p))
         Small m(p, c);
     else if (backward)

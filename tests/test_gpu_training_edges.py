@@ -117,6 +117,20 @@ def test_gradients_of_rows_with_small_shares(g, dtype, power, scale):
     _close(dW[far], (d.t() @ x)[far], ew[far], dtype, "dW")
 
 
+@pytest.mark.parametrize("dtype", list(T))
+def test_an_empty_batch_takes_no_workspace(g, monkeypatch, dtype):
+    def none(nbytes, device):
+        assert nbytes == 0
+        return None, 0
+
+    monkeypatch.setattr(g, "_workspace", none)
+    X, W, b, t = _inputs(8, 72, 900, dtype)
+    loss, lse = g.gpic_cross_entropy(X[:0], W, t[:0], b, want_lse=True)
+    gr = g.gpic_cross_entropy_backward(loss, X[:0], W, t[:0], loss, lse, b)
+    assert loss.shape == (0,) and gr.dX.shape == (0, 72)
+    assert not gr.dW.any() and not gr.db.any()
+
+
 # --------------------------------------------------------- norm and table
 @pytest.mark.parametrize("dtype", list(T))
 @pytest.mark.parametrize("shape", [(1, 1), (3, 7), (300, 64), (70, 2049), (1003, 300), (9, 33000),
