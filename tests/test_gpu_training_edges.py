@@ -6,6 +6,7 @@ Tolerances as derived in test_gpu_loss and test_gpu_training."""
 import pytest
 
 from test_gpu_loss import DEV, E, T, U, _check, _close, _inputs, _randn
+from test_gpu_training import _table_check
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
@@ -295,3 +296,26 @@ def test_norm_of_float32_rows_a_million_spreads_away(g, k):
         torch.arange(n, device=DEV) % 4][:, None]
     w, b, dY = _randn((k,), "f32", 2), _randn((k,), "f32", 3), _randn((n, k), "f32", 4)
     _norm_rows(g, X, w, b, dY, "f32", "million", False, False)
+
+
+# ------------------------------------------------------------------ table
+RUNS = [(15,), (16,), (17,), (1, 16, 17, 15, 33), (240, 1, 256, 257, 272, 273), (255, 241, 3)]
+
+
+@pytest.mark.parametrize("k", [3, 33, 520])
+@pytest.mark.parametrize("lengths", RUNS, ids=str)
+def test_table_runs_at_the_chunks_edges(g, lengths, k):
+    """Runs up to 16 positions, which a wave adds, and longer ones, which are cut at
+    multiples of 16, that start and end on, before and after them; up to 16 cuts, which a
+    wave joins, and 17 and more, which a workgroup does."""
+    n = 9000
+    ids, v = [], 0
+    while len(ids) < n:
+        for m in lengths:
+            ids += [v] * m
+            v += 2
+    ids = torch.tensor(ids[:n], device=DEV)
+    perm = torch.randperm(n, generator=torch.Generator().manual_seed(1)).to(DEV)
+    _table_check(g, n, k, v + 1, ids, "f32", 1.0, "in order")
+    _table_check(g, n, k, v + 1, ids[perm], "bf16", -0.5, "shuffled")
+    _table_check(g, n - 7, k, v + 1, (v - ids[7:]).int(), "f16", 2.0, "backwards")
