@@ -15,8 +15,9 @@
 //
 // What is rounded to the products' operands is D = exp(z - lse) - [target], at
 // most 1, without g: dX_i = g_i sum_v D_iv W_v, and dW_v = G sum_i D_iv (g_i / G x_i)
-// with the largest |g| G, so that the usual g, one for all rows, costs nothing.
-// float32 operands are split halves (encoder.h).
+// with the largest |g| G, so that the usual g, one for all rows, costs nothing;
+// float16's (g_i / G) x_i are under a power of two (share_max_kernel).  float32 operands
+// are split halves (encoder.h).
 #include <type_traits>
 
 #include "row_chunks.h"
@@ -53,8 +54,8 @@ struct FewArgs {
 // waves share the contraction in turns; wave w < NB CB ends (true) with rows
 // 16 (w mod NB) on and block w / NB, a lane with four columns, from `col` on, of
 // `row`.  Bound by reading W: one bfloat16 row, 4,096 -> 65,000, 109 us with the
-// join, 4.9 TB/s.  (Workgroups that stay and read a block ahead spilled at 16 waves,
-// 45 us for 38.)
+// join, 4.9 TB/s.  (Workgroups that stay and read a block ahead spilled at 16 waves:
+// 45 us where one row of 2,048 -> 32,000 took 38, which two blocks a workgroup now take 34 for.)
 template <int DT, int NB, int CB, int WAVES>
 __device__ __forceinline__ bool few_logits(const FewArgs &a, double (&v)[4], int64_t &row,
                                            int64_t &col)

@@ -131,7 +131,8 @@ __device__ __forceinline__ bool unsettled(const RowStats &q, float t, float inv)
 }
 
 // Such rows once more, from memory (a function of its own, which takes none of the
-// kernel's registers).  Values beyond 1e19 or so are scaled by 2^-100, which leaves
+// kernel's registers; 10,007 x 1,000 in float32, every row 1e5 spreads away 58 us for 16,
+// of 1e30 71).  Values beyond 1e19 or so are scaled by 2^-100, which leaves
 // everything that matters beside the largest.  Rows far from zero are counted again
 // from the corrected mean; rows of one value deviate by 0 then.
 template <int DT, int LANES>
@@ -204,10 +205,11 @@ __device__ __forceinline__ void norm_anew(const NormArgs &a, int64_t r, float2 *
 // Rows that LANES lanes hold in HOLD groups of eight columns each, with the next
 // row on its way while one is finished: the mean, then the deviations from it,
 // whose own sum corrects it, so that rows far from zero lose nothing.  Groups of
-// lanes take rows in turn over the whole grid.  Bound by memory: 16,384 x 2,048 in
-// bfloat16 24.5 us (5.5 TB/s), 31 with a row a wave and no next one on its way;
-// 10,007 x 1,000 in float32 17.1 (4.7); 1,024 workgroups, since 2,048 and more take
-// up to 30 % longer (16,384 x 2,048 in float32 45 us, 47, and 59 with 4,096).
+// lanes take rows in turn over the whole grid, up to 64 each; those that are not
+// settled come last (in their turn 26.5 us for 24.7).  Bound by memory: 16,384 x 2,048 in
+// bfloat16 24.7 us (5.4 TB/s), 31 with a row a wave and no next one on its way;
+// 10,007 x 1,000 in float32 16.0 (5.0); 1,024 workgroups, since 2,048 and more take
+// up to 30 % longer (16,384 x 2,048 in float32 46 us, 47, and 59 with 4,096).
 template <int DT, int LANES, int HOLD>
 __global__ __launch_bounds__(256) void norm_rows_kernel(NormArgs a)
 {
@@ -729,6 +731,9 @@ hipError_t launch_norm(const NormArgs &a, hipStream_t st)
         launch_rows<DT, 256, 4>(a, st);
     else if (a.k > 2048)
         launch_rows<DT, 256, 2>(a, st);
+    // Fewer rows than workgroups that stay: one each, in whose lanes more is under way.  us
+    // by waves and so: 32 x 2,048 in float32 4.7 and 3.0, 700 x 2,048 5.7 and 4.3, 256 x 1,000
+    // in bfloat16 3.6 and 3.2, 1,000 x 1,000 3.8 and 4.0; beyond, 2,000 x 700 4.9 and 6.7.
     else if (a.k > 512 && a.n < 1024)
         launch_rows<DT, 256, 1>(a, st);
     else if (a.k > 1024)
