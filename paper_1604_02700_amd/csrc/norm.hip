@@ -383,7 +383,7 @@ struct Deviation {
     __device__ __forceinline__ T of(T x) const { return (x * c - m) * r; }
 };
 
-// The sums over the first LANES lanes of a wave's groups
+// The sums over LANES lanes that share a row within a wave
 template <int LANES>
 __device__ __forceinline__ void wave_sums(float &s, float &t, float &u)
 {

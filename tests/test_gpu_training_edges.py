@@ -319,3 +319,37 @@ def test_table_runs_at_the_chunks_edges(g, lengths, k):
     _table_check(g, n, k, v + 1, ids, "f32", 1.0, "in order")
     _table_check(g, n, k, v + 1, ids[perm], "bf16", -0.5, "shuffled")
     _table_check(g, n - 7, k, v + 1, (v - ids[7:]).int(), "f16", 2.0, "backwards")
+
+
+@pytest.mark.parametrize("k", [24, 700, 9000])
+def test_norm_captured_once_and_replayed_over_other_rows(g, k):
+    """A captured pass over ordinary rows, replayed over large and far ones, and back;
+    a bias without weights."""
+    n = 300
+    X, b, dY = _randn((n, k), "f32", 1), _randn((k,), "f32", 2), _randn((n, k), "f32", 3)
+    ordinary = X.clone()
+    other = X * 1e25
+    other[::3] = X[::3] + 1e5
+    other[1::3] = 7.0
+
+    def both():
+        Y, stats = g.gpic_layer_norm(X, None, b, want_stats=True)
+        gr = g.gpic_layer_norm_backward(dY, X, None, stats)
+        return Y, stats, gr.dX, gr.dW, gr.db
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        both()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = both()
+    for rows in (ordinary, other, ordinary, other, other):
+        X.copy_(rows)
+        graph.replay()
+        want = both()
+        torch.cuda.synchronize()
+        for a, c in zip(got, want):
+            assert torch.equal(a, c) and bool(a.isfinite().all())
+    assert torch.equal(got[0][1::3], b.expand(100, k))
